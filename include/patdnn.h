@@ -15,8 +15,8 @@
  *
  * The three calls of the paper's problem statement are patdnn_encode, patdnn_conv and patdnn_free, with
  * patdnn_export / patdnn_decode / patdnn_strerror as inspection helpers.  Everything else declared here
- * (patdnn_conv_host, patdnn_conv_static, patdnn_check, patdnn_plan, patdnn_stack_*, patdnn_maxpool2x2, the launch
- * counter, patdnn_debug_wait, and the `variant` and `flags` fields of patdnn_desc) is an addition of this library
+ * (patdnn_conv_host, patdnn_conv_static, patdnn_check, patdnn_plan, patdnn_stack_*, patdnn_maxpool2x2, patdnn_norm_*,
+ * patdnn_mx4_*, patdnn_linear_*, the launch counter, patdnn_debug_wait, and the `variant` and `flags` fields of patdnn_desc) is an addition of this library
  * with no counterpart in the paper; each says so where it is declared.
  *
  * Conventions used by every call
@@ -62,7 +62,9 @@ enum {
     PATDNN_E_SCRATCH = 12       /* the layer needs more scratch than the fixed device buffer of patdnn_conv_static */
 };
 
-enum { PATDNN_F32 = 0, PATDNN_F16 = 1 };   /* storage type of weights and activations; accumulation is fp32 */
+enum { PATDNN_F32 = 0, PATDNN_F16 = 1,      /* storage type of weights and activations; accumulation is fp32 */
+       PATDNN_BF16 = 2 };                    /* bfloat16: group norm, 4-bit quantisation and linear layers only */
+enum { PATDNN_ACT_NONE = 0, PATDNN_ACT_RELU = 1, PATDNN_ACT_SILU = 2 };   /* activations of those: max(0, z); z / (1 + exp(-z)) */
 
 /* Kernel variants (an addition: the paper generates one code version per layer and tunes it offline).
  * AUTO compares, at encode time, an estimate of the tensor-core variant's time (the zero-padded dense work of nine
@@ -276,6 +278,89 @@ PATDNN_API int patdnn_stack_free(patdnn_stack s);
  * Not part of the paper's method; provided so that the VGG-shaped stack runs without any other library. */
 PATDNN_API int patdnn_maxpool2x2(const void *in, void *out, int32_t N, int32_t C, int32_t H, int32_t W, int32_t dtype,
                       void *stream);
+
+/*
+ * Group norm with an activation, channels last, and its gradient (addition; a batch norm is folded into a convolution's weights,
+ * a group norm depends on the input and cannot be).  For x[n][p][c], p one of P pixels, group g = c / (C / G):
+ *   mean, var over the P * C/G values of (n, g), rstd = 1 / sqrt(var + eps), xh = (x - mean) * rstd,
+ *   y = act(xh * gamma[c] + beta[c])
+ * All sums are fp32 and taken in a fixed order (the same call gives the same bits); y and dx are rounded once.  NaN and infinities
+ * reach exactly the (image, group)s that hold them.
+ *   desc       copied; a pixel's C channels are consecutive; pixels and images may be further apart than they are long:
+ *              strides in elements, 0 = dense.  y strides also hold for dy, x strides for dx.
+ *   E_SHAPE    N < 0, P < 1, C < 1, G < 1, C not a multiple of G, |strides| that overlap pixels (x_pixel < C, x_image < P * x_pixel ...),
+ *              eps negative or not finite; N <= 65535, C <= 2^20, P < 2^31, N * P * C < 2^40
+ *   E_DTYPE    dtype or act unknown
+ * A handle owns its workspace: calls that can overlap on the GPU need a handle each.  N = 0 launches nothing (the gradient
+ * writes zeros to dgamma and dbeta).
+ */
+typedef struct patdnn_norm_s *patdnn_norm;
+typedef struct {
+    int32_t N, C, G;            /* images, channels, groups */
+    int64_t P;                  /* pixels per image (H * W) */
+    int64_t x_pixel, x_image;   /* element strides of x and dx; 0 = dense */
+    int64_t y_pixel, y_image;   /* element strides of y and dy; 0 = dense */
+    float eps;
+    int32_t act;                /* PATDNN_ACT_* */
+    int32_t dtype;              /* of x, y, dy, dx: PATDNN_F32, _F16 or _BF16; gamma, beta and statistics are float */
+} patdnn_norm_desc;
+
+PATDNN_API int patdnn_norm_create(const patdnn_norm_desc *desc, patdnn_norm *out);
+/* y DEVICE; stats DEVICE float [N][G][2] (mean, rstd), or NULL; gamma, beta DEVICE float [C].  y must not overlap x.  Asynchronous. */
+PATDNN_API int patdnn_norm_run(patdnn_norm h, const void *x, const float *gamma, const float *beta, void *y, float *stats, void *stream);
+/* The same, written as a 4-bit matrix of N * P rows and C columns (see below) that patdnn_linear_run_mx4 reads. */
+PATDNN_API int patdnn_norm_run_mx4(patdnn_norm h, const void *x, const float *gamma, const float *beta, void *mx, float *stats,
+                                   void *stream);
+/* stats as patdnn_norm_run wrote them; dx DEVICE (x strides), dgamma, dbeta DEVICE float [C], all overwritten.  At z = 0 ReLU
+ * passes no gradient. */
+PATDNN_API int patdnn_norm_grad(patdnn_norm h, const void *x, const float *gamma, const float *beta, const float *stats, const void *dy,
+                                void *dx, float *dgamma, float *dbeta, void *stream);
+PATDNN_API int patdnn_norm_free(patdnn_norm h);
+
+/*
+ * Microscaled 4-bit matrices (addition).  A block is 32 consecutive columns of a row, the last one of a row may be shorter; its scale
+ * is 2^max(floor(log2(amax)) - 2, -127), held in 8 bits; an element is x / scale rounded to the nearest of 0, 0.5, 1, 1.5, 2,
+ * 3, 4, 6 (ties to the even code), sign kept, larger magnitudes become 6.  A block with an infinity or a NaN becomes 32 NaNs.
+ * The layout of the buffer is the library's own (tiles in the order in which the tensor cores read them); patdnn_mx4_dequantize
+ * gives the values.  Padding in it is not initialised and never reaches a result.
+ *   patdnn_mx4_bytes       size of the buffer for rows x cols, which depends on these alone; 16-byte aligned buffers are needed
+ *   patdnn_mx4_quantize    x DEVICE [rows][ld] of dtype -> mx DEVICE
+ *   patdnn_mx4_dequantize  mx DEVICE -> out DEVICE [rows][ld] of dtype (every value is exact in float and bfloat16; in half
+ *                          where the quantised matrix was half)
+ * Errors: E_NULL, E_SHAPE (rows < 0, cols < 1, ld < cols, cols > 2^20, rows * cols > 2^40, buffer not aligned), E_DTYPE, E_CUDA.
+ * rows = 0 launches nothing.  Asynchronous.
+ */
+PATDNN_API int patdnn_mx4_bytes(int64_t rows, int64_t cols, int64_t *bytes);
+PATDNN_API int patdnn_mx4_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, void *mx, void *stream);
+PATDNN_API int patdnn_mx4_dequantize(const void *mx, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, void *out, void *stream);
+
+/*
+ * Linear layers with 4-bit weights (addition): y[m][f] = act(bias[f] + sum_k q(x)[m][k] * q(w)[f][k]), q as above, products exact,
+ * sums fp32 on the block-scaled tensor cores, y rounded once.  A 1x1 convolution over channels-last pixels is this layer on
+ * N * P rows.  A row of x that holds a NaN or an infinity gives a row of NaNs, no other row.
+ *   patdnn_linear_encode   weights DEVICE [F][K] of desc->dtype, rows ldw apart (0 = K); bias DEVICE float [F] or NULL.  Quantises
+ *                          the weights once and copies the bias, on `stream`; returns after that is done.
+ *   patdnn_linear_run      x DEVICE [rows][ldx], y DEVICE [rows][ldy] of desc->dtype (ld 0 = dense); rows <= max_rows: quantises x into
+ *                          the handle's buffer, then multiplies.  Asynchronous; calls that can overlap need a handle each.
+ *   patdnn_linear_run_mx4  the same for rows that are 4-bit already (patdnn_mx4_quantize, patdnn_norm_run_mx4); any number of rows
+ *   patdnn_linear_check    waits for the device; E_DEVICE_TIMEOUT if a bounded device-side wait of this handle expired
+ * Errors: E_NULL, E_SHAPE (F, K < 1 or > 2^20, rows < 0 or > max_rows, a stride below its row's length), E_DTYPE, E_ALLOC, E_CUDA.
+ * rows = 0 launches nothing.
+ */
+typedef struct patdnn_linear_s *patdnn_linear;
+typedef struct {
+    int32_t F, K;               /* outputs, inputs */
+    int64_t max_rows;           /* rows that patdnn_linear_run may be given */
+    const float *bias;          /* DEVICE [F], or NULL for zeros */
+    int32_t act;                /* PATDNN_ACT_* */
+    int32_t dtype;              /* of weights, x and y: PATDNN_F32, _F16 or _BF16 */
+} patdnn_linear_desc;
+
+PATDNN_API int patdnn_linear_encode(const void *weights, int64_t ldw, const patdnn_linear_desc *desc, void *stream, patdnn_linear *out);
+PATDNN_API int patdnn_linear_run(patdnn_linear h, const void *x, int64_t rows, int64_t ldx, void *y, int64_t ldy, void *stream);
+PATDNN_API int patdnn_linear_run_mx4(patdnn_linear h, const void *mx, int64_t rows, void *y, int64_t ldy, void *stream);
+PATDNN_API int patdnn_linear_check(patdnn_linear h);
+PATDNN_API int patdnn_linear_free(patdnn_linear h);
 
 /* Number of this library's kernels launched by the process since the last reset (addition, for reports). */
 PATDNN_API int64_t patdnn_launch_count(void);

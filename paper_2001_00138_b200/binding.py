@@ -16,7 +16,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libpatdnn.so")
 
 OK = 0
-F32, F16 = 0, 1
+F32, F16, BF16 = 0, 1, 2                  # BF16: group norm, 4-bit matrices and linear layers only
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 VARIANT_AUTO, VARIANT_NOOPT, VARIANT_REORDER, VARIANT_TILED, VARIANT_DENSE_TC, VARIANT_PATTERN_RUN = 0, 1, 2, 3, 4, 5
 FLAG_HOST_ONLY = 1
 STATUS_NAMES = {0: "OK", 1: "E_NULL", 2: "E_SHAPE", 3: "E_PATTERN_SET", 4: "E_MASK", 5: "E_ORDER", 6: "E_CUDA",
@@ -27,6 +28,9 @@ EXPORTED_SYMBOLS = (
     "patdnn_plan", "patdnn_stack_create", "patdnn_stack_run", "patdnn_stack_run_host", "patdnn_stack_out_shape",
     "patdnn_stack_free", "patdnn_stack_submit_host", "patdnn_stack_wait_host", "patdnn_maxpool2x2", "patdnn_launch_count", "patdnn_reset_launch_count", "patdnn_strerror",
     "patdnn_last_cuda_error", "patdnn_version", "patdnn_debug_wait", "patdnn_stack_run_timed", "patdnn_stack_generated",
+    "patdnn_norm_create", "patdnn_norm_run", "patdnn_norm_run_mx4", "patdnn_norm_grad", "patdnn_norm_free",
+    "patdnn_mx4_bytes", "patdnn_mx4_quantize", "patdnn_mx4_dequantize",
+    "patdnn_linear_encode", "patdnn_linear_run", "patdnn_linear_run_mx4", "patdnn_linear_check", "patdnn_linear_free",
 )
 
 
@@ -57,6 +61,17 @@ class _PlanInfo(ctypes.Structure):
                 ("grid_x", ctypes.c_int32), ("grid_y", ctypes.c_int32), ("grid_z", ctypes.c_int32),
                 ("smem_bytes", ctypes.c_int32), ("device_bytes", ctypes.c_int64), ("entries", ctypes.c_int64),
                 ("generated", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class _NormDesc(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("C", ctypes.c_int32), ("G", ctypes.c_int32), ("P", ctypes.c_int64),
+                ("x_pixel", ctypes.c_int64), ("x_image", ctypes.c_int64), ("y_pixel", ctypes.c_int64),
+                ("y_image", ctypes.c_int64), ("eps", ctypes.c_float), ("act", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class _LinearDesc(ctypes.Structure):
+    _fields_ = [("F", ctypes.c_int32), ("K", ctypes.c_int32), ("max_rows", ctypes.c_int64), ("bias", ctypes.c_void_p),
+                ("act", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 _lib = None
@@ -93,6 +108,20 @@ def load() -> ctypes.CDLL:
     lib.patdnn_stack_generated.argtypes = [vp, ctypes.POINTER(i32)]
     lib.patdnn_stack_free.argtypes = [vp]
     lib.patdnn_maxpool2x2.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp]
+    i64 = ctypes.c_int64
+    lib.patdnn_norm_create.argtypes = [ctypes.POINTER(_NormDesc), ctypes.POINTER(vp)]
+    lib.patdnn_norm_run.argtypes = [vp] * 7
+    lib.patdnn_norm_run_mx4.argtypes = [vp] * 7
+    lib.patdnn_norm_grad.argtypes = [vp] * 10
+    lib.patdnn_norm_free.argtypes = [vp]
+    lib.patdnn_mx4_bytes.argtypes = [i64, i64, ctypes.POINTER(i64)]
+    lib.patdnn_mx4_quantize.argtypes = [vp, i32, i64, i64, i64, vp, vp]
+    lib.patdnn_mx4_dequantize.argtypes = [vp, i32, i64, i64, i64, vp, vp]
+    lib.patdnn_linear_encode.argtypes = [vp, i64, ctypes.POINTER(_LinearDesc), vp, ctypes.POINTER(vp)]
+    lib.patdnn_linear_run.argtypes = [vp, vp, i64, i64, vp, i64, vp]
+    lib.patdnn_linear_run_mx4.argtypes = [vp, vp, i64, vp, i64, vp]
+    lib.patdnn_linear_check.argtypes = [vp]
+    lib.patdnn_linear_free.argtypes = [vp]
     lib.patdnn_launch_count.restype = ctypes.c_int64
     lib.patdnn_reset_launch_count.restype = None
     for name in ("patdnn_strerror", "patdnn_last_cuda_error", "patdnn_version"):
@@ -280,6 +309,105 @@ class Stack:
     def free(self) -> None:
         if self._h:
             load().patdnn_stack_free(self._h)
+            self._h = 0
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def _opt(x) -> int:
+    return 0 if x is None else _ptr(x)
+
+
+class GroupNorm:
+    """Group norm with an activation over channels-last images [N][P][C], P pixels each (``patdnn_norm``).
+
+    ``x_pixel``, ``x_image`` are the element strides of x and dx, ``y_pixel``, ``y_image`` those of y and dy (0 = dense).
+    The handle owns its workspace: calls that can overlap on the GPU need a handle each."""
+
+    def __init__(self, N: int, P: int, C: int, groups: int, *, dtype: int = F32, act: int = ACT_NONE, eps: float = 1e-5,
+                 x_pixel: int = 0, x_image: int = 0, y_pixel: int = 0, y_image: int = 0):
+        d = _NormDesc(N=N, C=C, G=groups, P=P, x_pixel=x_pixel, x_image=x_image, y_pixel=y_pixel, y_image=y_image, eps=eps,
+                      act=act, dtype=dtype)
+        h = ctypes.c_void_p()
+        self._h = 0
+        _check(load().patdnn_norm_create(ctypes.byref(d), ctypes.byref(h)), "patdnn_norm_create")
+        self._h = h.value
+
+    def run(self, x, gamma, beta, y, stats=None, stream: int = 0) -> None:
+        """patdnn_norm_run: y = act(norm(x) * gamma + beta); ``stats`` receives (mean, rstd) [N][G][2]; asynchronous."""
+        _check(load().patdnn_norm_run(self._h, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _opt(stats), stream), "patdnn_norm_run")
+
+    def run_mx4(self, x, gamma, beta, mx, stats=None, stream: int = 0) -> None:
+        """patdnn_norm_run_mx4: the same, as a 4-bit matrix of N * P rows and C columns (``mx4_bytes(N * P, C)``)."""
+        _check(load().patdnn_norm_run_mx4(self._h, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(mx), _opt(stats), stream),
+               "patdnn_norm_run_mx4")
+
+    def grad(self, x, gamma, beta, stats, dy, dx, dgamma, dbeta, stream: int = 0) -> None:
+        """patdnn_norm_grad: gradients of ``run`` with its statistics; overwrites dx, dgamma, dbeta."""
+        _check(load().patdnn_norm_grad(self._h, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(stats), _ptr(dy), _ptr(dx), _ptr(dgamma),
+                                       _ptr(dbeta), stream), "patdnn_norm_grad")
+
+    def free(self) -> None:
+        if self._h:
+            load().patdnn_norm_free(self._h)
+            self._h = 0
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def mx4_bytes(rows: int, cols: int) -> int:
+    """Size of the buffer of a 4-bit matrix."""
+    v = ctypes.c_int64()
+    _check(load().patdnn_mx4_bytes(rows, cols, ctypes.byref(v)), "patdnn_mx4_bytes")
+    return int(v.value)
+
+
+def mx4_quantize(x, mx, rows: int, cols: int, *, dtype: int = F32, ld: int = 0, stream: int = 0) -> None:
+    """patdnn_mx4_quantize: rows of x (``ld`` elements apart, 0 = dense) -> 4-bit matrix."""
+    _check(load().patdnn_mx4_quantize(_ptr(x), dtype, rows, cols, ld, _ptr(mx), stream), "patdnn_mx4_quantize")
+
+
+def mx4_dequantize(mx, out, rows: int, cols: int, *, dtype: int = F32, ld: int = 0, stream: int = 0) -> None:
+    """patdnn_mx4_dequantize: the values that a 4-bit matrix stands for."""
+    _check(load().patdnn_mx4_dequantize(_ptr(mx), dtype, rows, cols, ld, _ptr(out), stream), "patdnn_mx4_dequantize")
+
+
+class Linear:
+    """A linear layer with 4-bit weights (``patdnn_linear``): y = act(q(x) q(weights)^T + bias).
+
+    ``weights`` DEVICE [F][K] of ``dtype`` (rows ``ldw`` apart), ``bias`` DEVICE float [F]; both are read during the call only."""
+
+    def __init__(self, weights, F: int, K: int, *, max_rows: int, dtype: int = F32, bias=None, act: int = ACT_NONE, ldw: int = 0,
+                 stream: int = 0):
+        d = _LinearDesc(F=F, K=K, max_rows=max_rows, bias=_opt(bias), act=act, dtype=dtype)
+        h = ctypes.c_void_p()
+        self._h = 0
+        _check(load().patdnn_linear_encode(_ptr(weights), ldw, ctypes.byref(d), stream, ctypes.byref(h)), "patdnn_linear_encode")
+        self._h = h.value
+
+    def run(self, x, y, rows: int, *, ldx: int = 0, ldy: int = 0, stream: int = 0) -> None:
+        """patdnn_linear_run: quantises the rows of x, then multiplies; asynchronous."""
+        _check(load().patdnn_linear_run(self._h, _ptr(x), rows, ldx, _ptr(y), ldy, stream), "patdnn_linear_run")
+
+    def run_mx4(self, mx, y, rows: int, *, ldy: int = 0, stream: int = 0) -> None:
+        """patdnn_linear_run_mx4: rows that are 4-bit already."""
+        _check(load().patdnn_linear_run_mx4(self._h, _ptr(mx), rows, _ptr(y), ldy, stream), "patdnn_linear_run_mx4")
+
+    def check(self) -> None:
+        """patdnn_linear_check: synchronise and raise if a device-side bounded wait expired."""
+        _check(load().patdnn_linear_check(self._h), "patdnn_linear_check")
+
+    def free(self) -> None:
+        if self._h:
+            load().patdnn_linear_free(self._h)
             self._h = 0
 
     def __del__(self):

@@ -16,6 +16,7 @@
 #include "../../include/patdnn.h"
 #include "fkw_encoder.hpp"
 #include "kernels.hpp"
+#include "ops.hpp"
 
 using namespace patdnn;
 
@@ -25,11 +26,20 @@ thread_local std::string g_cuda_error;
 std::atomic<int64_t> g_launches{0};
 std::mutex g_static_mutex;                    // serialises the host-side set-up of patdnn_conv_static
 
-int cuda_fail(cudaError_t e, const char *what) {
-    g_cuda_error = std::string(what) + ": " + cudaGetErrorString(e);
+}  // namespace
+
+int patdnn::cuda_fail(cudaError_t e, const char *what) {
+    try {
+        g_cuda_error = std::string(what) + ": " + cudaGetErrorString(e);
+    } catch (...) {                           // no memory for the text: the status still says it
+    }
     cudaGetLastError();                       // clear the sticky-free error state
     return PATDNN_E_CUDA;
 }
+void patdnn::count_launches(int n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
+
+namespace {
+
 #define CU(call)                                             \
     do {                                                     \
         cudaError_t e_ = (call);                             \

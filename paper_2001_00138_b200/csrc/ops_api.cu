@@ -1,0 +1,268 @@
+// C entry points of the group norm, the 4-bit matrices and the 4-bit linear layer (declared in include/patdnn.h).
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <new>
+
+#include "../../include/patdnn.h"
+#include "ops.hpp"
+
+using namespace patdnn;
+
+#define CU(call)                                             \
+    do {                                                     \
+        cudaError_t e_ = (call);                             \
+        if (e_ != cudaSuccess) return cuda_fail(e_, #call);  \
+    } while (0)
+
+struct patdnn_norm_s {
+    NormHandle h;
+    int device = -1;
+    ~patdnn_norm_s() {
+        cudaFree(h.ws);
+        cudaFree(h.counters);
+        cudaFree(h.stats);
+    }
+};
+
+struct patdnn_linear_s {
+    patdnn_linear_desc d{};
+    Mx4Shape shape{};                       // of the weights
+    uint8_t *w = nullptr, *x = nullptr;     // 4-bit weights; buffer for the rows of patdnn_linear_run
+    float *bias = nullptr;
+    int *status = nullptr;
+    ~patdnn_linear_s() {
+        cudaFree(w);
+        cudaFree(x);
+        cudaFree(bias);
+        cudaFree(status);
+    }
+};
+
+namespace {
+
+constexpr int64_t kMostColumns = int64_t(1) << 20;
+constexpr int64_t kMostElements = int64_t(1) << 40;
+
+bool known_type(int dtype) { return dtype == PATDNN_F32 || dtype == PATDNN_F16 || dtype == PATDNN_BF16; }
+bool known_act(int act) { return act == PATDNN_ACT_NONE || act == PATDNN_ACT_RELU || act == PATDNN_ACT_SILU; }
+bool mx_size_ok(int64_t rows, int64_t cols) {
+    return rows >= 0 && cols >= 1 && cols <= kMostColumns && rows <= kMostElements / cols && rows <= INT32_MAX;
+}
+bool aligned(const void *p, unsigned bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+int launched(cudaError_t e, int n, const char *what) {
+    if (e != cudaSuccess) return cuda_fail(e, what);
+    count_launches(n);
+    return PATDNN_OK;
+}
+
+template <typename T> cudaError_t allocate(T **p, size_t count) {
+    void *v = nullptr;
+    const cudaError_t e = cudaMalloc(&v, count * sizeof(T) < 16 ? 16 : count * sizeof(T));
+    *p = static_cast<T *>(v);
+    return e;
+}
+
+int product(patdnn_linear h, const Mx4Shape &xs, const void *mx, int64_t rows, void *y, int64_t ldy, cudaStream_t st) {
+    if (ceil_div(rows, 128) * ceil_div(h->d.F, 128) > INT32_MAX / 8) return PATDNN_E_SHAPE;   // CTAs of one launch
+    Mx4Params p{};
+    p.w = h->w; p.x = static_cast<const uint8_t *>(mx); p.bias = h->bias; p.y = y; p.status = h->status;
+    p.ldy = ldy; p.rows = rows; p.w_scales = h->shape.scales_at; p.x_scales = xs.scales_at;
+    p.F = h->d.F; p.width = h->shape.width; p.col_tiles = static_cast<int>(h->shape.col_tiles);
+    p.ksteps = static_cast<int>(ceil_div(h->d.K, 64));
+    p.act = h->d.act; p.dtype = h->d.dtype;
+    int n = 0;
+    const cudaError_t e = launch_mx4_linear(p, st, &n);
+    return launched(e, n, "4-bit product launch");
+}
+
+}  // namespace
+
+extern "C" {
+
+int patdnn_norm_create(const patdnn_norm_desc *desc, patdnn_norm *out) {
+    if (!desc || !out) return PATDNN_E_NULL;
+    if (!known_type(desc->dtype) || !known_act(desc->act)) return PATDNN_E_DTYPE;
+    if (desc->N < 0 || desc->N > 65535 || desc->P < 1 || desc->P > INT32_MAX || desc->C < 1 || desc->C > kMostColumns || desc->G < 1 ||
+        desc->C % desc->G || !std::isfinite(desc->eps) || desc->eps < 0.f)
+        return PATDNN_E_SHAPE;
+    if (desc->P > kMostElements / desc->C || (desc->N && desc->P * desc->C > kMostElements / desc->N)) return PATDNN_E_SHAPE;
+    NormShape s{};
+    s.N = desc->N; s.C = desc->C; s.G = desc->G; s.act = desc->act; s.dtype = desc->dtype; s.P = desc->P; s.eps = desc->eps;
+    for (int i = 0; i < 2; ++i) {
+        int64_t pixel = i ? desc->y_pixel : desc->x_pixel, image = i ? desc->y_image : desc->x_image;
+        if (pixel == 0) pixel = s.C;
+        if (pixel < s.C || pixel > kMostElements / s.P) return PATDNN_E_SHAPE;
+        if (image == 0) image = s.P * pixel;
+        if (image < (s.P - 1) * pixel + s.C || (s.N && image > (int64_t(1) << 60) / s.N)) return PATDNN_E_SHAPE;
+        (i ? s.y_pixel : s.x_pixel) = pixel;
+        (i ? s.y_image : s.x_image) = image;
+    }
+    patdnn_norm h = new (std::nothrow) patdnn_norm_s();
+    if (!h) return PATDNN_E_ALLOC;
+    h->h.s = s;
+    if (s.N > 0) {
+        plan_norm(h->h);
+        cudaError_t e = allocate(&h->h.ws, norm_workspace_floats(h->h));
+        if (e == cudaSuccess) e = allocate(&h->h.counters, static_cast<size_t>(s.G));
+        if (e == cudaSuccess) e = cudaMemset(h->h.counters, 0, sizeof(unsigned) * s.G);
+        if (e == cudaSuccess) e = allocate(&h->h.stats, static_cast<size_t>(s.N) * s.G * 2);
+        if (e == cudaSuccess) e = prepare_norm();
+        if (e == cudaSuccess) e = cudaDeviceSynchronize();              // the counters are zero on every stream from here on
+        if (e != cudaSuccess) {
+            const int rc = cuda_fail(e, "patdnn_norm_create");
+            delete h;
+            return rc;
+        }
+    }
+    *out = h;
+    return PATDNN_OK;
+}
+
+int patdnn_norm_run(patdnn_norm h, const void *x, const float *gamma, const float *beta, void *y, float *stats, void *stream) {
+    if (!h) return PATDNN_E_NULL;
+    if (h->h.s.N == 0) return PATDNN_OK;
+    if (!x || !gamma || !beta || !y) return PATDNN_E_NULL;
+    int n = 0;
+    const cudaError_t e = launch_group_norm(h->h, x, gamma, beta, y, stats, static_cast<cudaStream_t>(stream), &n);
+    return launched(e, n, "group norm launch");
+}
+
+int patdnn_norm_run_mx4(patdnn_norm h, const void *x, const float *gamma, const float *beta, void *mx, float *stats, void *stream) {
+    if (!h) return PATDNN_E_NULL;
+    const NormShape &s = h->h.s;
+    if (s.N == 0) return PATDNN_OK;
+    if (!x || !gamma || !beta || !mx) return PATDNN_E_NULL;
+    if (!aligned(mx, 16) || !mx_size_ok(s.N * s.P, s.C)) return PATDNN_E_SHAPE;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!stats) stats = h->h.stats;
+    int n = 0;
+    cudaError_t e = launch_group_norm(h->h, x, gamma, beta, nullptr, stats, st, &n);
+    if (e == cudaSuccess) e = launch_norm_quantize(s, mx4_shape(s.N * s.P, s.C), x, gamma, beta, stats, mx, st);
+    return launched(e, n + 1, "group norm launch");
+}
+
+int patdnn_norm_grad(patdnn_norm h, const void *x, const float *gamma, const float *beta, const float *stats, const void *dy, void *dx,
+                     float *dgamma, float *dbeta, void *stream) {
+    if (!h || !dgamma || !dbeta) return PATDNN_E_NULL;
+    const NormShape &s = h->h.s;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (s.N == 0) {
+        CU(cudaMemsetAsync(dgamma, 0, sizeof(float) * s.C, st));
+        CU(cudaMemsetAsync(dbeta, 0, sizeof(float) * s.C, st));
+        return PATDNN_OK;
+    }
+    if (!x || !gamma || !beta || !stats || !dy || !dx) return PATDNN_E_NULL;
+    int n = 0;
+    const cudaError_t e = launch_group_norm_grad(h->h, x, gamma, beta, stats, dy, dx, dgamma, dbeta, st, &n);
+    return launched(e, n, "group norm gradient launch");
+}
+
+int patdnn_norm_free(patdnn_norm h) {
+    delete h;
+    return PATDNN_OK;
+}
+
+int patdnn_mx4_bytes(int64_t rows, int64_t cols, int64_t *bytes) {
+    if (!bytes) return PATDNN_E_NULL;
+    if (!mx_size_ok(rows, cols)) return PATDNN_E_SHAPE;
+    *bytes = mx4_shape(rows, cols).bytes;
+    return PATDNN_OK;
+}
+
+int patdnn_mx4_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, void *mx, void *stream) {
+    if (!known_type(dtype)) return PATDNN_E_DTYPE;
+    if (!mx_size_ok(rows, cols)) return PATDNN_E_SHAPE;
+    if (ld == 0) ld = cols;
+    if (ld < cols || !aligned(mx, 16)) return PATDNN_E_SHAPE;
+    if (rows == 0) return PATDNN_OK;
+    if (!x || !mx) return PATDNN_E_NULL;
+    return launched(launch_mx4_quantize(mx4_shape(rows, cols), x, dtype, ld, mx, static_cast<cudaStream_t>(stream)), 1, "4-bit quantisation launch");
+}
+
+int patdnn_mx4_dequantize(const void *mx, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, void *out, void *stream) {
+    if (!known_type(dtype)) return PATDNN_E_DTYPE;
+    if (!mx_size_ok(rows, cols)) return PATDNN_E_SHAPE;
+    if (ld == 0) ld = cols;
+    if (ld < cols || !aligned(mx, 16)) return PATDNN_E_SHAPE;
+    if (rows == 0) return PATDNN_OK;
+    if (!out || !mx) return PATDNN_E_NULL;
+    return launched(launch_mx4_dequantize(mx4_shape(rows, cols), mx, out, dtype, ld, static_cast<cudaStream_t>(stream)), 1, "4-bit read-back launch");
+}
+
+int patdnn_linear_encode(const void *weights, int64_t ldw, const patdnn_linear_desc *desc, void *stream, patdnn_linear *out) {
+    if (!weights || !desc || !out) return PATDNN_E_NULL;
+    if (!known_type(desc->dtype) || !known_act(desc->act)) return PATDNN_E_DTYPE;
+    if (desc->F < 1 || desc->K < 1 || !mx_size_ok(desc->F, desc->K) || desc->F > kMostColumns || !mx_size_ok(desc->max_rows, desc->K))
+        return PATDNN_E_SHAPE;
+    if (ldw == 0) ldw = desc->K;
+    if (ldw < desc->K) return PATDNN_E_SHAPE;
+    patdnn_linear h = new (std::nothrow) patdnn_linear_s();
+    if (!h) return PATDNN_E_ALLOC;
+    h->d = *desc;
+    h->d.bias = nullptr;
+    h->shape = mx4_shape(desc->F, desc->K);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = allocate(&h->w, static_cast<size_t>(h->shape.bytes));
+    if (e == cudaSuccess && desc->max_rows) e = allocate(&h->x, static_cast<size_t>(mx4_shape(desc->max_rows, desc->K).bytes));
+    if (e == cudaSuccess) e = allocate(&h->status, 4);
+    if (e == cudaSuccess) e = cudaMemsetAsync(h->status, 0, 16, st);
+    if (e == cudaSuccess && desc->bias) {
+        e = allocate(&h->bias, static_cast<size_t>(desc->F));
+        if (e == cudaSuccess) e = cudaMemcpyAsync(h->bias, desc->bias, sizeof(float) * desc->F, cudaMemcpyDeviceToDevice, st);
+    }
+    if (e == cudaSuccess) e = prepare_mx4_linear();
+    if (e == cudaSuccess) e = launch_mx4_quantize(h->shape, weights, desc->dtype, ldw, h->w, st);
+    if (e == cudaSuccess) {
+        count_launches(1);
+        e = cudaStreamSynchronize(st);
+    }
+    if (e != cudaSuccess) {
+        const int rc = cuda_fail(e, "patdnn_linear_encode");
+        delete h;
+        return rc;
+    }
+    *out = h;
+    return PATDNN_OK;
+}
+
+int patdnn_linear_run(patdnn_linear h, const void *x, int64_t rows, int64_t ldx, void *y, int64_t ldy, void *stream) {
+    if (!h) return PATDNN_E_NULL;
+    if (ldx == 0) ldx = h->d.K;
+    if (ldy == 0) ldy = h->d.F;
+    if (rows < 0 || rows > h->d.max_rows || ldx < h->d.K || ldy < h->d.F) return PATDNN_E_SHAPE;
+    if (rows == 0) return PATDNN_OK;
+    if (!x || !y) return PATDNN_E_NULL;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const Mx4Shape xs = mx4_shape(rows, h->d.K);
+    const int rc = launched(launch_mx4_quantize(xs, x, h->d.dtype, ldx, h->x, st), 1, "4-bit quantisation launch");
+    return rc ? rc : product(h, xs, h->x, rows, y, ldy, st);
+}
+
+int patdnn_linear_run_mx4(patdnn_linear h, const void *mx, int64_t rows, void *y, int64_t ldy, void *stream) {
+    if (!h) return PATDNN_E_NULL;
+    if (ldy == 0) ldy = h->d.F;
+    if (!mx_size_ok(rows, h->d.K) || ldy < h->d.F || !aligned(mx, 16)) return PATDNN_E_SHAPE;
+    if (rows == 0) return PATDNN_OK;
+    if (!mx || !y) return PATDNN_E_NULL;
+    return product(h, mx4_shape(rows, h->d.K), mx, rows, y, ldy, static_cast<cudaStream_t>(stream));
+}
+
+int patdnn_linear_check(patdnn_linear h) {
+    if (!h) return PATDNN_E_NULL;
+    CU(cudaDeviceSynchronize());
+    int word = 0;
+    CU(cudaMemcpy(&word, h->status, sizeof(int), cudaMemcpyDeviceToHost));
+    if (!word) return PATDNN_OK;
+    CU(cudaMemset(h->status, 0, sizeof(int)));
+    return PATDNN_E_DEVICE_TIMEOUT;
+}
+
+int patdnn_linear_free(patdnn_linear h) {
+    delete h;
+    return PATDNN_OK;
+}
+
+}  // extern "C"
