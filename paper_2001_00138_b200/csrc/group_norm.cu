@@ -1,18 +1,19 @@
 // Group norm with an activation over channels-last tensors, and its gradient.
 //
 //   x [N][P][C], group g of channel c = c / (C / G); mean, var over the P * C/G values of (n, g), rstd = 1/sqrt(var + eps)
-//   xh = (x - mean) * rstd, z = xh * gamma_c + beta_c, y = act(z)
-//   gradient: dz = dy * act'(z); A_nc = sum_p dz, B_nc = sum_p dz * xh; dbeta = sum_n A, dgamma = sum_n B;
+//   d = x - mean, z = d * (rstd * gamma_c) + beta_c, y = act(z)
+//   gradient: dz = dy * act'(z); A_nc = sum_p dz, B_nc = rstd * sum_p dz * d; dbeta = sum_n A, dgamma = sum_n B;
 //   with m = P * C/G, s1 = sum_{c in g} gamma_c A_nc / m, s2 = sum_{c in g} gamma_c B_nc / m:
-//   dx = rstd * (gamma_c * dz - s1 - xh * s2)
+//   dx = rstd * gamma_c * dz - rstd * s1 - d * rstd^2 * s2
 //
 // Both are bound by HBM: the forward's floor is one read of x and one write of y, the gradient's one read of x and dy and one
 // write of dx.  Two forms:
 //   resident  a thread-block cluster (up to 8 CTAs) owns a slab of whole groups of one image, keeps it in shared memory
 //             while the statistics are formed and joined over distributed shared memory, and writes the result from there: one
 //             launch, every value read once.
-//   two-pass  images whose slabs do not fit: partial statistics per (chunk of pixels, channel), a small kernel that joins
-//             them, and an elementwise pass that reads x again (from L2 where it still is there).
+//   two-pass  images whose slabs do not fit: partial statistics per (chunk of pixels, group), a small kernel that joins
+//             them, and an elementwise pass that reads x again.  Images are taken in runs of at most kRunBytes, so that
+//             the second read comes from L2.
 // All sums are fp32 and joined in a fixed order.  Variances are never formed as a difference of two large sums: a thread sums (x - m)
 // and (x - m)^2 around its own running mean m, a few pixels at a time, and partial results are joined by their means.
 #include "ops.hpp"
@@ -32,11 +33,10 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBatch = 8;                   // pixels a thread loads at a time
 
 struct NormArgs {
     const void *x, *dy;
-    void *y;                                // dx in the gradient
+    void *y;                                // dx in the gradient; nullptr: statistics only
     const float *gamma, *beta, *stats_in;
     float *stats_out, *dgamma, *dbeta;
     float *ws;
@@ -44,7 +44,12 @@ struct NormArgs {
     int64_t x_pixel, x_image, y_pixel, y_image, P, chunk;
     int N, C, G, per;                       // per = C / G
     int slab, slabs, cluster, chunks, act;
+    int parts;                              // two-pass: slabs that share a group (1: slabs hold whole groups)
+    int n0;                                 // two-pass: first image of the run
     float eps, inv_count;
+    uint8_t *mx;                            // 4-bit output (resident form)
+    int64_t mx_scales;
+    int mx_width, mx_col_tiles;
 };
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -53,43 +58,48 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// Running mean and sum of squared deviations of V channels over the pixels a thread visits.  `add` takes a batch of up to kBatch pixels:
-// the sums are taken around the running mean (around the first pixel in the first batch), so a batch of b values loses
+// Running mean and sum of squared deviations of V channels over the pixels a thread visits, up to kMerge at a time:
+// the sums are taken around the running mean (around the first pixel in the first run), so a run of b values loses
 // at most about b rounding errors of the largest deviation.
+constexpr int kMerge = 32;
 template <int V>
 struct Moments {
-    float mean[V], m2[V], s1[V], s2[V];
+    Fv<V> mean, m2, s1, s2;
     int n;
     __device__ __forceinline__ void clear() {
         n = 0;
-#pragma unroll
-        for (int j = 0; j < V; ++j) mean[j] = m2[j] = 0.f;
+        mean = m2 = Fv<V>::all(0.f);
     }
     template <typename T>
-    __device__ __forceinline__ void begin(const Vec<T, V> &first) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            s1[j] = s2[j] = 0.f;
-            if (n == 0) mean[j] = to_float(first.v[j]);
-        }
+    __device__ __forceinline__ void begin(const Pack<T, V> &first) {
+        s1 = s2 = Fv<V>::all(0.f);
+        if (n == 0) mean = widen<T, V>(first);         // (NaN and infinities included: they end in every result)
     }
     template <typename T>
-    __device__ __forceinline__ void take(const Vec<T, V> &x) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float d = to_float(x.v[j]) - mean[j];
-            s1[j] += d;
-            s2[j] = fmaf(d, d, s2[j]);
-        }
+    __device__ __forceinline__ void take(const Pack<T, V> &x) {
+        const Fv<V> d = fma(mean, Fv<V>::all(-1.f), widen<T, V>(x));
+        s1 = s1 + d;
+        s2 = fma(d, d, s2);
     }
     __device__ __forceinline__ void end(int count) {
         n += count;
-        const float inv = __fdividef(1.f, static_cast<float>(n));
+        const Fv<V> inv = Fv<V>::all(__fdividef(1.f, static_cast<float>(n)));
+        const Fv<V> shift = s1 * inv;
+        mean = mean + shift;
+        m2 = (m2 + fma(s1 * Fv<V>::all(-1.f), shift, s2)).map([](float m) { return m < 0.f ? 0.f : m; });   // NaN stays NaN
+    }
+};
+
+// Groups of V neighbouring channels, the first of which is c.
+template <int V>
+struct Groups {
+    int g[V];
+    __device__ __forceinline__ Groups(int c, int per) {
+        int at = c / per, in = c - at * per;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const float shift = s1[j] * inv;
-            mean[j] += shift;
-            m2[j] = fmaxf(m2[j] + s2[j] - s1[j] * shift, 0.f) + 0.f * s2[j];   // the last term keeps NaN and infinity
+            g[j] = at;
+            if (++in == per) { in = 0; ++at; }
         }
     }
 };
@@ -109,41 +119,232 @@ __device__ __forceinline__ Place place_of(int channels) {
     q.on = q.row < q.rows;
     return q;
 }
+// A thread's own pixels q.row, q.row + q.rows, ... of a slab, brought to shared memory by asynchronous copies kDepth batches ahead of
+// their use, so that the bytes in flight cost no registers.  Every thread reads back only what it copied itself: no barrier.
+// KEEP: they stay in `tile` [pixels][channels]; otherwise they pass through a ring of kDepth batches, [batch][pixel of it][thread].
+// TENSORS (one or two) share at most 256 bytes per thread, so that three CTAs fit an SM.
+template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t to, const void *from) {
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ uint32_t shared_address(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LATER> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LATER) : "memory"); }
 
-// Joins the per-thread moments of a CTA per group of its slab.  red: [rows][channels] (mean, m2); a warp takes a group at a time:
-// first the mean over all its entries, then the squared deviations around it.  grp[g] = (mean, m2) over n0 * per values.
-__device__ __forceinline__ void join_groups(const float2 *red, int rows, int channels, int per, int64_t pixels, float2 *grp) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int groups = channels / per;
-    const float total = static_cast<float>(pixels) * per;
-    for (int g = warp; g < groups; g += kThreads / 32) {
-        float s = 0.f;
-        for (int r = lane; r < rows; r += 32) {
-            const float n = static_cast<float>((pixels - r + rows - 1) / rows);     // pixels that row r visited
-            float t = 0.f;
-            if (n > 0.f) for (int c = 0; c < per; ++c) t += red[r * channels + g * per + c].x;
-            s += n * t;
+template <typename T, int V, bool KEEP, int TENSORS>
+struct Stream {
+    static constexpr int kBytes = sizeof(T) * V;
+    static constexpr int kBatch = KEEP ? 8 : 4 / TENSORS;      // pixels a thread takes at a time
+    static constexpr int kDepth = 4;
+    const T *src;
+    int64_t src_step;                                  // elements between this thread's pixels
+    uint32_t to, from, step, ring, end;                // shared memory: next pixel to copy, next to read, distance; the ring's bounds
+    int left;                                          // pixels still to copy
+    __device__ __forceinline__ void begin(const T *first, int64_t stride, int pixels, const Place &q, T *space, int channels, int col) {
+        src = first + q.row * stride;
+        src_step = q.rows * stride;
+        step = (KEEP ? q.rows * channels : kThreads * V) * sizeof(T);
+        ring = shared_address(KEEP ? space + q.row * channels + col : space + threadIdx.x * V);
+        end = ring + kDepth * kBatch * step;
+        to = from = ring;
+        left = (pixels - q.row + q.rows - 1) / q.rows;
+    }
+    __device__ __forceinline__ void one() {
+        if constexpr (kBytes >= 4) {
+            copy_async<kBytes>(to, src);
+        } else {
+            const uint16_t t = *reinterpret_cast<const uint16_t *>(src);
+            asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"(t) : "memory");
         }
-        const float mean = warp_sum(s) / total;
-        float q = 0.f;
-        for (int r = lane; r < rows; r += 32) {
-            const float n = static_cast<float>((pixels - r + rows - 1) / rows);
-            if (n > 0.f)
-                for (int c = 0; c < per; ++c) {
-                    const float2 e = red[r * channels + g * per + c];
-                    const float d = e.x - mean;
-                    q += e.y + n * d * d;
-                }
+        src += src_step;
+        to += step;
+    }
+    __device__ __forceinline__ void copy() {           // one batch
+        if (left >= kBatch) {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) one();
+        } else {
+            for (int u = 0; u < left; ++u) one();
+        }
+        left -= kBatch;
+        if (!KEEP && to == end) to = ring;
+    }
+    __device__ __forceinline__ Pack<T, V> peek() const {
+        Pack<T, V> v;
+        v.load_shared(from);
+        return v;
+    }
+    __device__ __forceinline__ Pack<T, V> get() {
+        const Pack<T, V> v = peek();
+        from += step;
+        return v;
+    }
+    __device__ __forceinline__ void wrap() {           // after each batch read
+        if (!KEEP && from == end) from = ring;
+    }
+};
+
+// Moments of a thread's pixels.
+template <typename T, int V, bool KEEP>
+__device__ __forceinline__ void moments_of(Stream<T, V, KEEP, 1> &x, Moments<V> &m) {
+    constexpr int kBatch = Stream<T, V, KEEP, 1>::kBatch, kDepth = Stream<T, V, KEEP, 1>::kDepth;
+    m.clear();
+    int count = x.left;                                // pixels still to read
+#pragma unroll
+    for (int b = 0; b < kDepth; ++b) { x.copy(); copies_commit(); }
+    while (count > 0) {
+        const int run = min(count, kMerge);
+        copies_wait<kDepth - 1>();
+        m.begin(x.peek());
+        for (int left = run; left > 0; left -= kBatch) {
+            if (left < run) copies_wait<kDepth - 1>();
+            if (left >= kBatch) {
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) m.take(x.get());
+                x.wrap();
+            } else {
+                for (int u = 0; u < left; ++u) m.take(x.get());
+            }
+            x.copy();
+            copies_commit();
+        }
+        m.end(run);
+        count -= run;
+    }
+}
+
+// How many of a thread's V channels are joined in its registers: all of them or whole groups where sizes allow, else one.
+template <int V> __device__ __forceinline__ int joined_channels(int per) { return per % V == 0 ? V : V % per == 0 ? per : 1; }
+
+// Puts a thread's moments into red [rows][channels / joined], joined_channels at a time: the mean of their means, and the squared
+// deviations around it.
+template <int V>
+__device__ __forceinline__ void put_moments(const Moments<V> &m, const Place &q, int channels, int per, float2 *red) {
+    const int joined = joined_channels<V>(per);
+    float2 *to = red + q.row * (channels / joined) + q.col * V / joined;
+    if (joined == 1) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) to[j] = make_float2(m.mean.get(j), m.m2.get(j));
+        return;
+    }
+    const float n = static_cast<float>(m.n);
+    auto put = [&](int first, int count) {             // (unrolled: registers stay registers)
+        float s = 0.f, sq = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (j >= first && j < first + count) s += m.mean.get(j);
+        const float mean = s / static_cast<float>(count);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (j >= first && j < first + count) {
+                const float d = m.mean.get(j) - mean;
+                sq += fmaf(n * d, d, m.m2.get(j));
+            }
+        to[first / count] = make_float2(mean, sq);
+    };
+    if (joined == V) put(0, V);
+    if constexpr (V >= 4)
+        if (joined == 2) {
+#pragma unroll
+            for (int f = 0; f < V; f += 2) put(f, 2);
+        }
+    if constexpr (V >= 8)
+        if (joined == 4) {
+#pragma unroll
+            for (int f = 0; f < V; f += 4) put(f, 4);
+        }
+}
+
+// Joins the entries of red, `width` per group and row, per group.  A warp takes a group at a time: first the mean over all its
+// entries, then the squared deviations around it.  grp[g * stride] = (mean, m2).
+template <int V>
+__device__ __forceinline__ void join_groups(const float2 *red, int rows, int channels, int per, int pixels, float2 *grp, int64_t stride = 1) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int joined = joined_channels<V>(per), width = per / joined, pitch = channels / joined;
+    const int groups = channels / per;
+    const float inv_total = 1.f / (static_cast<float>(pixels) * static_cast<float>(width));
+    const int base = pixels / rows, extra = pixels - base * rows;      // row r visited base pixels, or one more
+    const int items = min(rows, pixels) * width;
+    const float many = static_cast<float>(joined);
+    for (int g = warp; g < groups; g += kThreads / 32) {
+        float s = 0.f, q = 0.f;
+        const float2 *from = red + g * width;
+        for (int i = lane; i < items; i += 32) {
+            const int r = i / width;
+            s = fmaf(static_cast<float>(base + (r < extra)), from[r * pitch + i - r * width].x, s);
+        }
+        const float mean = warp_sum(s) * inv_total;
+        for (int i = lane; i < items; i += 32) {
+            const int r = i / width;
+            const float2 e = from[r * pitch + i - r * width];
+            const float d = e.x - mean;
+            q += fmaf(static_cast<float>(base + (r < extra)) * many * d, d, e.y);
         }
         q = warp_sum(q);
-        if (lane == 0) grp[g] = make_float2(mean, q);
+        if (lane == 0) grp[g * stride] = make_float2(mean, q);
+    }
+}
+
+// act(norm) of a CTA's pixels from shared memory, as rows of a 4-bit matrix.  A thread keeps eight columns and walks over the
+// pixels; four neighbouring lanes share a block of 32.  The last slab also writes the zeros up to a multiple of 64 columns, which
+// the product's steps cover.
+template <typename T, int ACT>
+__device__ __forceinline__ void write_mx4(const NormArgs &a, const T *tile, const float2 *fin, int n, int64_t p0, int pixels, int c0, int channels) {
+    const int width = c0 + channels == a.C ? (a.C + 63) / 64 * 64 - c0 : channels;
+    const int units = width / 8, rows = kThreads / units;
+    const int unit = threadIdx.x % units, first = threadIdx.x / units;
+    const int c = unit * 8;
+    const Groups<8> at(c, a.per);
+    const Fv<8> shift = Fv<8>::make([&](int j) { return c + j < channels ? -fin[at.g[j]].x : 0.f; });
+    const Fv<8> scale = Fv<8>::make([&](int j) { return c + j < channels ? fin[at.g[j]].y * a.gamma[c0 + c + j] : 0.f; });
+    const Fv<8> beta = Fv<8>::make([&](int j) { return c + j < channels ? a.beta[c0 + c + j] : 0.f; });
+    const bool whole = c + 8 <= channels && channels % (16 / sizeof(T)) == 0;
+    const int ct = (c0 + c) / a.mx_width, in_tile = (c0 + c) - ct * a.mx_width;
+    const int scale_col = (in_tile >> 7) * 512 + ((in_tile >> 5) & 3);
+    const int row_bytes = a.mx_width / 2, code_bytes = 128 * row_bytes, scale_bytes = a.mx_width > 128 ? 1024 : 512;
+    const int row0 = static_cast<int>(n * a.P + p0);
+    for (int base = 0; base < pixels; base += rows) {
+        const int p = base + first;
+        const bool on = first < rows && p < pixels;
+        Fv<8> z = Fv<8>::all(0.f);
+        if (on) {
+            const T *src = tile + p * channels + c;
+            if (whole) {
+                constexpr int A = 16 / sizeof(T);
+                Pack<T, 8> t;
+#pragma unroll
+                for (int i = 0; i < 8 / A; ++i) {
+                    Pack<T, A> part;
+                    part.load_shared(shared_address(src + i * A));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) t.w[4 * i + k] = part.w[k];
+                }
+                z = widen<T, 8>(t);
+            } else {
+                z = Fv<8>::make([&](int j) { return c + j < channels ? to_float(src[j]) : 0.f; });
+            }
+            z = activate<ACT, 8>(fma(z + shift, scale, beta));
+        }
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = whole || c + j < channels ? z.get(j) : 0.f;
+        uint32_t codes;
+        const uint32_t byte = quantise8(v, codes);
+        if (on) {
+            const int row = row0 + p, r = row & 127;   // (a 4-bit matrix has fewer than 2^31 rows)
+            const int64_t t = static_cast<int64_t>(row >> 7) * a.mx_col_tiles + ct;
+            int at = r * row_bytes + in_tile / 2;
+            at ^= ((at >> 7) & (a.mx_width / 32 - 1)) << 4;
+            *reinterpret_cast<uint32_t *>(a.mx + t * code_bytes + at) = codes;
+            if ((unit & 3) == 0) a.mx[a.mx_scales + t * scale_bytes + scale_col + (r & 31) * 16 + (r >> 5) * 4] = static_cast<uint8_t>(byte);
+        }
     }
 }
 
 // ---- resident form ----------------------------------------------------------------------------------------------------
 // Shared memory: [chunk][slab] elements of x, then [rows][slab] float2, then [groups of the slab] float2 twice.
-template <typename T, int V>
-__global__ void __launch_bounds__(kThreads, 2) norm_resident_kernel(NormArgs a) {
+template <typename T, int V, int ACT, bool MX>
+__global__ void __launch_bounds__(kThreads, 3) norm_resident_kernel(NormArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     pdl_trigger();
     const int rank = blockIdx.x % a.cluster;
@@ -159,105 +360,123 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_kernel(NormArgs a) 
     float2 *fin = grp + a.slab / a.per;
     const int groups = channels / a.per;
     pdl_wait();
-
-    Moments<V> m;
-    m.clear();
     if (q.on) {
-        const T *src = static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + c0 + q.col * V;
-        for (int p = q.row; p < pixels; p += q.rows * kBatch) {
-            Vec<T, V> v[kBatch];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u)
-                if (p + u * q.rows < pixels) v[u] = *reinterpret_cast<const Vec<T, V> *>(src + (p + u * q.rows) * a.x_pixel);
-            m.begin(v[0]);
-            int count = 0;
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u)
-                if (p + u * q.rows < pixels) {
-                    m.take(v[u]);
-                    ++count;
-                    *reinterpret_cast<Vec<T, V> *>(tile + (p + u * q.rows) * channels + q.col * V) = v[u];
-                }
-            m.end(count);
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) red[q.row * channels + q.col * V + j] = make_float2(m.mean[j], m.m2[j]);
+        Moments<V> m;
+        Stream<T, V, true, 1> x;
+        x.begin(static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + c0 + q.col * V, a.x_pixel, pixels, q, tile, channels, q.col * V);
+        moments_of<T, V, true>(x, m);
+        put_moments<V>(m, q, channels, a.per, red);
     }
     __syncthreads();
-    join_groups(red, q.rows, channels, a.per, pixels, grp);
+    if (pixels > 0) join_groups<V>(red, q.rows, channels, a.per, pixels, grp);
     cg::cluster_group cluster = cg::this_cluster();
-    cluster.sync();
+    if (a.cluster > 1) cluster.sync(); else __syncthreads();
     for (int g = threadIdx.x; g < groups; g += kThreads) {
-        float s = 0.f, sq = 0.f;
-        for (int r = 0; r < a.cluster; ++r) {
-            const float cnt = static_cast<float>(max(int64_t(0), min(a.P - r * a.chunk, a.chunk)));
-            if (cnt > 0.f) s += cnt * cluster.map_shared_rank(grp, r)[g].x;
-        }
-        const float mean = s / static_cast<float>(a.P);
-        for (int r = 0; r < a.cluster; ++r) {
-            const float cnt = static_cast<float>(max(int64_t(0), min(a.P - r * a.chunk, a.chunk))) * a.per;
-            if (cnt > 0.f) {
-                const float2 e = cluster.map_shared_rank(grp, r)[g];
-                sq += e.y + cnt * (e.x - mean) * (e.x - mean);
+        float2 e = grp[g];
+        if (a.cluster > 1) {
+            float s = 0.f, sq = 0.f;
+            float2 all[8];
+            float cnt[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                cnt[r] = r < a.cluster ? static_cast<float>(max(int64_t(0), min(a.P - r * a.chunk, a.chunk))) : 0.f;
+                all[r] = cnt[r] > 0.f ? cluster.map_shared_rank(grp, r)[g] : make_float2(0.f, 0.f);
+                s = fmaf(cnt[r], all[r].x, s);
             }
+            const float mean = s / static_cast<float>(a.P);
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const float d = all[r].x - mean;
+                sq += fmaf(cnt[r] * static_cast<float>(a.per) * d, cnt[r] > 0.f ? d : 0.f, all[r].y);
+            }
+            e = make_float2(mean, sq);
         }
-        const float rstd = 1.f / sqrtf(sq * a.inv_count + a.eps);
-        fin[g] = make_float2(mean, rstd);
-        if (a.stats_out && rank == 0) {
-            float *o = a.stats_out + (static_cast<int64_t>(n) * a.G + c0 / a.per + g) * 2;
-            o[0] = mean; o[1] = rstd;
-        }
+        const float rstd = 1.f / sqrtf(e.y * a.inv_count + a.eps);
+        fin[g] = make_float2(e.x, rstd);
+        if (a.stats_out && rank == 0) reinterpret_cast<float2 *>(a.stats_out)[static_cast<int64_t>(n) * a.G + c0 / a.per + g] = fin[g];
     }
-    cluster.sync();                                    // fin is ready; nobody reads this CTA's grp after this point
+    // fin is ready; nobody reads this CTA's grp after this point
+    if (a.cluster > 1) cluster.sync(); else __syncthreads();
+    if constexpr (MX) {
+        write_mx4<T, ACT>(a, tile, fin, n, p0, pixels, c0, channels);
+        return;
+    }
     if (!q.on || !a.y) return;
-    float mean[V], scale[V], beta[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int c = q.col * V + j;
-        const float2 f = fin[c / a.per];
-        mean[j] = f.x; scale[j] = f.y * a.gamma[c0 + c]; beta[j] = a.beta[c0 + c];
-    }
-    T *dst = static_cast<T *>(a.y) + n * a.y_image + p0 * a.y_pixel + c0 + q.col * V;
+    const int col = q.col * V;
+    const Groups<V> at(col, a.per);
+    const Fv<V> shift = Fv<V>::make([&](int j) { return -fin[at.g[j]].x; });
+    const Fv<V> scale = Fv<V>::make([&](int j) { return fin[at.g[j]].y * a.gamma[c0 + col + j]; });
+    const Fv<V> beta = Fv<V>::make([&](int j) { return a.beta[c0 + col + j]; });
+    T *dst = static_cast<T *>(a.y) + n * a.y_image + (p0 + q.row) * a.y_pixel + c0 + q.col * V;
+    uint32_t src = shared_address(tile + q.row * channels + col);
+    const int64_t dst_step = q.rows * a.y_pixel;
+    const uint32_t src_step = q.rows * channels * sizeof(T);
 #pragma unroll 4
-    for (int p = q.row; p < pixels; p += q.rows) {
-        const Vec<T, V> v = *reinterpret_cast<const Vec<T, V> *>(tile + p * channels + q.col * V);
-        Vec<T, V> o;
-#pragma unroll
-        for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(activate(fmaf(to_float(v.v[j]) - mean[j], scale[j], beta[j]), a.act));
-        *reinterpret_cast<Vec<T, V> *>(dst + p * a.y_pixel) = o;
+    for (int p = q.row; p < pixels; p += q.rows, dst += dst_step, src += src_step) {
+        Pack<T, V> v;
+        v.load_shared(src);
+        narrow<T, V>(activate<ACT, V>(fma(widen<T, V>(v) + shift, scale, beta))).store(dst);
     }
 }
 
-// Sums A and B of the gradient over the pixels a thread visits, and dx; x, dy in registers.
+// What a thread keeps of its V channels: d = x - mean, z = d * scale + beta with scale = rstd * gamma.
 template <int V>
-struct Affine {
-    float mean[V], rstd[V], gamma[V], beta[V];
-    template <typename T>
-    __device__ __forceinline__ void slope(const Vec<T, V> &x, const Vec<T, V> &dy, int act, float (&xh)[V], float (&dz)[V]) const {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            xh[j] = (to_float(x.v[j]) - mean[j]) * rstd[j];
-            dz[j] = to_float(dy.v[j]) * activate_slope(fmaf(xh[j], gamma[j], beta[j]), act);
-        }
+struct Channels {
+    Fv<V> shift, scale, beta;                          // shift = -mean
+    __device__ __forceinline__ void load(const NormArgs &a, int n, int c) {
+        const float2 *st = reinterpret_cast<const float2 *>(a.stats_in) + static_cast<int64_t>(n) * a.G;
+        const Groups<V> at(c, a.per);
+        shift = Fv<V>::make([&](int j) { return -st[at.g[j]].x; });
+        scale = Fv<V>::make([&](int j) { return st[at.g[j]].y * a.gamma[c + j]; });
+        beta = Fv<V>::make([&](int j) { return a.beta[c + j]; });
+    }
+    template <int ACT, typename T>
+    __device__ __forceinline__ void slope(const Pack<T, V> &x, const Pack<T, V> &dy, Fv<V> &d, Fv<V> &dz) const {
+        d = widen<T, V>(x) + shift;
+        dz = through<ACT, V>(widen<T, V>(dy), fma(d, scale, beta));
+    }
+    // dx = scale * dz - k1 - d * k2; nk = -k
+    template <int ACT, typename T>
+    __device__ __forceinline__ Pack<T, V> dx(const Pack<T, V> &x, const Pack<T, V> &dy, const Fv<V> &nk1, const Fv<V> &nk2) const {
+        Fv<V> d, dz;
+        slope<ACT, T>(x, dy, d, dz);
+        return narrow<T, V>(fma(d, nk2, fma(scale, dz, nk1)));
     }
 };
 
-// dgamma and dbeta of the channels [c0, c0 + channels) from the per-image sums ws [N][C] (A, B), images in ascending order.
-__device__ __forceinline__ void sum_images(const NormArgs &a, int c0, int channels) {
-    for (int c = c0 + threadIdx.x; c < c0 + channels; c += kThreads) {
-        float sa = 0.f, sb = 0.f;
-        for (int n = 0; n < a.N; ++n) {
-            const float2 e = __ldcg(reinterpret_cast<const float2 *>(a.ws) + static_cast<int64_t>(n) * a.C + c);
-            sa += e.x; sb += e.y;
+// Sums of dz and dz * d over a thread's pixels.
+template <typename T, int V, int ACT, bool KEEP>
+__device__ __forceinline__ void sums_of(Stream<T, V, KEEP, 2> &x, Stream<T, V, KEEP, 2> &dy, const Channels<V> &f, Fv<V> &sa, Fv<V> &sb) {
+    constexpr int kBatch = Stream<T, V, KEEP, 2>::kBatch, kDepth = Stream<T, V, KEEP, 2>::kDepth;
+    sa = sb = Fv<V>::all(0.f);
+    auto take = [&]() {
+        Fv<V> d, dz;
+        f.template slope<ACT, T>(x.get(), dy.get(), d, dz);
+        sa = sa + dz;
+        sb = fma(dz, d, sb);
+    };
+    int count = x.left;
+#pragma unroll
+    for (int b = 0; b < kDepth; ++b) { x.copy(); dy.copy(); copies_commit(); }
+    for (; count > 0; count -= kBatch) {
+        copies_wait<kDepth - 1>();
+        if (count >= kBatch) {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) take();
+            x.wrap();
+            dy.wrap();
+        } else {
+            for (int u = 0; u < count; ++u) take();
         }
-        a.dbeta[c] = sa;
-        a.dgamma[c] = sb;
+        x.copy();
+        dy.copy();
+        copies_commit();
     }
 }
 
 // Shared memory: [chunk][slab] elements of x, the same of dy, [rows][slab] float2, [slab] float2 twice, [groups] float2.
-template <typename T, int V>
-__global__ void __launch_bounds__(kThreads, 2) norm_grad_resident_kernel(NormArgs a) {
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kThreads, 3) norm_grad_resident_kernel(NormArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ bool last;
     pdl_trigger();
@@ -274,48 +493,19 @@ __global__ void __launch_bounds__(kThreads, 2) norm_grad_resident_kernel(NormArg
     float2 *red = reinterpret_cast<float2 *>(smem + 2 * tile_bytes);
     float2 *sums = red + kThreads * V;                 // this CTA's (A, B) per channel
     float2 *whole = sums + a.slab;                     // the image's (A, B) per channel
-    float2 *fin = whole + a.slab;                      // (s1, s2) per group
+    float2 *fin = whole + a.slab;                      // (rstd * s1, rstd^2 * s2) per group
     pdl_wait();
 
-    Affine<V> f;
+    Channels<V> f;
     if (q.on) {
+        f.load(a, n, c0 + q.col * V);
+        Fv<V> sa, sb;
+        Stream<T, V, true, 2> x, dy;
+        x.begin(static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + c0 + q.col * V, a.x_pixel, pixels, q, xt, channels, q.col * V);
+        dy.begin(static_cast<const T *>(a.dy) + n * a.y_image + p0 * a.y_pixel + c0 + q.col * V, a.y_pixel, pixels, q, dt, channels, q.col * V);
+        sums_of<T, V, ACT, true>(x, dy, f, sa, sb);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c = c0 + q.col * V + j;
-            const float2 st = reinterpret_cast<const float2 *>(a.stats_in)[static_cast<int64_t>(n) * a.G + c / a.per];
-            f.mean[j] = st.x; f.rstd[j] = st.y; f.gamma[j] = a.gamma[c]; f.beta[j] = a.beta[c];
-        }
-        float sa[V], sb[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) sa[j] = sb[j] = 0.f;
-        const T *xs = static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + c0 + q.col * V;
-        const T *ds = static_cast<const T *>(a.dy) + n * a.y_image + p0 * a.y_pixel + c0 + q.col * V;
-        constexpr int kHalf = kBatch / 2;              // two tensors: the same bytes in flight
-        for (int p = q.row; p < pixels; p += q.rows * kHalf) {
-            Vec<T, V> xv[kHalf], dv[kHalf];
-#pragma unroll
-            for (int u = 0; u < kHalf; ++u)
-                if (p + u * q.rows < pixels) {
-                    xv[u] = *reinterpret_cast<const Vec<T, V> *>(xs + (p + u * q.rows) * a.x_pixel);
-                    dv[u] = *reinterpret_cast<const Vec<T, V> *>(ds + (p + u * q.rows) * a.y_pixel);
-                }
-#pragma unroll
-            for (int u = 0; u < kHalf; ++u)
-                if (p + u * q.rows < pixels) {
-                    float xh[V], dz[V];
-                    f.slope(xv[u], dv[u], a.act, xh, dz);
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        sa[j] += dz[j];
-                        sb[j] = fmaf(dz[j], xh[j], sb[j]);
-                    }
-                    const int at = (p + u * q.rows) * channels + q.col * V;
-                    *reinterpret_cast<Vec<T, V> *>(xt + at) = xv[u];
-                    *reinterpret_cast<Vec<T, V> *>(dt + at) = dv[u];
-                }
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) red[q.row * channels + q.col * V + j] = make_float2(sa[j], sb[j]);
+        for (int j = 0; j < V; ++j) red[q.row * channels + q.col * V + j] = make_float2(sa.get(j), sb.get(j));
     }
     __syncthreads();
     for (int c = threadIdx.x; c < channels; c += kThreads) {
@@ -324,10 +514,11 @@ __global__ void __launch_bounds__(kThreads, 2) norm_grad_resident_kernel(NormArg
             const float2 e = red[r * channels + c];
             s.x += e.x; s.y += e.y;
         }
+        s.y *= reinterpret_cast<const float2 *>(a.stats_in)[static_cast<int64_t>(n) * a.G + (c0 + c) / a.per].y;
         sums[c] = s;
     }
     cg::cluster_group cluster = cg::this_cluster();
-    cluster.sync();
+    if (a.cluster > 1) cluster.sync(); else __syncthreads();
     for (int c = threadIdx.x; c < channels; c += kThreads) {
         float2 s = make_float2(0.f, 0.f);
         for (int r = 0; r < a.cluster; ++r) {
@@ -346,30 +537,28 @@ __global__ void __launch_bounds__(kThreads, 2) norm_grad_resident_kernel(NormArg
             s1 = fmaf(gm, e.x, s1);
             s2 = fmaf(gm, e.y, s2);
         }
-        fin[g] = make_float2(s1 * a.inv_count, s2 * a.inv_count);
+        const float rstd = reinterpret_cast<const float2 *>(a.stats_in)[static_cast<int64_t>(n) * a.G + c0 / a.per + g].y;
+        fin[g] = make_float2(rstd * (s1 * a.inv_count), rstd * rstd * (s2 * a.inv_count));
     }
-    cluster.sync();                                    // fin is ready; nobody reads this CTA's sums after this point
-    if (q.on && a.y) {
-        float s1[V], s2[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float2 e = fin[(q.col * V + j) / a.per];
-            s1[j] = e.x; s2[j] = e.y;
-        }
-        T *dst = static_cast<T *>(a.y) + n * a.x_image + p0 * a.x_pixel + c0 + q.col * V;
+    // fin is ready; nobody reads this CTA's sums after this point
+    if (a.cluster > 1) cluster.sync(); else __syncthreads();
+    if (q.on) {
+        const Groups<V> at(q.col * V, a.per);
+        const Fv<V> nk1 = Fv<V>::make([&](int j) { return -fin[at.g[j]].x; });
+        const Fv<V> nk2 = Fv<V>::make([&](int j) { return -fin[at.g[j]].y; });
+        T *dst = static_cast<T *>(a.y) + n * a.x_image + (p0 + q.row) * a.x_pixel + c0 + q.col * V;
+        uint32_t xs = shared_address(xt + q.row * channels + q.col * V), ds = shared_address(dt + q.row * channels + q.col * V);
+        const int64_t dst_step = q.rows * a.x_pixel;
+        const uint32_t step = q.rows * channels * sizeof(T);
 #pragma unroll 2
-        for (int p = q.row; p < pixels; p += q.rows) {
-            const Vec<T, V> xv = *reinterpret_cast<const Vec<T, V> *>(xt + p * channels + q.col * V);
-            const Vec<T, V> dv = *reinterpret_cast<const Vec<T, V> *>(dt + p * channels + q.col * V);
-            float xh[V], dz[V];
-            f.slope(xv, dv, a.act, xh, dz);
-            Vec<T, V> o;
-#pragma unroll
-            for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(f.rstd[j] * (fmaf(f.gamma[j], dz[j], -s1[j]) - xh[j] * s2[j]));
-            *reinterpret_cast<Vec<T, V> *>(dst + p * a.x_pixel) = o;
+        for (int p = q.row; p < pixels; p += q.rows, dst += dst_step, xs += step, ds += step) {
+            Pack<T, V> xv, dv;
+            xv.load_shared(xs);
+            dv.load_shared(ds);
+            f.template dx<ACT, T>(xv, dv, nk1, nk2).store(dst);
         }
     }
-    // the last cluster of this slab to get here adds the images up; what it adds, and in which order, does not depend on who is last
+    // The last cluster of this slab to get here adds the images up, in ascending order: the result does not depend on which is last.
     if (rank != 0) return;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -379,57 +568,35 @@ __global__ void __launch_bounds__(kThreads, 2) norm_grad_resident_kernel(NormArg
         __threadfence();
     }
     __syncthreads();
-    if (last) sum_images(a, c0, channels);
+    if (!last) return;
+    for (int c = c0 + threadIdx.x; c < c0 + channels; c += kThreads) {
+        float sa = 0.f, sb = 0.f;
+#pragma unroll 8
+        for (int i = 0; i < a.N; ++i) {
+            const float2 e = __ldcg(reinterpret_cast<const float2 *>(a.ws) + static_cast<int64_t>(i) * a.C + c);
+            sa += e.x; sb += e.y;
+        }
+        a.dbeta[c] = sa;
+        a.dgamma[c] = sb;
+    }
 }
 
 // ---- two-pass form ----------------------------------------------------------------------------------------------------
-// blockIdx = (chunk, slab, image); ws [N][chunks][C] (mean, m2) of the chunk's pixels.
-template <typename T, int V>
-__global__ void __launch_bounds__(kThreads) norm_moments_kernel(NormArgs a) {
-    extern __shared__ __align__(16) unsigned char smem[];
-    float2 *red = reinterpret_cast<float2 *>(smem);
-    pdl_trigger();
-    const int n = blockIdx.z, c0 = blockIdx.y * a.slab, channels = min(a.slab, a.C - c0);
-    const int64_t p0 = blockIdx.x * a.chunk, p1 = min(a.P, p0 + a.chunk);
-    const int pixels = static_cast<int>(p1 - p0);
-    const Place q = place_of<V>(channels);
-    pdl_wait();
-    if (q.on) {
-        Moments<V> m;
-        m.clear();
-        const T *src = static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + c0 + q.col * V;
-        for (int p = q.row; p < pixels; p += q.rows * kBatch) {
-            Vec<T, V> v[kBatch];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u)
-                if (p + u * q.rows < pixels) v[u] = *reinterpret_cast<const Vec<T, V> *>(src + (p + u * q.rows) * a.x_pixel);
-            m.begin(v[0]);
-            int count = 0;
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u)
-                if (p + u * q.rows < pixels) {
-                    m.take(v[u]);
-                    ++count;
-                }
-            m.end(count);
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) red[q.row * channels + q.col * V + j] = make_float2(m.mean[j], m.m2[j]);
+// Channels of a slab: whole groups, or (parts > 1) one of the `parts` slabs of a group wider than a CTA.
+struct Span {
+    int c0, channels;
+};
+__device__ __forceinline__ Span span_of(const NormArgs &a, int slab) {
+    Span s;
+    if (a.parts > 1) {
+        const int part = slab % a.parts;
+        s.c0 = slab / a.parts * a.per + part * a.slab;
+        s.channels = min(a.slab, a.per - part * a.slab);
+    } else {
+        s.c0 = slab * a.slab;
+        s.channels = min(a.slab, a.C - s.c0);
     }
-    __syncthreads();
-    float2 *out = reinterpret_cast<float2 *>(a.ws) + (static_cast<int64_t>(n) * a.chunks + blockIdx.x) * a.C + c0;
-    for (int c = threadIdx.x; c < channels; c += kThreads) {
-        float s = 0.f, sq = 0.f;
-        const int rows = min(q.rows, pixels);
-        for (int r = 0; r < rows; ++r) s += static_cast<float>((pixels - r + q.rows - 1) / q.rows) * red[r * channels + c].x;
-        const float mean = s / static_cast<float>(pixels);
-        for (int r = 0; r < rows; ++r) {
-            const float2 e = red[r * channels + c];
-            const float d = e.x - mean;
-            sq += e.y + static_cast<float>((pixels - r + q.rows - 1) / q.rows) * d * d;
-        }
-        out[c] = make_float2(mean, sq);
-    }
+    return s;
 }
 
 __device__ __forceinline__ float block_sum(float v, float *scratch) {
@@ -443,124 +610,151 @@ __device__ __forceinline__ float block_sum(float v, float *scratch) {
     return s;
 }
 
-// One CTA per (group, image): joins the chunks' moments of the group's channels.
+// blockIdx = (chunk, slab, image of the run); ws [image of the run][cell][chunk] (mean, m2), a cell being a group or a part of one.
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads, 3) norm_moments_kernel(NormArgs a) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    float2 *red = reinterpret_cast<float2 *>(smem);
+    pdl_trigger();
+    const int n = blockIdx.z;
+    const Span s = span_of(a, blockIdx.y);
+    const int64_t p0 = blockIdx.x * a.chunk, p1 = min(a.P, p0 + a.chunk);
+    const int pixels = static_cast<int>(p1 - p0);
+    const Place q = place_of<V>(s.channels);
+    const int cells = a.parts > 1 ? a.slabs : a.G;
+    pdl_wait();
+    Moments<V> m;
+    if (q.on) {
+        Stream<T, V, false, 1> x;
+        x.begin(static_cast<const T *>(a.x) + (a.n0 + n) * a.x_image + p0 * a.x_pixel + s.c0 + q.col * V, a.x_pixel, pixels, q,
+                reinterpret_cast<T *>(smem), s.channels, 0);
+        moments_of<T, V, false>(x, m);
+    }
+    __syncthreads();                                   // red lies over the rings
+    if (q.on) put_moments<V>(m, q, s.channels, a.parts > 1 ? s.channels : a.per, red);
+    __syncthreads();
+    const int cell = a.parts > 1 ? blockIdx.y : s.c0 / a.per;
+    join_groups<V>(red, q.rows, s.channels, a.parts > 1 ? s.channels : a.per, pixels,
+                reinterpret_cast<float2 *>(a.ws) + (static_cast<int64_t>(n) * cells + cell) * a.chunks + blockIdx.x, a.chunks);
+}
+
+// One CTA per (group, image of the run): joins the chunks' moments, first their mean, then the squared deviations around it.
 __global__ void __launch_bounds__(kThreads) norm_join_kernel(NormArgs a) {
     __shared__ float scratch[kThreads / 32];
     pdl_trigger();
     pdl_wait();
-    const int g = blockIdx.x, n = blockIdx.y;
-    const float2 *part = reinterpret_cast<const float2 *>(a.ws) + static_cast<int64_t>(n) * a.chunks * a.C + g * a.per;
-    const int items = a.chunks * a.per;
+    const int g = blockIdx.x, n = blockIdx.y, items = a.chunks * a.parts;
+    const float2 *w = reinterpret_cast<const float2 *>(a.ws) + (static_cast<int64_t>(n) * a.G + g) * items;
+    auto values = [&](int i) {                         // how many values entry i stands for
+        const int part = i / a.chunks, k = i - part * a.chunks;
+        const int64_t pixels = min(a.chunk, a.P - k * a.chunk);
+        return static_cast<float>(pixels) * static_cast<float>(a.parts > 1 ? min(a.slab, a.per - part * a.slab) : a.per);
+    };
     float s = 0.f, sq = 0.f;
-    for (int i = threadIdx.x; i < items; i += kThreads) {
-        const int k = i / a.per, c = i % a.per;
-        const float cnt = static_cast<float>(min(a.chunk, a.P - k * a.chunk));
-        s += cnt * part[static_cast<int64_t>(k) * a.C + c].x;
-    }
+    for (int i = threadIdx.x; i < items; i += kThreads) s = fmaf(values(i), w[i].x, s);
     const float mean = block_sum(s, scratch) * a.inv_count;
     for (int i = threadIdx.x; i < items; i += kThreads) {
-        const int k = i / a.per, c = i % a.per;
-        const float cnt = static_cast<float>(min(a.chunk, a.P - k * a.chunk));
-        const float2 e = part[static_cast<int64_t>(k) * a.C + c];
-        sq += e.y + cnt * (e.x - mean) * (e.x - mean);
+        const float2 e = w[i];
+        const float d = e.x - mean;
+        sq += fmaf(values(i) * d, d, e.y);
     }
     sq = block_sum(sq, scratch);
-    if (threadIdx.x == 0) {
-        float *o = a.stats_out + (static_cast<int64_t>(n) * a.G + g) * 2;
-        o[0] = mean;
-        o[1] = 1.f / sqrtf(sq * a.inv_count + a.eps);
-    }
+    if (threadIdx.x == 0)
+        reinterpret_cast<float2 *>(a.stats_out)[static_cast<int64_t>(a.n0 + n) * a.G + g] = make_float2(mean, 1.f / sqrtf(sq * a.inv_count + a.eps));
 }
 
-template <typename T, int V>
-__global__ void __launch_bounds__(kThreads) norm_apply_kernel(NormArgs a) {
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kThreads, 3) norm_apply_kernel(NormArgs a) {
     pdl_trigger();
-    const int n = blockIdx.z, c0 = blockIdx.y * a.slab, channels = min(a.slab, a.C - c0);
+    const int n = a.n0 + blockIdx.z;
+    const Span s = span_of(a, blockIdx.y);
     const int64_t p0 = blockIdx.x * a.chunk, p1 = min(a.P, p0 + a.chunk);
     const int pixels = static_cast<int>(p1 - p0);
-    const Place q = place_of<V>(channels);
+    const Place q = place_of<V>(s.channels);
     pdl_wait();
     if (!q.on) return;
-    float mean[V], scale[V], beta[V];
+    extern __shared__ __align__(16) unsigned char smem[];
+    using S = Stream<T, V, false, 1>;
+    S x;
+    x.begin(static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + s.c0 + q.col * V, a.x_pixel, pixels, q, reinterpret_cast<T *>(smem), s.channels, 0);
+    int count = x.left;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int c = c0 + q.col * V + j;
-        const float2 f = reinterpret_cast<const float2 *>(a.stats_in)[static_cast<int64_t>(n) * a.G + c / a.per];
-        mean[j] = f.x; scale[j] = f.y * a.gamma[c]; beta[j] = a.beta[c];
-    }
-    const T *src = static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + c0 + q.col * V;
-    T *dst = static_cast<T *>(a.y) + n * a.y_image + p0 * a.y_pixel + c0 + q.col * V;
-#pragma unroll 4
-    for (int p = q.row; p < pixels; p += q.rows) {
-        const Vec<T, V> v = *reinterpret_cast<const Vec<T, V> *>(src + p * a.x_pixel);
-        Vec<T, V> o;
+    for (int b = 0; b < S::kDepth; ++b) { x.copy(); copies_commit(); }
+    Channels<V> f;
+    f.load(a, n, s.c0 + q.col * V);
+    T *dst = static_cast<T *>(a.y) + n * a.y_image + (p0 + q.row) * a.y_pixel + s.c0 + q.col * V;
+    const int64_t dst_step = q.rows * a.y_pixel;
+    auto put = [&]() {
+        narrow<T, V>(activate<ACT, V>(fma(widen<T, V>(x.get()) + f.shift, f.scale, f.beta))).store(dst);
+        dst += dst_step;
+    };
+    for (; count > 0; count -= S::kBatch) {
+        copies_wait<S::kDepth - 1>();
+        if (count >= S::kBatch) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(activate(fmaf(to_float(v.v[j]) - mean[j], scale[j], beta[j]), a.act));
-        *reinterpret_cast<Vec<T, V> *>(dst + p * a.y_pixel) = o;
+            for (int u = 0; u < S::kBatch; ++u) put();
+            x.wrap();
+        } else {
+            for (int u = 0; u < count; ++u) put();
+        }
+        x.copy();
+        copies_commit();
     }
 }
 
 // ws [N][chunks][C] (A, B) of the chunk's pixels.
-template <typename T, int V>
-__global__ void __launch_bounds__(kThreads) norm_grad_sums_kernel(NormArgs a) {
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kThreads, 3) norm_grad_sums_kernel(NormArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     float2 *red = reinterpret_cast<float2 *>(smem);
     pdl_trigger();
-    const int n = blockIdx.z, c0 = blockIdx.y * a.slab, channels = min(a.slab, a.C - c0);
+    const int n = a.n0 + blockIdx.z;
+    const Span s = span_of(a, blockIdx.y);
     const int64_t p0 = blockIdx.x * a.chunk, p1 = min(a.P, p0 + a.chunk);
     const int pixels = static_cast<int>(p1 - p0);
-    const Place q = place_of<V>(channels);
+    const Place q = place_of<V>(s.channels);
     pdl_wait();
+    Fv<V> sa, sb;
     if (q.on) {
-        Affine<V> f;
+        Channels<V> f;
+        f.load(a, n, s.c0 + q.col * V);
+        T *ring = reinterpret_cast<T *>(smem);
+        Stream<T, V, false, 2> x, dy;
+        x.begin(static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + s.c0 + q.col * V, a.x_pixel, pixels, q, ring, s.channels, 0);
+        dy.begin(static_cast<const T *>(a.dy) + n * a.y_image + p0 * a.y_pixel + s.c0 + q.col * V, a.y_pixel, pixels, q,
+                 ring + Stream<T, V, false, 2>::kDepth * Stream<T, V, false, 2>::kBatch * kThreads * V, s.channels, 0);
+        sums_of<T, V, ACT, false>(x, dy, f, sa, sb);
+    }
+    __syncthreads();                                   // red lies over the rings
+    if (q.on) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c = c0 + q.col * V + j;
-            const float2 st = reinterpret_cast<const float2 *>(a.stats_in)[static_cast<int64_t>(n) * a.G + c / a.per];
-            f.mean[j] = st.x; f.rstd[j] = st.y; f.gamma[j] = a.gamma[c]; f.beta[j] = a.beta[c];
-        }
-        float sa[V], sb[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) sa[j] = sb[j] = 0.f;
-        const T *xs = static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + c0 + q.col * V;
-        const T *ds = static_cast<const T *>(a.dy) + n * a.y_image + p0 * a.y_pixel + c0 + q.col * V;
-#pragma unroll 4
-        for (int p = q.row; p < pixels; p += q.rows) {
-            float xh[V], dz[V];
-            f.slope(*reinterpret_cast<const Vec<T, V> *>(xs + p * a.x_pixel), *reinterpret_cast<const Vec<T, V> *>(ds + p * a.y_pixel),
-                    a.act, xh, dz);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                sa[j] += dz[j];
-                sb[j] = fmaf(dz[j], xh[j], sb[j]);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) red[q.row * channels + q.col * V + j] = make_float2(sa[j], sb[j]);
+        for (int j = 0; j < V; ++j) red[q.row * s.channels + q.col * V + j] = make_float2(sa.get(j), sb.get(j));
     }
     __syncthreads();
-    float2 *out = reinterpret_cast<float2 *>(a.ws) + (static_cast<int64_t>(n) * a.chunks + blockIdx.x) * a.C + c0;
-    for (int c = threadIdx.x; c < channels; c += kThreads) {
-        float2 s = make_float2(0.f, 0.f);
+    float2 *out = reinterpret_cast<float2 *>(a.ws) + (static_cast<int64_t>(n) * a.chunks + blockIdx.x) * a.C + s.c0;
+    for (int c = threadIdx.x; c < s.channels; c += kThreads) {
+        float2 t = make_float2(0.f, 0.f);
         for (int r = 0; r < q.rows; ++r) {
-            const float2 e = red[r * channels + c];
-            s.x += e.x; s.y += e.y;
+            const float2 e = red[r * s.channels + c];
+            t.x += e.x; t.y += e.y;
         }
-        out[c] = s;
+        t.y *= reinterpret_cast<const float2 *>(a.stats_in)[static_cast<int64_t>(n) * a.G + (s.c0 + c) / a.per].y;
+        out[c] = t;
     }
 }
 
-// One CTA per (group, image): sums the chunks, writes (s1, s2) of the group behind the partial sums and the image's (A, B) per channel
-// into chunk 0's place.
+// One CTA per (group, image of the run): sums the chunks, writes (rstd s1, rstd^2 s2) of the group behind the partial sums and the
+// image's (A, B) per channel into chunk 0's place.
 __global__ void __launch_bounds__(kThreads) norm_grad_join_kernel(NormArgs a) {
     __shared__ float scratch[kThreads / 32];
     pdl_trigger();
     pdl_wait();
-    const int g = blockIdx.x, n = blockIdx.y;
+    const int g = blockIdx.x, n = a.n0 + blockIdx.y;
     float2 *part = reinterpret_cast<float2 *>(a.ws) + static_cast<int64_t>(n) * a.chunks * a.C + g * a.per;
     float s1 = 0.f, s2 = 0.f;
     for (int c = 0; c < a.per; ++c) {
         float sa = 0.f, sb = 0.f;
+#pragma unroll 4
         for (int k = threadIdx.x; k < a.chunks; k += kThreads) {
             const float2 e = part[static_cast<int64_t>(k) * a.C + c];
             sa += e.x; sb += e.y;
@@ -572,23 +766,27 @@ __global__ void __launch_bounds__(kThreads) norm_grad_join_kernel(NormArgs a) {
         s1 = fmaf(gm, sa, s1);
         s2 = fmaf(gm, sb, s2);
     }
-    if (threadIdx.x == 0)
-        reinterpret_cast<float2 *>(a.ws)[static_cast<int64_t>(a.N) * a.chunks * a.C + static_cast<int64_t>(n) * a.G + g] =
-            make_float2(s1 * a.inv_count, s2 * a.inv_count);
+    if (threadIdx.x == 0) {
+        const int64_t at = static_cast<int64_t>(n) * a.G + g;
+        const float rstd = reinterpret_cast<const float2 *>(a.stats_in)[at].y;
+        reinterpret_cast<float2 *>(a.ws)[static_cast<int64_t>(a.N) * a.chunks * a.C + at] = make_float2(rstd * (s1 * a.inv_count), rstd * rstd * (s2 * a.inv_count));
+    }
 }
 
-template <typename T, int V>
-__global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(NormArgs a) {
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kThreads, 3) norm_grad_apply_kernel(NormArgs a) {
     pdl_trigger();
-    const int n = blockIdx.z, c0 = blockIdx.y * a.slab, channels = min(a.slab, a.C - c0);
+    const int n = a.n0 + blockIdx.z;
+    const Span s = span_of(a, blockIdx.y);
     const int64_t p0 = blockIdx.x * a.chunk, p1 = min(a.P, p0 + a.chunk);
     const int pixels = static_cast<int>(p1 - p0);
-    const Place q = place_of<V>(channels);
+    const Place q = place_of<V>(s.channels);
     pdl_wait();
     const float2 *ws = reinterpret_cast<const float2 *>(a.ws);
-    if (n == 0 && blockIdx.x == 0)                     // one CTA per slab also adds the images up
-        for (int c = c0 + threadIdx.x; c < c0 + channels; c += kThreads) {
+    if (n == a.N - 1 && blockIdx.x == 0)               // in the last run, one CTA per slab also adds the images up
+        for (int c = s.c0 + threadIdx.x; c < s.c0 + s.channels; c += kThreads) {
             float sa = 0.f, sb = 0.f;
+#pragma unroll 8
             for (int i = 0; i < a.N; ++i) {
                 const float2 e = ws[static_cast<int64_t>(i) * a.chunks * a.C + c];
                 sa += e.x; sb += e.y;
@@ -596,30 +794,42 @@ __global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(NormArgs a) {
             a.dbeta[c] = sa;
             a.dgamma[c] = sb;
         }
-    if (!q.on || !a.y) return;
-    Affine<V> f;
-    float s1[V], s2[V];
+    if (!q.on) return;
+    Channels<V> f;
+    f.load(a, n, s.c0 + q.col * V);
+    const float2 *k = ws + static_cast<int64_t>(a.N) * a.chunks * a.C + static_cast<int64_t>(n) * a.G;
+    const Groups<V> at(s.c0 + q.col * V, a.per);
+    const Fv<V> nk1 = Fv<V>::make([&](int j) { return -k[at.g[j]].x; });
+    const Fv<V> nk2 = Fv<V>::make([&](int j) { return -k[at.g[j]].y; });
+    extern __shared__ __align__(16) unsigned char smem[];
+    using S = Stream<T, V, false, 2>;
+    S x, dy;
+    T *ring = reinterpret_cast<T *>(smem);
+    x.begin(static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + s.c0 + q.col * V, a.x_pixel, pixels, q, ring, s.channels, 0);
+    dy.begin(static_cast<const T *>(a.dy) + n * a.y_image + p0 * a.y_pixel + s.c0 + q.col * V, a.y_pixel, pixels, q,
+             ring + S::kDepth * S::kBatch * kThreads * V, s.channels, 0);
+    int count = x.left;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int c = c0 + q.col * V + j;
-        const int64_t g = static_cast<int64_t>(n) * a.G + c / a.per;
-        const float2 st = reinterpret_cast<const float2 *>(a.stats_in)[g];
-        f.mean[j] = st.x; f.rstd[j] = st.y; f.gamma[j] = a.gamma[c]; f.beta[j] = a.beta[c];
-        const float2 e = ws[static_cast<int64_t>(a.N) * a.chunks * a.C + g];
-        s1[j] = e.x; s2[j] = e.y;
-    }
-    const T *xs = static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + c0 + q.col * V;
-    const T *ds = static_cast<const T *>(a.dy) + n * a.y_image + p0 * a.y_pixel + c0 + q.col * V;
-    T *dst = static_cast<T *>(a.y) + n * a.x_image + p0 * a.x_pixel + c0 + q.col * V;
-#pragma unroll 4
-    for (int p = q.row; p < pixels; p += q.rows) {
-        float xh[V], dz[V];
-        f.slope(*reinterpret_cast<const Vec<T, V> *>(xs + p * a.x_pixel), *reinterpret_cast<const Vec<T, V> *>(ds + p * a.y_pixel),
-                a.act, xh, dz);
-        Vec<T, V> o;
+    for (int b = 0; b < S::kDepth; ++b) { x.copy(); dy.copy(); copies_commit(); }
+    T *dst = static_cast<T *>(a.y) + n * a.x_image + (p0 + q.row) * a.x_pixel + s.c0 + q.col * V;
+    const int64_t dst_step = q.rows * a.x_pixel;
+    auto put = [&]() {
+        f.template dx<ACT, T>(x.get(), dy.get(), nk1, nk2).store(dst);
+        dst += dst_step;
+    };
+    for (; count > 0; count -= S::kBatch) {
+        copies_wait<S::kDepth - 1>();
+        if (count >= S::kBatch) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(f.rstd[j] * (fmaf(f.gamma[j], dz[j], -s1[j]) - xh[j] * s2[j]));
-        *reinterpret_cast<Vec<T, V> *>(dst + p * a.x_pixel) = o;
+            for (int u = 0; u < S::kBatch; ++u) put();
+            x.wrap();
+            dy.wrap();
+        } else {
+            for (int u = 0; u < count; ++u) put();
+        }
+        x.copy();
+        dy.copy();
+        copies_commit();
     }
 }
 
@@ -633,11 +843,12 @@ int resident_smem(const NormShape &s, int width, int tensors, int slab, int64_t 
 }
 
 constexpr int kSmemMost = 220 * 1024;       // dynamic shared memory of one CTA
+constexpr int64_t kRunBytes = int64_t(64) << 20;   // two-pass: bytes of x (and dy) of the images that are taken together
 
-// Picks the slab and the cluster of the resident form by a time estimate: a CTA loads its share at its part of an SM's HBM rate
-// (44 bytes per ns), then stores it; `per_sm` CTAs overlap; every wave pays a fixed latency.  Slabs narrower than 128
-// bytes cost more per byte.
-NormPlan plan_one(const NormShape &s, int width, int tensors) {
+// Picks the slab and the cluster of the resident form by a time estimate: the CTAs of an SM move its share of the HBM rate (44
+// bytes per ns) if there are at least three of them, less if there are fewer; every wave pays a fixed latency.
+// Slabs narrower than 128 bytes cost more per byte.  `unit`: slabs are a multiple of so many channels (or all of them).
+NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
     NormPlan best;
     const int per = s.C / s.G, e = elem_bytes(s.dtype);
     double best_us = 1e30;
@@ -645,18 +856,19 @@ NormPlan plan_one(const NormShape &s, int width, int tensors) {
         if (s.G % k) continue;
         const int64_t slab = static_cast<int64_t>(k) * per;
         if (slab % width || slab / width > kThreads) continue;
-        if (slab * e < 64 && k < s.G) continue;
+        if (k < s.G && (slab * e < 64 || slab % unit)) continue;
         for (int cl = 1; cl <= 8; cl *= 2) {
             if (cl > s.P) break;
             const int64_t chunk = ceil_div(s.P, cl);
             const int smem = resident_smem(s, width, tensors, static_cast<int>(slab), chunk);
             if (smem > kSmemMost || static_cast<int64_t>(s.N) * (s.G / k) * cl > INT32_MAX) continue;
-            const int per_sm = std::min(2, (224 * 1024) / (smem + 2048));
+            const int per_sm = std::min(3, (224 * 1024) / (smem + 1024));
             const double ctas = static_cast<double>(s.N) * (s.G / k) * cl;
             const double waves = std::ceil(ctas / (148.0 * per_sm));
+            const double busy = std::min<double>(per_sm, ctas / 148.0 / waves);     // CTAs of an SM at a time
             const double bytes = static_cast<double>(chunk) * slab * e * (tensors + 1);
-            const double narrow = slab * e < 128 && k < s.G ? 1.2 : 1.0;
-            const double us = waves * ((per_sm * bytes / 44e3) * narrow * (per_sm == 1 ? 1.3 : 1.0) + 2.5 + (cl > 1 ? 0.5 : 0.0));
+            const double rate = 44e3 * std::min(1.0, (0.1 + 0.3 * std::max(1.0, busy))) * (slab * e < 128 && k < s.G ? 0.85 : 1.0);
+            const double us = waves * (std::max(1.0, busy) * bytes / rate + 2.0 + (cl > 1 ? 0.7 : 0.0));
             if (us < best_us) {
                 best_us = us;
                 best.resident = true; best.slab = static_cast<int>(slab); best.slabs = s.G / k; best.cluster = cl;
@@ -665,17 +877,44 @@ NormPlan plan_one(const NormShape &s, int width, int tensors) {
         }
     }
     if (best.resident) return best;
-    const int cols = std::min(s.C / width, kThreads);
-    best.slab = cols * width;
-    best.slabs = static_cast<int>(ceil_div(s.C, best.slab));
-    // about 64 KB per CTA, at least a few CTAs per SM over the whole tensor
-    const int64_t total = static_cast<int64_t>(s.N) * s.P;
-    int64_t chunk = std::max<int64_t>(1, 65536 / (static_cast<int64_t>(best.slab) * e));
-    chunk = std::min(chunk, std::max<int64_t>(kThreads / cols, ceil_div(total * best.slabs, 148 * 8)));
-    chunk = std::max(chunk, ceil_div(s.P, 4096));      // bounds the partial sums
-    best.chunk = std::min(chunk, s.P);
+    const int most = kThreads * width;                 // channels a CTA covers
+    if (per > most) {                                  // a group is cut into parts (width divides per: see plan_norm)
+        best.parts = static_cast<int>(ceil_div(per, most));
+        best.slab = static_cast<int>(ceil_div(ceil_div(per, best.parts), width) * width);
+        best.parts = static_cast<int>(ceil_div(per, best.slab));
+        best.slabs = s.G * best.parts;
+    } else {
+        int k = most / per;
+        while (k > 1 && (k * per) % width) --k;
+        k = std::min(k, s.G);
+        best.slab = k * per;
+        best.slabs = static_cast<int>(ceil_div(s.G, k));
+    }
+    const int64_t image = s.P * s.C * e * tensors;     // bytes
+    best.run = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(s.N, kRunBytes / image)));
+    // one wave of three CTAs per SM over a run: a last, partly filled wave would cost as much as a full one
+    const int64_t share = 148 * 3 / (static_cast<int64_t>(best.run) * best.slabs);         // CTAs per (image, slab)
+    const int64_t each = std::max<int64_t>(1, share);
+    const int rows = kThreads / (best.slab / width);
+    const int64_t chunk = std::max<int64_t>(ceil_div(s.P, each), rows);
+    best.chunk = std::min(std::max<int64_t>(chunk, ceil_div(s.P, 2048)), s.P);
     best.chunks = static_cast<int>(ceil_div(s.P, best.chunk));
     return best;
+}
+
+// Dynamic shared memory of the two-pass kernels: the rings, and over them the per-thread results.
+template <typename T, int V, int TENSORS> constexpr size_t ring_smem() {
+    using S = Stream<T, V, false, TENSORS>;
+    return static_cast<size_t>(kThreads) * std::max(8 * V, TENSORS * S::kDepth * S::kBatch * S::kBytes);
+}
+
+// A plan needs the vector width to divide the channels, and each group's where a group is wider than a CTA.
+bool width_fits(const NormShape &s, int v) {
+    const int per = s.C / s.G;
+    if (s.C % v) return false;
+    if (per % v == 0) return true;
+    const int64_t together = static_cast<int64_t>(per) * v;    // v groups hold a multiple of v channels
+    return together <= static_cast<int64_t>(kThreads) * v && s.G % v == 0;
 }
 
 // Widest access that the sizes, the strides and the addresses allow.
@@ -683,7 +922,7 @@ int width_index(const NormShape &s, std::initializer_list<const void *> pointers
     const int e = elem_bytes(s.dtype);
     for (int i = 0; i < kNormWidths; ++i) {
         const int v = norm_width(s.dtype, i);
-        bool ok = s.C % v == 0 && s.x_pixel % v == 0 && s.x_image % v == 0;
+        bool ok = width_fits(s, v) && s.x_pixel % v == 0 && s.x_image % v == 0;
         if (y_too) ok = ok && s.y_pixel % v == 0 && s.y_image % v == 0;
         for (const void *p : pointers) ok = ok && reinterpret_cast<uintptr_t>(p) % (static_cast<unsigned>(v) * e) == 0;
         if (ok) return i;
@@ -697,26 +936,26 @@ NormArgs args_of(const NormHandle &h, const NormPlan &p) {
     a.ws = h.ws; a.counters = h.counters;
     a.x_pixel = s.x_pixel; a.x_image = s.x_image; a.y_pixel = s.y_pixel; a.y_image = s.y_image;
     a.P = s.P; a.chunk = p.chunk; a.N = s.N; a.C = s.C; a.G = s.G; a.per = s.C / s.G;
-    a.slab = p.slab; a.slabs = p.slabs; a.cluster = p.cluster; a.chunks = p.chunks; a.act = s.act;
+    a.slab = p.slab; a.slabs = p.slabs; a.cluster = p.cluster; a.chunks = p.chunks; a.parts = p.parts; a.act = s.act;
     a.eps = s.eps;
     a.inv_count = static_cast<float>(1.0 / (static_cast<double>(s.P) * a.per));
     return a;
 }
 
+template <typename T, typename F> cudaError_t by_width(int index, F f) {
+    if (index == 0) return f(T{}, std::integral_constant<int, 16 / sizeof(T)>{});
+    if (index == 1) return f(T{}, std::integral_constant<int, 2>{});
+    return f(T{}, std::integral_constant<int, 1>{});
+}
+// f(type, std::integral_constant<int, V>)
 template <typename F> cudaError_t by_type(int dtype, int index, F f) {
-    if (dtype == PATDNN_F32) {
-        if (index == 0) return f(float{}, std::integral_constant<int, 4>{});
-        if (index == 1) return f(float{}, std::integral_constant<int, 2>{});
-        return f(float{}, std::integral_constant<int, 1>{});
-    }
-    if (dtype == PATDNN_F16) {
-        if (index == 0) return f(__half{}, std::integral_constant<int, 8>{});
-        if (index == 1) return f(__half{}, std::integral_constant<int, 2>{});
-        return f(__half{}, std::integral_constant<int, 1>{});
-    }
-    if (index == 0) return f(__nv_bfloat16{}, std::integral_constant<int, 8>{});
-    if (index == 1) return f(__nv_bfloat16{}, std::integral_constant<int, 2>{});
-    return f(__nv_bfloat16{}, std::integral_constant<int, 1>{});
+    if (dtype == PATDNN_F32) return by_width<float>(index, f);
+    if (dtype == PATDNN_F16) return by_width<__half>(index, f);
+    return by_width<__nv_bfloat16>(index, f);
+}
+
+dim3 resident_grid(const NormShape &s, const NormPlan &p) {
+    return dim3(static_cast<unsigned>(static_cast<int64_t>(s.N) * p.slabs * p.cluster));
 }
 
 }  // namespace
@@ -726,17 +965,20 @@ int norm_width(int dtype, int index) { return index == 0 ? 16 / elem_bytes(dtype
 void plan_norm(NormHandle &h) {
     for (int i = 0; i < kNormWidths; ++i) {
         const int v = norm_width(h.s.dtype, i);
-        if (h.s.C % v) continue;
-        h.fwd[i] = plan_one(h.s, v, 1);
-        h.bwd[i] = plan_one(h.s, v, 2);
+        if (!width_fits(h.s, v)) continue;
+        h.fwd[i] = plan_one(h.s, v, 1, 1);
+        h.mx4[i] = plan_one(h.s, v, 1, 32);
+        h.bwd[i] = plan_one(h.s, v, 2, 1);
     }
 }
 
 size_t norm_workspace_floats(const NormHandle &h) {
     size_t most = 0;
     for (int i = 0; i < kNormWidths; ++i)
-        for (const NormPlan *p : {&h.fwd[i], &h.bwd[i]})
-            most = std::max(most, static_cast<size_t>(h.s.N) * p->chunks * h.s.C * 2 + static_cast<size_t>(h.s.N) * h.s.G * 2);
+        for (const NormPlan *p : {&h.fwd[i], &h.mx4[i], &h.bwd[i]}) {
+            const size_t cells = std::max<size_t>(p->slabs, std::max(h.s.C, h.s.G));
+            most = std::max(most, static_cast<size_t>(h.s.N) * p->chunks * cells * 2 + static_cast<size_t>(h.s.N) * h.s.G * 2);
+        }
     return most;
 }
 
@@ -745,9 +987,18 @@ cudaError_t prepare_norm() {
         for (int i = 0; i < kNormWidths; ++i) {
             const cudaError_t e = by_type(dtype, i, [](auto t, auto v) {
                 using T = decltype(t);
-                cudaError_t r = cudaFuncSetAttribute(norm_resident_kernel<T, v.value>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost);
-                if (r == cudaSuccess)
-                    r = cudaFuncSetAttribute(norm_grad_resident_kernel<T, v.value>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost);
+                const cudaFuncAttribute what = cudaFuncAttributeMaxDynamicSharedMemorySize;
+                cudaError_t r = cudaFuncSetAttribute(norm_moments_kernel<T, v.value>, what, kSmemMost);
+                for (int act = PATDNN_ACT_NONE; act <= PATDNN_ACT_SILU && r == cudaSuccess; ++act)
+                    r = by_act(act, [&](auto c) {
+                        cudaError_t q = cudaFuncSetAttribute(norm_resident_kernel<T, v.value, c.value, false>, what, kSmemMost);
+                        if (q == cudaSuccess) q = cudaFuncSetAttribute(norm_resident_kernel<T, v.value, c.value, true>, what, kSmemMost);
+                        if (q == cudaSuccess) q = cudaFuncSetAttribute(norm_grad_resident_kernel<T, v.value, c.value>, what, kSmemMost);
+                        if (q == cudaSuccess) q = cudaFuncSetAttribute(norm_apply_kernel<T, v.value, c.value>, what, kSmemMost);
+                        if (q == cudaSuccess) q = cudaFuncSetAttribute(norm_grad_sums_kernel<T, v.value, c.value>, what, kSmemMost);
+                        if (q == cudaSuccess) q = cudaFuncSetAttribute(norm_grad_apply_kernel<T, v.value, c.value>, what, kSmemMost);
+                        return q;
+                    });
                 return r;
             });
             if (e != cudaSuccess) return e;
@@ -755,30 +1006,77 @@ cudaError_t prepare_norm() {
     return cudaSuccess;
 }
 
+namespace {
+
+// Two passes over runs of images; after_run(first image, images) launches what reads the statistics.
+template <typename F>
+cudaError_t two_pass(const NormHandle &h, const NormPlan &p, int i, NormArgs a, cudaStream_t st, int *launches, F after_run) {
+    const NormShape &s = h.s;
+    *launches = 0;
+    for (int n0 = 0; n0 < s.N; n0 += p.run) {
+        const int images = std::min(p.run, s.N - n0);
+        a.n0 = n0;
+        const dim3 grid(p.chunks, p.slabs, images);
+        cudaError_t e = by_type(s.dtype, i, [&](auto t, auto v) {
+            return launch_pdl(norm_moments_kernel<decltype(t), v.value>, grid, dim3(kThreads), ring_smem<decltype(t), v.value, 1>(), st, 1, a);
+        });
+        if (e == cudaSuccess) e = launch_pdl(norm_join_kernel, dim3(s.G, images), dim3(kThreads), 0, st, 1, a);
+        if (e == cudaSuccess) e = after_run(a, grid);
+        if (e != cudaSuccess) return e;
+        *launches += 3;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
 cudaError_t launch_group_norm(const NormHandle &h, const void *x, const float *gamma, const float *beta, void *y, float *stats,
                               cudaStream_t st, int *launches) {
     const NormShape &s = h.s;
-    const int i = y ? width_index(s, {x, y}, true) : width_index(s, {x}, false);
+    const int i = width_index(s, {x, y}, true);
     const NormPlan &p = h.fwd[i];
     NormArgs a = args_of(h, p);
     a.x = x; a.y = y; a.gamma = gamma; a.beta = beta; a.stats_out = stats;
     if (p.resident) {
         *launches = 1;
-        const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(s.N) * p.slabs * p.cluster));
         return by_type(s.dtype, i, [&](auto t, auto v) {
-            return launch_pdl(norm_resident_kernel<decltype(t), v.value>, grid, dim3(kThreads), p.smem, st, p.cluster, a);
+            return by_act(s.act, [&](auto c) {
+                return launch_pdl(norm_resident_kernel<decltype(t), v.value, c.value, false>, resident_grid(s, p), dim3(kThreads), p.smem, st, p.cluster, a);
+            });
         });
     }
     if (!stats) stats = h.stats;
     a.stats_out = stats; a.stats_in = stats;
-    *launches = y ? 3 : 2;
-    const dim3 grid(p.chunks, p.slabs, s.N);
-    return by_type(s.dtype, i, [&](auto t, auto v) {
-        using T = decltype(t);
-        cudaError_t e = launch_pdl(norm_moments_kernel<T, v.value>, grid, dim3(kThreads), static_cast<size_t>(kThreads) * v.value * 8, st, 1, a);
-        if (e == cudaSuccess) e = launch_pdl(norm_join_kernel, dim3(s.G, s.N), dim3(kThreads), 0, st, 1, a);
-        if (e == cudaSuccess && y) e = launch_pdl(norm_apply_kernel<T, v.value>, grid, dim3(kThreads), 0, st, 1, a);
-        return e;
+    return two_pass(h, p, i, a, st, launches, [&](const NormArgs &b, dim3 grid) {
+        return by_type(s.dtype, i, [&](auto t, auto v) {
+            return by_act(s.act, [&](auto c) {
+                return launch_pdl(norm_apply_kernel<decltype(t), v.value, c.value>, grid, dim3(kThreads), ring_smem<decltype(t), v.value, 1>(), st, 1, b);
+            });
+        });
+    });
+}
+
+cudaError_t launch_group_norm_mx4(const NormHandle &h, const void *x, const float *gamma, const float *beta, void *mx, float *stats,
+                                  cudaStream_t st, int *launches) {
+    const NormShape &s = h.s;
+    const int i = width_index(s, {x}, false);
+    const NormPlan &p = h.mx4[i];
+    const Mx4Shape m = mx4_shape(s.N * s.P, s.C);
+    NormArgs a = args_of(h, p);
+    a.x = x; a.gamma = gamma; a.beta = beta; a.stats_out = stats;
+    a.mx = static_cast<uint8_t *>(mx); a.mx_scales = m.scales_at; a.mx_width = m.width; a.mx_col_tiles = static_cast<int>(m.col_tiles);
+    if (p.resident) {
+        *launches = 1;
+        return by_type(s.dtype, i, [&](auto t, auto v) {
+            return by_act(s.act, [&](auto c) {
+                return launch_pdl(norm_resident_kernel<decltype(t), v.value, c.value, true>, resident_grid(s, p), dim3(kThreads), p.smem, st, p.cluster, a);
+            });
+        });
+    }
+    if (!stats) stats = h.stats;
+    a.stats_out = stats;
+    return two_pass(h, p, i, a, st, launches, [&](const NormArgs &b, dim3 grid) {
+        return launch_norm_quantize(s, m, x, gamma, beta, stats, b.n0 * s.P, static_cast<int64_t>(grid.z) * s.P, mx, st);
     });
 }
 
@@ -791,20 +1089,30 @@ cudaError_t launch_group_norm_grad(const NormHandle &h, const void *x, const flo
     a.x = x; a.dy = dy; a.y = dx; a.gamma = gamma; a.beta = beta; a.stats_in = stats; a.dgamma = dgamma; a.dbeta = dbeta;
     if (p.resident) {
         *launches = 1;
-        const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(s.N) * p.slabs * p.cluster));
         return by_type(s.dtype, i, [&](auto t, auto v) {
-            return launch_pdl(norm_grad_resident_kernel<decltype(t), v.value>, grid, dim3(kThreads), p.smem, st, p.cluster, a);
+            return by_act(s.act, [&](auto c) {
+                return launch_pdl(norm_grad_resident_kernel<decltype(t), v.value, c.value>, resident_grid(s, p), dim3(kThreads), p.smem, st, p.cluster, a);
+            });
         });
     }
-    *launches = 3;
-    const dim3 grid(p.chunks, p.slabs, s.N);
-    return by_type(s.dtype, i, [&](auto t, auto v) {
-        using T = decltype(t);
-        cudaError_t e = launch_pdl(norm_grad_sums_kernel<T, v.value>, grid, dim3(kThreads), static_cast<size_t>(kThreads) * v.value * 8, st, 1, a);
-        if (e == cudaSuccess) e = launch_pdl(norm_grad_join_kernel, dim3(s.G, s.N), dim3(kThreads), 0, st, 1, a);
-        if (e == cudaSuccess) e = launch_pdl(norm_grad_apply_kernel<T, v.value>, grid, dim3(kThreads), 0, st, 1, a);
-        return e;
-    });
+    *launches = 0;
+    for (int n0 = 0; n0 < s.N; n0 += p.run) {
+        const int images = std::min(p.run, s.N - n0);
+        a.n0 = n0;
+        const dim3 grid(p.chunks, p.slabs, images);
+        const cudaError_t e = by_type(s.dtype, i, [&](auto t, auto v) {
+            return by_act(s.act, [&](auto c) {
+                using T = decltype(t);
+                cudaError_t r = launch_pdl(norm_grad_sums_kernel<T, v.value, c.value>, grid, dim3(kThreads), ring_smem<T, v.value, 2>(), st, 1, a);
+                if (r == cudaSuccess) r = launch_pdl(norm_grad_join_kernel, dim3(s.G, images), dim3(kThreads), 0, st, 1, a);
+                if (r == cudaSuccess) r = launch_pdl(norm_grad_apply_kernel<T, v.value, c.value>, grid, dim3(kThreads), ring_smem<T, v.value, 2>(), st, 1, a);
+                return r;
+            });
+        });
+        if (e != cudaSuccess) return e;
+        *launches += 3;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace patdnn

@@ -11,6 +11,8 @@
 // r + 96 are neighbours in memory (16 bytes): 4 loads in flight per lane, and full 32-byte sectors for the scales.
 #include "ops.hpp"
 
+#include <algorithm>
+
 #include "kernels.hpp"
 #include "ops_device.cuh"
 
@@ -19,163 +21,220 @@ namespace {
 
 constexpr int kWarps = 8;
 
-// The two codes of (lo, hi) in one byte, lo in the lower half; nearest even, magnitudes above 6 become 6.
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    uint32_t r;
-    asm("{\n\t.reg .b8 b;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b, %2, %1;\n\t"
-        "cvt.u32.u8 %0, b;\n\t}" : "=r"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-
-// Scale byte of a block from the bits of its largest magnitude (sign bit clear), and the factor 1 / scale.
-__device__ __forceinline__ uint32_t scale_of(uint32_t amax_bits, float &inverse) {
-    const uint32_t field = amax_bits >> 23;            // biased exponent; 0 for zero and subnormals
-    if (field == 255) {
-        inverse = 0.f;
-        return 255;
-    }
-    const uint32_t byte = field > 2 ? field - 2 : 0;   // biased by 127: 2^(field - 127 - 2), at least 2^-127
-    // 1 / scale = 2^(127 - byte), byte <= 252: exponent field 254 - byte, always normal
-    inverse = __uint_as_float((254 - byte) << 23);
-    return byte;
-}
-
-// Eight values of one lane -> its 4 bytes of codes; returns the block's scale byte (the same in the four lanes of a block).
-__device__ __forceinline__ uint32_t quantise8(const float (&v)[8], uint32_t &codes) {
-    uint32_t top = 0;                                  // magnitudes compare like their bits; a NaN is above infinity
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    float inverse;
-    const uint32_t scale = scale_of(top, inverse);
-    codes = 0;
-    if (scale != 255) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) codes |= pack2(v[2 * j] * inverse, v[2 * j + 1] * inverse) << (8 * j);
-    }
-    return scale;
-}
-
 struct QuantArgs {
     const void *x;
     uint8_t *mx;
-    int64_t rows, cols, ld;
+    int64_t row0, rows, cols, ld;           // rows [row0, rows) of the matrix
     int64_t scales_at;
     int width, col_tiles, code_bytes, scale_bytes;
-    // group norm in front (norm kernels only): row = image * P + pixel
+    // group norm in front (NORM kernels only): row = image * P + pixel
     const float *gamma, *beta, *stats;
     int64_t P, x_image;
     int G, per, act;
 };
 
-// Columns [c, c + 8) of a row; 0 beyond the last column.  A = elements per access.
+// Eight columns of a row as they lie in memory, in 8 / A accesses.
 template <typename T, int A>
-__device__ __forceinline__ void load8(const T *row, int64_t c, int64_t cols, float (&v)[8]) {
-    if (c + 8 <= cols) {
+struct Raw {
+    Vec<T, A> v[8 / A];
+    __device__ __forceinline__ void load(const T *p) {
 #pragma unroll
-        for (int i = 0; i < 8 / A; ++i) {
-            const Vec<T, A> t = *reinterpret_cast<const Vec<T, A> *>(row + c + i * A);
+        for (int i = 0; i < 8 / A; ++i) v[i] = *reinterpret_cast<const Vec<T, A> *>(p + i * A);
+    }
+    __device__ __forceinline__ void load(const T *p, int count) {      // the first `count`, zeros after them
 #pragma unroll
-            for (int j = 0; j < A; ++j) v[i * A + j] = to_float(t.v[j]);
-        }
+        for (int i = 0; i < 8; ++i) v[i / A].v[i % A] = i < count ? p[i] : from_float<T>(0.f);
+    }
+    __device__ __forceinline__ float get(int i) const { return to_float(v[i / A].v[i % A]); }
+};
+
+// Bits of the largest magnitude among a lane's eight columns; two 16-bit values are compared at a time.
+template <typename T, int A> __device__ __forceinline__ uint32_t top_of(const Raw<T, A> &raw) {
+    if constexpr (sizeof(T) == 4) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = raw.get(j);
+        return top8(v);
     } else {
+        uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? to_float(row[c + j]) : 0.f;
+        for (int j = 0; j < 4; ++j) {
+            uint32_t two;
+            if constexpr (A >= 2) two = *reinterpret_cast<const uint32_t *>(&raw.v[2 * j / A].v[2 * j % A]);
+            else two = *reinterpret_cast<const uint16_t *>(&raw.v[2 * j].v[0]) | static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(&raw.v[2 * j + 1].v[0])) << 16;
+            top = __vmaxu2(top, two & 0x7fff7fffu);
+        }
+        const uint16_t one = static_cast<uint16_t>(max(top & 0xffffu, top >> 16));
+        return __float_as_uint(to_float(*reinterpret_cast<const T *>(&one)));
     }
 }
 
-// grid: x = column tiles, y.. = groups of 32 "row sets"; a warp's row set is rows r, r+32, r+64, r+96 of a row tile.
-// blockIdx.x = (row tile * 4 + quarter) * col_tiles + column tile; quarter: row sets 8 * quarter + warp.
-template <typename T, int A, bool NORM>
-__global__ void __launch_bounds__(kWarps * 32) mx4_quantize_kernel(QuantArgs a) {
+// CTAs per SM that the registers of two row sets allow
+template <typename T, int A> __host__ __device__ constexpr int quant_ctas() { return sizeof(T) == 4 || A == 1 ? 3 : 4; }
+
+// A unit is a quarter of a tile: (row tile * 4 + quarter) * col_tiles + column tile, a warp's row set r0 = 8 * quarter + warp being the
+// rows r0, r0 + 32, r0 + 64, r0 + 96 of the row tile.  CTAs walk over the units and load the next one before they quantise the present
+// one, so that loads are always in flight.
+template <typename T, int A>
+__global__ void __launch_bounds__(kWarps * 32, quant_ctas<T, A>()) mx4_quantize_kernel(QuantArgs a, unsigned units) {
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t tile = blockIdx.x;
-    const int ct = static_cast<int>(tile % a.col_tiles);
-    const int64_t rest = tile / a.col_tiles;
-    const int64_t rt = rest >> 2;
-    const int r0 = static_cast<int>(rest & 3) * kWarps + warp;         // first row of the set, 0 .. 31
+    const int row_bytes = a.width / 2;
+    const bool mine = lane * 8 < a.width;              // narrow tiles leave lanes idle
+    auto load = [&](unsigned unit, Raw<T, A> (&raw)[4]) {
+        const int ct = static_cast<int>(unit % static_cast<unsigned>(a.col_tiles));
+        const unsigned rest = unit / static_cast<unsigned>(a.col_tiles);
+        const int64_t row = static_cast<int64_t>(rest >> 2) * 128 + (rest & 3) * kWarps + warp;
+        const int64_t c = static_cast<int64_t>(ct) * a.width + lane * 8;
+        const T *src = static_cast<const T *>(a.x) + row * a.ld + c;
+        if (mine && c + 8 <= a.cols && row + 96 < a.rows) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) raw[k].load(src + 32 * k * a.ld);
+        } else {
+            const int count = mine ? static_cast<int>(max(int64_t(0), min(int64_t(8), a.cols - c))) : 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) raw[k].load(src + 32 * k * a.ld, row + 32 * k < a.rows ? count : 0);
+        }
+    };
+    auto store = [&](unsigned unit, const Raw<T, A> (&raw)[4]) {
+        const int ct = static_cast<int>(unit % static_cast<unsigned>(a.col_tiles));
+        const unsigned rest = unit / static_cast<unsigned>(a.col_tiles);
+        const int64_t rt = rest >> 2;
+        const int r0 = static_cast<int>(rest & 3) * kWarps + warp;
+        uint8_t *codes_out = a.mx + (rt * a.col_tiles + ct) * a.code_bytes;
+        uint8_t *scales_out = a.mx + a.scales_at + (rt * a.col_tiles + ct) * a.scale_bytes;
+        uint32_t sets[4];                              // lane of block b: scale byte of (row r0 + 32 k, b)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = raw[k].get(j);
+            uint32_t codes;
+            sets[k] = quantise8(v, top_of(raw[k]), codes);
+            if (rt * 128 + r0 + 32 * k < a.rows && mine) {
+                int at = (r0 + 32 * k) * row_bytes + lane * 4;
+                at ^= ((at >> 7) & (a.width / 32 - 1)) << 4;
+                *reinterpret_cast<uint32_t *>(codes_out + at) = codes;
+            }
+        }
+        // lanes 0 and 16 gather the scale bytes of blocks 0..3 and 4..7: 16 bytes each
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t w = sets[k];
+            w |= __shfl_down_sync(0xffffffffu, w, 4) << 8;
+            w |= __shfl_down_sync(0xffffffffu, w, 8) << 16;
+            sets[k] = w;
+        }
+        if ((lane & 15) == 0 && mine && rt * 128 + r0 < a.rows)
+            *reinterpret_cast<uint4 *>(scales_out + (lane >> 4) * 512 + r0 * 16) = make_uint4(sets[0], sets[1], sets[2], sets[3]);
+    };
+    pdl_wait();
+    unsigned unit = blockIdx.x;
+    Raw<T, A> now[4], next[4];
+    load(unit, now);
+    while (unit < units) {                             // (the same for all threads of the CTA)
+        const unsigned after = unit + gridDim.x;
+        if (after < units) load(after, next);
+        store(unit, now);
+        unit = after;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) now[k] = next[k];
+    }
+}
+
+// A group norm in front: blockIdx.x = row tile * col_tiles + column tile.  A warp takes four of the 32 row sets of a row tile, for which
+// the constants of its columns are loaded once per image.
+template <typename T, int A>
+__global__ void __launch_bounds__(kWarps * 32) norm_quantize_kernel(QuantArgs a) {
+    constexpr int kSets = 4, kParts = 32 / (kWarps * kSets);
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int ct = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.col_tiles));
+    const unsigned rest = blockIdx.x / static_cast<unsigned>(a.col_tiles);
+    const int64_t rt = a.row0 / 128 + rest / kParts;
     const int64_t c = static_cast<int64_t>(ct) * a.width + lane * 8;
-    const int tile_row = a.width / 2;                                  // bytes of a row of the code tile
+    const int row_bytes = a.width / 2;
     uint8_t *codes_out = a.mx + (rt * a.col_tiles + ct) * a.code_bytes;
     uint8_t *scales_out = a.mx + a.scales_at + (rt * a.col_tiles + ct) * a.scale_bytes;
+    const int count = lane * 8 < a.width ? static_cast<int>(max(int64_t(0), min(int64_t(8), a.cols - c))) : 0;
     pdl_wait();
-    if (rt * 128 + r0 >= a.rows) return;                               // warp-uniform; higher rows of the set do not exist either
-    const bool mine = lane * 8 < a.width;                              // narrow tiles leave lanes idle
-    float v[4][8];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int64_t row = rt * 128 + r0 + 32 * k;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[k][j] = 0.f;
-        if (row < a.rows && mine) {
-            const T *src = static_cast<const T *>(a.x);
-            if constexpr (NORM) src += (row / a.P) * a.x_image + (row % a.P) * a.ld;
-            else src += row * a.ld;
-            load8<T, A>(src, c, a.cols, v[k]);
-        }
-    }
-    if constexpr (NORM) {
-        float gm[8], bt[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bool in = mine && c + j < a.cols;
-            gm[j] = in ? a.gamma[c + j] : 0.f;
-            bt[j] = in ? a.beta[c + j] : 0.f;
-        }
+    float mean[8], scale[8], beta[8];                                  // of image `image`
+    int image = -1;
+    for (int set = 0; set < kSets; ++set) {
+        const int r0 = static_cast<int>(rest % kParts) * kWarps * kSets + set * kWarps + warp;
+        if (rt * 128 + r0 >= a.rows) return;                           // warp-uniform; higher rows of the set do not exist either
+        Raw<T, A> raw[4];
+        bool on[4];
+        int at_image[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int64_t row = rt * 128 + r0 + 32 * k;
-            if (row >= a.rows) continue;
-            const float2 *st = reinterpret_cast<const float2 *>(a.stats) + (row / a.P) * a.G;
+            on[k] = row >= a.row0 && row < a.rows;
+            const T *src = static_cast<const T *>(a.x) + c;
+            at_image[k] = static_cast<int>(static_cast<uint32_t>(row) / static_cast<uint32_t>(a.P));
+            src += at_image[k] * a.x_image + (row - at_image[k] * a.P) * a.ld;
+            if (on[k] && count == 8) raw[k].load(src);
+            else raw[k].load(src, on[k] ? count : 0);
+        }
+        uint32_t sets[4];                                              // lane of block b: scale byte of (row r0 + 32 k, b)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (!mine || c + j >= a.cols) continue;
-                const float2 f = st[(c + j) / a.per];
-                v[k][j] = activate(fmaf(v[k][j] - f.x, f.y * gm[j], bt[j]), a.act);
+        for (int k = 0; k < 4; ++k) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = raw[k].get(j);
+            if (on[k] && at_image[k] != image) {                   // warp-uniform
+                image = at_image[k];
+                const float2 *st = reinterpret_cast<const float2 *>(a.stats) + static_cast<int64_t>(image) * a.G;
+                int g = static_cast<int>(c) / a.per, left = a.per - static_cast<int>(c) % a.per;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool in = j < count;
+                    const float2 f = in ? st[g] : make_float2(0.f, 0.f);
+                    mean[j] = f.x;
+                    scale[j] = in ? f.y * a.gamma[c + j] : 0.f;
+                    beta[j] = in ? a.beta[c + j] : 0.f;
+                    if (--left == 0) { ++g; left = a.per; }
+                }
+            }
+            if (on[k]) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = j < count ? activate(fmaf(v[j] - mean[j], scale[j], beta[j]), a.act) : 0.f;
+            }
+            uint32_t codes;
+            sets[k] = quantise8(v, codes);
+            if (on[k] && lane * 8 < a.width) {
+                int at = (r0 + 32 * k) * row_bytes + lane * 4;
+                at ^= ((at >> 7) & (a.width / 32 - 1)) << 4;
+                *reinterpret_cast<uint32_t *>(codes_out + at) = codes;
+            }
+        }
+        // lanes 0 and 16 gather the scale bytes of blocks 0..3 and 4..7: 16 bytes each
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t w = sets[k];
+            w |= __shfl_down_sync(0xffffffffu, w, 4) << 8;
+            w |= __shfl_down_sync(0xffffffffu, w, 8) << 16;
+            sets[k] = w;
+        }
+        if ((lane & 15) == 0 && lane * 8 < a.width) {
+            uint32_t *to = reinterpret_cast<uint32_t *>(scales_out + (lane >> 4) * 512 + r0 * 16);
+            if (on[0] && on[1] && on[2] && on[3]) {
+                *reinterpret_cast<uint4 *>(to) = make_uint4(sets[0], sets[1], sets[2], sets[3]);
+            } else {                                                   // other rows of the set belong to another launch
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (on[k]) to[k] = sets[k];
             }
         }
     }
-    uint32_t sets[4];                                                  // lane of block b: byte of (row r0 + 32 k, b) in bits 0..7 of sets[k]
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        uint32_t codes;
-        sets[k] = quantise8(v[k], codes);
-        if (rt * 128 + r0 + 32 * k < a.rows && mine) {
-            int at = (r0 + 32 * k) * tile_row + lane * 4;
-            at ^= ((at >> 7) & (a.width / 32 - 1)) << 4;
-            *reinterpret_cast<uint32_t *>(codes_out + at) = codes;
-        }
-    }
-    // lanes 0 and 16 gather the scale bytes of blocks 0..3 and 4..7: 16 bytes each
-    uint32_t word[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        uint32_t w = sets[k];
-        w |= __shfl_down_sync(0xffffffffu, w, 4) << 8;
-        w |= __shfl_down_sync(0xffffffffu, w, 8) << 16;
-        word[k] = w;
-    }
-    if ((lane & 15) == 0 && lane * 8 < a.width)
-        *reinterpret_cast<uint4 *>(scales_out + (lane >> 4) * 512 + r0 * 16) = make_uint4(word[0], word[1], word[2], word[3]);
-}
-
-__device__ __forceinline__ float value_of(uint32_t code, float scale) {
-    // magnitudes of the codes 0..7 as 2 * value: 0 1 2 3 4 6 8 12
-    const uint32_t e = (code >> 1) & 3, m = code & 1;
-    const float mag = e == 0 ? 0.5f * static_cast<float>(m) : static_cast<float>((2 + m) << (e - 1)) * 0.5f;
-    return (code & 8 ? -mag : mag) * scale;
 }
 
 template <typename T, int A>
 __global__ void __launch_bounds__(kWarps * 32) mx4_dequantize_kernel(QuantArgs a, T *out) {
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t tile = blockIdx.x;
-    const int ct = static_cast<int>(tile % a.col_tiles);
-    const int64_t rest = tile / a.col_tiles;
+    const int ct = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.col_tiles));
+    const unsigned rest = blockIdx.x / static_cast<unsigned>(a.col_tiles);
     const int64_t rt = rest >> 2;
     const int r0 = static_cast<int>(rest & 3) * kWarps + warp;
     const int64_t c = static_cast<int64_t>(ct) * a.width + lane * 8;
@@ -199,9 +258,15 @@ __global__ void __launch_bounds__(kWarps * 32) mx4_dequantize_kernel(QuantArgs a
         if (row >= a.rows) continue;
         // 2^(byte - 127): byte 0 is the subnormal 2^-127, 255 is NaN
         const float s = scale[k] == 255 ? __uint_as_float(0x7fffffffu) : scale[k] ? __uint_as_float(scale[k] << 23) : __uint_as_float(0x00400000u);
+        __half2 h[4];
+        unpack8(codes[k], h);
         float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = value_of((codes[k] >> (4 * j)) & 15, s);
+        for (int j = 0; j < 4; ++j) {
+            const float2 f = __half22float2(h[j]);
+            v[2 * j] = f.x * s;
+            v[2 * j + 1] = f.y * s;
+        }
         T *dst = out + row * a.ld;
         if (c + 8 <= a.cols) {
 #pragma unroll
@@ -222,14 +287,14 @@ __global__ void __launch_bounds__(kWarps * 32) mx4_dequantize_kernel(QuantArgs a
 QuantArgs quant_args(const Mx4Shape &m, const void *x, int64_t ld, void *mx) {
     QuantArgs a{};
     a.x = x; a.mx = static_cast<uint8_t *>(mx);
-    a.rows = m.rows; a.cols = m.cols; a.ld = ld;
+    a.row0 = 0; a.rows = m.rows; a.cols = m.cols; a.ld = ld;
     a.scales_at = m.scales_at; a.width = m.width; a.col_tiles = static_cast<int>(m.col_tiles);
     a.code_bytes = m.code_bytes; a.scale_bytes = m.scale_bytes;
     a.P = 1; a.G = 1; a.per = 1;
     return a;
 }
 
-unsigned quant_grid(const Mx4Shape &m) {               // no CTA for quarters without rows in the last row tile
+unsigned quant_grid(const Mx4Shape &m) {               // no CTA for quarters of the last row tile that have no rows
     const int64_t last = m.rows - (m.row_tiles - 1) * 128;
     const int64_t quarters = (m.row_tiles - 1) * 4 + (last >= 32 ? 4 : ceil_div(last, kWarps));
     return static_cast<unsigned>(quarters * m.col_tiles);
@@ -255,18 +320,22 @@ template <typename F> cudaError_t by_access(int dtype, int i, F f) {
 
 cudaError_t launch_mx4_quantize(const Mx4Shape &m, const void *x, int dtype, int64_t ld, void *mx, cudaStream_t st) {
     const QuantArgs a = quant_args(m, x, ld, mx);
+    const unsigned units = quant_grid(m);
     return by_access(dtype, access_index(dtype, x, ld), [&](auto t, auto v) {
-        return launch_pdl(mx4_quantize_kernel<decltype(t), v.value, false>, dim3(quant_grid(m)), dim3(kWarps * 32), 0, st, 1, a);
+        const unsigned grid = std::min(units, static_cast<unsigned>(sm_count() * quant_ctas<decltype(t), v.value>()));
+        return launch_pdl(mx4_quantize_kernel<decltype(t), v.value>, dim3(grid), dim3(kWarps * 32), 0, st, 1, a, units);
     });
 }
 
 cudaError_t launch_norm_quantize(const NormShape &s, const Mx4Shape &m, const void *x, const float *gamma, const float *beta,
-                                 const float *stats, void *mx, cudaStream_t st) {
+                                 const float *stats, int64_t row0, int64_t rows, void *mx, cudaStream_t st) {
     QuantArgs a = quant_args(m, x, s.x_pixel, mx);
+    a.row0 = row0; a.rows = row0 + rows;
     a.gamma = gamma; a.beta = beta; a.stats = stats;
     a.P = s.P; a.x_image = s.x_image; a.G = s.G; a.per = s.C / s.G; a.act = s.act;
+    const int64_t tiles = ceil_div(a.rows, 128) - row0 / 128;
     return by_access(s.dtype, access_index(s.dtype, x, s.x_pixel, s.x_image), [&](auto t, auto v) {
-        return launch_pdl(mx4_quantize_kernel<decltype(t), v.value, true>, dim3(quant_grid(m)), dim3(kWarps * 32), 0, st, 1, a);
+        return launch_pdl(norm_quantize_kernel<decltype(t), v.value>, dim3(static_cast<unsigned>(tiles * m.col_tiles)), dim3(kWarps * 32), 0, st, 1, a);
     });
 }
 

@@ -25,24 +25,29 @@ struct NormPlan {
     int slab = 0, slabs = 0;                // channels per slab (whole groups when resident), slabs = ceil(C / slab)
     int cluster = 1;                        // resident: CTAs that share one (image, slab)
     int chunks = 1;                         // two passes: pixel chunks per image
+    int parts = 1;                          // two passes: slabs that share a group wider than a CTA
+    int run = 1;                            // two passes: images taken together
     int64_t chunk = 0;                      // pixels per CTA
     int smem = 0;                           // resident: dynamic shared memory
 };
-constexpr int kNormWidths = 3;              // vector widths a handle is planned for: 16 bytes, two elements, one element
+constexpr int kNormWidths = 3;              // a handle is planned for accesses of 16 bytes, 2 elements and 1 element
 struct NormHandle {
     NormShape s{};
-    NormPlan fwd[kNormWidths], bwd[kNormWidths];
+    NormPlan fwd[kNormWidths], mx4[kNormWidths], bwd[kNormWidths];
     float *ws = nullptr;                    // partial sums of the two-pass forms and of the gradient
-    unsigned *counters = nullptr;           // arrivals per channel slab (gradient); zero between calls
+    unsigned *counters = nullptr;           // [max(N, G)] arrivals per image or channel slab; zero between calls
     float *stats = nullptr;                 // [N][G][2] where the caller keeps none
 };
 int norm_width(int dtype, int index);       // elements per access for width index 0 .. 2
 void plan_norm(NormHandle &h);
 size_t norm_workspace_floats(const NormHandle &h);
 cudaError_t prepare_norm();                 // opt in to the dynamic shared memory
-// y == nullptr: statistics only
+// stats may be nullptr
 cudaError_t launch_group_norm(const NormHandle &h, const void *x, const float *gamma, const float *beta, void *y, float *stats,
                               cudaStream_t st, int *launches);
+// the same as rows of a 4-bit matrix (image * P + pixel)
+cudaError_t launch_group_norm_mx4(const NormHandle &h, const void *x, const float *gamma, const float *beta, void *mx, float *stats,
+                                  cudaStream_t st, int *launches);
 cudaError_t launch_group_norm_grad(const NormHandle &h, const void *x, const float *gamma, const float *beta, const float *stats,
                                    const void *dy, void *dx, float *dgamma, float *dbeta, cudaStream_t st, int *launches);
 
@@ -73,9 +78,9 @@ inline Mx4Shape mx4_shape(int64_t rows, int64_t cols) {
 }
 cudaError_t launch_mx4_quantize(const Mx4Shape &m, const void *x, int dtype, int64_t ld, void *mx, cudaStream_t st);
 cudaError_t launch_mx4_dequantize(const Mx4Shape &m, const void *mx, void *out, int dtype, int64_t ld, cudaStream_t st);
-// act((x - mean) * rstd * gamma + beta) of every pixel, quantised: row = image * P + pixel
+// act((x - mean) * rstd * gamma + beta) of the pixels of rows [row0, row0 + rows), row = image * P + pixel; m: the whole matrix
 cudaError_t launch_norm_quantize(const NormShape &s, const Mx4Shape &m, const void *x, const float *gamma, const float *beta,
-                                 const float *stats, void *mx, cudaStream_t st);
+                                 const float *stats, int64_t row0, int64_t rows, void *mx, cudaStream_t st);
 
 // ---- 4-bit product (mx4_linear.cu) ------------------------------------------------------------------------------------
 struct Mx4Params {

@@ -105,9 +105,10 @@ int patdnn_norm_create(const patdnn_norm_desc *desc, patdnn_norm *out) {
     h->h.s = s;
     if (s.N > 0) {
         plan_norm(h->h);
+        const size_t counters = static_cast<size_t>(s.N > s.G ? s.N : s.G);
         cudaError_t e = allocate(&h->h.ws, norm_workspace_floats(h->h));
-        if (e == cudaSuccess) e = allocate(&h->h.counters, static_cast<size_t>(s.G));
-        if (e == cudaSuccess) e = cudaMemset(h->h.counters, 0, sizeof(unsigned) * s.G);
+        if (e == cudaSuccess) e = allocate(&h->h.counters, counters);
+        if (e == cudaSuccess) e = cudaMemset(h->h.counters, 0, sizeof(unsigned) * counters);
         if (e == cudaSuccess) e = allocate(&h->h.stats, static_cast<size_t>(s.N) * s.G * 2);
         if (e == cudaSuccess) e = prepare_norm();
         if (e == cudaSuccess) e = cudaDeviceSynchronize();              // the counters are zero on every stream from here on
@@ -137,11 +138,9 @@ int patdnn_norm_run_mx4(patdnn_norm h, const void *x, const float *gamma, const 
     if (!x || !gamma || !beta || !mx) return PATDNN_E_NULL;
     if (!aligned(mx, 16) || !mx_size_ok(s.N * s.P, s.C)) return PATDNN_E_SHAPE;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (!stats) stats = h->h.stats;
     int n = 0;
-    cudaError_t e = launch_group_norm(h->h, x, gamma, beta, nullptr, stats, st, &n);
-    if (e == cudaSuccess) e = launch_norm_quantize(s, mx4_shape(s.N * s.P, s.C), x, gamma, beta, stats, mx, st);
-    return launched(e, n + 1, "group norm launch");
+    const cudaError_t e = launch_group_norm_mx4(h->h, x, gamma, beta, mx, stats, st, &n);
+    return launched(e, n, "group norm launch");
 }
 
 int patdnn_norm_grad(patdnn_norm h, const void *x, const float *gamma, const float *beta, const float *stats, const void *dy, void *dx,

@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/patdnn.h"
 
@@ -25,21 +26,260 @@ struct alignas(sizeof(T) * V) Vec {
     T v[V];
 };
 
-// 1 / (1 + exp(-z)): exp(-z) overflows to infinity for z < -88, where the quotient is 0, its limit in fp32.
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+// The same as 32-bit words (a single 16-bit element sits in the lower half), for code that takes the elements out by shifts.
+template <typename T, int V>
+struct Pack {
+    static constexpr int kBytes = sizeof(T) * V;
+    uint32_t w[kBytes < 4 ? 1 : kBytes / 4];
+    __device__ __forceinline__ void load(const T *p) {
+        if constexpr (kBytes == 16) { const uint4 t = *reinterpret_cast<const uint4 *>(p); w[0] = t.x; w[1] = t.y; w[2] = t.z; w[3] = t.w; }
+        else if constexpr (kBytes == 8) { const uint2 t = *reinterpret_cast<const uint2 *>(p); w[0] = t.x; w[1] = t.y; }
+        else if constexpr (kBytes == 4) w[0] = *reinterpret_cast<const uint32_t *>(p);
+        else w[0] = *reinterpret_cast<const uint16_t *>(p);
+    }
+    __device__ __forceinline__ void load_shared(uint32_t addr) {       // address as in PTX
+        if constexpr (kBytes == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
+        else if constexpr (kBytes == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr) : "memory");
+        else if constexpr (kBytes == 4) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(addr) : "memory");
+        else {
+            uint16_t t;
+            asm volatile("ld.shared.b16 %0, [%1];" : "=h"(t) : "r"(addr) : "memory");
+            w[0] = t;
+        }
+    }
+    __device__ __forceinline__ void store(T *p) const {
+        if constexpr (kBytes == 16) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        else if constexpr (kBytes == 8) *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+        else if constexpr (kBytes == 4) *reinterpret_cast<uint32_t *>(p) = w[0];
+        else *reinterpret_cast<uint16_t *>(p) = static_cast<uint16_t>(w[0]);
+    }
+};
+
+// V fp32 values.  Pairs are held in 64-bit registers and go through the packed instructions (one issue slot for two results, each
+// rounded as alone).
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 split(uint64_t p) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
+    return r;
+}
+template <int V>
+struct Fv {
+    uint64_t p[V / 2];
+    __device__ __forceinline__ static Fv all(float x) {
+        Fv r;
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) r.p[j] = pair_of(x, x);
+        return r;
+    }
+    template <typename F> __device__ __forceinline__ static Fv make(F f) {      // f(j) for j = 0 .. V-1
+        Fv r;
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) r.p[j] = pair_of(f(2 * j), f(2 * j + 1));
+        return r;
+    }
+    __device__ __forceinline__ float get(int j) const { return j & 1 ? split(p[j / 2]).y : split(p[j / 2]).x; }
+    template <typename F> __device__ __forceinline__ Fv map(F f) const {
+        Fv r;
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) {
+            const float2 t = split(p[j]);
+            r.p[j] = pair_of(f(t.x), f(t.y));
+        }
+        return r;
+    }
+};
+template <>
+struct Fv<1> {
+    float p[1];
+    __device__ __forceinline__ static Fv all(float x) { return Fv{{x}}; }
+    template <typename F> __device__ __forceinline__ static Fv make(F f) { return Fv{{f(0)}}; }
+    __device__ __forceinline__ float get(int) const { return p[0]; }
+    template <typename F> __device__ __forceinline__ Fv map(F f) const { return Fv{{f(p[0])}}; }
+};
+__device__ __forceinline__ float fma_(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ float add_(float a, float b) { return a + b; }
+__device__ __forceinline__ float mul_(float a, float b) { return a * b; }
+__device__ __forceinline__ uint64_t fma_(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul_(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+template <int V> __device__ __forceinline__ Fv<V> fma(const Fv<V> &a, const Fv<V> &b, const Fv<V> &c) {
+    Fv<V> r;
+#pragma unroll
+    for (int j = 0; j < (V + 1) / 2; ++j) r.p[j] = fma_(a.p[j], b.p[j], c.p[j]);
+    return r;
+}
+template <int V> __device__ __forceinline__ Fv<V> operator+(const Fv<V> &a, const Fv<V> &b) {
+    Fv<V> r;
+#pragma unroll
+    for (int j = 0; j < (V + 1) / 2; ++j) r.p[j] = add_(a.p[j], b.p[j]);
+    return r;
+}
+template <int V> __device__ __forceinline__ Fv<V> operator*(const Fv<V> &a, const Fv<V> &b) {
+    Fv<V> r;
+#pragma unroll
+    for (int j = 0; j < (V + 1) / 2; ++j) r.p[j] = mul_(a.p[j], b.p[j]);
+    return r;
+}
+template <typename T, int V> __device__ __forceinline__ Fv<V> widen(const Pack<T, V> &x) {
+    Fv<V> r;
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (V == 1) r.p[0] = __uint_as_float(x.w[0]);
+        else
+#pragma unroll
+            for (int j = 0; j < V / 2; ++j) r.p[j] = pair_of(__uint_as_float(x.w[2 * j]), __uint_as_float(x.w[2 * j + 1]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < (V + 1) / 2; ++j) {
+            float lo, hi;
+            if constexpr (std::is_same<T, __half>::value) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&x.w[j]));
+                lo = f.x; hi = f.y;
+            } else {                                   // bfloat16 is the upper half of a float
+                lo = __uint_as_float(x.w[j] << 16);
+                hi = __uint_as_float(x.w[j] & 0xffff0000u);
+            }
+            if constexpr (V == 1) r.p[0] = lo;
+            else r.p[j] = pair_of(lo, hi);
+        }
+    }
+    return r;
+}
+template <typename T, int V> __device__ __forceinline__ Pack<T, V> narrow(const Fv<V> &x) {
+    Pack<T, V> r;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.w[j] = __float_as_uint(x.get(j));
+    } else {
+#pragma unroll
+        for (int j = 0; j < (V + 1) / 2; ++j) {
+            const float2 f = make_float2(x.get(2 * j), V == 1 ? 0.f : x.get(2 * j + 1));
+            if constexpr (std::is_same<T, __half>::value) {
+                const __half2 h = __floats2half2_rn(f.x, f.y);
+                r.w[j] = *reinterpret_cast<const uint32_t *>(&h);
+            } else {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+                r.w[j] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+        }
+    }
+    return r;
+}
+
+// 1 / (1 + exp(-z)).  2^x and the reciprocal are the hardware's approximations (2 ulp, tiny results flushed to zero): 2^x overflows to
+// infinity for z < -88, whose reciprocal is 0, the limit.
+__device__ __forceinline__ float sigmoid(float z) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    return r;
+}
+template <int ACT, int V> __device__ __forceinline__ Fv<V> activate(const Fv<V> &z) {
+    if constexpr (ACT == PATDNN_ACT_RELU) return z.map([](float v) { return v < 0.f ? 0.f : v; });      // NaN stays NaN
+    else if constexpr (ACT == PATDNN_ACT_SILU) return z * z.map([](float v) { return sigmoid(v); });
+    else return z;
+}
+// g * act'(z); ReLU has slope 0 at z = 0 and passes a NaN of z on
+template <int ACT, int V> __device__ __forceinline__ Fv<V> through(const Fv<V> &g, const Fv<V> &z) {
+    if constexpr (ACT == PATDNN_ACT_RELU) {
+        return Fv<V>::make([&](int j) { return z.get(j) > 0.f ? g.get(j) : (z.get(j) <= 0.f ? 0.f : z.get(j)); });
+    } else if constexpr (ACT == PATDNN_ACT_SILU) {     // s (1 + z (1 - s)) = s + (z s) (1 - s)
+        const Fv<V> s = z.map([](float v) { return sigmoid(v); });
+        return g * fma(z * s, fma(s, Fv<V>::all(-1.f), Fv<V>::all(1.f)), s);
+    } else {
+        return g;
+    }
+}
 __device__ __forceinline__ float activate(float z, int act) {
-    if (act == PATDNN_ACT_RELU) return z < 0.f ? 0.f : z;          // NaN stays NaN
+    if (act == PATDNN_ACT_RELU) return z < 0.f ? 0.f : z;
     if (act == PATDNN_ACT_SILU) return z * sigmoid(z);
     return z;
 }
-// d act / d z; ReLU has slope 0 at z = 0
-__device__ __forceinline__ float activate_slope(float z, int act) {
-    if (act == PATDNN_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
-    if (act == PATDNN_ACT_SILU) {
-        const float s = sigmoid(z);
-        return s * fmaf(z, 1.f - s, 1.f);
+// f(std::integral_constant<int, ACT>)
+template <typename F> cudaError_t by_act(int act, F f) {
+    if (act == PATDNN_ACT_RELU) return f(std::integral_constant<int, PATDNN_ACT_RELU>{});
+    if (act == PATDNN_ACT_SILU) return f(std::integral_constant<int, PATDNN_ACT_SILU>{});
+    return f(std::integral_constant<int, PATDNN_ACT_NONE>{});
+}
+
+// The codes of eight values, the first in the lowest four bits; nearest even, magnitudes above 6 become 6.
+__device__ __forceinline__ uint32_t pack8(const float (&v)[8], float factor) {
+    uint32_t r;
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+        "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
+        : "=r"(r)
+        : "f"(v[0] * factor), "f"(v[1] * factor), "f"(v[2] * factor), "f"(v[3] * factor), "f"(v[4] * factor), "f"(v[5] * factor),
+          "f"(v[6] * factor), "f"(v[7] * factor));
+    return r;
+}
+// The eight values that such a word stands for, before scaling (exact in half).
+__device__ __forceinline__ void unpack8(uint32_t codes, __half2 (&h)[4]) {
+    uint32_t r[4];
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+        "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(codes));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = *reinterpret_cast<__half2 *>(&r[i]);
+}
+
+// Scale byte of a block from the bits of its largest magnitude (sign bit clear), and the factor 1 / scale.
+__device__ __forceinline__ uint32_t scale_of(uint32_t amax_bits, float &inverse) {
+    const uint32_t field = amax_bits >> 23;            // biased exponent; 0 for zero and subnormals
+    if (field == 255) {
+        inverse = 0.f;
+        return 255;
     }
-    return 1.f;
+    const uint32_t byte = field > 2 ? field - 2 : 0;   // biased by 127: 2^(field - 127 - 2), at least 2^-127
+    // 1 / scale = 2^(127 - byte), byte <= 252: exponent field 254 - byte, always normal
+    inverse = __uint_as_float((254 - byte) << 23);
+    return byte;
+}
+
+// Bits of the largest magnitude of eight values; a NaN among them gives a NaN.
+__device__ __forceinline__ uint32_t top8(const float (&v)[8]) {
+    float m;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(v[0]), "f"(v[1]), "f"(v[2]));
+    asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(v[3]), "f"(v[4]));
+    asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(v[5]), "f"(v[6]));
+    asm("max.NaN.abs.f32 %0, %0, %1, %1;" : "+f"(m) : "f"(v[7]));
+    return __float_as_uint(m) & 0x7fffffffu;
+}
+// Eight values of one lane -> its 4 bytes of codes; returns the block's scale byte (the same in the four lanes of a block).
+// `top`: bits of the lane's largest magnitude, sign clear (magnitudes compare like their bits, a NaN is above infinity).
+__device__ __forceinline__ uint32_t quantise8(const float (&v)[8], uint32_t top, uint32_t &codes) {
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    float inverse;
+    const uint32_t scale = scale_of(top, inverse);
+    codes = pack8(v, inverse);                         // a block that is not finite: any codes, its scale is NaN
+    return scale;
+}
+__device__ __forceinline__ uint32_t quantise8(const float (&v)[8], uint32_t &codes) {
+    return quantise8(v, top8(v), codes);
 }
 
 }  // namespace
