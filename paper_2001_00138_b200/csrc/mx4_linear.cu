@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
 
     const int row_bytes = p.width / 2;
     const int atoms = p.width > 128 ? 2 : 1;                             // scale atoms (128 columns each) per column tile
-    const int wide = p.tile_n > 128 ? 2 : 1;                             // row tiles of x that the tile spans
+    const int wide = 1;
     const uint32_t a_codes = 128 * row_bytes, b_codes = p.tile_n * row_bytes, sf_bytes = 512 * atoms;
     const uint32_t stage_bytes = (a_codes + b_codes + sf_bytes * (1 + wide) + 1023) & ~1023u;
     const int tmem_cols = wide == 2 ? 512 : 256, sf_base = wide == 2 ? 256 : 128, sf_cols = 8 + 8 * wide;
@@ -217,26 +217,267 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
     if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols));
 }
 
+// ---- many rows ----------------------------------------------------------------------------------------------------------
+// Tiles of 128 rows of x (M) by up to 256 rows of w (N), one persistent CTA per SM walking over them.  Warp 0 fills a ring of column
+// tiles, warp 1 issues the MMAs, warps 4 to 11 are the epilogue: they move the finished accumulator to registers, hand tensor memory back,
+// and convert and store while the next tile is multiplied.  A lane owns a row of y; 64-byte pieces of 32 rows pass through shared
+// memory so that they are stored as whole sectors, four lanes to a row.
+constexpr int kRowsThreads = 384;
+constexpr int kEpilogueWarps = 8;
+constexpr int kStageOut = 2048;                        // bytes an epilogue warp passes through shared memory at a time
+
+__device__ __forceinline__ void tmem_ld32_async(uint32_t addr, uint32_t *v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+          "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+          "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(addr) : "memory");
+}
+
+// One warp: 32 rows by 32 columns (16-bit types) or 16 columns (fp32) = 64 bytes a row, from registers to y.
+template <typename T>
+__device__ __forceinline__ void store_piece(const float (&v)[64 / sizeof(T)], unsigned char *stage, T *y, int64_t ldy, int64_t rows_left, int cols_left, bool vector) {
+    const int lane = threadIdx.x & 31;
+    constexpr int kCols = 64 / sizeof(T);
+    uint32_t w[16];
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(v[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            if constexpr (std::is_same<T, __half>::value) {
+                const __half2 h = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+                w[j] = *reinterpret_cast<const uint32_t *>(&h);
+            } else {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+                w[j] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+        }
+    }
+    // 16-byte unit q of row r sits at unit q ^ ((r >> 1) & 3): eight lanes of a store, and of a load, touch all banks once
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<uint4 *>(stage + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+    __syncwarp();
+    if (vector && cols_left >= kCols) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = i * 8 + (lane >> 2), q = lane & 3;
+            const uint4 t = *reinterpret_cast<const uint4 *>(stage + r * 64 + ((q ^ ((r >> 1) & 3)) << 4));
+            if (r < rows_left) *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(y + r * ldy) + q * 16) = t;
+        }
+    } else {
+        const int rows = static_cast<int>(rows_left < 32 ? rows_left : 32);
+        for (int i = lane; i < rows * kCols; i += 32) {
+            const int r = i / kCols, c = i % kCols, b = c * static_cast<int>(sizeof(T));
+            if (c < cols_left) y[r * ldy + c] = *reinterpret_cast<const T *>(stage + r * 64 + (((b >> 4) ^ ((r >> 1) & 3)) << 4) + (b & 15));
+        }
+    }
+}
+
+template <typename T, int ACT>
+__global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) {
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 2];
+    __shared__ uint32_t tmem_slot;
+    pdl_trigger();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const WaitCtx ctx{p.status, p.spin_limit ? p.spin_limit : kSpinLimit};
+    const uint32_t smem = (smem_u32(smem_raw) + 1023) & ~1023u;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * kMaxStages, done = empty + 8 * kMaxStages, drained = done + 8;
+
+    const int row_bytes = p.width / 2;
+    const int atoms = p.width > 128 ? 2 : 1;                             // scale atoms (128 columns each) per column tile
+    const int wide = p.tile_n / 128;                                     // row tiles of w per tile: 1 or 2
+    const uint32_t codes = 128 * row_bytes, sf_bytes = 512 * atoms;      // of one row tile
+    const uint32_t stage_bytes = ((1 + wide) * (codes + sf_bytes) + 1023) & ~1023u;
+    const int sf_base = p.tile_n, sf_cols = 8 + 8 * wide;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        mbar_init(done, 1);
+        mbar_init(drained, kEpilogueWarps);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const int64_t tiles = static_cast<int64_t>(p.f_tiles) * p.n_tiles;   // f_tiles of tile_n outputs, n_tiles of 128 rows
+    const int w_tiles = (p.F + 127) / 128;
+
+    if (warp == 0 && lane == 0) {
+        int issued = 0;
+        bool ok = true, waited = false;
+        for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+            const int ft = static_cast<int>(t % p.f_tiles);
+            const int64_t nt = t / p.f_tiles;
+            const int b_tiles = min(wide, w_tiles - ft * wide);
+            const uint32_t bytes = (1 + b_tiles) * (codes + sf_bytes);
+            for (int i = 0; i < p.col_tiles; ++i, ++issued) {
+                const int s = issued % p.stages;
+                if (issued >= p.stages && !mbar_wait(empty + 8 * s, (issued / p.stages - 1) & 1, ctx, 111)) { ok = false; break; }
+                const uint32_t at = smem + s * stage_bytes, bar = full + 8 * s;
+                const uint32_t sf = at + (1 + wide) * codes;
+                mbar_expect_tx(bar, bytes);
+                for (int b = 0; b < b_tiles; ++b) {
+                    const int64_t tile = static_cast<int64_t>(ft * wide + b) * p.col_tiles + i;
+                    bulk_load(at + (1 + b) * codes, p.w + tile * codes, codes, bar);
+                    bulk_load(sf + (1 + b) * sf_bytes, p.w + p.w_scales + tile * sf_bytes, sf_bytes, bar);
+                }
+                if (!waited) {                                           // weights do not depend on the previous kernel, x does
+                    pdl_wait();
+                    waited = true;
+                }
+                const int64_t tile = nt * p.col_tiles + i;
+                bulk_load(at, p.x + tile * codes, codes, bar);
+                bulk_load(sf, p.x + p.x_scales + tile * sf_bytes, sf_bytes, bar);
+            }
+        }
+        // no copy may still be in flight when the CTA ends, whatever happened to the other roles
+        for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait(full + 8 * (i % p.stages), (i / p.stages) & 1, ctx, 112);
+    } else if (warp == 1 && lane == 0) {
+        int used = 0, done_tiles = 0;
+        bool ok = true;
+        for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x, ++done_tiles) {
+            if (done_tiles > 0 && !mbar_wait(drained, (done_tiles - 1) & 1, ctx, 113)) break;
+            tc_fence_after();
+            for (int i = 0; i < p.col_tiles; ++i, ++used) {
+                const int s = used % p.stages;
+                if (!mbar_wait(full + 8 * s, (used / p.stages) & 1, ctx, 114)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t at = smem + s * stage_bytes, sf = at + (1 + wide) * codes;
+                const uint32_t sfa = tmem + sf_base + s * sf_cols, sfb = sfa + 8;
+                for (int k = 0; k < atoms; ++k) {
+                    copy_scales(sfa + 4 * k, scale_desc(sf + 512 * k));
+                    for (int b = 0; b < wide; ++b) copy_scales(sfb + 4 * (k * wide + b), scale_desc(sf + (1 + b) * sf_bytes + 512 * k));
+                }
+                const uint64_t da = operand_desc(at, row_bytes), db = operand_desc(at + codes, row_bytes);
+                const int steps = min(p.width / 64, p.ksteps - i * (p.width / 64));
+                for (int k = 0; k < steps; ++k)
+                    umma_mx4(tmem, da + 2 * k, db + 2 * k, mx4_instr_desc(p.tile_n, k & 1), sfa + 4 * (k >> 1), sfb + 4 * wide * (k >> 1), i | k);
+                umma_commit(empty + 8 * s);
+            }
+            umma_commit(done);
+        }
+        // no MMA may still run when tensor memory is freed
+        if (!ok) umma_commit(done);
+        else --done_tiles;
+        if (done_tiles >= 0) mbar_wait(done, done_tiles & 1, ctx, 116);
+    } else if (warp >= 4) {
+        pdl_wait();
+        const int e = warp - 4, quadrant = e & 3, half = e >> 2;         // lanes and columns of the accumulator this warp moves
+        const int cols = p.tile_n / 2;                                   // 64 or 128
+        unsigned char *stage = smem_raw + (smem - smem_u32(smem_raw)) + p.stages * stage_bytes + e * (kStageOut + 512);
+        float *bias = reinterpret_cast<float *>(stage + kStageOut);
+        const uint32_t from = tmem + (static_cast<uint32_t>(quadrant * 32) << 16) + half * cols;
+        T *const y = static_cast<T *>(p.y);
+        const bool vector = (reinterpret_cast<uintptr_t>(p.y) | static_cast<uint64_t>(p.ldy * sizeof(T))) % 16 == 0;
+        int k = 0;
+        for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x, ++k) {
+            const int f0 = static_cast<int>(t % p.f_tiles) * p.tile_n + half * cols;
+            const int64_t row0 = t / p.f_tiles * 128 + quadrant * 32;
+            __syncwarp();
+            for (int c = lane; c < cols; c += 32) bias[c] = p.bias && f0 + c < p.F ? p.bias[f0 + c] : 0.f;
+            if (!mbar_wait(done, k & 1, ctx, 115)) break;
+            tc_fence_after();
+            uint32_t v[128];
+#pragma unroll
+            for (int c = 0; c < 128; c += 32)
+                if (c < cols) tmem_ld32_async(from + c, v + c);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(drained) : "memory");
+            constexpr int kCols = 64 / sizeof(T);
+            const int64_t rows_left = p.rows - row0;
+#pragma unroll
+            for (int c = 0; c < 128; c += kCols) {
+                if (c >= cols || f0 + c >= p.F || rows_left <= 0) continue;
+                float o[kCols];
+#pragma unroll
+                for (int j = 0; j < kCols; j += 4) {
+                    const float4 b = *reinterpret_cast<const float4 *>(bias + c + j);
+                    o[j] = activate1<ACT>(__uint_as_float(v[c + j]) + b.x);
+                    o[j + 1] = activate1<ACT>(__uint_as_float(v[c + j + 1]) + b.y);
+                    o[j + 2] = activate1<ACT>(__uint_as_float(v[c + j + 2]) + b.z);
+                    o[j + 3] = activate1<ACT>(__uint_as_float(v[c + j + 3]) + b.w);
+                }
+                store_piece<T>(o, stage, y + row0 * p.ldy + f0 + c, p.ldy, rows_left, p.F - f0 - c, vector);
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+}
+
+template <typename F> cudaError_t by_output(int dtype, int act, F f) {
+    return by_act(act, [&](auto a) {
+        if (dtype == PATDNN_F32) return f(float{}, a);
+        if (dtype == PATDNN_F16) return f(__half{}, a);
+        return f(__nv_bfloat16{}, a);
+    });
+}
+constexpr int kLinearSmem = 226 * 1024;
+
 }  // namespace
 
-cudaError_t prepare_mx4_linear() { return cudaFuncSetAttribute(mx4_linear_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024); }
+cudaError_t prepare_mx4_linear() {
+    cudaError_t e = cudaFuncSetAttribute(mx4_linear_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinearSmem);
+    for (int dtype = 0; dtype < 3 && e == cudaSuccess; ++dtype)
+        for (int act = PATDNN_ACT_NONE; act <= PATDNN_ACT_SILU && e == cudaSuccess; ++act)
+            e = by_output(dtype, act, [](auto t, auto a) {
+                return cudaFuncSetAttribute(mx4_rows_kernel<decltype(t), a.value>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinearSmem);
+            });
+    return e;
+}
 
 cudaError_t launch_mx4_linear(Mx4Params p, cudaStream_t st, int *launches) {
     const int row_bytes = p.width / 2, atoms = p.width > 128 ? 2 : 1;
+    *launches = 1;
+    // Many rows: as soon as tiles of 128 x 256 (or 128 x 128) fill the SMs, the persistent kernel.
+    const int64_t row_tiles = ceil_div(p.rows, 128);
+    const int tile_f = p.F > 128 && row_tiles * ceil_div(p.F, 256) >= sm_count() ? 256 : 128;
+    if (p.rows > 64 && row_tiles * ceil_div(p.F, tile_f) >= sm_count()) {
+        p.tile_n = tile_f;
+        p.f_tiles = static_cast<int>(ceil_div(p.F, tile_f));
+        p.n_tiles = static_cast<int>(row_tiles);
+        p.splits = 1;
+        const int wide = tile_f / 128;
+        const int stage = ((1 + wide) * (128 * row_bytes + 512 * atoms) + 1023) / 1024 * 1024;
+        const int out = kEpilogueWarps * (kStageOut + 512) + 1024;
+        p.stages = std::min(kMaxStages, (kLinearSmem - out) / stage);
+        const int64_t tiles = static_cast<int64_t>(p.f_tiles) * p.n_tiles;
+        const unsigned grid = static_cast<unsigned>(std::min<int64_t>(tiles, sm_count()));
+        return by_output(p.dtype, p.act, [&](auto t, auto a) {
+            return launch_pdl(mx4_rows_kernel<decltype(t), a.value>, dim3(grid), dim3(kRowsThreads), p.stages * stage + out, st, 1, p);
+        });
+    }
     p.f_tiles = static_cast<int>(ceil_div(p.F, 128));
-    p.tile_n = p.rows <= 128 ? static_cast<int>(ceil_div(p.rows, 16) * 16)
-                             : (ceil_div(p.rows, 256) * p.f_tiles >= sm_count() ? 256 : 128);
+    p.tile_n = p.rows <= 128 ? static_cast<int>(ceil_div(p.rows, 16) * 16) : 128;
     p.n_tiles = static_cast<int>(ceil_div(p.rows, p.tile_n));
     const int64_t tiles = static_cast<int64_t>(p.f_tiles) * p.n_tiles;
     p.splits = 1;
     while (p.splits < 8 && tiles * p.splits * 2 <= sm_count() && p.splits * 2 <= p.col_tiles) p.splits *= 2;
     p.tiles_per_split = static_cast<int>(ceil_div(p.col_tiles, p.splits));
-    const int wide = p.tile_n > 128 ? 2 : 1;
-    const int stage = (128 * row_bytes + p.tile_n * row_bytes + 512 * atoms * (1 + wide) + 1023) / 1024 * 1024;
+    const int stage = (128 * row_bytes + p.tile_n * row_bytes + 512 * atoms * 2 + 1023) / 1024 * 1024;
     p.stages = std::max(1, std::min({kMaxStages, p.tiles_per_split, 200 * 1024 / stage}));
     const int slots = p.splits > 1 ? static_cast<int>(ceil_div(p.tile_n, p.splits)) * p.splits * 512 : 0;
     const int smem = std::max(p.stages * stage, slots) + 1024;
-    *launches = 1;
     return launch_pdl(mx4_linear_kernel, dim3(static_cast<unsigned>(tiles * p.splits)), dim3(kLinThreads), smem, st, p.splits, p);
 }
 

@@ -206,6 +206,11 @@ template <int ACT, int V> __device__ __forceinline__ Fv<V> through(const Fv<V> &
         return g;
     }
 }
+template <int ACT> __device__ __forceinline__ float activate1(float z) {
+    if constexpr (ACT == PATDNN_ACT_RELU) return z < 0.f ? 0.f : z;
+    else if constexpr (ACT == PATDNN_ACT_SILU) return z * sigmoid(z);
+    else return z;
+}
 __device__ __forceinline__ float activate(float z, int act) {
     if (act == PATDNN_ACT_RELU) return z < 0.f ? 0.f : z;
     if (act == PATDNN_ACT_SILU) return z * sigmoid(z);
