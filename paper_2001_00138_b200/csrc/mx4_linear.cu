@@ -82,10 +82,9 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
 
     const int row_bytes = p.width / 2;
     const int atoms = p.width > 128 ? 2 : 1;                             // scale atoms (128 columns each) per column tile
-    const int wide = 1;
     const uint32_t a_codes = 128 * row_bytes, b_codes = p.tile_n * row_bytes, sf_bytes = 512 * atoms;
-    const uint32_t stage_bytes = (a_codes + b_codes + sf_bytes * (1 + wide) + 1023) & ~1023u;
-    const int tmem_cols = wide == 2 ? 512 : 256, sf_base = wide == 2 ? 256 : 128, sf_cols = 8 + 8 * wide;
+    const uint32_t stage_bytes = (a_codes + b_codes + 2 * sf_bytes + 1023) & ~1023u;
+    const int tmem_cols = 256, sf_base = 128, sf_cols = 16;              // accumulator of up to 128 columns, scales per stage
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
@@ -106,63 +105,72 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
 
     const int t0 = rank * p.tiles_per_split, t1 = min(p.col_tiles, t0 + p.tiles_per_split);
     const int iters = max(0, t1 - t0);
-    const int64_t x_tiles = (p.rows + 127) / 128;
     const int64_t x_tile0 = static_cast<int64_t>(nt) * p.tile_n / 128;
     const int x_row0 = static_cast<int>(static_cast<int64_t>(nt) * p.tile_n % 128);
 
     if (warp == 0 && lane == 0) {
         const uint8_t *wc = p.w + static_cast<int64_t>(ft) * p.col_tiles * a_codes;
         const uint8_t *ws = p.w + p.w_scales + static_cast<int64_t>(ft) * p.col_tiles * sf_bytes;
-        const int b_tiles = static_cast<int>(min(static_cast<int64_t>(wide), x_tiles - x_tile0));
-        const uint32_t b_part = wide == 2 ? a_codes : b_codes;           // bytes of one row tile's part
-        const uint32_t bytes = a_codes + sf_bytes + b_tiles * (b_part + sf_bytes);
-        auto load_w = [&](int i) {
-            const int s = i % p.stages;
-            const uint32_t at = smem + s * stage_bytes, bar = full + 8 * s;
+        const uint32_t bytes = a_codes + b_codes + 2 * sf_bytes;
+        // (ring slots and phases advance without divisions: this is one thread, and its instructions bound short column tiles)
+        const uint8_t *xc = p.x + (x_tile0 * p.col_tiles + t0) * a_codes + x_row0 * row_bytes;
+        const uint8_t *xs = p.x + p.x_scales + (x_tile0 * p.col_tiles + t0) * sf_bytes;
+        wc += static_cast<int64_t>(t0) * a_codes;
+        ws += static_cast<int64_t>(t0) * sf_bytes;
+        auto load_w = [&](uint32_t at, uint32_t bar) {
             mbar_expect_tx(bar, bytes);
-            bulk_load(at, wc + static_cast<int64_t>(t0 + i) * a_codes, a_codes, bar);
-            bulk_load(at + a_codes + b_codes, ws + static_cast<int64_t>(t0 + i) * sf_bytes, sf_bytes, bar);
+            bulk_load(at, wc, a_codes, bar);
+            bulk_load(at + a_codes + b_codes, ws, sf_bytes, bar);
+            wc += a_codes;
+            ws += sf_bytes;
         };
-        auto load_x = [&](int i) {
-            const int s = i % p.stages;
-            const uint32_t at = smem + s * stage_bytes, bar = full + 8 * s;
-            for (int b = 0; b < b_tiles; ++b) {
-                const int64_t t = (x_tile0 + b) * p.col_tiles + t0 + i;
-                bulk_load(at + a_codes + b * a_codes, p.x + t * a_codes + x_row0 * row_bytes, b_part, bar);
-                bulk_load(at + a_codes + b_codes + sf_bytes * (1 + b), p.x + p.x_scales + t * sf_bytes, sf_bytes, bar);
-            }
+        auto load_x = [&](uint32_t at, uint32_t bar) {
+            bulk_load(at + a_codes, xc, b_codes, bar);
+            bulk_load(at + a_codes + b_codes + sf_bytes, xs, sf_bytes, bar);
+            xc += a_codes;
+            xs += sf_bytes;
         };
         // the weights do not depend on the previous kernel: fill the ring with them before waiting for it
         const int ahead = min(iters, p.stages);
-        for (int i = 0; i < ahead; ++i) load_w(i);
+        for (int i = 0; i < ahead; ++i) load_w(smem + i * stage_bytes, full + 8 * i);
         pdl_wait();
-        for (int i = 0; i < ahead; ++i) load_x(i);
-        int issued = ahead;
+        for (int i = 0; i < ahead; ++i) load_x(smem + i * stage_bytes, full + 8 * i);
+        int issued = ahead, slot = 0;
+        uint32_t phase = 0;
         for (int i = ahead; i < iters; ++i) {
-            if (!mbar_wait(empty + 8 * (i % p.stages), (i / p.stages - 1) & 1, ctx, 101)) break;
-            load_w(i);
-            load_x(i);
+            if (!mbar_wait(empty + 8 * slot, phase, ctx, 101)) break;
+            load_w(smem + slot * stage_bytes, full + 8 * slot);
+            load_x(smem + slot * stage_bytes, full + 8 * slot);
             ++issued;
+            if (++slot == p.stages) { slot = 0; phase ^= 1; }
         }
         // no copy may still be in flight when the CTA ends, whatever happened to the other roles
         for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait(full + 8 * (i % p.stages), (i / p.stages) & 1, ctx, 102);
     } else if (warp == 1 && lane == 0) {
-        for (int i = 0; i < iters; ++i) {
-            const int s = i % p.stages;
-            if (!mbar_wait(full + 8 * s, (i / p.stages) & 1, ctx, 103)) break;
+        int slot = 0, steps = min(p.ksteps - t0 * (p.width / 64), iters * (p.width / 64));
+        uint32_t phase = 0, accumulate = 0;
+        const uint32_t lower = mx4_instr_desc(p.tile_n, 0), upper = mx4_instr_desc(p.tile_n, 1);
+        for (int i = 0; i < iters; ++i, steps -= p.width / 64) {
+            if (!mbar_wait(full + 8 * slot, phase, ctx, 103)) break;
             tc_fence_after();
-            const uint32_t at = smem + s * stage_bytes;
-            const uint32_t sfa = tmem + sf_base + s * sf_cols, sfb = sfa + 8;
-            for (int k = 0; k < atoms; ++k) {
-                copy_scales(sfa + 4 * k, scale_desc(at + a_codes + b_codes + 512 * k));
-                for (int b = 0; b < wide; ++b)
-                    copy_scales(sfb + 4 * (k * wide + b), scale_desc(at + a_codes + b_codes + sf_bytes * (1 + b) + 512 * k));
+            const uint32_t at = smem + slot * stage_bytes, sf = at + a_codes + b_codes;
+            const uint32_t sfa = tmem + sf_base + slot * sf_cols, sfb = sfa + 8;
+            copy_scales(sfa, scale_desc(sf));
+            copy_scales(sfb, scale_desc(sf + sf_bytes));
+            if (atoms == 2) {
+                copy_scales(sfa + 4, scale_desc(sf + 512));
+                copy_scales(sfb + 4, scale_desc(sf + sf_bytes + 512));
             }
             const uint64_t da = operand_desc(at, row_bytes), db = operand_desc(at + a_codes, row_bytes);
-            const int steps = min(p.width / 64, p.ksteps - (t0 + i) * (p.width / 64));
-            for (int k = 0; k < steps; ++k)
-                umma_mx4(tmem, da + 2 * k, db + 2 * k, mx4_instr_desc(p.tile_n, k & 1), sfa + 4 * (k >> 1), sfb + 4 * wide * (k >> 1), i | k);
-            umma_commit(empty + 8 * s);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (k * 64 < p.width && k < steps) {
+                    umma_mx4(tmem, da + 2 * k, db + 2 * k, k & 1 ? upper : lower, sfa + 4 * (k >> 1), sfb + 4 * (k >> 1), accumulate);
+                    accumulate = 1;
+                }
+            }
+            umma_commit(empty + 8 * slot);
+            if (++slot == p.stages) { slot = 0; phase ^= 1; }
         }
         umma_commit(done);
     }
@@ -319,56 +327,75 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
     const int w_tiles = (p.F + 127) / 128;
 
     if (warp == 0 && lane == 0) {
-        int issued = 0;
+        int issued = 0, slot = 0;
+        uint32_t phase = 1;                                              // (the first pass over the ring does not wait)
         bool ok = true, waited = false;
         for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
             const int ft = static_cast<int>(t % p.f_tiles);
             const int64_t nt = t / p.f_tiles;
-            const int b_tiles = min(wide, w_tiles - ft * wide);
-            const uint32_t bytes = (1 + b_tiles) * (codes + sf_bytes);
-            for (int i = 0; i < p.col_tiles; ++i, ++issued) {
-                const int s = issued % p.stages;
-                if (issued >= p.stages && !mbar_wait(empty + 8 * s, (issued / p.stages - 1) & 1, ctx, 111)) { ok = false; break; }
-                const uint32_t at = smem + s * stage_bytes, bar = full + 8 * s;
+            const bool two = wide == 2 && ft * 2 + 1 < w_tiles;
+            const uint32_t bytes = (two ? 3 : 2) * (codes + sf_bytes);
+            const uint8_t *wc = p.w + static_cast<int64_t>(ft) * wide * p.col_tiles * codes;
+            const uint8_t *ws = p.w + p.w_scales + static_cast<int64_t>(ft) * wide * p.col_tiles * sf_bytes;
+            const int64_t next_codes = static_cast<int64_t>(p.col_tiles) * codes, next_scales = static_cast<int64_t>(p.col_tiles) * sf_bytes;
+            const uint8_t *xc = p.x + nt * next_codes, *xs = p.x + p.x_scales + nt * next_scales;
+            for (int i = 0; i < p.col_tiles; ++i) {
+                if (issued >= p.stages && !mbar_wait(empty + 8 * slot, phase, ctx, 111)) { ok = false; break; }
+                const uint32_t at = smem + slot * stage_bytes, bar = full + 8 * slot;
                 const uint32_t sf = at + (1 + wide) * codes;
                 mbar_expect_tx(bar, bytes);
-                for (int b = 0; b < b_tiles; ++b) {
-                    const int64_t tile = static_cast<int64_t>(ft * wide + b) * p.col_tiles + i;
-                    bulk_load(at + (1 + b) * codes, p.w + tile * codes, codes, bar);
-                    bulk_load(sf + (1 + b) * sf_bytes, p.w + p.w_scales + tile * sf_bytes, sf_bytes, bar);
+                bulk_load(at + codes, wc, codes, bar);
+                bulk_load(sf + sf_bytes, ws, sf_bytes, bar);
+                if (two) {
+                    bulk_load(at + 2 * codes, wc + next_codes, codes, bar);
+                    bulk_load(sf + 2 * sf_bytes, ws + next_scales, sf_bytes, bar);
                 }
                 if (!waited) {                                           // weights do not depend on the previous kernel, x does
                     pdl_wait();
                     waited = true;
                 }
-                const int64_t tile = nt * p.col_tiles + i;
-                bulk_load(at, p.x + tile * codes, codes, bar);
-                bulk_load(sf, p.x + p.x_scales + tile * sf_bytes, sf_bytes, bar);
+                bulk_load(at, xc, codes, bar);
+                bulk_load(sf, xs, sf_bytes, bar);
+                wc += codes; ws += sf_bytes; xc += codes; xs += sf_bytes;
+                ++issued;
+                if (++slot == p.stages) { slot = 0; phase ^= 1; }
             }
         }
         // no copy may still be in flight when the CTA ends, whatever happened to the other roles
         for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait(full + 8 * (i % p.stages), (i / p.stages) & 1, ctx, 112);
     } else if (warp == 1 && lane == 0) {
-        int used = 0, done_tiles = 0;
+        int slot = 0, done_tiles = 0;
+        uint32_t phase = 0;
+        const uint32_t lower = mx4_instr_desc(p.tile_n, 0), upper = mx4_instr_desc(p.tile_n, 1);
         bool ok = true;
         for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x, ++done_tiles) {
             if (done_tiles > 0 && !mbar_wait(drained, (done_tiles - 1) & 1, ctx, 113)) break;
             tc_fence_after();
-            for (int i = 0; i < p.col_tiles; ++i, ++used) {
-                const int s = used % p.stages;
-                if (!mbar_wait(full + 8 * s, (used / p.stages) & 1, ctx, 114)) { ok = false; break; }
+            int steps = p.ksteps;
+            uint32_t accumulate = 0;
+            for (int i = 0; i < p.col_tiles; ++i, steps -= p.width / 64) {
+                if (!mbar_wait(full + 8 * slot, phase, ctx, 114)) { ok = false; break; }
                 tc_fence_after();
-                const uint32_t at = smem + s * stage_bytes, sf = at + (1 + wide) * codes;
-                const uint32_t sfa = tmem + sf_base + s * sf_cols, sfb = sfa + 8;
-                for (int k = 0; k < atoms; ++k) {
-                    copy_scales(sfa + 4 * k, scale_desc(sf + 512 * k));
-                    for (int b = 0; b < wide; ++b) copy_scales(sfb + 4 * (k * wide + b), scale_desc(sf + (1 + b) * sf_bytes + 512 * k));
+                const uint32_t at = smem + slot * stage_bytes, sf = at + (1 + wide) * codes;
+                const uint32_t sfa = tmem + sf_base + slot * sf_cols, sfb = sfa + 8;
+                copy_scales(sfa, scale_desc(sf));
+                copy_scales(sfb, scale_desc(sf + sf_bytes));
+                if (wide == 2) copy_scales(sfb + 4, scale_desc(sf + 2 * sf_bytes));
+                if (atoms == 2) {
+                    copy_scales(sfa + 4, scale_desc(sf + 512));
+                    copy_scales(sfb + 4 * wide, scale_desc(sf + sf_bytes + 512));
+                    if (wide == 2) copy_scales(sfb + 12, scale_desc(sf + 2 * sf_bytes + 512));
                 }
                 const uint64_t da = operand_desc(at, row_bytes), db = operand_desc(at + codes, row_bytes);
-                const int steps = min(p.width / 64, p.ksteps - i * (p.width / 64));
-                for (int k = 0; k < steps; ++k)
-                    umma_mx4(tmem, da + 2 * k, db + 2 * k, mx4_instr_desc(p.tile_n, k & 1), sfa + 4 * (k >> 1), sfb + 4 * wide * (k >> 1), i | k);
-                umma_commit(empty + 8 * s);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (k * 64 < p.width && k < steps) {
+                        umma_mx4(tmem, da + 2 * k, db + 2 * k, k & 1 ? upper : lower, sfa + 4 * (k >> 1), sfb + 4 * wide * (k >> 1), accumulate);
+                        accumulate = 1;
+                    }
+                }
+                umma_commit(empty + 8 * slot);
+                if (++slot == p.stages) { slot = 0; phase ^= 1; }
             }
             umma_commit(done);
         }
