@@ -23,6 +23,16 @@ namespace {
 constexpr int kLinThreads = 256;
 constexpr int kMaxStages = 8;
 
+// The single-thread roles run as whole warps whose values are the same in all lanes (they then live in uniform registers, which the copy
+// and MMA instructions take their operands from); one elected lane issues.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const WaitCtx &ctx, int code) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctx, code));
+}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
@@ -73,7 +83,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
     __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 1];
     __shared__ uint32_t tmem_slot;
     pdl_trigger();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int rank = blockIdx.x % p.splits, tile = blockIdx.x / p.splits;
     const int ft = tile % p.f_tiles, nt = tile / p.f_tiles;
     const WaitCtx ctx{p.status, p.spin_limit ? p.spin_limit : kSpinLimit};
@@ -108,25 +118,28 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
     const int64_t x_tile0 = static_cast<int64_t>(nt) * p.tile_n / 128;
     const int x_row0 = static_cast<int>(static_cast<int64_t>(nt) * p.tile_n % 128);
 
-    if (warp == 0 && lane == 0) {
-        const uint8_t *wc = p.w + static_cast<int64_t>(ft) * p.col_tiles * a_codes;
-        const uint8_t *ws = p.w + p.w_scales + static_cast<int64_t>(ft) * p.col_tiles * sf_bytes;
+    if (warp == 0) {
+        const bool leader = elect_one();
         const uint32_t bytes = a_codes + b_codes + 2 * sf_bytes;
-        // (ring slots and phases advance without divisions: this is one thread, and its instructions bound short column tiles)
+        // (ring slots and phases advance without divisions: the instructions of this warp bound short column tiles)
+        const uint8_t *wc = p.w + (static_cast<int64_t>(ft) * p.col_tiles + t0) * a_codes;
+        const uint8_t *ws = p.w + p.w_scales + (static_cast<int64_t>(ft) * p.col_tiles + t0) * sf_bytes;
         const uint8_t *xc = p.x + (x_tile0 * p.col_tiles + t0) * a_codes + x_row0 * row_bytes;
         const uint8_t *xs = p.x + p.x_scales + (x_tile0 * p.col_tiles + t0) * sf_bytes;
-        wc += static_cast<int64_t>(t0) * a_codes;
-        ws += static_cast<int64_t>(t0) * sf_bytes;
         auto load_w = [&](uint32_t at, uint32_t bar) {
-            mbar_expect_tx(bar, bytes);
-            bulk_load(at, wc, a_codes, bar);
-            bulk_load(at + a_codes + b_codes, ws, sf_bytes, bar);
+            if (leader) {
+                mbar_expect_tx(bar, bytes);
+                bulk_load(at, wc, a_codes, bar);
+                bulk_load(at + a_codes + b_codes, ws, sf_bytes, bar);
+            }
             wc += a_codes;
             ws += sf_bytes;
         };
         auto load_x = [&](uint32_t at, uint32_t bar) {
-            bulk_load(at + a_codes, xc, b_codes, bar);
-            bulk_load(at + a_codes + b_codes + sf_bytes, xs, sf_bytes, bar);
+            if (leader) {
+                bulk_load(at + a_codes, xc, b_codes, bar);
+                bulk_load(at + a_codes + b_codes + sf_bytes, xs, sf_bytes, bar);
+            }
             xc += a_codes;
             xs += sf_bytes;
         };
@@ -138,7 +151,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
         int issued = ahead, slot = 0;
         uint32_t phase = 0;
         for (int i = ahead; i < iters; ++i) {
-            if (!mbar_wait(empty + 8 * slot, phase, ctx, 101)) break;
+            if (!warp_wait(empty + 8 * slot, phase, ctx, 101)) break;
             load_w(smem + slot * stage_bytes, full + 8 * slot);
             load_x(smem + slot * stage_bytes, full + 8 * slot);
             ++issued;
@@ -146,33 +159,37 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
         }
         // no copy may still be in flight when the CTA ends, whatever happened to the other roles
         for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait(full + 8 * (i % p.stages), (i / p.stages) & 1, ctx, 102);
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
+        const bool leader = elect_one();
         int slot = 0, steps = min(p.ksteps - t0 * (p.width / 64), iters * (p.width / 64));
         uint32_t phase = 0, accumulate = 0;
         const uint32_t lower = mx4_instr_desc(p.tile_n, 0), upper = mx4_instr_desc(p.tile_n, 1);
+        const uint64_t da0 = operand_desc(smem, row_bytes), db0 = operand_desc(smem + a_codes, row_bytes);
+        const uint64_t sa0 = scale_desc(smem + a_codes + b_codes), sb0 = scale_desc(smem + a_codes + b_codes + sf_bytes);
         for (int i = 0; i < iters; ++i, steps -= p.width / 64) {
-            if (!mbar_wait(full + 8 * slot, phase, ctx, 103)) break;
+            if (!warp_wait(full + 8 * slot, phase, ctx, 103)) break;
             tc_fence_after();
-            const uint32_t at = smem + slot * stage_bytes, sf = at + a_codes + b_codes;
+            const uint64_t shift = static_cast<uint64_t>(slot) * (stage_bytes >> 4);
             const uint32_t sfa = tmem + sf_base + slot * sf_cols, sfb = sfa + 8;
-            copy_scales(sfa, scale_desc(sf));
-            copy_scales(sfb, scale_desc(sf + sf_bytes));
-            if (atoms == 2) {
-                copy_scales(sfa + 4, scale_desc(sf + 512));
-                copy_scales(sfb + 4, scale_desc(sf + sf_bytes + 512));
-            }
-            const uint64_t da = operand_desc(at, row_bytes), db = operand_desc(at + a_codes, row_bytes);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (k * 64 < p.width && k < steps) {
-                    umma_mx4(tmem, da + 2 * k, db + 2 * k, k & 1 ? upper : lower, sfa + 4 * (k >> 1), sfb + 4 * (k >> 1), accumulate);
-                    accumulate = 1;
+            if (leader) {
+                copy_scales(sfa, sa0 + shift);
+                copy_scales(sfb, sb0 + shift);
+                if (atoms == 2) {
+                    copy_scales(sfa + 4, sa0 + shift + 32);
+                    copy_scales(sfb + 4, sb0 + shift + 32);
                 }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (k * 64 < p.width && k < steps)
+                        umma_mx4(tmem, da0 + shift + 2 * k, db0 + shift + 2 * k, k & 1 ? upper : lower, sfa + 4 * (k >> 1), sfb + 4 * (k >> 1), accumulate | k);
+                }
+                umma_commit(empty + 8 * slot);
             }
-            umma_commit(empty + 8 * slot);
+            __syncwarp();
+            accumulate = 1;
             if (++slot == p.stages) { slot = 0; phase ^= 1; }
         }
-        umma_commit(done);
+        if (leader) umma_commit(done);
     }
     __syncwarp();
     pdl_wait();
@@ -294,7 +311,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
     __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 2];
     __shared__ uint32_t tmem_slot;
     pdl_trigger();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const WaitCtx ctx{p.status, p.spin_limit ? p.spin_limit : kSpinLimit};
     const uint32_t smem = (smem_u32(smem_raw) + 1023) & ~1023u;
     const uint32_t full = smem_u32(bars), empty = full + 8 * kMaxStages, done = empty + 8 * kMaxStages, drained = done + 8;
@@ -326,83 +343,98 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
     const int64_t tiles = static_cast<int64_t>(p.f_tiles) * p.n_tiles;   // f_tiles of tile_n outputs, n_tiles of 128 rows
     const int w_tiles = (p.F + 127) / 128;
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
+        const bool leader = elect_one();
         int issued = 0, slot = 0;
         uint32_t phase = 1;                                              // (the first pass over the ring does not wait)
         bool ok = true, waited = false;
+        const uint32_t next_codes = p.col_tiles * codes, next_scales = p.col_tiles * sf_bytes;    // from one row tile to the next
+        int ft = static_cast<int>(blockIdx.x % static_cast<unsigned>(p.f_tiles));
+        int nt = static_cast<int>(blockIdx.x / static_cast<unsigned>(p.f_tiles));
         for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
-            const int ft = static_cast<int>(t % p.f_tiles);
-            const int64_t nt = t / p.f_tiles;
             const bool two = wide == 2 && ft * 2 + 1 < w_tiles;
             const uint32_t bytes = (two ? 3 : 2) * (codes + sf_bytes);
-            const uint8_t *wc = p.w + static_cast<int64_t>(ft) * wide * p.col_tiles * codes;
-            const uint8_t *ws = p.w + p.w_scales + static_cast<int64_t>(ft) * wide * p.col_tiles * sf_bytes;
-            const int64_t next_codes = static_cast<int64_t>(p.col_tiles) * codes, next_scales = static_cast<int64_t>(p.col_tiles) * sf_bytes;
-            const uint8_t *xc = p.x + nt * next_codes, *xs = p.x + p.x_scales + nt * next_scales;
+            const uint8_t *wc = p.w + static_cast<int64_t>(ft) * wide * next_codes;
+            const uint8_t *ws = p.w + p.w_scales + static_cast<int64_t>(ft) * wide * next_scales;
+            const uint8_t *xc = p.x + static_cast<int64_t>(nt) * next_codes, *xs = p.x + p.x_scales + static_cast<int64_t>(nt) * next_scales;
             for (int i = 0; i < p.col_tiles; ++i) {
-                if (issued >= p.stages && !mbar_wait(empty + 8 * slot, phase, ctx, 111)) { ok = false; break; }
+                if (issued >= p.stages && !warp_wait(empty + 8 * slot, phase, ctx, 111)) { ok = false; break; }
                 const uint32_t at = smem + slot * stage_bytes, bar = full + 8 * slot;
                 const uint32_t sf = at + (1 + wide) * codes;
-                mbar_expect_tx(bar, bytes);
-                bulk_load(at + codes, wc, codes, bar);
-                bulk_load(sf + sf_bytes, ws, sf_bytes, bar);
-                if (two) {
-                    bulk_load(at + 2 * codes, wc + next_codes, codes, bar);
-                    bulk_load(sf + 2 * sf_bytes, ws + next_scales, sf_bytes, bar);
+                if (leader) {
+                    mbar_expect_tx(bar, bytes);
+                    bulk_load(at + codes, wc, codes, bar);
+                    bulk_load(sf + sf_bytes, ws, sf_bytes, bar);
+                    if (two) {
+                        bulk_load(at + 2 * codes, wc + next_codes, codes, bar);
+                        bulk_load(sf + 2 * sf_bytes, ws + next_scales, sf_bytes, bar);
+                    }
                 }
                 if (!waited) {                                           // weights do not depend on the previous kernel, x does
                     pdl_wait();
                     waited = true;
                 }
-                bulk_load(at, xc, codes, bar);
-                bulk_load(sf, xs, sf_bytes, bar);
+                if (leader) {
+                    bulk_load(at, xc, codes, bar);
+                    bulk_load(sf, xs, sf_bytes, bar);
+                }
                 wc += codes; ws += sf_bytes; xc += codes; xs += sf_bytes;
                 ++issued;
                 if (++slot == p.stages) { slot = 0; phase ^= 1; }
             }
+            nt += p.step_n;                                              // the tile gridDim.x further on
+            ft += p.step_f;
+            if (ft >= p.f_tiles) { ft -= p.f_tiles; ++nt; }
         }
         // no copy may still be in flight when the CTA ends, whatever happened to the other roles
         for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait(full + 8 * (i % p.stages), (i / p.stages) & 1, ctx, 112);
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
+        const bool leader = elect_one();
         int slot = 0, done_tiles = 0;
         uint32_t phase = 0;
         const uint32_t lower = mx4_instr_desc(p.tile_n, 0), upper = mx4_instr_desc(p.tile_n, 1);
+        const uint64_t da0 = operand_desc(smem, row_bytes), db0 = operand_desc(smem + codes, row_bytes);
+        const uint64_t s0 = scale_desc(smem + (1 + wide) * codes);
+        const uint32_t row_scales = sf_bytes >> 4;                       // descriptor distance between the scales of two row tiles
         bool ok = true;
         for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x, ++done_tiles) {
-            if (done_tiles > 0 && !mbar_wait(drained, (done_tiles - 1) & 1, ctx, 113)) break;
+            if (done_tiles > 0 && !warp_wait(drained, (done_tiles - 1) & 1, ctx, 113)) break;
             tc_fence_after();
             int steps = p.ksteps;
             uint32_t accumulate = 0;
             for (int i = 0; i < p.col_tiles; ++i, steps -= p.width / 64) {
-                if (!mbar_wait(full + 8 * slot, phase, ctx, 114)) { ok = false; break; }
+                if (!warp_wait(full + 8 * slot, phase, ctx, 114)) { ok = false; break; }
                 tc_fence_after();
-                const uint32_t at = smem + slot * stage_bytes, sf = at + (1 + wide) * codes;
+                const uint64_t shift = static_cast<uint64_t>(slot) * (stage_bytes >> 4);
+                const uint64_t da = da0 + shift, db = db0 + shift, sd = s0 + shift;
                 const uint32_t sfa = tmem + sf_base + slot * sf_cols, sfb = sfa + 8;
-                copy_scales(sfa, scale_desc(sf));
-                copy_scales(sfb, scale_desc(sf + sf_bytes));
-                if (wide == 2) copy_scales(sfb + 4, scale_desc(sf + 2 * sf_bytes));
-                if (atoms == 2) {
-                    copy_scales(sfa + 4, scale_desc(sf + 512));
-                    copy_scales(sfb + 4 * wide, scale_desc(sf + sf_bytes + 512));
-                    if (wide == 2) copy_scales(sfb + 12, scale_desc(sf + 2 * sf_bytes + 512));
-                }
-                const uint64_t da = operand_desc(at, row_bytes), db = operand_desc(at + codes, row_bytes);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (k * 64 < p.width && k < steps) {
-                        umma_mx4(tmem, da + 2 * k, db + 2 * k, k & 1 ? upper : lower, sfa + 4 * (k >> 1), sfb + 4 * wide * (k >> 1), accumulate);
-                        accumulate = 1;
+                if (leader) {
+                    copy_scales(sfa, sd);
+                    copy_scales(sfb, sd + row_scales);
+                    if (wide == 2) copy_scales(sfb + 4, sd + 2 * row_scales);
+                    if (atoms == 2) {
+                        copy_scales(sfa + 4, sd + 32);
+                        copy_scales(sfb + 4 * wide, sd + row_scales + 32);
+                        if (wide == 2) copy_scales(sfb + 12, sd + 2 * row_scales + 32);
                     }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (k * 64 < p.width && k < steps)
+                            umma_mx4(tmem, da + 2 * k, db + 2 * k, k & 1 ? upper : lower, sfa + 4 * (k >> 1), sfb + 4 * wide * (k >> 1), accumulate | k);
+                    }
+                    umma_commit(empty + 8 * slot);
                 }
-                umma_commit(empty + 8 * slot);
+                __syncwarp();
+                accumulate = 1;
                 if (++slot == p.stages) { slot = 0; phase ^= 1; }
             }
-            umma_commit(done);
+            if (leader && ok) umma_commit(done);
+            __syncwarp();
         }
         // no MMA may still run when tensor memory is freed
-        if (!ok) umma_commit(done);
-        else --done_tiles;
-        if (done_tiles >= 0) mbar_wait(done, done_tiles & 1, ctx, 116);
+        if (leader && !ok) umma_commit(done);
+        __syncwarp();
+        if (done_tiles > 0) mbar_wait(done, (done_tiles - 1) & 1, ctx, 116);
     } else if (warp >= 4) {
         pdl_wait();
         const int e = warp - 4, quadrant = e & 3, half = e >> 2;         // lanes and columns of the accumulator this warp moves
@@ -490,6 +522,8 @@ cudaError_t launch_mx4_linear(Mx4Params p, cudaStream_t st, int *launches) {
         p.stages = std::min(kMaxStages, (kLinearSmem - out) / stage);
         const int64_t tiles = static_cast<int64_t>(p.f_tiles) * p.n_tiles;
         const unsigned grid = static_cast<unsigned>(std::min<int64_t>(tiles, sm_count()));
+        p.step_n = static_cast<int>(grid / p.f_tiles);
+        p.step_f = static_cast<int>(grid % p.f_tiles);
         return by_output(p.dtype, p.act, [&](auto t, auto a) {
             return launch_pdl(mx4_rows_kernel<decltype(t), a.value>, dim3(grid), dim3(kRowsThreads), p.stages * stage + out, st, 1, p);
         });

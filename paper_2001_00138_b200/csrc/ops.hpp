@@ -96,6 +96,7 @@ struct Mx4Params {
     int tile_n;
     int splits, tiles_per_split;            // cluster split of the column tiles
     int stages;
+    int step_n, step_f;                     // persistent kernel: from a CTA's tile to its next one
     uint32_t spin_limit;
 };
 cudaError_t prepare_mx4_linear();                       // opt in to the dynamic shared memory
