@@ -289,15 +289,15 @@ __device__ __forceinline__ void join_groups(const float2 *red, int rows, int cha
 // pixels; four neighbouring lanes share a block of 32.  The last slab also writes the zeros up to a multiple of 64 columns, which
 // the product's steps cover.
 template <typename T, int ACT>
-__device__ __forceinline__ void write_mx4(const NormArgs &a, const T *tile, const float2 *fin, int n, int64_t p0, int pixels, int c0, int channels) {
+__device__ __forceinline__ void write_mx4(const NormArgs &a, const T *tile, const float2 *fin, const float *gamma, const float *beta_of, int n, int64_t p0, int pixels, int c0, int channels) {
     const int width = c0 + channels == a.C ? (a.C + 63) / 64 * 64 - c0 : channels;
     const int units = width / 8, rows = kThreads / units;
     const int unit = threadIdx.x % units, first = threadIdx.x / units;
     const int c = unit * 8;
     const Groups<8> at(c, a.per);
     const Fv<8> shift = Fv<8>::make([&](int j) { return c + j < channels ? -fin[at.g[j]].x : 0.f; });
-    const Fv<8> scale = Fv<8>::make([&](int j) { return c + j < channels ? fin[at.g[j]].y * a.gamma[c0 + c + j] : 0.f; });
-    const Fv<8> beta = Fv<8>::make([&](int j) { return c + j < channels ? a.beta[c0 + c + j] : 0.f; });
+    const Fv<8> scale = Fv<8>::make([&](int j) { return c + j < channels ? fin[at.g[j]].y * gamma[c + j] : 0.f; });
+    const Fv<8> beta = Fv<8>::make([&](int j) { return c + j < channels ? beta_of[c + j] : 0.f; });
     const bool whole = c + 8 <= channels && channels % (16 / sizeof(T)) == 0;
     const int ct = (c0 + c) / a.mx_width, in_tile = (c0 + c) - ct * a.mx_width;
     const int scale_col = (in_tile >> 7) * 512 + ((in_tile >> 5) & 3);
@@ -342,7 +342,7 @@ __device__ __forceinline__ void write_mx4(const NormArgs &a, const T *tile, cons
 }
 
 // ---- resident form ----------------------------------------------------------------------------------------------------
-// Shared memory: [chunk][slab] elements of x, then [rows][slab] float2, then [groups of the slab] float2 twice.
+// Shared memory: [chunk][slab] elements of x, then [rows][slab] float2, then [groups of the slab] float2 twice, then gamma and beta.
 template <typename T, int V, int ACT, bool MX>
 __global__ void __launch_bounds__(kThreads, 3) norm_resident_kernel(NormArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
@@ -358,8 +358,13 @@ __global__ void __launch_bounds__(kThreads, 3) norm_resident_kernel(NormArgs a) 
     float2 *red = reinterpret_cast<float2 *>(smem + (a.chunk * a.slab * sizeof(T) + 15) / 16 * 16);
     float2 *grp = red + kThreads * V;
     float2 *fin = grp + a.slab / a.per;
+    float *gamma = reinterpret_cast<float *>(fin + a.slab / a.per), *beta_of = gamma + a.slab;
     const int groups = channels / a.per;
     pdl_wait();
+    for (int c = threadIdx.x; c < channels; c += kThreads) {           // in flight together with x
+        copy_async<4>(shared_address(gamma + c), a.gamma + c0 + c);
+        copy_async<4>(shared_address(beta_of + c), a.beta + c0 + c);
+    }
     if (q.on) {
         Moments<V> m;
         Stream<T, V, true, 1> x;
@@ -367,6 +372,7 @@ __global__ void __launch_bounds__(kThreads, 3) norm_resident_kernel(NormArgs a) 
         moments_of<T, V, true>(x, m);
         put_moments<V>(m, q, channels, a.per, red);
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
     if (pixels > 0) join_groups<V>(red, q.rows, channels, a.per, pixels, grp);
     cg::cluster_group cluster = cg::this_cluster();
@@ -398,15 +404,15 @@ __global__ void __launch_bounds__(kThreads, 3) norm_resident_kernel(NormArgs a) 
     // fin is ready; nobody reads this CTA's grp after this point
     if (a.cluster > 1) cluster.sync(); else __syncthreads();
     if constexpr (MX) {
-        write_mx4<T, ACT>(a, tile, fin, n, p0, pixels, c0, channels);
+        write_mx4<T, ACT>(a, tile, fin, gamma, beta_of, n, p0, pixels, c0, channels);
         return;
     }
     if (!q.on || !a.y) return;
     const int col = q.col * V;
     const Groups<V> at(col, a.per);
     const Fv<V> shift = Fv<V>::make([&](int j) { return -fin[at.g[j]].x; });
-    const Fv<V> scale = Fv<V>::make([&](int j) { return fin[at.g[j]].y * a.gamma[c0 + col + j]; });
-    const Fv<V> beta = Fv<V>::make([&](int j) { return a.beta[c0 + col + j]; });
+    const Fv<V> scale = Fv<V>::make([&](int j) { return fin[at.g[j]].y * gamma[col + j]; });
+    const Fv<V> beta = Fv<V>::make([&](int j) { return beta_of[col + j]; });
     T *dst = static_cast<T *>(a.y) + n * a.y_image + (p0 + q.row) * a.y_pixel + c0 + q.col * V;
     uint32_t src = shared_address(tile + q.row * channels + col);
     const int64_t dst_step = q.rows * a.y_pixel;
@@ -444,9 +450,17 @@ struct Channels {
     }
 };
 
-// Sums of dz and dz * d over a thread's pixels.
+// Begins the copies of two tensors; returns the number of a thread's pixels.
+template <typename S> __device__ __forceinline__ int start_copies(S &x, S &dy) {
+    const int count = x.left;
+#pragma unroll
+    for (int b = 0; b < S::kDepth; ++b) { x.copy(); dy.copy(); copies_commit(); }
+    return count;
+}
+
+// Sums of dz and dz * d over a thread's pixels, whose copies have begun.
 template <typename T, int V, int ACT, bool KEEP>
-__device__ __forceinline__ void sums_of(Stream<T, V, KEEP, 2> &x, Stream<T, V, KEEP, 2> &dy, const Channels<V> &f, Fv<V> &sa, Fv<V> &sb) {
+__device__ __forceinline__ void sums_of(Stream<T, V, KEEP, 2> &x, Stream<T, V, KEEP, 2> &dy, int count, const Channels<V> &f, Fv<V> &sa, Fv<V> &sb) {
     constexpr int kBatch = Stream<T, V, KEEP, 2>::kBatch, kDepth = Stream<T, V, KEEP, 2>::kDepth;
     sa = sb = Fv<V>::all(0.f);
     auto take = [&]() {
@@ -455,9 +469,6 @@ __device__ __forceinline__ void sums_of(Stream<T, V, KEEP, 2> &x, Stream<T, V, K
         sa = sa + dz;
         sb = fma(dz, d, sb);
     };
-    int count = x.left;
-#pragma unroll
-    for (int b = 0; b < kDepth; ++b) { x.copy(); dy.copy(); copies_commit(); }
     for (; count > 0; count -= kBatch) {
         copies_wait<kDepth - 1>();
         if (count >= kBatch) {
@@ -498,12 +509,13 @@ __global__ void __launch_bounds__(kThreads, 3) norm_grad_resident_kernel(NormArg
 
     Channels<V> f;
     if (q.on) {
-        f.load(a, n, c0 + q.col * V);
         Fv<V> sa, sb;
         Stream<T, V, true, 2> x, dy;
         x.begin(static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + c0 + q.col * V, a.x_pixel, pixels, q, xt, channels, q.col * V);
         dy.begin(static_cast<const T *>(a.dy) + n * a.y_image + p0 * a.y_pixel + c0 + q.col * V, a.y_pixel, pixels, q, dt, channels, q.col * V);
-        sums_of<T, V, ACT, true>(x, dy, f, sa, sb);
+        const int count = start_copies(x, dy);
+        f.load(a, n, c0 + q.col * V);                  // (arrives with the first copies)
+        sums_of<T, V, ACT, true>(x, dy, count, f, sa, sb);
 #pragma unroll
         for (int j = 0; j < V; ++j) red[q.row * channels + q.col * V + j] = make_float2(sa.get(j), sb.get(j));
     }
@@ -716,14 +728,15 @@ __global__ void __launch_bounds__(kThreads, 3) norm_grad_sums_kernel(NormArgs a)
     pdl_wait();
     Fv<V> sa, sb;
     if (q.on) {
-        Channels<V> f;
-        f.load(a, n, s.c0 + q.col * V);
         T *ring = reinterpret_cast<T *>(smem);
         Stream<T, V, false, 2> x, dy;
         x.begin(static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + s.c0 + q.col * V, a.x_pixel, pixels, q, ring, s.channels, 0);
         dy.begin(static_cast<const T *>(a.dy) + n * a.y_image + p0 * a.y_pixel + s.c0 + q.col * V, a.y_pixel, pixels, q,
                  ring + Stream<T, V, false, 2>::kDepth * Stream<T, V, false, 2>::kBatch * kThreads * V, s.channels, 0);
-        sums_of<T, V, ACT, false>(x, dy, f, sa, sb);
+        const int count = start_copies(x, dy);
+        Channels<V> f;
+        f.load(a, n, s.c0 + q.col * V);                // (arrives with the first copies)
+        sums_of<T, V, ACT, false>(x, dy, count, f, sa, sb);
     }
     __syncthreads();                                   // red lies over the rings
     if (q.on) {
@@ -837,7 +850,7 @@ __global__ void __launch_bounds__(kThreads, 3) norm_grad_apply_kernel(NormArgs a
 int resident_smem(const NormShape &s, int width, int tensors, int slab, int64_t chunk) {
     const int64_t tile = (chunk * slab * elem_bytes(s.dtype) + 15) / 16 * 16;
     const int64_t groups = slab / (s.C / s.G);
-    const int64_t small = tensors == 1 ? 2 * groups : 2 * slab + groups;
+    const int64_t small = tensors == 1 ? 2 * groups + slab : 2 * slab + groups;   // (gamma and beta: a float2's worth per channel)
     const int64_t total = tensors * tile + (static_cast<int64_t>(kThreads) * width + small) * 8;
     return total > (int64_t(1) << 30) ? (1 << 30) : static_cast<int>(total);
 }

@@ -27,6 +27,7 @@ struct QuantArgs {
     int64_t row0, rows, cols, ld;           // rows [row0, rows) of the matrix
     int64_t scales_at;
     int width, col_tiles, code_bytes, scale_bytes;
+    int step_ct, step_rest;                 // from a CTA's unit to its next one: column tiles, quarters of row tiles
     // group norm in front (NORM kernels only): row = image * P + pixel
     const float *gamma, *beta, *stats;
     int64_t P, x_image;
@@ -48,26 +49,60 @@ struct Raw {
     __device__ __forceinline__ float get(int i) const { return to_float(v[i / A].v[i % A]); }
 };
 
-// Bits of the largest magnitude among a lane's eight columns; two 16-bit values are compared at a time.
-template <typename T, int A> __device__ __forceinline__ uint32_t top_of(const Raw<T, A> &raw) {
-    if constexpr (sizeof(T) == 4) {
-        float v[8];
+// Eight columns of a row as 32-bit words, in accesses of A elements.
+template <typename T, int A>
+struct Row8 {
+    static constexpr int kWords = 8 * sizeof(T) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = raw.get(j);
-        return top8(v);
-    } else {
-        uint32_t top = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t two;
-            if constexpr (A >= 2) two = *reinterpret_cast<const uint32_t *>(&raw.v[2 * j / A].v[2 * j % A]);
-            else two = *reinterpret_cast<const uint16_t *>(&raw.v[2 * j].v[0]) | static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(&raw.v[2 * j + 1].v[0])) << 16;
-            top = __vmaxu2(top, two & 0x7fff7fffu);
-        }
-        const uint16_t one = static_cast<uint16_t>(max(top & 0xffffu, top >> 16));
-        return __float_as_uint(to_float(*reinterpret_cast<const T *>(&one)));
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
     }
-}
+    __device__ __forceinline__ void load(const T *p) {
+        if constexpr (sizeof(T) * A >= 4) {
+            constexpr int kPer = sizeof(T) * A / 4;    // words per access
+#pragma unroll
+            for (int i = 0; i < 8 / A; ++i) {
+                Pack<T, A> t;
+                t.load(p + i * A);
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) w[i * kPer + k] = t.w[k];
+            }
+        } else {
+            load(p, 8);
+        }
+    }
+    __device__ __forceinline__ void load(const T *p, int count) {      // the first `count`, zeros after them
+        clear();
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count) {
+                if constexpr (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+                else w[i / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t *>(p)[i]) << (16 * (i & 1));
+            }
+    }
+    __device__ __forceinline__ Fv<8> values() const {
+        Pack<T, 8> t;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) t.w[i] = w[i];
+        return widen<T, 8>(t);
+    }
+    // bits of the largest magnitude; two 16-bit values are compared at a time
+    __device__ __forceinline__ uint32_t top() const {
+        if constexpr (sizeof(T) == 4) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+            return top8(v);
+        } else {
+            uint32_t t = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+            t = max(t & 0xffffu, t >> 16);
+            if constexpr (std::is_same<T, __nv_bfloat16>::value) return t << 16;
+            const uint16_t one = static_cast<uint16_t>(t);
+            return __float_as_uint(__half2float(*reinterpret_cast<const __half *>(&one)));
+        }
+    }
+};
 
 // CTAs per SM that the registers of two row sets allow
 template <typename T, int A> __host__ __device__ constexpr int quant_ctas() { return sizeof(T) == 4 || A == 1 ? 3 : 4; }
@@ -76,67 +111,63 @@ template <typename T, int A> __host__ __device__ constexpr int quant_ctas() { re
 // rows r0, r0 + 32, r0 + 64, r0 + 96 of the row tile.  CTAs walk over the units and load the next one before they quantise the present
 // one, so that loads are always in flight.
 template <typename T, int A>
-__global__ void __launch_bounds__(kWarps * 32, quant_ctas<T, A>()) mx4_quantize_kernel(QuantArgs a, unsigned units) {
+__global__ void __launch_bounds__(kWarps * 32, quant_ctas<T, A>()) mx4_quantize_kernel(QuantArgs a, unsigned quarters) {
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int row_bytes = a.width / 2;
     const bool mine = lane * 8 < a.width;              // narrow tiles leave lanes idle
-    auto load = [&](unsigned unit, Raw<T, A> (&raw)[4]) {
-        const int ct = static_cast<int>(unit % static_cast<unsigned>(a.col_tiles));
-        const unsigned rest = unit / static_cast<unsigned>(a.col_tiles);
-        const int64_t row = static_cast<int64_t>(rest >> 2) * 128 + (rest & 3) * kWarps + warp;
-        const int64_t c = static_cast<int64_t>(ct) * a.width + lane * 8;
+    int ct = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.col_tiles));
+    unsigned rest = blockIdx.x / static_cast<unsigned>(a.col_tiles);
+    const int64_t down = 32 * a.ld;
+    auto load = [&](int at_ct, unsigned at_rest, Row8<T, A> (&raw)[4]) {
+        const int64_t row = static_cast<int64_t>(at_rest >> 2) * 128 + (at_rest & 3) * kWarps + warp;
+        const int64_t c = static_cast<int64_t>(at_ct) * a.width + lane * 8;
         const T *src = static_cast<const T *>(a.x) + row * a.ld + c;
         if (mine && c + 8 <= a.cols && row + 96 < a.rows) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) raw[k].load(src + 32 * k * a.ld);
+            for (int k = 0; k < 4; ++k, src += down) raw[k].load(src);
         } else {
             const int count = mine ? static_cast<int>(max(int64_t(0), min(int64_t(8), a.cols - c))) : 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) raw[k].load(src + 32 * k * a.ld, row + 32 * k < a.rows ? count : 0);
+            for (int k = 0; k < 4; ++k, src += down) raw[k].load(src, row + 32 * k < a.rows ? count : 0);
         }
     };
-    auto store = [&](unsigned unit, const Raw<T, A> (&raw)[4]) {
-        const int ct = static_cast<int>(unit % static_cast<unsigned>(a.col_tiles));
-        const unsigned rest = unit / static_cast<unsigned>(a.col_tiles);
+    auto store = [&](const Row8<T, A> (&raw)[4]) {
         const int64_t rt = rest >> 2;
         const int r0 = static_cast<int>(rest & 3) * kWarps + warp;
-        uint8_t *codes_out = a.mx + (rt * a.col_tiles + ct) * a.code_bytes;
-        uint8_t *scales_out = a.mx + a.scales_at + (rt * a.col_tiles + ct) * a.scale_bytes;
+        const int64_t left = a.rows - rt * 128 - r0;   // rows of the set exist where 32 k < left
+        const int64_t tile = rt * a.col_tiles + ct;
+        // 32 rows further down the tile, a 16-byte unit keeps its place in the row
+        int at = r0 * row_bytes + lane * 4;
+        at ^= ((at >> 7) & (a.width / 32 - 1)) << 4;
+        uint8_t *codes_out = a.mx + tile * a.code_bytes + at;
         uint32_t sets[4];                              // lane of block b: scale byte of (row r0 + 32 k, b)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float v[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = raw[k].get(j);
+        for (int k = 0; k < 4; ++k, codes_out += 32 * row_bytes) {
             uint32_t codes;
-            sets[k] = quantise8(v, top_of(raw[k]), codes);
-            if (rt * 128 + r0 + 32 * k < a.rows && mine) {
-                int at = (r0 + 32 * k) * row_bytes + lane * 4;
-                at ^= ((at >> 7) & (a.width / 32 - 1)) << 4;
-                *reinterpret_cast<uint32_t *>(codes_out + at) = codes;
-            }
+            sets[k] = quantise8(raw[k].values(), raw[k].top(), codes);
+            if (32 * k < left && mine) *reinterpret_cast<uint32_t *>(codes_out) = codes;
         }
         // lanes 0 and 16 gather the scale bytes of blocks 0..3 and 4..7: 16 bytes each
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            uint32_t w = sets[k];
-            w |= __shfl_down_sync(0xffffffffu, w, 4) << 8;
-            w |= __shfl_down_sync(0xffffffffu, w, 8) << 16;
-            sets[k] = w;
+            sets[k] |= __shfl_down_sync(0xffffffffu, sets[k], 4) << 8;
+            sets[k] |= __shfl_down_sync(0xffffffffu, sets[k], 8) << 16;
         }
-        if ((lane & 15) == 0 && mine && rt * 128 + r0 < a.rows)
-            *reinterpret_cast<uint4 *>(scales_out + (lane >> 4) * 512 + r0 * 16) = make_uint4(sets[0], sets[1], sets[2], sets[3]);
+        if ((lane & 15) == 0 && mine && left > 0)
+            *reinterpret_cast<uint4 *>(a.mx + a.scales_at + tile * a.scale_bytes + (lane >> 4) * 512 + r0 * 16) = make_uint4(sets[0], sets[1], sets[2], sets[3]);
     };
     pdl_wait();
-    unsigned unit = blockIdx.x;
-    Raw<T, A> now[4], next[4];
-    load(unit, now);
-    while (unit < units) {                             // (the same for all threads of the CTA)
-        const unsigned after = unit + gridDim.x;
-        if (after < units) load(after, next);
-        store(unit, now);
-        unit = after;
+    Row8<T, A> now[4], next[4];
+    if (rest < quarters) load(ct, rest, now);
+    while (rest < quarters) {                          // (the same for all threads of the CTA)
+        int next_ct = ct + a.step_ct;
+        unsigned next_rest = rest + a.step_rest;
+        if (next_ct >= a.col_tiles) { next_ct -= a.col_tiles; ++next_rest; }
+        if (next_rest < quarters) load(next_ct, next_rest, next);
+        store(now);
+        ct = next_ct;
+        rest = next_rest;
 #pragma unroll
         for (int k = 0; k < 4; ++k) now[k] = next[k];
     }
@@ -229,6 +260,29 @@ __global__ void __launch_bounds__(kWarps * 32) norm_quantize_kernel(QuantArgs a)
     }
 }
 
+// The values of eight codes with the scale 2^(byte - 127): byte 0 is the subnormal 2^-127, 255 is NaN.
+__device__ __forceinline__ float scale_value(uint32_t byte) {
+    return byte == 255 ? __uint_as_float(0x7fffffffu) : byte ? __uint_as_float(byte << 23) : __uint_as_float(0x00400000u);
+}
+// The value of one code: sign, two exponent bits, one mantissa bit; exponent 0 has the magnitudes 0 and 1/2.
+__device__ __forceinline__ float value_of(uint32_t code, float scale) {
+    const uint32_t e = (code >> 1) & 3, m = code & 1;
+    const float magnitude = e ? __uint_as_float(((e + 126) << 23) | (m << 22)) : 0.5f * static_cast<float>(m);
+    return (code & 8 ? -magnitude : magnitude) * scale;
+}
+__device__ __forceinline__ Fv<8> values_of(uint32_t codes, uint32_t byte) {
+    const float scale = scale_value(byte);
+    __half2 h[4];
+    unpack8(codes, h);
+    Fv<8> v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 f = __half22float2(h[j]);
+        v.p[j] = mul_(pair_of(f.x, f.y), pair_of(scale, scale));
+    }
+    return v;
+}
+
 template <typename T, int A>
 __global__ void __launch_bounds__(kWarps * 32) mx4_dequantize_kernel(QuantArgs a, T *out) {
     pdl_trigger();
@@ -256,30 +310,55 @@ __global__ void __launch_bounds__(kWarps * 32) mx4_dequantize_kernel(QuantArgs a
     for (int k = 0; k < 4; ++k) {
         const int64_t row = rt * 128 + r0 + 32 * k;
         if (row >= a.rows) continue;
-        // 2^(byte - 127): byte 0 is the subnormal 2^-127, 255 is NaN
-        const float s = scale[k] == 255 ? __uint_as_float(0x7fffffffu) : scale[k] ? __uint_as_float(scale[k] << 23) : __uint_as_float(0x00400000u);
-        __half2 h[4];
-        unpack8(codes[k], h);
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 f = __half22float2(h[j]);
-            v[2 * j] = f.x * s;
-            v[2 * j + 1] = f.y * s;
-        }
+        const Fv<8> v = values_of(codes[k], scale[k]);
         T *dst = out + row * a.ld;
         if (c + 8 <= a.cols) {
+            const Pack<T, 8> t = narrow<T, 8>(v);
+            constexpr int kPer = sizeof(T) * A / 4;
 #pragma unroll
             for (int i = 0; i < 8 / A; ++i) {
-                Vec<T, A> t;
+                Pack<T, A> part;
 #pragma unroll
-                for (int j = 0; j < A; ++j) t.v[j] = from_float<T>(v[i * A + j]);
-                *reinterpret_cast<Vec<T, A> *>(dst + c + i * A) = t;
+                for (int q = 0; q < kPer; ++q) part.w[q] = t.w[i * kPer + q];
+                part.store(dst + c + i * A);
             }
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (c + j < a.cols) dst[c + j] = from_float<T>(v[j]);
+                if (c + j < a.cols) dst[c + j] = from_float<T>(v.get(j));
+        }
+    }
+}
+
+// The same for outputs that allow accesses of one element only: a lane takes every 32nd column, so that a warp still stores
+// consecutive elements; eight lanes read the same word of codes.
+template <typename T>
+__global__ void __launch_bounds__(kWarps * 32) mx4_dequantize_single_kernel(QuantArgs a, T *out) {
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int ct = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.col_tiles));
+    const unsigned rest = blockIdx.x / static_cast<unsigned>(a.col_tiles);
+    const int64_t rt = rest >> 2;
+    const int r0 = static_cast<int>(rest & 3) * kWarps + warp;
+    const int row_bytes = a.width / 2;
+    const uint8_t *codes_in = a.mx + (rt * a.col_tiles + ct) * a.code_bytes;
+    const uint8_t *scales_in = a.mx + a.scales_at + (rt * a.col_tiles + ct) * a.scale_bytes;
+    const int cols = static_cast<int>(min(static_cast<int64_t>(a.width), a.cols - static_cast<int64_t>(ct) * a.width));
+    pdl_wait();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int64_t row = rt * 128 + r0 + 32 * k;
+        if (row >= a.rows) continue;
+        T *dst = out + row * a.ld + static_cast<int64_t>(ct) * a.width;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = 32 * j + lane;
+            if (c >= cols) continue;
+            int at = (r0 + 32 * k) * row_bytes + (c >> 3) * 4;
+            at ^= ((at >> 7) & (a.width / 32 - 1)) << 4;
+            const uint32_t word = *reinterpret_cast<const uint32_t *>(codes_in + at) >> (4 * (c & 7));
+            const uint32_t scale = scales_in[(c >> 7) * 512 + r0 * 16 + k * 4 + (j & 3)];
+            dst[c] = from_float<T>(value_of(word & 15, scale_value(scale)));
         }
     }
 }
@@ -319,11 +398,13 @@ template <typename F> cudaError_t by_access(int dtype, int i, F f) {
 }  // namespace
 
 cudaError_t launch_mx4_quantize(const Mx4Shape &m, const void *x, int dtype, int64_t ld, void *mx, cudaStream_t st) {
-    const QuantArgs a = quant_args(m, x, ld, mx);
+    QuantArgs a = quant_args(m, x, ld, mx);
     const unsigned units = quant_grid(m);
     return by_access(dtype, access_index(dtype, x, ld), [&](auto t, auto v) {
         const unsigned grid = std::min(units, static_cast<unsigned>(sm_count() * quant_ctas<decltype(t), v.value>()));
-        return launch_pdl(mx4_quantize_kernel<decltype(t), v.value>, dim3(grid), dim3(kWarps * 32), 0, st, 1, a, units);
+        a.step_ct = static_cast<int>(grid % m.col_tiles);
+        a.step_rest = static_cast<int>(grid / m.col_tiles);
+        return launch_pdl(mx4_quantize_kernel<decltype(t), v.value>, dim3(grid), dim3(kWarps * 32), 0, st, 1, a, static_cast<unsigned>(units / m.col_tiles));
     });
 }
 
@@ -343,7 +424,10 @@ cudaError_t launch_mx4_dequantize(const Mx4Shape &m, const void *mx, void *out, 
     const QuantArgs a = quant_args(m, nullptr, ld, const_cast<void *>(mx));
     return by_access(dtype, access_index(dtype, out, ld), [&](auto t, auto v) {
         using T = decltype(t);
-        return launch_pdl(mx4_dequantize_kernel<T, v.value>, dim3(quant_grid(m)), dim3(kWarps * 32), 0, st, 1, a, static_cast<T *>(out));
+        if constexpr (sizeof(T) * v.value < 4 || v.value == 1)
+            return launch_pdl(mx4_dequantize_single_kernel<T>, dim3(quant_grid(m)), dim3(kWarps * 32), 0, st, 1, a, static_cast<T *>(out));
+        else
+            return launch_pdl(mx4_dequantize_kernel<T, v.value>, dim3(quant_grid(m)), dim3(kWarps * 32), 0, st, 1, a, static_cast<T *>(out));
     });
 }
 

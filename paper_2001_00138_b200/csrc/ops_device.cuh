@@ -224,8 +224,9 @@ template <typename F> cudaError_t by_act(int act, F f) {
 }
 
 // The codes of eight values, the first in the lowest four bits; nearest even, magnitudes above 6 become 6.
-__device__ __forceinline__ uint32_t pack8(const float (&v)[8], float factor) {
+__device__ __forceinline__ uint32_t pack8(const Fv<8> &x, float factor) {
     uint32_t r;
+    const Fv<8> v = x * Fv<8>::all(factor);
     asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
         "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
         "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
@@ -233,8 +234,8 @@ __device__ __forceinline__ uint32_t pack8(const float (&v)[8], float factor) {
         "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
         "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
         : "=r"(r)
-        : "f"(v[0] * factor), "f"(v[1] * factor), "f"(v[2] * factor), "f"(v[3] * factor), "f"(v[4] * factor), "f"(v[5] * factor),
-          "f"(v[6] * factor), "f"(v[7] * factor));
+        : "f"(v.get(0)), "f"(v.get(1)), "f"(v.get(2)), "f"(v.get(3)), "f"(v.get(4)), "f"(v.get(5)),
+          "f"(v.get(6)), "f"(v.get(7)));
     return r;
 }
 // The eight values that such a word stands for, before scaling (exact in half).
@@ -275,7 +276,7 @@ __device__ __forceinline__ uint32_t top8(const float (&v)[8]) {
 }
 // Eight values of one lane -> its 4 bytes of codes; returns the block's scale byte (the same in the four lanes of a block).
 // `top`: bits of the lane's largest magnitude, sign clear (magnitudes compare like their bits, a NaN is above infinity).
-__device__ __forceinline__ uint32_t quantise8(const float (&v)[8], uint32_t top, uint32_t &codes) {
+__device__ __forceinline__ uint32_t quantise8(const Fv<8> &v, uint32_t top, uint32_t &codes) {
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     float inverse;
@@ -284,7 +285,7 @@ __device__ __forceinline__ uint32_t quantise8(const float (&v)[8], uint32_t top,
     return scale;
 }
 __device__ __forceinline__ uint32_t quantise8(const float (&v)[8], uint32_t &codes) {
-    return quantise8(v, top8(v), codes);
+    return quantise8(Fv<8>::make([&](int j) { return v[j]; }), top8(v), codes);
 }
 
 }  // namespace
