@@ -345,6 +345,18 @@ __global__ void __launch_bounds__(kWarps * 32) mx4_dequantize_single_kernel(Quan
     const uint8_t *scales_in = a.mx + a.scales_at + (rt * a.col_tiles + ct) * a.scale_bytes;
     const int cols = static_cast<int>(min(static_cast<int64_t>(a.width), a.cols - static_cast<int64_t>(ct) * a.width));
     pdl_wait();
+    uint32_t word[4][8], scale[4][8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = 32 * j + lane;
+            if (32 * j >= a.width) continue;           // (the whole tile is there to read, whatever rows and columns it holds)
+            int at = (r0 + 32 * k) * row_bytes + (c >> 3) * 4;
+            at ^= ((at >> 7) & (a.width / 32 - 1)) << 4;
+            word[k][j] = *reinterpret_cast<const uint32_t *>(codes_in + at);
+            scale[k][j] = scales_in[(c >> 7) * 512 + r0 * 16 + k * 4 + (j & 3)];
+        }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const int64_t row = rt * 128 + r0 + 32 * k;
@@ -353,12 +365,7 @@ __global__ void __launch_bounds__(kWarps * 32) mx4_dequantize_single_kernel(Quan
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int c = 32 * j + lane;
-            if (c >= cols) continue;
-            int at = (r0 + 32 * k) * row_bytes + (c >> 3) * 4;
-            at ^= ((at >> 7) & (a.width / 32 - 1)) << 4;
-            const uint32_t word = *reinterpret_cast<const uint32_t *>(codes_in + at) >> (4 * (c & 7));
-            const uint32_t scale = scales_in[(c >> 7) * 512 + r0 * 16 + k * 4 + (j & 3)];
-            dst[c] = from_float<T>(value_of(word & 15, scale_value(scale)));
+            if (c < cols) dst[c] = from_float<T>(value_of((word[k][j] >> (4 * (c & 7))) & 15, scale_value(scale[k][j])));
         }
     }
 }
