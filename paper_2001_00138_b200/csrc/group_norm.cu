@@ -341,6 +341,31 @@ __device__ __forceinline__ void write_mx4(const NormArgs &a, const T *tile, cons
     }
 }
 
+// act(norm) of a thread's pixels from shared memory.
+template <typename T, int V, int ACT>
+__device__ __forceinline__ void write_norm(const NormArgs &a, const T *tile, const float2 *fin, const float *gamma, const float *beta_of, int n, int64_t p0, int pixels,
+                                           int c0, int channels, const Place &q) {
+    const int col = q.col * V;
+    const Groups<V> at(col, a.per);
+    const Fv<V> shift = Fv<V>::make([&](int j) { return -fin[at.g[j]].x; });
+    const Fv<V> scale = Fv<V>::make([&](int j) { return fin[at.g[j]].y * gamma[col + j]; });
+    const Fv<V> beta = Fv<V>::make([&](int j) { return beta_of[col + j]; });
+    T *dst = static_cast<T *>(a.y) + n * a.y_image + (p0 + q.row) * a.y_pixel + c0 + q.col * V;
+    uint32_t src = shared_address(tile + q.row * channels + col);
+    const int64_t dst_step = q.rows * a.y_pixel;
+    const uint32_t src_step = q.rows * channels * sizeof(T);
+#pragma unroll 4
+    for (int p = q.row; p < pixels; p += q.rows, dst += dst_step, src += src_step) {
+        Pack<T, V> v;
+        v.load_shared(src);
+        narrow<T, V>(activate<ACT, V>(fma(widen<T, V>(v) + shift, scale, beta))).store(dst);
+    }
+}
+
+// A cluster's barrier in halves: nobody leaves before every CTA has read what it wants of the others' shared memory.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
 // ---- resident form ----------------------------------------------------------------------------------------------------
 // Shared memory: [chunk][slab] elements of x, then [rows][slab] float2, then [groups of the slab] float2 twice, then gamma and beta.
 template <typename T, int V, int ACT, bool MX>
@@ -401,27 +426,36 @@ __global__ void __launch_bounds__(kThreads, 3) norm_resident_kernel(NormArgs a) 
         fin[g] = make_float2(e.x, rstd);
         if (a.stats_out && rank == 0) reinterpret_cast<float2 *>(a.stats_out)[static_cast<int64_t>(n) * a.G + c0 / a.per + g] = fin[g];
     }
-    // fin is ready; nobody reads this CTA's grp after this point
-    if (a.cluster > 1) cluster.sync(); else __syncthreads();
-    if constexpr (MX) {
-        write_mx4<T, ACT>(a, tile, fin, gamma, beta_of, n, p0, pixels, c0, channels);
+    if (a.cluster > 1) cluster_arrive();               // the other CTAs' grp have been read
+    __syncthreads();
+    if constexpr (MX) write_mx4<T, ACT>(a, tile, fin, gamma, beta_of, n, p0, pixels, c0, channels);
+    else if (q.on) write_norm<T, V, ACT>(a, tile, fin, gamma, beta_of, n, p0, pixels, c0, channels, q);
+    if (a.cluster > 1) cluster_wait();
+}
+
+// Sums of red [rows][channels] over the rows, with all threads: part [kThreads]; out(channel, sum).
+template <typename F>
+__device__ __forceinline__ void sum_rows(const float2 *red, int rows, int channels, float2 *part, F out) {
+    const int parts = kThreads / channels;             // threads per channel
+    if (parts < 2) {
+        for (int c = threadIdx.x; c < channels; c += kThreads) {
+            float2 s = make_float2(0.f, 0.f);
+            for (int r = 0; r < rows; ++r) { s.x += red[r * channels + c].x; s.y += red[r * channels + c].y; }
+            out(c, s);
+        }
         return;
     }
-    if (!q.on || !a.y) return;
-    const int col = q.col * V;
-    const Groups<V> at(col, a.per);
-    const Fv<V> shift = Fv<V>::make([&](int j) { return -fin[at.g[j]].x; });
-    const Fv<V> scale = Fv<V>::make([&](int j) { return fin[at.g[j]].y * gamma[col + j]; });
-    const Fv<V> beta = Fv<V>::make([&](int j) { return beta_of[col + j]; });
-    T *dst = static_cast<T *>(a.y) + n * a.y_image + (p0 + q.row) * a.y_pixel + c0 + q.col * V;
-    uint32_t src = shared_address(tile + q.row * channels + col);
-    const int64_t dst_step = q.rows * a.y_pixel;
-    const uint32_t src_step = q.rows * channels * sizeof(T);
+    const int c = threadIdx.x % channels, p = threadIdx.x / channels;
+    float2 s = make_float2(0.f, 0.f);
+    if (p < parts) {
 #pragma unroll 4
-    for (int p = q.row; p < pixels; p += q.rows, dst += dst_step, src += src_step) {
-        Pack<T, V> v;
-        v.load_shared(src);
-        narrow<T, V>(activate<ACT, V>(fma(widen<T, V>(v) + shift, scale, beta))).store(dst);
+        for (int r = p; r < rows; r += parts) { s.x += red[r * channels + c].x; s.y += red[r * channels + c].y; }
+        part[threadIdx.x] = s;
+    }
+    __syncthreads();
+    if (p == 0) {
+        for (int k = 1; k < parts; ++k) { s.x += part[k * channels + c].x; s.y += part[k * channels + c].y; }
+        out(c, s);
     }
 }
 
@@ -435,6 +469,12 @@ struct Channels {
         shift = Fv<V>::make([&](int j) { return -st[at.g[j]].x; });
         scale = Fv<V>::make([&](int j) { return st[at.g[j]].y * a.gamma[c + j]; });
         beta = Fv<V>::make([&](int j) { return a.beta[c + j]; });
+    }
+    __device__ __forceinline__ void from_shared(const float2 *stats, const float *gamma, const float *beta_of, int c, int per) {
+        const Groups<V> at(c, per);
+        shift = Fv<V>::make([&](int j) { return -stats[at.g[j]].x; });
+        scale = Fv<V>::make([&](int j) { return stats[at.g[j]].y * gamma[c + j]; });
+        beta = Fv<V>::make([&](int j) { return beta_of[c + j]; });
     }
     template <int ACT, typename T>
     __device__ __forceinline__ void slope(const Pack<T, V> &x, const Pack<T, V> &dy, Fv<V> &d, Fv<V> &dz) const {
@@ -485,7 +525,8 @@ __device__ __forceinline__ void sums_of(Stream<T, V, KEEP, 2> &x, Stream<T, V, K
     }
 }
 
-// Shared memory: [chunk][slab] elements of x, the same of dy, [rows][slab] float2, [slab] float2 twice, [groups] float2.
+// Shared memory: [chunk][slab] elements of x, the same of dy, [rows][slab] float2, [slab] float2, [max(slab, kThreads)] float2,
+// [groups] float2 twice, gamma and beta.
 template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kThreads, 3) norm_grad_resident_kernel(NormArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
@@ -503,57 +544,77 @@ __global__ void __launch_bounds__(kThreads, 3) norm_grad_resident_kernel(NormArg
     T *dt = reinterpret_cast<T *>(smem + tile_bytes);
     float2 *red = reinterpret_cast<float2 *>(smem + 2 * tile_bytes);
     float2 *sums = red + kThreads * V;                 // this CTA's (A, B) per channel
-    float2 *whole = sums + a.slab;                     // the image's (A, B) per channel
-    float2 *fin = whole + a.slab;                      // (rstd * s1, rstd^2 * s2) per group
+    float2 *whole = sums + a.slab;                     // the image's (A, B) per channel; before that, parts of this CTA's
+    float2 *fin = whole + max(a.slab, kThreads);       // (rstd * s1, rstd^2 * s2) per group
+    float2 *stats = fin + a.slab / a.per;              // (mean, rstd) per group
+    float *gamma = reinterpret_cast<float *>(stats + a.slab / a.per), *beta = gamma + a.slab;
+    const int groups = channels / a.per;
     pdl_wait();
 
+    for (int g = threadIdx.x; g < groups; g += kThreads)               // in flight together with x and dy
+        copy_async<8>(shared_address(stats + g), reinterpret_cast<const float2 *>(a.stats_in) + static_cast<int64_t>(n) * a.G + c0 / a.per + g);
+    for (int c = threadIdx.x; c < channels; c += kThreads) {
+        copy_async<4>(shared_address(gamma + c), a.gamma + c0 + c);
+        copy_async<4>(shared_address(beta + c), a.beta + c0 + c);
+    }
+    copies_commit();
+    using S = Stream<T, V, true, 2>;
+    S x, dy;
+    int count = 0;
+    if (q.on) {
+        x.begin(static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + c0 + q.col * V, a.x_pixel, pixels, q, xt, channels, q.col * V);
+        dy.begin(static_cast<const T *>(a.dy) + n * a.y_image + p0 * a.y_pixel + c0 + q.col * V, a.y_pixel, pixels, q, dt, channels, q.col * V);
+        count = start_copies(x, dy);
+        copies_wait<S::kDepth>();                      // the constants: committed before kDepth batches
+    } else {
+        copies_wait<0>();
+    }
+    __syncthreads();
     Channels<V> f;
     if (q.on) {
         Fv<V> sa, sb;
-        Stream<T, V, true, 2> x, dy;
-        x.begin(static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + c0 + q.col * V, a.x_pixel, pixels, q, xt, channels, q.col * V);
-        dy.begin(static_cast<const T *>(a.dy) + n * a.y_image + p0 * a.y_pixel + c0 + q.col * V, a.y_pixel, pixels, q, dt, channels, q.col * V);
-        const int count = start_copies(x, dy);
-        f.load(a, n, c0 + q.col * V);                  // (arrives with the first copies)
+        f.from_shared(stats, gamma, beta, q.col * V, a.per);
         sums_of<T, V, ACT, true>(x, dy, count, f, sa, sb);
 #pragma unroll
         for (int j = 0; j < V; ++j) red[q.row * channels + q.col * V + j] = make_float2(sa.get(j), sb.get(j));
     }
     __syncthreads();
-    for (int c = threadIdx.x; c < channels; c += kThreads) {
-        float2 s = make_float2(0.f, 0.f);
-        for (int r = 0; r < q.rows; ++r) {
-            const float2 e = red[r * channels + c];
-            s.x += e.x; s.y += e.y;
-        }
-        s.y *= reinterpret_cast<const float2 *>(a.stats_in)[static_cast<int64_t>(n) * a.G + (c0 + c) / a.per].y;
-        sums[c] = s;
-    }
+    sum_rows(red, q.rows, channels, whole, [&](int c, float2 s) { sums[c] = make_float2(s.x, s.y * stats[c / a.per].y); });
     cg::cluster_group cluster = cg::this_cluster();
     if (a.cluster > 1) cluster.sync(); else __syncthreads();
     for (int c = threadIdx.x; c < channels; c += kThreads) {
-        float2 s = make_float2(0.f, 0.f);
-        for (int r = 0; r < a.cluster; ++r) {
-            const float2 e = cluster.map_shared_rank(sums, r)[c];
-            s.x += e.x; s.y += e.y;
+        float2 s = sums[c];
+        if (a.cluster > 1) {
+            float2 all[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) all[r] = r < a.cluster ? cluster.map_shared_rank(sums, r)[c] : make_float2(0.f, 0.f);
+            s = all[0];
+#pragma unroll
+            for (int r = 1; r < 8; ++r) { s.x += all[r].x; s.y += all[r].y; }
         }
         whole[c] = s;
         if (rank == 0) reinterpret_cast<float2 *>(a.ws)[static_cast<int64_t>(n) * a.C + c0 + c] = s;
     }
+    if (a.cluster > 1) cluster_arrive();               // the other CTAs' sums have been read
     __syncthreads();
-    for (int g = threadIdx.x; g < channels / a.per; g += kThreads) {
+    if (rank == 0 && threadIdx.x == kThreads - 1) {    // (its latency lies beside the rest of the work)
+        __threadfence();
+        last = atomicAdd(a.counters + slab, 1u) == static_cast<unsigned>(a.N) - 1;
+        if (last) a.counters[slab] = 0;
+        __threadfence();
+    }
+    for (int g = threadIdx.x; g < groups; g += kThreads) {
         float s1 = 0.f, s2 = 0.f;
         for (int c = 0; c < a.per; ++c) {
-            const float gm = a.gamma[c0 + g * a.per + c];
+            const float gm = gamma[g * a.per + c];
             const float2 e = whole[g * a.per + c];
             s1 = fmaf(gm, e.x, s1);
             s2 = fmaf(gm, e.y, s2);
         }
-        const float rstd = reinterpret_cast<const float2 *>(a.stats_in)[static_cast<int64_t>(n) * a.G + c0 / a.per + g].y;
+        const float rstd = stats[g].y;
         fin[g] = make_float2(rstd * (s1 * a.inv_count), rstd * rstd * (s2 * a.inv_count));
     }
-    // fin is ready; nobody reads this CTA's sums after this point
-    if (a.cluster > 1) cluster.sync(); else __syncthreads();
+    __syncthreads();
     if (q.on) {
         const Groups<V> at(q.col * V, a.per);
         const Fv<V> nk1 = Fv<V>::make([&](int j) { return -fin[at.g[j]].x; });
@@ -571,26 +632,18 @@ __global__ void __launch_bounds__(kThreads, 3) norm_grad_resident_kernel(NormArg
         }
     }
     // The last cluster of this slab to get here adds the images up, in ascending order: the result does not depend on which is last.
-    if (rank != 0) return;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence();
-        last = atomicAdd(a.counters + slab, 1u) == static_cast<unsigned>(a.N) - 1;
-        if (last) a.counters[slab] = 0;
-        __threadfence();
-    }
-    __syncthreads();
-    if (!last) return;
-    for (int c = c0 + threadIdx.x; c < c0 + channels; c += kThreads) {
-        float sa = 0.f, sb = 0.f;
+    if (rank == 0 && last)                             // (`last` was written before the barrier above)
+        for (int c = c0 + threadIdx.x; c < c0 + channels; c += kThreads) {
+            float sa = 0.f, sb = 0.f;
 #pragma unroll 8
-        for (int i = 0; i < a.N; ++i) {
-            const float2 e = __ldcg(reinterpret_cast<const float2 *>(a.ws) + static_cast<int64_t>(i) * a.C + c);
-            sa += e.x; sb += e.y;
+            for (int i = 0; i < a.N; ++i) {
+                const float2 e = __ldcg(reinterpret_cast<const float2 *>(a.ws) + static_cast<int64_t>(i) * a.C + c);
+                sa += e.x; sb += e.y;
+            }
+            a.dbeta[c] = sa;
+            a.dgamma[c] = sb;
         }
-        a.dbeta[c] = sa;
-        a.dgamma[c] = sb;
-    }
+    if (a.cluster > 1) cluster_wait();
 }
 
 // ---- two-pass form ----------------------------------------------------------------------------------------------------
@@ -745,15 +798,8 @@ __global__ void __launch_bounds__(kThreads, 3) norm_grad_sums_kernel(NormArgs a)
     }
     __syncthreads();
     float2 *out = reinterpret_cast<float2 *>(a.ws) + (static_cast<int64_t>(n) * a.chunks + blockIdx.x) * a.C + s.c0;
-    for (int c = threadIdx.x; c < s.channels; c += kThreads) {
-        float2 t = make_float2(0.f, 0.f);
-        for (int r = 0; r < q.rows; ++r) {
-            const float2 e = red[r * s.channels + c];
-            t.x += e.x; t.y += e.y;
-        }
-        t.y *= reinterpret_cast<const float2 *>(a.stats_in)[static_cast<int64_t>(n) * a.G + (s.c0 + c) / a.per].y;
-        out[c] = t;
-    }
+    const float2 *st = reinterpret_cast<const float2 *>(a.stats_in) + static_cast<int64_t>(n) * a.G;
+    sum_rows(red, q.rows, s.channels, red + kThreads * V, [&](int c, float2 t) { out[c] = make_float2(t.x, t.y * st[(s.c0 + c) / a.per].y); });
 }
 
 // One CTA per (group, image of the run): sums the chunks, writes (rstd s1, rstd^2 s2) of the group behind the partial sums and the
@@ -850,7 +896,7 @@ __global__ void __launch_bounds__(kThreads, 3) norm_grad_apply_kernel(NormArgs a
 int resident_smem(const NormShape &s, int width, int tensors, int slab, int64_t chunk) {
     const int64_t tile = (chunk * slab * elem_bytes(s.dtype) + 15) / 16 * 16;
     const int64_t groups = slab / (s.C / s.G);
-    const int64_t small = tensors == 1 ? 2 * groups + slab : 2 * slab + groups;   // (gamma and beta: a float2's worth per channel)
+    const int64_t small = 2 * groups + slab + (tensors == 1 ? 0 : slab + std::max(slab, kThreads));   // float2 (gamma and beta: one per channel)
     const int64_t total = tensors * tile + (static_cast<int64_t>(kThreads) * width + small) * 8;
     return total > (int64_t(1) << 30) ? (1 << 30) : static_cast<int>(total);
 }
@@ -918,7 +964,7 @@ NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
 // Dynamic shared memory of the two-pass kernels: the rings, and over them the per-thread results.
 template <typename T, int V, int TENSORS> constexpr size_t ring_smem() {
     using S = Stream<T, V, false, TENSORS>;
-    return static_cast<size_t>(kThreads) * std::max(8 * V, TENSORS * S::kDepth * S::kBatch * S::kBytes);
+    return static_cast<size_t>(kThreads) * std::max(8 * (V + 1), TENSORS * S::kDepth * S::kBatch * S::kBytes);   // (and a float2 each for sum_rows)
 }
 
 // A plan needs the vector width to divide the channels, and each group's where a group is wider than a CTA.
