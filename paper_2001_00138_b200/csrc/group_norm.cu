@@ -255,33 +255,41 @@ __device__ __forceinline__ void put_moments(const Moments<V> &m, const Place &q,
         }
 }
 
-// Joins the entries of red, `width` per group and row, per group.  A warp takes a group at a time: first the mean over all its
-// entries, then the squared deviations around it.  grp[g * stride] = (mean, m2).
+// Joins the entries of red, `width` per group and row, per group: first the mean over a group's entries, then the squared deviations
+// around it.  Teams of 1 to 32 neighbouring lanes share a group, as many as there are threads for.  grp[g * stride] = (mean, m2).
 template <int V>
 __device__ __forceinline__ void join_groups(const float2 *red, int rows, int channels, int per, int pixels, float2 *grp, int64_t stride = 1) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int joined = joined_channels<V>(per), width = per / joined, pitch = channels / joined;
     const int groups = channels / per;
-    const float inv_total = 1.f / (static_cast<float>(pixels) * static_cast<float>(width));
+    int team = 32;
+    while (team > 1 && groups * team > kThreads) team >>= 1;
+    const int member = threadIdx.x & (team - 1);
     const int base = pixels / rows, extra = pixels - base * rows;      // row r visited base pixels, or one more
-    const int items = min(rows, pixels) * width;
-    const float many = static_cast<float>(joined);
-    for (int g = warp; g < groups; g += kThreads / 32) {
-        float s = 0.f, q = 0.f;
+    const int used = min(rows, pixels);
+    const float inv_total = 1.f / (static_cast<float>(pixels) * static_cast<float>(width)), many = static_cast<float>(joined);
+    for (int g0 = 0; g0 < groups; g0 += kThreads / team) {             // (the same for all threads)
+        const int g = g0 + threadIdx.x / team;
         const float2 *from = red + g * width;
-        for (int i = lane; i < items; i += 32) {
-            const int r = i / width;
-            s = fmaf(static_cast<float>(base + (r < extra)), from[r * pitch + i - r * width].x, s);
-        }
-        const float mean = warp_sum(s) * inv_total;
-        for (int i = lane; i < items; i += 32) {
-            const int r = i / width;
-            const float2 e = from[r * pitch + i - r * width];
-            const float d = e.x - mean;
-            q += fmaf(static_cast<float>(base + (r < extra)) * many * d, d, e.y);
-        }
-        q = warp_sum(q);
-        if (lane == 0) grp[g * stride] = make_float2(mean, q);
+        float s = 0.f, q = 0.f;
+        if (g < groups)
+            for (int r = member; r < used; r += team) {
+                float t = 0.f;
+                for (int c = 0; c < width; ++c) t += from[r * pitch + c].x;
+                s = fmaf(static_cast<float>(base + (r < extra)), t, s);
+            }
+        for (int o = team >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        const float mean = s * inv_total;
+        if (g < groups)
+            for (int r = member; r < used; r += team) {
+                const float n = static_cast<float>(base + (r < extra)) * many;
+                for (int c = 0; c < width; ++c) {
+                    const float2 e = from[r * pitch + c];
+                    const float d = e.x - mean;
+                    q += fmaf(n * d, d, e.y);
+                }
+            }
+        for (int o = team >> 1; o > 0; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
+        if (member == 0 && g < groups) grp[g * stride] = make_float2(mean, q);
     }
 }
 
@@ -904,9 +912,11 @@ int resident_smem(const NormShape &s, int width, int tensors, int slab, int64_t 
 constexpr int kSmemMost = 220 * 1024;       // dynamic shared memory of one CTA
 constexpr int64_t kRunBytes = int64_t(64) << 20;   // two-pass: bytes of x (and dy) of the images that are taken together
 
-// Picks the slab and the cluster of the resident form by a time estimate: the CTAs of an SM move its share of the HBM rate (44
-// bytes per ns) if there are at least three of them, less if there are fewer; every wave pays a fixed latency.
-// Slabs narrower than 128 bytes cost more per byte.  `unit`: slabs are a multiple of so many channels (or all of them).
+// Picks the slab and the cluster of the resident form by a time estimate, fitted to measurements of ten shapes with every slab and
+// cluster that fits (7x7 to 56x56 pixels, 64 to 512 channels, the three types, both directions; its choice was the fastest or within
+// 3 % of it): the CTAs of an SM share its HBM rate of 44 bytes per ns; a wave costs half a microsecond, a cluster one more and 0.3 per
+// doubling; slabs narrower than 128 bytes cost 10 %; the gradient, bound by its arithmetic, wants three CTAs per SM.
+// `unit`: slabs are a multiple of so many channels (or all of them).
 NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
     NormPlan best;
     const int per = s.C / s.G, e = elem_bytes(s.dtype);
@@ -923,11 +933,11 @@ NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
             if (smem > kSmemMost || static_cast<int64_t>(s.N) * (s.G / k) * cl > INT32_MAX) continue;
             const int per_sm = std::min(3, (224 * 1024) / (smem + 1024));
             const double ctas = static_cast<double>(s.N) * (s.G / k) * cl;
-            const double waves = std::ceil(ctas / (148.0 * per_sm));
-            const double busy = std::min<double>(per_sm, ctas / 148.0 / waves);     // CTAs of an SM at a time
+            const double here = std::min<double>(per_sm, std::ceil(ctas / 148));           // CTAs of an SM at a time
+            const double waves = std::ceil(ctas / (148 * here));
             const double bytes = static_cast<double>(chunk) * slab * e * (tensors + 1);
-            const double rate = 44e3 * std::min(1.0, (0.1 + 0.3 * std::max(1.0, busy))) * (slab * e < 128 && k < s.G ? 0.85 : 1.0);
-            const double us = waves * (std::max(1.0, busy) * bytes / rate + 2.0 + (cl > 1 ? 0.7 : 0.0));
+            const double us = waves * (here * bytes / 44e3 * (slab * e < 128 && k < s.G ? 1.1 : 1.0) * (tensors == 2 ? 1 + 0.4 * (3 - here) : 1.0) +
+                                       0.5 + (cl > 1 ? 1.0 + 0.3 * std::log2(cl) : 0.0));
             if (us < best_us) {
                 best_us = us;
                 best.resident = true; best.slab = static_cast<int>(slab); best.slabs = s.G / k; best.cluster = cl;
@@ -950,7 +960,8 @@ NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
         best.slabs = static_cast<int>(ceil_div(s.G, k));
     }
     const int64_t image = s.P * s.C * e * tensors;     // bytes
-    best.run = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(s.N, kRunBytes / image)));
+    const int64_t runs = ceil_div(s.N, std::max<int64_t>(1, std::min<int64_t>(s.N, kRunBytes / image)));
+    best.run = static_cast<int>(ceil_div(s.N, runs));  // runs of about the same number of images
     // one wave of three CTAs per SM over a run: a last, partly filled wave would cost as much as a full one
     const int64_t share = 148 * 3 / (static_cast<int64_t>(best.run) * best.slabs);         // CTAs per (image, slab)
     const int64_t each = std::max<int64_t>(1, share);

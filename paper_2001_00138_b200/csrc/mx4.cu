@@ -49,61 +49,6 @@ struct Raw {
     __device__ __forceinline__ float get(int i) const { return to_float(v[i / A].v[i % A]); }
 };
 
-// Eight columns of a row as 32-bit words, in accesses of A elements.
-template <typename T, int A>
-struct Row8 {
-    static constexpr int kWords = 8 * sizeof(T) / 4;
-    uint32_t w[kWords];
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) w[i] = 0;
-    }
-    __device__ __forceinline__ void load(const T *p) {
-        if constexpr (sizeof(T) * A >= 4) {
-            constexpr int kPer = sizeof(T) * A / 4;    // words per access
-#pragma unroll
-            for (int i = 0; i < 8 / A; ++i) {
-                Pack<T, A> t;
-                t.load(p + i * A);
-#pragma unroll
-                for (int k = 0; k < kPer; ++k) w[i * kPer + k] = t.w[k];
-            }
-        } else {
-            load(p, 8);
-        }
-    }
-    __device__ __forceinline__ void load(const T *p, int count) {      // the first `count`, zeros after them
-        clear();
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < count) {
-                if constexpr (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
-                else w[i / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t *>(p)[i]) << (16 * (i & 1));
-            }
-    }
-    __device__ __forceinline__ Fv<8> values() const {
-        Pack<T, 8> t;
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) t.w[i] = w[i];
-        return widen<T, 8>(t);
-    }
-    // bits of the largest magnitude; two 16-bit values are compared at a time
-    __device__ __forceinline__ uint32_t top() const {
-        if constexpr (sizeof(T) == 4) {
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-            return top8(v);
-        } else {
-            uint32_t t = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
-            t = max(t & 0xffffu, t >> 16);
-            if constexpr (std::is_same<T, __nv_bfloat16>::value) return t << 16;
-            const uint16_t one = static_cast<uint16_t>(t);
-            return __float_as_uint(__half2float(*reinterpret_cast<const __half *>(&one)));
-        }
-    }
-};
-
 // CTAs per SM that the registers of two row sets allow
 template <typename T, int A> __host__ __device__ constexpr int quant_ctas() { return sizeof(T) == 4 || A == 1 ? 3 : 4; }
 

@@ -78,7 +78,12 @@ __device__ __forceinline__ void store_out(void *y, int64_t at, float v, int dtyp
 }
 
 // One tile of 128 weights rows x tile_n rows of x per CTA; the column tiles cut into `splits` ranges, one CTA of a cluster each.
+// X = void: the rows of x are 4-bit.  Otherwise they are elements of X, at most kFusedRows of them, and warps 2 to 7 quantise them
+// into the ring themselves, a column tile at a time each: one launch less.  Measured, half, 4096 -> 4096: 1 row 5.0 us against 6.4 us as
+// two launches, 8 rows 5.9 / 6.8; 25088 -> 4096: 10.0 / 12.1, 8 rows 12.0 / 12.5 (fp32 12.2 / 11.9, where it ends).
+template <typename X>
 __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p) {
+    constexpr bool kFused = !std::is_same<X, void>::value;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 1];
     __shared__ uint32_t tmem_slot;
@@ -98,7 +103,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
-            mbar_init(full + 8 * s, 1);
+            mbar_init(full + 8 * s, kFused ? 2 : 1);                     // the copies, and the warp that wrote the rows of x
             mbar_init(empty + 8 * s, 1);
         }
         mbar_init(done, 1);
@@ -116,15 +121,14 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
     const int t0 = rank * p.tiles_per_split, t1 = min(p.col_tiles, t0 + p.tiles_per_split);
     const int iters = max(0, t1 - t0);
     const int64_t x_tile0 = static_cast<int64_t>(nt) * p.tile_n / 128;
-    const int x_row0 = static_cast<int>(static_cast<int64_t>(nt) * p.tile_n % 128);
 
     if (warp == 0) {
         const bool leader = elect_one();
-        const uint32_t bytes = a_codes + b_codes + 2 * sf_bytes;
+        const uint32_t bytes = kFused ? a_codes + sf_bytes : a_codes + b_codes + 2 * sf_bytes;
         // (ring slots and phases advance without divisions: the instructions of this warp bound short column tiles)
         const uint8_t *wc = p.w + (static_cast<int64_t>(ft) * p.col_tiles + t0) * a_codes;
         const uint8_t *ws = p.w + p.w_scales + (static_cast<int64_t>(ft) * p.col_tiles + t0) * sf_bytes;
-        const uint8_t *xc = p.x + (x_tile0 * p.col_tiles + t0) * a_codes + x_row0 * row_bytes;
+        const uint8_t *xc = p.x + (x_tile0 * p.col_tiles + t0) * a_codes;
         const uint8_t *xs = p.x + p.x_scales + (x_tile0 * p.col_tiles + t0) * sf_bytes;
         auto load_w = [&](uint32_t at, uint32_t bar) {
             if (leader) {
@@ -136,7 +140,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
             ws += sf_bytes;
         };
         auto load_x = [&](uint32_t at, uint32_t bar) {
-            if (leader) {
+            if (leader && !kFused) {
                 bulk_load(at + a_codes, xc, b_codes, bar);
                 bulk_load(at + a_codes + b_codes + sf_bytes, xs, sf_bytes, bar);
             }
@@ -190,6 +194,40 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
             if (++slot == p.stages) { slot = 0; phase ^= 1; }
         }
         if (leader) umma_commit(done);
+    } else if constexpr (kFused) {
+        constexpr int kProducers = kLinThreads / 32 - 2, A = 16 / sizeof(X);
+        const X *x = static_cast<const X *>(p.x_raw);
+        const bool vector = (reinterpret_cast<uintptr_t>(x) | static_cast<uint64_t>(p.ldx * sizeof(X))) % 16 == 0;
+        const int rows = static_cast<int>(p.rows);
+        pdl_wait();
+        for (int i = warp - 2; i < iters; i += kProducers) {
+            const int slot = i % p.stages, turn = i / p.stages;
+            const int64_t c = static_cast<int64_t>(t0 + i) * p.width + lane * 8;
+            const int count = lane * 8 < p.width ? static_cast<int>(max(int64_t(0), min(int64_t(8), p.K - c))) : 0;
+            Row8<X, A> raw[kFusedRows];
+#pragma unroll
+            for (int r = 0; r < kFusedRows; ++r) {
+                const X *src = x + r * p.ldx + c;
+                if (vector && count == 8 && r < rows) raw[r].load(src);
+                else raw[r].load(src, r < rows ? count : 0);
+            }
+            if (turn > 0 && !warp_wait(empty + 8 * slot, (turn - 1) & 1, ctx, 105)) break;
+            unsigned char *at = smem_raw + (smem - smem_u32(smem_raw)) + slot * stage_bytes + a_codes;
+#pragma unroll
+            for (int r = 0; r < kFusedRows; ++r) {
+                if (r >= rows) break;
+                uint32_t codes, scales = quantise8(raw[r].values(), raw[r].top(), codes);
+                int place = r * row_bytes + lane * 4;
+                place ^= ((place >> 7) & (p.width / 32 - 1)) << 4;
+                if (lane * 8 < p.width) *reinterpret_cast<uint32_t *>(at + place) = codes;
+                scales |= __shfl_down_sync(0xffffffffu, scales, 4) << 8;
+                scales |= __shfl_down_sync(0xffffffffu, scales, 8) << 16;
+                if ((lane & 15) == 0 && lane * 8 < p.width) *reinterpret_cast<uint32_t *>(at + b_codes + sf_bytes + (lane >> 4) * 512 + r * 16) = scales;
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the tensor cores read them through the asynchronous proxy
+            __syncwarp();
+            if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full + 8 * slot) : "memory");
+        }
     }
     __syncwarp();
     pdl_wait();
@@ -214,7 +252,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
         // every CTA of the cluster finishes the columns j with j % splits == its rank: partial sums are pushed into its shared memory
         // and added in rank order
         float *slots = reinterpret_cast<float *>(smem_raw + (smem - smem_u32(smem_raw)));
-        const int owned = (p.tile_n + p.splits - 1) / p.splits;
+        const int shift = 31 - __clz(p.splits), owned = (p.tile_n + p.splits - 1) >> shift;      // splits is a power of two
         cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();                                                  // all pipelines are idle: their memory can be reused
         for (int c = (warp >> 2) * 16; c < p.tile_n; c += 32) {
@@ -223,17 +261,19 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
 #pragma unroll
             for (int j = 0; j < 16; ++j)
                 if (row0 + c + j < p.rows) {
-                    float *to = cluster.map_shared_rank(slots, (c + j) % p.splits);
-                    to[(rank * owned + (c + j) / p.splits) * 128 + (warp & 3) * 32 + lane] = iters ? __uint_as_float(v[j]) : 0.f;
+                    float *to = cluster.map_shared_rank(slots, (c + j) & (p.splits - 1));
+                    to[(rank * owned + ((c + j) >> shift)) * 128 + (warp & 3) * 32 + lane] = iters ? __uint_as_float(v[j]) : 0.f;
                 }
         }
         cluster.sync();
         if (ok && f < p.F)
             for (int j = (warp >> 2); j < owned; j += 2) {
-                const int64_t row = row0 + j * p.splits + rank;
-                if (j * p.splits + rank >= p.tile_n || row >= p.rows) break;
+                const int64_t row = row0 + (j << shift) + rank;
+                if ((j << shift) + rank >= p.tile_n || row >= p.rows) break;
                 float s = 0.f;
-                for (int r = 0; r < p.splits; ++r) s += slots[(r * owned + j) * 128 + (warp & 3) * 32 + lane];
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r < p.splits) s += slots[(r * owned + j) * 128 + (warp & 3) * 32 + lane];
                 store_out(p.y, row * p.ldy + f, activate(s + bias, p.act), p.dtype);
             }
     }
@@ -496,7 +536,11 @@ constexpr int kLinearSmem = 226 * 1024;
 }  // namespace
 
 cudaError_t prepare_mx4_linear() {
-    cudaError_t e = cudaFuncSetAttribute(mx4_linear_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinearSmem);
+    const cudaFuncAttribute what = cudaFuncAttributeMaxDynamicSharedMemorySize;
+    cudaError_t e = cudaFuncSetAttribute(mx4_linear_kernel<void>, what, kLinearSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(mx4_linear_kernel<float>, what, kLinearSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(mx4_linear_kernel<__half>, what, kLinearSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(mx4_linear_kernel<__nv_bfloat16>, what, kLinearSmem);
     for (int dtype = 0; dtype < 3 && e == cudaSuccess; ++dtype)
         for (int act = PATDNN_ACT_NONE; act <= PATDNN_ACT_SILU && e == cudaSuccess; ++act)
             e = by_output(dtype, act, [](auto t, auto a) {
@@ -511,7 +555,7 @@ cudaError_t launch_mx4_linear(Mx4Params p, cudaStream_t st, int *launches) {
     // Many rows: as soon as tiles of 128 x 256 (or 128 x 128) fill the SMs, the persistent kernel.
     const int64_t row_tiles = ceil_div(p.rows, 128);
     const int tile_f = p.F > 128 && row_tiles * ceil_div(p.F, 256) >= sm_count() ? 256 : 128;
-    if (p.rows > 64 && row_tiles * ceil_div(p.F, tile_f) >= sm_count()) {
+    if (!p.x_raw && p.rows > 64 && row_tiles * ceil_div(p.F, tile_f) >= sm_count()) {
         p.tile_n = tile_f;
         p.f_tiles = static_cast<int>(ceil_div(p.F, tile_f));
         p.n_tiles = static_cast<int>(row_tiles);
@@ -529,6 +573,7 @@ cudaError_t launch_mx4_linear(Mx4Params p, cudaStream_t st, int *launches) {
         });
     }
     p.f_tiles = static_cast<int>(ceil_div(p.F, 128));
+    // (row tiles start at multiples of 128: the scales of a tile start at a column of tensor memory that is a multiple of four)
     p.tile_n = p.rows <= 128 ? static_cast<int>(ceil_div(p.rows, 16) * 16) : 128;
     p.n_tiles = static_cast<int>(ceil_div(p.rows, p.tile_n));
     const int64_t tiles = static_cast<int64_t>(p.f_tiles) * p.n_tiles;
@@ -539,7 +584,9 @@ cudaError_t launch_mx4_linear(Mx4Params p, cudaStream_t st, int *launches) {
     p.stages = std::max(1, std::min({kMaxStages, p.tiles_per_split, 200 * 1024 / stage}));
     const int slots = p.splits > 1 ? static_cast<int>(ceil_div(p.tile_n, p.splits)) * p.splits * 512 : 0;
     const int smem = std::max(p.stages * stage, slots) + 1024;
-    return launch_pdl(mx4_linear_kernel, dim3(static_cast<unsigned>(tiles * p.splits)), dim3(kLinThreads), smem, st, p.splits, p);
+    const auto kernel = !p.x_raw ? mx4_linear_kernel<void> : p.dtype == PATDNN_F32 ? mx4_linear_kernel<float>
+                        : p.dtype == PATDNN_F16 ? mx4_linear_kernel<__half> : mx4_linear_kernel<__nv_bfloat16>;
+    return launch_pdl(kernel, dim3(static_cast<unsigned>(tiles * p.splits)), dim3(kLinThreads), smem, st, p.splits, p);
 }
 
 }  // namespace patdnn

@@ -85,6 +85,8 @@ cudaError_t launch_norm_quantize(const NormShape &s, const Mx4Shape &m, const vo
 // ---- 4-bit product (mx4_linear.cu) ------------------------------------------------------------------------------------
 struct Mx4Params {
     const uint8_t *w, *x;                   // 4-bit matrices [F][K], [rows][K] in the layout above
+    const void *x_raw;                      // or (x == nullptr) at most kFusedRows rows of x as they are, ldx elements apart
+    int64_t ldx, K;
     const float *bias;                      // [F] or nullptr
     void *y;
     int *status;
@@ -99,6 +101,7 @@ struct Mx4Params {
     int step_n, step_f;                     // persistent kernel: from a CTA's tile to its next one
     uint32_t spin_limit;
 };
+constexpr int kFusedRows = 8;               // rows that the product's kernel quantises itself
 cudaError_t prepare_mx4_linear();                       // opt in to the dynamic shared memory
 cudaError_t launch_mx4_linear(Mx4Params p, cudaStream_t st, int *launches);
 

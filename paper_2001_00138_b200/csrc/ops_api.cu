@@ -65,11 +65,12 @@ template <typename T> cudaError_t allocate(T **p, size_t count) {
     return e;
 }
 
-int product(patdnn_linear h, const Mx4Shape &xs, const void *mx, int64_t rows, void *y, int64_t ldy, cudaStream_t st) {
+// mx: 4-bit rows, or nullptr with the rows themselves at x
+int product(patdnn_linear h, const void *mx, const void *x, int64_t ldx, int64_t rows, void *y, int64_t ldy, cudaStream_t st) {
     if (ceil_div(rows, 128) * ceil_div(h->d.F, 128) > INT32_MAX / 8) return PATDNN_E_SHAPE;   // CTAs of one launch
     Mx4Params p{};
-    p.w = h->w; p.x = static_cast<const uint8_t *>(mx); p.bias = h->bias; p.y = y; p.status = h->status;
-    p.ldy = ldy; p.rows = rows; p.w_scales = h->shape.scales_at; p.x_scales = xs.scales_at;
+    p.w = h->w; p.x = static_cast<const uint8_t *>(mx); p.x_raw = x; p.ldx = ldx; p.K = h->d.K; p.bias = h->bias; p.y = y; p.status = h->status;
+    p.ldy = ldy; p.rows = rows; p.w_scales = h->shape.scales_at; p.x_scales = mx4_shape(rows, h->d.K).scales_at;
     p.F = h->d.F; p.width = h->shape.width; p.col_tiles = static_cast<int>(h->shape.col_tiles);
     p.ksteps = static_cast<int>(ceil_div(h->d.K, 64));
     p.act = h->d.act; p.dtype = h->d.dtype;
@@ -235,9 +236,9 @@ int patdnn_linear_run(patdnn_linear h, const void *x, int64_t rows, int64_t ldx,
     if (rows == 0) return PATDNN_OK;
     if (!x || !y) return PATDNN_E_NULL;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const Mx4Shape xs = mx4_shape(rows, h->d.K);
-    const int rc = launched(launch_mx4_quantize(xs, x, h->d.dtype, ldx, h->x, st), 1, "4-bit quantisation launch");
-    return rc ? rc : product(h, xs, h->x, rows, y, ldy, st);
+    if (rows <= kFusedRows) return product(h, nullptr, x, ldx, rows, y, ldy, st);
+    const int rc = launched(launch_mx4_quantize(mx4_shape(rows, h->d.K), x, h->d.dtype, ldx, h->x, st), 1, "4-bit quantisation launch");
+    return rc ? rc : product(h, h->x, nullptr, 0, rows, y, ldy, st);
 }
 
 int patdnn_linear_run_mx4(patdnn_linear h, const void *mx, int64_t rows, void *y, int64_t ldy, void *stream) {
@@ -246,7 +247,7 @@ int patdnn_linear_run_mx4(patdnn_linear h, const void *mx, int64_t rows, void *y
     if (!mx_size_ok(rows, h->d.K) || ldy < h->d.F || !aligned(mx, 16)) return PATDNN_E_SHAPE;
     if (rows == 0) return PATDNN_OK;
     if (!mx || !y) return PATDNN_E_NULL;
-    return product(h, mx4_shape(rows, h->d.K), mx, rows, y, ldy, static_cast<cudaStream_t>(stream));
+    return product(h, mx, nullptr, 0, rows, y, ldy, static_cast<cudaStream_t>(stream));
 }
 
 int patdnn_linear_check(patdnn_linear h) {
