@@ -916,11 +916,17 @@ constexpr int64_t kRunBytes = int64_t(64) << 20;   // two-pass: bytes of x (and 
 // cluster that fits (7x7 to 56x56 pixels, 64 to 512 channels, the three types, both directions; its choice was the fastest or within
 // 3 % of it): the CTAs of an SM share its HBM rate of 44 bytes per ns; a wave costs half a microsecond, a cluster one more and 0.3 per
 // doubling; slabs narrower than 128 bytes cost 10 %; the gradient, bound by its arithmetic, wants three CTAs per SM.
+// Besides, an SM takes at most kRate elements per us through its arithmetic (a third of that at single-element accesses, half for the
+// gradient; 4-bit rows are padded to 64 columns): few CTAs on a large image lose against the two passes.
 // `unit`: slabs are a multiple of so many channels (or all of them).
 NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
     NormPlan best;
     const int per = s.C / s.G, e = elem_bytes(s.dtype);
-    double best_us = 1e30;
+    const double slow = width == 1 ? 3 : width == 2 ? 1.5 : 1, kRate = 9000;
+    // two passes: three launches per run and the bytes once more, or the arithmetic of both passes on all SMs
+    const double elements = static_cast<double>(s.N) * s.P * s.C;
+    double best_us = 8.0 * ceil_div(static_cast<int64_t>(elements) * e * tensors, kRunBytes) +
+                     std::max(elements * e * (2 * tensors + 1) / 5.2e6, elements * 2 * slow * tensors / (148 * kRate));
     for (int k = 1; k <= s.G; ++k) {
         if (s.G % k) continue;
         const int64_t slab = static_cast<int64_t>(k) * per;
@@ -936,7 +942,10 @@ NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
             const double here = std::min<double>(per_sm, std::ceil(ctas / 148));           // CTAs of an SM at a time
             const double waves = std::ceil(ctas / (148 * here));
             const double bytes = static_cast<double>(chunk) * slab * e * (tensors + 1);
-            const double us = waves * (here * bytes / 44e3 * (slab * e < 128 && k < s.G ? 1.1 : 1.0) * (tensors == 2 ? 1 + 0.4 * (3 - here) : 1.0) +
+            const double wide = unit > 1 ? (slab + 63) / 64 * 64.0 : static_cast<double>(slab);
+            const double work = chunk * (slab * slow + wide) * (tensors == 2 ? 1.0 : 0.5) / kRate;
+            const double memory = here * bytes / 44e3 * (slab * e < 128 && k < s.G ? 1.1 : 1.0) * (tensors == 2 ? 1 + 0.4 * (3 - here) : 1.0);
+            const double us = waves * (std::max(memory, here * work) +
                                        0.5 + (cl > 1 ? 1.0 + 0.3 * std::log2(cl) : 0.0));
             if (us < best_us) {
                 best_us = us;

@@ -7,7 +7,7 @@
 //
 // Memory bound: sizeof(T) bytes read and 17/32 bytes written per element.  A warp takes one row of a column tile at a time: lane l
 // holds 8 consecutive columns, four lanes share a block (two shuffles give amax), every lane writes 4 bytes of codes and the warp
-// together one row of the tile, 128 consecutive bytes.  It takes four rows 32 apart, since the scales of rows r, r + 32, r + 64 and
+// together one row of the tile, 128 consecutive bytes (two or four rows of a narrow tile).  It takes four rows 32 apart, since the scales of rows r, r + 32, r + 64 and
 // r + 96 are neighbours in memory (16 bytes): 4 loads in flight per lane, and full 32-byte sectors for the scales.
 #include "ops.hpp"
 
@@ -27,7 +27,8 @@ struct QuantArgs {
     int64_t row0, rows, cols, ld;           // rows [row0, rows) of the matrix
     int64_t scales_at;
     int width, col_tiles, code_bytes, scale_bytes;
-    int step_ct, step_rest;                 // from a CTA's unit to its next one: column tiles, quarters of row tiles
+    int step_ct, step_rest;                 // from a CTA's unit to its next one: column tiles, parts of row tiles
+    int lanes, part_shift;                  // lanes to a row of a tile; log2 of the parts (CTAs) of a row tile
     // group norm in front (NORM kernels only): row = image * P + pixel
     const float *gamma, *beta, *stats;
     int64_t P, x_image;
@@ -52,38 +53,39 @@ struct Raw {
 // CTAs per SM that the registers of two row sets allow
 template <typename T, int A> __host__ __device__ constexpr int quant_ctas() { return sizeof(T) == 4 || A == 1 ? 3 : 4; }
 
-// A unit is a quarter of a tile: (row tile * 4 + quarter) * col_tiles + column tile, a warp's row set r0 = 8 * quarter + warp being the
-// rows r0, r0 + 32, r0 + 64, r0 + 96 of the row tile.  CTAs walk over the units and load the next one before they quantise the present
+// A row set r0 is the rows r0, r0 + 32, r0 + 64, r0 + 96 of a row tile; a warp takes one, or two or four of narrow tiles, `lanes` lanes
+// each.  A unit is a part of a tile, 8 warps' row sets: (row tile * parts + part) * col_tiles + column tile.  CTAs walk over the units and load the next one before they quantise the present
 // one, so that loads are always in flight.
 template <typename T, int A>
-__global__ void __launch_bounds__(kWarps * 32, quant_ctas<T, A>()) mx4_quantize_kernel(QuantArgs a, unsigned quarters) {
+__global__ void __launch_bounds__(kWarps * 32, quant_ctas<T, A>()) mx4_quantize_kernel(QuantArgs a, unsigned parts) {
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int row_bytes = a.width / 2;
-    const bool mine = lane * 8 < a.width;              // narrow tiles leave lanes idle
+    const int in_row = lane & (a.lanes - 1);           // this lane's place in its row
+    const int set = warp * (32 / a.lanes) + lane / a.lanes, sets_per_part = kWarps * (32 / a.lanes);
     int ct = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.col_tiles));
     unsigned rest = blockIdx.x / static_cast<unsigned>(a.col_tiles);
     const int64_t down = 32 * a.ld;
     auto load = [&](int at_ct, unsigned at_rest, Row8<T, A> (&raw)[4]) {
-        const int64_t row = static_cast<int64_t>(at_rest >> 2) * 128 + (at_rest & 3) * kWarps + warp;
-        const int64_t c = static_cast<int64_t>(at_ct) * a.width + lane * 8;
+        const int64_t row = static_cast<int64_t>(at_rest >> a.part_shift) * 128 + (at_rest & ((1 << a.part_shift) - 1)) * sets_per_part + set;
+        const int64_t c = static_cast<int64_t>(at_ct) * a.width + in_row * 8;
         const T *src = static_cast<const T *>(a.x) + row * a.ld + c;
-        if (mine && c + 8 <= a.cols && row + 96 < a.rows) {
+        if (c + 8 <= a.cols && row + 96 < a.rows) {
 #pragma unroll
             for (int k = 0; k < 4; ++k, src += down) raw[k].load(src);
         } else {
-            const int count = mine ? static_cast<int>(max(int64_t(0), min(int64_t(8), a.cols - c))) : 0;
+            const int count = static_cast<int>(max(int64_t(0), min(int64_t(8), a.cols - c)));
 #pragma unroll
             for (int k = 0; k < 4; ++k, src += down) raw[k].load(src, row + 32 * k < a.rows ? count : 0);
         }
     };
     auto store = [&](const Row8<T, A> (&raw)[4]) {
-        const int64_t rt = rest >> 2;
-        const int r0 = static_cast<int>(rest & 3) * kWarps + warp;
+        const int64_t rt = rest >> a.part_shift;
+        const int r0 = static_cast<int>(rest & ((1 << a.part_shift) - 1)) * sets_per_part + set;
         const int64_t left = a.rows - rt * 128 - r0;   // rows of the set exist where 32 k < left
         const int64_t tile = rt * a.col_tiles + ct;
         // 32 rows further down the tile, a 16-byte unit keeps its place in the row
-        int at = r0 * row_bytes + lane * 4;
+        int at = r0 * row_bytes + in_row * 4;
         at ^= ((at >> 7) & (a.width / 32 - 1)) << 4;
         uint8_t *codes_out = a.mx + tile * a.code_bytes + at;
         uint32_t sets[4];                              // lane of block b: scale byte of (row r0 + 32 k, b)
@@ -91,25 +93,26 @@ __global__ void __launch_bounds__(kWarps * 32, quant_ctas<T, A>()) mx4_quantize_
         for (int k = 0; k < 4; ++k, codes_out += 32 * row_bytes) {
             uint32_t codes;
             sets[k] = quantise8(raw[k].values(), raw[k].top(), codes);
-            if (32 * k < left && mine) *reinterpret_cast<uint32_t *>(codes_out) = codes;
+            if (32 * k < left) *reinterpret_cast<uint32_t *>(codes_out) = codes;
         }
-        // lanes 0 and 16 gather the scale bytes of blocks 0..3 and 4..7: 16 bytes each
+        // the first lane of every 16 of a row gathers the scale bytes of four blocks (two in the narrowest tiles): 16 bytes for four rows
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             sets[k] |= __shfl_down_sync(0xffffffffu, sets[k], 4) << 8;
-            sets[k] |= __shfl_down_sync(0xffffffffu, sets[k], 8) << 16;
+            const uint32_t upper = __shfl_down_sync(0xffffffffu, sets[k], 8) << 16;
+            if (a.lanes > 8) sets[k] |= upper;
         }
-        if ((lane & 15) == 0 && mine && left > 0)
-            *reinterpret_cast<uint4 *>(a.mx + a.scales_at + tile * a.scale_bytes + (lane >> 4) * 512 + r0 * 16) = make_uint4(sets[0], sets[1], sets[2], sets[3]);
+        if ((in_row & 15) == 0 && left > 0)
+            *reinterpret_cast<uint4 *>(a.mx + a.scales_at + tile * a.scale_bytes + (in_row >> 4) * 512 + r0 * 16) = make_uint4(sets[0], sets[1], sets[2], sets[3]);
     };
     pdl_wait();
     Row8<T, A> now[4], next[4];
-    if (rest < quarters) load(ct, rest, now);
-    while (rest < quarters) {                          // (the same for all threads of the CTA)
+    if (rest < parts) load(ct, rest, now);
+    while (rest < parts) {                          // (the same for all threads of the CTA)
         int next_ct = ct + a.step_ct;
         unsigned next_rest = rest + a.step_rest;
         if (next_ct >= a.col_tiles) { next_ct -= a.col_tiles; ++next_rest; }
-        if (next_rest < quarters) load(next_ct, next_rest, next);
+        if (next_rest < parts) load(next_ct, next_rest, next);
         store(now);
         ct = next_ct;
         rest = next_rest;
@@ -118,27 +121,27 @@ __global__ void __launch_bounds__(kWarps * 32, quant_ctas<T, A>()) mx4_quantize_
     }
 }
 
-// A group norm in front: blockIdx.x = row tile * col_tiles + column tile.  A warp takes four of the 32 row sets of a row tile, for which
-// the constants of its columns are loaded once per image.
+// A group norm in front: blockIdx.x = row tile * col_tiles + column tile.  The warps walk over the 32 row sets of a row tile; the constants
+// of a lane's columns are loaded once per image.
 template <typename T, int A>
 __global__ void __launch_bounds__(kWarps * 32) norm_quantize_kernel(QuantArgs a) {
-    constexpr int kSets = 4, kParts = 32 / (kWarps * kSets);
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int ct = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.col_tiles));
     const unsigned rest = blockIdx.x / static_cast<unsigned>(a.col_tiles);
-    const int64_t rt = a.row0 / 128 + rest / kParts;
-    const int64_t c = static_cast<int64_t>(ct) * a.width + lane * 8;
+    const int64_t rt = a.row0 / 128 + rest;
+    const int in_row = lane & (a.lanes - 1), together = 32 / a.lanes;  // this lane's place in its row; row sets a warp takes at a time
+    const int64_t c = static_cast<int64_t>(ct) * a.width + in_row * 8;
     const int row_bytes = a.width / 2;
     uint8_t *codes_out = a.mx + (rt * a.col_tiles + ct) * a.code_bytes;
     uint8_t *scales_out = a.mx + a.scales_at + (rt * a.col_tiles + ct) * a.scale_bytes;
-    const int count = lane * 8 < a.width ? static_cast<int>(max(int64_t(0), min(int64_t(8), a.cols - c))) : 0;
+    const int count = static_cast<int>(max(int64_t(0), min(int64_t(8), a.cols - c)));
     pdl_wait();
     float mean[8], scale[8], beta[8];                                  // of image `image`
     int image = -1;
-    for (int set = 0; set < kSets; ++set) {
-        const int r0 = static_cast<int>(rest % kParts) * kWarps * kSets + set * kWarps + warp;
-        if (rt * 128 + r0 >= a.rows) return;                           // warp-uniform; higher rows of the set do not exist either
+    for (int first = warp * together; first < 32; first += kWarps * together) {
+        if (rt * 128 + first >= a.rows) return;                        // (the same for the warp; higher rows of its sets do not exist either)
+        const int r0 = first + lane / a.lanes;
         Raw<T, A> raw[4];
         bool on[4];
         int at_image[4];
@@ -158,7 +161,7 @@ __global__ void __launch_bounds__(kWarps * 32) norm_quantize_kernel(QuantArgs a)
             float v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = raw[k].get(j);
-            if (on[k] && at_image[k] != image) {                   // warp-uniform
+            if (on[k] && at_image[k] != image) {
                 image = at_image[k];
                 const float2 *st = reinterpret_cast<const float2 *>(a.stats) + static_cast<int64_t>(image) * a.G;
                 int g = static_cast<int>(c) / a.per, left = a.per - static_cast<int>(c) % a.per;
@@ -178,22 +181,21 @@ __global__ void __launch_bounds__(kWarps * 32) norm_quantize_kernel(QuantArgs a)
             }
             uint32_t codes;
             sets[k] = quantise8(v, codes);
-            if (on[k] && lane * 8 < a.width) {
-                int at = (r0 + 32 * k) * row_bytes + lane * 4;
+            if (on[k]) {
+                int at = (r0 + 32 * k) * row_bytes + in_row * 4;
                 at ^= ((at >> 7) & (a.width / 32 - 1)) << 4;
                 *reinterpret_cast<uint32_t *>(codes_out + at) = codes;
             }
         }
-        // lanes 0 and 16 gather the scale bytes of blocks 0..3 and 4..7: 16 bytes each
+        // as in the kernel above
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            uint32_t w = sets[k];
-            w |= __shfl_down_sync(0xffffffffu, w, 4) << 8;
-            w |= __shfl_down_sync(0xffffffffu, w, 8) << 16;
-            sets[k] = w;
+            sets[k] |= __shfl_down_sync(0xffffffffu, sets[k], 4) << 8;
+            const uint32_t upper = __shfl_down_sync(0xffffffffu, sets[k], 8) << 16;
+            if (a.lanes > 8) sets[k] |= upper;
         }
-        if ((lane & 15) == 0 && lane * 8 < a.width) {
-            uint32_t *to = reinterpret_cast<uint32_t *>(scales_out + (lane >> 4) * 512 + r0 * 16);
+        if ((in_row & 15) == 0) {
+            uint32_t *to = reinterpret_cast<uint32_t *>(scales_out + (in_row >> 4) * 512 + r0 * 16);
             if (on[0] && on[1] && on[2] && on[3]) {
                 *reinterpret_cast<uint4 *>(to) = make_uint4(sets[0], sets[1], sets[2], sets[3]);
             } else {                                                   // other rows of the set belong to another launch
@@ -234,22 +236,23 @@ __global__ void __launch_bounds__(kWarps * 32) mx4_dequantize_kernel(QuantArgs a
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int ct = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.col_tiles));
     const unsigned rest = blockIdx.x / static_cast<unsigned>(a.col_tiles);
-    const int64_t rt = rest >> 2;
-    const int r0 = static_cast<int>(rest & 3) * kWarps + warp;
-    const int64_t c = static_cast<int64_t>(ct) * a.width + lane * 8;
+    const int in_row = lane & (a.lanes - 1), sets_per_part = kWarps * (32 / a.lanes);
+    const int64_t rt = rest >> a.part_shift;
+    const int r0 = static_cast<int>(rest & ((1 << a.part_shift) - 1)) * sets_per_part + warp * (32 / a.lanes) + lane / a.lanes;
+    const int64_t c = static_cast<int64_t>(ct) * a.width + in_row * 8;
     const int tile_row = a.width / 2;
     const uint8_t *codes_in = a.mx + (rt * a.col_tiles + ct) * a.code_bytes;
     const uint8_t *scales_in = a.mx + a.scales_at + (rt * a.col_tiles + ct) * a.scale_bytes;
     pdl_wait();
-    if (lane * 8 >= a.width || c >= a.cols) return;
+    if (c >= a.cols) return;
     uint32_t codes[4], scale[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         if (rt * 128 + r0 + 32 * k >= a.rows) continue;
-        int at = (r0 + 32 * k) * tile_row + lane * 4;
+        int at = (r0 + 32 * k) * tile_row + in_row * 4;
         at ^= ((at >> 7) & (a.width / 32 - 1)) << 4;
         codes[k] = *reinterpret_cast<const uint32_t *>(codes_in + at);
-        scale[k] = scales_in[(lane >> 4) * 512 + r0 * 16 + k * 4 + ((lane >> 2) & 3)];
+        scale[k] = scales_in[(in_row >> 4) * 512 + r0 * 16 + k * 4 + ((in_row >> 2) & 3)];
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -322,13 +325,16 @@ QuantArgs quant_args(const Mx4Shape &m, const void *x, int64_t ld, void *mx) {
     a.scales_at = m.scales_at; a.width = m.width; a.col_tiles = static_cast<int>(m.col_tiles);
     a.code_bytes = m.code_bytes; a.scale_bytes = m.scale_bytes;
     a.P = 1; a.G = 1; a.per = 1;
+    a.lanes = m.width / 8;
+    a.part_shift = m.width == 256 ? 2 : m.width == 128 ? 1 : 0;
     return a;
 }
 
-unsigned quant_grid(const Mx4Shape &m) {               // no CTA for quarters of the last row tile that have no rows
+// Units of a matrix whose CTAs take `sets` of the 32 row sets of a row tile; none for parts of the last row tile that have no rows.
+unsigned quant_grid(const Mx4Shape &m, int sets) {
     const int64_t last = m.rows - (m.row_tiles - 1) * 128;
-    const int64_t quarters = (m.row_tiles - 1) * 4 + (last >= 32 ? 4 : ceil_div(last, kWarps));
-    return static_cast<unsigned>(quarters * m.col_tiles);
+    const int64_t parts = (m.row_tiles - 1) * (32 / sets) + (last >= 32 ? 32 / sets : ceil_div(last, sets));
+    return static_cast<unsigned>(parts * m.col_tiles);
 }
 
 // elements per access: 16 bytes where addresses and strides allow, else two, else one
@@ -351,7 +357,7 @@ template <typename F> cudaError_t by_access(int dtype, int i, F f) {
 
 cudaError_t launch_mx4_quantize(const Mx4Shape &m, const void *x, int dtype, int64_t ld, void *mx, cudaStream_t st) {
     QuantArgs a = quant_args(m, x, ld, mx);
-    const unsigned units = quant_grid(m);
+    const unsigned units = quant_grid(m, kWarps * (32 / a.lanes));
     return by_access(dtype, access_index(dtype, x, ld), [&](auto t, auto v) {
         const unsigned grid = std::min(units, static_cast<unsigned>(sm_count() * quant_ctas<decltype(t), v.value>()));
         a.step_ct = static_cast<int>(grid % m.col_tiles);
@@ -377,9 +383,9 @@ cudaError_t launch_mx4_dequantize(const Mx4Shape &m, const void *mx, void *out, 
     return by_access(dtype, access_index(dtype, out, ld), [&](auto t, auto v) {
         using T = decltype(t);
         if constexpr (sizeof(T) * v.value < 4 || v.value == 1)
-            return launch_pdl(mx4_dequantize_single_kernel<T>, dim3(quant_grid(m)), dim3(kWarps * 32), 0, st, 1, a, static_cast<T *>(out));
+            return launch_pdl(mx4_dequantize_single_kernel<T>, dim3(quant_grid(m, kWarps)), dim3(kWarps * 32), 0, st, 1, a, static_cast<T *>(out));
         else
-            return launch_pdl(mx4_dequantize_kernel<T, v.value>, dim3(quant_grid(m)), dim3(kWarps * 32), 0, st, 1, a, static_cast<T *>(out));
+            return launch_pdl(mx4_dequantize_kernel<T, v.value>, dim3(quant_grid(m, kWarps * (32 / a.lanes))), dim3(kWarps * 32), 0, st, 1, a, static_cast<T *>(out));
     });
 }
 
