@@ -140,6 +140,8 @@ struct Stream {
     int64_t src_step;                                  // elements between this thread's pixels
     uint32_t to, from, step, ring, end;                // shared memory: next pixel to copy, next to read, distance; the ring's bounds
     int left;                                          // pixels still to copy
+    // BACK: from the thread's last pixel to its first
+    template <bool BACK = false>
     __device__ __forceinline__ void begin(const T *first, int64_t stride, int pixels, const Place &q, T *space, int channels, int col) {
         src = first + q.row * stride;
         src_step = q.rows * stride;
@@ -148,6 +150,10 @@ struct Stream {
         end = ring + kDepth * kBatch * step;
         to = from = ring;
         left = (pixels - q.row + q.rows - 1) / q.rows;
+        if constexpr (BACK) {
+            src += (left - 1) * src_step;
+            src_step = -src_step;
+        }
     }
     __device__ __forceinline__ void one() {
         if constexpr (kBytes >= 4) {
@@ -736,6 +742,7 @@ __global__ void __launch_bounds__(kThreads) norm_join_kernel(NormArgs a) {
         reinterpret_cast<float2 *>(a.stats_out)[static_cast<int64_t>(a.n0 + n) * a.G + g] = make_float2(mean, 1.f / sqrtf(sq * a.inv_count + a.eps));
 }
 
+// Each CTA takes its pixels in the opposite order of the pass before: what that one read last is still in L2.
 template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kThreads, 3) norm_apply_kernel(NormArgs a) {
     pdl_trigger();
@@ -749,14 +756,14 @@ __global__ void __launch_bounds__(kThreads, 3) norm_apply_kernel(NormArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     using S = Stream<T, V, false, 1>;
     S x;
-    x.begin(static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + s.c0 + q.col * V, a.x_pixel, pixels, q, reinterpret_cast<T *>(smem), s.channels, 0);
+    x.template begin<true>(static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + s.c0 + q.col * V, a.x_pixel, pixels, q, reinterpret_cast<T *>(smem), s.channels, 0);
     int count = x.left;
 #pragma unroll
     for (int b = 0; b < S::kDepth; ++b) { x.copy(); copies_commit(); }
     Channels<V> f;
     f.load(a, n, s.c0 + q.col * V);
-    T *dst = static_cast<T *>(a.y) + n * a.y_image + (p0 + q.row) * a.y_pixel + s.c0 + q.col * V;
-    const int64_t dst_step = q.rows * a.y_pixel;
+    const int64_t dst_step = -q.rows * a.y_pixel;
+    T *dst = static_cast<T *>(a.y) + n * a.y_image + (p0 + q.row) * a.y_pixel - (count - 1) * dst_step + s.c0 + q.col * V;
     auto put = [&]() {
         narrow<T, V>(activate<ACT, V>(fma(widen<T, V>(x.get()) + f.shift, f.scale, f.beta))).store(dst);
         dst += dst_step;
@@ -816,23 +823,25 @@ __global__ void __launch_bounds__(kThreads) norm_grad_join_kernel(NormArgs a) {
     __shared__ float scratch[kThreads / 32];
     pdl_trigger();
     pdl_wait();
-    const int g = blockIdx.x, n = a.n0 + blockIdx.y;
+    const int g = blockIdx.x, n = a.n0 + blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     float2 *part = reinterpret_cast<float2 *>(a.ws) + static_cast<int64_t>(n) * a.chunks * a.C + g * a.per;
     float s1 = 0.f, s2 = 0.f;
-    for (int c = 0; c < a.per; ++c) {
+    for (int c = warp; c < a.per; c += kThreads / 32) {                // a warp takes a channel at a time
         float sa = 0.f, sb = 0.f;
 #pragma unroll 4
-        for (int k = threadIdx.x; k < a.chunks; k += kThreads) {
+        for (int k = lane; k < a.chunks; k += 32) {
             const float2 e = part[static_cast<int64_t>(k) * a.C + c];
             sa += e.x; sb += e.y;
         }
-        sa = block_sum(sa, scratch);
-        sb = block_sum(sb, scratch);                   // (its barriers also order the reads above before the write below)
-        if (threadIdx.x == 0) part[c] = make_float2(sa, sb);
+        sa = warp_sum(sa);
+        sb = warp_sum(sb);
+        if (lane == 0) part[c] = make_float2(sa, sb);                  // (this lane alone has read chunk 0's entry)
         const float gm = a.gamma[g * a.per + c];
         s1 = fmaf(gm, sa, s1);
         s2 = fmaf(gm, sb, s2);
     }
+    s1 = block_sum(lane == 0 ? s1 : 0.f, scratch);
+    s2 = block_sum(lane == 0 ? s2 : 0.f, scratch);
     if (threadIdx.x == 0) {
         const int64_t at = static_cast<int64_t>(n) * a.G + g;
         const float rstd = reinterpret_cast<const float2 *>(a.stats_in)[at].y;
@@ -850,17 +859,23 @@ __global__ void __launch_bounds__(kThreads, 3) norm_grad_apply_kernel(NormArgs a
     const Place q = place_of<V>(s.channels);
     pdl_wait();
     const float2 *ws = reinterpret_cast<const float2 *>(a.ws);
-    if (n == a.N - 1 && blockIdx.x == 0)               // in the last run, one CTA per slab also adds the images up
-        for (int c = s.c0 + threadIdx.x; c < s.c0 + s.channels; c += kThreads) {
+    if (a.n0 + static_cast<int>(gridDim.z) == a.N && threadIdx.x < 32) {
+        // in the last run, the first warps of a slab's CTAs add the images up, a channel at a time: a lane takes every 32nd image
+        for (int c = blockIdx.z * gridDim.x + blockIdx.x; c < s.channels; c += gridDim.x * gridDim.z) {
             float sa = 0.f, sb = 0.f;
-#pragma unroll 8
-            for (int i = 0; i < a.N; ++i) {
-                const float2 e = ws[static_cast<int64_t>(i) * a.chunks * a.C + c];
+            for (int i = threadIdx.x; i < a.N; i += 32) {
+                const float2 e = ws[static_cast<int64_t>(i) * a.chunks * a.C + s.c0 + c];
                 sa += e.x; sb += e.y;
             }
-            a.dbeta[c] = sa;
-            a.dgamma[c] = sb;
+            sa = warp_sum(sa);
+            sb = warp_sum(sb);
+            if (threadIdx.x == 0) {
+                a.dbeta[s.c0 + c] = sa;
+                a.dgamma[s.c0 + c] = sb;
+            }
         }
+        __syncwarp();
+    }
     if (!q.on) return;
     Channels<V> f;
     f.load(a, n, s.c0 + q.col * V);
@@ -872,14 +887,14 @@ __global__ void __launch_bounds__(kThreads, 3) norm_grad_apply_kernel(NormArgs a
     using S = Stream<T, V, false, 2>;
     S x, dy;
     T *ring = reinterpret_cast<T *>(smem);
-    x.begin(static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + s.c0 + q.col * V, a.x_pixel, pixels, q, ring, s.channels, 0);
-    dy.begin(static_cast<const T *>(a.dy) + n * a.y_image + p0 * a.y_pixel + s.c0 + q.col * V, a.y_pixel, pixels, q,
+    x.template begin<true>(static_cast<const T *>(a.x) + n * a.x_image + p0 * a.x_pixel + s.c0 + q.col * V, a.x_pixel, pixels, q, ring, s.channels, 0);
+    dy.template begin<true>(static_cast<const T *>(a.dy) + n * a.y_image + p0 * a.y_pixel + s.c0 + q.col * V, a.y_pixel, pixels, q,
              ring + S::kDepth * S::kBatch * kThreads * V, s.channels, 0);
     int count = x.left;
 #pragma unroll
     for (int b = 0; b < S::kDepth; ++b) { x.copy(); dy.copy(); copies_commit(); }
-    T *dst = static_cast<T *>(a.y) + n * a.x_image + (p0 + q.row) * a.x_pixel + s.c0 + q.col * V;
-    const int64_t dst_step = q.rows * a.x_pixel;
+    const int64_t dst_step = -q.rows * a.x_pixel;
+    T *dst = static_cast<T *>(a.y) + n * a.x_image + (p0 + q.row) * a.x_pixel - (count - 1) * dst_step + s.c0 + q.col * V;
     auto put = [&]() {
         f.template dx<ACT, T>(x.get(), dy.get(), nk1, nk2).store(dst);
         dst += dst_step;
@@ -910,14 +925,14 @@ int resident_smem(const NormShape &s, int width, int tensors, int slab, int64_t 
 }
 
 constexpr int kSmemMost = 220 * 1024;       // dynamic shared memory of one CTA
-constexpr int64_t kRunBytes = int64_t(64) << 20;   // two-pass: bytes of x (and dy) of the images that are taken together
+constexpr int64_t kRunBytes = int64_t(160) << 20;   // two-pass: bytes of x (and dy) of the images that are taken together
 
 // Picks the slab and the cluster of the resident form by a time estimate, fitted to measurements of ten shapes with every slab and
 // cluster that fits (7x7 to 56x56 pixels, 64 to 512 channels, the three types, both directions; its choice was the fastest or within
 // 3 % of it): the CTAs of an SM share its HBM rate of 44 bytes per ns; a wave costs half a microsecond, a cluster one more and 0.3 per
 // doubling; slabs narrower than 128 bytes cost 10 %; the gradient, bound by its arithmetic, wants three CTAs per SM.
-// Besides, an SM takes at most kRate elements per us through its arithmetic (a third of that at single-element accesses, half for the
-// gradient; 4-bit rows are padded to 64 columns): few CTAs on a large image lose against the two passes.
+// Besides, an SM takes at most kRate elements per us through its arithmetic (a third of that at single-element accesses, a quarter for
+// the gradient; 4-bit rows are padded to 64 columns): few CTAs on a large image lose against the two passes.
 // `unit`: slabs are a multiple of so many channels (or all of them).
 NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
     NormPlan best;
@@ -926,7 +941,7 @@ NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
     // two passes: three launches per run and the bytes once more, or the arithmetic of both passes on all SMs
     const double elements = static_cast<double>(s.N) * s.P * s.C;
     double best_us = 8.0 * ceil_div(static_cast<int64_t>(elements) * e * tensors, kRunBytes) +
-                     std::max(elements * e * (2 * tensors + 1) / 5.2e6, elements * 2 * slow * tensors / (148 * kRate));
+                     std::max(elements * e * (2 * tensors + 1) / 5.2e6, elements * slow * (tensors == 2 ? 2.8 : 1.2) / (148 * kRate));
     for (int k = 1; k <= s.G; ++k) {
         if (s.G % k) continue;
         const int64_t slab = static_cast<int64_t>(k) * per;
@@ -943,7 +958,7 @@ NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
             const double waves = std::ceil(ctas / (148 * here));
             const double bytes = static_cast<double>(chunk) * slab * e * (tensors + 1);
             const double wide = unit > 1 ? (slab + 63) / 64 * 64.0 : static_cast<double>(slab);
-            const double work = chunk * (slab * slow + wide) * (tensors == 2 ? 1.0 : 0.5) / kRate;
+            const double work = chunk * (slab * slow + wide) * (tensors == 2 ? 2.0 : 0.5) / kRate;
             const double memory = here * bytes / 44e3 * (slab * e < 128 && k < s.G ? 1.1 : 1.0) * (tensors == 2 ? 1 + 0.4 * (3 - here) : 1.0);
             const double us = waves * (std::max(memory, here * work) +
                                        0.5 + (cl > 1 ? 1.0 + 0.3 * std::log2(cl) : 0.0));
