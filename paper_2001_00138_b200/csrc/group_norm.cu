@@ -310,7 +310,8 @@ __device__ __forceinline__ void write_mx4(const NormArgs &a, const T *tile, cons
     const int c = unit * 8;
     const Groups<8> at(c, a.per);
     const Fv<8> shift = Fv<8>::make([&](int j) { return c + j < channels ? -fin[at.g[j]].x : 0.f; });
-    const Fv<8> scale = Fv<8>::make([&](int j) { return c + j < channels ? fin[at.g[j]].y * gamma[c + j] : 0.f; });
+    const Fv<8> rstd = Fv<8>::make([&](int j) { return c + j < channels ? fin[at.g[j]].y : 0.f; });
+    const Fv<8> scale = Fv<8>::make([&](int j) { return c + j < channels ? gamma[c + j] : 0.f; });
     const Fv<8> beta = Fv<8>::make([&](int j) { return c + j < channels ? beta_of[c + j] : 0.f; });
     const bool whole = c + 8 <= channels && channels % (16 / sizeof(T)) == 0;
     const int ct = (c0 + c) / a.mx_width, in_tile = (c0 + c) - ct * a.mx_width;
@@ -337,7 +338,7 @@ __device__ __forceinline__ void write_mx4(const NormArgs &a, const T *tile, cons
             } else {
                 z = Fv<8>::make([&](int j) { return c + j < channels ? to_float(src[j]) : 0.f; });
             }
-            z = activate<ACT, 8>(fma(z + shift, scale, beta));
+            z = ((z + shift) * rstd * scale + beta).map([](float v) { return activate_plain<ACT>(v); });   // as written: see activate_plain
         }
         float v[8];
 #pragma unroll
@@ -436,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, 3) norm_resident_kernel(NormArgs a) 
             }
             e = make_float2(mean, sq);
         }
-        const float rstd = 1.f / sqrtf(e.y * a.inv_count + a.eps);
+        const float rstd = rsqrtf(e.y * a.inv_count + a.eps);
         fin[g] = make_float2(e.x, rstd);
         if (a.stats_out && rank == 0) reinterpret_cast<float2 *>(a.stats_out)[static_cast<int64_t>(n) * a.G + c0 / a.per + g] = fin[g];
     }
@@ -739,7 +740,7 @@ __global__ void __launch_bounds__(kThreads) norm_join_kernel(NormArgs a) {
     }
     sq = block_sum(sq, scratch);
     if (threadIdx.x == 0)
-        reinterpret_cast<float2 *>(a.stats_out)[static_cast<int64_t>(a.n0 + n) * a.G + g] = make_float2(mean, 1.f / sqrtf(sq * a.inv_count + a.eps));
+        reinterpret_cast<float2 *>(a.stats_out)[static_cast<int64_t>(a.n0 + n) * a.G + g] = make_float2(mean, rsqrtf(sq * a.inv_count + a.eps));
 }
 
 // Each CTA takes its pixels in the opposite order of the pass before: what that one read last is still in L2.

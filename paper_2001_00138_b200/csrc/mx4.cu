@@ -32,7 +32,7 @@ struct QuantArgs {
     // group norm in front (NORM kernels only): row = image * P + pixel
     const float *gamma, *beta, *stats;
     int64_t P, x_image;
-    int G, per, act;
+    int G, per;
 };
 
 // Eight columns of a row as they lie in memory, in 8 / A accesses.
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kWarps * 32, quant_ctas<T, A>()) mx4_quantize_
 
 // A group norm in front: blockIdx.x = row tile * col_tiles + column tile.  The warps walk over the 32 row sets of a row tile; the constants
 // of a lane's columns are loaded once per image.
-template <typename T, int A>
+template <typename T, int A, int ACT>
 __global__ void __launch_bounds__(kWarps * 32) norm_quantize_kernel(QuantArgs a) {
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(kWarps * 32) norm_quantize_kernel(QuantArgs a)
     uint8_t *scales_out = a.mx + a.scales_at + (rt * a.col_tiles + ct) * a.scale_bytes;
     const int count = static_cast<int>(max(int64_t(0), min(int64_t(8), a.cols - c)));
     pdl_wait();
-    float mean[8], scale[8], beta[8];                                  // of image `image`
+    float mean[8], rstd[8], gamma[8], beta[8];                         // of image `image`
     int image = -1;
     for (int first = warp * together; first < 32; first += kWarps * together) {
         if (rt * 128 + first >= a.rows) return;                        // (the same for the warp; higher rows of its sets do not exist either)
@@ -170,14 +170,16 @@ __global__ void __launch_bounds__(kWarps * 32) norm_quantize_kernel(QuantArgs a)
                     const bool in = j < count;
                     const float2 f = in ? st[g] : make_float2(0.f, 0.f);
                     mean[j] = f.x;
-                    scale[j] = in ? f.y * a.gamma[c + j] : 0.f;
+                    rstd[j] = f.y;
+                    gamma[j] = in ? a.gamma[c + j] : 0.f;
                     beta[j] = in ? a.beta[c + j] : 0.f;
                     if (--left == 0) { ++g; left = a.per; }
                 }
             }
             if (on[k]) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = j < count ? activate(fmaf(v[j] - mean[j], scale[j], beta[j]), a.act) : 0.f;
+                for (int j = 0; j < 8; ++j)                            // as written: see activate_plain
+                    v[j] = j < count ? activate_plain<ACT>(__fadd_rn(__fmul_rn(__fmul_rn(v[j] - mean[j], rstd[j]), gamma[j]), beta[j])) : 0.f;
             }
             uint32_t codes;
             sets[k] = quantise8(v, codes);
@@ -371,10 +373,12 @@ cudaError_t launch_norm_quantize(const NormShape &s, const Mx4Shape &m, const vo
     QuantArgs a = quant_args(m, x, s.x_pixel, mx);
     a.row0 = row0; a.rows = row0 + rows;
     a.gamma = gamma; a.beta = beta; a.stats = stats;
-    a.P = s.P; a.x_image = s.x_image; a.G = s.G; a.per = s.C / s.G; a.act = s.act;
+    a.P = s.P; a.x_image = s.x_image; a.G = s.G; a.per = s.C / s.G;
     const int64_t tiles = ceil_div(a.rows, 128) - row0 / 128;
     return by_access(s.dtype, access_index(s.dtype, x, s.x_pixel, s.x_image), [&](auto t, auto v) {
-        return launch_pdl(norm_quantize_kernel<decltype(t), v.value>, dim3(static_cast<unsigned>(tiles * m.col_tiles)), dim3(kWarps * 32), 0, st, 1, a);
+        return by_act(s.act, [&](auto c) {
+            return launch_pdl(norm_quantize_kernel<decltype(t), v.value, c.value>, dim3(static_cast<unsigned>(tiles * m.col_tiles)), dim3(kWarps * 32), 0, st, 1, a);
+        });
     });
 }
 

@@ -284,12 +284,14 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
 
 // ---- many rows ----------------------------------------------------------------------------------------------------------
 // Tiles of 128 rows of x (M) by up to 256 rows of w (N), one persistent CTA per SM walking over them.  Warp 0 fills a ring of column
-// tiles, warp 1 issues the MMAs, warps 4 to 11 are the epilogue: they move the finished accumulator to registers, hand tensor memory back,
-// and convert and store while the next tile is multiplied.  A lane owns a row of y; 64-byte pieces of 32 rows pass through shared
-// memory so that they are stored as whole sectors, four lanes to a row.
-constexpr int kRowsThreads = 384;
-constexpr int kEpilogueWarps = 8;
-constexpr int kStageOut = 2048;                        // bytes an epilogue warp passes through shared memory at a time
+// tiles, warp 1 issues the MMAs, warps 4 to 19 are the epilogue: they move the finished accumulator to registers, hand tensor memory back,
+// and convert and store while the next tile is multiplied.  A lane owns a row of y; pieces of 32 rows pass through shared memory so
+// that they are stored as whole sectors: 64 bytes of a row at a time where a tile has at most three column tiles and is bound by these
+// stores (100352 rows, 64 -> 256 columns, bf16: 15.9 us; 32-byte pieces 17.9, eight warps 16.8), else 32 bytes, whose smaller buffers
+// leave room for a fourth column tile in the ring (8192 rows, 4096 -> 4096: 56 us; 64-byte pieces and three column tiles 62).
+constexpr int kRowsThreads = 640;
+constexpr int kEpilogueWarps = 16;
+__host__ __device__ constexpr int stage_out(int piece) { return 32 * piece + 64 * 4; }     // shared memory of an epilogue warp: a piece of 32 rows, the bias of its columns
 
 __device__ __forceinline__ void tmem_ld32_async(uint32_t addr, uint32_t *v) {
     asm volatile(
@@ -302,50 +304,47 @@ __device__ __forceinline__ void tmem_ld32_async(uint32_t addr, uint32_t *v) {
         : "r"(addr) : "memory");
 }
 
-// One warp: 32 rows by 32 columns (16-bit types) or 16 columns (fp32) = 64 bytes a row, from registers to y.
-template <typename T>
-__device__ __forceinline__ void store_piece(const float (&v)[64 / sizeof(T)], unsigned char *stage, T *y, int64_t ldy, int64_t rows_left, int cols_left, bool vector) {
+// One warp: PIECE bytes of 32 rows, from registers to y.
+template <typename T, int PIECE>
+__device__ __forceinline__ void store_piece(const float (&v)[PIECE / sizeof(T)], unsigned char *stage, T *y, int64_t ldy, int rows_left, int cols_left, bool vector) {
     const int lane = threadIdx.x & 31;
-    constexpr int kCols = 64 / sizeof(T);
-    uint32_t w[16];
-    if constexpr (sizeof(T) == 4) {
+    constexpr int kCols = PIECE / sizeof(T), kUnits = PIECE / 16, kShift = PIECE == 64 ? 1 : 2;
+    uint32_t w[PIECE / 4];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(v[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            if constexpr (std::is_same<T, __half>::value) {
-                const __half2 h = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
-                w[j] = *reinterpret_cast<const uint32_t *>(&h);
-            } else {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-                w[j] = *reinterpret_cast<const uint32_t *>(&h);
-            }
+    for (int j = 0; j < PIECE / 4; ++j) {
+        if constexpr (sizeof(T) == 4) {
+            w[j] = __float_as_uint(v[j]);
+        } else if constexpr (std::is_same<T, __half>::value) {
+            const __half2 h = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+            w[j] = *reinterpret_cast<const uint32_t *>(&h);
+        } else {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+            w[j] = *reinterpret_cast<const uint32_t *>(&h);
         }
     }
-    // 16-byte unit q of row r sits at unit q ^ ((r >> 1) & 3): eight lanes of a store, and of a load, touch all banks once
+    // 16-byte unit q of row r sits at unit q ^ (r >> kShift): eight lanes of a store, and of a load, touch all banks once
+    auto place = [&](int r, int q) { return r * PIECE + ((q ^ ((r >> kShift) & (kUnits - 1))) << 4); };
     __syncwarp();
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<uint4 *>(stage + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+    for (int q = 0; q < kUnits; ++q) *reinterpret_cast<uint4 *>(stage + place(lane, q)) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
     __syncwarp();
     if (vector && cols_left >= kCols) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = i * 8 + (lane >> 2), q = lane & 3;
-            const uint4 t = *reinterpret_cast<const uint4 *>(stage + r * 64 + ((q ^ ((r >> 1) & 3)) << 4));
+        for (int i = 0; i < kUnits; ++i) {
+            const int r = i * (32 / kUnits) + lane / kUnits, q = lane % kUnits;
+            const uint4 t = *reinterpret_cast<const uint4 *>(stage + place(r, q));
             if (r < rows_left) *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(y + r * ldy) + q * 16) = t;
         }
     } else {
-        const int rows = static_cast<int>(rows_left < 32 ? rows_left : 32);
+        const int rows = min(rows_left, 32);
         for (int i = lane; i < rows * kCols; i += 32) {
             const int r = i / kCols, c = i % kCols, b = c * static_cast<int>(sizeof(T));
-            if (c < cols_left) y[r * ldy + c] = *reinterpret_cast<const T *>(stage + r * 64 + (((b >> 4) ^ ((r >> 1) & 3)) << 4) + (b & 15));
+            if (c < cols_left) y[r * ldy + c] = *reinterpret_cast<const T *>(stage + place(r, b >> 4) + (b & 15));
         }
     }
 }
 
-template <typename T, int ACT>
+template <typename T, int ACT, int PIECE>
 __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 2];
@@ -477,33 +476,36 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
         if (done_tiles > 0) mbar_wait(done, (done_tiles - 1) & 1, ctx, 116);
     } else if (warp >= 4) {
         pdl_wait();
-        const int e = warp - 4, quadrant = e & 3, half = e >> 2;         // lanes and columns of the accumulator this warp moves
-        const int cols = p.tile_n / 2;                                   // 64 or 128
-        unsigned char *stage = smem_raw + (smem - smem_u32(smem_raw)) + p.stages * stage_bytes + e * (kStageOut + 512);
-        float *bias = reinterpret_cast<float *>(stage + kStageOut);
-        const uint32_t from = tmem + (static_cast<uint32_t>(quadrant * 32) << 16) + half * cols;
+        const int e = warp - 4, quadrant = e & 3, quarter = e >> 2;      // lanes and columns of the accumulator this warp moves
+        const int cols = p.tile_n / 4;                                   // 32 or 64
+        unsigned char *stage = smem_raw + (smem - smem_u32(smem_raw)) + p.stages * stage_bytes + e * stage_out(PIECE);
+        float *bias = reinterpret_cast<float *>(stage + 32 * PIECE);
+        const uint32_t from = tmem + (static_cast<uint32_t>(quadrant * 32) << 16) + quarter * cols;
         T *const y = static_cast<T *>(p.y);
         const bool vector = (reinterpret_cast<uintptr_t>(p.y) | static_cast<uint64_t>(p.ldy * sizeof(T))) % 16 == 0;
-        int k = 0;
-        for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x, ++k) {
-            const int f0 = static_cast<int>(t % p.f_tiles) * p.tile_n + half * cols;
-            const int64_t row0 = t / p.f_tiles * 128 + quadrant * 32;
+        int ft = static_cast<int>(blockIdx.x % static_cast<unsigned>(p.f_tiles));
+        int nt = static_cast<int>(blockIdx.x / static_cast<unsigned>(p.f_tiles));
+        uint32_t phase = 0;
+        for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+            const int f0 = ft * p.tile_n + quarter * cols;
+            const int64_t row0 = static_cast<int64_t>(nt) * 128 + quadrant * 32;
             __syncwarp();
             for (int c = lane; c < cols; c += 32) bias[c] = p.bias && f0 + c < p.F ? p.bias[f0 + c] : 0.f;
-            if (!mbar_wait(done, k & 1, ctx, 115)) break;
+            if (!mbar_wait(done, phase, ctx, 115)) break;
+            phase ^= 1;
             tc_fence_after();
-            uint32_t v[128];
-#pragma unroll
-            for (int c = 0; c < 128; c += 32)
-                if (c < cols) tmem_ld32_async(from + c, v + c);
+            uint32_t v[64];
+            tmem_ld32_async(from, v);
+            if (cols == 64) tmem_ld32_async(from + 32, v + 32);
             asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
             tc_fence_before();
             __syncwarp();
             if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(drained) : "memory");
-            constexpr int kCols = 64 / sizeof(T);
-            const int64_t rows_left = p.rows - row0;
+            constexpr int kCols = PIECE / sizeof(T);
+            const int rows_left = static_cast<int>(min(static_cast<int64_t>(32), p.rows - row0));
+            T *out = y + row0 * p.ldy + f0;
 #pragma unroll
-            for (int c = 0; c < 128; c += kCols) {
+            for (int c = 0; c < 64; c += kCols) {
                 if (c >= cols || f0 + c >= p.F || rows_left <= 0) continue;
                 float o[kCols];
 #pragma unroll
@@ -514,8 +516,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
                     o[j + 2] = activate1<ACT>(__uint_as_float(v[c + j + 2]) + b.z);
                     o[j + 3] = activate1<ACT>(__uint_as_float(v[c + j + 3]) + b.w);
                 }
-                store_piece<T>(o, stage, y + row0 * p.ldy + f0 + c, p.ldy, rows_left, p.F - f0 - c, vector);
+                store_piece<T, PIECE>(o, stage, out + c, p.ldy, rows_left, p.F - f0 - c, vector);
             }
+            nt += p.step_n;
+            ft += p.step_f;
+            if (ft >= p.f_tiles) { ft -= p.f_tiles; ++nt; }
         }
     }
     __syncwarp();
@@ -543,8 +548,9 @@ cudaError_t prepare_mx4_linear() {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(mx4_linear_kernel<__nv_bfloat16>, what, kLinearSmem);
     for (int dtype = 0; dtype < 3 && e == cudaSuccess; ++dtype)
         for (int act = PATDNN_ACT_NONE; act <= PATDNN_ACT_SILU && e == cudaSuccess; ++act)
-            e = by_output(dtype, act, [](auto t, auto a) {
-                return cudaFuncSetAttribute(mx4_rows_kernel<decltype(t), a.value>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinearSmem);
+            e = by_output(dtype, act, [&](auto t, auto a) {
+                const cudaError_t r = cudaFuncSetAttribute(mx4_rows_kernel<decltype(t), a.value, 32>, what, kLinearSmem);
+                return r == cudaSuccess ? cudaFuncSetAttribute(mx4_rows_kernel<decltype(t), a.value, 64>, what, kLinearSmem) : r;
             });
     return e;
 }
@@ -562,14 +568,16 @@ cudaError_t launch_mx4_linear(Mx4Params p, cudaStream_t st, int *launches) {
         p.splits = 1;
         const int wide = tile_f / 128;
         const int stage = ((1 + wide) * (128 * row_bytes + 512 * atoms) + 1023) / 1024 * 1024;
-        const int out = kEpilogueWarps * (kStageOut + 512) + 1024;
+        const int piece = p.col_tiles <= 3 ? 64 : 32;
+        const int out = kEpilogueWarps * stage_out(piece) + 1024;
         p.stages = std::min(kMaxStages, (kLinearSmem - out) / stage);
         const int64_t tiles = static_cast<int64_t>(p.f_tiles) * p.n_tiles;
         const unsigned grid = static_cast<unsigned>(std::min<int64_t>(tiles, sm_count()));
         p.step_n = static_cast<int>(grid / p.f_tiles);
         p.step_f = static_cast<int>(grid % p.f_tiles);
         return by_output(p.dtype, p.act, [&](auto t, auto a) {
-            return launch_pdl(mx4_rows_kernel<decltype(t), a.value>, dim3(grid), dim3(kRowsThreads), p.stages * stage + out, st, 1, p);
+            const auto kernel = piece == 64 ? mx4_rows_kernel<decltype(t), a.value, 64> : mx4_rows_kernel<decltype(t), a.value, 32>;
+            return launch_pdl(kernel, dim3(grid), dim3(kRowsThreads), p.stages * stage + out, st, 1, p);
         });
     }
     p.f_tiles = static_cast<int>(ceil_div(p.F, 128));
