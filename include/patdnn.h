@@ -54,7 +54,7 @@ enum {
     PATDNN_E_MASK = 4,          /* a kernel's mask is neither empty nor a pattern of the set (Section 4.2) */
     PATDNN_E_ORDER = 5,         /* caller-supplied filter order is not a permutation */
     PATDNN_E_CUDA = 6,          /* a CUDA call failed; patdnn_last_cuda_error() has the text */
-    PATDNN_E_NO_DEVICE = 7,     /* handle was encoded host-only, or no CUDA device is usable */
+    PATDNN_E_NO_DEVICE = 7,     /* handle was encoded host-only, no CUDA device is usable, or another one is current (norm, linear) */
     PATDNN_E_DEVICE_TIMEOUT = 8,/* a bounded device-side wait expired */
     PATDNN_E_DTYPE = 9,         /* unknown dtype / variant value */
     PATDNN_E_ALLOC = 10,        /* host allocation failed */
@@ -290,9 +290,11 @@ PATDNN_API int patdnn_maxpool2x2(const void *in, void *out, int32_t N, int32_t C
  *              strides in elements, 0 = dense.  y strides also hold for dy, x strides for dx.
  *   E_SHAPE    N < 0, P < 1, C < 1, G < 1, C not a multiple of G, |strides| that overlap pixels (x_pixel < C, x_image < P * x_pixel ...),
  *              eps negative or not finite; N <= 65535, C <= 2^20, P < 2^31, N * P * C < 2^40
+ *              in the calls: a tensor that is not aligned to its elements, statistics that are not aligned to 8 bytes
  *   E_DTYPE    dtype or act unknown
+ *   E_NO_DEVICE  another device is current than when the handle was made
  * A handle owns its workspace: calls that can overlap on the GPU need a handle each.  N = 0 launches nothing (the gradient
- * writes zeros to dgamma and dbeta).
+ * writes zeros to dgamma and dbeta).  patdnn_norm_create waits for the device; the other calls are asynchronous on `stream`.
  */
 typedef struct patdnn_norm_s *patdnn_norm;
 typedef struct {
@@ -344,7 +346,8 @@ PATDNN_API int patdnn_mx4_dequantize(const void *mx, int32_t dtype, int64_t rows
  *                          the handle's buffer, then multiplies.  Asynchronous; calls that can overlap need a handle each.
  *   patdnn_linear_run_mx4  the same for rows that are 4-bit already (patdnn_mx4_quantize, patdnn_norm_run_mx4); any number of rows
  *   patdnn_linear_check    waits for the device; E_DEVICE_TIMEOUT if a bounded device-side wait of this handle expired
- * Errors: E_NULL, E_SHAPE (F, K < 1 or > 2^20, rows < 0 or > max_rows, a stride below its row's length), E_DTYPE, E_ALLOC, E_CUDA.
+ * Errors: E_NULL, E_SHAPE (F, K < 1 or > 2^20, rows < 0 or > max_rows, a stride below its row's length, a tensor that is not aligned to
+ * its elements), E_DTYPE, E_ALLOC, E_CUDA, E_NO_DEVICE (another device is current than when the handle was made).
  * rows = 0 launches nothing.
  */
 typedef struct patdnn_linear_s *patdnn_linear;

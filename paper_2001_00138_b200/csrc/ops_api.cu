@@ -29,6 +29,7 @@ struct patdnn_norm_s {
 struct patdnn_linear_s {
     patdnn_linear_desc d{};
     Mx4Shape shape{};                       // of the weights
+    int device = -1;
     uint8_t *w = nullptr, *x = nullptr;     // 4-bit weights; buffer for the rows of patdnn_linear_run
     float *bias = nullptr;
     int *status = nullptr;
@@ -51,6 +52,14 @@ bool mx_size_ok(int64_t rows, int64_t cols) {
     return rows >= 0 && cols >= 1 && cols <= kMostColumns && rows <= kMostElements / cols && rows <= INT32_MAX;
 }
 bool aligned(const void *p, unsigned bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+bool elements_aligned(const void *p, int dtype) { return aligned(p, static_cast<unsigned>(elem_bytes(dtype))); }
+
+// A handle's buffers belong to the device that was current when it was made.
+int on_device(int device) {
+    int now = -1;
+    CU(cudaGetDevice(&now));
+    return now == device ? PATDNN_OK : PATDNN_E_NO_DEVICE;
+}
 
 int launched(cudaError_t e, int n, const char *what) {
     if (e != cudaSuccess) return cuda_fail(e, what);
@@ -105,6 +114,12 @@ int patdnn_norm_create(const patdnn_norm_desc *desc, patdnn_norm *out) {
     if (!h) return PATDNN_E_ALLOC;
     h->h.s = s;
     if (s.N > 0) {
+        const cudaError_t de = cudaGetDevice(&h->device);
+        if (de != cudaSuccess) {
+            const int rc = cuda_fail(de, "cudaGetDevice");
+            delete h;
+            return rc;
+        }
         plan_norm(h->h);
         const size_t counters = static_cast<size_t>(s.N > s.G ? s.N : s.G);
         cudaError_t e = allocate(&h->h.ws, norm_workspace_floats(h->h));
@@ -127,6 +142,9 @@ int patdnn_norm_run(patdnn_norm h, const void *x, const float *gamma, const floa
     if (!h) return PATDNN_E_NULL;
     if (h->h.s.N == 0) return PATDNN_OK;
     if (!x || !gamma || !beta || !y) return PATDNN_E_NULL;
+    const int dtype = h->h.s.dtype;
+    if (!elements_aligned(x, dtype) || !elements_aligned(y, dtype) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(stats, 8)) return PATDNN_E_SHAPE;
+    if (const int rc = on_device(h->device)) return rc;
     int n = 0;
     const cudaError_t e = launch_group_norm(h->h, x, gamma, beta, y, stats, static_cast<cudaStream_t>(stream), &n);
     return launched(e, n, "group norm launch");
@@ -137,7 +155,9 @@ int patdnn_norm_run_mx4(patdnn_norm h, const void *x, const float *gamma, const 
     const NormShape &s = h->h.s;
     if (s.N == 0) return PATDNN_OK;
     if (!x || !gamma || !beta || !mx) return PATDNN_E_NULL;
-    if (!aligned(mx, 16) || !mx_size_ok(s.N * s.P, s.C)) return PATDNN_E_SHAPE;
+    if (!aligned(mx, 16) || !mx_size_ok(s.N * s.P, s.C) || !elements_aligned(x, s.dtype) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(stats, 8))
+        return PATDNN_E_SHAPE;
+    if (const int rc = on_device(h->device)) return rc;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     int n = 0;
     const cudaError_t e = launch_group_norm_mx4(h->h, x, gamma, beta, mx, stats, st, &n);
@@ -155,6 +175,10 @@ int patdnn_norm_grad(patdnn_norm h, const void *x, const float *gamma, const flo
         return PATDNN_OK;
     }
     if (!x || !gamma || !beta || !stats || !dy || !dx) return PATDNN_E_NULL;
+    if (!elements_aligned(x, s.dtype) || !elements_aligned(dy, s.dtype) || !elements_aligned(dx, s.dtype) || !aligned(gamma, 4) || !aligned(beta, 4) ||
+        !aligned(stats, 8) || !aligned(dgamma, 4) || !aligned(dbeta, 4))
+        return PATDNN_E_SHAPE;
+    if (const int rc = on_device(h->device)) return rc;
     int n = 0;
     const cudaError_t e = launch_group_norm_grad(h->h, x, gamma, beta, stats, dy, dx, dgamma, dbeta, st, &n);
     return launched(e, n, "group norm gradient launch");
@@ -176,7 +200,7 @@ int patdnn_mx4_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols
     if (!known_type(dtype)) return PATDNN_E_DTYPE;
     if (!mx_size_ok(rows, cols)) return PATDNN_E_SHAPE;
     if (ld == 0) ld = cols;
-    if (ld < cols || !aligned(mx, 16)) return PATDNN_E_SHAPE;
+    if (ld < cols || !aligned(mx, 16) || !elements_aligned(x, dtype)) return PATDNN_E_SHAPE;
     if (rows == 0) return PATDNN_OK;
     if (!x || !mx) return PATDNN_E_NULL;
     return launched(launch_mx4_quantize(mx4_shape(rows, cols), x, dtype, ld, mx, static_cast<cudaStream_t>(stream)), 1, "4-bit quantisation launch");
@@ -186,7 +210,7 @@ int patdnn_mx4_dequantize(const void *mx, int32_t dtype, int64_t rows, int64_t c
     if (!known_type(dtype)) return PATDNN_E_DTYPE;
     if (!mx_size_ok(rows, cols)) return PATDNN_E_SHAPE;
     if (ld == 0) ld = cols;
-    if (ld < cols || !aligned(mx, 16)) return PATDNN_E_SHAPE;
+    if (ld < cols || !aligned(mx, 16) || !elements_aligned(out, dtype)) return PATDNN_E_SHAPE;
     if (rows == 0) return PATDNN_OK;
     if (!out || !mx) return PATDNN_E_NULL;
     return launched(launch_mx4_dequantize(mx4_shape(rows, cols), mx, out, dtype, ld, static_cast<cudaStream_t>(stream)), 1, "4-bit read-back launch");
@@ -198,14 +222,15 @@ int patdnn_linear_encode(const void *weights, int64_t ldw, const patdnn_linear_d
     if (desc->F < 1 || desc->K < 1 || !mx_size_ok(desc->F, desc->K) || desc->F > kMostColumns || !mx_size_ok(desc->max_rows, desc->K))
         return PATDNN_E_SHAPE;
     if (ldw == 0) ldw = desc->K;
-    if (ldw < desc->K) return PATDNN_E_SHAPE;
+    if (ldw < desc->K || !elements_aligned(weights, desc->dtype) || !aligned(desc->bias, 4)) return PATDNN_E_SHAPE;
     patdnn_linear h = new (std::nothrow) patdnn_linear_s();
     if (!h) return PATDNN_E_ALLOC;
     h->d = *desc;
     h->d.bias = nullptr;
     h->shape = mx4_shape(desc->F, desc->K);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    cudaError_t e = allocate(&h->w, static_cast<size_t>(h->shape.bytes));
+    cudaError_t e = cudaGetDevice(&h->device);
+    if (e == cudaSuccess) e = allocate(&h->w, static_cast<size_t>(h->shape.bytes));
     if (e == cudaSuccess && desc->max_rows) e = allocate(&h->x, static_cast<size_t>(mx4_shape(desc->max_rows, desc->K).bytes));
     if (e == cudaSuccess) e = allocate(&h->status, 4);
     if (e == cudaSuccess) e = cudaMemsetAsync(h->status, 0, 16, st);
@@ -232,9 +257,11 @@ int patdnn_linear_run(patdnn_linear h, const void *x, int64_t rows, int64_t ldx,
     if (!h) return PATDNN_E_NULL;
     if (ldx == 0) ldx = h->d.K;
     if (ldy == 0) ldy = h->d.F;
-    if (rows < 0 || rows > h->d.max_rows || ldx < h->d.K || ldy < h->d.F) return PATDNN_E_SHAPE;
+    if (rows < 0 || rows > h->d.max_rows || ldx < h->d.K || ldy < h->d.F || !elements_aligned(x, h->d.dtype) || !elements_aligned(y, h->d.dtype))
+        return PATDNN_E_SHAPE;
     if (rows == 0) return PATDNN_OK;
     if (!x || !y) return PATDNN_E_NULL;
+    if (const int rc = on_device(h->device)) return rc;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (rows <= kFusedRows) return product(h, nullptr, x, ldx, rows, y, ldy, st);
     const int rc = launched(launch_mx4_quantize(mx4_shape(rows, h->d.K), x, h->d.dtype, ldx, h->x, st), 1, "4-bit quantisation launch");
@@ -244,14 +271,16 @@ int patdnn_linear_run(patdnn_linear h, const void *x, int64_t rows, int64_t ldx,
 int patdnn_linear_run_mx4(patdnn_linear h, const void *mx, int64_t rows, void *y, int64_t ldy, void *stream) {
     if (!h) return PATDNN_E_NULL;
     if (ldy == 0) ldy = h->d.F;
-    if (!mx_size_ok(rows, h->d.K) || ldy < h->d.F || !aligned(mx, 16)) return PATDNN_E_SHAPE;
+    if (!mx_size_ok(rows, h->d.K) || ldy < h->d.F || !aligned(mx, 16) || !elements_aligned(y, h->d.dtype)) return PATDNN_E_SHAPE;
     if (rows == 0) return PATDNN_OK;
     if (!mx || !y) return PATDNN_E_NULL;
+    if (const int rc = on_device(h->device)) return rc;
     return product(h, mx, nullptr, 0, rows, y, ldy, static_cast<cudaStream_t>(stream));
 }
 
 int patdnn_linear_check(patdnn_linear h) {
     if (!h) return PATDNN_E_NULL;
+    if (const int rc = on_device(h->device)) return rc;
     CU(cudaDeviceSynchronize());
     int word = 0;
     CU(cudaMemcpy(&word, h->status, sizeof(int), cudaMemcpyDeviceToHost));

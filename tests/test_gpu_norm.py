@@ -226,6 +226,8 @@ def test_null_pointers_are_refused():
         with pytest.raises(B.PatdnnError) as e:
             call()
         assert e.value.status == 1
-    with pytest.raises(B.PatdnnError) as e:
-        h.run_mx4(64, 64, 64, 72)
-    assert e.value.status == 2
+    for call in (lambda: h.run_mx4(64, 64, 64, 72), lambda: h.run(66, 64, 64, 64), lambda: h.run(64, 64, 64, 64, stats=68), lambda: h.run(64, 66, 64, 64),
+                 lambda: h.grad(64, 64, 64, 64, 64, 66, 64, 64), lambda: h.grad(64, 64, 64, 68, 64, 64, 64, 64)):
+        with pytest.raises(B.PatdnnError) as e:
+            call()
+        assert e.value.status == 2

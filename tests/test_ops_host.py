@@ -52,6 +52,8 @@ def test_mx4_refusals(call):
     refused(E_SHAPE, call, 64, 64, -1, 32)
     refused(E_SHAPE, B.mx4_quantize, 64, 72, 1, 32)           # the 4-bit buffer is not 16-byte aligned
     refused(E_SHAPE, B.mx4_dequantize, 72, 64, 1, 32)
+    refused(E_SHAPE, B.mx4_quantize, 66, 64, 1, 32)           # a tensor that is not aligned to its elements
+    refused(E_SHAPE, B.mx4_dequantize, 64, 66, 1, 32)
     refused(E_NULL, call, 0, 0, 1, 32)
     call(0, 0, 0, 32)                                         # no rows: nothing to do
 
