@@ -142,7 +142,10 @@ def _check(rc: int, where: str) -> None:
 
 def _ptr(x) -> int:
     """Raw address of a device buffer: an int, or anything with ``data_ptr()``."""
-    return int(x.data_ptr()) if hasattr(x, "data_ptr") else int(x)
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        return int(x)
 
 
 class Layer:
@@ -320,6 +323,7 @@ class Stack:
 
 def _opt(x) -> int:
     return 0 if x is None else _ptr(x)
+
 
 
 class GroupNorm:
