@@ -155,22 +155,23 @@ struct Stream {
             src_step = -src_step;
         }
     }
-    __device__ __forceinline__ void one() {
-        if constexpr (kBytes >= 4) {
-            copy_async<kBytes>(to, src);
-        } else {
-            const uint16_t t = *reinterpret_cast<const uint16_t *>(src);
-            asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"(t) : "memory");
-        }
-        src += src_step;
-        to += step;
-    }
     __device__ __forceinline__ void copy() {           // one batch
         if (left >= kBatch) {
+            if constexpr (kBytes >= 4) {
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) one();
+                for (int u = 0; u < kBatch; ++u, src += src_step, to += step) copy_async<kBytes>(to, src);
+            } else {                                   // two bytes are too few for an asynchronous copy: all loads before the first store
+                uint16_t t[kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u, src += src_step) t[u] = *reinterpret_cast<const uint16_t *>(src);
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u, to += step) asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"(t[u]) : "memory");
+            }
         } else {
-            for (int u = 0; u < left; ++u) one();
+            for (int u = 0; u < left; ++u, src += src_step, to += step) {
+                if constexpr (kBytes >= 4) copy_async<kBytes>(to, src);
+                else asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"(*reinterpret_cast<const uint16_t *>(src)) : "memory");
+            }
         }
         left -= kBatch;
         if (!KEEP && to == end) to = ring;
@@ -300,12 +301,24 @@ __device__ __forceinline__ void join_groups(const float2 *red, int rows, int cha
 }
 
 // act(norm) of a CTA's pixels from shared memory, as rows of a 4-bit matrix.  A thread keeps eight columns and walks over the
-// pixels; four neighbouring lanes share a block of 32.  The last slab also writes the zeros up to a multiple of 64 columns, which
-// the product's steps cover.
+// pixels; four neighbouring lanes share a block of 32.  The product's steps cover 64 columns: where the last one holds a single block,
+// the other is written as zeros.
 template <typename T, int ACT>
 __device__ __forceinline__ void write_mx4(const NormArgs &a, const T *tile, const float2 *fin, const float *gamma, const float *beta_of, int n, int64_t p0, int pixels, int c0, int channels) {
-    const int width = c0 + channels == a.C ? (a.C + 63) / 64 * 64 - c0 : channels;
-    const int units = width / 8, rows = kThreads / units;
+    const int row0 = static_cast<int>(n * a.P + p0);   // (a 4-bit matrix has fewer than 2^31 rows)
+    const int row_bytes = a.mx_width / 2, code_bytes = 128 * row_bytes, scale_bytes = a.mx_width > 128 ? 1024 : 512;
+    const int units = (channels + 31) / 32 * 4, rows = kThreads / units;
+    if (c0 + channels == a.C && (a.C - 1) / 32 % 2 == 0) {             // an odd number of blocks: the one beside the last is zero
+        const int c = (a.C + 31) / 32 * 32, ct = c / a.mx_width, in_tile = c - ct * a.mx_width;
+        for (int p = threadIdx.x; p < pixels; p += kThreads) {
+            const int row = row0 + p, r = row & 127;
+            const int64_t t = static_cast<int64_t>(row >> 7) * a.mx_col_tiles + ct;
+            int at = r * row_bytes + in_tile / 2;
+            at ^= ((at >> 7) & (a.mx_width / 32 - 1)) << 4;
+            *reinterpret_cast<uint4 *>(a.mx + t * code_bytes + at) = make_uint4(0, 0, 0, 0);
+            a.mx[a.mx_scales + t * scale_bytes + (in_tile >> 7) * 512 + ((in_tile >> 5) & 3) + (r & 31) * 16 + (r >> 5) * 4] = 0;
+        }
+    }
     const int unit = threadIdx.x % units, first = threadIdx.x / units;
     const int c = unit * 8;
     const Groups<8> at(c, a.per);
@@ -316,8 +329,6 @@ __device__ __forceinline__ void write_mx4(const NormArgs &a, const T *tile, cons
     const bool whole = c + 8 <= channels && channels % (16 / sizeof(T)) == 0;
     const int ct = (c0 + c) / a.mx_width, in_tile = (c0 + c) - ct * a.mx_width;
     const int scale_col = (in_tile >> 7) * 512 + ((in_tile >> 5) & 3);
-    const int row_bytes = a.mx_width / 2, code_bytes = 128 * row_bytes, scale_bytes = a.mx_width > 128 ? 1024 : 512;
-    const int row0 = static_cast<int>(n * a.P + p0);
     for (int base = 0; base < pixels; base += rows) {
         const int p = base + first;
         const bool on = first < rows && p < pixels;
@@ -346,7 +357,7 @@ __device__ __forceinline__ void write_mx4(const NormArgs &a, const T *tile, cons
         uint32_t codes;
         const uint32_t byte = quantise8(v, codes);
         if (on) {
-            const int row = row0 + p, r = row & 127;   // (a 4-bit matrix has fewer than 2^31 rows)
+            const int row = row0 + p, r = row & 127;
             const int64_t t = static_cast<int64_t>(row >> 7) * a.mx_col_tiles + ct;
             int at = r * row_bytes + in_tile / 2;
             at ^= ((at >> 7) & (a.mx_width / 32 - 1)) << 4;
@@ -933,7 +944,7 @@ constexpr int64_t kRunBytes = int64_t(160) << 20;   // two-pass: bytes of x (and
 // 3 % of it): the CTAs of an SM share its HBM rate of 44 bytes per ns; a wave costs half a microsecond, a cluster one more and 0.3 per
 // doubling; slabs narrower than 128 bytes cost 10 %; the gradient, bound by its arithmetic, wants three CTAs per SM.
 // Besides, an SM takes at most kRate elements per us through its arithmetic (a third of that at single-element accesses, a quarter for
-// the gradient; 4-bit rows are padded to 64 columns): few CTAs on a large image lose against the two passes.
+// the gradient; twice the time for 4-bit rows, padded to 32 columns, and six times where SiLU is formed as written): few CTAs on a large image lose against the two passes.
 // `unit`: slabs are a multiple of so many channels (or all of them).
 NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
     NormPlan best;
@@ -958,7 +969,7 @@ NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
             const double here = std::min<double>(per_sm, std::ceil(ctas / 148));           // CTAs of an SM at a time
             const double waves = std::ceil(ctas / (148 * here));
             const double bytes = static_cast<double>(chunk) * slab * e * (tensors + 1);
-            const double wide = unit > 1 ? (slab + 63) / 64 * 64.0 : static_cast<double>(slab);
+            const double wide = unit > 1 ? (slab + 31) / 32 * 32.0 * (s.act == PATDNN_ACT_SILU ? 6 : 2) : static_cast<double>(slab);
             const double work = chunk * (slab * slow + wide) * (tensors == 2 ? 2.0 : 0.5) / kRate;
             const double memory = here * bytes / 44e3 * (slab * e < 128 && k < s.G ? 1.1 : 1.0) * (tensors == 2 ? 1 + 0.4 * (3 - here) : 1.0);
             const double us = waves * (std::max(memory, here * work) +

@@ -121,15 +121,16 @@ __global__ void __launch_bounds__(kWarps * 32, quant_ctas<T, A>()) mx4_quantize_
     }
 }
 
-// A group norm in front: blockIdx.x = row tile * col_tiles + column tile.  The warps walk over the 32 row sets of a row tile; the constants
-// of a lane's columns are loaded once per image.
+// A group norm in front: blockIdx.x = (row tile * parts + part) * col_tiles + column tile.  The warps of a tile's `parts` CTAs (more than
+// one where there are too few tiles for the SMs) walk over its 32 row sets; the constants of a lane's columns are loaded once per image.
 template <typename T, int A, int ACT>
 __global__ void __launch_bounds__(kWarps * 32) norm_quantize_kernel(QuantArgs a) {
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int ct = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.col_tiles));
     const unsigned rest = blockIdx.x / static_cast<unsigned>(a.col_tiles);
-    const int64_t rt = a.row0 / 128 + rest;
+    const int parts = 1 << a.part_shift, part = static_cast<int>(rest) & (parts - 1);
+    const int64_t rt = a.row0 / 128 + (rest >> a.part_shift);
     const int in_row = lane & (a.lanes - 1), together = 32 / a.lanes;  // this lane's place in its row; row sets a warp takes at a time
     const int64_t c = static_cast<int64_t>(ct) * a.width + in_row * 8;
     const int row_bytes = a.width / 2;
@@ -139,7 +140,7 @@ __global__ void __launch_bounds__(kWarps * 32) norm_quantize_kernel(QuantArgs a)
     pdl_wait();
     float mean[8], rstd[8], gamma[8], beta[8];                         // of image `image`
     int image = -1;
-    for (int first = warp * together; first < 32; first += kWarps * together) {
+    for (int first = (part * kWarps + warp) * together; first < 32; first += parts * kWarps * together) {
         if (rt * 128 + first >= a.rows) return;                        // (the same for the warp; higher rows of its sets do not exist either)
         const int r0 = first + lane / a.lanes;
         Raw<T, A> raw[4];
@@ -375,9 +376,11 @@ cudaError_t launch_norm_quantize(const NormShape &s, const Mx4Shape &m, const vo
     a.gamma = gamma; a.beta = beta; a.stats = stats;
     a.P = s.P; a.x_image = s.x_image; a.G = s.G; a.per = s.C / s.G;
     const int64_t tiles = ceil_div(a.rows, 128) - row0 / 128;
+    // (part_shift as quant_args left it: as many parts as there are warps' row sets in a tile)
+    while (a.part_shift > 0 && (tiles * m.col_tiles << a.part_shift) > 4 * sm_count()) --a.part_shift;
     return by_access(s.dtype, access_index(s.dtype, x, s.x_pixel, s.x_image), [&](auto t, auto v) {
         return by_act(s.act, [&](auto c) {
-            return launch_pdl(norm_quantize_kernel<decltype(t), v.value, c.value>, dim3(static_cast<unsigned>(tiles * m.col_tiles)), dim3(kWarps * 32), 0, st, 1, a);
+            return launch_pdl(norm_quantize_kernel<decltype(t), v.value, c.value>, dim3(static_cast<unsigned>(tiles * m.col_tiles << a.part_shift)), dim3(kWarps * 32), 0, st, 1, a);
         });
     });
 }

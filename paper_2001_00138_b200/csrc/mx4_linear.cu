@@ -336,10 +336,11 @@ __device__ __forceinline__ void store_piece(const float (&v)[PIECE / sizeof(T)],
             if (r < rows_left) *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(y + r * ldy) + q * 16) = t;
         }
     } else {
-        const int rows = min(rows_left, 32);
-        for (int i = lane; i < rows * kCols; i += 32) {
-            const int r = i / kCols, c = i % kCols, b = c * static_cast<int>(sizeof(T));
-            if (c < cols_left) y[r * ldy + c] = *reinterpret_cast<const T *>(stage + place(r, b >> 4) + (b & 15));
+        const int c = lane % kCols, b = c * static_cast<int>(sizeof(T));
+        if (c < cols_left) {
+#pragma unroll 8
+            for (int r = lane / kCols; r < 32; r += 32 / kCols)
+                if (r < rows_left) y[r * ldy + c] = *reinterpret_cast<const T *>(stage + place(r, b >> 4) + (b & 15));
         }
     }
 }
@@ -486,11 +487,19 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
         int ft = static_cast<int>(blockIdx.x % static_cast<unsigned>(p.f_tiles));
         int nt = static_cast<int>(blockIdx.x / static_cast<unsigned>(p.f_tiles));
         uint32_t phase = 0;
+        auto bias_of = [&](int f) { return p.bias && f < p.F ? p.bias[f] : 0.f; };
+        float ahead0 = bias_of(ft * p.tile_n + quarter * cols + lane), ahead1 = bias_of(ft * p.tile_n + quarter * cols + 32 + lane);
         for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
             const int f0 = ft * p.tile_n + quarter * cols;
             const int64_t row0 = static_cast<int64_t>(nt) * 128 + quadrant * 32;
+            nt += p.step_n;                                              // the tile gridDim.x further on, whose bias is fetched meanwhile
+            ft += p.step_f;
+            if (ft >= p.f_tiles) { ft -= p.f_tiles; ++nt; }
             __syncwarp();
-            for (int c = lane; c < cols; c += 32) bias[c] = p.bias && f0 + c < p.F ? p.bias[f0 + c] : 0.f;
+            bias[lane] = ahead0;
+            if (cols == 64) bias[32 + lane] = ahead1;
+            ahead0 = bias_of(ft * p.tile_n + quarter * cols + lane);
+            ahead1 = bias_of(ft * p.tile_n + quarter * cols + 32 + lane);
             if (!mbar_wait(done, phase, ctx, 115)) break;
             phase ^= 1;
             tc_fence_after();
@@ -518,9 +527,6 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
                 }
                 store_piece<T, PIECE>(o, stage, out + c, p.ldy, rows_left, p.F - f0 - c, vector);
             }
-            nt += p.step_n;
-            ft += p.step_f;
-            if (ft >= p.f_tiles) { ft -= p.f_tiles; ++nt; }
         }
     }
     __syncwarp();
@@ -585,8 +591,12 @@ cudaError_t launch_mx4_linear(Mx4Params p, cudaStream_t st, int *launches) {
     p.tile_n = p.rows <= 128 ? static_cast<int>(ceil_div(p.rows, 16) * 16) : 128;
     p.n_tiles = static_cast<int>(ceil_div(p.rows, p.tile_n));
     const int64_t tiles = static_cast<int64_t>(p.f_tiles) * p.n_tiles;
+    // Exchanging partial sums takes time in proportion to the rows: with up to 64 a column tile per CTA is enough (64 x 2048 -> 1000: 4.7 us
+    // in eight splits, 6.9 in none), with more it takes sixteen column tiles, four to a CTA (300 x 4096 -> 1000: 8.4 us, 11.5 in none;
+    // but 1000 x 2048 -> 256 with its eight: 8.2 us in none, 10.4 in two splits).
+    const int least = p.tile_n <= 64 ? 1 : p.col_tiles < 16 ? p.col_tiles : 4;
     p.splits = 1;
-    while (p.splits < 8 && tiles * p.splits * 2 <= sm_count() && p.splits * 2 <= p.col_tiles) p.splits *= 2;
+    while (p.splits < 8 && tiles * p.splits * 2 <= sm_count() && p.col_tiles >= p.splits * 2 * least) p.splits *= 2;
     p.tiles_per_split = static_cast<int>(ceil_div(p.col_tiles, p.splits));
     const int stage = (128 * row_bytes + p.tile_n * row_bytes + 512 * atoms * 2 + 1023) / 1024 * 1024;
     p.stages = std::max(1, std::min({kMaxStages, p.tiles_per_split, 200 * 1024 / stage}));
