@@ -9,6 +9,8 @@
 // holds 8 consecutive columns, four lanes share a block (two shuffles give amax), every lane writes 4 bytes of codes and the warp
 // together one row of the tile, 128 consecutive bytes (two or four rows of a narrow tile).  It takes four rows 32 apart, since the scales of rows r, r + 32, r + 64 and
 // r + 96 are neighbours in memory (16 bytes): 4 loads in flight per lane, and full 32-byte sectors for the scales.
+// Measured, 16384 x 4096 bf16: 36 us for 134 MB read and 36 MB written (67 % of the issue slots), 27 to 33 us back; an 8192 x 4096
+// matrix that is in L2 15.6 us.
 #include "ops.hpp"
 
 #include <algorithm>
