@@ -255,3 +255,48 @@ def test_another_stream_and_a_captured_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want)
+
+
+def test_offsets_beyond_32_bits():
+    """A matrix of more than 2^31 elements: quantised, read back, and multiplied; its first and last rows are looked at."""
+    import torch
+    from paper_2001_00138_b200 import binding as B
+    rows, K, F = 2 ** 23 + 133, 256, 16
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(rows, K, dtype=torch.bfloat16, device="cuda")
+    for lo in range(0, rows, 1 << 20):                      # in pieces: the generator's fp32 values are never all there at once
+        x[lo:lo + (1 << 20)].copy_(torch.randn(min(1 << 20, rows - lo), K, generator=g, device="cuda"))
+    w = torch.randn(F, K, generator=g, device="cuda").bfloat16()
+    mx = torch.empty(B.mx4_bytes(rows, K), dtype=torch.uint8, device="cuda")
+    back, y = torch.empty_like(x), torch.empty(rows, F, dtype=torch.bfloat16, device="cuda")
+    B.mx4_quantize(x, mx, rows, K, dtype=B.BF16, stream=stream())
+    B.mx4_dequantize(mx, back, rows, K, dtype=B.BF16, stream=stream())
+    lin = B.Linear(w, F, K, max_rows=0, dtype=B.BF16, stream=stream())
+    lin.run_mx4(mx, y, rows, stream=stream())
+    lin.check()
+    wq = R.quantise(w.double().cpu().numpy())
+    for part in (slice(0, 200), slice(2 ** 23 - 70, 2 ** 23 + 133)):
+        xq = R.quantise(x[part].double().cpu().numpy())
+        assert np.array_equal(back[part].double().cpu().numpy(), xq)
+        ref = xq @ wq.T
+        R.within(y[part].double().cpu().numpy(), ref, 14 * 2.0 ** -23 * (np.abs(xq) @ np.abs(wq).T) + R.UNIT["bf16"] * np.abs(ref) * 1.01 + R.TINY["bf16"], "y")
+
+
+@pytest.mark.parametrize("rows", [3, 40])
+def test_row_strides_beyond_32_bits(rows):
+    """Rows so far apart that the last ones lie beyond 2^31 elements, for the kernel that quantises few rows itself and for two launches."""
+    import torch
+    from paper_2001_00138_b200 import binding as B
+    K, F = 300, 130
+    ld = 2 ** 31 // (rows - 1) + 64
+    g = torch.Generator().manual_seed(rows)
+    x, w = torch.randn(rows, K, generator=g).half(), (torch.randn(F, K, generator=g) / 17).half()
+    fx, fy = (torch.empty((rows - 1) * ld + n, dtype=torch.float16, device="cuda") for n in (K, F))
+    xv, y = torch.as_strided(fx, (rows, K), (ld, 1)), torch.as_strided(fy, (rows, F), (ld, 1))
+    xv.copy_(x)
+    lin = B.Linear(w.cuda(), F, K, max_rows=rows, dtype=B.F16, stream=stream())
+    lin.run(xv, y, rows, ldx=ld, ldy=ld, stream=stream())
+    lin.check()
+    xq, wq = R.quantise(x.double().numpy()), R.quantise(w.double().numpy())
+    ref = xq @ wq.T
+    R.within(y.double().cpu().numpy(), ref, 15 * 2.0 ** -23 * (np.abs(xq) @ np.abs(wq).T) + R.UNIT["f16"] * np.abs(ref) * 1.01 + R.TINY["f16"], "y")

@@ -231,3 +231,37 @@ def test_null_pointers_are_refused():
         with pytest.raises(B.PatdnnError) as e:
             call()
         assert e.value.status == 2
+
+
+@pytest.mark.parametrize("P", [40, 60000])
+def test_offsets_beyond_32_bits(P):
+    """The second image begins 2^31 + 8 elements behind the first, in x, y, dy and dx."""
+    import torch
+    from paper_2001_00138_b200 import binding as B
+    N, C, G = 2, 64, 8
+    far = 2 ** 31 + 8
+    g = torch.Generator().manual_seed(P)
+    x = (torch.randn(N, P, C, generator=g) + torch.randn(C, generator=g)).bfloat16()
+    dy = torch.randn(N, P, C, generator=g).bfloat16()
+    gamma, beta = 1 + 0.3 * torch.randn(C, generator=g), 0.3 * torch.randn(C, generator=g)
+
+    def place(v):
+        flat = torch.empty(far + P * C, dtype=torch.bfloat16, device="cuda")
+        view = torch.as_strided(flat, (N, P, C), (far, C, 1))
+        view.copy_(v)
+        return view
+
+    xv, dv, y, dx = place(x), place(dy), place(torch.zeros(N, P, C)), place(torch.zeros(N, P, C))
+    h = B.GroupNorm(N, P, C, G, dtype=B.BF16, act=B.ACT_SILU, eps=EPS, x_image=far, y_image=far)
+    stats = torch.empty(N, G, 2, device="cuda")
+    dgamma, dbeta = torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    st = torch.cuda.current_stream().cuda_stream
+    h.run(xv, gamma.cuda(), beta.cuda(), y, stats, st)
+    h.grad(xv, gamma.cuda(), beta.cuda(), stats, dv, dx, dgamma, dbeta, st)
+    torch.cuda.synchronize()
+    ref = R.norm_grad(x.double().numpy(), gamma.double().numpy(), beta.double().numpy(), G, EPS, "silu", dy.double().numpy())
+    f = ref["fwd"]
+    size = np.abs(gamma.double().numpy()) * (np.abs(f["xh"]) + np.abs(f["mc"]) * f["rc"] + 1) + np.abs(beta.double().numpy())
+    R.within(y.double().cpu().numpy(), f["y"], 40 * R.EPS24 * size + R.UNIT["bf16"] * np.abs(f["y"]) * 1.01 + R.TINY["bf16"], "y")
+    R.within(dx.double().cpu().numpy(), ref["dx"], 128 * R.EPS24 * ref["dx_size"] * (1 + np.abs(f["mc"]) * f["rc"]) + R.UNIT["bf16"] * np.abs(ref["dx"]) * 1.01 + 1e-6, "dx")
+    R.within(dbeta.double().cpu().numpy(), ref["dbeta"], 128 * R.EPS24 * ref["dbeta_size"], "dbeta")
