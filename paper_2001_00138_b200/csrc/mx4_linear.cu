@@ -310,7 +310,7 @@ __device__ __forceinline__ void tmem_ld32_async(uint32_t addr, uint32_t *v) {
 
 // One warp: PIECE bytes of 32 rows, from registers to y.
 template <typename T, int PIECE>
-__device__ __forceinline__ void store_piece(const float (&v)[PIECE / sizeof(T)], unsigned char *stage, T *y, int64_t ldy, int rows_left, int cols_left, bool vector) {
+__device__ __forceinline__ void store_piece(const float (&v)[PIECE / sizeof(T)], unsigned char *stage, T *y, int64_t ldy, int rows_left, int cols_left, int aligned) {
     const int lane = threadIdx.x & 31;
     constexpr int kCols = PIECE / sizeof(T), kUnits = PIECE / 16, kShift = PIECE == 64 ? 1 : 2;
     uint32_t w[PIECE / 4];
@@ -332,12 +332,24 @@ __device__ __forceinline__ void store_piece(const float (&v)[PIECE / sizeof(T)],
 #pragma unroll
     for (int q = 0; q < kUnits; ++q) *reinterpret_cast<uint4 *>(stage + place(lane, q)) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
     __syncwarp();
-    if (vector && cols_left >= kCols) {
+    if (aligned == 16 && cols_left >= kCols) {
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
             const int r = i * (32 / kUnits) + lane / kUnits, q = lane % kUnits;
             const uint4 t = *reinterpret_cast<const uint4 *>(stage + place(r, q));
             if (r < rows_left) *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(y + r * ldy) + q * 16) = t;
+        }
+    } else if (sizeof(T) == 2 && aligned >= 4) {       // pairs of columns
+        constexpr int kPairs = PIECE / 4;
+        const int c = lane % kPairs * 2;
+        if (c < cols_left) {
+#pragma unroll 8
+            for (int r = lane / kPairs; r < 32; r += 32 / kPairs) {
+                if (r >= rows_left) continue;
+                const uint32_t t = *reinterpret_cast<const uint32_t *>(stage + place(r, c >> 3) + (c * 2 & 15));
+                if (c + 1 < cols_left) *reinterpret_cast<uint32_t *>(y + r * ldy + c) = t;
+                else *reinterpret_cast<uint16_t *>(y + r * ldy + c) = static_cast<uint16_t>(t);
+            }
         }
     } else {
         const int c = lane % kCols, b = c * static_cast<int>(sizeof(T));
@@ -487,7 +499,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
         float *bias = reinterpret_cast<float *>(stage + 32 * PIECE);
         const uint32_t from = tmem + (static_cast<uint32_t>(quadrant * 32) << 16) + quarter * cols;
         T *const y = static_cast<T *>(p.y);
-        const bool vector = (reinterpret_cast<uintptr_t>(p.y) | static_cast<uint64_t>(p.ldy * sizeof(T))) % 16 == 0;
+        const uint64_t places = reinterpret_cast<uintptr_t>(p.y) | static_cast<uint64_t>(p.ldy * sizeof(T));
+        const int aligned = places % 16 == 0 ? 16 : places % 4 == 0 ? 4 : 2;
         int ft = static_cast<int>(blockIdx.x % static_cast<unsigned>(p.f_tiles));
         int nt = static_cast<int>(blockIdx.x / static_cast<unsigned>(p.f_tiles));
         uint32_t phase = 0;
@@ -529,7 +542,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
                     o[j + 2] = activate1<ACT>(__uint_as_float(v[c + j + 2]) + b.z);
                     o[j + 3] = activate1<ACT>(__uint_as_float(v[c + j + 3]) + b.w);
                 }
-                store_piece<T, PIECE>(o, stage, out + c, p.ldy, rows_left, p.F - f0 - c, vector);
+                store_piece<T, PIECE>(o, stage, out + c, p.ldy, rows_left, p.F - f0 - c, aligned);
             }
         }
     }
