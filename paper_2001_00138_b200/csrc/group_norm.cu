@@ -11,9 +11,9 @@
 //   resident  a thread-block cluster (up to 8 CTAs) owns a slab of whole groups of one image, keeps it in shared memory
 //             while the statistics are formed and joined over distributed shared memory, and writes the result from there: one
 //             launch, every value read once.
-//   two-pass  images whose slabs do not fit: partial statistics per (chunk of pixels, group), a small kernel that joins
-//             them, and an elementwise pass that reads x again.  Images are taken in runs of at most kRunBytes, so that
-//             the second read comes from L2.
+//   two-pass  images whose slabs do not fit, or for which one launch would keep too few SMs busy: partial statistics per (chunk of
+//             pixels, group), a small kernel that joins them, and an elementwise pass that reads x again.  Images are taken in runs of
+//             at most kRunBytes, and the second pass walks backwards, so that part of that read comes from L2.
 // Measured: forward 2 x 512 x 512 x 128 bf16 SiLU 75 us (statistics 29 us, 4.6 TB/s; join 3.5; elementwise 39, bound by the special-function
 // unit and instruction issue), floor 41 us; gradient 32 x 56 x 56 x 256 bf16 SiLU 56 us (26 + 4.6 + 27), floor 24 us, bound by issue;
 // resident forward 32 x 56 x 56 x 64 fp16 ReLU 10.8 us, floor 3.9.

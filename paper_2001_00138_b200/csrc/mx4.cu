@@ -75,6 +75,12 @@ __global__ void __launch_bounds__(kWarps * 32, quant_ctas<T, A>()) mx4_quantize_
         if (c + 8 <= a.cols && row + 96 < a.rows) {
 #pragma unroll
             for (int k = 0; k < 4; ++k, src += down) raw[k].load(src);
+        } else if (c + 8 <= a.cols) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k, src += down) {
+                if (row + 32 * k < a.rows) raw[k].load(src);
+                else raw[k].clear();
+            }
         } else {
             const int count = static_cast<int>(max(int64_t(0), min(int64_t(8), a.cols - c)));
 #pragma unroll
