@@ -297,35 +297,28 @@ __global__ void __launch_bounds__(kWarps * 32) mx4_dequantize_single_kernel(Quan
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int ct = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.col_tiles));
     const unsigned rest = blockIdx.x / static_cast<unsigned>(a.col_tiles);
-    const int64_t rt = rest >> 2;
-    const int r0 = static_cast<int>(rest & 3) * kWarps + warp;
-    const int row_bytes = a.width / 2;
+    const int64_t row = static_cast<int64_t>(rest) * kWarps + warp, rt = row >> 7;        // a warp takes one row of a column tile
+    const int r = static_cast<int>(row & 127), row_bytes = a.width / 2;
     const uint8_t *codes_in = a.mx + (rt * a.col_tiles + ct) * a.code_bytes;
-    const uint8_t *scales_in = a.mx + a.scales_at + (rt * a.col_tiles + ct) * a.scale_bytes;
+    const uint8_t *scales_in = a.mx + a.scales_at + (rt * a.col_tiles + ct) * a.scale_bytes + (r & 31) * 16 + (r >> 5) * 4;
     const int cols = static_cast<int>(min(static_cast<int64_t>(a.width), a.cols - static_cast<int64_t>(ct) * a.width));
     pdl_wait();
-    uint32_t word[4][8], scale[4][8];
+    if (row >= a.rows) return;
+    uint32_t word[8], scale[8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int j = 0; j < 8; ++j) {
+        const int c = 32 * j + lane;
+        if (32 * j >= a.width) continue;               // (the whole tile is there to read, whatever columns it holds)
+        int at = r * row_bytes + (c >> 3) * 4;
+        at ^= ((at >> 7) & (a.width / 32 - 1)) << 4;
+        word[j] = *reinterpret_cast<const uint32_t *>(codes_in + at);
+        scale[j] = scales_in[(c >> 7) * 512 + (j & 3)];
+    }
+    T *dst = out + row * a.ld + static_cast<int64_t>(ct) * a.width;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int c = 32 * j + lane;
-            if (32 * j >= a.width) continue;           // (the whole tile is there to read, whatever rows and columns it holds)
-            int at = (r0 + 32 * k) * row_bytes + (c >> 3) * 4;
-            at ^= ((at >> 7) & (a.width / 32 - 1)) << 4;
-            word[k][j] = *reinterpret_cast<const uint32_t *>(codes_in + at);
-            scale[k][j] = scales_in[(c >> 7) * 512 + r0 * 16 + k * 4 + (j & 3)];
-        }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int64_t row = rt * 128 + r0 + 32 * k;
-        if (row >= a.rows) continue;
-        T *dst = out + row * a.ld + static_cast<int64_t>(ct) * a.width;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int c = 32 * j + lane;
-            if (c < cols) dst[c] = from_float<T>(value_of((word[k][j] >> (4 * (c & 7))) & 15, scale_value(scale[k][j])));
-        }
+    for (int j = 0; j < 8; ++j) {
+        const int c = 32 * j + lane;
+        if (c < cols) dst[c] = from_float<T>(value_of((word[j] >> (4 * (c & 7))) & 15, scale_value(scale[j])));
     }
 }
 
@@ -398,7 +391,7 @@ cudaError_t launch_mx4_dequantize(const Mx4Shape &m, const void *mx, void *out, 
     return by_access(dtype, access_index(dtype, out, ld), [&](auto t, auto v) {
         using T = decltype(t);
         if constexpr (sizeof(T) * v.value < 4 || v.value == 1)
-            return launch_pdl(mx4_dequantize_single_kernel<T>, dim3(quant_grid(m, kWarps)), dim3(kWarps * 32), 0, st, 1, a, static_cast<T *>(out));
+            return launch_pdl(mx4_dequantize_single_kernel<T>, dim3(static_cast<unsigned>(ceil_div(m.rows, kWarps) * m.col_tiles)), dim3(kWarps * 32), 0, st, 1, a, static_cast<T *>(out));
         else
             return launch_pdl(mx4_dequantize_kernel<T, v.value>, dim3(quant_grid(m, kWarps * (32 / a.lanes))), dim3(kWarps * 32), 0, st, 1, a, static_cast<T *>(out));
     });
