@@ -352,7 +352,10 @@ __device__ __forceinline__ void write_mx4(const NormArgs &a, const T *tile, cons
             } else {
                 z = Fv<8>::make([&](int j) { return c + j < channels ? to_float(src[j]) : 0.f; });
             }
-            z = ((z + shift) * rstd * scale + beta).map([](float v) { return activate_plain<ACT>(v); });   // as written: see activate_plain
+            // as written: see activate_plain.  The last product and sum are scalar: a packed product and the packed sum behind it
+            // become one fused operation with one rounding, whatever roundings they state.
+            const Fv<8> xh = (z + shift) * rstd;
+            z = Fv<8>::make([&](int j) { return activate_plain<ACT>(__fadd_rn(__fmul_rn(xh.get(j), scale.get(j)), beta.get(j))); });
         }
         float v[8];
 #pragma unroll
