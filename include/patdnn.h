@@ -284,7 +284,7 @@ PATDNN_API int patdnn_maxpool2x2(const void *in, void *out, int32_t N, int32_t C
  * a group norm depends on the input and cannot be).  For x[n][p][c], p one of P pixels, group g = c / (C / G):
  *   mean, var over the P * C/G values of (n, g), rstd = 1 / sqrt(var + eps), xh = (x - mean) * rstd,
  *   y = act(xh * gamma[c] + beta[c])
- * All sums are fp32 and taken in a fixed order (the same call gives the same bits); y and dx are rounded once.  NaN and infinities
+ * Sums are fp32, joined in fp32 or fp64 in a fixed order (the same call gives the same bits); y and dx are rounded once.  NaN and infinities
  * reach exactly the (image, group)s that hold them.
  *   desc       copied; a pixel's C channels are consecutive; pixels and images may be further apart than they are long:
  *              strides in elements, 0 = dense.  y strides also hold for dy, x strides for dx.

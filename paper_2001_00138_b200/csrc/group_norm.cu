@@ -17,7 +17,9 @@
 // Measured: forward 2 x 512 x 512 x 128 bf16 SiLU 75 us (statistics 29 us, 4.6 TB/s; join 3.5; elementwise 39, bound by the special-function
 // unit and instruction issue), floor 41 us; gradient 32 x 56 x 56 x 256 bf16 SiLU 56 us (26 + 4.6 + 27), floor 24 us, bound by issue;
 // resident forward 32 x 56 x 56 x 64 fp16 ReLU 10.8 us, floor 3.9.
-// All sums are fp32 and joined in a fixed order.  Variances are never formed as a difference of two large sums: a thread sums (x - m)
+// All sums are fp32 per thread, joined in fp64 and in a fixed order, so that mean and variance are rounded to fp32 about once: values that
+// are held in 4 bits afterwards jump, and every rounding less is a jump less (100352 x 64: 0.36 values per call differ from
+// a plain fp32 evaluation's, 0.57 with joins in fp32).  Variances are never formed as a difference of two large sums: a thread sums (x - m)
 // and (x - m)^2 around its own running mean m, a few pixels at a time, and partial results are joined by their means.
 #include "ops.hpp"
 
@@ -50,12 +52,13 @@ struct NormArgs {
     int parts;                              // two-pass: slabs that share a group (1: slabs hold whole groups)
     int n0;                                 // two-pass: first image of the run
     float eps, inv_count;
+    double inv_values;                      // the same in fp64
     uint8_t *mx;                            // 4-bit output (resident form)
     int64_t mx_scales;
     int mx_width, mx_col_tiles;
 };
 
-__device__ __forceinline__ float warp_sum(float v) {
+template <typename F> __device__ __forceinline__ F warp_sum(F v) {     // float or double
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
@@ -63,8 +66,9 @@ __device__ __forceinline__ float warp_sum(float v) {
 
 // Running mean and sum of squared deviations of V channels over the pixels a thread visits, up to kMerge at a time:
 // the sums are taken around the running mean (around the first pixel in the first run), so a run of b values loses
-// at most about b rounding errors of the largest deviation.
-constexpr int kMerge = 32;
+// at most about b rounding errors of the largest deviation.  16 rather than 32: the rstd of 1024 groups of 6272 values then differ from the
+// once-rounded ones in 5 % instead of 13 % (squares of 16-bit values often tie, so their errors do not average out), for 0.1 us of 33.
+constexpr int kMerge = 16;
 template <int V>
 struct Moments {
     Fv<V> mean, m2, s1, s2;
@@ -265,10 +269,11 @@ __device__ __forceinline__ void put_moments(const Moments<V> &m, const Place &q,
         }
 }
 
-// Joins the entries of red, `width` per group and row, per group: first the mean over a group's entries, then the squared deviations
-// around it.  Teams of 1 to 32 neighbouring lanes share a group, as many as there are threads for.  grp[g * stride] = (mean, m2).
-template <int V>
-__device__ __forceinline__ void join_groups(const float2 *red, int rows, int channels, int per, int pixels, float2 *grp, int64_t stride = 1) {
+// Joins the entries of red, `width` per group and row, per group: n, mean and squared deviations of each around the first one's mean, in one
+// pass; what the entries bring of their own is summed in fp64, and so is the correction to the joint mean, which cancels.  Teams of 1 to 32
+// neighbouring lanes share a group, as many as there are threads for.  out(group, mean, m2).
+template <int V, typename F>
+__device__ __forceinline__ void join_groups(const float2 *red, int rows, int channels, int per, int pixels, F out) {
     const int joined = joined_channels<V>(per), width = per / joined, pitch = channels / joined;
     const int groups = channels / per;
     int team = 32;
@@ -276,30 +281,30 @@ __device__ __forceinline__ void join_groups(const float2 *red, int rows, int cha
     const int member = threadIdx.x & (team - 1);
     const int base = pixels / rows, extra = pixels - base * rows;      // row r visited base pixels, or one more
     const int used = min(rows, pixels);
-    const float inv_total = 1.f / (static_cast<float>(pixels) * static_cast<float>(width)), many = static_cast<float>(joined);
+    const float many = static_cast<float>(joined), total = static_cast<float>(pixels) * static_cast<float>(per);
     for (int g0 = 0; g0 < groups; g0 += kThreads / team) {             // (the same for all threads)
         const int g = g0 + threadIdx.x / team;
         const float2 *from = red + g * width;
-        float s = 0.f, q = 0.f;
-        if (g < groups)
-            for (int r = member; r < used; r += team) {
-                float t = 0.f;
-                for (int c = 0; c < width; ++c) t += from[r * pitch + c].x;
-                s = fmaf(static_cast<float>(base + (r < extra)), t, s);
-            }
-        for (int o = team >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        const float mean = s * inv_total;
-        if (g < groups)
+        float s = 0.f, around = 0.f;
+        double q = 0.;
+        if (g < groups) {
+            around = from[0].x;
             for (int r = member; r < used; r += team) {
                 const float n = static_cast<float>(base + (r < extra)) * many;
                 for (int c = 0; c < width; ++c) {
                     const float2 e = from[r * pitch + c];
-                    const float d = e.x - mean;
+                    const float d = e.x - around;
+                    s = fmaf(n, d, s);
                     q += fmaf(n * d, d, e.y);
                 }
             }
-        for (int o = team >> 1; o > 0; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
-        if (member == 0 && g < groups) grp[g * stride] = make_float2(mean, q);
+        }
+        for (int o = team >> 1; o > 0; o >>= 1) {
+            s += __shfl_xor_sync(0xffffffffu, s, o);
+            q += __shfl_xor_sync(0xffffffffu, q, o);
+        }
+        const float shift = s / total;
+        if (member == 0 && g < groups) out(g, static_cast<double>(around) + shift, ::fma(-static_cast<double>(s), static_cast<double>(shift), q));
     }
 }
 
@@ -398,8 +403,13 @@ __device__ __forceinline__ void write_norm(const NormArgs &a, const T *tile, con
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
+// (mean, rstd) from the mean and the sum of squared deviations
+__device__ __forceinline__ float2 statistics(const NormArgs &a, double mean, double m2) {
+    return make_float2(static_cast<float>(mean), rsqrtf(static_cast<float>(m2 * a.inv_values) + a.eps));
+}
+
 // ---- resident form ----------------------------------------------------------------------------------------------------
-// Shared memory: [chunk][slab] elements of x, then [rows][slab] float2, then [groups of the slab] float2 twice, then gamma and beta.
+// Shared memory: [chunk][slab] elements of x, then [rows][slab] float2, then [groups of the slab] double2 and float2, then gamma and beta.
 template <typename T, int V, int ACT, bool MX>
 __global__ void __launch_bounds__(kThreads, 3) norm_resident_kernel(NormArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
@@ -413,8 +423,8 @@ __global__ void __launch_bounds__(kThreads, 3) norm_resident_kernel(NormArgs a) 
     const Place q = place_of<V>(channels);
     T *tile = reinterpret_cast<T *>(smem);
     float2 *red = reinterpret_cast<float2 *>(smem + (a.chunk * a.slab * sizeof(T) + 15) / 16 * 16);
-    float2 *grp = red + kThreads * V;
-    float2 *fin = grp + a.slab / a.per;
+    double2 *grp = reinterpret_cast<double2 *>(red + kThreads * V);    // this CTA's (mean, squared deviations) per group
+    float2 *fin = reinterpret_cast<float2 *>(grp + a.slab / a.per);    // the image's (mean, rstd)
     float *gamma = reinterpret_cast<float *>(fin + a.slab / a.per), *beta_of = gamma + a.slab;
     const int groups = channels / a.per;
     pdl_wait();
@@ -431,31 +441,29 @@ __global__ void __launch_bounds__(kThreads, 3) norm_resident_kernel(NormArgs a) 
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    if (pixels > 0) join_groups<V>(red, q.rows, channels, a.per, pixels, grp);
+    if (pixels > 0) join_groups<V>(red, q.rows, channels, a.per, pixels, [&](int g, double mean, double m2) { grp[g] = make_double2(mean, m2); });
     cg::cluster_group cluster = cg::this_cluster();
     if (a.cluster > 1) cluster.sync(); else __syncthreads();
     for (int g = threadIdx.x; g < groups; g += kThreads) {
-        float2 e = grp[g];
+        double2 e = grp[g];
         if (a.cluster > 1) {
-            float s = 0.f, sq = 0.f;
-            float2 all[8];
-            float cnt[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                cnt[r] = r < a.cluster ? static_cast<float>(max(int64_t(0), min(a.P - r * a.chunk, a.chunk))) : 0.f;
-                all[r] = cnt[r] > 0.f ? cluster.map_shared_rank(grp, r)[g] : make_float2(0.f, 0.f);
-                s = fmaf(cnt[r], all[r].x, s);
+            // around the first CTA's mean; in fp64 the square of the sum takes nothing from the sum of squares that matters
+            const double around = cluster.map_shared_rank(grp, 0)[g].x;
+            double s = 0., sq = 0., m2 = 0.;
+#pragma unroll 4
+            for (int r = 0; r < a.cluster; ++r) {
+                const double n = static_cast<double>(a.per) * static_cast<int>(max(int64_t(0), min(a.P - r * a.chunk, a.chunk)));
+                if (n == 0.) break;                    // (nor do the CTAs behind it have pixels)
+                const double2 o = cluster.map_shared_rank(grp, r)[g];
+                const double d = o.x - around;
+                s = ::fma(n, d, s);
+                sq = ::fma(n * d, d, sq);
+                m2 += o.y;
             }
-            const float mean = s / static_cast<float>(a.P);
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const float d = all[r].x - mean;
-                sq += fmaf(cnt[r] * static_cast<float>(a.per) * d, cnt[r] > 0.f ? d : 0.f, all[r].y);
-            }
-            e = make_float2(mean, sq);
+            const double shift = s * a.inv_values;
+            e = make_double2(around + shift, m2 + ::fma(-s, shift, sq));
         }
-        const float rstd = rsqrtf(e.y * a.inv_count + a.eps);
-        fin[g] = make_float2(e.x, rstd);
+        fin[g] = statistics(a, e.x, e.y);
         if (a.stats_out && rank == 0) reinterpret_cast<float2 *>(a.stats_out)[static_cast<int64_t>(n) * a.G + c0 / a.per + g] = fin[g];
     }
     if (a.cluster > 1) cluster_arrive();               // the other CTAs' grp have been read
@@ -696,15 +704,21 @@ __device__ __forceinline__ Span span_of(const NormArgs &a, int slab) {
     return s;
 }
 
-__device__ __forceinline__ float block_sum(float v, float *scratch) {
-    v = warp_sum(v);
+// Sums of two values over the CTA.
+template <typename F> __device__ __forceinline__ void block_sums(F &a, F &b, F (*scratch)[2]) {
+    a = warp_sum(a);
+    b = warp_sum(b);
+    if ((threadIdx.x & 31) == 0) {
+        scratch[threadIdx.x >> 5][0] = a;
+        scratch[threadIdx.x >> 5][1] = b;
+    }
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-    __syncthreads();
-    float s = 0.f;
+    a = b = 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) s += scratch[w];
-    return s;
+    for (int w = 0; w < kThreads / 32; ++w) {
+        a += scratch[w][0];
+        b += scratch[w][1];
+    }
 }
 
 // blockIdx = (chunk, slab, image of the run); ws [image of the run][cell][chunk] (mean, m2), a cell being a group or a part of one.
@@ -731,33 +745,32 @@ __global__ void __launch_bounds__(kThreads, 3) norm_moments_kernel(NormArgs a) {
     if (q.on) put_moments<V>(m, q, s.channels, a.parts > 1 ? s.channels : a.per, red);
     __syncthreads();
     const int cell = a.parts > 1 ? blockIdx.y : s.c0 / a.per;
-    join_groups<V>(red, q.rows, s.channels, a.parts > 1 ? s.channels : a.per, pixels,
-                reinterpret_cast<float2 *>(a.ws) + (static_cast<int64_t>(n) * cells + cell) * a.chunks + blockIdx.x, a.chunks);
+    float2 *to = reinterpret_cast<float2 *>(a.ws) + (static_cast<int64_t>(n) * cells + cell) * a.chunks + blockIdx.x;
+    join_groups<V>(red, q.rows, s.channels, a.parts > 1 ? s.channels : a.per, pixels, [&](int g, double mean, double m2) {
+        to[static_cast<int64_t>(g) * a.chunks] = make_float2(static_cast<float>(mean), static_cast<float>(m2));
+    });
 }
 
-// One CTA per (group, image of the run): joins the chunks' moments, first their mean, then the squared deviations around it.
+// One CTA per (group, image of the run): joins the chunks' moments around the first one's mean, in fp64.
 __global__ void __launch_bounds__(kThreads) norm_join_kernel(NormArgs a) {
-    __shared__ float scratch[kThreads / 32];
+    __shared__ double scratch[kThreads / 32][2];
     pdl_trigger();
     pdl_wait();
     const int g = blockIdx.x, n = blockIdx.y, items = a.chunks * a.parts;
     const float2 *w = reinterpret_cast<const float2 *>(a.ws) + (static_cast<int64_t>(n) * a.G + g) * items;
-    auto values = [&](int i) {                         // how many values entry i stands for
-        const int part = i / a.chunks, k = i - part * a.chunks;
-        const int64_t pixels = min(a.chunk, a.P - k * a.chunk);
-        return static_cast<float>(pixels) * static_cast<float>(a.parts > 1 ? min(a.slab, a.per - part * a.slab) : a.per);
-    };
-    float s = 0.f, sq = 0.f;
-    for (int i = threadIdx.x; i < items; i += kThreads) s = fmaf(values(i), w[i].x, s);
-    const float mean = block_sum(s, scratch) * a.inv_count;
+    const float around = w[0].x;
+    double s = 0., q = 0.;
     for (int i = threadIdx.x; i < items; i += kThreads) {
+        const int part = i / a.chunks, k = i - part * a.chunks;
+        const double values = static_cast<double>(min(a.chunk, a.P - k * a.chunk)) * (a.parts > 1 ? min(a.slab, a.per - part * a.slab) : a.per);
         const float2 e = w[i];
-        const float d = e.x - mean;
-        sq += fmaf(values(i) * d, d, e.y);
+        const double d = e.x - around;
+        s = ::fma(values, d, s);
+        q += ::fma(values * d, d, static_cast<double>(e.y));
     }
-    sq = block_sum(sq, scratch);
-    if (threadIdx.x == 0)
-        reinterpret_cast<float2 *>(a.stats_out)[static_cast<int64_t>(a.n0 + n) * a.G + g] = make_float2(mean, rsqrtf(sq * a.inv_count + a.eps));
+    block_sums(s, q, scratch);
+    const double shift = s * a.inv_values;
+    if (threadIdx.x == 0) reinterpret_cast<float2 *>(a.stats_out)[static_cast<int64_t>(a.n0 + n) * a.G + g] = statistics(a, around + shift, ::fma(-s, shift, q));
 }
 
 // Each CTA takes its pixels in the opposite order of the pass before: what that one read last is still in L2.
@@ -838,7 +851,7 @@ __global__ void __launch_bounds__(kThreads, 3) norm_grad_sums_kernel(NormArgs a)
 // One CTA per (group, image of the run): sums the chunks, writes (rstd s1, rstd^2 s2) of the group behind the partial sums and the
 // image's (A, B) per channel into chunk 0's place.
 __global__ void __launch_bounds__(kThreads) norm_grad_join_kernel(NormArgs a) {
-    __shared__ float scratch[kThreads / 32];
+    __shared__ float scratch[kThreads / 32][2];
     pdl_trigger();
     pdl_wait();
     const int g = blockIdx.x, n = a.n0 + blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -858,8 +871,8 @@ __global__ void __launch_bounds__(kThreads) norm_grad_join_kernel(NormArgs a) {
         s1 = fmaf(gm, sa, s1);
         s2 = fmaf(gm, sb, s2);
     }
-    s1 = block_sum(lane == 0 ? s1 : 0.f, scratch);
-    s2 = block_sum(lane == 0 ? s2 : 0.f, scratch);
+    if (lane) s1 = s2 = 0.f;
+    block_sums(s1, s2, scratch);
     if (threadIdx.x == 0) {
         const int64_t at = static_cast<int64_t>(n) * a.G + g;
         const float rstd = reinterpret_cast<const float2 *>(a.stats_in)[at].y;
@@ -937,7 +950,7 @@ __global__ void __launch_bounds__(kThreads, 3) norm_grad_apply_kernel(NormArgs a
 int resident_smem(const NormShape &s, int width, int tensors, int slab, int64_t chunk) {
     const int64_t tile = (chunk * slab * elem_bytes(s.dtype) + 15) / 16 * 16;
     const int64_t groups = slab / (s.C / s.G);
-    const int64_t small = 2 * groups + slab + (tensors == 1 ? 0 : slab + std::max(slab, kThreads));   // float2 (gamma and beta: one per channel)
+    const int64_t small = (tensors == 1 ? 3 * groups : 2 * groups + slab + std::max(slab, kThreads)) + slab;   // float2 (gamma and beta: one per channel)
     const int64_t total = tensors * tile + (static_cast<int64_t>(kThreads) * width + small) * 8;
     return total > (int64_t(1) << 30) ? (1 << 30) : static_cast<int>(total);
 }
@@ -1050,7 +1063,8 @@ NormArgs args_of(const NormHandle &h, const NormPlan &p) {
     a.P = s.P; a.chunk = p.chunk; a.N = s.N; a.C = s.C; a.G = s.G; a.per = s.C / s.G;
     a.slab = p.slab; a.slabs = p.slabs; a.cluster = p.cluster; a.chunks = p.chunks; a.parts = p.parts; a.act = s.act;
     a.eps = s.eps;
-    a.inv_count = static_cast<float>(1.0 / (static_cast<double>(s.P) * a.per));
+    a.inv_values = 1.0 / (static_cast<double>(s.P) * a.per);
+    a.inv_count = static_cast<float>(a.inv_values);
     return a;
 }
 

@@ -61,3 +61,31 @@ def test_the_steps_are_rounded_one_by_one(N, P, C, G, act, slack, dtype):
     want = R.quantise(R.act(z.reshape(rows, C).astype(np.float64), act))
     off = got != want
     assert not off.any(), f"{int(off.sum())} of {off.size} values are not the stated ones, first at {np.argwhere(off)[:4].tolist()}"
+
+
+@pytest.mark.parametrize("N, P, C, G, dtype", [(32, 3136, 64, 32, "bf16"), (64, 196, 512, 32, "f32"), (8, 60000, 64, 32, "bf16"), (16, 20011, 48, 16, "f32")])
+def test_statistics_are_rounded_about_once(N, P, C, G, dtype):
+    """mean and rstd equal fl(mean) and rsqrt(fl(fl(variance) + eps)) in at least 7 groups of 8, and are a step of fp32 away in the others.
+
+    A thread's own fp32 sums are off by a few 2^-25 of the values' spread s; over the threads of a group that leaves some 2^-25 s / 8, joined
+    without further rounding.  With means of about 2 s, whose steps are 2^-22 s, and variances whose steps are 2^-23 of them, the rounding then
+    differs in about one group of 20."""
+    import torch
+    from paper_2001_00138_b200 import binding as B
+    tt, dt = {"f32": (torch.float32, B.F32), "bf16": (torch.bfloat16, B.BF16)}[dtype]
+    g = torch.Generator(device="cuda").manual_seed(P)
+    x = (torch.randn(N, P, C, generator=g, device="cuda") + 2.5).to(tt)
+    one, zero = torch.ones(C, device="cuda"), torch.zeros(C, device="cuda")
+    st = torch.cuda.current_stream().cuda_stream
+    var, mean = torch.var_mean(x.double().reshape(N, P, G, -1), dim=(1, 3), correction=0)
+    rstd = torch.rsqrt(var.float() + 1e-5)
+    h = B.GroupNorm(N, P, C, G, dtype=dt)
+    y, mx = torch.empty_like(x), torch.empty(B.mx4_bytes(N * P, C), dtype=torch.uint8, device="cuda")
+    for call in (lambda s: h.run(x, one, zero, y, s, st), lambda s: h.run_mx4(x, one, zero, mx, s, st)):
+        stats = torch.empty(N, G, 2, device="cuda")
+        call(stats)
+        torch.cuda.synchronize()
+        for got, want, what in ((stats[..., 0], mean.float(), "mean"), (stats[..., 1], rstd, "rstd")):
+            step = (got.view(torch.int32) if got.is_contiguous() else got.contiguous().view(torch.int32)) - want.contiguous().view(torch.int32)
+            assert step.abs().max() <= 1, (what, int(step.abs().max()))
+            assert (step != 0).float().mean() <= 1 / 8, (what, (step != 0).float().mean().item())
