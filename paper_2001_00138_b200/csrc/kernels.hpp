@@ -16,7 +16,9 @@ namespace patdnn {
 // Every kernel of the library is launched with the programmatic-stream-serialization attribute: its CTAs may become
 // resident while the previous kernel of the stream is still draining, run their set-up (barriers, TMEM allocation,
 // bias slice), and block in pdl_wait() until the previous kernel has completed and its writes are visible.  No global
-// data that an earlier kernel may produce is touched before pdl_wait().  PATDNN_PDL=0 turns the attribute off.
+// data that an earlier kernel may produce is touched before pdl_wait().  PATDNN_DEBUG=pdl=0 turns the attribute off.
+// A kernel that allocates tensor memory calls pdl_trigger() behind the barrier that follows the allocation: its successor's CTAs hold
+// columns of their own while they wait for it, so they may arrive only when every CTA of it holds its columns.
 #ifdef __CUDACC__
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

@@ -89,7 +89,6 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 1];
     __shared__ uint32_t tmem_slot;
-    pdl_trigger();
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int rank = blockIdx.x % p.splits, tile = blockIdx.x / p.splits;
     const int ft = tile % p.f_tiles, nt = tile / p.f_tiles;
@@ -118,6 +117,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    pdl_trigger();                                                       // not before the allocation: see kernels.hpp
     const uint32_t tmem = tmem_slot;
 
     const int t0 = rank * p.tiles_per_split, t1 = min(p.col_tiles, t0 + p.tiles_per_split);
@@ -366,7 +366,6 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 2];
     __shared__ uint32_t tmem_slot;
-    pdl_trigger();
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const WaitCtx ctx{p.status, p.spin_limit ? p.spin_limit : kSpinLimit};
     const uint32_t smem = (smem_u32(smem_raw) + 1023) & ~1023u;
@@ -395,6 +394,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    pdl_trigger();                                                       // not before the allocation: see kernels.hpp
     const uint32_t tmem = tmem_slot;
     const int64_t tiles = static_cast<int64_t>(p.f_tiles) * p.n_tiles;   // f_tiles of tile_n outputs, n_tiles of 128 rows
     const int w_tiles = (p.F + 127) / 128;

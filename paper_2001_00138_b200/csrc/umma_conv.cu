@@ -403,7 +403,6 @@ conv_umma_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     __shared__ float s_bias[BN];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    pdl_trigger();
     const int stages = p.stages;
     const uint32_t bar_full = smem_u32(&bars[0]), bar_empty = smem_u32(&bars[8]), bar_acc = smem_u32(&bars[16]);
     const WaitCtx status{p.status, p.spin_limit ? p.spin_limit : kSpinLimit};
@@ -446,6 +445,7 @@ conv_umma_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    pdl_trigger();                                              // not before the allocation: see kernels.hpp
     const uint32_t tmem_base = tmem_slot;
     // The weights do not depend on the previous kernel: the producer thread fetches the weight tiles of the first ring
     // slots before it waits for that kernel, so they travel (from HBM, when the L2 is cold) while it drains.
@@ -653,7 +653,6 @@ conv_umma_halo_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_con
     const int KB = p.KB;
     const int nshift = p.taps == 9 ? 3 : 1;                     // 3 horizontal shifts x 3 vertical taps, or one gathered tap
 
-    pdl_trigger();
     if (threadIdx.x == 0) {
         for (int s = 0; s < 8; ++s) {
             mbar_init(bar_fa + 8 * s, GATHER ? kGatherThreads / 32 : 1); mbar_init(bar_ea + 8 * s, ISSUERS);
@@ -670,6 +669,7 @@ conv_umma_halo_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_con
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    pdl_trigger();                                              // not before the allocation: see kernels.hpp
     const uint32_t tmem_base = tmem_slot;
 
     auto decode = [&](int t, int &ft, int &x0, int &y0, int &n) {
@@ -992,7 +992,6 @@ conv_umma_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_con
     const int KB = p.KB;
     const int n_clusters = gridDim.x / 2, cluster_id = blockIdx.x / 2;
 
-    pdl_trigger();
     if (threadIdx.x == 0) {
         for (int s = 0; s < 8; ++s) {
             mbar_init(bar_fa + 8 * s, 2); mbar_init(bar_ea + 8 * s, 1);
@@ -1010,6 +1009,7 @@ conv_umma_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_con
     __syncthreads();
     cluster_sync_all();                                          // both CTAs' barriers exist before anyone signals them
     tc_fence_after();
+    pdl_trigger();                                              // not before the allocation: see kernels.hpp
     const uint32_t tmem_base = tmem_slot;
     pdl_wait();
 
