@@ -363,6 +363,23 @@ PATDNN_API int patdnn_linear_encode(const void *weights, int64_t ldw, const patd
 PATDNN_API int patdnn_linear_run(patdnn_linear h, const void *x, int64_t rows, int64_t ldx, void *y, int64_t ldy, void *stream);
 PATDNN_API int patdnn_linear_run_mx4(patdnn_linear h, const void *mx, int64_t rows, void *y, int64_t ldy, void *stream);
 PATDNN_API int patdnn_linear_check(patdnn_linear h);
+
+/* How the product of a linear layer is launched (inspection, like patdnn_plan; touches no device).  from_4_bit_rows: 0 for patdnn_linear_run,
+ * else patdnn_linear_run_mx4.  Errors: E_NULL, E_SHAPE. */
+typedef struct {
+    int32_t persistent;         /* 1: the kernel for many rows, one CTA per SM; 0: one tile per CTA or cluster */
+    int32_t quantises;          /* 1: the product's kernel quantises the rows itself */
+    int32_t tile_rows, tile_outputs;
+    int32_t column_tiles;       /* tiles of up to 256 inputs */
+    int32_t splits;             /* CTAs of a cluster that share a tile's column tiles */
+    int32_t stages;             /* column tiles in the ring of copies */
+    int32_t piece_bytes;        /* persistent: bytes of a row of y that are stored at a time */
+    int32_t grid;               /* CTAs */
+    int32_t smem_bytes;         /* dynamic shared memory of a CTA */
+    int32_t tensor_columns;     /* columns of tensor memory that a CTA allocates */
+    int32_t reserved;
+} patdnn_linear_plan_info;
+PATDNN_API int patdnn_linear_plan(int32_t F, int32_t K, int64_t rows, int32_t from_4_bit_rows, patdnn_linear_plan_info *info);
 PATDNN_API int patdnn_linear_free(patdnn_linear h);
 
 /* Number of this library's kernels launched by the process since the last reset (addition, for reports). */

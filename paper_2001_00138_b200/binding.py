@@ -30,7 +30,7 @@ EXPORTED_SYMBOLS = (
     "patdnn_last_cuda_error", "patdnn_version", "patdnn_debug_wait", "patdnn_stack_run_timed", "patdnn_stack_generated",
     "patdnn_norm_create", "patdnn_norm_run", "patdnn_norm_run_mx4", "patdnn_norm_grad", "patdnn_norm_free",
     "patdnn_mx4_bytes", "patdnn_mx4_quantize", "patdnn_mx4_dequantize",
-    "patdnn_linear_encode", "patdnn_linear_run", "patdnn_linear_run_mx4", "patdnn_linear_check", "patdnn_linear_free",
+    "patdnn_linear_encode", "patdnn_linear_run", "patdnn_linear_run_mx4", "patdnn_linear_check", "patdnn_linear_plan", "patdnn_linear_free",
 )
 
 
@@ -72,6 +72,11 @@ class _NormDesc(ctypes.Structure):
 class _LinearDesc(ctypes.Structure):
     _fields_ = [("F", ctypes.c_int32), ("K", ctypes.c_int32), ("max_rows", ctypes.c_int64), ("bias", ctypes.c_void_p),
                 ("act", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class _LinearPlan(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("persistent", "quantises", "tile_rows", "tile_outputs", "column_tiles", "splits", "stages",
+                                              "piece_bytes", "grid", "smem_bytes", "tensor_columns", "reserved")]
 
 
 _lib = None
@@ -121,6 +126,7 @@ def load() -> ctypes.CDLL:
     lib.patdnn_linear_run.argtypes = [vp, vp, i64, i64, vp, i64, vp]
     lib.patdnn_linear_run_mx4.argtypes = [vp, vp, i64, vp, i64, vp]
     lib.patdnn_linear_check.argtypes = [vp]
+    lib.patdnn_linear_plan.argtypes = [i32, i32, i64, i32, ctypes.POINTER(_LinearPlan)]
     lib.patdnn_linear_free.argtypes = [vp]
     lib.patdnn_launch_count.restype = ctypes.c_int64
     lib.patdnn_reset_launch_count.restype = None
@@ -419,6 +425,13 @@ class Linear:
             self.free()
         except Exception:
             pass
+
+
+def linear_plan(F: int, K: int, rows: int, *, from_4_bit_rows: bool = False) -> dict:
+    """patdnn_linear_plan: how ``Linear.run`` (or ``run_mx4``) launches its product; needs no device."""
+    info = _LinearPlan()
+    _check(load().patdnn_linear_plan(F, K, rows, int(from_4_bit_rows), ctypes.byref(info)), "patdnn_linear_plan")
+    return {n: int(getattr(info, n)) for n, _ in info._fields_ if n != "reserved"}
 
 
 def maxpool2x2(x, out, N: int, C: int, H: int, W: int, dtype: int = F32, stream: int = 0) -> None:

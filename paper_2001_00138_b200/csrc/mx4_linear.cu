@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
     const int atoms = p.width > 128 ? 2 : 1;                             // scale atoms (128 columns each) per column tile
     const uint32_t a_codes = 128 * row_bytes, b_codes = p.tile_n * row_bytes, sf_bytes = 512 * atoms;
     const uint32_t stage_bytes = (a_codes + b_codes + 2 * sf_bytes + 1023) & ~1023u;
-    const int tmem_cols = 256, sf_base = 128, sf_cols = 16;              // accumulator of up to 128 columns, scales per stage
+    const int tmem_cols = p.tensor_columns, sf_base = p.tile_n, sf_cols = 16;    // behind the accumulator: scales per stage
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
     const int wide = p.tile_n / 128;                                     // row tiles of w per tile: 1 or 2
     const uint32_t codes = 128 * row_bytes, sf_bytes = 512 * atoms;      // of one row tile
     const uint32_t stage_bytes = ((1 + wide) * (codes + sf_bytes) + 1023) & ~1023u;
-    const int sf_base = p.tile_n, sf_cols = 8 + 8 * wide;
+    const int tmem_cols = p.tensor_columns, sf_base = p.tile_n, sf_cols = 8 + 8 * wide;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(tmem_cols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     tc_fence_before();
@@ -549,7 +549,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols));
 }
 
 template <typename F> cudaError_t by_output(int dtype, int act, F f) {
@@ -560,6 +560,7 @@ template <typename F> cudaError_t by_output(int dtype, int act, F f) {
     });
 }
 constexpr int kLinearSmem = 226 * 1024;
+constexpr int kSmemPerSm = 228 * 1024;
 
 }  // namespace
 
@@ -578,30 +579,41 @@ cudaError_t prepare_mx4_linear() {
     return e;
 }
 
-cudaError_t launch_mx4_linear(Mx4Params p, cudaStream_t st, int *launches) {
+// Columns of tensor memory come in powers of two, at least 32.
+static int allocation_of(int columns) {
+    int n = 32;
+    while (n < columns) n *= 2;
+    return n;
+}
+
+Mx4Launch plan_mx4_linear(Mx4Params &p) {
+    const Mx4Shape shape = mx4_shape(p.F, p.K);
+    p.width = shape.width;
+    p.col_tiles = static_cast<int>(shape.col_tiles);
+    p.ksteps = static_cast<int>(ceil_div(p.K, 64));
     const int row_bytes = p.width / 2, atoms = p.width > 128 ? 2 : 1;
-    *launches = 1;
+    Mx4Launch l{};
     // Many rows: as soon as tiles of 128 x 256 (or 128 x 128) fill the SMs, the persistent kernel.
     const int64_t row_tiles = ceil_div(p.rows, 128);
     const int tile_f = p.F > 128 && row_tiles * ceil_div(p.F, 256) >= sm_count() ? 256 : 128;
     if (!p.x_raw && p.rows > 64 && row_tiles * ceil_div(p.F, tile_f) >= sm_count()) {
+        l.persistent = true;
         p.tile_n = tile_f;
         p.f_tiles = static_cast<int>(ceil_div(p.F, tile_f));
         p.n_tiles = static_cast<int>(row_tiles);
         p.splits = 1;
         const int wide = tile_f / 128;
         const int stage = ((1 + wide) * (128 * row_bytes + 512 * atoms) + 1023) / 1024 * 1024;
-        const int piece = p.col_tiles <= 3 ? 64 : 32;
-        const int out = kEpilogueWarps * stage_out(piece) + 1024;
+        l.piece = p.col_tiles <= 3 ? 64 : 32;
+        const int out = kEpilogueWarps * stage_out(l.piece) + 1024;
         p.stages = std::min(kMaxStages, (kLinearSmem - out) / stage);
+        p.tensor_columns = 512;                        // (one CTA per SM: its threads take most of the registers)
         const int64_t tiles = static_cast<int64_t>(p.f_tiles) * p.n_tiles;
-        const unsigned grid = static_cast<unsigned>(std::min<int64_t>(tiles, sm_count()));
-        p.step_n = static_cast<int>(grid / p.f_tiles);
-        p.step_f = static_cast<int>(grid % p.f_tiles);
-        return by_output(p.dtype, p.act, [&](auto t, auto a) {
-            const auto kernel = piece == 64 ? mx4_rows_kernel<decltype(t), a.value, 64> : mx4_rows_kernel<decltype(t), a.value, 32>;
-            return launch_pdl(kernel, dim3(grid), dim3(kRowsThreads), p.stages * stage + out, st, 1, p);
-        });
+        l.grid = static_cast<unsigned>(std::min<int64_t>(tiles, sm_count()));
+        p.step_n = static_cast<int>(l.grid / p.f_tiles);
+        p.step_f = static_cast<int>(l.grid % p.f_tiles);
+        l.smem = p.stages * stage + out;
+        return l;
     }
     p.f_tiles = static_cast<int>(ceil_div(p.F, 128));
     // (row tiles start at multiples of 128: the scales of a tile start at a column of tensor memory that is a multiple of four)
@@ -618,10 +630,27 @@ cudaError_t launch_mx4_linear(Mx4Params p, cudaStream_t st, int *launches) {
     const int stage = (128 * row_bytes + p.tile_n * row_bytes + 512 * atoms * 2 + 1023) / 1024 * 1024;
     p.stages = std::max(1, std::min({kMaxStages, p.tiles_per_split, 200 * 1024 / stage}));
     const int slots = p.splits > 1 ? static_cast<int>(ceil_div(p.tile_n, p.splits)) * p.splits * 512 : 0;
-    const int smem = std::max(p.stages * stage, slots) + 1024;
+    p.tensor_columns = allocation_of(p.tile_n + 16 * p.stages);
+    // The CTAs of a cluster wait for one another while they hold their columns, so none may find an SM's tensor memory full of CTAs that
+    // wait likewise.  Every CTA takes shared memory in proportion to its columns (of 228 KB, 1 KB of which the system keeps per CTA, and of
+    // 512 columns): where shared memory fits, tensor memory does.  The clusters of the convolutions take more than that share.
+    const int share = kSmemPerSm / 512 * p.tensor_columns - 1024;
+    l.smem = std::max({p.stages * stage + 1024, slots + 1024, share});
+    l.grid = static_cast<unsigned>(tiles * p.splits);
+    return l;
+}
+
+cudaError_t launch_mx4_linear(Mx4Params p, cudaStream_t st, int *launches) {
+    const Mx4Launch l = plan_mx4_linear(p);
+    *launches = 1;
+    if (l.persistent)
+        return by_output(p.dtype, p.act, [&](auto t, auto a) {
+            const auto kernel = l.piece == 64 ? mx4_rows_kernel<decltype(t), a.value, 64> : mx4_rows_kernel<decltype(t), a.value, 32>;
+            return launch_pdl(kernel, dim3(l.grid), dim3(kRowsThreads), l.smem, st, 1, p);
+        });
     const auto kernel = !p.x_raw ? mx4_linear_kernel<void> : p.dtype == PATDNN_F32 ? mx4_linear_kernel<float>
                         : p.dtype == PATDNN_F16 ? mx4_linear_kernel<__half> : mx4_linear_kernel<__nv_bfloat16>;
-    return launch_pdl(kernel, dim3(static_cast<unsigned>(tiles * p.splits)), dim3(kLinThreads), smem, st, p.splits, p);
+    return launch_pdl(kernel, dim3(l.grid), dim3(kLinThreads), l.smem, st, p.splits, p);
 }
 
 }  // namespace patdnn

@@ -98,11 +98,20 @@ struct Mx4Params {
     int tile_n;
     int splits, tiles_per_split;            // cluster split of the column tiles
     int stages;
+    int tensor_columns;                     // of tensor memory that a CTA allocates
     int step_n, step_f;                     // persistent kernel: from a CTA's tile to its next one
     uint32_t spin_limit;
 };
+struct Mx4Launch {                          // how a product is launched
+    bool persistent;                        // the kernel for many rows
+    int piece;                              // persistent: bytes of a row of y that are stored at a time
+    int smem;                               // dynamic shared memory
+    unsigned grid;
+};
 constexpr int kFusedRows = 8;               // rows that the product's kernel quantises itself
 cudaError_t prepare_mx4_linear();                       // opt in to the dynamic shared memory
+// Shapes of p (F, K, rows, x_raw) -> its tiling and the launch; no device is touched.
+Mx4Launch plan_mx4_linear(Mx4Params &p);
 cudaError_t launch_mx4_linear(Mx4Params p, cudaStream_t st, int *launches);
 
 }  // namespace patdnn

@@ -74,15 +74,15 @@ template <typename T> cudaError_t allocate(T **p, size_t count) {
     return e;
 }
 
+bool too_many_tiles(int64_t rows, int64_t F) { return ceil_div(rows, 128) * ceil_div(F, 128) > INT32_MAX / 8; }   // CTAs of one launch
+
 // mx: 4-bit rows, or nullptr with the rows themselves at x
 int product(patdnn_linear h, const void *mx, const void *x, int64_t ldx, int64_t rows, void *y, int64_t ldy, cudaStream_t st) {
-    if (ceil_div(rows, 128) * ceil_div(h->d.F, 128) > INT32_MAX / 8) return PATDNN_E_SHAPE;   // CTAs of one launch
+    if (too_many_tiles(rows, h->d.F)) return PATDNN_E_SHAPE;
     Mx4Params p{};
     p.w = h->w; p.x = static_cast<const uint8_t *>(mx); p.x_raw = x; p.ldx = ldx; p.K = h->d.K; p.bias = h->bias; p.y = y; p.status = h->status;
     p.ldy = ldy; p.rows = rows; p.w_scales = h->shape.scales_at; p.x_scales = mx4_shape(rows, h->d.K).scales_at;
-    p.F = h->d.F; p.width = h->shape.width; p.col_tiles = static_cast<int>(h->shape.col_tiles);
-    p.ksteps = static_cast<int>(ceil_div(h->d.K, 64));
-    p.act = h->d.act; p.dtype = h->d.dtype;
+    p.F = h->d.F; p.act = h->d.act; p.dtype = h->d.dtype;
     int n = 0;
     const cudaError_t e = launch_mx4_linear(p, st, &n);
     return launched(e, n, "4-bit product launch");
@@ -276,6 +276,22 @@ int patdnn_linear_run_mx4(patdnn_linear h, const void *mx, int64_t rows, void *y
     if (!mx || !y) return PATDNN_E_NULL;
     if (const int rc = on_device(h->device)) return rc;
     return product(h, mx, nullptr, 0, rows, y, ldy, static_cast<cudaStream_t>(stream));
+}
+
+int patdnn_linear_plan(int32_t F, int32_t K, int64_t rows, int32_t from_4_bit_rows, patdnn_linear_plan_info *info) {
+    if (!info) return PATDNN_E_NULL;
+    if (F < 1 || F > kMostColumns || !mx_size_ok(F, K) || !mx_size_ok(rows, K) || rows < 1 || too_many_tiles(rows, F)) return PATDNN_E_SHAPE;
+    Mx4Params p{};
+    p.F = F; p.K = K; p.rows = rows;
+    const bool fused = !from_4_bit_rows && rows <= kFusedRows;
+    p.x_raw = fused ? info : nullptr;                  // (not read)
+    const Mx4Launch l = plan_mx4_linear(p);
+    *info = patdnn_linear_plan_info{};
+    info->persistent = l.persistent; info->quantises = fused;
+    info->tile_rows = l.persistent ? 128 : p.tile_n; info->tile_outputs = l.persistent ? p.tile_n : 128;
+    info->column_tiles = p.col_tiles; info->splits = p.splits; info->stages = p.stages;
+    info->piece_bytes = l.piece; info->grid = static_cast<int32_t>(l.grid); info->smem_bytes = l.smem; info->tensor_columns = p.tensor_columns;
+    return PATDNN_OK;
 }
 
 int patdnn_linear_check(patdnn_linear h) {

@@ -1419,7 +1419,8 @@ void plan_dense(int F, int C, int N, int H, int W, int dtype, DensePlan &pl, boo
                 pl.TW = btw; pl.TH = th; pl.TN = 1; pl.tiles_x = tx; pl.tiles_y = ty; pl.tiles_n = N;
                 pl.box_bytes = (th + 2) * btw * 128;
                 pl.na = na; pl.stages = nb;
-                pl.smem_bytes = na * a_stage + nb * b_stage + 1024;
+                // (all of it: a pair holds all of two SMs' tensor memory, see plan_mx4_linear)
+                pl.smem_bytes = std::max(na * a_stage + nb * b_stage + 1024, 222 * 1024);
                 pl.n_tiles = n_pairs;                            // pair tiles
                 pl.grid = 2 * std::min(n_pairs, n_sm / 2);
                 pl.tail_tiles = 0;

@@ -41,3 +41,39 @@ def test_dependents_start_after_the_allocation(name, body):
     barrier = body.index("__syncthreads()", alloc)
     assert all(t > barrier for t in triggers)
     assert "tcgen05.alloc" not in body[alloc + 1:]
+
+
+def linear_sizes():
+    rows = [1, 2, 8, 9, 16, 17, 48, 64, 65, 100, 128, 129, 300, 777, 3000, 20000]
+    return [(f, k, m) for f in (1, 128, 130, 1000, 4096, 40000) for k in (1, 64, 65, 128, 129, 512, 1000, 4096, 25088, 1 << 20) for m in rows]
+
+
+def test_ctas_that_fit_an_sm_find_tensor_memory():
+    """The CTAs of a cluster wait for one another while they hold columns: CTAs of the product that fit an SM by their shared memory (228 KB,
+    1 KB of it kept per CTA) fit by their columns (512), whatever other such CTA is there."""
+    from paper_2001_00138_b200 import binding as B
+    clusters = 0
+    for F, K, rows in linear_sizes():
+        for mx in (False, True):
+            p = B.linear_plan(F, K, rows, from_4_bit_rows=mx)
+            what = (F, K, rows, mx, p)
+            columns = p["tensor_columns"]
+            assert columns in (32, 64, 128, 256, 512), what
+            wide = p["tile_outputs"] // 128
+            used = p["tile_outputs"] + (8 + 8 * wide) * p["stages"] if p["persistent"] else p["tile_rows"] + 16 * p["stages"]
+            assert used <= columns, what
+            assert p["smem_bytes"] <= 226 * 1024, what
+            if p["persistent"]:
+                assert p["splits"] == 1, what              # waits for nothing but earlier grids
+            else:
+                assert (p["smem_bytes"] + 1024) * 512 >= columns * 228 * 1024, what
+            clusters += p["splits"] > 1
+    assert clusters > 100
+
+
+def test_linear_plan_refusals():
+    from paper_2001_00138_b200 import binding as B
+    for args in ((0, 32, 1), (32, 0, 1), (32, 32, 0), (32, 2 ** 21, 1), (2 ** 21, 32, 1), (2 ** 20, 1, 2 ** 31 - 1)):
+        with pytest.raises(B.PatdnnError) as e:
+            B.linear_plan(*args)
+        assert e.value.status == 2
