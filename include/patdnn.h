@@ -396,6 +396,9 @@ PATDNN_API void patdnn_reset_launch_count(void);
  * Errors: E_NULL, E_SHAPE (negative iteration).
  */
 PATDNN_API int patdnn_debug_wait(patdnn_handle h, uint32_t polls, int32_t skip_load_iteration);
+/* The same for a linear layer; the iteration is the column tile in a CTA's own walk.  The rows that a kernel does not finish are unspecified;
+ * patdnn_linear_check reports it, and until it has, later calls on the handle may give up too. */
+PATDNN_API int patdnn_linear_debug_wait(patdnn_linear h, uint32_t polls, int32_t skip_load_iteration);
 
 PATDNN_API const char *patdnn_strerror(int status);
 PATDNN_API const char *patdnn_last_cuda_error(void);   /* text of the last CUDA failure seen by this thread ("" if none) */

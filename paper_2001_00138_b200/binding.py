@@ -30,7 +30,8 @@ EXPORTED_SYMBOLS = (
     "patdnn_last_cuda_error", "patdnn_version", "patdnn_debug_wait", "patdnn_stack_run_timed", "patdnn_stack_generated",
     "patdnn_norm_create", "patdnn_norm_run", "patdnn_norm_run_mx4", "patdnn_norm_grad", "patdnn_norm_free",
     "patdnn_mx4_bytes", "patdnn_mx4_quantize", "patdnn_mx4_dequantize",
-    "patdnn_linear_encode", "patdnn_linear_run", "patdnn_linear_run_mx4", "patdnn_linear_check", "patdnn_linear_plan", "patdnn_linear_free",
+    "patdnn_linear_encode", "patdnn_linear_run", "patdnn_linear_run_mx4", "patdnn_linear_check", "patdnn_linear_plan", "patdnn_linear_debug_wait",
+    "patdnn_linear_free",
 )
 
 
@@ -126,6 +127,7 @@ def load() -> ctypes.CDLL:
     lib.patdnn_linear_run.argtypes = [vp, vp, i64, i64, vp, i64, vp]
     lib.patdnn_linear_run_mx4.argtypes = [vp, vp, i64, vp, i64, vp]
     lib.patdnn_linear_check.argtypes = [vp]
+    lib.patdnn_linear_debug_wait.argtypes = [vp, ctypes.c_uint32, i32]
     lib.patdnn_linear_plan.argtypes = [i32, i32, i64, i32, ctypes.POINTER(_LinearPlan)]
     lib.patdnn_linear_free.argtypes = [vp]
     lib.patdnn_launch_count.restype = ctypes.c_int64
@@ -414,6 +416,11 @@ class Linear:
     def check(self) -> None:
         """patdnn_linear_check: synchronise and raise if a device-side bounded wait expired."""
         _check(load().patdnn_linear_check(self._h), "patdnn_linear_check")
+
+    def debug_wait(self, polls: int, skip_load_iteration: int = 0) -> None:
+        """patdnn_linear_debug_wait: bound of the device-side waits (polls; 0 = default) and the test hook that withholds the
+        copies of one column tile."""
+        _check(load().patdnn_linear_debug_wait(self._h, polls, skip_load_iteration), "patdnn_linear_debug_wait")
 
     def free(self) -> None:
         if self._h:

@@ -132,8 +132,8 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
         const uint8_t *ws = p.w + p.w_scales + (static_cast<int64_t>(ft) * p.col_tiles + t0) * sf_bytes;
         const uint8_t *xc = p.x + (x_tile0 * p.col_tiles + t0) * a_codes;
         const uint8_t *xs = p.x + p.x_scales + (x_tile0 * p.col_tiles + t0) * sf_bytes;
-        auto load_w = [&](uint32_t at, uint32_t bar) {
-            if (leader) {
+        auto load_w = [&](int i, uint32_t at, uint32_t bar) {
+            if (leader && i + 1 != p.test_skip_load) {
                 mbar_expect_tx(bar, bytes);
                 bulk_load(at, wc, a_codes, bar);
                 bulk_load(at + a_codes + b_codes, ws, sf_bytes, bar);
@@ -141,8 +141,8 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
             wc += a_codes;
             ws += sf_bytes;
         };
-        auto load_x = [&](uint32_t at, uint32_t bar) {
-            if (leader && !kFused) {
+        auto load_x = [&](int i, uint32_t at, uint32_t bar) {
+            if (leader && !kFused && i + 1 != p.test_skip_load) {
                 bulk_load(at + a_codes, xc, b_codes, bar);
                 bulk_load(at + a_codes + b_codes + sf_bytes, xs, sf_bytes, bar);
             }
@@ -151,15 +151,15 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
         };
         // the weights do not depend on the previous kernel: fill the ring with them before waiting for it
         const int ahead = min(iters, p.stages);
-        for (int i = 0; i < ahead; ++i) load_w(smem + i * stage_bytes, full + 8 * i);
+        for (int i = 0; i < ahead; ++i) load_w(i, smem + i * stage_bytes, full + 8 * i);
         pdl_wait();
-        for (int i = 0; i < ahead; ++i) load_x(smem + i * stage_bytes, full + 8 * i);
+        for (int i = 0; i < ahead; ++i) load_x(i, smem + i * stage_bytes, full + 8 * i);
         int issued = ahead, slot = 0;
         uint32_t phase = 0;
         for (int i = ahead; i < iters; ++i) {
             if (!warp_wait(empty + 8 * slot, phase, ctx, 101)) break;
-            load_w(smem + slot * stage_bytes, full + 8 * slot);
-            load_x(smem + slot * stage_bytes, full + 8 * slot);
+            load_w(i, smem + slot * stage_bytes, full + 8 * slot);
+            load_x(i, smem + slot * stage_bytes, full + 8 * slot);
             ++issued;
             if (++slot == p.stages) { slot = 0; phase ^= 1; }
         }
@@ -417,7 +417,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
                 if (issued >= p.stages && !warp_wait(empty + 8 * slot, phase, ctx, 111)) { ok = false; break; }
                 const uint32_t at = smem + slot * stage_bytes, bar = full + 8 * slot;
                 const uint32_t sf = at + (1 + wide) * codes;
-                if (leader) {
+                const bool copies = leader && issued + 1 != p.test_skip_load;
+                if (copies) {
                     mbar_expect_tx(bar, bytes);
                     bulk_load(at + codes, wc, codes, bar);
                     bulk_load(sf + sf_bytes, ws, sf_bytes, bar);
@@ -430,7 +431,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
                     pdl_wait();
                     waited = true;
                 }
-                if (leader) {
+                if (copies) {
                     bulk_load(at, xc, codes, bar);
                     bulk_load(sf, xs, sf_bytes, bar);
                 }

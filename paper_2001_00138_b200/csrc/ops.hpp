@@ -100,7 +100,8 @@ struct Mx4Params {
     int stages;
     int tensor_columns;                     // of tensor memory that a CTA allocates
     int step_n, step_f;                     // persistent kernel: from a CTA's tile to its next one
-    uint32_t spin_limit;
+    uint32_t spin_limit;                    // polls of a bounded wait (0 = the default)
+    int test_skip_load;                     // test hook: every CTA leaves out the copies of this (1-based) column tile of its walk (0 = off)
 };
 struct Mx4Launch {                          // how a product is launched
     bool persistent;                        // the kernel for many rows

@@ -33,6 +33,8 @@ struct patdnn_linear_s {
     uint8_t *w = nullptr, *x = nullptr;     // 4-bit weights; buffer for the rows of patdnn_linear_run
     float *bias = nullptr;
     int *status = nullptr;
+    uint32_t spin_limit = 0;                // patdnn_linear_debug_wait
+    int test_skip_load = 0;
     ~patdnn_linear_s() {
         cudaFree(w);
         cudaFree(x);
@@ -82,6 +84,7 @@ int product(patdnn_linear h, const void *mx, const void *x, int64_t ldx, int64_t
     Mx4Params p{};
     p.w = h->w; p.x = static_cast<const uint8_t *>(mx); p.x_raw = x; p.ldx = ldx; p.K = h->d.K; p.bias = h->bias; p.y = y; p.status = h->status;
     p.ldy = ldy; p.rows = rows; p.w_scales = h->shape.scales_at; p.x_scales = mx4_shape(rows, h->d.K).scales_at;
+    p.spin_limit = h->spin_limit; p.test_skip_load = h->test_skip_load;
     p.F = h->d.F; p.act = h->d.act; p.dtype = h->d.dtype;
     int n = 0;
     const cudaError_t e = launch_mx4_linear(p, st, &n);
@@ -303,6 +306,14 @@ int patdnn_linear_check(patdnn_linear h) {
     if (!word) return PATDNN_OK;
     CU(cudaMemset(h->status, 0, sizeof(int)));
     return PATDNN_E_DEVICE_TIMEOUT;
+}
+
+int patdnn_linear_debug_wait(patdnn_linear h, uint32_t polls, int32_t skip_load_iteration) {
+    if (!h) return PATDNN_E_NULL;
+    if (skip_load_iteration < 0) return PATDNN_E_SHAPE;
+    h->spin_limit = polls;
+    h->test_skip_load = skip_load_iteration;
+    return PATDNN_OK;
 }
 
 int patdnn_linear_free(patdnn_linear h) {
