@@ -388,7 +388,7 @@ PATDNN_API void patdnn_reset_launch_count(void);
 
 /*
  * patdnn_debug_wait (addition; test hook of the failure-detection path) -- every device-side wait of the tensor-core
- * kernels is bounded: after `polls` unsuccessful polls of a barrier (0 = the default, about two seconds) a kernel
+ * kernels is bounded: after `polls` unsuccessful polls of a barrier (0 = the default, about eight seconds) a kernel
  * records a status word, lets all its roles fall through to the common exit, frees its tensor memory and returns;
  * patdnn_check then reports PATDNN_E_DEVICE_TIMEOUT and clears the word.  `skip_load_iteration` > 0 makes the
  * producer of the one-tile-per-CTA kernel leave out the loads of that (1-based) iteration of its channel/tap loop, so

@@ -172,6 +172,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
         const uint32_t lower = mx4_instr_desc(p.tile_n, 0), upper = mx4_instr_desc(p.tile_n, 1);
         const uint64_t da0 = operand_desc(smem, row_bytes), db0 = operand_desc(smem + a_codes, row_bytes);
         const uint64_t sa0 = scale_desc(smem + a_codes + b_codes), sb0 = scale_desc(smem + a_codes + b_codes + sf_bytes);
+        pdl_wait();                                                      // the bound of the waits below is for this kernel's copies alone
         for (int i = 0; i < iters; ++i, steps -= p.width / 64) {
             if (!warp_wait(full + 8 * slot, phase, ctx, 103)) break;
             tc_fence_after();
@@ -454,6 +455,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
         const uint64_t s0 = scale_desc(smem + (1 + wide) * codes);
         const uint32_t row_scales = sf_bytes >> 4;                       // descriptor distance between the scales of two row tiles
         bool ok = true;
+        pdl_wait();                                                      // the bound of the waits below is for this kernel's copies alone
         for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x, ++done_tiles) {
             if (done_tiles > 0 && !warp_wait(drained, (done_tiles - 1) & 1, ctx, 113)) break;
             tc_fence_after();

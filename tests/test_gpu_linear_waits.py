@@ -1,7 +1,7 @@
 """Bounded waits of the linear layer's kernels: one that runs out ends the kernel through its normal exit, patdnn_linear_check reports it, and the
 handle works again afterwards.
 
-Nothing here faults, traps or hangs the GPU: the bound is shortened to about a millisecond and the copies of one column tile are left out
+Nothing here faults, traps or hangs the GPU: the bound is shortened to a few milliseconds and the copies of one column tile are left out
 (patdnn_linear_debug_wait), so that the consumers' wait for them runs out.
 """
 import pytest
@@ -44,7 +44,7 @@ def test_a_wait_that_runs_out_is_reported_and_the_handle_keeps_working(form):
     lin.run(x, y, rows, stream=st)
     lin.check()
     assert torch.equal(y, want)
-    lin.debug_wait(1024, skip)                             # about a millisecond per wait
+    lin.debug_wait(1024, skip)                             # about four milliseconds per wait
     lin.run(x, y, rows, stream=st)
     with pytest.raises(B.PatdnnError) as e:
         lin.check()
@@ -55,6 +55,36 @@ def test_a_wait_that_runs_out_is_reported_and_the_handle_keeps_working(form):
     lin.run(x, y, rows, stream=st)
     lin.check()
     assert torch.equal(y, want)
+
+
+def test_the_bound_does_not_count_the_kernel_before():
+    """A kernel may arrive while its predecessor runs.  Its waits are for its own copies, so a predecessor that takes longer than they may does
+    not use them up: here about 0.06 ms (16 polls), behind a product of several times that."""
+    import torch
+    rows, K, F = 256, 2 ** 20, 2304
+    long, lx, _, ly, st = make(F, K, rows)
+    lin, x, w, y, _ = make(128, 64, 3, seed=1)
+    lin40, x40, w40, y40, _ = make(128, 64, 40, seed=2)
+    long.run(lx, ly, rows, stream=st)
+    a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    torch.cuda.synchronize()
+    a.record()
+    long.run(lx, ly, rows, stream=st)
+    b.record()
+    torch.cuda.synchronize()
+    assert a.elapsed_time(b) > 0.4, a.elapsed_time(b)
+    for layer in (lin, lin40):
+        layer.debug_wait(16, 0)
+    from paper_2001_00138_b200 import binding as B
+    mx = torch.empty(B.mx4_bytes(40, 64), dtype=torch.uint8, device="cuda")
+    B.mx4_quantize(x40, mx, 40, 64, dtype=B.BF16, stream=st)
+    for layer, call in ((lin, lambda: lin.run(x, y, 3, stream=st)), (lin40, lambda: lin40.run_mx4(mx, y40, 40, stream=st))):
+        long.run(lx, ly, rows, stream=st)
+        call()
+        layer.check()
+    long.check()
+    assert torch.equal(y, (x.double() @ w.double().t()).bfloat16())
+    assert torch.equal(y40, (x40.double() @ w40.double().t()).bfloat16())
 
 
 def test_debug_wait_refusals():
