@@ -48,7 +48,7 @@ struct NormArgs {
     unsigned *counters;
     int64_t x_pixel, x_image, y_pixel, y_image, P, chunk;
     int N, C, G, per;                       // per = C / G
-    int slab, slabs, cluster, chunks, act;
+    int slab, slabs, cluster, chunks;
     int parts;                              // two-pass: slabs that share a group (1: slabs hold whole groups)
     int n0;                                 // two-pass: first image of the run
     float eps, inv_count;
@@ -959,20 +959,24 @@ constexpr int kSmemMost = 220 * 1024;       // dynamic shared memory of one CTA
 constexpr int64_t kRunBytes = int64_t(160) << 20;   // two-pass: bytes of x (and dy) of the images that are taken together
 
 // Picks the slab and the cluster of the resident form by a time estimate, fitted to measurements of ten shapes with every slab and
-// cluster that fits (7x7 to 56x56 pixels, 64 to 512 channels, the three types, both directions; its choice was the fastest or within
-// 3 % of it): the CTAs of an SM share its HBM rate of 44 bytes per ns; a wave costs half a microsecond, a cluster one more and 0.3 per
-// doubling; slabs narrower than 128 bytes cost 10 %; the gradient, bound by its arithmetic, wants three CTAs per SM.
-// Besides, an SM takes at most kRate elements per us through its arithmetic (a third of that at single-element accesses, a quarter for
-// the gradient; twice the time for 4-bit rows, padded to 32 columns, and six times where SiLU is formed as written): few CTAs on a large image lose against the two passes.
+// cluster that fits (7x7 to 56x56 pixels, 64 to 512 channels, the three types, both directions): the CTAs of an SM share its HBM rate of
+// 44 bytes per ns; a wave costs half a microsecond, a cluster one more and 0.3 per doubling; slabs narrower than 128 bytes cost 10 %; the
+// gradient, bound by its arithmetic, wants three CTAs per SM.
+// Besides, an SM takes at most kRate elements per us through its arithmetic, one half of that time for the statistics and the other for
+// writing: few CTAs on a large image lose against the two passes.  The half of the statistics counts three times at single-element accesses
+// (1.5 times at two elements), that of writing twice for 4-bit rows, padded to 32 columns, and six times where their SiLU is formed as
+// written; in the gradient both count four times.
+// In that sweep its choice of slab and cluster was the fastest or within 3 % of it, for 16- and 32-bit outputs.  As a time it is rough: it gives 10 us for
+// 32 x 56 x 56 x 64 bf16 into 4-bit rows, which take 16, latency of eight warps per SM.
 // `unit`: slabs are a multiple of so many channels (or all of them).
 NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
     NormPlan best;
     const int per = s.C / s.G, e = elem_bytes(s.dtype);
-    const double slow = width == 1 ? 3 : width == 2 ? 1.5 : 1, kRate = 9000;
+    const double slow = width == 1 ? 3 : width == 2 ? 1.5 : 1, kRate = 9000, sms = sm_count();
     // two passes: three launches per run and the bytes once more, or the arithmetic of both passes on all SMs
     const double elements = static_cast<double>(s.N) * s.P * s.C;
     double best_us = 8.0 * ceil_div(static_cast<int64_t>(elements) * e * tensors, kRunBytes) +
-                     std::max(elements * e * (2 * tensors + 1) / 5.2e6, elements * slow * (tensors == 2 ? 2.8 : 1.2) / (148 * kRate));
+                     std::max(elements * e * (2 * tensors + 1) / 5.2e6, elements * slow * (tensors == 2 ? 2.8 : 1.2) / (sms * kRate));
     for (int k = 1; k <= s.G; ++k) {
         if (s.G % k) continue;
         const int64_t slab = static_cast<int64_t>(k) * per;
@@ -985,8 +989,8 @@ NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
             if (smem > kSmemMost || static_cast<int64_t>(s.N) * (s.G / k) * cl > INT32_MAX) continue;
             const int per_sm = std::min(3, (224 * 1024) / (smem + 1024));
             const double ctas = static_cast<double>(s.N) * (s.G / k) * cl;
-            const double here = std::min<double>(per_sm, std::ceil(ctas / 148));           // CTAs of an SM at a time
-            const double waves = std::ceil(ctas / (148 * here));
+            const double here = std::min<double>(per_sm, std::ceil(ctas / sms));           // CTAs of an SM at a time
+            const double waves = std::ceil(ctas / (sms * here));
             const double bytes = static_cast<double>(chunk) * slab * e * (tensors + 1);
             const double wide = unit > 1 ? (slab + 31) / 32 * 32.0 * (s.act == PATDNN_ACT_SILU ? 6 : 2) : static_cast<double>(slab);
             const double work = chunk * (slab * slow + wide) * (tensors == 2 ? 2.0 : 0.5) / kRate;
@@ -1018,7 +1022,7 @@ NormPlan plan_one(const NormShape &s, int width, int tensors, int unit) {
     const int64_t runs = ceil_div(s.N, std::max<int64_t>(1, std::min<int64_t>(s.N, kRunBytes / image)));
     best.run = static_cast<int>(ceil_div(s.N, runs));  // runs of about the same number of images
     // one wave of three CTAs per SM over a run: a last, partly filled wave would cost as much as a full one
-    const int64_t share = 148 * 3 / (static_cast<int64_t>(best.run) * best.slabs);         // CTAs per (image, slab)
+    const int64_t share = static_cast<int64_t>(sm_count()) * 3 / (static_cast<int64_t>(best.run) * best.slabs);         // CTAs per (image, slab)
     const int64_t each = std::max<int64_t>(1, share);
     const int rows = kThreads / (best.slab / width);
     const int64_t chunk = std::max<int64_t>(ceil_div(s.P, each), rows);
@@ -1061,7 +1065,7 @@ NormArgs args_of(const NormHandle &h, const NormPlan &p) {
     a.ws = h.ws; a.counters = h.counters;
     a.x_pixel = s.x_pixel; a.x_image = s.x_image; a.y_pixel = s.y_pixel; a.y_image = s.y_image;
     a.P = s.P; a.chunk = p.chunk; a.N = s.N; a.C = s.C; a.G = s.G; a.per = s.C / s.G;
-    a.slab = p.slab; a.slabs = p.slabs; a.cluster = p.cluster; a.chunks = p.chunks; a.parts = p.parts; a.act = s.act;
+    a.slab = p.slab; a.slabs = p.slabs; a.cluster = p.cluster; a.chunks = p.chunks; a.parts = p.parts;
     a.eps = s.eps;
     a.inv_values = 1.0 / (static_cast<double>(s.P) * a.per);
     a.inv_count = static_cast<float>(a.inv_values);

@@ -35,7 +35,7 @@ struct NormHandle {
     NormShape s{};
     NormPlan fwd[kNormWidths], mx4[kNormWidths], bwd[kNormWidths];
     float *ws = nullptr;                    // partial sums of the two-pass forms and of the gradient
-    unsigned *counters = nullptr;           // [max(N, G)] arrivals per image or channel slab; zero between calls
+    unsigned *counters = nullptr;           // [G] arrivals of images per channel slab (there are at most G); zero between calls
     float *stats = nullptr;                 // [N][G][2] where the caller keeps none
 };
 int norm_width(int dtype, int index);       // elements per access for width index 0 .. 2

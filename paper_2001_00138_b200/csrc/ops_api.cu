@@ -30,7 +30,7 @@ struct patdnn_linear_s {
     patdnn_linear_desc d{};
     Mx4Shape shape{};                       // of the weights
     int device = -1;
-    uint8_t *w = nullptr, *x = nullptr;     // 4-bit weights; buffer for the rows of patdnn_linear_run
+    uint8_t *w = nullptr, *x = nullptr;     // 4-bit weights; buffer for the rows of patdnn_linear_run where max_rows is above kFusedRows
     float *bias = nullptr;
     int *status = nullptr;
     uint32_t spin_limit = 0;                // patdnn_linear_debug_wait
@@ -124,7 +124,7 @@ int patdnn_norm_create(const patdnn_norm_desc *desc, patdnn_norm *out) {
             return rc;
         }
         plan_norm(h->h);
-        const size_t counters = static_cast<size_t>(s.N > s.G ? s.N : s.G);
+        const size_t counters = static_cast<size_t>(s.G);
         cudaError_t e = allocate(&h->h.ws, norm_workspace_floats(h->h));
         if (e == cudaSuccess) e = allocate(&h->h.counters, counters);
         if (e == cudaSuccess) e = cudaMemset(h->h.counters, 0, sizeof(unsigned) * counters);
@@ -234,7 +234,7 @@ int patdnn_linear_encode(const void *weights, int64_t ldw, const patdnn_linear_d
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = allocate(&h->w, static_cast<size_t>(h->shape.bytes));
-    if (e == cudaSuccess && desc->max_rows) e = allocate(&h->x, static_cast<size_t>(mx4_shape(desc->max_rows, desc->K).bytes));
+    if (e == cudaSuccess && desc->max_rows > kFusedRows) e = allocate(&h->x, static_cast<size_t>(mx4_shape(desc->max_rows, desc->K).bytes));
     if (e == cudaSuccess) e = allocate(&h->status, 4);
     if (e == cudaSuccess) e = cudaMemsetAsync(h->status, 0, 16, st);
     if (e == cudaSuccess && desc->bias) {
