@@ -448,17 +448,22 @@ __global__ void __launch_bounds__(kThreads, 3) norm_resident_kernel(NormArgs a) 
         double2 e = grp[g];
         if (a.cluster > 1) {
             // around the first CTA's mean; in fp64 the square of the sum takes nothing from the sum of squares that matters
-            const double around = cluster.map_shared_rank(grp, 0)[g].x;
-            double s = 0., sq = 0., m2 = 0.;
-#pragma unroll 4
-            for (int r = 0; r < a.cluster; ++r) {
-                const double n = static_cast<double>(a.per) * static_cast<int>(max(int64_t(0), min(a.P - r * a.chunk, a.chunk)));
-                if (n == 0.) break;                    // (nor do the CTAs behind it have pixels)
-                const double2 o = cluster.map_shared_rank(grp, r)[g];
-                const double d = o.x - around;
-                s = ::fma(n, d, s);
-                sq = ::fma(n * d, d, sq);
-                m2 += o.y;
+            double around = 0., s = 0., sq = 0., m2 = 0.;
+            for (int first = 0; first < a.cluster; first += 4) {
+                double2 o[4];                          // in flight together
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (first + k < a.cluster) o[k] = cluster.map_shared_rank(grp, first + k)[g];
+                if (first == 0) around = o[0].x;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int64_t count = min(a.P - (first + k) * a.chunk, a.chunk);
+                    if (first + k >= a.cluster || count <= 0) continue;                    // (a CTA without pixels has written none)
+                    const double n = static_cast<double>(a.per) * static_cast<int>(count), d = o[k].x - around;
+                    s = ::fma(n, d, s);
+                    sq = ::fma(n * d, d, sq);
+                    m2 += o[k].y;
+                }
             }
             const double shift = s * a.inv_values;
             e = make_double2(around + shift, m2 + ::fma(-s, shift, sq));
