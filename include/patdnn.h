@@ -288,7 +288,7 @@ PATDNN_API int patdnn_maxpool2x2(const void *in, void *out, int32_t N, int32_t C
  * reach exactly the (image, group)s that hold them.
  *   desc       copied; a pixel's C channels are consecutive; pixels and images may be further apart than they are long:
  *              strides in elements, 0 = dense.  y strides also hold for dy, x strides for dx.
- *   E_SHAPE    N < 0, P < 1, C < 1, G < 1, C not a multiple of G, |strides| that overlap pixels (x_pixel < C, x_image < P * x_pixel ...),
+ *   E_SHAPE    N < 0, P < 1, C < 1, G < 1, C not a multiple of G, strides that overlap (x_pixel < C, x_image < (P - 1) * x_pixel + C ...),
  *              eps negative or not finite; N <= 65535, C <= 2^20, P < 2^31, N * P * C < 2^40
  *              in the calls: a tensor that is not aligned to its elements, statistics that are not aligned to 8 bytes
  *   E_DTYPE    dtype or act unknown
@@ -313,8 +313,8 @@ PATDNN_API int patdnn_norm_run(patdnn_norm h, const void *x, const float *gamma,
 /* The same, written as a 4-bit matrix of N * P rows and C columns (see below) that patdnn_linear_run_mx4 reads. */
 PATDNN_API int patdnn_norm_run_mx4(patdnn_norm h, const void *x, const float *gamma, const float *beta, void *mx, float *stats,
                                    void *stream);
-/* stats as patdnn_norm_run wrote them; dx DEVICE (x strides), dgamma, dbeta DEVICE float [C], all overwritten.  At z = 0 ReLU
- * passes no gradient. */
+/* stats as patdnn_norm_run wrote them; dx DEVICE (x strides), dgamma, dbeta DEVICE float [C], all overwritten, none of them overlapping
+ * an input.  At z = 0 ReLU passes no gradient. */
 PATDNN_API int patdnn_norm_grad(patdnn_norm h, const void *x, const float *gamma, const float *beta, const float *stats, const void *dy,
                                 void *dx, float *dgamma, float *dbeta, void *stream);
 PATDNN_API int patdnn_norm_free(patdnn_norm h);
@@ -344,7 +344,8 @@ PATDNN_API int patdnn_mx4_dequantize(const void *mx, int32_t dtype, int64_t rows
  *                          the weights once and copies the bias, on `stream`; returns after that is done.
  *   patdnn_linear_run      x DEVICE [rows][ldx], y DEVICE [rows][ldy] of desc->dtype (ld 0 = dense); rows <= max_rows: quantises x into
  *                          the handle's buffer, then multiplies.  Asynchronous; calls that can overlap need a handle each.
- *   patdnn_linear_run_mx4  the same for rows that are 4-bit already (patdnn_mx4_quantize, patdnn_norm_run_mx4); any number of rows
+ *   patdnn_linear_run_mx4  the same for rows that are 4-bit already (patdnn_mx4_quantize, patdnn_norm_run_mx4); any number of them, but all of
+ *                          the matrix's: where its scales lie depends on its number of rows
  *   patdnn_linear_check    waits for the device; E_DEVICE_TIMEOUT if a bounded device-side wait of this handle expired
  * Errors: E_NULL, E_SHAPE (F, K < 1 or > 2^20, rows < 0 or > max_rows, a stride below its row's length, a tensor that is not aligned to
  * its elements), E_DTYPE, E_ALLOC, E_CUDA, E_NO_DEVICE (another device is current than when the handle was made).

@@ -14,9 +14,10 @@
 //   two-pass  images whose slabs do not fit, or for which one launch would keep too few SMs busy: partial statistics per (chunk of
 //             pixels, group), a small kernel that joins them, and an elementwise pass that reads x again.  Images are taken in runs of
 //             at most kRunBytes, and the second pass walks backwards, so that part of that read comes from L2.
-// Measured: forward 2 x 512 x 512 x 128 bf16 SiLU 75 us (statistics 29 us, 4.6 TB/s; join 3.5; elementwise 39, bound by the special-function
-// unit and instruction issue), floor 41 us; gradient 32 x 56 x 56 x 256 bf16 SiLU 56 us (26 + 4.6 + 27), floor 24 us, bound by issue;
-// resident forward 32 x 56 x 56 x 64 fp16 ReLU 10.8 us, floor 3.9.
+// Measured: forward 2 x 512 x 512 x 128 bf16 SiLU 75 us (statistics 29.5 us, 4.6 TB/s; join 3; elementwise 39, 6.9 TB/s: memory), floor 41
+// us, of two passes 61; gradient 32 x 56 x 56 x 256 bf16 SiLU 56 us (26 + 4.6 + 27), floor 24 us: half of the issue slots at 31 % of the
+// warps (80 registers, some spilled), latency more than anything; resident forward 32 x 56 x 56 x 64 fp16 ReLU 10.8 us, floor 3.9, and into
+// 4-bit rows 16 us, with eight warps per SM and 39 % of the issue slots: latency.
 // All sums are fp32 per thread, joined in fp64 and in a fixed order, so that mean and variance are rounded to fp32 about once: values that
 // are held in 4 bits afterwards jump, and every rounding less is a jump less (100352 x 64: 0.36 values per call differ from
 // a plain fp32 evaluation's, 0.57 with joins in fp32).  Variances are never formed as a difference of two large sums: a thread sums (x - m)

@@ -190,8 +190,9 @@ __device__ __forceinline__ float sigmoid(float z) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
     return r;
 }
-// The same for pairs with one reciprocal for two: 1/a = b / (a b).  The special-function unit is what bounds SiLU over 16-bit tensors
-// (2 x 512 x 512 x 128 values: its elementwise pass takes 39 us with 1.5 of its operations per element, 41 with 2).  Arguments below -43 are
+// The same for pairs with one reciprocal for two: 1/a = b / (a b).  It takes a quarter off the work of the special-function unit (the
+// elementwise pass over 2 x 512 x 512 x 128 16-bit values: 39 us with 1.5 of its operations per element, 41 with 2; at 6.9 TB/s memory is
+// what bounds it then, the unit is at 63 %).  Arguments below -43 are
 // taken as -43, so that the product of two denominators stays in range, and a NaN as -43 too, so that it does not reach its neighbour:
 // it comes back with z itself.
 __device__ __forceinline__ float at_least(float z) {   // max(z, -43); NaN stays NaN
