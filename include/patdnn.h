@@ -16,7 +16,7 @@
  * The three calls of the paper's problem statement are patdnn_encode, patdnn_conv and patdnn_free, with
  * patdnn_export / patdnn_decode / patdnn_strerror as inspection helpers.  Everything else declared here
  * (patdnn_conv_host, patdnn_conv_static, patdnn_check, patdnn_plan, patdnn_stack_*, patdnn_maxpool2x2, patdnn_norm_*,
- * patdnn_mx4_*, patdnn_linear_*, the launch counter, patdnn_debug_wait, and the `variant` and `flags` fields of patdnn_desc) is an addition of this library
+ * patdnn_mx4_*, patdnn_linear_*, patdnn_rms_*, patdnn_mx8_*, patdnn_linear8_*, patdnn_gated_*, the launch counter, patdnn_debug_wait, and the `variant` and `flags` fields of patdnn_desc) is an addition of this library
  * with no counterpart in the paper; each says so where it is declared.
  *
  * Conventions used by every call
@@ -54,7 +54,7 @@ enum {
     PATDNN_E_MASK = 4,          /* a kernel's mask is neither empty nor a pattern of the set (Section 4.2) */
     PATDNN_E_ORDER = 5,         /* caller-supplied filter order is not a permutation */
     PATDNN_E_CUDA = 6,          /* a CUDA call failed; patdnn_last_cuda_error() has the text */
-    PATDNN_E_NO_DEVICE = 7,     /* handle was encoded host-only, no CUDA device is usable, or another one is current (norm, linear) */
+    PATDNN_E_NO_DEVICE = 7,     /* handle was encoded host-only, no CUDA device is usable, or another one is current (norms, linear, gated) */
     PATDNN_E_DEVICE_TIMEOUT = 8,/* a bounded device-side wait expired */
     PATDNN_E_DTYPE = 9,         /* unknown dtype / variant value */
     PATDNN_E_ALLOC = 10,        /* host allocation failed */
@@ -63,7 +63,7 @@ enum {
 };
 
 enum { PATDNN_F32 = 0, PATDNN_F16 = 1,      /* storage type of weights and activations; accumulation is fp32 */
-       PATDNN_BF16 = 2 };                    /* bfloat16: group norm, 4-bit quantisation and linear layers only */
+       PATDNN_BF16 = 2 };                    /* bfloat16: norms, 4-bit and 8-bit matrices, linear layers and the gated block only */
 enum { PATDNN_ACT_NONE = 0, PATDNN_ACT_RELU = 1, PATDNN_ACT_SILU = 2 };   /* activations of those: max(0, z); z / (1 + exp(-z)) */
 
 /* Kernel variants (an addition: the paper generates one code version per layer and tunes it offline).
@@ -382,6 +382,76 @@ typedef struct {
 } patdnn_linear_plan_info;
 PATDNN_API int patdnn_linear_plan(int32_t F, int32_t K, int64_t rows, int32_t from_4_bit_rows, patdnn_linear_plan_info *info);
 PATDNN_API int patdnn_linear_free(patdnn_linear h);
+
+/*
+ * RMS norm of rows with the residual's addition in front, and its gradient (addition).  For row m of C columns:
+ *   s = x + residual (s = x without one), rstd = 1 / sqrt(mean(s^2) + eps), y = s * rstd * gamma
+ *   gradient, xh = s * rstd, u = dy * gamma:  dx = rstd * (u - xh * mean(u * xh)) + dsum;  dgamma = sum over rows of dy * xh
+ * s is formed and kept in fp32 for the statistics and for y; the stored sum, y and dx are rounded once.  Sums are fp32, in a fixed order
+ * (the same call gives the same bits); rows whose squares leave fp32's range are scaled by a power of two.  A row that holds a NaN or an
+ * infinity spoils itself alone (and dgamma).
+ *   desc       copied; a row's columns are consecutive; strides in elements, 0 = dense: x_row of x and dx, r_row of residual, sum, s and
+ *              dsum, y_row of y and dy
+ *   E_SHAPE    C < 1 or > 65536, a stride below C or above 2^31, eps negative or not finite; in the calls: rows < 0 or > 2^31 - 1,
+ *              rows * C > 2^40, a tensor that is not aligned to its elements, an 8-bit buffer that is not aligned to 16 bytes
+ *   E_DTYPE    dtype unknown
+ *   E_NO_DEVICE  another device is current than when the handle was made
+ * A handle owns the gradient's workspace: gradient calls that can overlap on the GPU need a handle each; patdnn_rms_run and _run_mx8 use
+ * none.  rows = 0 launches nothing (the gradient writes zeros to dgamma).  Asynchronous on `stream`, but for patdnn_rms_create.
+ */
+typedef struct patdnn_rms_s *patdnn_rms;
+typedef struct {
+    int32_t C;
+    int32_t dtype;              /* of x, residual, sum, y, s, dy, dsum, dx: PATDNN_F32, _F16 or _BF16; gamma, rstd, dgamma are float */
+    int64_t x_row, r_row, y_row;
+    float eps;
+} patdnn_rms_desc;
+
+PATDNN_API int patdnn_rms_create(const patdnn_rms_desc *desc, patdnn_rms *out);
+/* residual DEVICE or NULL; gamma DEVICE float [C]; sum DEVICE or NULL: receives s, and may be residual itself (or x itself where x_row =
+ * r_row); y DEVICE, overlapping none of the others; rstd DEVICE float [rows] or NULL. */
+PATDNN_API int patdnn_rms_run(patdnn_rms h, const void *x, const void *residual, const float *gamma, void *sum, void *y, float *rstd,
+                              int64_t rows, void *stream);
+/* The same, written as an 8-bit matrix of `rows` rows and C columns (see below) that patdnn_linear8_run_mx8 reads. */
+PATDNN_API int patdnn_rms_run_mx8(patdnn_rms h, const void *x, const void *residual, const float *gamma, void *sum, void *mx, float *rstd,
+                                  int64_t rows, void *stream);
+/* s as the run stored it (x where there was no residual and x_row = r_row), rstd as it wrote it; dsum DEVICE or NULL: the gradient that
+ * reaches s on its other way; dx, the gradient of x and of residual, may be dy, dsum or s itself where their strides are the same; dgamma
+ * DEVICE float [C].  Both are overwritten. */
+PATDNN_API int patdnn_rms_grad(patdnn_rms h, const void *s, const float *gamma, const float *rstd, const void *dy, const void *dsum, void *dx,
+                               float *dgamma, int64_t rows, void *stream);
+PATDNN_API int patdnn_rms_free(patdnn_rms h);
+
+/*
+ * Microscaled 8-bit matrices (addition).  A block is 128 consecutive columns of a row, the last one of a row may be shorter; its scale
+ * is 2^max(ceil(log2(amax / 448)), -127), held in 8 bits; an element is x / scale rounded to the nearest E4M3 value (sign, 4 exponent and
+ * 3 mantissa bits; 448 is the largest), ties to even, so that nothing saturates.  A block with an infinity or a NaN becomes NaNs.
+ * The layout of the buffer is the library's own (tiles in the order in which the tensor cores read them); patdnn_mx8_dequantize
+ * gives the values.  Padding in it never reaches a result.
+ *   patdnn_mx8_bytes       size of the buffer for rows x cols, which depends on these alone; 16-byte aligned buffers are needed
+ *   patdnn_mx8_quantize    x DEVICE [rows][ld] of dtype -> mx DEVICE
+ *   patdnn_mx8_dequantize  mx DEVICE -> out DEVICE [rows][ld] of dtype, rounded once (in float and bfloat16 every value is exact, but for
+ *                          values that rounded up to 2^128, which become infinities; in half, values above 65504 or below 2^-14 round)
+ * Errors: E_NULL, E_SHAPE (rows < 0, cols < 1, ld < cols, cols > 2^20, rows * cols > 2^40, buffer not aligned), E_DTYPE, E_CUDA.
+ * rows = 0 launches nothing.  Asynchronous.
+ */
+PATDNN_API int patdnn_mx8_bytes(int64_t rows, int64_t cols, int64_t *bytes);
+PATDNN_API int patdnn_mx8_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, void *mx, void *stream);
+PATDNN_API int patdnn_mx8_dequantize(const void *mx, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, void *out, void *stream);
+
+/*
+ * Linear layers with 8-bit weights (addition): y[m][f] = act(bias[f] + sum_k q(x)[m][k] * q(w)[f][k]), q as above, sums fp32 on the
+ * block-scaled tensor cores, y rounded once.  Calls, arguments and errors are those of patdnn_linear_* with patdnn_mx8_* rows
+ * (patdnn_mx8_quantize, patdnn_rms_run_mx8) in place of 4-bit ones.
+ */
+typedef struct patdnn_linear8_s *patdnn_linear8;
+PATDNN_API int patdnn_linear8_encode(const void *weights, int64_t ldw, const patdnn_linear_desc *desc, void *stream, patdnn_linear8 *out);
+PATDNN_API int patdnn_linear8_run(patdnn_linear8 h, const void *x, int64_t rows, int64_t ldx, void *y, int64_t ldy, void *stream);
+PATDNN_API int patdnn_linear8_run_mx8(patdnn_linear8 h, const void *mx, int64_t rows, void *y, int64_t ldy, void *stream);
+PATDNN_API int patdnn_linear8_check(patdnn_linear8 h);
+PATDNN_API int patdnn_linear8_plan(int32_t F, int32_t K, int64_t rows, int32_t from_8_bit_rows, patdnn_linear_plan_info *info);
+PATDNN_API int patdnn_linear8_debug_wait(patdnn_linear8 h, uint32_t polls, int32_t skip_load_iteration);
+PATDNN_API int patdnn_linear8_free(patdnn_linear8 h);
 
 /* Number of this library's kernels launched by the process since the last reset (addition, for reports). */
 PATDNN_API int64_t patdnn_launch_count(void);

@@ -16,7 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libpatdnn.so")
 
 OK = 0
-F32, F16, BF16 = 0, 1, 2                  # BF16: group norm, 4-bit matrices and linear layers only
+F32, F16, BF16 = 0, 1, 2                  # BF16: norms, 4-bit and 8-bit matrices, linear layers and the gated block only
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 VARIANT_AUTO, VARIANT_NOOPT, VARIANT_REORDER, VARIANT_TILED, VARIANT_DENSE_TC, VARIANT_PATTERN_RUN = 0, 1, 2, 3, 4, 5
 FLAG_HOST_ONLY = 1
@@ -32,6 +32,10 @@ EXPORTED_SYMBOLS = (
     "patdnn_mx4_bytes", "patdnn_mx4_quantize", "patdnn_mx4_dequantize",
     "patdnn_linear_encode", "patdnn_linear_run", "patdnn_linear_run_mx4", "patdnn_linear_check", "patdnn_linear_plan", "patdnn_linear_debug_wait",
     "patdnn_linear_free",
+    "patdnn_rms_create", "patdnn_rms_run", "patdnn_rms_run_mx8", "patdnn_rms_grad", "patdnn_rms_free",
+    "patdnn_mx8_bytes", "patdnn_mx8_quantize", "patdnn_mx8_dequantize",
+    "patdnn_linear8_encode", "patdnn_linear8_run", "patdnn_linear8_run_mx8", "patdnn_linear8_check", "patdnn_linear8_plan",
+    "patdnn_linear8_debug_wait", "patdnn_linear8_free",
 )
 
 
@@ -73,6 +77,11 @@ class _NormDesc(ctypes.Structure):
 class _LinearDesc(ctypes.Structure):
     _fields_ = [("F", ctypes.c_int32), ("K", ctypes.c_int32), ("max_rows", ctypes.c_int64), ("bias", ctypes.c_void_p),
                 ("act", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class _RmsDesc(ctypes.Structure):
+    _fields_ = [("C", ctypes.c_int32), ("dtype", ctypes.c_int32), ("x_row", ctypes.c_int64), ("r_row", ctypes.c_int64),
+                ("y_row", ctypes.c_int64), ("eps", ctypes.c_float)]
 
 
 class _LinearPlan(ctypes.Structure):
@@ -130,6 +139,17 @@ def load() -> ctypes.CDLL:
     lib.patdnn_linear_debug_wait.argtypes = [vp, ctypes.c_uint32, i32]
     lib.patdnn_linear_plan.argtypes = [i32, i32, i64, i32, ctypes.POINTER(_LinearPlan)]
     lib.patdnn_linear_free.argtypes = [vp]
+    lib.patdnn_rms_create.argtypes = [ctypes.POINTER(_RmsDesc), ctypes.POINTER(vp)]
+    lib.patdnn_rms_run.argtypes = [vp] * 7 + [i64, vp]
+    lib.patdnn_rms_run_mx8.argtypes = [vp] * 7 + [i64, vp]
+    lib.patdnn_rms_grad.argtypes = [vp] * 8 + [i64, vp]
+    lib.patdnn_rms_free.argtypes = [vp]
+    lib.patdnn_mx8_bytes.argtypes = lib.patdnn_mx4_bytes.argtypes
+    lib.patdnn_mx8_quantize.argtypes = lib.patdnn_mx4_quantize.argtypes
+    lib.patdnn_mx8_dequantize.argtypes = lib.patdnn_mx4_dequantize.argtypes
+    for name in ("encode", "run", "check", "debug_wait", "plan", "free"):
+        getattr(lib, "patdnn_linear8_" + name).argtypes = getattr(lib, "patdnn_linear_" + name).argtypes
+    lib.patdnn_linear8_run_mx8.argtypes = lib.patdnn_linear_run_mx4.argtypes
     lib.patdnn_launch_count.restype = ctypes.c_int64
     lib.patdnn_reset_launch_count.restype = None
     for name in ("patdnn_strerror", "patdnn_last_cuda_error", "patdnn_version"):
@@ -438,6 +458,110 @@ def linear_plan(F: int, K: int, rows: int, *, from_4_bit_rows: bool = False) -> 
     """patdnn_linear_plan: how ``Linear.run`` (or ``run_mx4``) launches its product; needs no device."""
     info = _LinearPlan()
     _check(load().patdnn_linear_plan(F, K, rows, int(from_4_bit_rows), ctypes.byref(info)), "patdnn_linear_plan")
+    return {n: int(getattr(info, n)) for n, _ in info._fields_ if n != "reserved"}
+
+
+class RmsNorm:
+    """RMS norm of rows with the residual's addition in front (``patdnn_rms``): s = x + residual, y = s / rms(s) * gamma.
+
+    ``x_row`` is the element stride of x and dx, ``r_row`` that of residual, sum, s and dsum, ``y_row`` that of y and dy (0 = dense).
+    Gradient calls that can overlap on the GPU need a handle each."""
+
+    def __init__(self, C: int, *, dtype: int = F32, eps: float = 1e-6, x_row: int = 0, r_row: int = 0, y_row: int = 0):
+        d = _RmsDesc(C=C, dtype=dtype, x_row=x_row, r_row=r_row, y_row=y_row, eps=eps)
+        h = ctypes.c_void_p()
+        self._h = 0
+        _check(load().patdnn_rms_create(ctypes.byref(d), ctypes.byref(h)), "patdnn_rms_create")
+        self._h = h.value
+
+    def run(self, x, gamma, y, rows: int, *, residual=None, sum=None, rstd=None, stream: int = 0) -> None:
+        """patdnn_rms_run: ``sum`` receives s (it may be ``residual`` itself), ``rstd`` 1 / rms of every row; asynchronous."""
+        _check(load().patdnn_rms_run(self._h, _ptr(x), _opt(residual), _ptr(gamma), _opt(sum), _ptr(y), _opt(rstd), rows, stream), "patdnn_rms_run")
+
+    def run_mx8(self, x, gamma, mx, rows: int, *, residual=None, sum=None, rstd=None, stream: int = 0) -> None:
+        """patdnn_rms_run_mx8: the same, as an 8-bit matrix of ``rows`` rows and C columns (``mx8_bytes(rows, C)``)."""
+        _check(load().patdnn_rms_run_mx8(self._h, _ptr(x), _opt(residual), _ptr(gamma), _opt(sum), _ptr(mx), _opt(rstd), rows, stream),
+               "patdnn_rms_run_mx8")
+
+    def grad(self, s, gamma, rstd, dy, dx, dgamma, rows: int, *, dsum=None, stream: int = 0) -> None:
+        """patdnn_rms_grad: gradients of ``run`` with its sum and rstd; overwrites dx and dgamma."""
+        _check(load().patdnn_rms_grad(self._h, _ptr(s), _ptr(gamma), _ptr(rstd), _ptr(dy), _opt(dsum), _ptr(dx), _ptr(dgamma), rows, stream),
+               "patdnn_rms_grad")
+
+    def free(self) -> None:
+        if self._h:
+            load().patdnn_rms_free(self._h)
+            self._h = 0
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def mx8_bytes(rows: int, cols: int) -> int:
+    """Size of the buffer of an 8-bit matrix."""
+    v = ctypes.c_int64()
+    _check(load().patdnn_mx8_bytes(rows, cols, ctypes.byref(v)), "patdnn_mx8_bytes")
+    return int(v.value)
+
+
+def mx8_quantize(x, mx, rows: int, cols: int, *, dtype: int = F32, ld: int = 0, stream: int = 0) -> None:
+    """patdnn_mx8_quantize: rows of x (``ld`` elements apart, 0 = dense) -> 8-bit matrix."""
+    _check(load().patdnn_mx8_quantize(_ptr(x), dtype, rows, cols, ld, _ptr(mx), stream), "patdnn_mx8_quantize")
+
+
+def mx8_dequantize(mx, out, rows: int, cols: int, *, dtype: int = F32, ld: int = 0, stream: int = 0) -> None:
+    """patdnn_mx8_dequantize: the values that an 8-bit matrix stands for."""
+    _check(load().patdnn_mx8_dequantize(_ptr(mx), dtype, rows, cols, ld, _ptr(out), stream), "patdnn_mx8_dequantize")
+
+
+class Linear8:
+    """A linear layer with 8-bit weights (``patdnn_linear8``): y = act(q(x) q(weights)^T + bias).
+
+    ``weights`` DEVICE [F][K] of ``dtype`` (rows ``ldw`` apart), ``bias`` DEVICE float [F]; both are read during the call only."""
+
+    def __init__(self, weights, F: int, K: int, *, max_rows: int, dtype: int = F32, bias=None, act: int = ACT_NONE, ldw: int = 0,
+                 stream: int = 0):
+        d = _LinearDesc(F=F, K=K, max_rows=max_rows, bias=_opt(bias), act=act, dtype=dtype)
+        h = ctypes.c_void_p()
+        self._h = 0
+        _check(load().patdnn_linear8_encode(_ptr(weights), ldw, ctypes.byref(d), stream, ctypes.byref(h)), "patdnn_linear8_encode")
+        self._h = h.value
+
+    def run(self, x, y, rows: int, *, ldx: int = 0, ldy: int = 0, stream: int = 0) -> None:
+        """patdnn_linear8_run: quantises the rows of x, then multiplies; asynchronous."""
+        _check(load().patdnn_linear8_run(self._h, _ptr(x), rows, ldx, _ptr(y), ldy, stream), "patdnn_linear8_run")
+
+    def run_mx8(self, mx, y, rows: int, *, ldy: int = 0, stream: int = 0) -> None:
+        """patdnn_linear8_run_mx8: rows that are 8-bit already."""
+        _check(load().patdnn_linear8_run_mx8(self._h, _ptr(mx), rows, _ptr(y), ldy, stream), "patdnn_linear8_run_mx8")
+
+    def check(self) -> None:
+        """patdnn_linear8_check: synchronise and raise if a device-side bounded wait expired."""
+        _check(load().patdnn_linear8_check(self._h), "patdnn_linear8_check")
+
+    def debug_wait(self, polls: int, skip_load_iteration: int = 0) -> None:
+        """patdnn_linear8_debug_wait: as :meth:`Linear.debug_wait`."""
+        _check(load().patdnn_linear8_debug_wait(self._h, polls, skip_load_iteration), "patdnn_linear8_debug_wait")
+
+    def free(self) -> None:
+        if self._h:
+            load().patdnn_linear8_free(self._h)
+            self._h = 0
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def linear8_plan(F: int, K: int, rows: int, *, from_8_bit_rows: bool = False) -> dict:
+    """patdnn_linear8_plan: how ``Linear8.run`` (or ``run_mx8``) launches its product; needs no device."""
+    info = _LinearPlan()
+    _check(load().patdnn_linear8_plan(F, K, rows, int(from_8_bit_rows), ctypes.byref(info)), "patdnn_linear8_plan")
     return {n: int(getattr(info, n)) for n, _ in info._fields_ if n != "reserved"}
 
 

@@ -1,0 +1,88 @@
+// Internal interfaces of the feed-forward operators: RMS norm with the residual's addition, 8-bit matrices, the linear layer with 8-bit
+// weights, and the gated block.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "ops.hpp"
+
+namespace patdnn {
+
+// ---- 8-bit blocks (mx8.cu) ---------------------------------------------------------------------------------------------
+// A matrix of R rows and K columns is cut into tiles of 128 rows by 128 columns.  All code tiles come first ([row tile][column tile]),
+// 128 rows of 128 bytes each; inside a tile the 16-byte unit u of row r sits at unit u ^ (r & 7), the order in which the tensor cores
+// read it from shared memory, so that a tile is ONE contiguous copy.  Then the scales: per row tile and FOUR column tiles 512 bytes,
+// the scale byte of (row r, column tile t) at (r % 32) * 16 + (r / 32) * 4 + t % 4, the order in which they are copied to tensor memory.
+struct Mx8Shape {
+    int64_t rows, cols;
+    int64_t row_tiles, col_tiles, groups;   // groups: of four column tiles
+    int64_t scales_at, bytes;               // offset of the scales; size of the whole buffer
+};
+constexpr int kMx8Tile = 128 * 128, kMx8Scales = 512;
+inline Mx8Shape mx8_shape(int64_t rows, int64_t cols) {
+    Mx8Shape m{};
+    m.rows = rows; m.cols = cols;
+    m.row_tiles = ceil_div(rows, 128);
+    m.col_tiles = ceil_div(cols, 128);
+    m.groups = ceil_div(m.col_tiles, 4);
+    m.scales_at = m.row_tiles * m.col_tiles * kMx8Tile;
+    m.bytes = m.scales_at + m.row_tiles * m.groups * kMx8Scales;
+    return m;
+}
+cudaError_t launch_mx8_quantize(const Mx8Shape &m, const void *x, int dtype, int64_t ld, void *mx, cudaStream_t st);
+cudaError_t launch_mx8_dequantize(const Mx8Shape &m, const void *mx, void *out, int dtype, int64_t ld, cudaStream_t st);
+
+// ---- 8-bit product (mx8_linear.cu) --------------------------------------------------------------------------------------
+struct Mx8Params {
+    const uint8_t *w, *x;                   // 8-bit matrices [F][K], [rows][K] in the layout above
+    const void *x_raw;                      // or (x == nullptr) at most kFusedRows rows of x as they are, ldx elements apart
+    int64_t ldx, K;
+    const float *bias;                      // [F] or nullptr
+    void *y;
+    int *status;
+    int64_t ldy, rows;
+    int64_t w_scales, x_scales;             // offsets of the scales
+    int F, col_tiles, groups, ksteps;       // groups of four column tiles; ksteps: K-steps of 32 columns that hold data
+    int act, dtype;
+    int f_tiles, n_tiles;                   // tiles of rows of w; of rows of x
+    int tile_n;                             // rows of the N operand in a tile
+    int splits, tiles_per_split;            // cluster split of the column tiles
+    int stages;
+    int tensor_columns;                     // of tensor memory that a CTA allocates
+    int step_n, step_f;                     // persistent kernel: from a CTA's tile to its next one
+    uint32_t spin_limit;                    // polls of a bounded wait (0 = the default)
+    int test_skip_load;                     // test hook: every CTA leaves out the copies of this (1-based) column tile of its walk (0 = off)
+};
+using Mx8Launch = Mx4Launch;
+cudaError_t prepare_mx8_linear();                       // opt in to the dynamic shared memory
+Mx8Launch plan_mx8_linear(Mx8Params &p);                // shapes of p (F, K, rows, x_raw) -> its tiling and the launch; no device is touched
+cudaError_t launch_mx8_linear(Mx8Params p, cudaStream_t st, int *launches);
+
+// ---- RMS norm (rms_norm.cu) --------------------------------------------------------------------------------------------
+constexpr int kRmsMostColumns = 1 << 16;    // a row is held in the registers of at most eight CTAs
+struct RmsShape {
+    int C, dtype;
+    float eps;
+    int64_t x_row, r_row, y_row;            // strides in elements
+};
+struct RmsCall {
+    const void *x, *residual;               // residual may be nullptr
+    const float *gamma;
+    void *sum, *y, *mx;                     // sum, and one of y and mx, may be nullptr
+    float *rstd;                            // may be nullptr
+    int64_t rows;
+};
+cudaError_t launch_rms_norm(const RmsShape &s, const RmsCall &c, cudaStream_t st);
+struct RmsGradCall {
+    const void *s, *dy, *dsum;              // dsum may be nullptr
+    const float *gamma, *rstd;
+    void *dx;
+    float *dgamma, *ws;
+    int64_t rows;
+};
+size_t rms_workspace_floats(const RmsShape &s);
+cudaError_t launch_rms_grad(const RmsShape &s, const RmsGradCall &c, cudaStream_t st, int *launches);
+
+}  // namespace patdnn
