@@ -59,7 +59,8 @@ enum {
     PATDNN_E_DTYPE = 9,         /* unknown dtype / variant value */
     PATDNN_E_ALLOC = 10,        /* host allocation failed */
     PATDNN_E_STACK = 11,        /* layers of a stack do not chain (shape or dtype mismatch) */
-    PATDNN_E_SCRATCH = 12       /* the layer needs more scratch than the fixed device buffer of patdnn_conv_static */
+    PATDNN_E_SCRATCH = 12       /* the layer needs more scratch than the fixed device buffer of patdnn_conv_static; a gated block
+                                 * without its gradient's workspace */
 };
 
 enum { PATDNN_F32 = 0, PATDNN_F16 = 1,      /* storage type of weights and activations; accumulation is fp32 */
@@ -452,6 +453,56 @@ PATDNN_API int patdnn_linear8_check(patdnn_linear8 h);
 PATDNN_API int patdnn_linear8_plan(int32_t F, int32_t K, int64_t rows, int32_t from_8_bit_rows, patdnn_linear_plan_info *info);
 PATDNN_API int patdnn_linear8_debug_wait(patdnn_linear8 h, uint32_t polls, int32_t skip_load_iteration);
 PATDNN_API int patdnn_linear8_free(patdnn_linear8 h);
+
+/*
+ * Gated feed-forward block (addition): both projections, the activation and the product in one kernel, and their gradients.
+ *   g = x wg^T, u = x wu^T, h = act(g) * u                          x [rows][K], wg and wu [F][K], h [rows][F]
+ *   dg = dh * u * act'(g), du = dh * act(g);  dx = dg wg + du wu, dwg = dg^T x, dwu = du^T x
+ * Sums are fp32 on the tensor cores, in a fixed order; g and u stay in fp32 for h, which is rounded once.  For the gradient the run stores
+ * g and u rounded to the tensors' type (gu), and dg and du are rounded to it as operands of the products; dx, dwg and dwu are rounded once
+ * more.  At g = 0 ReLU passes no gradient.  A row of x that is not finite spoils its row of h alone.
+ *   desc       copied; rows of consecutive elements; strides in elements, 0 = dense: x_row of x and dx, w_row of the four weight tensors,
+ *              h_row of h and dh; gu is dense, [rows][2][F], g before u.  grad != 0: gradients will be asked for (more workspace)
+ *   patdnn_gated_run       gu DEVICE or NULL
+ *   patdnn_gated_grad      dx DEVICE or NULL, dwg and dwu DEVICE or both NULL: what is asked for is overwritten; none may overlap an input
+ *   patdnn_gated_check     waits for the device; E_DEVICE_TIMEOUT if a bounded device-side wait of this handle expired
+ *   patdnn_gated_debug_wait  as patdnn_linear_debug_wait; the iteration is the block of 64 in a CTA's own walk
+ * Errors: E_NULL, E_SHAPE (F, K < 1 or > 2^20, rows < 0 or > max_rows, more than 2^31 - 1 or 2^40 elements, a stride below its row's length or
+ * above 2^31, a tensor that is not aligned to its elements, or x, wg or wu with rows that are whole 16-byte units apart and not aligned to 16
+ * bytes), E_DTYPE (F16 and BF16 only), E_SCRATCH (a gradient without desc.grad), E_ALLOC, E_CUDA, E_NO_DEVICE (another device is current).
+ * A handle owns its workspace (19 MB, and what max_rows needs for gradients and for rows that are not whole 16-byte units apart, which are
+ * packed first): calls that can overlap need a handle each, others may share one, whatever their weights.  rows = 0 launches nothing (the
+ * gradient writes zeros to dwg and dwu).  patdnn_gated_create waits for the device; the calls are asynchronous on `stream`.
+ */
+typedef struct patdnn_gated_s *patdnn_gated;
+typedef struct {
+    int32_t F, K;               /* outputs (of either projection), inputs */
+    int64_t max_rows;
+    int64_t x_row, w_row, h_row;
+    int32_t act;                /* PATDNN_ACT_* */
+    int32_t dtype;              /* of every tensor: PATDNN_F16 or _BF16 */
+    int32_t grad;
+    int32_t reserved;
+} patdnn_gated_desc;
+
+PATDNN_API int patdnn_gated_create(const patdnn_gated_desc *desc, patdnn_gated *out);
+PATDNN_API int patdnn_gated_run(patdnn_gated h, const void *x, const void *wg, const void *wu, void *hidden, void *gu, int64_t rows, void *stream);
+PATDNN_API int patdnn_gated_grad(patdnn_gated h, const void *x, const void *wg, const void *wu, const void *gu, const void *dh, void *dx, void *dwg,
+                                 void *dwu, int64_t rows, void *stream);
+PATDNN_API int patdnn_gated_check(patdnn_gated h);
+PATDNN_API int patdnn_gated_debug_wait(patdnn_gated h, uint32_t polls, int32_t skip_load_iteration);
+
+/* How a product of the block is launched (inspection; touches no device).  product: 0 for h, 1 for dx, 2 for dwg and dwu.  Errors: E_NULL, E_SHAPE. */
+typedef struct {
+    int32_t row_tiles, column_tiles;    /* tiles of the product */
+    int32_t blocks;                     /* of 64 along the summed dimension */
+    int32_t splits, blocks_per_split;   /* ranges of them that share a tile */
+    int32_t grid;                       /* CTAs */
+    int32_t stages;                     /* blocks in the ring of copies */
+    int32_t smem_bytes;                 /* dynamic shared memory of a CTA */
+} patdnn_gated_plan_info;
+PATDNN_API int patdnn_gated_plan(int32_t F, int32_t K, int64_t rows, int32_t product, patdnn_gated_plan_info *info);
+PATDNN_API int patdnn_gated_free(patdnn_gated h);
 
 /* Number of this library's kernels launched by the process since the last reset (addition, for reports). */
 PATDNN_API int64_t patdnn_launch_count(void);

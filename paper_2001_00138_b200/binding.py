@@ -36,6 +36,8 @@ EXPORTED_SYMBOLS = (
     "patdnn_mx8_bytes", "patdnn_mx8_quantize", "patdnn_mx8_dequantize",
     "patdnn_linear8_encode", "patdnn_linear8_run", "patdnn_linear8_run_mx8", "patdnn_linear8_check", "patdnn_linear8_plan",
     "patdnn_linear8_debug_wait", "patdnn_linear8_free",
+    "patdnn_gated_create", "patdnn_gated_run", "patdnn_gated_grad", "patdnn_gated_check", "patdnn_gated_plan", "patdnn_gated_debug_wait",
+    "patdnn_gated_free",
 )
 
 
@@ -82,6 +84,15 @@ class _LinearDesc(ctypes.Structure):
 class _RmsDesc(ctypes.Structure):
     _fields_ = [("C", ctypes.c_int32), ("dtype", ctypes.c_int32), ("x_row", ctypes.c_int64), ("r_row", ctypes.c_int64),
                 ("y_row", ctypes.c_int64), ("eps", ctypes.c_float)]
+
+
+class _GatedDesc(ctypes.Structure):
+    _fields_ = [("F", ctypes.c_int32), ("K", ctypes.c_int32), ("max_rows", ctypes.c_int64), ("x_row", ctypes.c_int64), ("w_row", ctypes.c_int64),
+                ("h_row", ctypes.c_int64), ("act", ctypes.c_int32), ("dtype", ctypes.c_int32), ("grad", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class _GatedPlan(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("row_tiles", "column_tiles", "blocks", "splits", "blocks_per_split", "grid", "stages", "smem_bytes")]
 
 
 class _LinearPlan(ctypes.Structure):
@@ -150,6 +161,13 @@ def load() -> ctypes.CDLL:
     for name in ("encode", "run", "check", "debug_wait", "plan", "free"):
         getattr(lib, "patdnn_linear8_" + name).argtypes = getattr(lib, "patdnn_linear_" + name).argtypes
     lib.patdnn_linear8_run_mx8.argtypes = lib.patdnn_linear_run_mx4.argtypes
+    lib.patdnn_gated_create.argtypes = [ctypes.POINTER(_GatedDesc), ctypes.POINTER(vp)]
+    lib.patdnn_gated_run.argtypes = [vp] * 6 + [i64, vp]
+    lib.patdnn_gated_grad.argtypes = [vp] * 9 + [i64, vp]
+    lib.patdnn_gated_check.argtypes = [vp]
+    lib.patdnn_gated_plan.argtypes = [i32, i32, i64, i32, ctypes.POINTER(_GatedPlan)]
+    lib.patdnn_gated_debug_wait.argtypes = [vp, ctypes.c_uint32, i32]
+    lib.patdnn_gated_free.argtypes = [vp]
     lib.patdnn_launch_count.restype = ctypes.c_int64
     lib.patdnn_reset_launch_count.restype = None
     for name in ("patdnn_strerror", "patdnn_last_cuda_error", "patdnn_version"):
@@ -563,6 +581,56 @@ def linear8_plan(F: int, K: int, rows: int, *, from_8_bit_rows: bool = False) ->
     info = _LinearPlan()
     _check(load().patdnn_linear8_plan(F, K, rows, int(from_8_bit_rows), ctypes.byref(info)), "patdnn_linear8_plan")
     return {n: int(getattr(info, n)) for n, _ in info._fields_ if n != "reserved"}
+
+
+class Gated:
+    """Gated feed-forward block (``patdnn_gated``): h = act(x wg^T) * (x wu^T), and its gradients; F16 or BF16.
+
+    ``x_row`` is the element stride of x and dx, ``w_row`` that of wg, wu, dwg and dwu, ``h_row`` that of h and dh (0 = dense); ``grad`` asks for
+    the gradient's workspace.  Calls that can overlap on the GPU need a handle each; others may share one, whatever their weights."""
+
+    def __init__(self, F: int, K: int, *, max_rows: int, dtype: int = BF16, act: int = ACT_SILU, x_row: int = 0, w_row: int = 0, h_row: int = 0,
+                 grad: bool = False):
+        d = _GatedDesc(F=F, K=K, max_rows=max_rows, x_row=x_row, w_row=w_row, h_row=h_row, act=act, dtype=dtype, grad=int(grad))
+        h = ctypes.c_void_p()
+        self._h = 0
+        _check(load().patdnn_gated_create(ctypes.byref(d), ctypes.byref(h)), "patdnn_gated_create")
+        self._h = h.value
+
+    def run(self, x, wg, wu, h, rows: int, *, gu=None, stream: int = 0) -> None:
+        """patdnn_gated_run: ``gu`` [rows][2][F] receives both projections, for the gradient; asynchronous."""
+        _check(load().patdnn_gated_run(self._h, _ptr(x), _ptr(wg), _ptr(wu), _ptr(h), _opt(gu), rows, stream), "patdnn_gated_run")
+
+    def grad(self, x, wg, wu, gu, dh, dx, dwg, dwu, rows: int, *, stream: int = 0) -> None:
+        """patdnn_gated_grad: gradients of ``run`` with its gu; ``dx``, or ``dwg`` and ``dwu``, may be None."""
+        _check(load().patdnn_gated_grad(self._h, _ptr(x), _ptr(wg), _ptr(wu), _ptr(gu), _ptr(dh), _opt(dx), _opt(dwg), _opt(dwu), rows, stream),
+               "patdnn_gated_grad")
+
+    def check(self) -> None:
+        """patdnn_gated_check: synchronise and raise if a device-side bounded wait expired."""
+        _check(load().patdnn_gated_check(self._h), "patdnn_gated_check")
+
+    def debug_wait(self, polls: int, skip_load_iteration: int = 0) -> None:
+        """patdnn_gated_debug_wait: bound of the device-side waits (polls; 0 = default) and the test hook that withholds the copies of one block."""
+        _check(load().patdnn_gated_debug_wait(self._h, polls, skip_load_iteration), "patdnn_gated_debug_wait")
+
+    def free(self) -> None:
+        if self._h:
+            load().patdnn_gated_free(self._h)
+            self._h = 0
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def gated_plan(F: int, K: int, rows: int, product: int = 0) -> dict:
+    """patdnn_gated_plan: how a product of the gated block is launched (0: h, 1: dx, 2: dwg and dwu); needs no device."""
+    info = _GatedPlan()
+    _check(load().patdnn_gated_plan(F, K, rows, product, ctypes.byref(info)), "patdnn_gated_plan")
+    return {n: int(getattr(info, n)) for n, _ in info._fields_}
 
 
 def maxpool2x2(x, out, N: int, C: int, H: int, W: int, dtype: int = F32, stream: int = 0) -> None:

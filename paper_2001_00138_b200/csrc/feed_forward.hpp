@@ -85,4 +85,42 @@ struct RmsGradCall {
 size_t rms_workspace_floats(const RmsShape &s);
 cudaError_t launch_rms_grad(const RmsShape &s, const RmsGradCall &c, cudaStream_t st, int *launches);
 
+// ---- gated feed-forward block (gated.cu, gated_aux.cu) ---------------------------------------------------------------------
+enum GatedMode { kGatedForward = 0, kGatedInput = 1, kGatedWeights = 2 };   // h; dx; dwg and dwu
+struct GatedShape {
+    int F, K, act, dtype;                   // dtype: F16 or BF16
+    int64_t x_row, w_row, h_row;            // strides in elements
+};
+struct GatedPlan {
+    int m_tiles, n_tiles;                   // tiles of 256 rows, and of 256 columns of the product (forward: 128 outputs, gate and up)
+    int k_blocks, splits, per_split;        // blocks of 64 along the summed dimension; ranges of them that share a tile; blocks of a range
+    int grid, stages, smem;                 // CTAs; blocks in the ring of copies; dynamic shared memory
+};
+GatedPlan plan_gated(int F, int K, int64_t rows, int mode);
+constexpr int kGatedUnitFloats = 256 * 256; // partial sums of a (tile, split) unit
+constexpr int kGatedCounters = 16;          // of a tile: epilogue warps of both CTAs
+struct GatedWork {                          // a handle's buffers
+    void *dgu;                              // [max_rows][2 Fp]: dg, du in the handle's type, Fp = F rounded up to 64; nullptr without gradients
+    float *partial;
+    unsigned *arrivals;                     // zero between calls
+    int *status;
+};
+inline int gated_padded(int F) { return (F + 63) / 64 * 64; }
+struct GatedCall {
+    const void *x, *wg, *wu;                // rows 16-byte aligned, x_row / w_row apart
+    int64_t x_row, w_row;                   // of these (not of the outputs)
+    void *h, *gu;                           // forward; gu may be nullptr
+    void *dx, *dwg, *dwu;
+    int64_t rows;
+    uint32_t spin_limit;
+    int test_skip_load;
+};
+int units_most();                           // units that run at a time: pairs of SMs
+cudaError_t prepare_gated();
+cudaError_t launch_gated(const GatedShape &s, const GatedCall &c, const GatedWork &w, int mode, cudaStream_t st);
+// rows of a 16-bit matrix to rows `to_row` apart, zeros behind them
+cudaError_t launch_gated_pack(const void *x, int64_t rows, int cols, int64_t row, void *to, int64_t to_row, int dtype, cudaStream_t st);
+// dgu from gu [rows][2 F] and dh
+cudaError_t launch_gated_slopes(const GatedShape &s, const void *gu, const void *dh, void *dgu, int64_t rows, cudaStream_t st);
+
 }  // namespace patdnn

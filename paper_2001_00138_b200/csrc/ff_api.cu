@@ -1,4 +1,4 @@
-// C entry points of the RMS norm, the 8-bit matrices and the linear layer with 8-bit weights (declared in include/patdnn.h).
+// C entry points of the RMS norm, the 8-bit matrices, the linear layer with 8-bit weights and the gated block (declared in include/patdnn.h).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -38,6 +38,24 @@ struct patdnn_linear8_s {
         cudaFree(x);
         cudaFree(bias);
         cudaFree(status);
+    }
+};
+
+struct patdnn_gated_s {
+    GatedShape s{};
+    GatedWork w{};
+    int64_t max_rows = 0;
+    int device = -1;
+    void *x = nullptr, *weights = nullptr;  // packed rows, where theirs cannot be copied as they lie
+    uint32_t spin_limit = 0;                // patdnn_gated_debug_wait
+    int test_skip_load = 0;
+    ~patdnn_gated_s() {
+        cudaFree(w.dgu);
+        cudaFree(w.partial);
+        cudaFree(w.arrivals);
+        cudaFree(w.status);
+        cudaFree(x);
+        cudaFree(weights);
     }
 };
 
@@ -110,6 +128,36 @@ int rms_forward(patdnn_rms h, const void *x, const void *residual, const float *
     c.x = x; c.residual = residual; c.gamma = gamma; c.sum = sum; c.rstd = rstd; c.rows = rows;
     (mx ? c.mx : c.y) = out;
     return launched(launch_rms_norm(s, c, st), 1, "RMS norm launch");
+}
+
+// The gated block's tiles: 256 rows by 128 outputs, or 256 columns.
+bool gated_too_large(int64_t rows, int64_t F, int64_t K) {
+    return ceil_div(rows, 256) * ceil_div(std::max(F, K), 128) > INT32_MAX / 8 || 2 * ceil_div(F, 256) * ceil_div(K, 256) > INT32_MAX / 8;
+}
+bool copies_as_it_lies(int64_t row) { return row % 8 == 0; }           // rows of whole 16-byte units
+bool operand_aligned(const void *p, int64_t row) { return aligned(p, copies_as_it_lies(row) ? 16 : 2); }
+int64_t packed_row(int64_t K) { return (K + 7) / 8 * 8; }
+
+// x and the weights of a call as the products read them: packed first, where they cannot be copied as they lie.
+int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu, int64_t rows, GatedCall &c, cudaStream_t st) {
+    const GatedShape &s = h->s;
+    c.x = x; c.wg = wg; c.wu = wu; c.x_row = s.x_row; c.w_row = s.w_row; c.rows = rows;
+    c.spin_limit = h->spin_limit; c.test_skip_load = h->test_skip_load;
+    const int64_t row = packed_row(s.K);
+    if (h->x) {
+        if (const int rc = launched(launch_gated_pack(x, rows, s.K, s.x_row, h->x, row, s.dtype, st), 1, "packing launch")) return rc;
+        c.x = h->x;
+        c.x_row = row;
+    }
+    if (h->weights) {
+        void *second = static_cast<uint16_t *>(h->weights) + s.F * row;
+        if (const int rc = launched(launch_gated_pack(wg, s.F, s.K, s.w_row, h->weights, row, s.dtype, st), 1, "packing launch")) return rc;
+        if (const int rc = launched(launch_gated_pack(wu, s.F, s.K, s.w_row, second, row, s.dtype, st), 1, "packing launch")) return rc;
+        c.wg = h->weights;
+        c.wu = second;
+        c.w_row = row;
+    }
+    return PATDNN_OK;
 }
 
 }  // namespace
@@ -293,6 +341,127 @@ int patdnn_linear8_debug_wait(patdnn_linear8 h, uint32_t polls, int32_t skip_loa
 }
 
 int patdnn_linear8_free(patdnn_linear8 h) {
+    delete h;
+    return PATDNN_OK;
+}
+
+int patdnn_gated_create(const patdnn_gated_desc *desc, patdnn_gated *out) {
+    if (!desc || !out) return PATDNN_E_NULL;
+    if ((desc->dtype != PATDNN_F16 && desc->dtype != PATDNN_BF16) || !known_act(desc->act)) return PATDNN_E_DTYPE;
+    if (!size_ok(desc->F, desc->K) || desc->F < 1 || desc->F > kMostColumns || !size_ok(desc->max_rows, desc->K) || !size_ok(desc->max_rows, desc->F) ||
+        gated_too_large(desc->max_rows, desc->F, desc->K))
+        return PATDNN_E_SHAPE;
+    GatedShape s{};
+    s.F = desc->F; s.K = desc->K; s.act = desc->act; s.dtype = desc->dtype;
+    s.x_row = desc->x_row ? desc->x_row : s.K;
+    s.w_row = desc->w_row ? desc->w_row : s.K;
+    s.h_row = desc->h_row ? desc->h_row : s.F;
+    for (int64_t row : {s.x_row, s.w_row, s.h_row})
+        if (row > (int64_t(1) << 31)) return PATDNN_E_SHAPE;
+    if (s.x_row < s.K || s.w_row < s.K || s.h_row < s.F) return PATDNN_E_SHAPE;
+    patdnn_gated h = new (std::nothrow) patdnn_gated_s();
+    if (!h) return PATDNN_E_ALLOC;
+    h->s = s;
+    h->max_rows = desc->max_rows;
+    const size_t counters = static_cast<size_t>(units_most()) * kGatedCounters, row = static_cast<size_t>(packed_row(s.K));
+    uint16_t *dgu = nullptr, *x = nullptr, *weights = nullptr;
+    cudaError_t e = cudaGetDevice(&h->device);
+    if (e == cudaSuccess) e = allocate(&h->w.partial, static_cast<size_t>(units_most()) * kGatedUnitFloats);
+    if (e == cudaSuccess) e = allocate(&h->w.arrivals, counters);
+    if (e == cudaSuccess) e = cudaMemset(h->w.arrivals, 0, counters * sizeof(unsigned));
+    if (e == cudaSuccess) e = allocate(&h->w.status, 4);
+    if (e == cudaSuccess) e = cudaMemset(h->w.status, 0, 16);
+    if (e == cudaSuccess && desc->grad) e = allocate(&dgu, static_cast<size_t>(desc->max_rows) * 2 * gated_padded(s.F));
+    h->w.dgu = dgu;
+    if (e == cudaSuccess && !copies_as_it_lies(s.x_row)) e = allocate(&x, static_cast<size_t>(desc->max_rows) * row);
+    h->x = x;
+    if (e == cudaSuccess && !copies_as_it_lies(s.w_row)) e = allocate(&weights, 2 * static_cast<size_t>(s.F) * row);
+    h->weights = weights;
+    if (e == cudaSuccess) e = prepare_gated();
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();                  // the counters are zero on every stream from here on
+    if (e != cudaSuccess) return failed(h, e, "patdnn_gated_create");
+    *out = h;
+    return PATDNN_OK;
+}
+
+int patdnn_gated_run(patdnn_gated h, const void *x, const void *wg, const void *wu, void *hidden, void *gu, int64_t rows, void *stream) {
+    if (!h) return PATDNN_E_NULL;
+    const GatedShape &s = h->s;
+    if (rows < 0 || rows > h->max_rows || !operand_aligned(x, s.x_row) || !operand_aligned(wg, s.w_row) || !operand_aligned(wu, s.w_row) ||
+        !aligned(hidden, 2) || !aligned(gu, 2))
+        return PATDNN_E_SHAPE;
+    if (rows == 0) return PATDNN_OK;
+    if (!x || !wg || !wu || !hidden) return PATDNN_E_NULL;
+    if (const int rc = on_device(h->device)) return rc;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    GatedCall c{};
+    if (const int rc = gated_operands(h, x, wg, wu, rows, c, st)) return rc;
+    c.h = hidden; c.gu = gu;
+    return launched(launch_gated(s, c, h->w, kGatedForward, st), 1, "gated block launch");
+}
+
+int patdnn_gated_grad(patdnn_gated h, const void *x, const void *wg, const void *wu, const void *gu, const void *dh, void *dx, void *dwg, void *dwu,
+                      int64_t rows, void *stream) {
+    if (!h) return PATDNN_E_NULL;
+    if (!h->w.dgu) return PATDNN_E_SCRATCH;
+    const GatedShape &s = h->s;
+    if (rows < 0 || rows > h->max_rows || !operand_aligned(x, s.x_row) || !operand_aligned(wg, s.w_row) || !operand_aligned(wu, s.w_row) ||
+        !aligned(gu, 2) || !aligned(dh, 2) || !aligned(dx, 2) || !aligned(dwg, 2) || !aligned(dwu, 2))
+        return PATDNN_E_SHAPE;
+    if (!dwg != !dwu) return PATDNN_E_NULL;
+    if (rows > 0 && (!x || !wg || !wu || !gu || !dh)) return PATDNN_E_NULL;
+    if (const int rc = on_device(h->device)) return rc;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (rows == 0) {
+        for (void *w : {dwg, dwu})
+            if (w) CU(cudaMemset2DAsync(w, static_cast<size_t>(s.w_row) * 2, 0, static_cast<size_t>(s.K) * 2, s.F, st));
+        return PATDNN_OK;
+    }
+    if (!dx && !dwg) return PATDNN_OK;
+    GatedCall c{};
+    if (const int rc = gated_operands(h, x, wg, wu, rows, c, st)) return rc;
+    c.dx = dx; c.dwg = dwg; c.dwu = dwu;
+    if (const int rc = launched(launch_gated_slopes(s, gu, dh, h->w.dgu, rows, st), 1, "gated block gradient launch")) return rc;
+    if (dx)
+        if (const int rc = launched(launch_gated(s, c, h->w, kGatedInput, st), 1, "gated block gradient launch")) return rc;
+    return dwg ? launched(launch_gated(s, c, h->w, kGatedWeights, st), 1, "gated block gradient launch") : PATDNN_OK;
+}
+
+int patdnn_gated_plan(int32_t F, int32_t K, int64_t rows, int32_t product, patdnn_gated_plan_info *info) {
+    if (!info) return PATDNN_E_NULL;
+    if (!size_ok(F, K) || F < 1 || F > kMostColumns || !size_ok(rows, K) || !size_ok(rows, F) || rows < 1 || gated_too_large(rows, F, K) || product < 0 ||
+        product > 2)
+        return PATDNN_E_SHAPE;
+    const GatedPlan p = plan_gated(F, K, rows, product);
+    *info = patdnn_gated_plan_info{};
+    info->row_tiles = p.m_tiles; info->column_tiles = p.n_tiles; info->blocks = p.k_blocks; info->splits = p.splits; info->blocks_per_split = p.per_split;
+    info->grid = p.grid; info->stages = p.stages; info->smem_bytes = p.smem;
+    return PATDNN_OK;
+}
+
+int patdnn_gated_check(patdnn_gated h) {
+    if (!h) return PATDNN_E_NULL;
+    if (const int rc = on_device(h->device)) return rc;
+    CU(cudaDeviceSynchronize());
+    int word = 0;
+    CU(cudaMemcpy(&word, h->w.status, sizeof(int), cudaMemcpyDeviceToHost));
+    if (!word) return PATDNN_OK;
+    // what was given up may have left partial sums uncounted
+    CU(cudaMemset(h->w.arrivals, 0, sizeof(unsigned) * units_most() * kGatedCounters));
+    CU(cudaMemset(h->w.status, 0, sizeof(int)));
+    CU(cudaDeviceSynchronize());
+    return PATDNN_E_DEVICE_TIMEOUT;
+}
+
+int patdnn_gated_debug_wait(patdnn_gated h, uint32_t polls, int32_t skip_load_iteration) {
+    if (!h) return PATDNN_E_NULL;
+    if (skip_load_iteration < 0) return PATDNN_E_SHAPE;
+    h->spin_limit = polls;
+    h->test_skip_load = skip_load_iteration;
+    return PATDNN_OK;
+}
+
+int patdnn_gated_free(patdnn_gated h) {
     delete h;
     return PATDNN_OK;
 }

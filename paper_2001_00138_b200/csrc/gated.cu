@@ -1,0 +1,407 @@
+// Products of the gated feed-forward block on the tensor cores, 16-bit operands, fp32 sums in tensor memory:
+//
+//   forward   h = act(x wg^T) * (x wu^T)        a tile of 128 outputs takes both projections, and the epilogue multiplies them
+//   input     dx = dg wg + du wu                one sum over both: dg and du lie side by side, the weights' tiles change half way
+//   weights   dwg = dg^T x, dwu = du^T x        a tile of either
+//
+// Pairs of CTAs (cta_group::2) work on tiles of 256 rows x 256 columns: each CTA copies its 128 rows of A and 128 of the 256 rows of B, 32 KB
+// per 64 of the summed dimension, for 512 cycles of MMAs.  Forward operands have the summed dimension innermost (K-major); where it is the
+// outer one (wg and wu for dx; dg, du and x for dwg, dwu) the MMAs read the tiles as they lie, transposed (MN-major), so nothing is ever
+// transposed in memory.  Persistent: warp 0 copies, warp 1 of the pair's first CTA multiplies, warps 4 to 11 drain one accumulator (two, of
+// 256 columns each, fill tensor memory) while the other one is summed.
+// Few tiles: the summed dimension is cut into ranges, and the last of a tile's warps to arrive adds the partial sums in the ranges' order
+// (nobody waits, and the same call gives the same bits).
+#include <algorithm>
+
+#include "feed_forward.hpp"
+#include "linear_device.cuh"
+
+namespace patdnn {
+namespace {
+
+constexpr int kThreads = 384;
+constexpr int kEpilogueWarps = 8;
+constexpr int kMostStages = 6;
+constexpr int kHalf = 128 * 128;                       // bytes of one CTA's part of an operand in a stage: 128 rows x 64 columns
+constexpr int kStage = 2 * kHalf;
+constexpr int kPiece = 64;                             // bytes of a row that the epilogue stores at a time
+constexpr int kStaging = 32 * kPiece;                  // shared memory of an epilogue warp
+constexpr int kSmem = 226 * 1024;                      // all of an SM's: a pair holds all of two SMs' tensor memory (see plan_mx4_linear)
+
+struct GatedParams {
+    void *out0, *out1, *gu;                            // h, nullptr | dx, nullptr | dwg, dwu
+    int64_t rows, ld;                                  // rows of the output (of either); its stride
+    int cols;                                          // columns of the output
+    int m_tiles, n_tiles, k_blocks, splits, per_split, stages;
+    int f_blocks;                                      // input: blocks of 64 of the gate's part; weights: 256-row tiles of it
+    int f_padded;                                      // columns from dg to du
+    float *partial;
+    unsigned *arrivals;
+    int *status;
+    uint32_t spin_limit;
+    int test_skip_load;
+};
+
+__device__ __forceinline__ uint32_t cta_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t in_cta(uint32_t local, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(local), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void pair_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void expect_pair(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void arrive_pair(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
+}
+// An operand part of 128 x 64 elements.  K-major: 128 rows of 128 bytes, groups of 8 rows 1024 bytes apart, K = 16 is 32 bytes further on.
+// MN-major: two chunks of 64 columns, 64 rows (the summed dimension) of 128 bytes each, 8192 bytes apart; K = 16 is 16 rows further on.
+template <bool KMAJOR> __device__ __forceinline__ uint64_t part_desc(uint32_t addr) {
+    constexpr uint64_t leading = KMAJOR ? 1 : 8192 >> 4;
+    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (leading << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
+}
+template <bool KMAJOR> constexpr uint64_t kNextK = KMAJOR ? 2 : 2048 >> 4;
+
+template <int MODE, typename T, int ACT>
+__global__ void __launch_bounds__(kThreads, 1)
+gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1, const GatedParams p) {
+    constexpr bool A_K = MODE != kGatedWeights, B_K = MODE == kGatedForward;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ __align__(8) unsigned long long bars[2 * kMostStages + 4];
+    __shared__ uint32_t tmem_slot;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const uint32_t rank = cta_rank();
+    const WaitCtx ctx{p.status, p.spin_limit ? p.spin_limit : kSpinLimit};
+    const uint32_t smem = (smem_u32(smem_raw) + 1023) & ~1023u;
+    // full: in the first CTA, an arrival with its bytes from each CTA; empty, done: one per CTA, told by the first CTA's MMAs; drained: in the first CTA
+    const uint32_t full = smem_u32(bars), empty = full + 8 * kMostStages, done = empty + 8 * kMostStages, drained = done + 16;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(full + 8 * s, 2);
+            mbar_init(empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(done + 8 * b, 1);
+            mbar_init(drained + 8 * b, 2 * kEpilogueWarps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) tmem_allocate_pair(&tmem_slot, 512);
+    tc_fence_before();
+    __syncthreads();
+    pair_barrier();                                    // both CTAs' barriers exist, and their tensor memory
+    tc_fence_after();
+    pdl_trigger();                                     // not before the allocation: see kernels.hpp
+    const uint32_t tmem = tmem_slot;
+    pdl_wait();
+
+    const int units = p.m_tiles * p.n_tiles * p.splits, first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    if (warp == 0) {
+        const bool leader = elect_one();
+        const uint32_t full0 = in_cta(full, 0);
+        int slot = 0, issued = 0;
+        uint32_t phase = 1;                            // (the first pass over the ring does not wait)
+        bool ok = true;
+        for (int u = first; ok && u < units; u += step) {
+            const int tile = u / p.splits, k0 = (u - tile * p.splits) * p.per_split, k1 = min(p.k_blocks, k0 + p.per_split);
+            const int nt = tile / p.m_tiles, mt = tile - nt * p.m_tiles;
+            for (int k = k0; k < k1; ++k) {
+                if (issued >= p.stages && !warp_wait(empty + 8 * slot, phase, ctx, 121)) { ok = false; break; }
+                if (leader && issued + 1 != p.test_skip_load) {
+                    const uint32_t bar = full0 + 8 * slot, a = smem + slot * kStage, b = a + kHalf;
+                    expect_pair(bar, kStage);
+                    if constexpr (MODE == kGatedForward) {             // this CTA: 128 rows of x, and the gate's or the up projection's weights
+                        tile_load(a, &map_a, bar, k * 64, mt * 256 + rank * 128);
+                        tile_load(b, rank == 0 ? &map_b0 : &map_b1, bar, k * 64, nt * 128);
+                    } else if constexpr (MODE == kGatedInput) {
+                        const bool up = k >= p.f_blocks;
+                        const CUtensorMap *map = up ? &map_b1 : &map_b0;
+                        const int f = (up ? k - p.f_blocks : k) * 64, n = nt * 256 + rank * 128;
+                        tile_load(a, &map_a, bar, k * 64, mt * 256 + rank * 128);
+                        tile_load(b, map, bar, n, f);
+                        tile_load(b + kHalf / 2, map, bar, n + 64, f);
+                    } else {
+                        const int up = mt >= p.f_blocks;
+                        const int f = up * p.f_padded + (mt - up * p.f_blocks) * 256 + rank * 128, n = nt * 256 + rank * 128;
+                        tile_load(a, &map_a, bar, f, k * 64);
+                        tile_load(a + kHalf / 2, &map_a, bar, f + 64, k * 64);
+                        tile_load(b, &map_b0, bar, n, k * 64);
+                        tile_load(b + kHalf / 2, &map_b0, bar, n + 64, k * 64);
+                    }
+                }
+                ++issued;
+                if (++slot == p.stages) { slot = 0; phase ^= 1; }
+            }
+        }
+        // no copy of either CTA may still be in flight when the pair ends, whatever happened to the other roles
+        if (rank == 0)
+            for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait(full + 8 * (i % p.stages), (i / p.stages) & 1, ctx, 122);
+    } else if (warp == 1 && rank == 0) {
+        const bool leader = elect_one();
+        constexpr uint32_t idesc = (1u << 4) | (std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u) | (A_K ? 0u : 1u << 15) |
+                                   (B_K ? 0u : 1u << 16) | (uint32_t(256 >> 3) << 17) | (uint32_t(256 >> 4) << 24);
+        const uint32_t peer_empty = in_cta(empty, 1), peer_done = in_cta(done, 1), own_empty = in_cta(empty, 0), own_done = in_cta(done, 0);
+        const uint64_t da0 = part_desc<A_K>(smem), db0 = part_desc<B_K>(smem + kHalf);
+        int slot = 0, t = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int u = first; ok && u < units; u += step, ++t) {
+            const int split = u % p.splits, k0 = split * p.per_split, k1 = min(p.k_blocks, k0 + p.per_split);
+            const int buf = t & 1;
+            if (t > 1 && !warp_wait(drained + 8 * buf, ((t >> 1) - 1) & 1, ctx, 123)) break;
+            tc_fence_after();
+            uint32_t accumulate = 0;
+            for (int k = k0; k < k1; ++k) {
+                if (!warp_wait(full + 8 * slot, phase, ctx, 124)) { ok = false; break; }
+                tc_fence_after();
+                if (leader) {
+                    const uint64_t shift = static_cast<uint64_t>(slot) * (kStage >> 4);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        mma_pair(tmem + buf * 256, da0 + shift + j * kNextK<A_K>, db0 + shift + j * kNextK<B_K>, idesc, accumulate | j);
+                    commit_pair(own_empty + 8 * slot);
+                    commit_pair(peer_empty + 8 * slot);
+                }
+                __syncwarp();
+                accumulate = 1;
+                if (++slot == p.stages) { slot = 0; phase ^= 1; }
+            }
+            if (leader && ok) {
+                commit_pair(own_done + 8 * buf);
+                commit_pair(peer_done + 8 * buf);
+            }
+            __syncwarp();
+        }
+        // no MMA may still run when tensor memory is freed
+        const int last = t - 1;
+        if (leader && !ok) commit_pair(own_done + 8 * (last & 1));
+        __syncwarp();
+        if (last >= 0) mbar_wait(done + 8 * (last & 1), (last >> 1) & 1, ctx, 125);
+    } else if (warp >= 4) {
+        const int e = warp - 4, quadrant = e & 3, half = e >> 2;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(quadrant * 32) << 16);
+        const uint32_t drained0 = in_cta(drained, 0);
+        unsigned char *stage = smem_raw + (smem - smem_u32(smem_raw)) + p.stages * kStage + e * kStaging;
+        int t = 0;
+        for (int u = first; u < units; u += step, ++t) {
+            const int tile = u / p.splits, buf = t & 1;
+            const int nt = tile / p.m_tiles;
+            int mt = tile - nt * p.m_tiles;
+            if (!mbar_wait(done + 8 * buf, (t >> 1) & 1, ctx, 126)) break;
+            tc_fence_after();
+            T *out = static_cast<T *>(p.out0);
+            if constexpr (MODE == kGatedWeights) {
+                if (mt >= p.f_blocks) {
+                    mt -= p.f_blocks;
+                    out = static_cast<T *>(p.out1);
+                }
+            }
+            const int64_t row0 = static_cast<int64_t>(mt) * 256 + rank * 128 + quadrant * 32;
+            const int rows_left = static_cast<int>(max(static_cast<int64_t>(-1), min(static_cast<int64_t>(32), p.rows - row0)));
+            // chunk j of the warp, 32 columns of the accumulator: forward gate, up, gate, up of its 64 outputs
+            auto column = [&](int j) { return MODE == kGatedForward ? (j & 1) * 128 + half * 64 + (j >> 1) * 32 : half * 128 + j * 32; };
+            const float *parts = nullptr;
+            bool mine = true;
+            if (p.splits > 1) {
+                constexpr int kWarpFloats = 4 * 32 * 32;
+                const int64_t unit_floats = kGatedUnitFloats, place = (static_cast<int64_t>(rank) * kEpilogueWarps + e) * kWarpFloats;
+                float *to = p.partial + u * unit_floats + place;
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t v[32];
+                    tmem_ld32(lanes + buf * 256 + column(j), v);
+                    if (lane < rows_left) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) to[(j * 32 + i) * 32 + lane] = __uint_as_float(v[i]);
+                    }
+                }
+                __threadfence();
+                __syncwarp();
+                unsigned before = 0;
+                unsigned *counter = p.arrivals + static_cast<int64_t>(tile) * kGatedCounters + rank * kEpilogueWarps + e;
+                if (lane == 0) before = atomicAdd(counter, 1u);
+                before = __shfl_sync(0xffffffffu, before, 0);
+                mine = before + 1 == static_cast<unsigned>(p.splits);
+                if (mine) {
+                    if (lane == 0) *counter = 0;
+                    __threadfence();
+                    parts = p.partial + static_cast<int64_t>(tile) * p.splits * unit_floats + place;
+                }
+            }
+            auto fetch = [&](int j, float (&v)[32]) {
+                if (p.splits == 1) {
+                    uint32_t w[32];
+                    tmem_ld32(lanes + buf * 256 + column(j), w);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(w[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = 0.f;
+                    if (lane < rows_left)
+                        for (int s = 0; s < p.splits; ++s) {
+                            const float *from = parts + static_cast<int64_t>(s) * kGatedUnitFloats + j * 1024 + lane;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] += __ldcg(from + i * 32);
+                        }
+                }
+            };
+            auto put = [&](const float (&v)[32], T *base, int64_t ld, int col, int left) {
+                const uint64_t places = reinterpret_cast<uintptr_t>(base) | static_cast<uint64_t>(ld * sizeof(T));
+                const int aligned = places % 16 == 0 ? 16 : places % 4 == 0 ? 4 : 2;
+                store_piece<T, kPiece>(v, stage, base + row0 * ld + col, ld, rows_left, left, aligned);
+            };
+            if (mine && rows_left > 0) {
+                if constexpr (MODE == kGatedForward) {
+                    for (int c = 0; c < 2; ++c) {
+                        const int f = nt * 128 + half * 64 + c * 32;
+                        if (f >= p.cols) break;
+                        float g[32], up[32];
+                        fetch(2 * c, g);
+                        fetch(2 * c + 1, up);
+                        if (p.gu) {
+                            T *gu = static_cast<T *>(p.gu);
+                            put(g, gu, 2 * static_cast<int64_t>(p.cols), f, p.cols - f);
+                            put(up, gu + p.cols, 2 * static_cast<int64_t>(p.cols), f, p.cols - f);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) g[i] = activate1<ACT>(g[i]) * up[i];
+                        put(g, out, p.ld, f, p.cols - f);
+                    }
+                } else {
+                    for (int j = 0; j < 4; ++j) {
+                        const int n = nt * 256 + half * 128 + j * 32;
+                        if (n >= p.cols) break;
+                        float v[32];
+                        fetch(j, v);
+                        put(v, out, p.ld, n, p.cols - n);
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_pair(drained0 + 8 * buf);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    pair_barrier();                                    // nobody's shared or tensor memory goes away under its peer
+    if (warp == 2) tmem_free_pair(tmem, 512);
+}
+
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+    static const EncodeTiled fn = [] {
+        void *sym = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        const bool ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &found) == cudaSuccess && found == cudaDriverEntryPointSuccess;
+        return ok ? reinterpret_cast<EncodeTiled>(sym) : nullptr;
+    }();
+    return fn;
+}
+// A matrix of `rows` rows and `cols` columns, `row` elements apart (a multiple of 8), read in boxes of 64 columns and `box` rows; zeros outside.
+cudaError_t make_map(CUtensorMap *map, int dtype, const void *base, int64_t rows, int64_t cols, int64_t row, int box) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(row) * 2};
+    const cuuint32_t boxes[2] = {64, static_cast<cuuint32_t>(box)}, ones[2] = {1, 1};
+    const CUresult r = encode(map, dtype == PATDNN_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims,
+                              strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+// f(T{}, std::integral_constant<int, ACT>): the gradients' products have no activation
+template <typename F> cudaError_t by_kernel(int mode, int dtype, int act, F f) {
+    auto go = [&](auto t) {
+        using T = decltype(t);
+        if (mode == kGatedInput) return f(gated_kernel<kGatedInput, T, PATDNN_ACT_NONE>);
+        if (mode == kGatedWeights) return f(gated_kernel<kGatedWeights, T, PATDNN_ACT_NONE>);
+        return by_act(act, [&](auto a) { return f(gated_kernel<kGatedForward, T, a.value>); });
+    };
+    return dtype == PATDNN_F16 ? go(__half{}) : go(__nv_bfloat16{});
+}
+
+}  // namespace
+
+int units_most() { return std::max(1, sm_count() / 2); }
+
+GatedPlan plan_gated(int F, int K, int64_t rows, int mode) {
+    GatedPlan p{};
+    const int64_t m = mode == kGatedWeights ? 2 * ceil_div(F, 256) : ceil_div(rows, 256);
+    p.m_tiles = static_cast<int>(m);
+    p.n_tiles = static_cast<int>(mode == kGatedForward ? ceil_div(F, 128) : ceil_div(K, 256));
+    p.k_blocks = static_cast<int>(mode == kGatedForward ? ceil_div(K, 64) : mode == kGatedInput ? 2 * ceil_div(F, 64) : ceil_div(rows, 64));
+    const int64_t tiles = m * p.n_tiles, most = units_most();
+    // Tiles for half the pairs of SMs or fewer: ranges of at least four blocks share a tile.
+    p.splits = 1;
+    if (tiles * 2 <= most) p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most / tiles, p.k_blocks / 4)));
+    p.per_split = static_cast<int>(ceil_div(p.k_blocks, p.splits));
+    p.splits = static_cast<int>(ceil_div(p.k_blocks, p.per_split));
+    p.grid = 2 * static_cast<int>(std::min(tiles * p.splits, most));
+    p.stages = kMostStages;
+    p.smem = kSmem;
+    return p;
+}
+
+cudaError_t prepare_gated() {
+    for (int dtype : {PATDNN_F16, PATDNN_BF16})
+        for (int mode : {kGatedForward, kGatedInput, kGatedWeights})
+            for (int act : {PATDNN_ACT_NONE, PATDNN_ACT_RELU, PATDNN_ACT_SILU}) {
+                const cudaError_t e = by_kernel(mode, dtype, act, [](auto kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
+                if (e != cudaSuccess) return e;
+            }
+    return cudaSuccess;
+}
+
+cudaError_t launch_gated(const GatedShape &s, const GatedCall &c, const GatedWork &w, int mode, cudaStream_t st) {
+    const GatedPlan plan = plan_gated(s.F, s.K, c.rows, mode);
+    const int padded = gated_padded(s.F);
+    GatedParams p{};
+    p.m_tiles = plan.m_tiles; p.n_tiles = plan.n_tiles; p.k_blocks = plan.k_blocks; p.splits = plan.splits; p.per_split = plan.per_split; p.stages = plan.stages;
+    p.partial = w.partial; p.arrivals = w.arrivals; p.status = w.status; p.spin_limit = c.spin_limit; p.test_skip_load = c.test_skip_load;
+    CUtensorMap a, b0, b1;
+    cudaError_t e;
+    if (mode == kGatedForward) {
+        p.out0 = c.h; p.gu = c.gu; p.rows = c.rows; p.ld = s.h_row; p.cols = s.F;
+        e = make_map(&a, s.dtype, c.x, c.rows, s.K, c.x_row, 128);
+        if (e == cudaSuccess) e = make_map(&b0, s.dtype, c.wg, s.F, s.K, c.w_row, 128);
+        if (e == cudaSuccess) e = make_map(&b1, s.dtype, c.wu, s.F, s.K, c.w_row, 128);
+    } else if (mode == kGatedInput) {
+        p.out0 = c.dx; p.rows = c.rows; p.ld = s.x_row; p.cols = s.K; p.f_blocks = padded / 64;
+        e = make_map(&a, s.dtype, w.dgu, c.rows, 2 * static_cast<int64_t>(padded), 2 * static_cast<int64_t>(padded), 128);
+        if (e == cudaSuccess) e = make_map(&b0, s.dtype, c.wg, s.F, s.K, c.w_row, 64);
+        if (e == cudaSuccess) e = make_map(&b1, s.dtype, c.wu, s.F, s.K, c.w_row, 64);
+    } else {
+        p.out0 = c.dwg; p.out1 = c.dwu; p.rows = s.F; p.ld = s.w_row; p.cols = s.K; p.f_blocks = plan.m_tiles / 2; p.f_padded = padded;
+        e = make_map(&a, s.dtype, w.dgu, c.rows, 2 * static_cast<int64_t>(padded), 2 * static_cast<int64_t>(padded), 64);
+        if (e == cudaSuccess) e = make_map(&b0, s.dtype, c.x, c.rows, s.K, c.x_row, 64);
+        b1 = b0;
+    }
+    if (e != cudaSuccess) return e;
+    return by_kernel(mode, s.dtype, s.act, [&](auto kernel) { return launch_pdl(kernel, dim3(plan.grid), dim3(kThreads), plan.smem, st, 2, a, b0, b1, p); });
+}
+
+}  // namespace patdnn

@@ -38,6 +38,14 @@ __device__ __forceinline__ void tmem_allocate(uint32_t *slot, uint32_t columns) 
 __device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns) {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns));
 }
+// The same for the two CTAs of a pair, each of which calls it.
+__device__ __forceinline__ void tmem_allocate_pair(uint32_t *slot, uint32_t columns) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free_pair(uint32_t tmem, uint32_t columns) {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+}
 // 32 rows of 16 bytes, not swizzled: 8-row groups 128 bytes apart.
 __device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
     return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (uint64_t(1) << 16) | (uint64_t(128 >> 4) << 32) | (uint64_t(1) << 46);

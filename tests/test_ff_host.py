@@ -118,3 +118,25 @@ def test_dependents_start_after_the_allocation(name, body):
     barrier = body.index("__syncthreads()", body.index("tmem_allocate"))
     assert len(triggers) == 1 and triggers[0] > barrier
     assert len(re.findall(r"\btmem_allocate\w*\(", body)) == 1 and len(re.findall(r"\btmem_free\w*\(", body)) == 1
+
+
+@pytest.mark.parametrize("status, kw", [(E_SHAPE, dict(F=0)), (E_SHAPE, dict(K=0)), (E_SHAPE, dict(max_rows=-1)), (E_SHAPE, dict(max_rows=2 ** 31)),
+                                        (E_SHAPE, dict(x_row=63)), (E_SHAPE, dict(w_row=-64)), (E_SHAPE, dict(h_row=31)), (E_SHAPE, dict(h_row=2 ** 31 + 1)),
+                                        (E_SHAPE, dict(K=2 ** 21)), (E_SHAPE, dict(F=2 ** 21)), (E_DTYPE, dict(dtype=B.F32)), (E_DTYPE, dict(dtype=5)),
+                                        (E_DTYPE, dict(act=9))])
+def test_gated_refusals(status, kw):
+    refused(status, B.Gated, **(dict(F=32, K=64, max_rows=4) | kw))
+
+
+def test_gated_plans():
+    for F, K in ((1, 1), (64, 64), (130, 1000), (1333, 1000), (8192, 4096), (40000, 16384)):
+        for rows in (1, 8, 100, 256, 300, 777, 5000, 100000):
+            for product in range(3):
+                p = B.gated_plan(F, K, rows, product)
+                assert p["splits"] * p["blocks_per_split"] >= p["blocks"] > (p["splits"] - 1) * p["blocks_per_split"], p      # no range is empty
+                tiles = p["row_tiles"] * p["column_tiles"]
+                assert p["splits"] == 1 or tiles * p["splits"] <= 74, p        # a unit of partial sums each, of 74
+                assert 2 <= p["grid"] <= 148 and p["grid"] % 2 == 0
+    for args in ((0, 32, 1), (32, 0, 1), (32, 32, 0), (32, 2 ** 21, 1), (2 ** 21, 32, 1), (2 ** 20, 1, 2 ** 31 - 1)):
+        refused(E_SHAPE, B.gated_plan, *args)
+    refused(E_SHAPE, B.gated_plan, 32, 32, 1, 3)
