@@ -42,32 +42,6 @@ struct GatedParams {
     int test_skip_load;
 };
 
-__device__ __forceinline__ uint32_t cta_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t in_cta(uint32_t local, uint32_t rank) {
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(local), "r"(rank));
-    return a;
-}
-__device__ __forceinline__ void pair_barrier() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void expect_pair(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void arrive_pair(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1) {
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
-}
-__device__ __forceinline__ void commit_pair(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
 __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -94,12 +68,12 @@ gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const uint32_t rank = cta_rank();
     const WaitCtx ctx{p.status, p.spin_limit ? p.spin_limit : kSpinLimit};
     const uint32_t smem = (smem_u32(smem_raw) + 1023) & ~1023u;
-    // full: in the first CTA, an arrival with its bytes from each CTA; empty, done: one per CTA, told by the first CTA's MMAs; drained: in the first CTA
+    // full: in the first CTA, which expects the bytes of both (the second one's may come first: a phase ends with the arrival); empty, done: one per CTA, told by the first CTA's MMAs; drained: in the first CTA
     const uint32_t full = smem_u32(bars), empty = full + 8 * kMostStages, done = empty + 8 * kMostStages, drained = done + 16;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
-            mbar_init(full + 8 * s, 2);
+            mbar_init(full + 8 * s, 1);
             mbar_init(empty + 8 * s, 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -131,7 +105,7 @@ gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 if (issued >= p.stages && !warp_wait(empty + 8 * slot, phase, ctx, 121)) { ok = false; break; }
                 if (leader && issued + 1 != p.test_skip_load) {
                     const uint32_t bar = full0 + 8 * slot, a = smem + slot * kStage, b = a + kHalf;
-                    expect_pair(bar, kStage);
+                    if (rank == 0) mbar_expect_tx(full + 8 * slot, 2 * kStage);
                     if constexpr (MODE == kGatedForward) {             // this CTA: 128 rows of x, and the gate's or the up projection's weights
                         tile_load(a, &map_a, bar, k * 64, mt * 256 + rank * 128);
                         tile_load(b, rank == 0 ? &map_b0 : &map_b1, bar, k * 64, nt * 128);
@@ -310,27 +284,10 @@ gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     if (warp == 2) tmem_free_pair(tmem, 512);
 }
 
-typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiled encode_tiled() {
-    static const EncodeTiled fn = [] {
-        void *sym = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        const bool ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &found) == cudaSuccess && found == cudaDriverEntryPointSuccess;
-        return ok ? reinterpret_cast<EncodeTiled>(sym) : nullptr;
-    }();
-    return fn;
-}
 // A matrix of `rows` rows and `cols` columns, `row` elements apart (a multiple of 8), read in boxes of 64 columns and `box` rows; zeros outside.
 cudaError_t make_map(CUtensorMap *map, int dtype, const void *base, int64_t rows, int64_t cols, int64_t row, int box) {
-    const EncodeTiled encode = encode_tiled();
-    if (!encode) return cudaErrorNotSupported;
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(row) * 2};
-    const cuuint32_t boxes[2] = {64, static_cast<cuuint32_t>(box)}, ones[2] = {1, 1};
-    const CUresult r = encode(map, dtype == PATDNN_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims,
-                              strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+    return encode_map(map, dtype == PATDNN_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, cols, rows, row * 2, 64, box,
+                      CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 // f(T{}, std::integral_constant<int, ACT>): the gradients' products have no activation

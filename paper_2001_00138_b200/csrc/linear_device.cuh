@@ -1,6 +1,8 @@
 // Device and host pieces that the linear layers share: warp-uniform roles, bulk copies, operand and scale descriptors, reads of tensor
 // memory, and the epilogue's way from registers to rows of y.
 #pragma once
+#include <cuda.h>
+
 #include <type_traits>
 
 #include "kernels.hpp"
@@ -45,6 +47,32 @@ __device__ __forceinline__ void tmem_allocate_pair(uint32_t *slot, uint32_t colu
 }
 __device__ __forceinline__ void tmem_free_pair(uint32_t tmem, uint32_t columns) {
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+}
+// Pairs of CTAs.  Barriers that both use lie in the first CTA.  The second one's copies count on the first one's barrier; it is the first one
+// that expects the bytes of both: an arrival across the pair with release semantics, once per block of copies, takes longer than the block's
+// MMAs (measured: 4096 x 4096 x 16384 bf16 677 us, 319 us without).
+__device__ __forceinline__ uint32_t cta_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t in_cta(uint32_t local, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(local), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void pair_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void arrive_pair(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 // 32 rows of 16 bytes, not swizzled: 8-row groups 128 bytes apart.
 __device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
@@ -143,6 +171,29 @@ template <typename F> cudaError_t by_output(int dtype, int act, F f) {
 }
 constexpr int kLinearSmem = 226 * 1024;
 constexpr int kSmemPerSm = 228 * 1024;
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+inline EncodeTiled encode_tiled() {
+    static const EncodeTiled fn = [] {
+        void *sym = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        const bool ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &found) == cudaSuccess && found == cudaDriverEntryPointSuccess;
+        return ok ? reinterpret_cast<EncodeTiled>(sym) : nullptr;
+    }();
+    return fn;
+}
+// A matrix of `rows` rows of `cols` elements, `row_bytes` apart (a multiple of 16), read in boxes; zeros outside.
+inline cudaError_t encode_map(CUtensorMap *map, CUtensorMapDataType type, const void *base, int64_t cols, int64_t rows, int64_t row_bytes, int box_cols, int box_rows,
+                              CUtensorMapSwizzle swizzle) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(row_bytes)};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows)}, ones[2] = {1, 1};
+    const CUresult r = encode(map, type, 2, const_cast<void *>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 // Columns of tensor memory come in powers of two, at least 32.
 inline int allocation_of(int columns) {
     int n = 32;
