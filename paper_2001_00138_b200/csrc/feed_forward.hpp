@@ -51,11 +51,10 @@ struct Mx8Params {
     int splits, tiles_per_split;            // cluster split of the column tiles
     int stages;
     int tensor_columns;                     // of tensor memory that a CTA allocates
-    int step_n, step_f;                     // persistent kernel: from a CTA's tile to its next one
     uint32_t spin_limit;                    // polls of a bounded wait (0 = the default)
     int test_skip_load;                     // test hook: every CTA leaves out the copies of this (1-based) column tile of its walk (0 = off)
 };
-using Mx8Launch = Mx4Launch;
+using Mx8Launch = Mx4Launch;               // persistent: pairs of CTAs
 cudaError_t prepare_mx8_linear();                       // opt in to the dynamic shared memory
 Mx8Launch plan_mx8_linear(Mx8Params &p);                // shapes of p (F, K, rows, x_raw) -> its tiling and the launch; no device is touched
 cudaError_t launch_mx8_linear(Mx8Params p, cudaStream_t st, int *launches);

@@ -315,7 +315,7 @@ int patdnn_linear8_plan(int32_t F, int32_t K, int64_t rows, int32_t from_8_bit_r
     const Mx8Launch l = plan_mx8_linear(p);
     *info = patdnn_linear_plan_info{};
     info->persistent = l.persistent; info->quantises = fused;
-    info->tile_rows = l.persistent ? 128 : p.tile_n; info->tile_outputs = l.persistent ? p.tile_n : 128;
+    info->tile_rows = l.persistent ? 256 : p.tile_n; info->tile_outputs = l.persistent ? p.tile_n : 128;
     info->column_tiles = p.col_tiles; info->splits = p.splits; info->stages = p.stages;
     info->piece_bytes = l.piece; info->grid = static_cast<int32_t>(l.grid); info->smem_bytes = l.smem; info->tensor_columns = p.tensor_columns;
     return PATDNN_OK;

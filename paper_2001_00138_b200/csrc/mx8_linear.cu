@@ -235,177 +235,171 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx8_linear_kernel(Mx8Params p)
     if (warp == 2) tmem_free(tmem, tmem_cols);
 }
 
-// ---- many rows ----------------------------------------------------------------------------------------------------------
-// Tiles of 128 rows of x (M) by up to 256 rows of w (N), one persistent CTA per SM walking over them.  Warp 0 fills a ring of column
-// tiles, warp 1 issues the MMAs, warps 4 to 19 are the epilogue: they move the finished accumulator to registers, hand tensor memory back,
-// and convert and store while the next tile is multiplied.  A lane owns a row of y; pieces of 32 rows pass through shared memory so
-// that they are stored as whole sectors.
+// ---- many rows ------------------------------------------------------------------------------------------------------------
+// Tiles of 256 rows of x (M) by 256 rows of w (N) for pairs of CTAs (cta_group::2), which walk over them: each copies its 128 rows of x and 128 of
+// the 256 rows of w, and all the scales that its MMAs need (its own rows', both halves' of w).  Warp 0 fills a ring of column tiles, warp 1
+// of the first CTA issues the MMAs, warps 4 to 19 are the epilogue: they move the finished accumulator to registers, hand tensor memory back,
+// and convert and store while the next tile is multiplied.  A lane owns a row of y; pieces of 32 rows pass through shared memory so that they
+// are stored as whole sectors.
+// Per column tile a CTA writes 33 KB into shared memory and the MMAs read 32 KB from it in the 512 cycles that they take (tiles of 128 x 256 for
+// a single CTA: 51 and 48 KB, more than its 128 bytes per cycle).  The tiles come as tensor-map copies of rows that are swizzled already,
+// since only such copies may count on the other CTA's barrier.
 constexpr int kRowsThreads = 640;
 constexpr int kEpilogueWarps = 16;
-template <typename T, int ACT, int PIECE>
-__global__ void __launch_bounds__(kRowsThreads, 1) mx8_rows_kernel(Mx8Params p) {
+constexpr int kPiece = 32;                                               // bytes of a row of y that are stored at a time
+constexpr int kPairStages = 6;
+constexpr int kPairStage = 2 * kTileCodes + 2048;                        // codes, and three chunks of scales
+__device__ __forceinline__ void copy_scales_pair(uint32_t tmem, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void umma_mx8_pair(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+struct Mx8Maps {
+    CUtensorMap x, w, x_scales, w_scales;
+};
+
+template <typename T, int ACT>
+__global__ void __launch_bounds__(kRowsThreads, 1) mx8_pair_kernel(const __grid_constant__ Mx8Maps maps, const Mx8Params p) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 2];
+    __shared__ __align__(8) unsigned long long bars[2 * kPairStages + 2];
     __shared__ uint32_t tmem_slot;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const uint32_t rank = cta_rank();
     const WaitCtx ctx{p.status, p.spin_limit ? p.spin_limit : kSpinLimit};
     const uint32_t smem = (smem_u32(smem_raw) + 1023) & ~1023u;
-    const uint32_t full = smem_u32(bars), empty = full + 8 * kMaxStages, done = empty + 8 * kMaxStages, drained = done + 8;
-
-    const int wide = p.tile_n / 128;                                     // row tiles of w per tile: 1 or 2
-    constexpr uint32_t codes = kTileCodes, sf_bytes = kMx8Scales;        // of one row tile
-    const uint32_t stage_bytes = ((1 + wide) * (codes + sf_bytes) + 1023) & ~1023u;
-    const int tmem_cols = p.tensor_columns, sf_base = p.tile_n, sf_cols = 4 + 4 * wide;
+    // full: in the first CTA; empty, done: one per CTA, told by the first CTA's MMAs; drained: in the first CTA, by the epilogue warps of both
+    const uint32_t full = smem_u32(bars), empty = full + 8 * kPairStages, done = empty + 8 * kPairStages, drained = done + 8;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < p.stages; ++s) {
+        for (int s = 0; s < kPairStages; ++s) {
             mbar_init(full + 8 * s, 1);
             mbar_init(empty + 8 * s, 1);
         }
         mbar_init(done, 1);
-        mbar_init(drained, kEpilogueWarps);
+        mbar_init(drained, 2 * kEpilogueWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 2) tmem_allocate(&tmem_slot, tmem_cols);
+    if (warp == 2) tmem_allocate_pair(&tmem_slot, 512);
     tc_fence_before();
     __syncthreads();
+    pair_barrier();                                                      // both CTAs' barriers exist, and their tensor memory
     tc_fence_after();
     pdl_trigger();                                                       // not before the allocation: see kernels.hpp
     const uint32_t tmem = tmem_slot;
-    const int64_t tiles = static_cast<int64_t>(p.f_tiles) * p.n_tiles;   // f_tiles of tile_n outputs, n_tiles of 128 rows
-    const int w_tiles = (p.F + 127) / 128;
+    const int tiles = p.f_tiles * p.n_tiles, first = blockIdx.x >> 1, step = gridDim.x >> 1;     // of 256 outputs and of 256 rows
 
     if (warp == 0) {
         const bool leader = elect_one();
+        const uint32_t full0 = in_cta(full, 0);
         int issued = 0, slot = 0;
         uint32_t phase = 1;                                              // (the first pass over the ring does not wait)
-        bool ok = true, waited = false;
-        const uint32_t next_codes = p.col_tiles * codes, next_scales = p.groups * sf_bytes;    // from one row tile to the next
-        int ft = static_cast<int>(blockIdx.x % static_cast<unsigned>(p.f_tiles));
-        int nt = static_cast<int>(blockIdx.x / static_cast<unsigned>(p.f_tiles));
-        for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
-            const bool two = wide == 2 && ft * 2 + 1 < w_tiles;
-            const uint32_t bytes = (two ? 3 : 2) * (codes + sf_bytes);
-            const uint8_t *wc = p.w + static_cast<int64_t>(ft) * wide * next_codes;
-            const uint8_t *ws = p.w + p.w_scales + static_cast<int64_t>(ft) * wide * next_scales;
-            const uint8_t *xc = p.x + static_cast<int64_t>(nt) * next_codes, *xs = p.x + p.x_scales + static_cast<int64_t>(nt) * next_scales;
+        bool ok = true;
+        pdl_wait();
+        for (int t = first; ok && t < tiles; t += step) {
+            const int nt = t / p.f_tiles, ft = t - nt * p.f_tiles;
+            const int xr = nt * 2 + static_cast<int>(rank), wr = ft * 2 + static_cast<int>(rank);      // row tiles of 128
             for (int i = 0; i < p.col_tiles; ++i) {
-                if (issued >= p.stages && !warp_wait(empty + 8 * slot, phase, ctx, 111)) { ok = false; break; }
-                const uint32_t at = smem + slot * stage_bytes, bar = full + 8 * slot;
-                const uint32_t sf = at + (1 + wide) * codes;
-                const bool copies = leader && issued + 1 != p.test_skip_load;
-                if (copies) {
-                    mbar_expect_tx(bar, bytes);
-                    bulk_load(at + codes, wc, codes, bar);
-                    bulk_load(sf + sf_bytes, ws, sf_bytes, bar);
-                    if (two) {
-                        bulk_load(at + 2 * codes, wc + next_codes, codes, bar);
-                        bulk_load(sf + 2 * sf_bytes, ws + next_scales, sf_bytes, bar);
-                    }
+                if (issued >= kPairStages && !warp_wait(empty + 8 * slot, phase, ctx, 131)) { ok = false; break; }
+                if (leader && issued + 1 != p.test_skip_load) {
+                    const uint32_t at = smem + slot * kPairStage, bar = full0 + 8 * slot;
+                    if (rank == 0) mbar_expect_tx(full + 8 * slot, 2 * (2 * kTileCodes + 3 * kMx8Scales));
+                    // (row tiles that do not exist are outside the maps: zeros)
+                    tile_load(at, &maps.x, bar, 0, (xr * p.col_tiles + i) * 128);
+                    tile_load(at + kTileCodes, &maps.w, bar, 0, (wr * p.col_tiles + i) * 128);
+                    const uint32_t sf = at + 2 * kTileCodes;
+                    tile_load(sf, &maps.x_scales, bar, 0, (xr * p.groups + (i >> 2)) * 4);
+                    tile_load(sf + kMx8Scales, &maps.w_scales, bar, 0, (ft * 2 * p.groups + (i >> 2)) * 4);
+                    tile_load(sf + 2 * kMx8Scales, &maps.w_scales, bar, 0, ((ft * 2 + 1) * p.groups + (i >> 2)) * 4);
                 }
-                if (!waited) {                                           // weights do not depend on the previous kernel, x does
-                    pdl_wait();
-                    waited = true;
-                }
-                if (copies) {
-                    bulk_load(at, xc, codes, bar);
-                    bulk_load(sf, xs, sf_bytes, bar);
-                }
-                wc += codes; xc += codes;
-                if ((i & 3) == 3) { ws += sf_bytes; xs += sf_bytes; }
                 ++issued;
-                if (++slot == p.stages) { slot = 0; phase ^= 1; }
+                if (++slot == kPairStages) { slot = 0; phase ^= 1; }
             }
-            nt += p.step_n;                                              // the tile gridDim.x further on
-            ft += p.step_f;
-            if (ft >= p.f_tiles) { ft -= p.f_tiles; ++nt; }
         }
-        // no copy may still be in flight when the CTA ends, whatever happened to the other roles
-        for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait(full + 8 * (i % p.stages), (i / p.stages) & 1, ctx, 112);
-    } else if (warp == 1) {
+        // no copy of either CTA may still be in flight when the pair ends, whatever happened to the other roles
+        if (rank == 0)
+            for (int i = max(0, issued - kPairStages); i < issued; ++i) mbar_wait(full + 8 * (i % kPairStages), (i / kPairStages) & 1, ctx, 132);
+    } else if (warp == 1 && rank == 0) {
         const bool leader = elect_one();
         int slot = 0, done_tiles = 0;
         uint32_t phase = 0;
-        const uint32_t idesc = mx8_instr_desc(p.tile_n, 0), next_byte = (1u << 4) | (1u << 29);
-        const uint64_t da0 = smem_desc_sw128(smem), db0 = smem_desc_sw128(smem + codes);
-        const uint64_t s0 = scale_desc(smem + (1 + wide) * codes);
-        constexpr uint32_t row_scales = sf_bytes >> 4;                   // descriptor distance between the scales of two row tiles
+        const uint32_t idesc = (uint32_t(256 >> 3) << 17) | (1u << 23) | (uint32_t(256 >> 4) << 24), next_byte = (1u << 4) | (1u << 29);
+        const uint64_t da0 = smem_desc_sw128(smem), db0 = smem_desc_sw128(smem + kTileCodes), s0 = scale_desc(smem + 2 * kTileCodes);
+        const uint32_t own_empty = in_cta(empty, 0), peer_empty = in_cta(empty, 1), own_done = in_cta(done, 0), peer_done = in_cta(done, 1);
         bool ok = true;
         pdl_wait();                                                      // the bound of the waits below is for this kernel's copies alone
-        for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x, ++done_tiles) {
-            if (done_tiles > 0 && !warp_wait(drained, (done_tiles - 1) & 1, ctx, 113)) break;
+        for (int t = first; ok && t < tiles; t += step, ++done_tiles) {
+            if (done_tiles > 0 && !warp_wait(drained, (done_tiles - 1) & 1, ctx, 133)) break;
             tc_fence_after();
             int steps = p.ksteps;
             uint32_t accumulate = 0;
             for (int i = 0; i < p.col_tiles; ++i, steps -= 4) {
-                if (!warp_wait(full + 8 * slot, phase, ctx, 114)) { ok = false; break; }
+                if (!warp_wait(full + 8 * slot, phase, ctx, 134)) { ok = false; break; }
                 tc_fence_after();
-                const uint64_t shift = static_cast<uint64_t>(slot) * (stage_bytes >> 4);
-                const uint64_t da = da0 + shift, db = db0 + shift, sd = s0 + shift;
-                const uint32_t sfa = tmem + sf_base + slot * sf_cols, sfb = sfa + 4;
+                const uint64_t shift = static_cast<uint64_t>(slot) * (kPairStage >> 4);
+                const uint32_t sfa = tmem + 256 + slot * 12, sfb = sfa + 4;
                 const uint32_t which = idesc + (i & 3) * next_byte;
                 if (leader) {
-                    copy_scales(sfa, sd);
-                    copy_scales(sfb, sd + row_scales);
-                    if (wide == 2) copy_scales(sfb + 4, sd + 2 * row_scales);
+                    copy_scales_pair(sfa, s0 + shift);
+                    copy_scales_pair(sfb, s0 + shift + (kMx8Scales >> 4));
+                    copy_scales_pair(sfb + 4, s0 + shift + 2 * (kMx8Scales >> 4));
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        if (k < steps) umma_mx8(tmem, da + 2 * k, db + 2 * k, which, sfa, sfb, accumulate | k);
-                    umma_commit(empty + 8 * slot);
+                        if (k < steps) umma_mx8_pair(tmem, da0 + shift + 2 * k, db0 + shift + 2 * k, which, sfa, sfb, accumulate | k);
+                    commit_pair(own_empty + 8 * slot);
+                    commit_pair(peer_empty + 8 * slot);
                 }
                 __syncwarp();
                 accumulate = 1;
-                if (++slot == p.stages) { slot = 0; phase ^= 1; }
+                if (++slot == kPairStages) { slot = 0; phase ^= 1; }
             }
-            if (leader && ok) umma_commit(done);
+            if (leader && ok) {
+                commit_pair(own_done);
+                commit_pair(peer_done);
+            }
             __syncwarp();
         }
         // no MMA may still run when tensor memory is freed
-        if (leader && !ok) umma_commit(done);
+        if (leader && !ok) commit_pair(own_done);
         __syncwarp();
-        if (done_tiles > 0) mbar_wait(done, (done_tiles - 1) & 1, ctx, 116);
+        if (done_tiles > 0) mbar_wait(done, (done_tiles - 1) & 1, ctx, 136);
     } else if (warp >= 4) {
         pdl_wait();
         const int e = warp - 4, quadrant = e & 3, quarter = e >> 2;      // lanes and columns of the accumulator this warp moves
-        const int cols = p.tile_n / 4;                                   // 32 or 64
-        unsigned char *stage = smem_raw + (smem - smem_u32(smem_raw)) + p.stages * stage_bytes + e * stage_out(PIECE);
-        float *bias = reinterpret_cast<float *>(stage + 32 * PIECE);
-        const uint32_t from = tmem + (static_cast<uint32_t>(quadrant * 32) << 16) + quarter * cols;
+        unsigned char *stage = smem_raw + (smem - smem_u32(smem_raw)) + kPairStages * kPairStage + e * stage_out(kPiece);
+        float *bias = reinterpret_cast<float *>(stage + 32 * kPiece);
+        const uint32_t from = tmem + (static_cast<uint32_t>(quadrant * 32) << 16) + quarter * 64, drained0 = in_cta(drained, 0);
         T *const y = static_cast<T *>(p.y);
         const uint64_t places = reinterpret_cast<uintptr_t>(p.y) | static_cast<uint64_t>(p.ldy * sizeof(T));
         const int aligned = places % 16 == 0 ? 16 : places % 4 == 0 ? 4 : 2;
-        int ft = static_cast<int>(blockIdx.x % static_cast<unsigned>(p.f_tiles));
-        int nt = static_cast<int>(blockIdx.x / static_cast<unsigned>(p.f_tiles));
         uint32_t phase = 0;
-        auto bias_of = [&](int f) { return p.bias && f < p.F ? p.bias[f] : 0.f; };
-        float ahead0 = bias_of(ft * p.tile_n + quarter * cols + lane), ahead1 = bias_of(ft * p.tile_n + quarter * cols + 32 + lane);
-        for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-            const int f0 = ft * p.tile_n + quarter * cols;
-            const int64_t row0 = static_cast<int64_t>(nt) * 128 + quadrant * 32;
-            nt += p.step_n;                                              // the tile gridDim.x further on, whose bias is fetched meanwhile
-            ft += p.step_f;
-            if (ft >= p.f_tiles) { ft -= p.f_tiles; ++nt; }
+        for (int t = first; t < tiles; t += step) {
+            const int nt = t / p.f_tiles, f0 = (t - nt * p.f_tiles) * 256 + quarter * 64;
+            const int64_t row0 = static_cast<int64_t>(nt) * 256 + rank * 128 + quadrant * 32;
             __syncwarp();
-            bias[lane] = ahead0;
-            if (cols == 64) bias[32 + lane] = ahead1;
-            ahead0 = bias_of(ft * p.tile_n + quarter * cols + lane);
-            ahead1 = bias_of(ft * p.tile_n + quarter * cols + 32 + lane);
-            if (!mbar_wait(done, phase, ctx, 115)) break;
+#pragma unroll
+            for (int c = lane; c < 64; c += 32) bias[c] = p.bias && f0 + c < p.F ? p.bias[f0 + c] : 0.f;
+            __syncwarp();
+            if (!mbar_wait(done, phase, ctx, 135)) break;
             phase ^= 1;
             tc_fence_after();
             uint32_t v[64];
             tmem_ld32_async(from, v);
-            if (cols == 64) tmem_ld32_async(from + 32, v + 32);
+            tmem_ld32_async(from + 32, v + 32);
             asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(drained) : "memory");
-            constexpr int kCols = PIECE / sizeof(T);
-            const int rows_left = static_cast<int>(min(static_cast<int64_t>(32), p.rows - row0));
+            if (lane == 0) arrive_pair(drained0);
+            constexpr int kCols = kPiece / sizeof(T);
+            const int rows_left = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(32), p.rows - row0)));
             T *out = y + row0 * p.ldy + f0;
 #pragma unroll
             for (int c = 0; c < 64; c += kCols) {
-                if (c >= cols || f0 + c >= p.F || rows_left <= 0) continue;
+                if (f0 + c >= p.F || rows_left == 0) continue;
                 float o[kCols];
 #pragma unroll
                 for (int j = 0; j < kCols; j += 4) {
@@ -415,16 +409,24 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx8_rows_kernel(Mx8Params p) 
                     o[j + 2] = activate1<ACT>(__uint_as_float(v[c + j + 2]) + b.z);
                     o[j + 3] = activate1<ACT>(__uint_as_float(v[c + j + 3]) + b.w);
                 }
-                store_piece<T, PIECE>(o, stage, out + c, p.ldy, rows_left, p.F - f0 - c, aligned);
+                store_piece<T, kPiece>(o, stage, out + c, p.ldy, rows_left, p.F - f0 - c, aligned);
             }
         }
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 2) tmem_free(tmem, tmem_cols);
+    pair_barrier();                                                      // nobody's shared or tensor memory goes away under its peer
+    if (warp == 2) tmem_free_pair(tmem, 512);
 }
 
+// The codes of a matrix as rows of 128 bytes, its scales as four rows of 128 bytes per chunk.
+cudaError_t codes_map(CUtensorMap *map, const uint8_t *base, int64_t row_tiles, int64_t col_tiles) {
+    return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, 128, row_tiles * col_tiles * 128, 128, 128, 128, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+cudaError_t scales_map(CUtensorMap *map, const uint8_t *base, int64_t row_tiles, int64_t groups) {
+    return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, 128, row_tiles * groups * 4, 128, 128, 4, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
 
 }  // namespace
 
@@ -437,8 +439,7 @@ cudaError_t prepare_mx8_linear() {
     for (int dtype = 0; dtype < 3 && e == cudaSuccess; ++dtype)
         for (int act = PATDNN_ACT_NONE; act <= PATDNN_ACT_SILU && e == cudaSuccess; ++act)
             e = by_output(dtype, act, [&](auto t, auto a) {
-                const cudaError_t r = cudaFuncSetAttribute(mx8_rows_kernel<decltype(t), a.value, 32>, what, kLinearSmem);
-                return r == cudaSuccess ? cudaFuncSetAttribute(mx8_rows_kernel<decltype(t), a.value, 64>, what, kLinearSmem) : r;
+                return cudaFuncSetAttribute(mx8_pair_kernel<decltype(t), a.value>, what, kLinearSmem);
             });
     return e;
 }
@@ -449,28 +450,6 @@ Mx8Launch plan_mx8_linear(Mx8Params &p) {
     p.groups = static_cast<int>(shape.groups);
     p.ksteps = static_cast<int>(ceil_div(p.K, 32));
     Mx8Launch l{};
-    // Many rows: as soon as tiles of 128 x 256 (or 128 x 128) fill the SMs, the persistent kernel.
-    const int64_t row_tiles = ceil_div(p.rows, 128);
-    const int tile_f = p.F > 128 && row_tiles * ceil_div(p.F, 256) >= sm_count() ? 256 : 128;
-    if (!p.x_raw && p.rows > 64 && row_tiles * ceil_div(p.F, tile_f) >= sm_count()) {
-        l.persistent = true;
-        p.tile_n = tile_f;
-        p.f_tiles = static_cast<int>(ceil_div(p.F, tile_f));
-        p.n_tiles = static_cast<int>(row_tiles);
-        p.splits = 1;
-        const int wide = tile_f / 128;
-        const int stage = ((1 + wide) * (kTileCodes + kMx8Scales) + 1023) / 1024 * 1024;
-        l.piece = p.col_tiles <= 6 ? 64 : 32;
-        const int out = kEpilogueWarps * stage_out(l.piece) + 1024;
-        p.stages = std::min(kMaxStages, (kLinearSmem - out) / stage);
-        p.tensor_columns = 512;                        // (one CTA per SM: its threads take most of the registers)
-        const int64_t tiles = static_cast<int64_t>(p.f_tiles) * p.n_tiles;
-        l.grid = static_cast<unsigned>(std::min<int64_t>(tiles, sm_count()));
-        p.step_n = static_cast<int>(l.grid / p.f_tiles);
-        p.step_f = static_cast<int>(l.grid % p.f_tiles);
-        l.smem = p.stages * stage + out;
-        return l;
-    }
     p.f_tiles = static_cast<int>(ceil_div(p.F, 128));
     // (row tiles start at multiples of 128: the scales of a tile start at a column of tensor memory that is a multiple of four)
     p.tile_n = p.rows <= 128 ? static_cast<int>(ceil_div(p.rows, 16) * 16) : 128;
@@ -481,6 +460,24 @@ Mx8Launch plan_mx8_linear(Mx8Params &p) {
     p.splits = 1;
     while (p.splits < 8 && tiles * p.splits * 2 <= sm_count() && p.col_tiles >= p.splits * 2 * least) p.splits *= 2;
     p.tiles_per_split = static_cast<int>(ceil_div(p.col_tiles, p.splits));
+    // Pairs of CTAs where an estimate in cycles says so: a column tile takes about as long in both kernels (512 cycles of MMAs for 256 x 256
+    // on two SMs; the traffic of 128 x 128 through one SM's shared memory), so rounds over the SMs decide.
+    const int64_t pairs = std::max(1, sm_count() / 2), pair_tiles = ceil_div(p.rows, 256) * ceil_div(p.F, 256);
+    const int64_t alone = ceil_div(tiles * p.splits, sm_count()) * (p.tiles_per_split * 600 + 2500);
+    const int64_t paired = ceil_div(pair_tiles, pairs) * p.col_tiles * 560 + 3500;
+    if (!p.x_raw && paired < alone) {
+        l.persistent = true;
+        p.tile_n = 256;
+        p.f_tiles = static_cast<int>(ceil_div(p.F, 256));
+        p.n_tiles = static_cast<int>(ceil_div(p.rows, 256));
+        p.splits = 1;
+        p.stages = kPairStages;
+        l.piece = kPiece;
+        p.tensor_columns = 512;
+        l.grid = 2 * static_cast<unsigned>(std::min(pair_tiles, pairs));
+        l.smem = kLinearSmem;                          // all of an SM's: a pair holds all of two SMs' tensor memory (see plan_mx4_linear)
+        return l;
+    }
     const int stage = kTileCodes + p.tile_n * 128 + 2 * kMx8Scales;
     p.stages = std::max(1, std::min({kMaxStages, p.tiles_per_split, 200 * 1024 / stage}));
     const int slots = p.splits > 1 ? static_cast<int>(ceil_div(p.tile_n, p.splits)) * p.splits * 512 : 0;
@@ -495,11 +492,18 @@ Mx8Launch plan_mx8_linear(Mx8Params &p) {
 cudaError_t launch_mx8_linear(Mx8Params p, cudaStream_t st, int *launches) {
     const Mx8Launch l = plan_mx8_linear(p);
     *launches = 1;
-    if (l.persistent)
+    if (l.persistent) {
+        Mx8Maps maps;
+        const int64_t x_tiles = ceil_div(p.rows, 128), w_tiles = ceil_div(p.F, 128);
+        cudaError_t e = codes_map(&maps.x, p.x, x_tiles, p.col_tiles);
+        if (e == cudaSuccess) e = codes_map(&maps.w, p.w, w_tiles, p.col_tiles);
+        if (e == cudaSuccess) e = scales_map(&maps.x_scales, p.x + p.x_scales, x_tiles, p.groups);
+        if (e == cudaSuccess) e = scales_map(&maps.w_scales, p.w + p.w_scales, w_tiles, p.groups);
+        if (e != cudaSuccess) return e;
         return by_output(p.dtype, p.act, [&](auto t, auto a) {
-            const auto kernel = l.piece == 64 ? mx8_rows_kernel<decltype(t), a.value, 64> : mx8_rows_kernel<decltype(t), a.value, 32>;
-            return launch_pdl(kernel, dim3(l.grid), dim3(kRowsThreads), l.smem, st, 1, p);
+            return launch_pdl(mx8_pair_kernel<decltype(t), a.value>, dim3(l.grid), dim3(kRowsThreads), l.smem, st, 2, maps, p);
         });
+    }
     const auto kernel = !p.x_raw ? mx8_linear_kernel<void> : p.dtype == PATDNN_F32 ? mx8_linear_kernel<float>
                         : p.dtype == PATDNN_F16 ? mx8_linear_kernel<__half> : mx8_linear_kernel<__nv_bfloat16>;
     return launch_pdl(kernel, dim3(l.grid), dim3(kLinThreads), l.smem, st, p.splits, p);

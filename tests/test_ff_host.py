@@ -79,7 +79,7 @@ def test_ctas_of_the_8_bit_product_that_fit_an_sm_find_tensor_memory():
             what = (F, K, rows, mx, p)
             columns = p["tensor_columns"]
             assert columns in (32, 64, 128, 256, 512), what
-            used = p["tile_outputs"] + (4 + p["tile_outputs"] // 32) * p["stages"] if p["persistent"] else p["tile_rows"] + 8 * p["stages"]
+            used = p["tile_outputs"] + 12 * p["stages"] if p["persistent"] else p["tile_rows"] + 8 * p["stages"]
             assert used <= columns, what
             assert p["smem_bytes"] <= 226 * 1024, what
             if p["persistent"]:

@@ -145,8 +145,9 @@ FORMS = {  # rows, K, F, 8-bit rows, and what patdnn_linear8_plan says
     "256 outputs, ring wraps": (9500, 1100, 513, False, dict(persistent=1, tile_outputs=256, column_tiles=9)),
     "256 outputs, one column tile": (40000, 90, 600, True, dict(persistent=1, tile_outputs=256, column_tiles=1)),
     "256 outputs, full tiles": (10000, 1024, 768, True, dict(persistent=1, tile_outputs=256, column_tiles=8)),
-    "128 outputs, ring wraps": (20000, 2000, 100, True, dict(persistent=1, tile_outputs=128, column_tiles=16)),
-    "128 outputs, odd last tile": (3000, 1100, 1100, True, dict(persistent=1, tile_outputs=128)),
+    "256 outputs, few of them": (20000, 2000, 100, True, dict(persistent=1, tile_outputs=256, column_tiles=16)),
+    "256 outputs, fewer tiles than pairs": (3000, 1100, 1100, True, dict(persistent=1, tile_outputs=256, grid=120)),
+    "no cluster, several tiles of rows": (1000, 300, 300, True, dict(persistent=0, splits=1, tile_rows=128)),
 }
 
 
@@ -309,7 +310,7 @@ def test_row_strides_beyond_32_bits(rows):
 
 
 @pytest.mark.parametrize("form, skip", [("quantises its rows, one tile", 1), ("quantises its rows, cluster of four", 2), ("a cluster of eight", 3),
-                                        ("no cluster, ring wraps", 9), ("128 outputs, ring wraps", 7), ("256 outputs, ring wraps", 11)])
+                                        ("no cluster, ring wraps", 9), ("256 outputs, few of them", 7), ("256 outputs, ring wraps", 11)])
 def test_a_wait_that_runs_out_is_reported_and_the_handle_keeps_working(form, skip):
     """The bound is shortened to a few milliseconds and the copies of one column tile are left out, so that the consumers' wait for them runs out."""
     import torch
