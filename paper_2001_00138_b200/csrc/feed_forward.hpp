@@ -97,11 +97,9 @@ struct GatedPlan {
 };
 GatedPlan plan_gated(int F, int K, int64_t rows, int mode);
 constexpr int kGatedUnitFloats = 256 * 256; // partial sums of a (tile, split) unit
-constexpr int kGatedCounters = 16;          // of a tile: epilogue warps of both CTAs
 struct GatedWork {                          // a handle's buffers
     void *dgu;                              // [max_rows][2 Fp]: dg, du in the handle's type, Fp = F rounded up to 64; nullptr without gradients
     float *partial;
-    unsigned *arrivals;                     // zero between calls
     int *status;
 };
 inline int gated_padded(int F) { return (F + 63) / 64 * 64; }
@@ -116,7 +114,7 @@ struct GatedCall {
 };
 int units_most();                           // units that run at a time: pairs of SMs
 cudaError_t prepare_gated();
-cudaError_t launch_gated(const GatedShape &s, const GatedCall &c, const GatedWork &w, int mode, cudaStream_t st);
+cudaError_t launch_gated(const GatedShape &s, const GatedCall &c, const GatedWork &w, int mode, cudaStream_t st, int *launches);
 // rows of a 16-bit matrix to rows `to_row` apart, zeros behind them
 cudaError_t launch_gated_pack(const void *x, int64_t rows, int cols, int64_t row, void *to, int64_t to_row, int dtype, cudaStream_t st);
 // dgu from gu [rows][2 F] and dh

@@ -52,7 +52,6 @@ struct patdnn_gated_s {
     ~patdnn_gated_s() {
         cudaFree(w.dgu);
         cudaFree(w.partial);
-        cudaFree(w.arrivals);
         cudaFree(w.status);
         cudaFree(x);
         cudaFree(weights);
@@ -158,6 +157,12 @@ int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu
         c.w_row = row;
     }
     return PATDNN_OK;
+}
+
+int gated_product(patdnn_gated h, const GatedCall &c, int mode, cudaStream_t st) {
+    int n = 0;
+    const cudaError_t e = launch_gated(h->s, c, h->w, mode, st, &n);
+    return launched(e, n, "gated block launch");
 }
 
 }  // namespace
@@ -363,12 +368,10 @@ int patdnn_gated_create(const patdnn_gated_desc *desc, patdnn_gated *out) {
     if (!h) return PATDNN_E_ALLOC;
     h->s = s;
     h->max_rows = desc->max_rows;
-    const size_t counters = static_cast<size_t>(units_most()) * kGatedCounters, row = static_cast<size_t>(packed_row(s.K));
+    const size_t row = static_cast<size_t>(packed_row(s.K));
     uint16_t *dgu = nullptr, *x = nullptr, *weights = nullptr;
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = allocate(&h->w.partial, static_cast<size_t>(units_most()) * kGatedUnitFloats);
-    if (e == cudaSuccess) e = allocate(&h->w.arrivals, counters);
-    if (e == cudaSuccess) e = cudaMemset(h->w.arrivals, 0, counters * sizeof(unsigned));
     if (e == cudaSuccess) e = allocate(&h->w.status, 4);
     if (e == cudaSuccess) e = cudaMemset(h->w.status, 0, 16);
     if (e == cudaSuccess && desc->grad) e = allocate(&dgu, static_cast<size_t>(desc->max_rows) * 2 * gated_padded(s.F));
@@ -378,7 +381,7 @@ int patdnn_gated_create(const patdnn_gated_desc *desc, patdnn_gated *out) {
     if (e == cudaSuccess && !copies_as_it_lies(s.w_row)) e = allocate(&weights, 2 * static_cast<size_t>(s.F) * row);
     h->weights = weights;
     if (e == cudaSuccess) e = prepare_gated();
-    if (e == cudaSuccess) e = cudaDeviceSynchronize();                  // the counters are zero on every stream from here on
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();                  // the status word is zero on every stream from here on
     if (e != cudaSuccess) return failed(h, e, "patdnn_gated_create");
     *out = h;
     return PATDNN_OK;
@@ -397,7 +400,7 @@ int patdnn_gated_run(patdnn_gated h, const void *x, const void *wg, const void *
     GatedCall c{};
     if (const int rc = gated_operands(h, x, wg, wu, rows, c, st)) return rc;
     c.h = hidden; c.gu = gu;
-    return launched(launch_gated(s, c, h->w, kGatedForward, st), 1, "gated block launch");
+    return gated_product(h, c, kGatedForward, st);
 }
 
 int patdnn_gated_grad(patdnn_gated h, const void *x, const void *wg, const void *wu, const void *gu, const void *dh, void *dx, void *dwg, void *dwu,
@@ -423,8 +426,8 @@ int patdnn_gated_grad(patdnn_gated h, const void *x, const void *wg, const void 
     c.dx = dx; c.dwg = dwg; c.dwu = dwu;
     if (const int rc = launched(launch_gated_slopes(s, gu, dh, h->w.dgu, rows, st), 1, "gated block gradient launch")) return rc;
     if (dx)
-        if (const int rc = launched(launch_gated(s, c, h->w, kGatedInput, st), 1, "gated block gradient launch")) return rc;
-    return dwg ? launched(launch_gated(s, c, h->w, kGatedWeights, st), 1, "gated block gradient launch") : PATDNN_OK;
+        if (const int rc = gated_product(h, c, kGatedInput, st)) return rc;
+    return dwg ? gated_product(h, c, kGatedWeights, st) : PATDNN_OK;
 }
 
 int patdnn_gated_plan(int32_t F, int32_t K, int64_t rows, int32_t product, patdnn_gated_plan_info *info) {
@@ -446,10 +449,7 @@ int patdnn_gated_check(patdnn_gated h) {
     int word = 0;
     CU(cudaMemcpy(&word, h->w.status, sizeof(int), cudaMemcpyDeviceToHost));
     if (!word) return PATDNN_OK;
-    // what was given up may have left partial sums uncounted
-    CU(cudaMemset(h->w.arrivals, 0, sizeof(unsigned) * units_most() * kGatedCounters));
     CU(cudaMemset(h->w.status, 0, sizeof(int)));
-    CU(cudaDeviceSynchronize());
     return PATDNN_E_DEVICE_TIMEOUT;
 }
 

@@ -9,8 +9,7 @@
 // outer one (wg and wu for dx; dg, du and x for dwg, dwu) the MMAs read the tiles as they lie, transposed (MN-major), so nothing is ever
 // transposed in memory.  Persistent: warp 0 copies, warp 1 of the pair's first CTA multiplies, warps 4 to 11 drain one accumulator (two, of
 // 256 columns each, fill tensor memory) while the other one is summed.
-// Few tiles: the summed dimension is cut into ranges, and the last of a tile's warps to arrive adds the partial sums in the ranges' order
-// (nobody waits, and the same call gives the same bits).
+// Few tiles: the summed dimension is cut into ranges whose partial sums go to memory, and a second kernel adds them in the ranges' order.
 #include <algorithm>
 
 #include "feed_forward.hpp"
@@ -35,8 +34,8 @@ struct GatedParams {
     int m_tiles, n_tiles, k_blocks, splits, per_split, stages;
     int f_blocks;                                      // input: blocks of 64 of the gate's part; weights: 256-row tiles of it
     int f_padded;                                      // columns from dg to du
+    int box_rows;                                      // rows of A that a CTA copies: fewer than 128 where the product has fewer (K-major A)
     float *partial;
-    unsigned *arrivals;
     int *status;
     uint32_t spin_limit;
     int test_skip_load;
@@ -56,6 +55,11 @@ template <bool KMAJOR> __device__ __forceinline__ uint64_t part_desc(uint32_t ad
     return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (leading << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
 }
 template <bool KMAJOR> constexpr uint64_t kNextK = KMAJOR ? 2 : 2048 >> 4;
+
+// Partial sums of a unit: a piece per epilogue warp of either CTA, [chunk of 32 columns][column][row].
+__device__ __forceinline__ float *part_of(float *partial, int64_t unit, uint32_t rank, int e) {
+    return partial + unit * kGatedUnitFloats + (static_cast<int>(rank) * kEpilogueWarps + e) * (kGatedUnitFloats / (2 * kEpilogueWarps));
+}
 
 template <int MODE, typename T, int ACT>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -95,6 +99,11 @@ gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     if (warp == 0) {
         const bool leader = elect_one();
         const uint32_t full0 = in_cta(full, 0);
+        // Rows that do not exist are not copied where they are all of a CTA's, or where the product has fewer rows than a tile: the MMAs read whatever is
+        // there and give rows that nobody stores.  (Filling 127 of 128 rows with zeros took the copies twice the time of 128 rows: one row,
+        // 1536 -> 8192, 17.7 us against 14.4 us for 128 rows.)
+        const uint32_t a_bytes = p.box_rows * 128, expected = 2 * kHalf + (A_K && p.rows <= 128 ? 1 : 2) * a_bytes;
+        const bool has_rows = !A_K || rank == 0 || p.rows > 128;
         int slot = 0, issued = 0;
         uint32_t phase = 1;                            // (the first pass over the ring does not wait)
         bool ok = true;
@@ -105,15 +114,15 @@ gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 if (issued >= p.stages && !warp_wait(empty + 8 * slot, phase, ctx, 121)) { ok = false; break; }
                 if (leader && issued + 1 != p.test_skip_load) {
                     const uint32_t bar = full0 + 8 * slot, a = smem + slot * kStage, b = a + kHalf;
-                    if (rank == 0) mbar_expect_tx(full + 8 * slot, 2 * kStage);
+                    if (rank == 0) mbar_expect_tx(full + 8 * slot, expected);
                     if constexpr (MODE == kGatedForward) {             // this CTA: 128 rows of x, and the gate's or the up projection's weights
-                        tile_load(a, &map_a, bar, k * 64, mt * 256 + rank * 128);
+                        if (has_rows) tile_load(a, &map_a, bar, k * 64, mt * 256 + rank * 128);
                         tile_load(b, rank == 0 ? &map_b0 : &map_b1, bar, k * 64, nt * 128);
                     } else if constexpr (MODE == kGatedInput) {
                         const bool up = k >= p.f_blocks;
                         const CUtensorMap *map = up ? &map_b1 : &map_b0;
                         const int f = (up ? k - p.f_blocks : k) * 64, n = nt * 256 + rank * 128;
-                        tile_load(a, &map_a, bar, k * 64, mt * 256 + rank * 128);
+                        if (has_rows) tile_load(a, &map_a, bar, k * 64, mt * 256 + rank * 128);
                         tile_load(b, map, bar, n, f);
                         tile_load(b + kHalf / 2, map, bar, n + 64, f);
                     } else {
@@ -196,56 +205,29 @@ gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             const int rows_left = static_cast<int>(max(static_cast<int64_t>(-1), min(static_cast<int64_t>(32), p.rows - row0)));
             // chunk j of the warp, 32 columns of the accumulator: forward gate, up, gate, up of its 64 outputs
             auto column = [&](int j) { return MODE == kGatedForward ? (j & 1) * 128 + half * 64 + (j >> 1) * 32 : half * 128 + j * 32; };
-            const float *parts = nullptr;
-            bool mine = true;
             if (p.splits > 1) {
-                constexpr int kWarpFloats = 4 * 32 * 32;
-                const int64_t unit_floats = kGatedUnitFloats, place = (static_cast<int64_t>(rank) * kEpilogueWarps + e) * kWarpFloats;
-                float *to = p.partial + u * unit_floats + place;
+                float *to = part_of(p.partial, u, rank, e) + lane;
                 for (int j = 0; j < 4; ++j) {
                     uint32_t v[32];
                     tmem_ld32(lanes + buf * 256 + column(j), v);
                     if (lane < rows_left) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) to[(j * 32 + i) * 32 + lane] = __uint_as_float(v[i]);
+                        for (int i = 0; i < 32; ++i) to[(j * 32 + i) * 32] = __uint_as_float(v[i]);
                     }
-                }
-                __threadfence();
-                __syncwarp();
-                unsigned before = 0;
-                unsigned *counter = p.arrivals + static_cast<int64_t>(tile) * kGatedCounters + rank * kEpilogueWarps + e;
-                if (lane == 0) before = atomicAdd(counter, 1u);
-                before = __shfl_sync(0xffffffffu, before, 0);
-                mine = before + 1 == static_cast<unsigned>(p.splits);
-                if (mine) {
-                    if (lane == 0) *counter = 0;
-                    __threadfence();
-                    parts = p.partial + static_cast<int64_t>(tile) * p.splits * unit_floats + place;
                 }
             }
             auto fetch = [&](int j, float (&v)[32]) {
-                if (p.splits == 1) {
-                    uint32_t w[32];
-                    tmem_ld32(lanes + buf * 256 + column(j), w);
+                uint32_t w[32];
+                tmem_ld32(lanes + buf * 256 + column(j), w);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(w[i]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = 0.f;
-                    if (lane < rows_left)
-                        for (int s = 0; s < p.splits; ++s) {
-                            const float *from = parts + static_cast<int64_t>(s) * kGatedUnitFloats + j * 1024 + lane;
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) v[i] += __ldcg(from + i * 32);
-                        }
-                }
+                for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(w[i]);
             };
             auto put = [&](const float (&v)[32], T *base, int64_t ld, int col, int left) {
                 const uint64_t places = reinterpret_cast<uintptr_t>(base) | static_cast<uint64_t>(ld * sizeof(T));
                 const int aligned = places % 16 == 0 ? 16 : places % 4 == 0 ? 4 : 2;
                 store_piece<T, kPiece>(v, stage, base + row0 * ld + col, ld, rows_left, left, aligned);
             };
-            if (mine && rows_left > 0) {
+            if (p.splits == 1 && rows_left > 0) {
                 if constexpr (MODE == kGatedForward) {
                     for (int c = 0; c < 2; ++c) {
                         const int f = nt * 128 + half * 64 + c * 32;
@@ -284,19 +266,74 @@ gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     if (warp == 2) tmem_free_pair(tmem, 512);
 }
 
+// The sums of a tile's ranges, in their order, and the epilogue.  A warp takes 32 rows and 16 columns (forward: of both projections); the eight
+// warps of a CTA are the eight epilogue warps' pieces of one CTA's half of the tile.
+template <int MODE, typename T, int ACT>
+__global__ void __launch_bounds__(256) gated_join_kernel(const GatedParams p) {
+    constexpr int kPieces = MODE == kGatedForward ? 4 : 8, kWide = 16;
+    __shared__ __align__(16) unsigned char staging[8][32 * kWide * sizeof(T)];
+    pdl_trigger();
+    const int e = threadIdx.x >> 5, lane = threadIdx.x & 31, quadrant = e & 3, half = e >> 2;
+    const int piece = blockIdx.x % kPieces, rank = blockIdx.x / kPieces & 1, tile = blockIdx.x / (2 * kPieces);
+    const int nt = tile / p.m_tiles;
+    int mt = tile - nt * p.m_tiles;
+    T *out = static_cast<T *>(p.out0);
+    if (MODE == kGatedWeights && mt >= p.f_blocks) {
+        mt -= p.f_blocks;
+        out = static_cast<T *>(p.out1);
+    }
+    const int64_t row0 = static_cast<int64_t>(mt) * 256 + rank * 128 + quadrant * 32;
+    const int rows_left = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(32), p.rows - row0)));
+    const int col = MODE == kGatedForward ? nt * 128 + half * 64 + piece * kWide : nt * 256 + half * 128 + piece * kWide, left = p.cols - col;
+    if (rows_left == 0 || left <= 0) return;
+    pdl_wait();
+    auto sum = [&](int chunk, int first, float (&v)[kWide]) {          // columns [first, first + 16) of a chunk
+#pragma unroll
+        for (int i = 0; i < kWide; ++i) v[i] = 0.f;
+        if (lane >= rows_left) return;
+        const float *from = part_of(p.partial, static_cast<int64_t>(tile) * p.splits, rank, e) + (chunk * 32 + first) * 32 + lane;
+#pragma unroll 4
+        for (int s = 0; s < p.splits; ++s, from += kGatedUnitFloats) {
+#pragma unroll
+            for (int i = 0; i < kWide; ++i) v[i] += from[i * 32];
+        }
+    };
+    auto put = [&](const float (&v)[kWide], T *base, int64_t ld) {
+        const uint64_t places = reinterpret_cast<uintptr_t>(base) | static_cast<uint64_t>(ld * sizeof(T));
+        const int aligned = places % 16 == 0 ? 16 : places % 4 == 0 ? 4 : 2;
+        store_piece<T, kWide * sizeof(T)>(v, staging[e], base + row0 * ld + col, ld, rows_left, left, aligned);
+    };
+    float v[kWide];
+    if constexpr (MODE == kGatedForward) {
+        float up[kWide];
+        sum(piece >> 1 << 1, (piece & 1) * kWide, v);
+        sum((piece >> 1 << 1) + 1, (piece & 1) * kWide, up);
+        if (p.gu) {
+            T *gu = static_cast<T *>(p.gu);
+            put(v, gu, 2 * static_cast<int64_t>(p.cols));
+            put(up, gu + p.cols, 2 * static_cast<int64_t>(p.cols));
+        }
+#pragma unroll
+        for (int i = 0; i < kWide; ++i) v[i] = activate1<ACT>(v[i]) * up[i];
+    } else {
+        sum(piece >> 1, (piece & 1) * kWide, v);
+    }
+    put(v, out, p.ld);
+}
+
 // A matrix of `rows` rows and `cols` columns, `row` elements apart (a multiple of 8), read in boxes of 64 columns and `box` rows; zeros outside.
 cudaError_t make_map(CUtensorMap *map, int dtype, const void *base, int64_t rows, int64_t cols, int64_t row, int box) {
     return encode_map(map, dtype == PATDNN_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, cols, rows, row * 2, 64, box,
                       CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-// f(T{}, std::integral_constant<int, ACT>): the gradients' products have no activation
+// f(product, join): the gradients' products have no activation
 template <typename F> cudaError_t by_kernel(int mode, int dtype, int act, F f) {
     auto go = [&](auto t) {
         using T = decltype(t);
-        if (mode == kGatedInput) return f(gated_kernel<kGatedInput, T, PATDNN_ACT_NONE>);
-        if (mode == kGatedWeights) return f(gated_kernel<kGatedWeights, T, PATDNN_ACT_NONE>);
-        return by_act(act, [&](auto a) { return f(gated_kernel<kGatedForward, T, a.value>); });
+        if (mode == kGatedInput) return f(gated_kernel<kGatedInput, T, PATDNN_ACT_NONE>, gated_join_kernel<kGatedInput, T, PATDNN_ACT_NONE>);
+        if (mode == kGatedWeights) return f(gated_kernel<kGatedWeights, T, PATDNN_ACT_NONE>, gated_join_kernel<kGatedWeights, T, PATDNN_ACT_NONE>);
+        return by_act(act, [&](auto a) { return f(gated_kernel<kGatedForward, T, a.value>, gated_join_kernel<kGatedForward, T, a.value>); });
     };
     return dtype == PATDNN_F16 ? go(__half{}) : go(__nv_bfloat16{});
 }
@@ -327,28 +364,29 @@ cudaError_t prepare_gated() {
     for (int dtype : {PATDNN_F16, PATDNN_BF16})
         for (int mode : {kGatedForward, kGatedInput, kGatedWeights})
             for (int act : {PATDNN_ACT_NONE, PATDNN_ACT_RELU, PATDNN_ACT_SILU}) {
-                const cudaError_t e = by_kernel(mode, dtype, act, [](auto kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
+                const cudaError_t e = by_kernel(mode, dtype, act, [](auto kernel, auto) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
                 if (e != cudaSuccess) return e;
             }
     return cudaSuccess;
 }
 
-cudaError_t launch_gated(const GatedShape &s, const GatedCall &c, const GatedWork &w, int mode, cudaStream_t st) {
+cudaError_t launch_gated(const GatedShape &s, const GatedCall &c, const GatedWork &w, int mode, cudaStream_t st, int *launches) {
     const GatedPlan plan = plan_gated(s.F, s.K, c.rows, mode);
     const int padded = gated_padded(s.F);
     GatedParams p{};
     p.m_tiles = plan.m_tiles; p.n_tiles = plan.n_tiles; p.k_blocks = plan.k_blocks; p.splits = plan.splits; p.per_split = plan.per_split; p.stages = plan.stages;
-    p.partial = w.partial; p.arrivals = w.arrivals; p.status = w.status; p.spin_limit = c.spin_limit; p.test_skip_load = c.test_skip_load;
+    p.partial = w.partial; p.status = w.status; p.spin_limit = c.spin_limit; p.test_skip_load = c.test_skip_load;
     CUtensorMap a, b0, b1;
     cudaError_t e;
+    p.box_rows = mode == kGatedWeights ? 128 : static_cast<int>(std::min<int64_t>(128, c.rows));
     if (mode == kGatedForward) {
         p.out0 = c.h; p.gu = c.gu; p.rows = c.rows; p.ld = s.h_row; p.cols = s.F;
-        e = make_map(&a, s.dtype, c.x, c.rows, s.K, c.x_row, 128);
+        e = make_map(&a, s.dtype, c.x, c.rows, s.K, c.x_row, p.box_rows);
         if (e == cudaSuccess) e = make_map(&b0, s.dtype, c.wg, s.F, s.K, c.w_row, 128);
         if (e == cudaSuccess) e = make_map(&b1, s.dtype, c.wu, s.F, s.K, c.w_row, 128);
     } else if (mode == kGatedInput) {
         p.out0 = c.dx; p.rows = c.rows; p.ld = s.x_row; p.cols = s.K; p.f_blocks = padded / 64;
-        e = make_map(&a, s.dtype, w.dgu, c.rows, 2 * static_cast<int64_t>(padded), 2 * static_cast<int64_t>(padded), 128);
+        e = make_map(&a, s.dtype, w.dgu, c.rows, 2 * static_cast<int64_t>(padded), 2 * static_cast<int64_t>(padded), p.box_rows);
         if (e == cudaSuccess) e = make_map(&b0, s.dtype, c.wg, s.F, s.K, c.w_row, 64);
         if (e == cudaSuccess) e = make_map(&b1, s.dtype, c.wu, s.F, s.K, c.w_row, 64);
     } else {
@@ -358,7 +396,12 @@ cudaError_t launch_gated(const GatedShape &s, const GatedCall &c, const GatedWor
         b1 = b0;
     }
     if (e != cudaSuccess) return e;
-    return by_kernel(mode, s.dtype, s.act, [&](auto kernel) { return launch_pdl(kernel, dim3(plan.grid), dim3(kThreads), plan.smem, st, 2, a, b0, b1, p); });
+    *launches = plan.splits > 1 ? 2 : 1;
+    return by_kernel(mode, s.dtype, s.act, [&](auto product, auto join) {
+        const cudaError_t r = launch_pdl(product, dim3(plan.grid), dim3(kThreads), plan.smem, st, 2, a, b0, b1, p);
+        if (r != cudaSuccess || plan.splits == 1) return r;
+        return launch_pdl(join, dim3(plan.m_tiles * plan.n_tiles * (mode == kGatedForward ? 8 : 16)), dim3(256), 0, st, 1, p);
+    });
 }
 
 }  // namespace patdnn
