@@ -5,7 +5,8 @@
 //   or a NaN gets the scale NaN (255): all its values read back as NaN.  A block of zeros has scale 2^-127.
 //
 // Memory bound: sizeof(T) bytes read and 129/128 written per element.  A warp takes 512 columns of four rows 32 apart, whose 16 scale bytes are
-// neighbours in memory: 8 loads of 16 bytes in flight per lane (16-bit types), and scales stored as words.
+// neighbours in memory: 8 loads of 16 bytes in flight per lane (16-bit types), and scales stored 16 bytes at a time.  Small matrices are spread
+// over four times the warps, one row each.
 #include "feed_forward.hpp"
 
 #include <algorithm>
@@ -25,30 +26,31 @@ struct Mx8Args {
     int col_tiles, groups;
 };
 
-template <typename T, int A>
+// ROWS: of a row set that a warp takes, 4 or 1
+template <typename T, int A, int ROWS>
 __global__ void __launch_bounds__(kWarps * 32) mx8_quantize_kernel(Mx8Args a, unsigned units) {
     pdl_trigger();
-    const unsigned unit = blockIdx.x * kWarps + (threadIdx.x >> 5);    // (row set, group of columns)
+    const unsigned unit = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);   // (row or row set, group of columns)
     if (unit >= units) return;
     const int lane = threadIdx.x & 31;
     const int group = static_cast<int>(unit % static_cast<unsigned>(a.groups));
-    const int64_t set = unit / static_cast<unsigned>(a.groups), rt = set >> 5;
-    const int r0 = static_cast<int>(set & 31);
+    const int64_t set = unit / static_cast<unsigned>(a.groups), rt = ROWS == 4 ? set >> 5 : set >> 7;
+    const int r0 = static_cast<int>(ROWS == 4 ? set & 31 : set & 127); // its first row in the row tile
     const int64_t c0 = static_cast<int64_t>(group) * kColumns;
     const int left = static_cast<int>(min(static_cast<int64_t>(kColumns), a.cols - c0));
     const int padded = (left + 127) & ~127;
     pdl_wait();
-    Strip<T, A, 16> raw[4];
+    Strip<T, A, 16> raw[ROWS];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < ROWS; ++k) {
         const int64_t row = rt * 128 + r0 + 32 * k;
         if (row < a.rows) raw[k].load(static_cast<const T *>(a.x) + row * a.ld + c0, left);
     }
     constexpr int PER = A == 8 ? 1 : 4 / A, BLOCKS = 16 / A / PER;     // accesses to a block; blocks that a lane knows (A = 8: every other one)
     uint8_t *codes = a.mx + (rt * a.col_tiles + static_cast<int64_t>(group) * 4) * kMx8Tile;
-    uint32_t words[4];
+    uint32_t words[ROWS];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < ROWS; ++k) {
         words[k] = 0;
         if (rt * 128 + r0 + 32 * k >= a.rows) continue;                // (the same for the warp)
         float v[16];
@@ -73,29 +75,41 @@ __global__ void __launch_bounds__(kWarps * 32) mx8_quantize_kernel(Mx8Args a, un
             }
         }
     }
-    if (lane == 0)                                     // (the words of rows that do not exist belong to nothing)
-        *reinterpret_cast<uint4 *>(a.mx + a.scales_at + (rt * a.groups + group) * kMx8Scales + r0 * 16) = make_uint4(words[0], words[1], words[2], words[3]);
+    if (lane == 0) {                                   // (the words of rows that do not exist belong to nothing)
+        uint8_t *scales = a.mx + a.scales_at + (rt * a.groups + group) * kMx8Scales + mx8_scale_place(r0, 0);
+        if constexpr (ROWS == 4) *reinterpret_cast<uint4 *>(scales) = make_uint4(words[0], words[1], words[2], words[3]);
+        else *reinterpret_cast<uint32_t *>(scales) = words[0];
+    }
 }
 
-template <typename T, int A>
+template <typename T, int A, int ROWS>
 __global__ void __launch_bounds__(kWarps * 32) mx8_dequantize_kernel(Mx8Args a, T *out, unsigned units) {
     pdl_trigger();
-    const unsigned unit = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const unsigned unit = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
     if (unit >= units) return;
     const int lane = threadIdx.x & 31;
     const int group = static_cast<int>(unit % static_cast<unsigned>(a.groups));
-    const int64_t set = unit / static_cast<unsigned>(a.groups), rt = set >> 5;
-    const int r0 = static_cast<int>(set & 31);
+    const int64_t set = unit / static_cast<unsigned>(a.groups), rt = ROWS == 4 ? set >> 5 : set >> 7;
+    const int r0 = static_cast<int>(ROWS == 4 ? set & 31 : set & 127); // its first row in the row tile
     const int64_t c0 = static_cast<int64_t>(group) * kColumns;
     const int left = static_cast<int>(min(static_cast<int64_t>(kColumns), a.cols - c0));
     const uint8_t *codes = a.mx + (rt * a.col_tiles + static_cast<int64_t>(group) * 4) * kMx8Tile;
     pdl_wait();
-    const uint4 scales = *reinterpret_cast<const uint4 *>(a.mx + a.scales_at + (rt * a.groups + group) * kMx8Scales + r0 * 16);
-    const uint32_t words[4] = {scales.x, scales.y, scales.z, scales.w};
+    const uint8_t *scales = a.mx + a.scales_at + (rt * a.groups + group) * kMx8Scales + mx8_scale_place(r0, 0);
+    uint32_t words[ROWS];
+    if constexpr (ROWS == 4) {
+        const uint4 four = *reinterpret_cast<const uint4 *>(scales);
+        words[0] = four.x;
+        words[1] = four.y;
+        words[2] = four.z;
+        words[3] = four.w;
+    } else {
+        words[0] = *reinterpret_cast<const uint32_t *>(scales);
+    }
     constexpr int NA = 16 / A;
-    uint32_t raw[4][NA][A == 8 ? 2 : 1];
+    uint32_t raw[ROWS][NA][A == 8 ? 2 : 1];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < ROWS; ++k) {
         if (rt * 128 + r0 + 32 * k >= a.rows) continue;
 #pragma unroll
         for (int j = 0; j < NA; ++j) {
@@ -112,7 +126,7 @@ __global__ void __launch_bounds__(kWarps * 32) mx8_dequantize_kernel(Mx8Args a, 
         }
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < ROWS; ++k) {
         const int64_t row = rt * 128 + r0 + 32 * k;
         if (row >= a.rows) continue;
         Strip<T, A, 16> s;
@@ -140,28 +154,34 @@ Mx8Args args_of(const Mx8Shape &m, const void *x, int64_t ld, void *mx) {
     a.col_tiles = static_cast<int>(m.col_tiles); a.groups = static_cast<int>(m.groups);
     return a;
 }
-// row sets (rows r, r + 32, r + 64, r + 96 of a row tile) times groups of columns; at most 2^24 row tiles of 32 sets and ... of 2^40 elements
-int64_t units_of(const Mx8Shape &m) {
-    const int64_t last = m.rows - (m.row_tiles - 1) * 128;
-    return ((m.row_tiles - 1) * 32 + std::min<int64_t>(32, last)) * m.groups;
+// f(rows of a warp, units, CTAs, warps of a CTA).  Units are row sets (rows r, r + 32, r + 64, r + 96 of a row tile), or rows where sets would be
+// fewer than two warps per scheduler; times groups of columns.  (2^40 elements in rows of one column are 2^29 sets.)
+template <typename F> cudaError_t by_units(const Mx8Shape &m, F f) {
+    const int64_t last = m.rows - (m.row_tiles - 1) * 128, sets = ((m.row_tiles - 1) * 32 + std::min<int64_t>(32, last)) * m.groups;
+    if (sets >= static_cast<int64_t>(sm_count()) * 8) return f(std::integral_constant<int, 4>{}, static_cast<unsigned>(sets), dim3(static_cast<unsigned>(ceil_div(sets, kWarps))), dim3(kWarps * 32));
+    const int64_t rows = m.rows * m.groups;
+    const int warps = rows >= static_cast<int64_t>(sm_count()) * 8 ? 8 : rows >= static_cast<int64_t>(sm_count()) * 4 ? 4 : 2;
+    return f(std::integral_constant<int, 1>{}, static_cast<unsigned>(rows), dim3(static_cast<unsigned>(ceil_div(rows, warps))), dim3(warps * 32));
 }
 
 }  // namespace
 
 cudaError_t launch_mx8_quantize(const Mx8Shape &m, const void *x, int dtype, int64_t ld, void *mx, cudaStream_t st) {
     const Mx8Args a = args_of(m, x, ld, mx);
-    const unsigned units = static_cast<unsigned>(units_of(m));
     return by_strip(dtype, strip_width(dtype, {x}, {ld}), [&](auto t, auto v) {
-        return launch_pdl(mx8_quantize_kernel<decltype(t), v.value>, dim3((units + kWarps - 1) / kWarps), dim3(kWarps * 32), 0, st, 1, a, units);
+        return by_units(m, [&](auto rows, unsigned units, dim3 grid, dim3 block) {
+            return launch_pdl(mx8_quantize_kernel<decltype(t), v.value, rows.value>, grid, block, 0, st, 1, a, units);
+        });
     });
 }
 
 cudaError_t launch_mx8_dequantize(const Mx8Shape &m, const void *mx, void *out, int dtype, int64_t ld, cudaStream_t st) {
     const Mx8Args a = args_of(m, nullptr, ld, const_cast<void *>(mx));
-    const unsigned units = static_cast<unsigned>(units_of(m));
     return by_strip(dtype, strip_width(dtype, {out}, {ld}), [&](auto t, auto v) {
         using T = decltype(t);
-        return launch_pdl(mx8_dequantize_kernel<T, v.value>, dim3((units + kWarps - 1) / kWarps), dim3(kWarps * 32), 0, st, 1, a, static_cast<T *>(out), units);
+        return by_units(m, [&](auto rows, unsigned units, dim3 grid, dim3 block) {
+            return launch_pdl(mx8_dequantize_kernel<T, v.value, rows.value>, grid, block, 0, st, 1, a, static_cast<T *>(out), units);
+        });
     });
 }
 

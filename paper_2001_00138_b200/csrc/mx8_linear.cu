@@ -8,16 +8,12 @@
 // rows persistent CTAs walk over tiles of 128 rows x 256 outputs.
 #include "feed_forward.hpp"
 
-#include <cooperative_groups.h>
-
 #include <algorithm>
 
 #include "linear_device.cuh"
 #include "mx8_device.cuh"
 
 namespace patdnn {
-
-namespace cg = cooperative_groups;
 
 namespace {
 
@@ -37,11 +33,10 @@ __device__ __forceinline__ void umma_mx8(uint32_t d, uint64_t da, uint64_t db, u
         ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
 }
 // One tile of 128 weights rows x tile_n rows of x per CTA; the column tiles cut into `splits` ranges, one CTA of a cluster each.
-// X = void: the rows of x are 8-bit.  Otherwise they are elements of X, at most kFusedRows of them, and warps 2 to 7 quantise them
-// into the ring themselves, a column tile at a time each: one launch less.
-template <typename X>
+// kFused: the rows of x are elements of T, at most kFusedRows of them, and warps 2 to 7 quantise them into the ring themselves, a column tile at
+// a time each: one launch less.  Otherwise they are 8-bit.
+template <typename T, int ACT, bool kFused>
 __global__ void __launch_bounds__(kLinThreads, 1) mx8_linear_kernel(Mx8Params p) {
-    constexpr bool kFused = !std::is_same<X, void>::value;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 1];
     __shared__ uint32_t tmem_slot;
@@ -143,25 +138,25 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx8_linear_kernel(Mx8Params p)
         if (leader) umma_commit(done);
     } else if constexpr (kFused) {
         constexpr int kProducers = kLinThreads / 32 - 2;
-        const X *x = static_cast<const X *>(p.x_raw);
-        const bool vector = (reinterpret_cast<uintptr_t>(x) | static_cast<uint64_t>(p.ldx * sizeof(X))) % (4 * sizeof(X)) == 0;
+        const T *x = static_cast<const T *>(p.x_raw);
+        const bool vector = (reinterpret_cast<uintptr_t>(x) | static_cast<uint64_t>(p.ldx * sizeof(T))) % (4 * sizeof(T)) == 0;
         const int rows = static_cast<int>(p.rows);
         pdl_wait();
         for (int i = warp - 2; i < iters; i += kProducers) {
             const int slot = i % p.stages, turn = i / p.stages;
             const int64_t c = static_cast<int64_t>(t0 + i) * 128 + lane * 4;
             const int count = static_cast<int>(max(int64_t(0), min(int64_t(4), p.K - c)));
-            Pack<X, 4> raw[kFusedRows];
+            Pack<T, 4> raw[kFusedRows];
 #pragma unroll
             for (int r = 0; r < kFusedRows; ++r) {
-                const X *src = x + r * p.ldx + c;
+                const T *src = x + r * p.ldx + c;
                 if (vector && count == 4 && r < rows) {
                     raw[r].load(src);
                 } else {
-                    X v[4];
+                    T v[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = r < rows && e < count ? src[e] : from_float<X>(0.f);
-                    raw[r] = narrow<X, 4>(Fv<4>::make([&](int e) { return to_float(v[e]); }));
+                    for (int e = 0; e < 4; ++e) v[e] = r < rows && e < count ? src[e] : from_float<T>(0.f);
+                    raw[r] = narrow<T, 4>(Fv<4>::make([&](int e) { return to_float(v[e]); }));
                 }
             }
             if (turn > 0 && !warp_wait(empty + 8 * slot, (turn - 1) & 1, ctx, 105)) break;
@@ -169,7 +164,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx8_linear_kernel(Mx8Params p)
 #pragma unroll
             for (int r = 0; r < kFusedRows; ++r) {
                 if (r >= rows) break;
-                const Fv<4> f = widen<X, 4>(raw[r]);
+                const Fv<4> f = widen<T, 4>(raw[r]);
                 const float v[4] = {f.get(0), f.get(1), f.get(2), f.get(3)};
                 const uint32_t top = __reduce_max_sync(0xffffffffu, magnitude_bits(max_abs(max_abs(v[0], v[1]), max_abs(v[2], v[3]))));
                 float inverse;
@@ -186,49 +181,50 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx8_linear_kernel(Mx8Params p)
     pdl_wait();
     const bool ok = mbar_wait(done, 0, ctx, 104);
     tc_fence_after();
-    const int f = ft * 128 + (warp & 3) * 32 + lane;
+    const int place = (warp & 3) * 32 + lane, f = ft * 128 + place;      // lanes are outputs: a warp stores 32 consecutive ones of a row
     const float bias = p.bias && f < p.F ? p.bias[f] : 0.f;
     const int64_t row0 = static_cast<int64_t>(nt) * p.tile_n;
+    const int rows = static_cast<int>(min(static_cast<int64_t>(p.tile_n), p.rows - row0));
     const uint32_t lanes = tmem + ((warp & 3) * 32u << 16);
+    T *const y = static_cast<T *>(p.y) + row0 * p.ldy + f;
     if (p.splits == 1) {
-        for (int c = (warp >> 2) * 16; c < p.tile_n; c += 32) {
+        for (int c = (warp >> 2) * 16; c < rows; c += 32) {
             uint32_t v[16];
             tmem_ld16(lanes + c, v);
             if (ok && f < p.F) {
+                T *to = y + c * p.ldy;
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (row0 + c + j < p.rows)
-                        store_out(p.y, (row0 + c + j) * p.ldy + f, activate(__uint_as_float(v[j]) + bias, p.act), p.dtype);
+                for (int j = 0; j < 16; ++j, to += p.ldy)
+                    if (c + j < rows) *to = from_float<T>(activate1<ACT>(__uint_as_float(v[j]) + bias));
             }
         }
     } else {
         // every CTA of the cluster finishes the columns j with j % splits == its rank: partial sums are pushed into its shared memory
         // and added in rank order
-        float *slots = reinterpret_cast<float *>(smem_raw + (smem - smem_u32(smem_raw)));
         const int shift = 31 - __clz(p.splits), owned = (p.tile_n + p.splits - 1) >> shift;      // splits is a power of two
-        cg::cluster_group cluster = cg::this_cluster();
-        cluster.sync();                                                  // all pipelines are idle: their memory can be reused
-        for (int c = (warp >> 2) * 16; c < p.tile_n; c += 32) {
+        pair_barrier();                                                  // all pipelines are idle: their memory can be reused
+        const uint32_t slots = smem + (rank * owned * 128 + place) * 4;
+        for (int c = (warp >> 2) * 16; c < rows; c += 32) {
             uint32_t v[16];
             tmem_ld16(lanes + c, v);
 #pragma unroll
             for (int j = 0; j < 16; ++j)
-                if (row0 + c + j < p.rows) {
-                    float *to = cluster.map_shared_rank(slots, (c + j) & (p.splits - 1));
-                    to[(rank * owned + ((c + j) >> shift)) * 128 + (warp & 3) * 32 + lane] = iters ? __uint_as_float(v[j]) : 0.f;
-                }
+                if (c + j < rows)
+                    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cta(slots + ((c + j) >> shift) * 512, j & (p.splits - 1))), "r"(iters ? v[j] : 0u) : "memory");
         }
-        cluster.sync();
-        if (ok && f < p.F)
-            for (int j = (warp >> 2); j < owned; j += 2) {
-                const int64_t row = row0 + (j << shift) + rank;
-                if ((j << shift) + rank >= p.tile_n || row >= p.rows) break;
-                float s = 0.f;
+        pair_barrier();
+        if (ok && f < p.F) {
+            const float *from = reinterpret_cast<const float *>(smem_raw + (smem - smem_u32(smem_raw))) + place;
+            const int mine = (rows - rank + p.splits - 1) >> shift;      // of the owned columns, those that are rows of x
+#pragma unroll 4
+            for (int j = warp >> 2; j < mine; j += 2) {
+                float sum = 0.f;
 #pragma unroll
                 for (int r = 0; r < 8; ++r)
-                    if (r < p.splits) s += slots[(r * owned + j) * 128 + (warp & 3) * 32 + lane];
-                store_out(p.y, row * p.ldy + f, activate(s + bias, p.act), p.dtype);
+                    if (r < p.splits) sum += from[(r * owned + j) * 128];
+                y[((j << shift) + rank) * p.ldy] = from_float<T>(activate1<ACT>(sum + bias));
             }
+        }
     }
     tc_fence_before();
     __syncthreads();
@@ -432,14 +428,13 @@ cudaError_t scales_map(CUtensorMap *map, const uint8_t *base, int64_t row_tiles,
 
 cudaError_t prepare_mx8_linear() {
     const cudaFuncAttribute what = cudaFuncAttributeMaxDynamicSharedMemorySize;
-    cudaError_t e = cudaFuncSetAttribute(mx8_linear_kernel<void>, what, kLinearSmem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(mx8_linear_kernel<float>, what, kLinearSmem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(mx8_linear_kernel<__half>, what, kLinearSmem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(mx8_linear_kernel<__nv_bfloat16>, what, kLinearSmem);
+    cudaError_t e = cudaSuccess;
     for (int dtype = 0; dtype < 3 && e == cudaSuccess; ++dtype)
         for (int act = PATDNN_ACT_NONE; act <= PATDNN_ACT_SILU && e == cudaSuccess; ++act)
             e = by_output(dtype, act, [&](auto t, auto a) {
-                return cudaFuncSetAttribute(mx8_pair_kernel<decltype(t), a.value>, what, kLinearSmem);
+                cudaError_t r = cudaFuncSetAttribute(mx8_pair_kernel<decltype(t), a.value>, what, kLinearSmem);
+                if (r == cudaSuccess) r = cudaFuncSetAttribute(mx8_linear_kernel<decltype(t), a.value, false>, what, kLinearSmem);
+                return r == cudaSuccess ? cudaFuncSetAttribute(mx8_linear_kernel<decltype(t), a.value, true>, what, kLinearSmem) : r;
             });
     return e;
 }
@@ -504,9 +499,10 @@ cudaError_t launch_mx8_linear(Mx8Params p, cudaStream_t st, int *launches) {
             return launch_pdl(mx8_pair_kernel<decltype(t), a.value>, dim3(l.grid), dim3(kRowsThreads), l.smem, st, 2, maps, p);
         });
     }
-    const auto kernel = !p.x_raw ? mx8_linear_kernel<void> : p.dtype == PATDNN_F32 ? mx8_linear_kernel<float>
-                        : p.dtype == PATDNN_F16 ? mx8_linear_kernel<__half> : mx8_linear_kernel<__nv_bfloat16>;
-    return launch_pdl(kernel, dim3(l.grid), dim3(kLinThreads), l.smem, st, p.splits, p);
+    return by_output(p.dtype, p.act, [&](auto t, auto a) {
+        const auto kernel = p.x_raw ? mx8_linear_kernel<decltype(t), a.value, true> : mx8_linear_kernel<decltype(t), a.value, false>;
+        return launch_pdl(kernel, dim3(l.grid), dim3(kLinThreads), l.smem, st, p.splits, p);
+    });
 }
 
 }  // namespace patdnn
