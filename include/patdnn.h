@@ -500,6 +500,8 @@ typedef struct {
     int32_t grid;                       /* CTAs */
     int32_t stages;                     /* blocks in the ring of copies */
     int32_t smem_bytes;                 /* dynamic shared memory of a CTA */
+    int32_t tensor_columns;             /* columns of tensor memory that a CTA allocates */
+    int32_t few_rows;                   /* 1: the kernel that streams the weights, column tiles of 64 outputs; 0: pairs of CTAs */
 } patdnn_gated_plan_info;
 PATDNN_API int patdnn_gated_plan(int32_t F, int32_t K, int64_t rows, int32_t product, patdnn_gated_plan_info *info);
 PATDNN_API int patdnn_gated_free(patdnn_gated h);

@@ -92,7 +92,8 @@ class _GatedDesc(ctypes.Structure):
 
 
 class _GatedPlan(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int32) for n in ("row_tiles", "column_tiles", "blocks", "splits", "blocks_per_split", "grid", "stages", "smem_bytes")]
+    _fields_ = [(n, ctypes.c_int32) for n in ("row_tiles", "column_tiles", "blocks", "splits", "blocks_per_split", "grid", "stages", "smem_bytes",
+                                               "tensor_columns", "few_rows")]
 
 
 class _LinearPlan(ctypes.Structure):

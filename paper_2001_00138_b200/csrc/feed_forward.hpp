@@ -94,6 +94,9 @@ struct GatedPlan {
     int m_tiles, n_tiles;                   // tiles of 256 rows, and of 256 columns of the product (forward: 128 outputs, gate and up)
     int k_blocks, splits, per_split;        // blocks of 64 along the summed dimension; ranges of them that share a tile; blocks of a range
     int grid, stages, smem;                 // CTAs; blocks in the ring of copies; dynamic shared memory
+    int tensor_columns;                     // of tensor memory that a CTA allocates
+    bool few;                               // forward, few rows: n_tiles of 64 outputs, tiles of tile_n rows, splits in a cluster
+    int tile_n;
 };
 GatedPlan plan_gated(int F, int K, int64_t rows, int mode);
 constexpr int kGatedUnitFloats = 256 * 256; // partial sums of a (tile, split) unit

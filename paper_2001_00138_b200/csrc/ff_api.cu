@@ -439,6 +439,7 @@ int patdnn_gated_plan(int32_t F, int32_t K, int64_t rows, int32_t product, patdn
     *info = patdnn_gated_plan_info{};
     info->row_tiles = p.m_tiles; info->column_tiles = p.n_tiles; info->blocks = p.k_blocks; info->splits = p.splits; info->blocks_per_split = p.per_split;
     info->grid = p.grid; info->stages = p.stages; info->smem_bytes = p.smem;
+    info->few_rows = p.few; info->tensor_columns = p.tensor_columns;
     return PATDNN_OK;
 }
 

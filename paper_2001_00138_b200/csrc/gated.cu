@@ -9,6 +9,7 @@
 // outer one (wg and wu for dx; dg, du and x for dwg, dwu) the MMAs read the tiles as they lie, transposed (MN-major), so nothing is ever
 // transposed in memory.  Persistent: warp 0 copies, warp 1 of the pair's first CTA multiplies, warps 4 to 11 drain one accumulator (two, of
 // 256 columns each, fill tensor memory) while the other one is summed.
+// Forward of up to 128 rows: another kernel streams the weights, which are then the M operand (see there).
 // Few tiles: the summed dimension is cut into ranges whose partial sums go to memory, and a second kernel adds them in the ranges' order.
 #include <algorithm>
 
@@ -321,6 +322,140 @@ __global__ void __launch_bounds__(256) gated_join_kernel(const GatedParams p) {
     put(v, out, p.ld);
 }
 
+// ---- forward, few rows -----------------------------------------------------------------------------------------------------
+// The weights are the M operand, 64 rows of wg and the same 64 of wu in a tile, the rows of x the N operand (16 to 128): a CTA per 64 outputs and
+// range of the summed dimension, whose weights it streams.  The CTAs of a cluster share a tile; their partial sums are pushed into the shared
+// memory of the one that finishes a row of x, where g and u of an output meet.
+constexpr int kRowsThreads = 256;
+constexpr int kMostRowsStages = 12;
+
+struct GatedRowsParams {
+    void *h, *gu;
+    int64_t ldh;
+    int rows, F, k_blocks, per_split, splits, stages, tile_n, tensor_columns;
+    int *status;
+    uint32_t spin_limit;
+    int test_skip_load;
+};
+
+__device__ __forceinline__ void tile_load_own(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+
+template <typename T, int ACT>
+__global__ void __launch_bounds__(kRowsThreads, 1)
+gated_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_u, const GatedRowsParams p) {
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ __align__(8) unsigned long long bars[2 * kMostRowsStages + 1];
+    __shared__ uint32_t tmem_slot;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const int rank = blockIdx.x % p.splits, f0 = blockIdx.x / p.splits * 64;
+    const WaitCtx ctx{p.status, p.spin_limit ? p.spin_limit : kSpinLimit};
+    const uint32_t smem = (smem_u32(smem_raw) + 1023) & ~1023u;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * kMostRowsStages, done = empty + 8 * kMostRowsStages;
+    const uint32_t stage_bytes = kHalf + p.tile_n * 128;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        mbar_init(done, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) tmem_allocate(&tmem_slot, p.tensor_columns);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_trigger();                                     // not before the allocation: see kernels.hpp
+    const uint32_t tmem = tmem_slot;
+    pdl_wait();
+
+    const int k0 = rank * p.per_split, k1 = min(p.k_blocks, k0 + p.per_split);
+    if (warp == 0) {
+        const bool leader = elect_one();
+        int slot = 0, issued = 0;
+        uint32_t phase = 1;                            // (the first pass over the ring does not wait)
+        for (int k = k0; k < k1; ++k) {
+            if (issued >= p.stages && !warp_wait(empty + 8 * slot, phase, ctx, 141)) break;
+            if (leader && issued + 1 != p.test_skip_load) {
+                const uint32_t at = smem + slot * stage_bytes, bar = full + 8 * slot;
+                mbar_expect_tx(bar, kHalf + p.rows * 128);             // (rows that do not exist are whatever is there: their sums are not read)
+                tile_load_own(at, &map_g, bar, k * 64, f0);
+                tile_load_own(at + kHalf / 2, &map_u, bar, k * 64, f0);
+                tile_load_own(at + kHalf, &map_x, bar, k * 64, 0);
+            }
+            ++issued;
+            if (++slot == p.stages) { slot = 0; phase ^= 1; }
+        }
+        // no copy may still be in flight when the CTA ends, whatever happened to the other roles
+        for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait(full + 8 * (i % p.stages), (i / p.stages) & 1, ctx, 142);
+    } else if (warp == 1) {
+        const bool leader = elect_one();
+        const uint32_t idesc = instr_desc(std::is_same<T, __nv_bfloat16>::value ? 1 : 0, p.tile_n);
+        const uint64_t da0 = smem_desc_sw128(smem), db0 = smem_desc_sw128(smem + kHalf);
+        int slot = 0;
+        uint32_t phase = 0, accumulate = 0;
+        for (int k = k0; k < k1; ++k) {
+            if (!warp_wait(full + 8 * slot, phase, ctx, 143)) break;
+            tc_fence_after();
+            if (leader) {
+                const uint64_t shift = static_cast<uint64_t>(slot) * (stage_bytes >> 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) umma_f16(tmem, da0 + shift + 2 * j, db0 + shift + 2 * j, idesc, accumulate | j);
+                umma_commit(empty + 8 * slot);
+            }
+            __syncwarp();
+            accumulate = 1;
+            if (++slot == p.stages) { slot = 0; phase ^= 1; }
+        }
+        if (leader) umma_commit(done);
+    }
+    __syncwarp();
+    const bool ok = mbar_wait(done, 0, ctx, 144);
+    tc_fence_after();
+    // CTA r of the cluster finishes the rows j with j % splits == r
+    const int shift = 31 - __clz(p.splits), owned = (p.tile_n + p.splits - 1) >> shift;          // splits is a power of two
+    const int place = (warp & 3) * 32 + lane;
+    pair_barrier();                                    // all pipelines of the cluster are idle: their memory can be reused
+    const uint32_t slots = smem + (rank * owned * 128 + place) * 4, lanes = tmem + ((warp & 3) * 32u << 16);
+    for (int c = (warp >> 2) * 16; c < p.rows; c += 32) {
+        uint32_t v[16];
+        tmem_ld16(lanes + c, v);
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (c + j < p.rows)
+                asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cta(slots + ((c + j) >> shift) * 512, j & (p.splits - 1))), "r"(k1 > k0 ? v[j] : 0u) : "memory");
+    }
+    pair_barrier();
+    const int f = threadIdx.x & 63;
+    if (ok && f0 + f < p.F) {
+        const float *from = reinterpret_cast<const float *>(smem_raw + (smem - smem_u32(smem_raw))) + f;
+        const int mine = (p.rows - rank + p.splits - 1) >> shift;
+#pragma unroll 2
+        for (int j = threadIdx.x >> 6; j < mine; j += kRowsThreads / 64) {
+            float g = 0.f, up = 0.f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < p.splits) {
+                    g += from[(r * owned + j) * 128];
+                    up += from[(r * owned + j) * 128 + 64];
+                }
+            const int64_t row = (j << shift) + rank;
+            if (p.gu) {
+                T *gu = static_cast<T *>(p.gu) + row * 2 * p.F + f0 + f;
+                gu[0] = from_float<T>(g);
+                gu[p.F] = from_float<T>(up);
+            }
+            static_cast<T *>(p.h)[row * p.ldh + f0 + f] = from_float<T>(activate1<ACT>(g) * up);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 2) tmem_free(tmem, p.tensor_columns);
+}
+
 // A matrix of `rows` rows and `cols` columns, `row` elements apart (a multiple of 8), read in boxes of 64 columns and `box` rows; zeros outside.
 cudaError_t make_map(CUtensorMap *map, int dtype, const void *base, int64_t rows, int64_t cols, int64_t row, int box) {
     return encode_map(map, dtype == PATDNN_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, cols, rows, row * 2, 64, box,
@@ -338,12 +473,35 @@ template <typename F> cudaError_t by_kernel(int mode, int dtype, int act, F f) {
     return dtype == PATDNN_F16 ? go(__half{}) : go(__nv_bfloat16{});
 }
 
+template <typename F> cudaError_t by_rows_kernel(int dtype, int act, F f) {
+    return by_act(act, [&](auto a) { return dtype == PATDNN_F16 ? f(gated_rows_kernel<__half, a.value>) : f(gated_rows_kernel<__nv_bfloat16, a.value>); });
+}
+
 }  // namespace
 
 int units_most() { return std::max(1, sm_count() / 2); }
 
 GatedPlan plan_gated(int F, int K, int64_t rows, int mode) {
     GatedPlan p{};
+    if (mode == kGatedForward && rows <= 128) {
+        p.few = true;
+        p.tile_n = static_cast<int>(ceil_div(rows, 16) * 16);
+        p.m_tiles = 1;
+        p.n_tiles = static_cast<int>(ceil_div(F, 64));
+        p.k_blocks = static_cast<int>(ceil_div(K, 64));
+        p.splits = 1;
+        while (p.splits < 8 && p.n_tiles * p.splits * 2 <= sm_count() && p.k_blocks >= p.splits * 8) p.splits *= 2;
+        p.per_split = static_cast<int>(ceil_div(p.k_blocks, p.splits));
+        p.grid = p.n_tiles * p.splits;
+        const int stage = kHalf + p.tile_n * 128;
+        // more CTAs than SMs: two to an SM
+        p.stages = std::max(1, std::min({kMostRowsStages, p.per_split, (p.grid > sm_count() ? 110 * 1024 : 200 * 1024) / stage}));
+        p.tensor_columns = allocation_of(p.tile_n);
+        const int owned = static_cast<int>(ceil_div(p.tile_n, p.splits));
+        // (shared memory in proportion to tensor memory, see plan_mx4_linear)
+        p.smem = std::max({p.stages * stage + 1024, p.splits * owned * 512 + 1024, kSmemPerSm / 512 * p.tensor_columns - 1024});
+        return p;
+    }
     const int64_t m = mode == kGatedWeights ? 2 * ceil_div(F, 256) : ceil_div(rows, 256);
     p.m_tiles = static_cast<int>(m);
     p.n_tiles = static_cast<int>(mode == kGatedForward ? ceil_div(F, 128) : ceil_div(K, 256));
@@ -357,6 +515,7 @@ GatedPlan plan_gated(int F, int K, int64_t rows, int mode) {
     p.grid = 2 * static_cast<int>(std::min(tiles * p.splits, most));
     p.stages = kMostStages;
     p.smem = kSmem;
+    p.tensor_columns = 512;
     return p;
 }
 
@@ -366,6 +525,8 @@ cudaError_t prepare_gated() {
             for (int act : {PATDNN_ACT_NONE, PATDNN_ACT_RELU, PATDNN_ACT_SILU}) {
                 const cudaError_t e = by_kernel(mode, dtype, act, [](auto kernel, auto) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
                 if (e != cudaSuccess) return e;
+                const cudaError_t r = by_rows_kernel(dtype, act, [](auto kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
+                if (r != cudaSuccess) return r;
             }
     return cudaSuccess;
 }
@@ -373,11 +534,23 @@ cudaError_t prepare_gated() {
 cudaError_t launch_gated(const GatedShape &s, const GatedCall &c, const GatedWork &w, int mode, cudaStream_t st, int *launches) {
     const GatedPlan plan = plan_gated(s.F, s.K, c.rows, mode);
     const int padded = gated_padded(s.F);
+    CUtensorMap a, b0, b1;
+    cudaError_t e;
+    *launches = plan.splits > 1 && !plan.few ? 2 : 1;
+    if (plan.few) {
+        GatedRowsParams p{};
+        p.h = c.h; p.gu = c.gu; p.ldh = s.h_row; p.rows = static_cast<int>(c.rows); p.F = s.F;
+        p.k_blocks = plan.k_blocks; p.per_split = plan.per_split; p.splits = plan.splits; p.stages = plan.stages; p.tile_n = plan.tile_n;
+        p.tensor_columns = plan.tensor_columns; p.status = w.status; p.spin_limit = c.spin_limit; p.test_skip_load = c.test_skip_load;
+        e = make_map(&a, s.dtype, c.x, c.rows, s.K, c.x_row, p.rows);
+        if (e == cudaSuccess) e = make_map(&b0, s.dtype, c.wg, s.F, s.K, c.w_row, 64);
+        if (e == cudaSuccess) e = make_map(&b1, s.dtype, c.wu, s.F, s.K, c.w_row, 64);
+        if (e != cudaSuccess) return e;
+        return by_rows_kernel(s.dtype, s.act, [&](auto kernel) { return launch_pdl(kernel, dim3(plan.grid), dim3(kRowsThreads), plan.smem, st, plan.splits, a, b0, b1, p); });
+    }
     GatedParams p{};
     p.m_tiles = plan.m_tiles; p.n_tiles = plan.n_tiles; p.k_blocks = plan.k_blocks; p.splits = plan.splits; p.per_split = plan.per_split; p.stages = plan.stages;
     p.partial = w.partial; p.status = w.status; p.spin_limit = c.spin_limit; p.test_skip_load = c.test_skip_load;
-    CUtensorMap a, b0, b1;
-    cudaError_t e;
     p.box_rows = mode == kGatedWeights ? 128 : static_cast<int>(std::min<int64_t>(128, c.rows));
     if (mode == kGatedForward) {
         p.out0 = c.h; p.gu = c.gu; p.rows = c.rows; p.ld = s.h_row; p.cols = s.F;
@@ -396,7 +569,6 @@ cudaError_t launch_gated(const GatedShape &s, const GatedCall &c, const GatedWor
         b1 = b0;
     }
     if (e != cudaSuccess) return e;
-    *launches = plan.splits > 1 ? 2 : 1;
     return by_kernel(mode, s.dtype, s.act, [&](auto product, auto join) {
         const cudaError_t r = launch_pdl(product, dim3(plan.grid), dim3(kThreads), plan.smem, st, 2, a, b0, b1, p);
         if (r != cudaSuccess || plan.splits == 1) return r;
