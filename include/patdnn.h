@@ -470,7 +470,7 @@ PATDNN_API int patdnn_linear8_free(patdnn_linear8 h);
  * Errors: E_NULL, E_SHAPE (F, K < 1 or > 2^20, rows < 0 or > max_rows, more than 2^31 - 1 or 2^40 elements, a stride below its row's length or
  * above 2^31, a tensor that is not aligned to its elements, or x, wg or wu with rows that are whole 16-byte units apart and not aligned to 16
  * bytes), E_DTYPE (F16 and BF16 only), E_SCRATCH (a gradient without desc.grad), E_ALLOC, E_CUDA, E_NO_DEVICE (another device is current).
- * A handle owns its workspace (19 MB, and what max_rows needs for gradients and for rows that are not whole 16-byte units apart, which are
+ * A handle owns its workspace (39 MB, and what max_rows needs for gradients and for rows that are not whole 16-byte units apart, which are
  * packed first): calls that can overlap need a handle each, others may share one, whatever their weights.  rows = 0 launches nothing (the
  * gradient writes zeros to dwg and dwu).  patdnn_gated_create waits for the device; the calls are asynchronous on `stream`.
  */
@@ -501,7 +501,7 @@ typedef struct {
     int32_t stages;                     /* blocks in the ring of copies */
     int32_t smem_bytes;                 /* dynamic shared memory of a CTA */
     int32_t tensor_columns;             /* columns of tensor memory that a CTA allocates */
-    int32_t few_rows;                   /* 1: the kernel that streams the weights, column tiles of 64 outputs; 0: pairs of CTAs */
+    int32_t few_rows;                   /* 1: the kernel that streams the weights, tiles of 128 rows and 64 outputs; 0: pairs of CTAs */
 } patdnn_gated_plan_info;
 PATDNN_API int patdnn_gated_plan(int32_t F, int32_t K, int64_t rows, int32_t product, patdnn_gated_plan_info *info);
 PATDNN_API int patdnn_gated_free(patdnn_gated h);

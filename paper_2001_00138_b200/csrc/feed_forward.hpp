@@ -85,7 +85,6 @@ size_t rms_workspace_floats(const RmsShape &s);
 cudaError_t launch_rms_grad(const RmsShape &s, const RmsGradCall &c, cudaStream_t st, int *launches);
 
 // ---- gated feed-forward block (gated.cu, gated_aux.cu) ---------------------------------------------------------------------
-enum GatedMode { kGatedForward = 0, kGatedInput = 1, kGatedWeights = 2 };   // h; dx; dwg and dwu
 struct GatedShape {
     int F, K, act, dtype;                   // dtype: F16 or BF16
     int64_t x_row, w_row, h_row;            // strides in elements
@@ -98,8 +97,11 @@ struct GatedPlan {
     bool few;                               // forward, few rows: n_tiles of 64 outputs, tiles of tile_n rows, splits in a cluster
     int tile_n;
 };
-GatedPlan plan_gated(int F, int K, int64_t rows, int mode);
+GatedPlan plan_gated_forward(int F, int K, int64_t rows);
+// [0] dx, [1] dwg and dwu; one launch, whose grid both have
+void plan_gated_gradient(int F, int K, int64_t rows, bool dx, bool dw, GatedPlan (&plan)[2]);
 constexpr int kGatedUnitFloats = 256 * 256; // partial sums of a (tile, split) unit
+constexpr int kGatedUnits = 2;              // such units that a call may need, per pair of SMs (see plan_gated_gradient)
 struct GatedWork {                          // a handle's buffers
     void *dgu;                              // [max_rows][2 Fp]: dg, du in the handle's type, Fp = F rounded up to 64; nullptr without gradients
     float *partial;
@@ -115,9 +117,10 @@ struct GatedCall {
     uint32_t spin_limit;
     int test_skip_load;
 };
-int units_most();                           // units that run at a time: pairs of SMs
+int pairs_most();                           // pairs of CTAs that run at a time
 cudaError_t prepare_gated();
-cudaError_t launch_gated(const GatedShape &s, const GatedCall &c, const GatedWork &w, int mode, cudaStream_t st, int *launches);
+cudaError_t launch_gated_forward(const GatedShape &s, const GatedCall &c, const GatedWork &w, cudaStream_t st, int *launches);
+cudaError_t launch_gated_gradient(const GatedShape &s, const GatedCall &c, const GatedWork &w, cudaStream_t st, int *launches);   // from dgu
 // rows of a 16-bit matrix to rows `to_row` apart, zeros behind them
 cudaError_t launch_gated_pack(const void *x, int64_t rows, int cols, int64_t row, void *to, int64_t to_row, int dtype, cudaStream_t st);
 // dgu from gu [rows][2 F] and dh

@@ -159,12 +159,6 @@ int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu
     return PATDNN_OK;
 }
 
-int gated_product(patdnn_gated h, const GatedCall &c, int mode, cudaStream_t st) {
-    int n = 0;
-    const cudaError_t e = launch_gated(h->s, c, h->w, mode, st, &n);
-    return launched(e, n, "gated block launch");
-}
-
 }  // namespace
 
 extern "C" {
@@ -371,7 +365,7 @@ int patdnn_gated_create(const patdnn_gated_desc *desc, patdnn_gated *out) {
     const size_t row = static_cast<size_t>(packed_row(s.K));
     uint16_t *dgu = nullptr, *x = nullptr, *weights = nullptr;
     cudaError_t e = cudaGetDevice(&h->device);
-    if (e == cudaSuccess) e = allocate(&h->w.partial, static_cast<size_t>(units_most()) * kGatedUnitFloats);
+    if (e == cudaSuccess) e = allocate(&h->w.partial, static_cast<size_t>(pairs_most()) * kGatedUnits * kGatedUnitFloats);
     if (e == cudaSuccess) e = allocate(&h->w.status, 4);
     if (e == cudaSuccess) e = cudaMemset(h->w.status, 0, 16);
     if (e == cudaSuccess && desc->grad) e = allocate(&dgu, static_cast<size_t>(desc->max_rows) * 2 * gated_padded(s.F));
@@ -400,7 +394,9 @@ int patdnn_gated_run(patdnn_gated h, const void *x, const void *wg, const void *
     GatedCall c{};
     if (const int rc = gated_operands(h, x, wg, wu, rows, c, st)) return rc;
     c.h = hidden; c.gu = gu;
-    return gated_product(h, c, kGatedForward, st);
+    int n = 0;
+    const cudaError_t e = launch_gated_forward(s, c, h->w, st, &n);
+    return launched(e, n, "gated block launch");
 }
 
 int patdnn_gated_grad(patdnn_gated h, const void *x, const void *wg, const void *wu, const void *gu, const void *dh, void *dx, void *dwg, void *dwu,
@@ -425,9 +421,9 @@ int patdnn_gated_grad(patdnn_gated h, const void *x, const void *wg, const void 
     if (const int rc = gated_operands(h, x, wg, wu, rows, c, st)) return rc;
     c.dx = dx; c.dwg = dwg; c.dwu = dwu;
     if (const int rc = launched(launch_gated_slopes(s, gu, dh, h->w.dgu, rows, st), 1, "gated block gradient launch")) return rc;
-    if (dx)
-        if (const int rc = gated_product(h, c, kGatedInput, st)) return rc;
-    return dwg ? gated_product(h, c, kGatedWeights, st) : PATDNN_OK;
+    int n = 0;
+    const cudaError_t e = launch_gated_gradient(s, c, h->w, st, &n);
+    return launched(e, n, "gated block gradient launch");
 }
 
 int patdnn_gated_plan(int32_t F, int32_t K, int64_t rows, int32_t product, patdnn_gated_plan_info *info) {
@@ -435,7 +431,9 @@ int patdnn_gated_plan(int32_t F, int32_t K, int64_t rows, int32_t product, patdn
     if (!size_ok(F, K) || F < 1 || F > kMostColumns || !size_ok(rows, K) || !size_ok(rows, F) || rows < 1 || gated_too_large(rows, F, K) || product < 0 ||
         product > 2)
         return PATDNN_E_SHAPE;
-    const GatedPlan p = plan_gated(F, K, rows, product);
+    GatedPlan gradient[2];
+    plan_gated_gradient(F, K, rows, true, true, gradient);
+    const GatedPlan p = product ? gradient[product - 1] : plan_gated_forward(F, K, rows);
     *info = patdnn_gated_plan_info{};
     info->row_tiles = p.m_tiles; info->column_tiles = p.n_tiles; info->blocks = p.k_blocks; info->splits = p.splits; info->blocks_per_split = p.per_split;
     info->grid = p.grid; info->stages = p.stages; info->smem_bytes = p.smem;

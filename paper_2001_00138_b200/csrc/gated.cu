@@ -9,8 +9,9 @@
 // outer one (wg and wu for dx; dg, du and x for dwg, dwu) the MMAs read the tiles as they lie, transposed (MN-major), so nothing is ever
 // transposed in memory.  Persistent: warp 0 copies, warp 1 of the pair's first CTA multiplies, warps 4 to 11 drain one accumulator (two, of
 // 256 columns each, fill tensor memory) while the other one is summed.
-// Forward of up to 128 rows: another kernel streams the weights, which are then the M operand (see there).
-// Few tiles: the summed dimension is cut into ranges whose partial sums go to memory, and a second kernel adds them in the ranges' order.
+// Forward of few rows: another kernel, whose M operand are the weights (see there).
+// Both products of the gradient are one launch, the tiles of the second filling up what the first leaves of the rounds over the SMs.  Few
+// tiles: the summed dimension is cut into ranges whose partial sums go to memory, and a second kernel adds them in the ranges' order.
 #include <algorithm>
 
 #include "feed_forward.hpp"
@@ -22,24 +23,36 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kEpilogueWarps = 8;
 constexpr int kMostStages = 6;
+constexpr int kMostPairs = 128;
 constexpr int kHalf = 128 * 128;                       // bytes of one CTA's part of an operand in a stage: 128 rows x 64 columns
 constexpr int kStage = 2 * kHalf;
 constexpr int kPiece = 64;                             // bytes of a row that the epilogue stores at a time
 constexpr int kStaging = 32 * kPiece;                  // shared memory of an epilogue warp
-constexpr int kSmem = 226 * 1024;                      // all of an SM's: a pair holds all of two SMs' tensor memory (see plan_mx4_linear)
+// Shared memory that keeps other kernels with tensor memory off the SM (they take 13 KB at least), since a pair holds all of two SMs' tensor memory
+// (see plan_mx4_linear), and leaves the join's CTAs (8 KB) room to arrive before this kernel ends.
+constexpr int kSmem = 217 * 1024;
 
-struct GatedParams {
-    void *out0, *out1, *gu;                            // h, nullptr | dx, nullptr | dwg, dwu
+struct Product {
+    void *out0, *out1;                                 // h, nullptr | dx, nullptr | dwg, dwu
     int64_t rows, ld;                                  // rows of the output (of either); its stride
     int cols;                                          // columns of the output
-    int m_tiles, n_tiles, k_blocks, splits, per_split, stages;
+    int m_tiles, n_tiles, k_blocks, splits, per_split;
     int f_blocks;                                      // input: blocks of 64 of the gate's part; weights: 256-row tiles of it
+    int box_rows;                                      // rows of A that a CTA copies: fewer than 128 where a K-major product has fewer
+    int units;                                         // tiles times splits
+    int slot;                                          // of its first unit among the partial sums
+};
+// Pair q of P takes the units q, q + P, ... of the first product, then those from more[q] to more[q + 1] of the second.
+struct GatedParams {
+    Product of[2];
+    void *gu;                                          // forward: both projections, or nullptr
+    int stages;
     int f_padded;                                      // columns from dg to du
-    int box_rows;                                      // rows of A that a CTA copies: fewer than 128 where the product has fewer (K-major A)
     float *partial;
     int *status;
     uint32_t spin_limit;
     int test_skip_load;
+    int more[kMostPairs + 1];
 };
 
 __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
@@ -62,10 +75,24 @@ __device__ __forceinline__ float *part_of(float *partial, int64_t unit, uint32_t
     return partial + unit * kGatedUnitFloats + (static_cast<int>(rank) * kEpilogueWarps + e) * (kGatedUnitFloats / (2 * kEpilogueWarps));
 }
 
-template <int MODE, typename T, int ACT>
-__global__ void __launch_bounds__(kThreads, 1)
-gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1, const GatedParams p) {
-    constexpr bool A_K = MODE != kGatedWeights, B_K = MODE == kGatedForward;
+struct GatedMaps {
+    CUtensorMap a, b0, b1;                             // forward x, wg, wu; input dgu, wg, wu
+    CUtensorMap wa, wb;                                // weights dgu, x
+};
+
+// The i-th unit of pair q: its number, -1 behind the last.
+__device__ __forceinline__ int unit_of(const GatedParams &p, int q, int pairs, int i, int &which) {
+    const int u = q + i * pairs, units = p.of[0].units;
+    which = 0;
+    if (u < units) return u;
+    which = 1;
+    const int before = q < units ? (units - q + pairs - 1) / pairs : 0, v = p.more[q] + i - before;
+    return v < p.more[q + 1] ? v : -1;
+}
+
+// GRAD: the products are dx and dwg, dwu; else the one is h
+template <bool GRAD, typename T, int ACT>
+__global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constant__ GatedMaps maps, const __grid_constant__ GatedParams p) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long bars[2 * kMostStages + 4];
     __shared__ uint32_t tmem_slot;
@@ -96,43 +123,44 @@ gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const uint32_t tmem = tmem_slot;
     pdl_wait();
 
-    const int units = p.m_tiles * p.n_tiles * p.splits, first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    int which, u;
     if (warp == 0) {
         const bool leader = elect_one();
         const uint32_t full0 = in_cta(full, 0);
-        // Rows that do not exist are not copied where they are all of a CTA's, or where the product has fewer rows than a tile: the MMAs read whatever is
-        // there and give rows that nobody stores.  (Filling 127 of 128 rows with zeros took the copies twice the time of 128 rows: one row,
-        // 1536 -> 8192, 17.7 us against 14.4 us for 128 rows.)
-        const uint32_t a_bytes = p.box_rows * 128, expected = 2 * kHalf + (A_K && p.rows <= 128 ? 1 : 2) * a_bytes;
-        const bool has_rows = !A_K || rank == 0 || p.rows > 128;
         int slot = 0, issued = 0;
         uint32_t phase = 1;                            // (the first pass over the ring does not wait)
         bool ok = true;
-        for (int u = first; ok && u < units; u += step) {
-            const int tile = u / p.splits, k0 = (u - tile * p.splits) * p.per_split, k1 = min(p.k_blocks, k0 + p.per_split);
-            const int nt = tile / p.m_tiles, mt = tile - nt * p.m_tiles;
+        for (int i = 0; ok && (u = unit_of(p, pair, pairs, i, which)) >= 0; ++i) {
+            const Product &q = p.of[which];
+            const int tile = u / q.splits, k0 = (u - tile * q.splits) * q.per_split, k1 = min(q.k_blocks, k0 + q.per_split);
+            const int nt = tile / q.m_tiles, mt = tile - nt * q.m_tiles;
+            // K-major rows that do not exist are not copied where they are all of a CTA's, or where the product has fewer rows than a tile: the MMAs read
+            // whatever is there and give rows that nobody stores.  (Filling 127 of 128 rows with zeros took the copies twice the time of 128 rows.)
+            const bool one = !(GRAD && which) && q.rows <= 128, has_rows = !one || rank == 0;
+            const uint32_t expected = 2 * kHalf + (one ? 1 : 2) * q.box_rows * 128;
             for (int k = k0; k < k1; ++k) {
                 if (issued >= p.stages && !warp_wait(empty + 8 * slot, phase, ctx, 121)) { ok = false; break; }
                 if (leader && issued + 1 != p.test_skip_load) {
                     const uint32_t bar = full0 + 8 * slot, a = smem + slot * kStage, b = a + kHalf;
                     if (rank == 0) mbar_expect_tx(full + 8 * slot, expected);
-                    if constexpr (MODE == kGatedForward) {             // this CTA: 128 rows of x, and the gate's or the up projection's weights
-                        if (has_rows) tile_load(a, &map_a, bar, k * 64, mt * 256 + rank * 128);
-                        tile_load(b, rank == 0 ? &map_b0 : &map_b1, bar, k * 64, nt * 128);
-                    } else if constexpr (MODE == kGatedInput) {
-                        const bool up = k >= p.f_blocks;
-                        const CUtensorMap *map = up ? &map_b1 : &map_b0;
-                        const int f = (up ? k - p.f_blocks : k) * 64, n = nt * 256 + rank * 128;
-                        if (has_rows) tile_load(a, &map_a, bar, k * 64, mt * 256 + rank * 128);
+                    if constexpr (!GRAD) {             // this CTA: 128 rows of x, and the gate's or the up projection's weights
+                        if (has_rows) tile_load(a, &maps.a, bar, k * 64, mt * 256 + rank * 128);
+                        tile_load(b, rank == 0 ? &maps.b0 : &maps.b1, bar, k * 64, nt * 128);
+                    } else if (which == 0) {
+                        const bool up = k >= q.f_blocks;
+                        const CUtensorMap *map = up ? &maps.b1 : &maps.b0;
+                        const int f = (up ? k - q.f_blocks : k) * 64, n = nt * 256 + rank * 128;
+                        if (has_rows) tile_load(a, &maps.a, bar, k * 64, mt * 256 + rank * 128);
                         tile_load(b, map, bar, n, f);
                         tile_load(b + kHalf / 2, map, bar, n + 64, f);
                     } else {
-                        const int up = mt >= p.f_blocks;
-                        const int f = up * p.f_padded + (mt - up * p.f_blocks) * 256 + rank * 128, n = nt * 256 + rank * 128;
-                        tile_load(a, &map_a, bar, f, k * 64);
-                        tile_load(a + kHalf / 2, &map_a, bar, f + 64, k * 64);
-                        tile_load(b, &map_b0, bar, n, k * 64);
-                        tile_load(b + kHalf / 2, &map_b0, bar, n + 64, k * 64);
+                        const int up = mt >= q.f_blocks;
+                        const int f = up * p.f_padded + (mt - up * q.f_blocks) * 256 + rank * 128, n = nt * 256 + rank * 128;
+                        tile_load(a, &maps.wa, bar, f, k * 64);
+                        tile_load(a + kHalf / 2, &maps.wa, bar, f + 64, k * 64);
+                        tile_load(b, &maps.wb, bar, n, k * 64);
+                        tile_load(b + kHalf / 2, &maps.wb, bar, n + 64, k * 64);
                     }
                 }
                 ++issued;
@@ -144,16 +172,20 @@ gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait(full + 8 * (i % p.stages), (i / p.stages) & 1, ctx, 122);
     } else if (warp == 1 && rank == 0) {
         const bool leader = elect_one();
-        constexpr uint32_t idesc = (1u << 4) | (std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u) | (A_K ? 0u : 1u << 15) |
-                                   (B_K ? 0u : 1u << 16) | (uint32_t(256 >> 3) << 17) | (uint32_t(256 >> 4) << 24);
+        constexpr uint32_t common = (1u << 4) | (std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u) | (GRAD ? 1u << 16 : 0u) |
+                                    (uint32_t(256 >> 3) << 17) | (uint32_t(256 >> 4) << 24);       // GRAD: B is MN-major
         const uint32_t peer_empty = in_cta(empty, 1), peer_done = in_cta(done, 1), own_empty = in_cta(empty, 0), own_done = in_cta(done, 0);
-        const uint64_t da0 = part_desc<A_K>(smem), db0 = part_desc<B_K>(smem + kHalf);
+        const uint64_t db0 = part_desc<!GRAD>(smem + kHalf);
         int slot = 0, t = 0;
         uint32_t phase = 0;
         bool ok = true;
-        for (int u = first; ok && u < units; u += step, ++t) {
-            const int split = u % p.splits, k0 = split * p.per_split, k1 = min(p.k_blocks, k0 + p.per_split);
+        for (; ok && (u = unit_of(p, pair, pairs, t, which)) >= 0; ++t) {
+            const Product &q = p.of[which];
+            const int split = u % q.splits, k0 = split * q.per_split, k1 = min(q.k_blocks, k0 + q.per_split);
             const int buf = t & 1;
+            const bool turned = GRAD && which == 1;                    // A is MN-major too
+            const uint32_t idesc = common | (turned ? 1u << 15 : 0u);
+            const uint64_t da0 = turned ? part_desc<false>(smem) : part_desc<true>(smem), next = turned ? kNextK<false> : kNextK<true>;
             if (t > 1 && !warp_wait(drained + 8 * buf, ((t >> 1) - 1) & 1, ctx, 123)) break;
             tc_fence_after();
             uint32_t accumulate = 0;
@@ -164,7 +196,7 @@ gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     const uint64_t shift = static_cast<uint64_t>(slot) * (kStage >> 4);
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        mma_pair(tmem + buf * 256, da0 + shift + j * kNextK<A_K>, db0 + shift + j * kNextK<B_K>, idesc, accumulate | j);
+                        mma_pair(tmem + buf * 256, da0 + shift + j * next, db0 + shift + j * kNextK<!GRAD>, idesc, accumulate | j);
                     commit_pair(own_empty + 8 * slot);
                     commit_pair(peer_empty + 8 * slot);
                 }
@@ -188,70 +220,69 @@ gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quadrant * 32) << 16);
         const uint32_t drained0 = in_cta(drained, 0);
         unsigned char *stage = smem_raw + (smem - smem_u32(smem_raw)) + p.stages * kStage + e * kStaging;
-        int t = 0;
-        for (int u = first; u < units; u += step, ++t) {
-            const int tile = u / p.splits, buf = t & 1;
-            const int nt = tile / p.m_tiles;
-            int mt = tile - nt * p.m_tiles;
+        for (int t = 0; (u = unit_of(p, pair, pairs, t, which)) >= 0; ++t) {
+            const Product &q = p.of[which];
+            const int tile = u / q.splits, buf = t & 1;
+            const int nt = tile / q.m_tiles;
+            int mt = tile - nt * q.m_tiles;
             if (!mbar_wait(done + 8 * buf, (t >> 1) & 1, ctx, 126)) break;
             tc_fence_after();
-            T *out = static_cast<T *>(p.out0);
-            if constexpr (MODE == kGatedWeights) {
-                if (mt >= p.f_blocks) {
-                    mt -= p.f_blocks;
-                    out = static_cast<T *>(p.out1);
-                }
+            T *out = static_cast<T *>(q.out0);
+            if (GRAD && which == 1 && mt >= q.f_blocks) {
+                mt -= q.f_blocks;
+                out = static_cast<T *>(q.out1);
             }
             const int64_t row0 = static_cast<int64_t>(mt) * 256 + rank * 128 + quadrant * 32;
-            const int rows_left = static_cast<int>(max(static_cast<int64_t>(-1), min(static_cast<int64_t>(32), p.rows - row0)));
+            const int rows_left = static_cast<int>(max(static_cast<int64_t>(-1), min(static_cast<int64_t>(32), q.rows - row0)));
             // chunk j of the warp, 32 columns of the accumulator: forward gate, up, gate, up of its 64 outputs
-            auto column = [&](int j) { return MODE == kGatedForward ? (j & 1) * 128 + half * 64 + (j >> 1) * 32 : half * 128 + j * 32; };
-            if (p.splits > 1) {
-                float *to = part_of(p.partial, u, rank, e) + lane;
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t v[32];
-                    tmem_ld32(lanes + buf * 256 + column(j), v);
-                    if (lane < rows_left) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) to[(j * 32 + i) * 32] = __uint_as_float(v[i]);
-                    }
-                }
-            }
-            auto fetch = [&](int j, float (&v)[32]) {
-                uint32_t w[32];
-                tmem_ld32(lanes + buf * 256 + column(j), w);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(w[i]);
+            auto fetch = [&](int j, uint32_t (&v)[32]) {
+                tmem_ld32(lanes + buf * 256 + (GRAD ? half * 128 + j * 32 : (j & 1) * 128 + half * 64 + (j >> 1) * 32), v);
             };
             auto put = [&](const float (&v)[32], T *base, int64_t ld, int col, int left) {
                 const uint64_t places = reinterpret_cast<uintptr_t>(base) | static_cast<uint64_t>(ld * sizeof(T));
                 const int aligned = places % 16 == 0 ? 16 : places % 4 == 0 ? 4 : 2;
                 store_piece<T, kPiece>(v, stage, base + row0 * ld + col, ld, rows_left, left, aligned);
             };
-            if (p.splits == 1 && rows_left > 0) {
-                if constexpr (MODE == kGatedForward) {
+            if (q.splits > 1) {
+                float *to = part_of(p.partial, q.slot + u, rank, e) + lane;
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t v[32];
+                    fetch(j, v);
+                    if (lane < rows_left) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) to[(j * 32 + i) * 32] = __uint_as_float(v[i]);
+                    }
+                }
+            } else if (rows_left > 0) {
+                if constexpr (!GRAD) {
                     for (int c = 0; c < 2; ++c) {
                         const int f = nt * 128 + half * 64 + c * 32;
-                        if (f >= p.cols) break;
+                        if (f >= q.cols) break;
+                        uint32_t w0[32], w1[32];
+                        fetch(2 * c, w0);
+                        fetch(2 * c + 1, w1);
                         float g[32], up[32];
-                        fetch(2 * c, g);
-                        fetch(2 * c + 1, up);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) g[i] = __uint_as_float(w0[i]), up[i] = __uint_as_float(w1[i]);
                         if (p.gu) {
                             T *gu = static_cast<T *>(p.gu);
-                            put(g, gu, 2 * static_cast<int64_t>(p.cols), f, p.cols - f);
-                            put(up, gu + p.cols, 2 * static_cast<int64_t>(p.cols), f, p.cols - f);
+                            put(g, gu, 2 * static_cast<int64_t>(q.cols), f, q.cols - f);
+                            put(up, gu + q.cols, 2 * static_cast<int64_t>(q.cols), f, q.cols - f);
                         }
 #pragma unroll
                         for (int i = 0; i < 32; ++i) g[i] = activate1<ACT>(g[i]) * up[i];
-                        put(g, out, p.ld, f, p.cols - f);
+                        put(g, out, q.ld, f, q.cols - f);
                     }
                 } else {
                     for (int j = 0; j < 4; ++j) {
                         const int n = nt * 256 + half * 128 + j * 32;
-                        if (n >= p.cols) break;
+                        if (n >= q.cols) break;
+                        uint32_t w[32];
+                        fetch(j, w);
                         float v[32];
-                        fetch(j, v);
-                        put(v, out, p.ld, n, p.cols - n);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(w[i]);
+                        put(v, out, q.ld, n, q.cols - n);
                     }
                 }
             }
@@ -269,32 +300,35 @@ gated_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 
 // The sums of a tile's ranges, in their order, and the epilogue.  A warp takes 32 rows and 16 columns (forward: of both projections); the eight
 // warps of a CTA are the eight epilogue warps' pieces of one CTA's half of the tile.
-template <int MODE, typename T, int ACT>
-__global__ void __launch_bounds__(256) gated_join_kernel(const GatedParams p) {
-    constexpr int kPieces = MODE == kGatedForward ? 4 : 8, kWide = 16;
+template <bool GRAD, typename T, int ACT>
+__global__ void __launch_bounds__(256) gated_join_kernel(const __grid_constant__ GatedParams p, int first_ctas) {
+    constexpr int kPieces = GRAD ? 8 : 4, kWide = 16;
     __shared__ __align__(16) unsigned char staging[8][32 * kWide * sizeof(T)];
     pdl_trigger();
     const int e = threadIdx.x >> 5, lane = threadIdx.x & 31, quadrant = e & 3, half = e >> 2;
-    const int piece = blockIdx.x % kPieces, rank = blockIdx.x / kPieces & 1, tile = blockIdx.x / (2 * kPieces);
-    const int nt = tile / p.m_tiles;
-    int mt = tile - nt * p.m_tiles;
-    T *out = static_cast<T *>(p.out0);
-    if (MODE == kGatedWeights && mt >= p.f_blocks) {
-        mt -= p.f_blocks;
-        out = static_cast<T *>(p.out1);
+    const bool second = GRAD && static_cast<int>(blockIdx.x) >= first_ctas;                      // CTAs of the first product come first
+    const int block = blockIdx.x - (second ? first_ctas : 0);
+    const Product &q = p.of[second];
+    const int piece = block % kPieces, rank = block / kPieces & 1, tile = block / (2 * kPieces);
+    const int nt = tile / q.m_tiles;
+    int mt = tile - nt * q.m_tiles;
+    T *out = static_cast<T *>(q.out0);
+    if (second && mt >= q.f_blocks) {
+        mt -= q.f_blocks;
+        out = static_cast<T *>(q.out1);
     }
     const int64_t row0 = static_cast<int64_t>(mt) * 256 + rank * 128 + quadrant * 32;
-    const int rows_left = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(32), p.rows - row0)));
-    const int col = MODE == kGatedForward ? nt * 128 + half * 64 + piece * kWide : nt * 256 + half * 128 + piece * kWide, left = p.cols - col;
+    const int rows_left = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(32), q.rows - row0)));
+    const int col = GRAD ? nt * 256 + half * 128 + piece * kWide : nt * 128 + half * 64 + piece * kWide, left = q.cols - col;
     if (rows_left == 0 || left <= 0) return;
     pdl_wait();
     auto sum = [&](int chunk, int first, float (&v)[kWide]) {          // columns [first, first + 16) of a chunk
 #pragma unroll
         for (int i = 0; i < kWide; ++i) v[i] = 0.f;
         if (lane >= rows_left) return;
-        const float *from = part_of(p.partial, static_cast<int64_t>(tile) * p.splits, rank, e) + (chunk * 32 + first) * 32 + lane;
+        const float *from = part_of(p.partial, q.slot + static_cast<int64_t>(tile) * q.splits, rank, e) + (chunk * 32 + first) * 32 + lane;
 #pragma unroll 4
-        for (int s = 0; s < p.splits; ++s, from += kGatedUnitFloats) {
+        for (int s = 0; s < q.splits; ++s, from += kGatedUnitFloats) {
 #pragma unroll
             for (int i = 0; i < kWide; ++i) v[i] += from[i * 32];
         }
@@ -305,34 +339,34 @@ __global__ void __launch_bounds__(256) gated_join_kernel(const GatedParams p) {
         store_piece<T, kWide * sizeof(T)>(v, staging[e], base + row0 * ld + col, ld, rows_left, left, aligned);
     };
     float v[kWide];
-    if constexpr (MODE == kGatedForward) {
+    if constexpr (!GRAD) {
         float up[kWide];
         sum(piece >> 1 << 1, (piece & 1) * kWide, v);
         sum((piece >> 1 << 1) + 1, (piece & 1) * kWide, up);
         if (p.gu) {
             T *gu = static_cast<T *>(p.gu);
-            put(v, gu, 2 * static_cast<int64_t>(p.cols));
-            put(up, gu + p.cols, 2 * static_cast<int64_t>(p.cols));
+            put(v, gu, 2 * static_cast<int64_t>(q.cols));
+            put(up, gu + q.cols, 2 * static_cast<int64_t>(q.cols));
         }
 #pragma unroll
         for (int i = 0; i < kWide; ++i) v[i] = activate1<ACT>(v[i]) * up[i];
     } else {
         sum(piece >> 1, (piece & 1) * kWide, v);
     }
-    put(v, out, p.ld);
+    put(v, out, q.ld);
 }
 
 // ---- forward, few rows -----------------------------------------------------------------------------------------------------
-// The weights are the M operand, 64 rows of wg and the same 64 of wu in a tile, the rows of x the N operand (16 to 128): a CTA per 64 outputs and
-// range of the summed dimension, whose weights it streams.  The CTAs of a cluster share a tile; their partial sums are pushed into the shared
+// The weights are the M operand, 64 rows of wg and the same 64 of wu in a tile, the rows of x the N operand (16 to 128 of them): a CTA per 64 outputs,
+// 128 rows and range of the summed dimension, whose weights it streams.  The CTAs of a cluster share a tile; their partial sums are pushed into the shared
 // memory of the one that finishes a row of x, where g and u of an output meet.
 constexpr int kRowsThreads = 256;
 constexpr int kMostRowsStages = 12;
 
 struct GatedRowsParams {
     void *h, *gu;
-    int64_t ldh;
-    int rows, F, k_blocks, per_split, splits, stages, tile_n, tensor_columns;
+    int64_t ldh, rows;
+    int F, n_tiles, k_blocks, per_split, splits, stages, tile_n, box_rows, tensor_columns;
     int *status;
     uint32_t spin_limit;
     int test_skip_load;
@@ -350,7 +384,9 @@ gated_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     __shared__ __align__(8) unsigned long long bars[2 * kMostRowsStages + 1];
     __shared__ uint32_t tmem_slot;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const int rank = blockIdx.x % p.splits, f0 = blockIdx.x / p.splits * 64;
+    const int rank = blockIdx.x % p.splits, tile = blockIdx.x / p.splits, mt = tile / p.n_tiles, f0 = (tile - mt * p.n_tiles) * 64;
+    const int64_t row0 = static_cast<int64_t>(mt) * 128;
+    const int rows = static_cast<int>(min(static_cast<int64_t>(128), p.rows - row0));
     const WaitCtx ctx{p.status, p.spin_limit ? p.spin_limit : kSpinLimit};
     const uint32_t smem = (smem_u32(smem_raw) + 1023) & ~1023u;
     const uint32_t full = smem_u32(bars), empty = full + 8 * kMostRowsStages, done = empty + 8 * kMostRowsStages;
@@ -381,10 +417,10 @@ gated_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
             if (issued >= p.stages && !warp_wait(empty + 8 * slot, phase, ctx, 141)) break;
             if (leader && issued + 1 != p.test_skip_load) {
                 const uint32_t at = smem + slot * stage_bytes, bar = full + 8 * slot;
-                mbar_expect_tx(bar, kHalf + p.rows * 128);             // (rows that do not exist are whatever is there: their sums are not read)
+                mbar_expect_tx(bar, kHalf + p.box_rows * 128);         // (rows behind the box are whatever is there: their sums are not read)
                 tile_load_own(at, &map_g, bar, k * 64, f0);
                 tile_load_own(at + kHalf / 2, &map_u, bar, k * 64, f0);
-                tile_load_own(at + kHalf, &map_x, bar, k * 64, 0);
+                tile_load_own(at + kHalf, &map_x, bar, k * 64, static_cast<int>(row0));
             }
             ++issued;
             if (++slot == p.stages) { slot = 0; phase ^= 1; }
@@ -420,19 +456,19 @@ gated_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     const int place = (warp & 3) * 32 + lane;
     pair_barrier();                                    // all pipelines of the cluster are idle: their memory can be reused
     const uint32_t slots = smem + (rank * owned * 128 + place) * 4, lanes = tmem + ((warp & 3) * 32u << 16);
-    for (int c = (warp >> 2) * 16; c < p.rows; c += 32) {
+    for (int c = (warp >> 2) * 16; c < rows; c += 32) {
         uint32_t v[16];
         tmem_ld16(lanes + c, v);
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-            if (c + j < p.rows)
+            if (c + j < rows)
                 asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cta(slots + ((c + j) >> shift) * 512, j & (p.splits - 1))), "r"(k1 > k0 ? v[j] : 0u) : "memory");
     }
     pair_barrier();
     const int f = threadIdx.x & 63;
     if (ok && f0 + f < p.F) {
         const float *from = reinterpret_cast<const float *>(smem_raw + (smem - smem_u32(smem_raw))) + f;
-        const int mine = (p.rows - rank + p.splits - 1) >> shift;
+        const int mine = (rows - rank + p.splits - 1) >> shift;
 #pragma unroll 2
         for (int j = threadIdx.x >> 6; j < mine; j += kRowsThreads / 64) {
             float g = 0.f, up = 0.f;
@@ -442,7 +478,7 @@ gated_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
                     g += from[(r * owned + j) * 128];
                     up += from[(r * owned + j) * 128 + 64];
                 }
-            const int64_t row = (j << shift) + rank;
+            const int64_t row = row0 + (j << shift) + rank;
             if (p.gu) {
                 T *gu = static_cast<T *>(p.gu) + row * 2 * p.F + f0 + f;
                 gu[0] = from_float<T>(g);
@@ -463,36 +499,55 @@ cudaError_t make_map(CUtensorMap *map, int dtype, const void *base, int64_t rows
 }
 
 // f(product, join): the gradients' products have no activation
-template <typename F> cudaError_t by_kernel(int mode, int dtype, int act, F f) {
+template <typename F> cudaError_t by_kernel(bool grad, int dtype, int act, F f) {
     auto go = [&](auto t) {
         using T = decltype(t);
-        if (mode == kGatedInput) return f(gated_kernel<kGatedInput, T, PATDNN_ACT_NONE>, gated_join_kernel<kGatedInput, T, PATDNN_ACT_NONE>);
-        if (mode == kGatedWeights) return f(gated_kernel<kGatedWeights, T, PATDNN_ACT_NONE>, gated_join_kernel<kGatedWeights, T, PATDNN_ACT_NONE>);
-        return by_act(act, [&](auto a) { return f(gated_kernel<kGatedForward, T, a.value>, gated_join_kernel<kGatedForward, T, a.value>); });
+        if (grad) return f(gated_kernel<true, T, PATDNN_ACT_NONE>, gated_join_kernel<true, T, PATDNN_ACT_NONE>);
+        return by_act(act, [&](auto a) { return f(gated_kernel<false, T, a.value>, gated_join_kernel<false, T, a.value>); });
     };
     return dtype == PATDNN_F16 ? go(__half{}) : go(__nv_bfloat16{});
 }
-
 template <typename F> cudaError_t by_rows_kernel(int dtype, int act, F f) {
     return by_act(act, [&](auto a) { return dtype == PATDNN_F16 ? f(gated_rows_kernel<__half, a.value>) : f(gated_rows_kernel<__nv_bfloat16, a.value>); });
 }
 
 }  // namespace
 
-int units_most() { return std::max(1, sm_count() / 2); }
+int pairs_most() { return std::min(kMostPairs, std::max(1, sm_count() / 2)); }
 
-GatedPlan plan_gated(int F, int K, int64_t rows, int mode) {
+// Cuts the summed dimension into `splits` ranges or a few less, none of them empty.
+static void cut(GatedPlan &p, int64_t splits) {
+    p.per_split = static_cast<int>(ceil_div(p.k_blocks, std::max<int64_t>(1, splits)));
+    p.splits = static_cast<int>(ceil_div(p.k_blocks, p.per_split));
+}
+static int64_t units_of(const GatedPlan &p) { return static_cast<int64_t>(p.m_tiles) * p.n_tiles * p.splits; }
+constexpr int64_t kJoinBlocks = 20;                    // what partial sums cost, their stores and the join, in blocks of a tile (6 us, measured)
+
+GatedPlan plan_gated_forward(int F, int K, int64_t rows) {
     GatedPlan p{};
-    if (mode == kGatedForward && rows <= 128) {
+    p.k_blocks = static_cast<int>(ceil_div(K, 64));
+    p.m_tiles = static_cast<int>(ceil_div(rows, 256));
+    p.n_tiles = static_cast<int>(ceil_div(F, 128));
+    const int64_t tiles = static_cast<int64_t>(p.m_tiles) * p.n_tiles, pairs = pairs_most();
+    // as many ranges as give the shortest longest walk, with no more partial sums than fit
+    int64_t best = 1, shortest = ceil_div(tiles, pairs) * p.k_blocks;
+    for (int64_t n = 2; n <= p.k_blocks / 4 && tiles * n <= kGatedUnits * pairs; ++n) {
+        const int64_t walk = ceil_div(tiles * n, pairs) * ceil_div(p.k_blocks, n) + kJoinBlocks;
+        if (walk < shortest) best = n, shortest = walk;
+    }
+    // Few rows: a block of its tile takes about as long as one of a pair's, which is four times as large.  Launch and fill take about six blocks' time
+    // in each round, 14 once for the pairs; the exchange in a cluster four.
+    const int64_t f_tiles = ceil_div(F, 64), ctas = ceil_div(rows, 128) * f_tiles;
+    int64_t ranges = 1;
+    while (ranges < 8 && ctas * ranges * 2 <= sm_count() && p.k_blocks >= ranges * 8) ranges *= 2;
+    if (rows <= 128 || ceil_div(ctas * ranges, sm_count()) * (ceil_div(p.k_blocks, ranges) + 6) + (ranges > 1 ? 4 : 0) < shortest + 14) {
         p.few = true;
-        p.tile_n = static_cast<int>(ceil_div(rows, 16) * 16);
-        p.m_tiles = 1;
-        p.n_tiles = static_cast<int>(ceil_div(F, 64));
-        p.k_blocks = static_cast<int>(ceil_div(K, 64));
-        p.splits = 1;
-        while (p.splits < 8 && p.n_tiles * p.splits * 2 <= sm_count() && p.k_blocks >= p.splits * 8) p.splits *= 2;
-        p.per_split = static_cast<int>(ceil_div(p.k_blocks, p.splits));
-        p.grid = p.n_tiles * p.splits;
+        p.tile_n = rows < 128 ? static_cast<int>(ceil_div(rows, 16) * 16) : 128;
+        p.m_tiles = static_cast<int>(ceil_div(rows, 128));
+        p.n_tiles = static_cast<int>(f_tiles);
+        p.splits = static_cast<int>(ranges);
+        p.per_split = static_cast<int>(ceil_div(p.k_blocks, ranges));
+        p.grid = static_cast<int>(ctas * ranges);
         const int stage = kHalf + p.tile_n * 128;
         // more CTAs than SMs: two to an SM
         p.stages = std::max(1, std::min({kMostRowsStages, p.per_split, (p.grid > sm_count() ? 110 * 1024 : 200 * 1024) / stage}));
@@ -502,78 +557,155 @@ GatedPlan plan_gated(int F, int K, int64_t rows, int mode) {
         p.smem = std::max({p.stages * stage + 1024, p.splits * owned * 512 + 1024, kSmemPerSm / 512 * p.tensor_columns - 1024});
         return p;
     }
-    const int64_t m = mode == kGatedWeights ? 2 * ceil_div(F, 256) : ceil_div(rows, 256);
-    p.m_tiles = static_cast<int>(m);
-    p.n_tiles = static_cast<int>(mode == kGatedForward ? ceil_div(F, 128) : ceil_div(K, 256));
-    p.k_blocks = static_cast<int>(mode == kGatedForward ? ceil_div(K, 64) : mode == kGatedInput ? 2 * ceil_div(F, 64) : ceil_div(rows, 64));
-    const int64_t tiles = m * p.n_tiles, most = units_most();
-    // Tiles for half the pairs of SMs or fewer: ranges of at least four blocks share a tile.
-    p.splits = 1;
-    if (tiles * 2 <= most) p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most / tiles, p.k_blocks / 4)));
-    p.per_split = static_cast<int>(ceil_div(p.k_blocks, p.splits));
-    p.splits = static_cast<int>(ceil_div(p.k_blocks, p.per_split));
-    p.grid = 2 * static_cast<int>(std::min(tiles * p.splits, most));
+    cut(p, best);
+    p.grid = 2 * static_cast<int>(std::min(units_of(p), pairs));
     p.stages = kMostStages;
     p.smem = kSmem;
     p.tensor_columns = 512;
     return p;
 }
 
-cudaError_t prepare_gated() {
-    for (int dtype : {PATDNN_F16, PATDNN_BF16})
-        for (int mode : {kGatedForward, kGatedInput, kGatedWeights})
-            for (int act : {PATDNN_ACT_NONE, PATDNN_ACT_RELU, PATDNN_ACT_SILU}) {
-                const cudaError_t e = by_kernel(mode, dtype, act, [](auto kernel, auto) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
-                if (e != cudaSuccess) return e;
-                const cudaError_t r = by_rows_kernel(dtype, act, [](auto kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
-                if (r != cudaSuccess) return r;
+void plan_gated_gradient(int F, int K, int64_t rows, bool dx, bool dw, GatedPlan (&plan)[2]) {
+    plan[0] = plan[1] = GatedPlan{};
+    const int64_t pairs = pairs_most();
+    plan[0].m_tiles = static_cast<int>(ceil_div(rows, 256));
+    plan[0].k_blocks = gated_padded(F) / 64 * 2;
+    plan[1].m_tiles = static_cast<int>(2 * ceil_div(F, 256));
+    plan[1].k_blocks = static_cast<int>(ceil_div(rows, 64));
+    int64_t blocks = 0;
+    for (int i = 0; i < 2; ++i) {
+        plan[i].n_tiles = (i ? dw : dx) ? static_cast<int>(ceil_div(K, 256)) : 0;
+        blocks += static_cast<int64_t>(plan[i].m_tiles) * plan[i].n_tiles * plan[i].k_blocks;
+    }
+    // Ranges of about a pair's share of all blocks, of two shares, or none: the first product's units go round the pairs, the second's fill up.
+    const int64_t share = std::max<int64_t>(4, ceil_div(blocks, pairs));
+    int64_t shortest = INT64_MAX;
+    GatedPlan best[2] = {plan[0], plan[1]};
+    for (int a = 0; a < 4; ++a)
+        for (int b = 0; b < 4; ++b) {
+            const int64_t longest[4] = {INT32_MAX, share, share + share / 4, 2 * share};
+            cut(plan[0], ceil_div(plan[0].k_blocks, longest[a]));
+            cut(plan[1], ceil_div(plan[1].k_blocks, longest[b]));
+            const int64_t u0 = units_of(plan[0]), u1 = units_of(plan[1]);
+            if ((plan[0].splits > 1 ? u0 : 0) + (plan[1].splits > 1 ? u1 : 0) > kGatedUnits * pairs) continue;
+            const int64_t even = ceil_div(u0 * plan[0].per_split + u1 * plan[1].per_split, pairs) + (u1 ? plan[1].per_split / 2 : 0);
+            const int64_t walk = std::max({ceil_div(u0, pairs) * plan[0].per_split, u1 ? static_cast<int64_t>(plan[1].per_split) : 0, even}) +
+                                 (plan[0].splits + plan[1].splits > 2 ? kJoinBlocks : 0);
+            if (walk < shortest) {
+                shortest = walk;
+                best[0] = plan[0];
+                best[1] = plan[1];
             }
+        }
+    int64_t units = 0;
+    for (int i = 0; i < 2; ++i) {
+        plan[i] = best[i];
+        units += units_of(plan[i]);
+        plan[i].stages = kMostStages;
+        plan[i].smem = kSmem;
+        plan[i].tensor_columns = 512;
+    }
+    plan[0].grid = plan[1].grid = 2 * static_cast<int>(std::min(units, pairs));
+}
+
+cudaError_t prepare_gated() {
+    auto allow = [](auto kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); };
+    for (int dtype : {PATDNN_F16, PATDNN_BF16})
+        for (int act : {PATDNN_ACT_NONE, PATDNN_ACT_RELU, PATDNN_ACT_SILU}) {
+            cudaError_t e = by_kernel(false, dtype, act, [&](auto product, auto) { return allow(product); });
+            if (e == cudaSuccess) e = by_kernel(true, dtype, act, [&](auto product, auto) { return allow(product); });
+            if (e == cudaSuccess) e = by_rows_kernel(dtype, act, allow);
+            if (e != cudaSuccess) return e;
+        }
     return cudaSuccess;
 }
 
-cudaError_t launch_gated(const GatedShape &s, const GatedCall &c, const GatedWork &w, int mode, cudaStream_t st, int *launches) {
-    const GatedPlan plan = plan_gated(s.F, s.K, c.rows, mode);
-    const int padded = gated_padded(s.F);
-    CUtensorMap a, b0, b1;
-    cudaError_t e;
-    *launches = plan.splits > 1 && !plan.few ? 2 : 1;
+static Product product_of(const GatedPlan &plan, int slot) {
+    Product q{};
+    q.m_tiles = plan.m_tiles; q.n_tiles = plan.n_tiles; q.k_blocks = plan.k_blocks; q.splits = plan.splits; q.per_split = plan.per_split;
+    q.units = static_cast<int>(units_of(plan));
+    q.box_rows = 128;
+    q.slot = slot;
+    return q;
+}
+
+static cudaError_t launch_products(const GatedMaps &maps, GatedParams &p, const GatedShape &s, const GatedCall &c, const GatedWork &w, int grid, bool grad,
+                                   cudaStream_t st, int *launches) {
+    p.stages = kMostStages; p.partial = w.partial; p.status = w.status; p.spin_limit = c.spin_limit; p.test_skip_load = c.test_skip_load;
+    int joins[2];
+    for (int i = 0; i < 2; ++i) joins[i] = p.of[i].splits > 1 ? p.of[i].m_tiles * p.of[i].n_tiles * (grad ? 16 : 8) : 0;
+    *launches = joins[0] + joins[1] > 0 ? 2 : 1;
+    return by_kernel(grad, s.dtype, s.act, [&](auto product, auto join) {
+        const cudaError_t r = launch_pdl(product, dim3(grid), dim3(kThreads), kSmem, st, 2, maps, p);
+        if (r != cudaSuccess || *launches == 1) return r;
+        return launch_pdl(join, dim3(joins[0] + joins[1]), dim3(256), 0, st, 1, p, joins[0]);
+    });
+}
+
+cudaError_t launch_gated_forward(const GatedShape &s, const GatedCall &c, const GatedWork &w, cudaStream_t st, int *launches) {
+    const GatedPlan plan = plan_gated_forward(s.F, s.K, c.rows);
+    GatedMaps maps{};
+    const int box = static_cast<int>(std::min<int64_t>(128, c.rows)), weights = plan.few ? 64 : 128;
+    cudaError_t e = make_map(&maps.a, s.dtype, c.x, c.rows, s.K, c.x_row, box);
+    if (e == cudaSuccess) e = make_map(&maps.b0, s.dtype, c.wg, s.F, s.K, c.w_row, weights);
+    if (e == cudaSuccess) e = make_map(&maps.b1, s.dtype, c.wu, s.F, s.K, c.w_row, weights);
+    if (e != cudaSuccess) return e;
     if (plan.few) {
         GatedRowsParams p{};
-        p.h = c.h; p.gu = c.gu; p.ldh = s.h_row; p.rows = static_cast<int>(c.rows); p.F = s.F;
+        p.h = c.h; p.gu = c.gu; p.ldh = s.h_row; p.rows = c.rows; p.F = s.F; p.n_tiles = plan.n_tiles; p.box_rows = box;
         p.k_blocks = plan.k_blocks; p.per_split = plan.per_split; p.splits = plan.splits; p.stages = plan.stages; p.tile_n = plan.tile_n;
         p.tensor_columns = plan.tensor_columns; p.status = w.status; p.spin_limit = c.spin_limit; p.test_skip_load = c.test_skip_load;
-        e = make_map(&a, s.dtype, c.x, c.rows, s.K, c.x_row, p.rows);
-        if (e == cudaSuccess) e = make_map(&b0, s.dtype, c.wg, s.F, s.K, c.w_row, 64);
-        if (e == cudaSuccess) e = make_map(&b1, s.dtype, c.wu, s.F, s.K, c.w_row, 64);
-        if (e != cudaSuccess) return e;
-        return by_rows_kernel(s.dtype, s.act, [&](auto kernel) { return launch_pdl(kernel, dim3(plan.grid), dim3(kRowsThreads), plan.smem, st, plan.splits, a, b0, b1, p); });
+        *launches = 1;
+        return by_rows_kernel(s.dtype, s.act, [&](auto kernel) {
+            return launch_pdl(kernel, dim3(plan.grid), dim3(kRowsThreads), plan.smem, st, plan.splits, maps.a, maps.b0, maps.b1, p);
+        });
     }
     GatedParams p{};
-    p.m_tiles = plan.m_tiles; p.n_tiles = plan.n_tiles; p.k_blocks = plan.k_blocks; p.splits = plan.splits; p.per_split = plan.per_split; p.stages = plan.stages;
-    p.partial = w.partial; p.status = w.status; p.spin_limit = c.spin_limit; p.test_skip_load = c.test_skip_load;
-    p.box_rows = mode == kGatedWeights ? 128 : static_cast<int>(std::min<int64_t>(128, c.rows));
-    if (mode == kGatedForward) {
-        p.out0 = c.h; p.gu = c.gu; p.rows = c.rows; p.ld = s.h_row; p.cols = s.F;
-        e = make_map(&a, s.dtype, c.x, c.rows, s.K, c.x_row, p.box_rows);
-        if (e == cudaSuccess) e = make_map(&b0, s.dtype, c.wg, s.F, s.K, c.w_row, 128);
-        if (e == cudaSuccess) e = make_map(&b1, s.dtype, c.wu, s.F, s.K, c.w_row, 128);
-    } else if (mode == kGatedInput) {
-        p.out0 = c.dx; p.rows = c.rows; p.ld = s.x_row; p.cols = s.K; p.f_blocks = padded / 64;
-        e = make_map(&a, s.dtype, w.dgu, c.rows, 2 * static_cast<int64_t>(padded), 2 * static_cast<int64_t>(padded), p.box_rows);
-        if (e == cudaSuccess) e = make_map(&b0, s.dtype, c.wg, s.F, s.K, c.w_row, 64);
-        if (e == cudaSuccess) e = make_map(&b1, s.dtype, c.wu, s.F, s.K, c.w_row, 64);
-    } else {
-        p.out0 = c.dwg; p.out1 = c.dwu; p.rows = s.F; p.ld = s.w_row; p.cols = s.K; p.f_blocks = plan.m_tiles / 2; p.f_padded = padded;
-        e = make_map(&a, s.dtype, w.dgu, c.rows, 2 * static_cast<int64_t>(padded), 2 * static_cast<int64_t>(padded), 64);
-        if (e == cudaSuccess) e = make_map(&b0, s.dtype, c.x, c.rows, s.K, c.x_row, 64);
-        b1 = b0;
+    p.gu = c.gu;
+    Product &q = p.of[0] = product_of(plan, 0);
+    q.out0 = c.h; q.rows = c.rows; q.ld = s.h_row; q.cols = s.F;
+    return launch_products(maps, p, s, c, w, plan.grid, false, st, launches);
+}
+
+cudaError_t launch_gated_gradient(const GatedShape &s, const GatedCall &c, const GatedWork &w, cudaStream_t st, int *launches) {
+    GatedPlan plan[2];
+    plan_gated_gradient(s.F, s.K, c.rows, c.dx != nullptr, c.dwg != nullptr, plan);
+    const int padded = gated_padded(s.F);
+    const int64_t dgu_row = 2 * static_cast<int64_t>(padded);
+    GatedMaps maps{};
+    GatedParams p{};
+    p.f_padded = padded;
+    Product &x = p.of[0] = product_of(plan[0], 0), &dw = p.of[1] = product_of(plan[1], plan[0].splits > 1 ? x.units : 0);
+    cudaError_t e = cudaSuccess;
+    if (c.dx) {
+        x.out0 = c.dx; x.rows = c.rows; x.ld = s.x_row; x.cols = s.K; x.f_blocks = padded / 64;
+        x.box_rows = static_cast<int>(std::min<int64_t>(128, c.rows));
+        e = make_map(&maps.a, s.dtype, w.dgu, c.rows, dgu_row, dgu_row, x.box_rows);
+        if (e == cudaSuccess) e = make_map(&maps.b0, s.dtype, c.wg, s.F, s.K, c.w_row, 64);
+        if (e == cudaSuccess) e = make_map(&maps.b1, s.dtype, c.wu, s.F, s.K, c.w_row, 64);
+    }
+    if (c.dwg && e == cudaSuccess) {
+        dw.out0 = c.dwg; dw.out1 = c.dwu; dw.rows = s.F; dw.ld = s.w_row; dw.cols = s.K; dw.f_blocks = dw.m_tiles / 2;
+        e = make_map(&maps.wa, s.dtype, w.dgu, c.rows, dgu_row, dgu_row, 64);
+        if (e == cudaSuccess) e = make_map(&maps.wb, s.dtype, c.x, c.rows, s.K, c.x_row, 64);
     }
     if (e != cudaSuccess) return e;
-    return by_kernel(mode, s.dtype, s.act, [&](auto product, auto join) {
-        const cudaError_t r = launch_pdl(product, dim3(plan.grid), dim3(kThreads), plan.smem, st, 2, a, b0, b1, p);
-        if (r != cudaSuccess || plan.splits == 1) return r;
-        return launch_pdl(join, dim3(plan.m_tiles * plan.n_tiles * (mode == kGatedForward ? 8 : 16)), dim3(256), 0, st, 1, p);
-    });
+    // The second product's units go to the pairs that the first one left with the fewest blocks: up to a common level, what remains one by one.
+    const int pairs = plan[0].grid / 2;
+    const int64_t level = (static_cast<int64_t>(x.units) * x.per_split + static_cast<int64_t>(dw.units) * dw.per_split) / pairs;
+    int64_t given = 0, load[kMostPairs];
+    int order[kMostPairs], count[kMostPairs];
+    for (int q = 0; q < pairs; ++q) {
+        const int64_t before = static_cast<int64_t>(x.units / pairs + (q < x.units % pairs)) * x.per_split;
+        count[q] = static_cast<int>(std::max<int64_t>(0, std::min((level - before) / dw.per_split, dw.units - given)));
+        given += count[q];
+        load[q] = before + static_cast<int64_t>(count[q]) * dw.per_split;
+        order[q] = q;
+    }
+    std::sort(order, order + pairs, [&](int a, int b) { return load[a] != load[b] ? load[a] < load[b] : a < b; });
+    for (int i = 0; given < dw.units; ++given, i = i + 1 < pairs ? i + 1 : 0) ++count[order[i]];
+    for (int q = 0; q < pairs; ++q) p.more[q + 1] = p.more[q] + count[q];
+    return launch_products(maps, p, s, c, w, plan[0].grid, true, st, launches);
 }
 
 }  // namespace patdnn

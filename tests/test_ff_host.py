@@ -131,18 +131,20 @@ def test_gated_refusals(status, kw):
 def test_gated_plans():
     for F, K in ((1, 1), (64, 64), (130, 1000), (1333, 1000), (8192, 4096), (40000, 16384)):
         for rows in (1, 8, 100, 256, 300, 777, 5000, 100000):
+            parts = [0, 0, 0]
             for product in range(3):
                 p = B.gated_plan(F, K, rows, product)
                 assert p["splits"] * p["blocks_per_split"] >= p["blocks"] > (p["splits"] - 1) * p["blocks_per_split"], p      # no range is empty
                 tiles = p["row_tiles"] * p["column_tiles"]
                 if p["few_rows"]:
-                    assert product == 0 and rows <= 128 and p["grid"] == tiles * p["splits"] and p["splits"] <= 8
+                    assert product == 0 and p["grid"] == tiles * p["splits"] and p["splits"] <= 8
                     # the CTAs of a cluster wait for one another: where they fit an SM by shared memory they do by tensor memory
-                    assert rows <= p["tensor_columns"] <= 128 and (p["smem_bytes"] + 1024) * 512 >= p["tensor_columns"] * 228 * 1024, p
+                    assert min(rows, 128) <= p["tensor_columns"] <= 128 and (p["smem_bytes"] + 1024) * 512 >= p["tensor_columns"] * 228 * 1024, p
                 else:
-                    assert p["splits"] == 1 or tiles * p["splits"] <= 74, p    # a unit of partial sums each, of 74
-                    assert 2 <= p["grid"] <= 148 and p["grid"] % 2 == 0 and p["smem_bytes"] == 226 * 1024
+                    parts[product] = tiles * p["splits"] if p["splits"] > 1 else 0
+                    assert 2 <= p["grid"] <= 148 and p["grid"] % 2 == 0
                 assert p["smem_bytes"] <= 226 * 1024
+            assert parts[0] <= 148 and parts[1] + parts[2] <= 148           # units of partial sums that there is room for
     for args in ((0, 32, 1), (32, 0, 1), (32, 32, 0), (32, 2 ** 21, 1), (2 ** 21, 32, 1), (2 ** 20, 1, 2 ** 31 - 1)):
         refused(E_SHAPE, B.gated_plan, *args)
     refused(E_SHAPE, B.gated_plan, 32, 32, 1, 3)

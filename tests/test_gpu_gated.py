@@ -98,7 +98,7 @@ def exact_case(M, K, F, dtype, name, **kw):
     c.block.free()
 
 
-SIZES = [(1, 4096, 100), (9, 2050, 1000), (40, 1024, 9999), (100, 3000, 40), (128, 8000, 520), (1, 1, 1), (1, 8, 8), (2, 64, 128), (3, 17, 5), (1, 512, 300), (7, 1000, 1333), (16, 256, 256), (65, 63, 65), (128, 128, 64), (129, 130, 129), (255, 520, 384), (256, 256, 128),
+SIZES = [(150, 20000, 256), (2500, 700, 2600), (200, 700, 70), (1, 4096, 100), (9, 2050, 1000), (40, 1024, 9999), (100, 3000, 40), (128, 8000, 520), (1, 1, 1), (1, 8, 8), (2, 64, 128), (3, 17, 5), (1, 512, 300), (7, 1000, 1333), (16, 256, 256), (65, 63, 65), (128, 128, 64), (129, 130, 129), (255, 520, 384), (256, 256, 128),
          (300, 1000, 1333), (513, 64, 1000), (1000, 2000, 136), (4000, 40, 24), (20000, 72, 100), (2500, 300, 700)]
 
 
@@ -267,8 +267,9 @@ def test_another_stream_a_captured_graph_and_other_weights():
 
 
 FORMS = {  # rows, K, F, product, block that is left out, what patdnn_gated_plan says
-    "forward, one range": (300, 700, 2600, 0, 3, dict(splits=1, blocks=11, few_rows=0)),
-    "forward, split": (150, 4096, 256, 0, 2, dict(splits=16, few_rows=0)),
+    "forward, one range": (2500, 700, 2600, 0, 13, dict(splits=1, blocks=11, few_rows=0)),
+    "forward, split": (150, 20000, 256, 0, 2, dict(splits=35, few_rows=0)),
+    "forward, rows of two tiles": (150, 4096, 256, 0, 2, dict(splits=8, few_rows=1, row_tiles=2)),
     "forward, few rows": (1, 4096, 8192, 0, 31, dict(splits=1, few_rows=1, blocks=64)),
     "forward, few rows, cluster of eight": (40, 4096, 256, 0, 2, dict(splits=8, few_rows=1)),
     "forward, few rows, more CTAs than SMs": (100, 200, 20000, 0, 3, dict(splits=1, few_rows=1)),
