@@ -121,9 +121,13 @@ int pairs_most();                           // pairs of CTAs that run at a time
 cudaError_t prepare_gated();
 cudaError_t launch_gated_forward(const GatedShape &s, const GatedCall &c, const GatedWork &w, cudaStream_t st, int *launches);
 cudaError_t launch_gated_gradient(const GatedShape &s, const GatedCall &c, const GatedWork &w, cudaStream_t st, int *launches);   // from dgu
-// rows of a 16-bit matrix to rows `to_row` apart, zeros behind them
-cudaError_t launch_gated_pack(const void *x, int64_t rows, int cols, int64_t row, void *to, int64_t to_row, int dtype, cudaStream_t st);
-// dgu from gu [rows][2 F] and dh
-cudaError_t launch_gated_slopes(const GatedShape &s, const void *gu, const void *dh, void *dgu, int64_t rows, cudaStream_t st);
+// In front of them, one launch: K columns of 16-bit rows to rows `to_row` apart, zeros behind them (rows = 0: nothing to pack), and, where dgu is not
+// nullptr, dgu from gu [rows][2 F] and dh
+struct GatedPack {
+    const void *from;
+    void *to;
+    int64_t rows, row, to_row;
+};
+cudaError_t launch_gated_operands(const GatedShape &s, const GatedPack (&packs)[3], const void *gu, const void *dh, void *dgu, int64_t rows, cudaStream_t st);
 
 }  // namespace patdnn

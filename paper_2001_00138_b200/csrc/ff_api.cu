@@ -137,26 +137,28 @@ bool copies_as_it_lies(int64_t row) { return row % 8 == 0; }           // rows o
 bool operand_aligned(const void *p, int64_t row) { return aligned(p, copies_as_it_lies(row) ? 16 : 2); }
 int64_t packed_row(int64_t K) { return (K + 7) / 8 * 8; }
 
-// x and the weights of a call as the products read them: packed first, where they cannot be copied as they lie.
-int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu, int64_t rows, GatedCall &c, cudaStream_t st) {
+// x and the weights of a call as the products read them: packed first, where they cannot be copied as they lie.  gu, dh: the gradient's; or nullptr
+int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu, const void *gu, const void *dh, int64_t rows, GatedCall &c, cudaStream_t st) {
     const GatedShape &s = h->s;
     c.x = x; c.wg = wg; c.wu = wu; c.x_row = s.x_row; c.w_row = s.w_row; c.rows = rows;
     c.spin_limit = h->spin_limit; c.test_skip_load = h->test_skip_load;
     const int64_t row = packed_row(s.K);
+    GatedPack packs[3] = {};
     if (h->x) {
-        if (const int rc = launched(launch_gated_pack(x, rows, s.K, s.x_row, h->x, row, s.dtype, st), 1, "packing launch")) return rc;
+        packs[0] = {x, h->x, rows, s.x_row, row};
         c.x = h->x;
         c.x_row = row;
     }
     if (h->weights) {
         void *second = static_cast<uint16_t *>(h->weights) + s.F * row;
-        if (const int rc = launched(launch_gated_pack(wg, s.F, s.K, s.w_row, h->weights, row, s.dtype, st), 1, "packing launch")) return rc;
-        if (const int rc = launched(launch_gated_pack(wu, s.F, s.K, s.w_row, second, row, s.dtype, st), 1, "packing launch")) return rc;
+        packs[1] = {wg, h->weights, s.F, s.w_row, row};
+        packs[2] = {wu, second, s.F, s.w_row, row};
         c.wg = h->weights;
         c.wu = second;
         c.w_row = row;
     }
-    return PATDNN_OK;
+    if (!h->x && !h->weights && !gu) return PATDNN_OK;
+    return launched(launch_gated_operands(s, packs, gu, dh, gu ? h->w.dgu : nullptr, rows, st), 1, "gated block operands launch");
 }
 
 }  // namespace
@@ -392,7 +394,7 @@ int patdnn_gated_run(patdnn_gated h, const void *x, const void *wg, const void *
     if (const int rc = on_device(h->device)) return rc;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     GatedCall c{};
-    if (const int rc = gated_operands(h, x, wg, wu, rows, c, st)) return rc;
+    if (const int rc = gated_operands(h, x, wg, wu, nullptr, nullptr, rows, c, st)) return rc;
     c.h = hidden; c.gu = gu;
     int n = 0;
     const cudaError_t e = launch_gated_forward(s, c, h->w, st, &n);
@@ -418,9 +420,8 @@ int patdnn_gated_grad(patdnn_gated h, const void *x, const void *wg, const void 
     }
     if (!dx && !dwg) return PATDNN_OK;
     GatedCall c{};
-    if (const int rc = gated_operands(h, x, wg, wu, rows, c, st)) return rc;
+    if (const int rc = gated_operands(h, x, wg, wu, gu, dh, rows, c, st)) return rc;
     c.dx = dx; c.dwg = dwg; c.dwu = dwu;
-    if (const int rc = launched(launch_gated_slopes(s, gu, dh, h->w.dgu, rows, st), 1, "gated block gradient launch")) return rc;
     int n = 0;
     const cudaError_t e = launch_gated_gradient(s, c, h->w, st, &n);
     return launched(e, n, "gated block gradient launch");

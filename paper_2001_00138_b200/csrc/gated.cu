@@ -20,17 +20,15 @@
 namespace patdnn {
 namespace {
 
-constexpr int kThreads = 384;
-constexpr int kEpilogueWarps = 8;
+constexpr int kThreads = 640;
+constexpr int kEpilogueWarps = 16;
 constexpr int kMostStages = 6;
 constexpr int kMostPairs = 128;
 constexpr int kHalf = 128 * 128;                       // bytes of one CTA's part of an operand in a stage: 128 rows x 64 columns
 constexpr int kStage = 2 * kHalf;
 constexpr int kPiece = 64;                             // bytes of a row that the epilogue stores at a time
 constexpr int kStaging = 32 * kPiece;                  // shared memory of an epilogue warp
-// Shared memory that keeps other kernels with tensor memory off the SM (they take 13 KB at least), since a pair holds all of two SMs' tensor memory
-// (see plan_mx4_linear), and leaves the join's CTAs (8 KB) room to arrive before this kernel ends.
-constexpr int kSmem = 217 * 1024;
+constexpr int kSmem = 226 * 1024;                      // all of an SM's: a pair holds all of two SMs' tensor memory (see plan_mx4_linear)
 
 struct Product {
     void *out0, *out1;                                 // h, nullptr | dx, nullptr | dwg, dwu
@@ -70,7 +68,7 @@ template <bool KMAJOR> __device__ __forceinline__ uint64_t part_desc(uint32_t ad
 }
 template <bool KMAJOR> constexpr uint64_t kNextK = KMAJOR ? 2 : 2048 >> 4;
 
-// Partial sums of a unit: a piece per epilogue warp of either CTA, [chunk of 32 columns][column][row].
+// Partial sums of a unit: a piece per epilogue warp of either CTA, [64 columns][32 rows].
 __device__ __forceinline__ float *part_of(float *partial, int64_t unit, uint32_t rank, int e) {
     return partial + unit * kGatedUnitFloats + (static_cast<int>(rank) * kEpilogueWarps + e) * (kGatedUnitFloats / (2 * kEpilogueWarps));
 }
@@ -88,6 +86,40 @@ __device__ __forceinline__ int unit_of(const GatedParams &p, int q, int pairs, i
     which = 1;
     const int before = q < units ? (units - q + pairs - 1) / pairs : 0, v = p.more[q] + i - before;
     return v < p.more[q + 1] ? v : -1;
+}
+
+// One warp: 64 columns of 32 rows of 16-bit values, 128 bytes each, from registers to rows aligned to 16 bytes, 16 rows at a time through `stage`.
+template <typename T>
+__device__ __forceinline__ void store_lines(const float (&v)[2][32], unsigned char *stage, T *y, int64_t ldy, int rows_left) {
+    const int lane = threadIdx.x & 31;
+    uint32_t w[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        const float lo = v[j >> 4][(2 * j) & 31], hi = v[j >> 4][(2 * j + 1) & 31];
+        if constexpr (std::is_same<T, __half>::value) {
+            const __half2 h = __floats2half2_rn(lo, hi);
+            w[j] = *reinterpret_cast<const uint32_t *>(&h);
+        } else {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+            w[j] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {             // 16-byte unit u of row r sits at unit u ^ (r & 7)
+        __syncwarp();
+        if ((lane >> 4) == half) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                *reinterpret_cast<uint4 *>(stage + (lane & 15) * 128 + ((u ^ (lane & 7)) << 4)) = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = i * 4 + (lane >> 3), u = lane & 7;
+            const uint4 t = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((u ^ (r & 7)) << 4));
+            if (half * 16 + r < rows_left) *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(y + (half * 16 + r) * ldy) + u * 16) = t;
+        }
+    }
 }
 
 // GRAD: the products are dx and dwg, dwu; else the one is h
@@ -216,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
         __syncwarp();
         if (last >= 0) mbar_wait(done + 8 * (last & 1), (last >> 1) & 1, ctx, 125);
     } else if (warp >= 4) {
-        const int e = warp - 4, quadrant = e & 3, half = e >> 2;
+        const int e = warp - 4, quadrant = e & 3, quarter = e >> 2;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quadrant * 32) << 16);
         const uint32_t drained0 = in_cta(drained, 0);
         unsigned char *stage = smem_raw + (smem - smem_u32(smem_raw)) + p.stages * kStage + e * kStaging;
@@ -225,8 +257,6 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
             const int tile = u / q.splits, buf = t & 1;
             const int nt = tile / q.m_tiles;
             int mt = tile - nt * q.m_tiles;
-            if (!mbar_wait(done + 8 * buf, (t >> 1) & 1, ctx, 126)) break;
-            tc_fence_after();
             T *out = static_cast<T *>(q.out0);
             if (GRAD && which == 1 && mt >= q.f_blocks) {
                 mt -= q.f_blocks;
@@ -234,61 +264,51 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
             }
             const int64_t row0 = static_cast<int64_t>(mt) * 256 + rank * 128 + quadrant * 32;
             const int rows_left = static_cast<int>(max(static_cast<int64_t>(-1), min(static_cast<int64_t>(32), q.rows - row0)));
-            // chunk j of the warp, 32 columns of the accumulator: forward gate, up, gate, up of its 64 outputs
-            auto fetch = [&](int j, uint32_t (&v)[32]) {
-                tmem_ld32(lanes + buf * 256 + (GRAD ? half * 128 + j * 32 : (j & 1) * 128 + half * 64 + (j >> 1) * 32), v);
-            };
-            auto put = [&](const float (&v)[32], T *base, int64_t ld, int col, int left) {
-                const uint64_t places = reinterpret_cast<uintptr_t>(base) | static_cast<uint64_t>(ld * sizeof(T));
-                const int aligned = places % 16 == 0 ? 16 : places % 4 == 0 ? 4 : 2;
-                store_piece<T, kPiece>(v, stage, base + row0 * ld + col, ld, rows_left, left, aligned);
-            };
-            if (q.splits > 1) {
-                float *to = part_of(p.partial, q.slot + u, rank, e) + lane;
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t v[32];
-                    fetch(j, v);
-                    if (lane < rows_left) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) to[(j * 32 + i) * 32] = __uint_as_float(v[i]);
-                    }
-                }
-            } else if (rows_left > 0) {
-                if constexpr (!GRAD) {
-                    for (int c = 0; c < 2; ++c) {
-                        const int f = nt * 128 + half * 64 + c * 32;
-                        if (f >= q.cols) break;
-                        uint32_t w0[32], w1[32];
-                        fetch(2 * c, w0);
-                        fetch(2 * c + 1, w1);
-                        float g[32], up[32];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) g[i] = __uint_as_float(w0[i]), up[i] = __uint_as_float(w1[i]);
-                        if (p.gu) {
-                            T *gu = static_cast<T *>(p.gu);
-                            put(g, gu, 2 * static_cast<int64_t>(q.cols), f, q.cols - f);
-                            put(up, gu + q.cols, 2 * static_cast<int64_t>(q.cols), f, q.cols - f);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) g[i] = activate1<ACT>(g[i]) * up[i];
-                        put(g, out, q.ld, f, q.cols - f);
-                    }
-                } else {
-                    for (int j = 0; j < 4; ++j) {
-                        const int n = nt * 256 + half * 128 + j * 32;
-                        if (n >= q.cols) break;
-                        uint32_t w[32];
-                        fetch(j, w);
-                        float v[32];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(w[i]);
-                        put(v, out, q.ld, n, q.cols - n);
-                    }
-                }
-            }
+            if (!mbar_wait(done + 8 * buf, (t >> 1) & 1, ctx, 126)) break;
+            tc_fence_after();
+            // 64 columns of the accumulator; forward: 32 of the gate's and the same 32 of the up projection's
+            float v[2][32];
+            const uint32_t from = lanes + buf * 256 + quarter * (GRAD ? 64 : 32);
+            tmem_ld32_async(from, reinterpret_cast<uint32_t *>(v[0]));
+            tmem_ld32_async(from + (GRAD ? 32 : 128), reinterpret_cast<uint32_t *>(v[1]));
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
             tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive_pair(drained0 + 8 * buf);
+            auto put = [&](const float (&w)[32], T *base, int64_t ld, int col, int left) {
+                const uint64_t places = reinterpret_cast<uintptr_t>(base) | static_cast<uint64_t>(ld * sizeof(T));
+                const int aligned = places % 16 == 0 ? 16 : places % 4 == 0 ? 4 : 2;
+                store_piece<T, kPiece>(w, stage, base + row0 * ld + col, ld, rows_left, left, aligned);
+            };
+            if (rows_left <= 0) continue;
+            if (q.splits > 1) {
+                float *to = part_of(p.partial, q.slot + u, rank, e) + lane;
+                if (lane < rows_left) {
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) to[i * 32] = v[i >> 5][i & 31];
+                }
+            } else if constexpr (!GRAD) {
+                const int f = nt * 128 + quarter * 32;
+                if (f >= q.cols) continue;
+                if (p.gu) {
+                    T *gu = static_cast<T *>(p.gu);
+                    put(v[0], gu, 2 * static_cast<int64_t>(q.cols), f, q.cols - f);
+                    put(v[1], gu + q.cols, 2 * static_cast<int64_t>(q.cols), f, q.cols - f);
+                }
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[0][i] = activate1<ACT>(v[0][i]) * v[1][i];
+                put(v[0], out, q.ld, f, q.cols - f);
+            } else {
+                const int n = nt * 256 + quarter * 64;
+                const uint64_t places = reinterpret_cast<uintptr_t>(out) | static_cast<uint64_t>(q.ld * sizeof(T));
+                if (places % 16 == 0 && q.cols - n >= 64) {
+                    store_lines<T>(v, stage, out + row0 * q.ld + n, q.ld, rows_left);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        if (n + 32 * j < q.cols) put(v[j], out, q.ld, n + 32 * j, q.cols - n - 32 * j);
+                }
+            }
         }
     }
     __syncwarp();
@@ -298,19 +318,22 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
     if (warp == 2) tmem_free_pair(tmem, 512);
 }
 
-// The sums of a tile's ranges, in their order, and the epilogue.  A warp takes 32 rows and 16 columns (forward: of both projections); the eight
-// warps of a CTA are the eight epilogue warps' pieces of one CTA's half of the tile.
+// The sums of a tile's ranges, and the epilogue.  A CTA takes 32 rows and 16 columns of an epilogue warp's piece (forward: of both projections); its
+// warps share the ranges, w, w + 8, ... to warp w, and the first one adds their sums in order.  (A warp alone waits 0.8 us per range.)
+constexpr int kJoinWarps = 8;
+
 template <bool GRAD, typename T, int ACT>
-__global__ void __launch_bounds__(256) gated_join_kernel(const __grid_constant__ GatedParams p, int first_ctas) {
-    constexpr int kPieces = GRAD ? 8 : 4, kWide = 16;
-    __shared__ __align__(16) unsigned char staging[8][32 * kWide * sizeof(T)];
+__global__ void __launch_bounds__(kJoinWarps * 32) gated_join_kernel(const __grid_constant__ GatedParams p, int first_ctas) {
+    constexpr int kPieces = GRAD ? 4 : 2, kWide = 16, kSums = GRAD ? 1 : 2;
+    __shared__ float sums[kJoinWarps][kSums][kWide][32];
+    __shared__ __align__(16) unsigned char staging[32 * kWide * sizeof(T)];
     pdl_trigger();
-    const int e = threadIdx.x >> 5, lane = threadIdx.x & 31, quadrant = e & 3, half = e >> 2;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     const bool second = GRAD && static_cast<int>(blockIdx.x) >= first_ctas;                      // CTAs of the first product come first
     const int block = blockIdx.x - (second ? first_ctas : 0);
     const Product &q = p.of[second];
-    const int piece = block % kPieces, rank = block / kPieces & 1, tile = block / (2 * kPieces);
-    const int nt = tile / q.m_tiles;
+    const int piece = block % kPieces, e = block / kPieces % kEpilogueWarps, rank = block / (kEpilogueWarps * kPieces) & 1;
+    const int tile = block / (2 * kEpilogueWarps * kPieces), quadrant = e & 3, quarter = e >> 2, nt = tile / q.m_tiles;
     int mt = tile - nt * q.m_tiles;
     T *out = static_cast<T *>(q.out0);
     if (second && mt >= q.f_blocks) {
@@ -319,41 +342,52 @@ __global__ void __launch_bounds__(256) gated_join_kernel(const __grid_constant__
     }
     const int64_t row0 = static_cast<int64_t>(mt) * 256 + rank * 128 + quadrant * 32;
     const int rows_left = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(32), q.rows - row0)));
-    const int col = GRAD ? nt * 256 + half * 128 + piece * kWide : nt * 128 + half * 64 + piece * kWide, left = q.cols - col;
+    const int col = (GRAD ? nt * 256 + quarter * 64 : nt * 128 + quarter * 32) + piece * kWide, left = q.cols - col;
     if (rows_left == 0 || left <= 0) return;
     pdl_wait();
-    auto sum = [&](int chunk, int first, float (&v)[kWide]) {          // columns [first, first + 16) of a chunk
+    float v[kSums][kWide] = {};
+    if (lane < rows_left) {
+        const float *from = part_of(p.partial, q.slot + static_cast<int64_t>(tile) * q.splits + warp, rank, e) + piece * kWide * 32 + lane;
+        for (int s = warp; s < q.splits; s += warps, from += static_cast<int64_t>(warps) * kGatedUnitFloats) {
+            float a[kSums][kWide];
 #pragma unroll
-        for (int i = 0; i < kWide; ++i) v[i] = 0.f;
-        if (lane >= rows_left) return;
-        const float *from = part_of(p.partial, q.slot + static_cast<int64_t>(tile) * q.splits, rank, e) + (chunk * 32 + first) * 32 + lane;
-#pragma unroll 4
-        for (int s = 0; s < q.splits; ++s, from += kGatedUnitFloats) {
+            for (int k = 0; k < kSums; ++k)
 #pragma unroll
-            for (int i = 0; i < kWide; ++i) v[i] += from[i * 32];
+                for (int i = 0; i < kWide; ++i) a[k][i] = from[(k * 32 + i) * 32];
+#pragma unroll
+            for (int k = 0; k < kSums; ++k)
+#pragma unroll
+                for (int i = 0; i < kWide; ++i) v[k][i] += a[k][i];
         }
-    };
-    auto put = [&](const float (&v)[kWide], T *base, int64_t ld) {
+    }
+    if (warp > 0) {
+#pragma unroll
+        for (int k = 0; k < kSums; ++k)
+#pragma unroll
+            for (int i = 0; i < kWide; ++i) sums[warp][k][i][lane] = v[k][i];
+    }
+    __syncthreads();
+    if (warp > 0) return;
+    for (int w = 1; w < warps; ++w)
+#pragma unroll
+        for (int k = 0; k < kSums; ++k)
+#pragma unroll
+            for (int i = 0; i < kWide; ++i) v[k][i] += sums[w][k][i][lane];
+    auto put = [&](const float (&w)[kWide], T *base, int64_t ld) {
         const uint64_t places = reinterpret_cast<uintptr_t>(base) | static_cast<uint64_t>(ld * sizeof(T));
         const int aligned = places % 16 == 0 ? 16 : places % 4 == 0 ? 4 : 2;
-        store_piece<T, kWide * sizeof(T)>(v, staging[e], base + row0 * ld + col, ld, rows_left, left, aligned);
+        store_piece<T, kWide * sizeof(T)>(w, staging, base + row0 * ld + col, ld, rows_left, left, aligned);
     };
-    float v[kWide];
     if constexpr (!GRAD) {
-        float up[kWide];
-        sum(piece >> 1 << 1, (piece & 1) * kWide, v);
-        sum((piece >> 1 << 1) + 1, (piece & 1) * kWide, up);
         if (p.gu) {
             T *gu = static_cast<T *>(p.gu);
-            put(v, gu, 2 * static_cast<int64_t>(q.cols));
-            put(up, gu + q.cols, 2 * static_cast<int64_t>(q.cols));
+            put(v[0], gu, 2 * static_cast<int64_t>(q.cols));
+            put(v[1], gu + q.cols, 2 * static_cast<int64_t>(q.cols));
         }
 #pragma unroll
-        for (int i = 0; i < kWide; ++i) v[i] = activate1<ACT>(v[i]) * up[i];
-    } else {
-        sum(piece >> 1, (piece & 1) * kWide, v);
+        for (int i = 0; i < kWide; ++i) v[0][i] = activate1<ACT>(v[0][i]) * v[1][i];
     }
-    put(v, out, q.ld);
+    put(v[0], out, q.ld);
 }
 
 // ---- forward, few rows -----------------------------------------------------------------------------------------------------
@@ -515,11 +549,14 @@ template <typename F> cudaError_t by_rows_kernel(int dtype, int act, F f) {
 
 int pairs_most() { return std::min(kMostPairs, std::max(1, sm_count() / 2)); }
 
+constexpr int64_t kEpilogueBlocks = 6;
 // Cuts the summed dimension into `splits` ranges or a few less, none of them empty.
 static void cut(GatedPlan &p, int64_t splits) {
     p.per_split = static_cast<int>(ceil_div(p.k_blocks, std::max<int64_t>(1, splits)));
     p.splits = static_cast<int>(ceil_div(p.k_blocks, p.per_split));
 }
+// A unit's time in blocks: short ones wait for the epilogue of the one before.
+static int64_t time_of(const GatedPlan &p) { return std::max<int64_t>(p.per_split, kEpilogueBlocks); }
 static int64_t units_of(const GatedPlan &p) { return static_cast<int64_t>(p.m_tiles) * p.n_tiles * p.splits; }
 constexpr int64_t kJoinBlocks = 20;                    // what partial sums cost, their stores and the join, in blocks of a tile (6 us, measured)
 
@@ -588,8 +625,8 @@ void plan_gated_gradient(int F, int K, int64_t rows, bool dx, bool dw, GatedPlan
             cut(plan[1], ceil_div(plan[1].k_blocks, longest[b]));
             const int64_t u0 = units_of(plan[0]), u1 = units_of(plan[1]);
             if ((plan[0].splits > 1 ? u0 : 0) + (plan[1].splits > 1 ? u1 : 0) > kGatedUnits * pairs) continue;
-            const int64_t even = ceil_div(u0 * plan[0].per_split + u1 * plan[1].per_split, pairs) + (u1 ? plan[1].per_split / 2 : 0);
-            const int64_t walk = std::max({ceil_div(u0, pairs) * plan[0].per_split, u1 ? static_cast<int64_t>(plan[1].per_split) : 0, even}) +
+            const int64_t even = ceil_div(u0 * time_of(plan[0]) + u1 * time_of(plan[1]), pairs) + (u1 ? time_of(plan[1]) / 2 : 0);
+            const int64_t walk = std::max({ceil_div(u0, pairs) * time_of(plan[0]), u1 ? time_of(plan[1]) : 0, even}) +
                                  (plan[0].splits + plan[1].splits > 2 ? kJoinBlocks : 0);
             if (walk < shortest) {
                 shortest = walk;
@@ -633,12 +670,13 @@ static cudaError_t launch_products(const GatedMaps &maps, GatedParams &p, const 
                                    cudaStream_t st, int *launches) {
     p.stages = kMostStages; p.partial = w.partial; p.status = w.status; p.spin_limit = c.spin_limit; p.test_skip_load = c.test_skip_load;
     int joins[2];
-    for (int i = 0; i < 2; ++i) joins[i] = p.of[i].splits > 1 ? p.of[i].m_tiles * p.of[i].n_tiles * (grad ? 16 : 8) : 0;
+    for (int i = 0; i < 2; ++i) joins[i] = p.of[i].splits > 1 ? p.of[i].m_tiles * p.of[i].n_tiles * 2 * kEpilogueWarps * (grad ? 4 : 2) : 0;
+    const int join_warps = std::min(kJoinWarps, std::max(p.of[0].splits, p.of[1].splits));
     *launches = joins[0] + joins[1] > 0 ? 2 : 1;
     return by_kernel(grad, s.dtype, s.act, [&](auto product, auto join) {
         const cudaError_t r = launch_pdl(product, dim3(grid), dim3(kThreads), kSmem, st, 2, maps, p);
         if (r != cudaSuccess || *launches == 1) return r;
-        return launch_pdl(join, dim3(joins[0] + joins[1]), dim3(256), 0, st, 1, p, joins[0]);
+        return launch_pdl(join, dim3(joins[0] + joins[1]), dim3(join_warps * 32), 0, st, 1, p, joins[0]);
     });
 }
 
@@ -692,14 +730,15 @@ cudaError_t launch_gated_gradient(const GatedShape &s, const GatedCall &c, const
     if (e != cudaSuccess) return e;
     // The second product's units go to the pairs that the first one left with the fewest blocks: up to a common level, what remains one by one.
     const int pairs = plan[0].grid / 2;
-    const int64_t level = (static_cast<int64_t>(x.units) * x.per_split + static_cast<int64_t>(dw.units) * dw.per_split) / pairs;
+    const int64_t x_time = time_of(plan[0]), dw_time = time_of(plan[1]);
+    const int64_t level = (x.units * x_time + dw.units * dw_time) / pairs;
     int64_t given = 0, load[kMostPairs];
     int order[kMostPairs], count[kMostPairs];
     for (int q = 0; q < pairs; ++q) {
-        const int64_t before = static_cast<int64_t>(x.units / pairs + (q < x.units % pairs)) * x.per_split;
-        count[q] = static_cast<int>(std::max<int64_t>(0, std::min((level - before) / dw.per_split, dw.units - given)));
+        const int64_t before = (x.units / pairs + (q < x.units % pairs)) * x_time;
+        count[q] = static_cast<int>(std::max<int64_t>(0, std::min((level - before) / dw_time, dw.units - given)));
         given += count[q];
-        load[q] = before + static_cast<int64_t>(count[q]) * dw.per_split;
+        load[q] = before + count[q] * dw_time;
         order[q] = q;
     }
     std::sort(order, order + pairs, [&](int a, int b) { return load[a] != load[b] ? load[a] < load[b] : a < b; });
