@@ -81,6 +81,7 @@ struct RmsGradCall {
     float *dgamma, *ws;
     int64_t rows;
 };
+cudaError_t prepare_rms();                  // opt in to the dynamic shared memory
 size_t rms_workspace_floats(const RmsShape &s);
 cudaError_t launch_rms_grad(const RmsShape &s, const RmsGradCall &c, cudaStream_t st, int *launches);
 

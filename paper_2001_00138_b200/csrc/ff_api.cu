@@ -182,6 +182,7 @@ int patdnn_rms_create(const patdnn_rms_desc *desc, patdnn_rms *out) {
     h->s = s;
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = allocate(&h->ws, rms_workspace_floats(s));
+    if (e == cudaSuccess) e = prepare_rms();
     if (e != cudaSuccess) return failed(h, e, "patdnn_rms_create");
     *out = h;
     return PATDNN_OK;

@@ -59,18 +59,18 @@ template <int A> __device__ __forceinline__ void store_codes(uint8_t *to, const 
     }
 }
 
-// A warp takes consecutive columns of a row in accesses of A elements per lane: access j, lane l, element e is column (32 j + l) A + e, so
-// that every access of the warp is one contiguous piece whatever A is.
-// E elements per lane, from `p` (the warp's first column); `left` of the row's columns are there, zeros behind them.
-template <typename T, int A, int E>
+// L lanes (all of a warp, or a half or a quarter of it) take consecutive columns of a row in accesses of A elements per lane: access j, lane l,
+// element e is column (L j + l) A + e, so that every access is one contiguous piece whatever A is.
+// E elements per lane, from `p` (the first column); `left` of the row's columns are there, zeros behind them.
+template <typename T, int A, int E, int L = 32>
 struct Strip {
     static constexpr int NA = E / A;
     Pack<T, A> v[NA];
     __device__ __forceinline__ void load(const T *p, int left) {
-        const int lane = threadIdx.x & 31;
+        const int lane = threadIdx.x & (L - 1);
 #pragma unroll
         for (int j = 0; j < NA; ++j) {
-            const int c = (32 * j + lane) * A;
+            const int c = (L * j + lane) * A;
             if (c + A <= left) {
                 v[j].load(p + c);
             } else {
@@ -88,10 +88,10 @@ struct Strip {
         }
     }
     __device__ __forceinline__ void store(T *p, int left) const {
-        const int lane = threadIdx.x & 31;
+        const int lane = threadIdx.x & (L - 1);
 #pragma unroll
         for (int j = 0; j < NA; ++j) {
-            const int c = (32 * j + lane) * A;
+            const int c = (L * j + lane) * A;
             if (c + A <= left) {
                 v[j].store(p + c);
             } else if constexpr (A > 1) {
@@ -118,33 +118,31 @@ struct Strip {
     }
 };
 
-// The warp's strip of a row as 8-bit blocks.  `codes`: the row's place in its first column tile (tile base, row 0 of the tile), `scales`:
+// The strip of a row as 8-bit blocks.  `codes`: the row's place in its first column tile (tile base, row 0 of the tile), `scales`:
 // the row tile's scales; `r`: row of the row tile; c0: the strip's first column (a multiple of 128); `padded`: columns up to the end of the
-// last column tile, which are written.
-template <int A, int E>
+// last column tile, which are written as far as the strip goes.
+template <int A, int E, int L>
 __device__ __forceinline__ void store_blocks(uint8_t *codes, uint8_t *scales, int r, int64_t c0, int64_t padded, const float (&v)[E]) {
-    constexpr int PER = A == 8 ? 1 : 4 / A;            // accesses to a block (of 16 bytes: two blocks to an access)
-    const int lane = threadIdx.x & 31;
+    constexpr int NA = E / A, ONE = L * A >= 128 ? 1 : 128 / (L * A), PER = ONE < NA ? ONE : NA;   // accesses to a block (256 columns: two blocks to an access)
+    constexpr int LANES = L * A > 128 ? 128 / A : L;   // lanes that share a block
+    const int lane = threadIdx.x & (L - 1);
 #pragma unroll
-    for (int q = 0; q < E / A; q += PER) {
+    for (int q = 0; q < NA; q += PER) {
         float m = max_abs(v[q * A], v[q * A + A * PER - 1]);
 #pragma unroll
         for (int e = 1; e < A * PER - 1; ++e) m = max_abs(m, v[q * A + e]);
         uint32_t top = magnitude_bits(m);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 4));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 8));
-        if constexpr (A < 8) top = max(top, __shfl_xor_sync(0xffffffffu, top, 16));
+#pragma unroll
+        for (int s = 1; s < LANES; s *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
         float inverse;
         const uint32_t byte = scale8_of(top, inverse);
 #pragma unroll
         for (int j = q; j < q + PER; ++j) {
-            const int64_t c = c0 + (32 * j + lane) * A;
+            const int64_t c = c0 + (L * j + lane) * A;
             if (c >= padded) continue;
             const int64_t t = c >> 7;
             store_codes<A>(codes + t * (128 * 128) + mx8_place(r, static_cast<int>(c & 127)), v + j * A, inverse);
-            if (j == q && (A == 8 ? (lane & 15) == 0 : lane == 0)) scales[(t >> 2) * 512 + mx8_scale_place(r, static_cast<int>(t))] = static_cast<uint8_t>(byte);
+            if (j == q && (lane & (LANES - 1)) == 0) scales[(t >> 2) * 512 + mx8_scale_place(r, static_cast<int>(t))] = static_cast<uint8_t>(byte);
         }
     }
 }

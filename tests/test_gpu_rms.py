@@ -39,7 +39,7 @@ def forward_reference(x, r, gamma):
     return s, rstd, s * rstd * gamma.double()
 
 
-SIZES = [(1, 1), (1, 8), (3, 31), (2, 127), (5, 128), (4, 129), (40, 256), (33, 257), (7, 1000), (1, 4096), (300, 1001), (3000, 512), (200, 2050), (700, 4096), (5, 5000),
+SIZES = [(5001, 36), (3002, 100), (2999, 7), (70, 64), (700, 65), (333, 2560), (1, 1), (1, 8), (3, 31), (2, 127), (5, 128), (4, 129), (40, 256), (33, 257), (7, 1000), (1, 4096), (300, 1001), (3000, 512), (200, 2050), (700, 4096), (5, 5000),
          (260, 8192), (3, 8193), (170, 12345), (2, 16384), (40, 20001), (3, 65536)]
 
 
@@ -76,7 +76,7 @@ def test_forward(M, C, dtype, slack, offset):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("M, C", [(1, 1), (3, 31), (40, 127), (130, 128), (257, 129), (33, 1000), (1, 4096), (500, 2048), (9, 5001), (300, 8192), (140, 9000), (3, 65536)])
+@pytest.mark.parametrize("M, C", [(5001, 36), (3002, 100), (2999, 7), (200, 2560), (1, 1), (3, 31), (40, 127), (130, 128), (257, 129), (33, 1000), (1, 4096), (500, 2048), (9, 5001), (300, 8192), (140, 9000), (3, 65536)])
 @pytest.mark.parametrize("slack", [0, 8, 2, 3])
 def test_8_bit_form(M, C, dtype, slack):
     """Equal to the quantisation (tested by itself) of the fp32 values that the formula gives step by step with the statistics that the call returns."""
