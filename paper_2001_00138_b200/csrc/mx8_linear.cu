@@ -450,8 +450,10 @@ Mx8Launch plan_mx8_linear(Mx8Params &p) {
     p.tile_n = p.rows <= 128 ? static_cast<int>(ceil_div(p.rows, 16) * 16) : 128;
     p.n_tiles = static_cast<int>(ceil_div(p.rows, p.tile_n));
     const int64_t tiles = static_cast<int64_t>(p.f_tiles) * p.n_tiles;
-    // Exchanging partial sums takes time in proportion to the rows: with up to 64 two column tiles per CTA are enough, with more it takes eight.
-    const int least = p.tile_n <= 64 ? 2 : 8;
+    // Exchanging partial sums takes time in proportion to the rows, 3 us for 128: with up to 64 two column tiles per CTA are enough, with more it takes
+    // sixteen column tiles, four to a CTA (333 x 2048 -> 1000: 8.6 us in four splits, 10.1 in two; 256 x 1024 -> 1024: 6.2 in none, 7.6 in four).
+    // (Lanes push consecutive words to a finisher; 16 bytes per lane, further apart, took 2 us more.)
+    const int least = p.tile_n <= 64 ? 2 : p.col_tiles < 16 ? p.col_tiles : 4;
     p.splits = 1;
     while (p.splits < 8 && tiles * p.splits * 2 <= sm_count() && p.col_tiles >= p.splits * 2 * least) p.splits *= 2;
     p.tiles_per_split = static_cast<int>(ceil_div(p.col_tiles, p.splits));

@@ -139,7 +139,8 @@ FORMS = {  # rows, K, F, 8-bit rows, and what patdnn_linear8_plan says
     "quantises its rows, one tile": (8, 60, 30000, False, dict(quantises=1, splits=1)),
     "a cluster of eight": (40, 8192, 256, True, dict(persistent=0, splits=8)),
     "a cluster of eight, many rows": (128, 16384, 300, False, dict(persistent=0, splits=8, tile_rows=128)),
-    "a cluster of two, uneven": (200, 2300, 400, True, dict(persistent=0, splits=2, column_tiles=18)),
+    "a cluster of two, uneven": (200, 2300, 4000, True, dict(persistent=0, splits=2, column_tiles=18)),
+    "a cluster of four, uneven": (200, 2300, 400, True, dict(persistent=0, splits=4, column_tiles=18)),
     "no cluster, ring wraps": (300, 1500, 700, True, dict(persistent=0, splits=1, column_tiles=12)),
     "256 outputs, odd last tile": (9500, 300, 513, True, dict(persistent=1, tile_outputs=256, column_tiles=3)),
     "256 outputs, ring wraps": (9500, 1100, 513, False, dict(persistent=1, tile_outputs=256, column_tiles=9)),
