@@ -21,28 +21,35 @@ struct AuxJob {
     void *to;
     int64_t row, dh_row, to_row;                       // strides in elements
     int64_t units;                                     // rows times pieces
-    int cols, padded, pieces, width;                   // padded: columns that are written; pieces of 256 of them; elements per access
+    int cols, padded, pieces;                          // padded: columns that are written; pieces of 256 of them
+    int aligned;                                       // slopes: rows of gu and dh are, to 16 bytes
 };
 struct AuxArgs {
     AuxJob job[kJobs];
     int64_t units;
 };
 
-template <typename T, int A>
+template <typename T>
 __device__ __forceinline__ void pack(const AuxJob &a, int64_t row, int c0) {
-    Strip<T, A, 8> s;
-    s.load(static_cast<const T *>(a.x) + row * a.row + c0, a.cols - c0);
+    Strip<T, 8, 8> s;
+    s.load_any(static_cast<const T *>(a.x) + row * a.row + c0, a.cols - c0);
     s.store(static_cast<T *>(a.to) + row * a.to_row + c0, a.padded - c0);
 }
 
-template <typename T, int A, int ACT>
+template <typename T, bool ALIGNED, int ACT>
 __device__ __forceinline__ void slopes(const AuxJob &a, int64_t row, int c0) {
     const int left = a.cols - c0;
-    Strip<T, A, 8> sg, su, sd;
-    const T *g = static_cast<const T *>(a.x) + row * a.row + c0;
-    sg.load(g, left);
-    su.load(g + a.cols, left);
-    sd.load(static_cast<const T *>(a.dh) + row * a.dh_row + c0, left);
+    Strip<T, 8, 8> sg, su, sd;
+    const T *g = static_cast<const T *>(a.x) + row * a.row + c0, *dh = static_cast<const T *>(a.dh) + row * a.dh_row + c0;
+    if constexpr (ALIGNED) {
+        sg.load(g, left);
+        su.load(g + a.cols, left);
+        sd.load(dh, left);
+    } else {
+        sg.load_any(g, left);
+        su.load_any(g + a.cols, left);
+        sd.load_any(dh, left);
+    }
     float fg[8], fu[8], fd[8];
     sg.widen_to(fg);
     su.widen_to(fu);
@@ -81,13 +88,10 @@ __global__ void __launch_bounds__(kWarps * 32) gated_operands_kernel(const __gri
         const int64_t row = u / a.pieces;
         const int c0 = static_cast<int>(u - row * a.pieces) * kColumns;
         if (j == kJobs - 1) {
-            if (a.width == 8) slopes<T, 8, ACT>(a, row, c0);
-            else if (a.width == 2) slopes<T, 2, ACT>(a, row, c0);
-            else slopes<T, 1, ACT>(a, row, c0);
-        } else if (a.width == 2) {                     // (rows of whole 16-byte units are not packed, and aligned else)
-            pack<T, 2>(a, row, c0);
+            if (a.aligned) slopes<T, true, ACT>(a, row, c0);
+            else slopes<T, false, ACT>(a, row, c0);
         } else {
-            pack<T, 1>(a, row, c0);
+            pack<T>(a, row, c0);
         }
     }
 }
@@ -102,7 +106,6 @@ cudaError_t launch_gated_operands(const GatedShape &s, const GatedPack (&packs)[
         a.x = packs[i].from; a.to = packs[i].to; a.row = packs[i].row; a.to_row = packs[i].to_row; a.cols = s.K; a.padded = static_cast<int>(packs[i].to_row);
         a.pieces = static_cast<int>(ceil_div(a.padded, kColumns));
         a.units = packs[i].rows * a.pieces;
-        a.width = std::min(2, strip_width(s.dtype, {a.x}, {a.row}));
     }
     if (dgu) {
         AuxJob &a = args.job[kJobs - 1];
@@ -110,7 +113,7 @@ cudaError_t launch_gated_operands(const GatedShape &s, const GatedPack (&packs)[
         a.cols = s.F; a.padded = gated_padded(s.F); a.to_row = 2 * static_cast<int64_t>(a.padded);
         a.pieces = static_cast<int>(ceil_div(a.padded, kColumns));
         a.units = rows * a.pieces;
-        a.width = strip_width(s.dtype, {gu, dh}, {s.F, s.h_row});
+        a.aligned = strip_width(s.dtype, {gu, dh}, {s.F, s.h_row}) == 8;
     }
     for (const AuxJob &a : args.job) args.units += a.units;
     const dim3 grid(static_cast<unsigned>(std::min<int64_t>(ceil_div(args.units, kWarps), static_cast<int64_t>(sm_count()) * 32)));

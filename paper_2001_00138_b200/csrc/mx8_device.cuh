@@ -87,6 +87,48 @@ struct Strip {
             }
         }
     }
+    // The same for A = 16 bytes from rows that are aligned to their elements only: a lane reads the aligned 16 bytes in which its own begin, takes the
+    // next ones from the next lane and shifts.  Only 16-byte units that hold an element of the row are read.  All lanes of the warp call it.
+    __device__ __forceinline__ void load_any(const T *p, int left) {
+        static_assert(sizeof(T) * A == 16, "whole units");
+        const int lane = threadIdx.x & (L - 1);
+#pragma unroll
+        for (int j = 0; j < NA; ++j) {
+            const T *from = p + j * L * A;
+            const int here = left - j * L * A, over = static_cast<int>(reinterpret_cast<uintptr_t>(from) & 15);          // bytes in front of the row's
+            const int bytes = here * static_cast<int>(sizeof(T)), first = lane * 16 - over;
+            const uint4 *unit = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(from) + first);
+            uint4 a = make_uint4(0, 0, 0, 0), b = a;
+            if (first < bytes) a = *unit;
+            if (lane == L - 1 && over && first + 16 < bytes) b = unit[1];
+            uint32_t w[8] = {a.x, a.y, a.z, a.w, 0, 0, 0, 0};
+            const uint32_t tail[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t t = __shfl_down_sync(0xffffffffu, w[i], 1, L);
+                w[4 + i] = lane == L - 1 ? tail[i] : t;
+            }
+            if (over & 8) {
+#pragma unroll
+                for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+            }
+            if (over & 4) {
+#pragma unroll
+                for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[j].w[i] = __funnelshift_r(w[i], w[i + 1], (over & 2) * 8);
+            const int there = here - lane * A;         // of the lane's elements
+            if (there < A) {
+#pragma unroll
+                for (int e = 0; e < A; ++e)
+                    if (e >= there) {
+                        if constexpr (sizeof(T) == 4) v[j].w[e] = 0;
+                        else v[j].w[e / 2] &= e & 1 ? 0xffffu : 0xffff0000u;
+                    }
+            }
+        }
+    }
     __device__ __forceinline__ void store(T *p, int left) const {
         const int lane = threadIdx.x & (L - 1);
 #pragma unroll

@@ -400,14 +400,16 @@ RmsPlan plan_of(int C, int64_t rows, int E, int warps, int ctas_per_sm) {
     p.grid = static_cast<int>(std::min(ctas, std::max<int64_t>(1, most))) * p.cluster;
     return p;
 }
+// Eight columns to a lane leave clearly fewer lanes without any than sixteen.
+bool narrow(int C) { return 10 * ceil_div(C, 512) * 512 > 13 * ceil_div(C, 256) * 256; }
 // Few rows are spread over as many warps as can be; many take more columns per lane, so that more bytes are in flight.
 RmsPlan plan_forward(int C, int64_t rows) {
-    if (C <= 256 || (C <= kMostWarps * 256 && rows <= sm_count())) return plan_of(C, rows, 8, 8, 4);
+    if (C <= 256 || (C <= kMostWarps * 256 && (rows <= sm_count() || narrow(C)))) return plan_of(C, rows, 8, 8, 4);
     return plan_of(C, rows, 16, 8, 2);
 }
 RmsPlan plan_backward(int C, int64_t rows, int dtype) {
     const bool few = rows <= 2 * sm_count();           // a row or two per CTA: nothing to copy ahead
-    const bool eight = C <= 256 || (C <= kMostWarps * 256 && (few || dtype == PATDNN_F32)) || (dtype == PATDNN_F32 && C <= 8 * kMostWarps * 256);
+    const bool eight = C <= 256 || (C <= kMostWarps * 256 && (few || narrow(C) || dtype == PATDNN_F32)) || (dtype == PATDNN_F32 && C <= 8 * kMostWarps * 256);
     RmsPlan p = plan_of(C, rows, eight ? 8 : 16, few ? 8 : grad_warps(eight ? 8 : 16), 1);
     p.async = !few;
     return p;

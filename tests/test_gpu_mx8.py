@@ -19,12 +19,12 @@ def act_of(name):
     return [B.ACT_NONE, B.ACT_RELU, B.ACT_SILU][ACTS.index(name)]
 
 
-SIZES = [(1, 1), (1, 31), (3, 32), (2, 33), (8, 63), (33, 64), (128, 65), (129, 128), (31, 129), (97, 200), (5, 256), (7, 511), (256, 513), (130, 2049), (40, 4096)]
+SIZES = [(20001, 60), (5003, 127), (3001, 250), (30000, 8), (1, 1), (1, 31), (3, 32), (2, 33), (8, 63), (33, 64), (128, 65), (129, 128), (31, 129), (97, 200), (5, 256), (7, 511), (256, 513), (130, 2049), (40, 4096)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("rows, cols", SIZES)
-@pytest.mark.parametrize("slack, offset", [(0, 0), (8, 0), (2, 2), (3, 1)])
+@pytest.mark.parametrize("slack, offset", [(0, 0), (8, 0), (2, 2), (3, 1), (5, 7), (1, 6)])
 def test_quantise_and_back(rows, cols, dtype, slack, offset):
     import torch
     from paper_2001_00138_b200 import binding as B
