@@ -166,7 +166,8 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
         for (int i = 0; ok && (u = unit_of(p, pair, pairs, i, which)) >= 0; ++i) {
             const Product &q = p.of[which];
             const int tile = u / q.splits, k0 = (u - tile * q.splits) * q.per_split, k1 = min(q.k_blocks, k0 + q.per_split);
-            const int nt = tile / q.m_tiles, mt = tile - nt * q.m_tiles;
+            int mt, nt;
+            banded(tile, q.m_tiles, q.n_tiles, mt, nt);
             // K-major rows that do not exist are not copied where they are all of a CTA's, or where the product has fewer rows than a tile: the MMAs read
             // whatever is there and give rows that nobody stores.  (Filling 127 of 128 rows with zeros took the copies twice the time of 128 rows.)
             const bool one = !(GRAD && which) && q.rows <= 128, has_rows = !one || rank == 0;
@@ -255,8 +256,8 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
         for (int t = 0; (u = unit_of(p, pair, pairs, t, which)) >= 0; ++t) {
             const Product &q = p.of[which];
             const int tile = u / q.splits, buf = t & 1;
-            const int nt = tile / q.m_tiles;
-            int mt = tile - nt * q.m_tiles;
+            int mt, nt;
+            banded(tile, q.m_tiles, q.n_tiles, mt, nt);
             T *out = static_cast<T *>(q.out0);
             if (GRAD && which == 1 && mt >= q.f_blocks) {
                 mt -= q.f_blocks;
@@ -333,8 +334,9 @@ __global__ void __launch_bounds__(kJoinWarps * 32) gated_join_kernel(const __gri
     const int block = blockIdx.x - (second ? first_ctas : 0);
     const Product &q = p.of[second];
     const int piece = block % kPieces, e = block / kPieces % kEpilogueWarps, rank = block / (kEpilogueWarps * kPieces) & 1;
-    const int tile = block / (2 * kEpilogueWarps * kPieces), quadrant = e & 3, quarter = e >> 2, nt = tile / q.m_tiles;
-    int mt = tile - nt * q.m_tiles;
+    const int tile = block / (2 * kEpilogueWarps * kPieces), quadrant = e & 3, quarter = e >> 2;
+    int mt, nt;
+    banded(tile, q.m_tiles, q.n_tiles, mt, nt);
     T *out = static_cast<T *>(q.out0);
     if (second && mt >= q.f_blocks) {
         mt -= q.f_blocks;

@@ -32,6 +32,15 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, int row_bytes) {
     return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (uint64_t(1) << 16) | (static_cast<uint64_t>(row_bytes * 8 >> 4) << 32) |
            (uint64_t(1) << 46) | (layout << 61);
 }
+// Tiles in the order in which the CTAs (or pairs) take them: bands of 16 tiles of one operand, in a band all tiles of the other one after the other.
+// Those that run at a time then share both operands about evenly, and a band stays in L2 while the other operand passes.  (Without bands, 64 x 8
+// tiles of 256 x 256 with a summed dimension of 4096 read the larger operand, 134 MB, eight times.)
+__device__ __forceinline__ void banded(int tile, int m_tiles, int n_tiles, int &mt, int &nt) {
+    constexpr int kBand = 16;
+    const int band = tile / (kBand * n_tiles), rest = tile - band * kBand * n_tiles, here = min(kBand, m_tiles - band * kBand);
+    nt = rest / here;
+    mt = band * kBand + rest - nt * here;
+}
 // Tensor memory of a CTA: one whole warp takes it and publishes its address behind the next barrier, one whole warp gives it back.
 __device__ __forceinline__ void tmem_allocate(uint32_t *slot, uint32_t columns) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(columns) : "memory");

@@ -297,7 +297,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx8_pair_kernel(const __grid_
         bool ok = true;
         pdl_wait();
         for (int t = first; ok && t < tiles; t += step) {
-            const int nt = t / p.f_tiles, ft = t - nt * p.f_tiles;
+            int ft, nt;
+            banded(t, p.f_tiles, p.n_tiles, ft, nt);
             const int xr = nt * 2 + static_cast<int>(rank), wr = ft * 2 + static_cast<int>(rank);      // row tiles of 128
             for (int i = 0; i < p.col_tiles; ++i) {
                 if (issued >= kPairStages && !warp_wait(empty + 8 * slot, phase, ctx, 131)) { ok = false; break; }
@@ -374,7 +375,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx8_pair_kernel(const __grid_
         const int aligned = places % 16 == 0 ? 16 : places % 4 == 0 ? 4 : 2;
         uint32_t phase = 0;
         for (int t = first; t < tiles; t += step) {
-            const int nt = t / p.f_tiles, f0 = (t - nt * p.f_tiles) * 256 + quarter * 64;
+            int ft, nt;
+            banded(t, p.f_tiles, p.n_tiles, ft, nt);
+            const int f0 = ft * 256 + quarter * 64;
             const int64_t row0 = static_cast<int64_t>(nt) * 256 + rank * 128 + quadrant * 32;
             __syncwarp();
 #pragma unroll
