@@ -40,7 +40,8 @@ struct Product {
     int units;                                         // tiles times splits
     int slot;                                          // of its first unit among the partial sums
 };
-// Pair q of P takes the units q, q + P, ... of the first product, then those from more[q] to more[q + 1] of the second.
+// Pair q of P takes the units q, q + P, ... of the first product, then of the second those from more[q] to more[q + 1], which even the pairs out, and
+// the units more[P] + q, more[P] + q + P, ..., `common` of them: what runs at a time lies together, as the bands of tiles want it.
 struct GatedParams {
     Product of[2];
     void *gu;                                          // forward: both projections, or nullptr
@@ -50,6 +51,7 @@ struct GatedParams {
     int *status;
     uint32_t spin_limit;
     int test_skip_load;
+    int common;
     int more[kMostPairs + 1];
 };
 
@@ -84,8 +86,8 @@ __device__ __forceinline__ int unit_of(const GatedParams &p, int q, int pairs, i
     which = 0;
     if (u < units) return u;
     which = 1;
-    const int before = q < units ? (units - q + pairs - 1) / pairs : 0, v = p.more[q] + i - before;
-    return v < p.more[q + 1] ? v : -1;
+    const int later = i - (q < units ? (units - q + pairs - 1) / pairs : 0), v = p.more[q] + later, round = v - p.more[q + 1];
+    return round < 0 ? v : round < p.common ? p.more[pairs] + round * pairs + q : -1;
 }
 
 // One warp: 64 columns of 32 rows of 16-bit values, 128 bytes each, from registers to rows aligned to 16 bytes, 16 rows at a time through `stage`.
@@ -745,7 +747,8 @@ cudaError_t launch_gated_gradient(const GatedShape &s, const GatedCall &c, const
     }
     std::sort(order, order + pairs, [&](int a, int b) { return load[a] != load[b] ? load[a] < load[b] : a < b; });
     for (int i = 0; given < dw.units; ++given, i = i + 1 < pairs ? i + 1 : 0) ++count[order[i]];
-    for (int q = 0; q < pairs; ++q) p.more[q + 1] = p.more[q] + count[q];
+    p.common = *std::min_element(count, count + pairs);
+    for (int q = 0; q < pairs; ++q) p.more[q + 1] = p.more[q] + count[q] - p.common;
     return launch_products(maps, p, s, c, w, plan[0].grid, true, st, launches);
 }
 

@@ -36,7 +36,7 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, int row_bytes) {
 // Those that run at a time then share both operands about evenly, and a band stays in L2 while the other operand passes.  (Without bands, 64 x 8
 // tiles of 256 x 256 with a summed dimension of 4096 read the larger operand, 134 MB, eight times.)
 __device__ __forceinline__ void banded(int tile, int m_tiles, int n_tiles, int &mt, int &nt) {
-    constexpr int kBand = 16;
+    constexpr int kBand = 8;
     const int band = tile / (kBand * n_tiles), rest = tile - band * kBand * n_tiles, here = min(kBand, m_tiles - band * kBand);
     nt = rest / here;
     mt = band * kBand + rest - nt * here;
