@@ -237,6 +237,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx8_linear_kernel(Mx8Params p)
 // of the first CTA issues the MMAs, warps 4 to 19 are the epilogue: they move the finished accumulator to registers, hand tensor memory back,
 // and convert and store while the next tile is multiplied.  A lane owns a row of y; pieces of 32 rows pass through shared memory so that they
 // are stored as whole sectors.
+// The scales of four column tiles come and go to tensor memory with the first of them (for each of them: 9 us of 100 for 8192 x 4096 -> 4096).
 // Per column tile a CTA writes 33 KB into shared memory and the MMAs read 32 KB from it in the 512 cycles that they take (tiles of 128 x 256 for
 // a single CTA: 51 and 48 KB, more than its 128 bytes per cycle).  The tiles come as tensor-map copies of rows that are swizzled already,
 // since only such copies may count on the other CTA's barrier.
@@ -304,14 +305,17 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx8_pair_kernel(const __grid_
                 if (issued >= kPairStages && !warp_wait(empty + 8 * slot, phase, ctx, 131)) { ok = false; break; }
                 if (leader && issued + 1 != p.test_skip_load) {
                     const uint32_t at = smem + slot * kPairStage, bar = full0 + 8 * slot;
-                    if (rank == 0) mbar_expect_tx(full + 8 * slot, 2 * (2 * kTileCodes + 3 * kMx8Scales));
+                    const bool scales = (i & 3) == 0;                    // of this column tile and the next three
+                    if (rank == 0) mbar_expect_tx(full + 8 * slot, 2 * (2 * kTileCodes + (scales ? 3 * kMx8Scales : 0)));
                     // (row tiles that do not exist are outside the maps: zeros)
                     tile_load(at, &maps.x, bar, 0, (xr * p.col_tiles + i) * 128);
                     tile_load(at + kTileCodes, &maps.w, bar, 0, (wr * p.col_tiles + i) * 128);
-                    const uint32_t sf = at + 2 * kTileCodes;
-                    tile_load(sf, &maps.x_scales, bar, 0, (xr * p.groups + (i >> 2)) * 4);
-                    tile_load(sf + kMx8Scales, &maps.w_scales, bar, 0, (ft * 2 * p.groups + (i >> 2)) * 4);
-                    tile_load(sf + 2 * kMx8Scales, &maps.w_scales, bar, 0, ((ft * 2 + 1) * p.groups + (i >> 2)) * 4);
+                    if (scales) {
+                        const uint32_t sf = at + 2 * kTileCodes;
+                        tile_load(sf, &maps.x_scales, bar, 0, (xr * p.groups + (i >> 2)) * 4);
+                        tile_load(sf + kMx8Scales, &maps.w_scales, bar, 0, (ft * 2 * p.groups + (i >> 2)) * 4);
+                        tile_load(sf + 2 * kMx8Scales, &maps.w_scales, bar, 0, ((ft * 2 + 1) * p.groups + (i >> 2)) * 4);
+                    }
                 }
                 ++issued;
                 if (++slot == kPairStages) { slot = 0; phase ^= 1; }
@@ -323,7 +327,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx8_pair_kernel(const __grid_
     } else if (warp == 1 && rank == 0) {
         const bool leader = elect_one();
         int slot = 0, done_tiles = 0;
-        uint32_t phase = 0;
+        uint32_t phase = 0, group = kPairStages - 1;                     // the scales' place in tensor memory: one of as many as there are stages,
+                                                                         // so that the MMAs that used it last are done when it is written again
         const uint32_t idesc = (uint32_t(256 >> 3) << 17) | (1u << 23) | (uint32_t(256 >> 4) << 24), next_byte = (1u << 4) | (1u << 29);
         const uint64_t da0 = smem_desc_sw128(smem), db0 = smem_desc_sw128(smem + kTileCodes), s0 = scale_desc(smem + 2 * kTileCodes);
         const uint32_t own_empty = in_cta(empty, 0), peer_empty = in_cta(empty, 1), own_done = in_cta(done, 0), peer_done = in_cta(done, 1);
@@ -338,12 +343,15 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx8_pair_kernel(const __grid_
                 if (!warp_wait(full + 8 * slot, phase, ctx, 134)) { ok = false; break; }
                 tc_fence_after();
                 const uint64_t shift = static_cast<uint64_t>(slot) * (kPairStage >> 4);
-                const uint32_t sfa = tmem + 256 + slot * 12, sfb = sfa + 4;
+                if ((i & 3) == 0) group = group == kPairStages - 1 ? 0 : group + 1;
+                const uint32_t sfa = tmem + 256 + group * 12, sfb = sfa + 4;
                 const uint32_t which = idesc + (i & 3) * next_byte;
                 if (leader) {
-                    copy_scales_pair(sfa, s0 + shift);
-                    copy_scales_pair(sfb, s0 + shift + (kMx8Scales >> 4));
-                    copy_scales_pair(sfb + 4, s0 + shift + 2 * (kMx8Scales >> 4));
+                    if ((i & 3) == 0) {
+                        copy_scales_pair(sfa, s0 + shift);
+                        copy_scales_pair(sfb, s0 + shift + (kMx8Scales >> 4));
+                        copy_scales_pair(sfb + 4, s0 + shift + 2 * (kMx8Scales >> 4));
+                    }
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         if (k < steps) umma_mx8_pair(tmem, da0 + shift + 2 * k, db0 + shift + 2 * k, which, sfa, sfb, accumulate | k);
