@@ -50,6 +50,7 @@ struct Mx8Params {
     int tile_n;                             // rows of the N operand in a tile
     int splits, tiles_per_split;            // cluster split of the column tiles
     int stages;
+    int band;                               // pairs of CTAs: tiles of rows of w to a band
     int tensor_columns;                     // of tensor memory that a CTA allocates
     uint32_t spin_limit;                    // polls of a bounded wait (0 = the default)
     int test_skip_load;                     // test hook: every CTA leaves out the copies of this (1-based) column tile of its walk (0 = off)

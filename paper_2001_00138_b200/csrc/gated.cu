@@ -39,6 +39,7 @@ struct Product {
     int box_rows;                                      // rows of A that a CTA copies: fewer than 128 where a K-major product has fewer
     int units;                                         // tiles times splits
     int slot;                                          // of its first unit among the partial sums
+    int band;                                          // tiles of rows to a band
 };
 // Pair q of P takes the units q, q + P, ... of the first product, then of the second those from more[q] to more[q + 1], which even the pairs out, and
 // the units more[P] + q, more[P] + q + P, ..., `common` of them: what runs at a time lies together, as the bands of tiles want it.
@@ -169,7 +170,7 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
             const Product &q = p.of[which];
             const int tile = u / q.splits, k0 = (u - tile * q.splits) * q.per_split, k1 = min(q.k_blocks, k0 + q.per_split);
             int mt, nt;
-            banded(tile, q.m_tiles, q.n_tiles, mt, nt);
+            banded(tile, q.band, q.m_tiles, q.n_tiles, mt, nt);
             // K-major rows that do not exist are not copied where they are all of a CTA's, or where the product has fewer rows than a tile: the MMAs read
             // whatever is there and give rows that nobody stores.  (Filling 127 of 128 rows with zeros took the copies twice the time of 128 rows.)
             const bool one = !(GRAD && which) && q.rows <= 128, has_rows = !one || rank == 0;
@@ -259,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
             const Product &q = p.of[which];
             const int tile = u / q.splits, buf = t & 1;
             int mt, nt;
-            banded(tile, q.m_tiles, q.n_tiles, mt, nt);
+            banded(tile, q.band, q.m_tiles, q.n_tiles, mt, nt);
             T *out = static_cast<T *>(q.out0);
             if (GRAD && which == 1 && mt >= q.f_blocks) {
                 mt -= q.f_blocks;
@@ -338,7 +339,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) gated_join_kernel(const __gri
     const int piece = block % kPieces, e = block / kPieces % kEpilogueWarps, rank = block / (kEpilogueWarps * kPieces) & 1;
     const int tile = block / (2 * kEpilogueWarps * kPieces), quadrant = e & 3, quarter = e >> 2;
     int mt, nt;
-    banded(tile, q.m_tiles, q.n_tiles, mt, nt);
+    banded(tile, q.band, q.m_tiles, q.n_tiles, mt, nt);
     T *out = static_cast<T *>(q.out0);
     if (second && mt >= q.f_blocks) {
         mt -= q.f_blocks;
@@ -667,6 +668,7 @@ static Product product_of(const GatedPlan &plan, int slot) {
     q.units = static_cast<int>(units_of(plan));
     q.box_rows = 128;
     q.slot = slot;
+    q.band = band_of(plan.m_tiles, plan.n_tiles, static_cast<int64_t>(256) * 64 * 2 * plan.k_blocks);
     return q;
 }
 

@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx8_pair_kernel(const __grid_
         pdl_wait();
         for (int t = first; ok && t < tiles; t += step) {
             int ft, nt;
-            banded(t, p.f_tiles, p.n_tiles, ft, nt);
+            banded(t, p.band, p.f_tiles, p.n_tiles, ft, nt);
             const int xr = nt * 2 + static_cast<int>(rank), wr = ft * 2 + static_cast<int>(rank);      // row tiles of 128
             for (int i = 0; i < p.col_tiles; ++i) {
                 if (issued >= kPairStages && !warp_wait(empty + 8 * slot, phase, ctx, 131)) { ok = false; break; }
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx8_pair_kernel(const __grid_
                     const uint32_t at = smem + slot * kPairStage, bar = full0 + 8 * slot;
                     const bool scales = (i & 3) == 0;                    // of this column tile and the next three
                     if (rank == 0) mbar_expect_tx(full + 8 * slot, 2 * (2 * kTileCodes + (scales ? 3 * kMx8Scales : 0)));
-                    // (row tiles that do not exist are outside the maps: zeros)
+                    // (row tiles that do not exist are outside the maps: zeros; what fits the GPU has fewer than 2^31 rows of 128 bytes)
                     tile_load(at, &maps.x, bar, 0, (xr * p.col_tiles + i) * 128);
                     tile_load(at + kTileCodes, &maps.w, bar, 0, (wr * p.col_tiles + i) * 128);
                     if (scales) {
@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx8_pair_kernel(const __grid_
         uint32_t phase = 0;
         for (int t = first; t < tiles; t += step) {
             int ft, nt;
-            banded(t, p.f_tiles, p.n_tiles, ft, nt);
+            banded(t, p.band, p.f_tiles, p.n_tiles, ft, nt);
             const int f0 = ft * 256 + quarter * 64;
             const int64_t row0 = static_cast<int64_t>(nt) * 256 + rank * 128 + quadrant * 32;
             __syncwarp();
@@ -478,6 +478,7 @@ Mx8Launch plan_mx8_linear(Mx8Params &p) {
         p.tile_n = 256;
         p.f_tiles = static_cast<int>(ceil_div(p.F, 256));
         p.n_tiles = static_cast<int>(ceil_div(p.rows, 256));
+        p.band = band_of(p.f_tiles, p.n_tiles, static_cast<int64_t>(256) * 128 * p.col_tiles);
         p.splits = 1;
         p.stages = kPairStages;
         l.piece = kPiece;

@@ -109,8 +109,8 @@ def test_whole_numbers(M, K, F, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
-@pytest.mark.parametrize("slack, wslack, hslack", [(8, 0, 0), (0, 8, 8), (3, 0, 1), (0, 3, 0), (1, 1, 2), (2, 5, 3)])
-@pytest.mark.parametrize("M, K, F", [(5, 200, 72), (300, 136, 333), (40, 65, 64)])
+@pytest.mark.parametrize("slack, wslack, hslack", [(8, 0, 0), (0, 8, 8), (3, 0, 1), (0, 3, 0), (1, 1, 2), (2, 5, 3), (4, 4, 4), (7, 7, 7)])
+@pytest.mark.parametrize("M, K, F", [(5, 200, 72), (300, 136, 333), (40, 65, 64), (290, 100, 60)])
 def test_strides(M, K, F, dtype, slack, wslack, hslack):
     exact_case(M, K, F, dtype, "relu", slack=slack, wslack=wslack, hslack=hslack)
 
