@@ -17,6 +17,7 @@ namespace patdnn {
 namespace {
 
 constexpr int kMostWarps = 16;
+constexpr int kGradSmem = 226 * 1024;                  // dynamic shared memory of a CTA of the gradient, at most
 
 struct RmsArgs {
     const void *x, *residual, *dsum;
@@ -411,6 +412,9 @@ RmsPlan plan_backward(int C, int64_t rows, int dtype) {
     const bool few = rows <= 2 * sm_count();           // a row or two per CTA: nothing to copy ahead
     const bool eight = C <= 256 || (C <= kMostWarps * 256 && (few || narrow(C) || dtype == PATDNN_F32)) || (dtype == PATDNN_F32 && C <= 8 * kMostWarps * 256);
     RmsPlan p = plan_of(C, rows, eight ? 8 : 16, few ? 8 : grad_warps(eight ? 8 : 16), 1);
+    // Two rows of twelve warps, fp32: their copies and gamma do not fit (5000 x 2900: 16 columns to a lane 43 us, one row at a time 53).
+    if (!few && eight && dtype == PATDNN_F32 && p.threads * RmsCopies<float, 4, 8, true>::kThreadBytes + p.warps * 256 * 4 > kGradSmem)
+        p = plan_of(C, rows, 16, grad_warps(16), 1);
     p.async = !few;
     return p;
 }
@@ -452,7 +456,7 @@ cudaError_t prepare_rms() {
                 p.L = k == 0 ? 8 : k == 1 ? 16 : 32;
                 const cudaError_t e = by_strip(dtype, width, [&](auto t, auto v) {
                     return by_columns(p, [&](auto n, auto l) {
-                        const cudaError_t r = cudaFuncSetAttribute(rms_grad_kernel<decltype(t), v.value, n.value, l.value, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);
+                        const cudaError_t r = cudaFuncSetAttribute(rms_grad_kernel<decltype(t), v.value, n.value, l.value, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGradSmem);
                         return r == cudaSuccess ? cudaFuncSetAttribute(rms_grad_kernel<decltype(t), v.value, n.value, l.value, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 100 * 1024) : r;
                     });
                 });

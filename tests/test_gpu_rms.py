@@ -321,3 +321,23 @@ def test_rows_whose_squares_leave_the_range_of_fp32(C):
         check(rstd[:, None], rs, (adds(C) + 8) / 2 * R.EPS24 * rs * 1.01, "rstd")
         want = x.double() * rs * gamma.double()
         check(y, want, ((adds(C) + 8) / 2 + 4) * 1.01 * R.EPS24 * want.abs() + R.TINY["f32"], "y")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_gradient_of_rows_of_every_length(dtype):
+    """Every number of warps to a row, for rows one by one and for many; against the formula, with the bounds of test_gradient."""
+    import torch
+    from paper_2001_00138_b200 import binding as B
+    for M in (60, 700):
+        for C in [256 * w - 116 for w in range(1, 17)] + [512 * w - 31 for w in range(9, 17)] + [33000]:
+            tt, dt, (_, s), (_, dy), gamma = case(M, C, dtype, 0, M + C)
+            ds = torch.ones(M, C, device="cuda", dtype=tt)
+            rstd = ((s.double() ** 2).mean(1) + EPS).rsqrt().float()
+            dx, dgamma = torch.empty_like(s), torch.empty(C, device="cuda")
+            B.RmsNorm(C, dtype=dt, eps=EPS).grad(s, gamma, rstd, dy, dx, dgamma, M, dsum=ds, stream=stream())
+            torch.cuda.synchronize()
+            want, xh, u, m = gradient_reference(s, gamma, rstd, dy, ds)
+            rs = rstd.double()[:, None]
+            size = rs * (u.abs() * 3 + xh.abs() * (m.abs() * 4 + (u * xh).abs().mean(1, keepdim=True) * (adds(C) + 4))) + want.abs() * 2
+            check(dx, want, 1.01 * R.EPS24 * size + R.UNIT[dtype] * 1.01 * want.abs() + R.TINY[dtype], f"dx {M} x {C}")
+            check(dgamma, (dy.double() * xh).sum(0), (M / 18 + 80) * R.EPS24 * (dy.double() * xh).abs().sum(0), f"dgamma {M} x {C}")
