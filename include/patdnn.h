@@ -460,10 +460,11 @@ PATDNN_API int patdnn_linear8_free(patdnn_linear8 h);
  *   dg = dh * u * act'(g), du = dh * act(g);  dx = dg wg + du wu, dwg = dg^T x, dwu = du^T x
  * Sums are fp32 on the tensor cores, in a fixed order; g and u stay in fp32 for h, which is rounded once.  For the gradient the run stores
  * g and u rounded to the tensors' type (gu), and dg and du are rounded to it as operands of the products; dx, dwg and dwu are rounded once
- * more.  At g = 0 ReLU passes no gradient.  A row of x that is not finite spoils its row of h alone.
+ * more.  At g = 0 ReLU passes no gradient.  A row of x that is not finite spoils its row of h alone.  Where g or u leaves the range of the
+ * type, gu holds an infinity; SiLU has its limits there (0 and slope 0 at -infinity, slope 1 at infinity).
  *   desc       copied; rows of consecutive elements; strides in elements, 0 = dense: x_row of x and dx, w_row of the four weight tensors,
  *              h_row of h and dh; gu is dense, [rows][2][F], g before u.  grad != 0: gradients will be asked for (more workspace)
- *   patdnn_gated_run       gu DEVICE or NULL
+ *   patdnn_gated_run       gu DEVICE or NULL; hidden and gu overlap no input
  *   patdnn_gated_grad      dx DEVICE or NULL, dwg and dwu DEVICE or both NULL: what is asked for is overwritten; none may overlap an input
  *   patdnn_gated_check     waits for the device; E_DEVICE_TIMEOUT if a bounded device-side wait of this handle expired
  *   patdnn_gated_debug_wait  as patdnn_linear_debug_wait; the iteration is the block of 64 in a CTA's own walk

@@ -61,9 +61,9 @@ __device__ __forceinline__ void slopes(const AuxJob &a, int64_t row, int c0) {
             act = fg[e] < 0.f ? 0.f : fg[e];
             slope = fg[e] > 0.f ? 1.f : fg[e] <= 0.f ? 0.f : fg[e];
         } else if constexpr (ACT == PATDNN_ACT_SILU) {
-            const float s = sigmoid(fg[e]);
-            act = fg[e] * s;
-            slope = fmaf(act, 1.f - s, s);
+            const float s = sigmoid(fg[e]);            // at infinities (g left the range of the type) the limits: 0 and 0, or g and 1
+            act = s == 0.f ? 0.f : fg[e] * s;
+            slope = s == 1.f ? 1.f : fmaf(act, 1.f - s, s);
         }
         fg[e] = fd[e] * fu[e] * slope;
         fu[e] = fd[e] * act;

@@ -353,3 +353,38 @@ def test_refusals_of_calls():
     odd = B.Gated(16, 24, max_rows=4, dtype=B.F16, x_row=25, w_row=27)     # such rows are packed, wherever they lie
     odd.run(p + 2, p + 4, p + 6, torch.zeros(4, 16, dtype=torch.float16, device="cuda"), 1, stream=stream())
     odd.check()
+
+
+@pytest.mark.parametrize("name", ["relu", "silu"])
+def test_gradient_where_the_gate_leaves_the_range_of_the_type(name):
+    """g of +-2^17 is an infinity in half; the activation has its limits there: no gradient below, slope 1 above.  Exact values all the way."""
+    import torch
+    from paper_2001_00138_b200 import binding as B
+    M, K, F = 40, 16, 72
+    b = B.Gated(F, K, max_rows=M, dtype=B.F16, act=act_of(name), grad=True)
+    x, dh = torch.zeros(M, K, device="cuda", dtype=torch.half), torch.zeros(M, F, device="cuda", dtype=torch.half)
+    wg, wu = torch.zeros(F, K, device="cuda", dtype=torch.half), torch.zeros(F, K, device="cuda", dtype=torch.half)
+    x[:, 0], x[:, 1] = 256.0, 1.0
+    wg[0::2, 0], wg[1::2, 0] = 512.0, -512.0
+    wu[:, 1] = 2.0 ** -8
+    gu, h = torch.empty(M, 2, F, device="cuda", dtype=torch.half), torch.empty(M, F, device="cuda", dtype=torch.half)
+    b.run(x, wg, wu, h, M, gu=gu, stream=stream())
+    dh[:, 1::2] = 1.0                                      # below: nothing flows
+    dh[:, 0::2] = 0.0
+    dx, dwg, dwu = torch.empty_like(x), torch.empty_like(wg), torch.empty_like(wu)
+    dh_below = dh.clone()
+    torch.cuda.synchronize()
+    assert torch.isinf(gu[:, 0]).all()
+    assert torch.equal(h[:, 0::2], torch.full_like(h[:, 0::2], 512.0)) and not h[:, 1::2].any()
+    g = gu.clone()
+    g[:, 0, 0::2] = 1.0                                    # (the ones above apart: 0 * infinity has no value)
+    b.grad(x, wg, wu, g, dh_below, dx, dwg, dwu, M, stream=stream())
+    torch.cuda.synchronize()
+    assert not dx.any() and not dwg.any() and not dwu.any()
+    dh[:, 1::2] = 0.0
+    dh[:, 0::2] = 1.0                                      # above: dg = dh u, du = dh g
+    b.grad(x, wg, wu, gu, dh, dx, dwg, dwu, M, stream=stream())
+    torch.cuda.synchronize()
+    assert torch.equal(dwg[0::2, 1], torch.full_like(dwg[0::2, 1], M * 2.0 ** -8)) and torch.equal(dwg[0::2, 0], torch.full_like(dwg[0::2, 0], M * 1.0))
+    assert torch.isinf(dwu[0::2, :2]).all() and not dwg[1::2].any()
+    assert b.check() is None
