@@ -72,3 +72,48 @@ def test_the_chain_in_one_captured_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(z, want[0]) and torch.equal(carried, want[1])
+
+
+def test_calls_on_two_streams_at_once():
+    """A handle each: gradients of the block and of the norm on one stream, the block and 8-bit products on another, in turn and together."""
+    import torch
+    from paper_2001_00138_b200 import binding as pat
+    g = torch.Generator(device="cuda").manual_seed(5)
+
+    def normal(*shape, scale=1.0):
+        return (torch.randn(*shape, generator=g, device="cuda") * scale).bfloat16()
+
+    sides = []
+    for rows, width, hidden in ((700, 512, 1100), (40, 1000, 2048)):
+        x, dh, carried = normal(rows, width), normal(rows, hidden), normal(rows, width)
+        wg, wu, down = normal(hidden, width, scale=width ** -0.5), normal(hidden, width, scale=width ** -0.5), normal(width, hidden, scale=hidden ** -0.5)
+        gamma, rstd = torch.rand(width, generator=g, device="cuda"), torch.ones(rows, device="cuda")
+        out = dict(gu=normal(rows, 2, hidden), h=dh.clone(), dx=x.clone(), dwg=wg.clone(), dwu=wu.clone(), o=x.clone(), dn=x.clone(), dgamma=gamma.clone())
+        norm, block = pat.RmsNorm(width, dtype=pat.BF16), pat.Gated(hidden, width, max_rows=rows, dtype=pat.BF16, grad=True)
+        back = pat.Linear8(down, width, hidden, max_rows=rows, dtype=pat.BF16, stream=torch.cuda.current_stream().cuda_stream)
+
+        def side(st, rows=rows, x=x, dh=dh, carried=carried, wg=wg, wu=wu, gamma=gamma, rstd=rstd, o=out, norm=norm, block=block, back=back):
+            block.run(x, wg, wu, o["h"], rows, gu=o["gu"], stream=st)
+            back.run(o["h"], o["o"], rows, stream=st)
+            block.grad(x, wg, wu, o["gu"], dh, o["dx"], o["dwg"], o["dwu"], rows, stream=st)
+            norm.grad(carried, gamma, rstd, o["dx"], o["dn"], o["dgamma"], rows, dsum=o["o"], stream=st)
+
+        sides.append((side, out, (block, back)))
+    wants = []
+    for side, out, _ in sides:
+        side(torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        wants.append({k: v.clone() for k, v in out.items()})
+        for v in out.values():
+            v.zero_()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for st, (side, _, _) in zip(streams, sides):
+            side(st.cuda_stream)
+    torch.cuda.synchronize()
+    for (_, out, handles), want in zip(sides, wants):
+        for h in handles:
+            h.check()
+        for k, v in want.items():
+            assert torch.isfinite(v).all() and torch.equal(out[k], v), k
