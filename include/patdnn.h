@@ -443,7 +443,8 @@ PATDNN_API int patdnn_mx8_dequantize(const void *mx, int32_t dtype, int64_t rows
 /*
  * Linear layers with 8-bit weights (addition): y[m][f] = act(bias[f] + sum_k q(x)[m][k] * q(w)[f][k]), q as above, sums fp32 on the
  * block-scaled tensor cores, y rounded once.  Calls, arguments and errors are those of patdnn_linear_* with patdnn_mx8_* rows
- * (patdnn_mx8_quantize, patdnn_rms_run_mx8) in place of 4-bit ones.
+ * (patdnn_mx8_quantize, patdnn_rms_run_mx8) in place of 4-bit ones.  In patdnn_linear_plan_info a column tile is 128 inputs, and the
+ * persistent kernel's tiles are worked on by pairs of CTAs.
  */
 typedef struct patdnn_linear8_s *patdnn_linear8;
 PATDNN_API int patdnn_linear8_encode(const void *weights, int64_t ldw, const patdnn_linear_desc *desc, void *stream, patdnn_linear8 *out);
