@@ -473,7 +473,7 @@ PATDNN_API int patdnn_linear8_free(patdnn_linear8 h);
  * above 2^31, a tensor that is not aligned to its elements, or x, wg or wu with rows that are whole 16-byte units apart and not aligned to 16
  * bytes), E_DTYPE (F16 and BF16 only), E_SCRATCH (a gradient without desc.grad), E_ALLOC, E_CUDA, E_NO_DEVICE (another device is current).
  * A handle owns its workspace (39 MB, and what max_rows needs for gradients and for rows that are not whole 16-byte units apart, which are
- * packed first): calls that can overlap need a handle each, others may share one, whatever their weights.  rows = 0 launches nothing (the
+ * packed or copied first): calls that can overlap need a handle each, others may share one, whatever their weights.  rows = 0 launches nothing (the
  * gradient writes zeros to dwg and dwu).  patdnn_gated_create waits for the device; the calls are asynchronous on `stream`.
  */
 typedef struct patdnn_gated_s *patdnn_gated;

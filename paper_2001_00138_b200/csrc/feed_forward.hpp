@@ -100,6 +100,12 @@ struct GatedPlan {
     int tile_n;
 };
 GatedPlan plan_gated_forward(int F, int K, int64_t rows);
+// Few rows, weights whose rows are not whole 16-byte units apart, read as they lie (see gated_rows_kernel): every `phases`-th row begins at the same place
+// of a unit.
+constexpr int kMostPhases = 8, kPhasedRows = 128;
+inline int gated_phases(int64_t w_row) { return w_row % 8 == 0 ? 1 : w_row % 4 == 0 ? 2 : w_row % 2 == 0 ? 4 : 8; }
+inline int gated_phased_row(int K) { return (K + kMostPhases - 1 + 7) / 8 * 8; }       // of a shifted copy of x
+GatedPlan plan_gated_phased(int F, int K, int64_t rows, int phases);
 // [0] dx, [1] dwg and dwu; one launch, whose grid both have
 void plan_gated_gradient(int F, int K, int64_t rows, bool dx, bool dw, GatedPlan (&plan)[2]);
 constexpr int kGatedUnitFloats = 256 * 256; // partial sums of a (tile, split) unit
@@ -116,6 +122,7 @@ struct GatedCall {
     void *h, *gu;                           // forward; gu may be nullptr
     void *dx, *dwg, *dwu;
     int64_t rows;
+    int phases;                             // 0, or forward: wg and wu as the caller's, x a copy per phase, shifted as its rows of the weights are
     uint32_t spin_limit;
     int test_skip_load;
 };
@@ -125,11 +132,17 @@ cudaError_t launch_gated_forward(const GatedShape &s, const GatedCall &c, const 
 cudaError_t launch_gated_gradient(const GatedShape &s, const GatedCall &c, const GatedWork &w, cudaStream_t st, int *launches);   // from dgu
 // In front of them, one launch: K columns of 16-bit rows to rows `to_row` apart, zeros behind them (rows = 0: nothing to pack), and, where dgu is not
 // nullptr, dgu from gu [rows][2 F] and dh
+// copies > 0: as many copies of all rows, copy i shifted by shift[i] columns, zeros in front
 struct GatedPack {
     const void *from;
     void *to;
     int64_t rows, row, to_row;
+    int copies;
+    uint8_t shift[kMostPhases];
 };
+inline int gated_shift(const void *base, int64_t w_row, int phase) {                   // elements between a row and the 16-byte unit in which it begins
+    return static_cast<int>((reinterpret_cast<uintptr_t>(base) + static_cast<uintptr_t>(phase) * w_row * 2) % 16 / 2);
+}
 cudaError_t launch_gated_operands(const GatedShape &s, const GatedPack (&packs)[3], const void *gu, const void *dh, void *dgu, int64_t rows, cudaStream_t st);
 
 }  // namespace patdnn

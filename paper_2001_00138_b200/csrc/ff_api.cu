@@ -47,6 +47,7 @@ struct patdnn_gated_s {
     int64_t max_rows = 0;
     int device = -1;
     void *x = nullptr, *weights = nullptr;  // packed rows, where theirs cannot be copied as they lie
+    void *shifted = nullptr;                // copies of few rows of x, beside `weights`
     uint32_t spin_limit = 0;                // patdnn_gated_debug_wait
     int test_skip_load = 0;
     ~patdnn_gated_s() {
@@ -55,6 +56,7 @@ struct patdnn_gated_s {
         cudaFree(w.status);
         cudaFree(x);
         cudaFree(weights);
+        cudaFree(shifted);
     }
 };
 
@@ -144,15 +146,26 @@ int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu
     c.spin_limit = h->spin_limit; c.test_skip_load = h->test_skip_load;
     const int64_t row = packed_row(s.K);
     GatedPack packs[3] = {};
+    // Few rows: a copy of x per phase instead of packed weights, as long as those are fewer rows (8 x 6899 -> 4222: 26 us, 80 packed; 128 x 1001 -> 1001:
+    // 9.9 and 10.2; 128 x 6899 -> 700: 25.5 and 20.2)
+    const int phases = gated_phases(s.w_row);
+    if (h->shifted && !gu && rows <= kPhasedRows && phases <= s.F && s.K + kMostPhases <= phases * s.w_row && phases * rows <= s.F && gated_shift(wg, s.w_row, 0) == gated_shift(wu, s.w_row, 0)) {
+        packs[0] = {x, h->shifted, rows, s.x_row, gated_phased_row(s.K), phases, {}};
+        for (int j = 0; j < phases; ++j) packs[0].shift[j] = static_cast<uint8_t>(gated_shift(wg, s.w_row, j));
+        c.x = h->shifted;
+        c.x_row = gated_phased_row(s.K);
+        c.phases = phases;
+        return launched(launch_gated_operands(s, packs, nullptr, nullptr, nullptr, rows, st), 1, "gated block operands launch");
+    }
     if (h->x) {
-        packs[0] = {x, h->x, rows, s.x_row, row};
+        packs[0] = {x, h->x, rows, s.x_row, row, 0, {}};
         c.x = h->x;
         c.x_row = row;
     }
     if (h->weights) {
         void *second = static_cast<uint16_t *>(h->weights) + s.F * row;
-        packs[1] = {wg, h->weights, s.F, s.w_row, row};
-        packs[2] = {wu, second, s.F, s.w_row, row};
+        packs[1] = {wg, h->weights, s.F, s.w_row, row, 0, {}};
+        packs[2] = {wu, second, s.F, s.w_row, row, 0, {}};
         c.wg = h->weights;
         c.wu = second;
         c.w_row = row;
@@ -366,7 +379,7 @@ int patdnn_gated_create(const patdnn_gated_desc *desc, patdnn_gated *out) {
     h->s = s;
     h->max_rows = desc->max_rows;
     const size_t row = static_cast<size_t>(packed_row(s.K));
-    uint16_t *dgu = nullptr, *x = nullptr, *weights = nullptr;
+    uint16_t *dgu = nullptr, *x = nullptr, *weights = nullptr, *shifted = nullptr;
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = allocate(&h->w.partial, static_cast<size_t>(pairs_most()) * kGatedUnits * kGatedUnitFloats);
     if (e == cudaSuccess) e = allocate(&h->w.status, 4);
@@ -377,6 +390,9 @@ int patdnn_gated_create(const patdnn_gated_desc *desc, patdnn_gated *out) {
     h->x = x;
     if (e == cudaSuccess && !copies_as_it_lies(s.w_row)) e = allocate(&weights, 2 * static_cast<size_t>(s.F) * row);
     h->weights = weights;
+    if (e == cudaSuccess && weights)
+        e = allocate(&shifted, static_cast<size_t>(std::min<int64_t>(kPhasedRows, desc->max_rows)) * gated_phases(s.w_row) * gated_phased_row(s.K));
+    h->shifted = shifted;
     if (e == cudaSuccess) e = prepare_gated();
     if (e == cudaSuccess) e = cudaDeviceSynchronize();                  // the status word is zero on every stream from here on
     if (e != cudaSuccess) return failed(h, e, "patdnn_gated_create");

@@ -399,6 +399,10 @@ __global__ void __launch_bounds__(kJoinWarps * 32) gated_join_kernel(const __gri
 // The weights are the M operand, 64 rows of wg and the same 64 of wu in a tile, the rows of x the N operand (16 to 128 of them): a CTA per 64 outputs,
 // 128 rows and range of the summed dimension, whose weights it streams.  The CTAs of a cluster share a tile; their partial sums are pushed into the shared
 // memory of the one that finishes a row of x, where g and u of an output meet.
+// PHASED: rows of the weights are not whole 16-byte units apart, which tensor maps cannot describe; but of 2, 4 or 8 rows every first, every second and so on are.
+// A tile takes 64 rows of one such phase, from the 16-byte unit in which each begins: all of them are `shift` columns further right than they should be,
+// and so is the copy of x that the phase is multiplied with.  What lies in front of the rows is zeroed where it has arrived.  (8 x 6899 -> 4222: 26 us;
+// packing the weights in front 80; rows that are whole units apart 22.)
 constexpr int kRowsThreads = 256;
 constexpr int kMostRowsStages = 12;
 
@@ -406,6 +410,8 @@ struct GatedRowsParams {
     void *h, *gu;
     int64_t ldh, rows;
     int F, n_tiles, k_blocks, per_split, splits, stages, tile_n, box_rows, tensor_columns;
+    int phases, weight_rows;                           // weight_rows: of the weights' boxes
+    uint8_t shift[kMostPhases];
     int *status;
     uint32_t spin_limit;
     int test_skip_load;
@@ -416,14 +422,19 @@ __device__ __forceinline__ void tile_load_own(uint32_t dst, const CUtensorMap *m
                  ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
 }
 
-template <typename T, int ACT>
+template <bool PHASED> struct GatedRowsMaps {
+    CUtensorMap x, g[PHASED ? kMostPhases : 1], u[PHASED ? kMostPhases : 1];
+};
+
+template <typename T, int ACT, bool PHASED>
 __global__ void __launch_bounds__(kRowsThreads, 1)
-gated_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_u, const GatedRowsParams p) {
+gated_rows_kernel(const __grid_constant__ GatedRowsMaps<PHASED> maps, const __grid_constant__ GatedRowsParams p) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long bars[2 * kMostRowsStages + 1];
     __shared__ uint32_t tmem_slot;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const int rank = blockIdx.x % p.splits, tile = blockIdx.x / p.splits, mt = tile / p.n_tiles, f0 = (tile - mt * p.n_tiles) * 64;
+    const int rank = blockIdx.x % p.splits, tile = blockIdx.x / p.splits, mt = tile / p.n_tiles, ft = tile - mt * p.n_tiles;
+    const int phase_of = PHASED ? ft % p.phases : 0, f0 = (PHASED ? ft / p.phases : ft) * 64;   // row f0 of the phase's
     const int64_t row0 = static_cast<int64_t>(mt) * 128;
     const int rows = static_cast<int>(min(static_cast<int64_t>(128), p.rows - row0));
     const WaitCtx ctx{p.status, p.spin_limit ? p.spin_limit : kSpinLimit};
@@ -456,10 +467,11 @@ gated_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
             if (issued >= p.stages && !warp_wait(empty + 8 * slot, phase, ctx, 141)) break;
             if (leader && issued + 1 != p.test_skip_load) {
                 const uint32_t at = smem + slot * stage_bytes, bar = full + 8 * slot;
-                mbar_expect_tx(bar, kHalf + p.box_rows * 128);         // (rows behind the box are whatever is there: their sums are not read)
-                tile_load_own(at, &map_g, bar, k * 64, f0);
-                tile_load_own(at + kHalf / 2, &map_u, bar, k * 64, f0);
-                tile_load_own(at + kHalf, &map_x, bar, k * 64, static_cast<int>(row0));
+                // (rows behind the boxes are whatever is there: their sums are not read)
+                mbar_expect_tx(bar, (2 * (PHASED ? p.weight_rows : 64) + p.box_rows) * 128);
+                tile_load_own(at, &maps.g[phase_of], bar, k * 64, f0);
+                tile_load_own(at + kHalf / 2, &maps.u[phase_of], bar, k * 64, f0);
+                tile_load_own(at + kHalf, &maps.x, bar, k * 64, static_cast<int>(row0 + (PHASED ? phase_of * p.rows : 0)));
             }
             ++issued;
             if (++slot == p.stages) { slot = 0; phase ^= 1; }
@@ -474,6 +486,13 @@ gated_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         uint32_t phase = 0, accumulate = 0;
         for (int k = k0; k < k1; ++k) {
             if (!warp_wait(full + 8 * slot, phase, ctx, 143)) break;
+            if (PHASED && k == 0 && p.shift[phase_of]) {               // what lies in front of the 128 rows: whatever it is, it is no part of the sums
+                unsigned char *at = smem_raw + (smem - smem_u32(smem_raw)) + slot * stage_bytes;
+                for (int r = lane; r < 128; r += 32)
+                    for (int e = 0; e < p.shift[phase_of]; ++e) *reinterpret_cast<uint16_t *>(at + r * 128 + ((r & 7) << 4) + 2 * e) = 0;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            }
             tc_fence_after();
             if (leader) {
                 const uint64_t shift = static_cast<uint64_t>(slot) * (stage_bytes >> 4);
@@ -504,8 +523,8 @@ gated_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
                 asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cta(slots + ((c + j) >> shift) * 512, j & (p.splits - 1))), "r"(k1 > k0 ? v[j] : 0u) : "memory");
     }
     pair_barrier();
-    const int f = threadIdx.x & 63;
-    if (ok && f0 + f < p.F) {
+    const int f = threadIdx.x & 63, column = PHASED ? (f0 + f) * p.phases + phase_of : f0 + f;
+    if (ok && column < p.F) {
         const float *from = reinterpret_cast<const float *>(smem_raw + (smem - smem_u32(smem_raw))) + f;
         const int mine = (rows - rank + p.splits - 1) >> shift;
 #pragma unroll 2
@@ -519,11 +538,11 @@ gated_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
                 }
             const int64_t row = row0 + (j << shift) + rank;
             if (p.gu) {
-                T *gu = static_cast<T *>(p.gu) + row * 2 * p.F + f0 + f;
+                T *gu = static_cast<T *>(p.gu) + row * 2 * p.F + column;
                 gu[0] = from_float<T>(g);
                 gu[p.F] = from_float<T>(up);
             }
-            static_cast<T *>(p.h)[row * p.ldh + f0 + f] = from_float<T>(activate1<ACT>(g) * up);
+            static_cast<T *>(p.h)[row * p.ldh + column] = from_float<T>(activate1<ACT>(g) * up);
         }
     }
     tc_fence_before();
@@ -546,8 +565,10 @@ template <typename F> cudaError_t by_kernel(bool grad, int dtype, int act, F f) 
     };
     return dtype == PATDNN_F16 ? go(__half{}) : go(__nv_bfloat16{});
 }
-template <typename F> cudaError_t by_rows_kernel(int dtype, int act, F f) {
-    return by_act(act, [&](auto a) { return dtype == PATDNN_F16 ? f(gated_rows_kernel<__half, a.value>) : f(gated_rows_kernel<__nv_bfloat16, a.value>); });
+template <bool PHASED, typename F> cudaError_t by_rows_kernel(int dtype, int act, F f) {
+    return by_act(act, [&](auto a) {
+        return dtype == PATDNN_F16 ? f(gated_rows_kernel<__half, a.value, PHASED>) : f(gated_rows_kernel<__nv_bfloat16, a.value, PHASED>);
+    });
 }
 
 }  // namespace
@@ -565,6 +586,32 @@ static int64_t time_of(const GatedPlan &p) { return std::max<int64_t>(p.per_spli
 static int64_t units_of(const GatedPlan &p) { return static_cast<int64_t>(p.m_tiles) * p.n_tiles * p.splits; }
 constexpr int64_t kJoinBlocks = 20;                    // what partial sums cost, their stores and the join, in blocks of a tile (6 us, measured)
 
+static GatedPlan plan_few(int f_tiles, int k_blocks, int64_t rows) {
+    GatedPlan p{};
+    p.few = true;
+    p.k_blocks = k_blocks;
+    p.tile_n = rows < 128 ? static_cast<int>(ceil_div(rows, 16) * 16) : 128;
+    p.m_tiles = static_cast<int>(ceil_div(rows, 128));
+    p.n_tiles = f_tiles;
+    const int64_t ctas = static_cast<int64_t>(p.m_tiles) * f_tiles;
+    p.splits = 1;
+    while (p.splits < 8 && ctas * p.splits * 2 <= sm_count() && k_blocks >= p.splits * 8) p.splits *= 2;
+    p.per_split = static_cast<int>(ceil_div(k_blocks, p.splits));
+    p.grid = static_cast<int>(ctas * p.splits);
+    const int stage = kHalf + p.tile_n * 128;
+    // more CTAs than SMs: two to an SM
+    p.stages = std::max(1, std::min({kMostRowsStages, p.per_split, (p.grid > sm_count() ? 110 * 1024 : 200 * 1024) / stage}));
+    p.tensor_columns = allocation_of(p.tile_n);
+    const int owned = static_cast<int>(ceil_div(p.tile_n, p.splits));
+    // (shared memory in proportion to tensor memory, see plan_mx4_linear)
+    p.smem = std::max({p.stages * stage + 1024, p.splits * owned * 512 + 1024, kSmemPerSm / 512 * p.tensor_columns - 1024});
+    return p;
+}
+
+GatedPlan plan_gated_phased(int F, int K, int64_t rows, int phases) {
+    return plan_few(static_cast<int>(phases * ceil_div(ceil_div(F, phases), 64)), static_cast<int>(ceil_div(K + kMostPhases - 1, 64)), rows);
+}
+
 GatedPlan plan_gated_forward(int F, int K, int64_t rows) {
     GatedPlan p{};
     p.k_blocks = static_cast<int>(ceil_div(K, 64));
@@ -579,26 +626,8 @@ GatedPlan plan_gated_forward(int F, int K, int64_t rows) {
     }
     // Few rows: a block of its tile takes about as long as one of a pair's, which is four times as large.  Launch and fill take about six blocks' time
     // in each round, 14 once for the pairs; the exchange in a cluster four.
-    const int64_t f_tiles = ceil_div(F, 64), ctas = ceil_div(rows, 128) * f_tiles;
-    int64_t ranges = 1;
-    while (ranges < 8 && ctas * ranges * 2 <= sm_count() && p.k_blocks >= ranges * 8) ranges *= 2;
-    if (rows <= 128 || ceil_div(ctas * ranges, sm_count()) * (ceil_div(p.k_blocks, ranges) + 6) + (ranges > 1 ? 4 : 0) < shortest + 14) {
-        p.few = true;
-        p.tile_n = rows < 128 ? static_cast<int>(ceil_div(rows, 16) * 16) : 128;
-        p.m_tiles = static_cast<int>(ceil_div(rows, 128));
-        p.n_tiles = static_cast<int>(f_tiles);
-        p.splits = static_cast<int>(ranges);
-        p.per_split = static_cast<int>(ceil_div(p.k_blocks, ranges));
-        p.grid = static_cast<int>(ctas * ranges);
-        const int stage = kHalf + p.tile_n * 128;
-        // more CTAs than SMs: two to an SM
-        p.stages = std::max(1, std::min({kMostRowsStages, p.per_split, (p.grid > sm_count() ? 110 * 1024 : 200 * 1024) / stage}));
-        p.tensor_columns = allocation_of(p.tile_n);
-        const int owned = static_cast<int>(ceil_div(p.tile_n, p.splits));
-        // (shared memory in proportion to tensor memory, see plan_mx4_linear)
-        p.smem = std::max({p.stages * stage + 1024, p.splits * owned * 512 + 1024, kSmemPerSm / 512 * p.tensor_columns - 1024});
-        return p;
-    }
+    const GatedPlan few = plan_few(static_cast<int>(ceil_div(F, 64)), p.k_blocks, rows);
+    if (rows <= 128 || ceil_div(few.grid, sm_count()) * (few.per_split + 6) + (few.splits > 1 ? 4 : 0) < shortest + 14) return few;
     cut(p, best);
     p.grid = 2 * static_cast<int>(std::min(units_of(p), pairs));
     p.stages = kMostStages;
@@ -656,7 +685,8 @@ cudaError_t prepare_gated() {
         for (int act : {PATDNN_ACT_NONE, PATDNN_ACT_RELU, PATDNN_ACT_SILU}) {
             cudaError_t e = by_kernel(false, dtype, act, [&](auto product, auto) { return allow(product); });
             if (e == cudaSuccess) e = by_kernel(true, dtype, act, [&](auto product, auto) { return allow(product); });
-            if (e == cudaSuccess) e = by_rows_kernel(dtype, act, allow);
+            if (e == cudaSuccess) e = by_rows_kernel<false>(dtype, act, allow);
+            if (e == cudaSuccess) e = by_rows_kernel<true>(dtype, act, allow);
             if (e != cudaSuccess) return e;
         }
     return cudaSuccess;
@@ -686,7 +716,36 @@ static cudaError_t launch_products(const GatedMaps &maps, GatedParams &p, const 
     });
 }
 
+template <bool PHASED>
+static cudaError_t launch_rows(const GatedRowsMaps<PHASED> &maps, GatedRowsParams &p, const GatedPlan &plan, const GatedShape &s, const GatedCall &c, const GatedWork &w,
+                               cudaStream_t st, int *launches) {
+    p.h = c.h; p.gu = c.gu; p.ldh = s.h_row; p.rows = c.rows; p.F = s.F; p.n_tiles = plan.n_tiles; p.box_rows = static_cast<int>(std::min<int64_t>(128, c.rows));
+    p.k_blocks = plan.k_blocks; p.per_split = plan.per_split; p.splits = plan.splits; p.stages = plan.stages; p.tile_n = plan.tile_n;
+    p.tensor_columns = plan.tensor_columns; p.status = w.status; p.spin_limit = c.spin_limit; p.test_skip_load = c.test_skip_load;
+    *launches = 1;
+    return by_rows_kernel<PHASED>(s.dtype, s.act, [&](auto kernel) {
+        return launch_pdl(kernel, dim3(plan.grid), dim3(kRowsThreads), plan.smem, st, plan.splits, maps, p);
+    });
+}
+
+static cudaError_t launch_phased(const GatedShape &s, const GatedCall &c, const GatedWork &w, cudaStream_t st, int *launches) {
+    const GatedPlan plan = plan_gated_phased(s.F, s.K, c.rows, c.phases);
+    GatedRowsMaps<true> maps{};
+    GatedRowsParams p{};
+    p.phases = c.phases;
+    p.weight_rows = static_cast<int>(std::min<int64_t>(64, ceil_div(s.F, c.phases)));
+    cudaError_t e = make_map(&maps.x, s.dtype, c.x, c.phases * c.rows, c.x_row, c.x_row, static_cast<int>(std::min<int64_t>(128, c.rows)));
+    for (int j = 0; j < c.phases && e == cudaSuccess; ++j) {
+        p.shift[j] = static_cast<uint8_t>(gated_shift(c.wg, c.w_row, j));
+        const int64_t rows = ceil_div(s.F - j, c.phases), first = j * c.w_row - p.shift[j];      // first: at a multiple of 16 bytes
+        e = make_map(&maps.g[j], s.dtype, static_cast<const uint16_t *>(c.wg) + first, rows, s.K + p.shift[j], c.phases * c.w_row, p.weight_rows);
+        if (e == cudaSuccess) e = make_map(&maps.u[j], s.dtype, static_cast<const uint16_t *>(c.wu) + first, rows, s.K + p.shift[j], c.phases * c.w_row, p.weight_rows);
+    }
+    return e != cudaSuccess ? e : launch_rows<true>(maps, p, plan, s, c, w, st, launches);
+}
+
 cudaError_t launch_gated_forward(const GatedShape &s, const GatedCall &c, const GatedWork &w, cudaStream_t st, int *launches) {
+    if (c.phases) return launch_phased(s, c, w, st, launches);
     const GatedPlan plan = plan_gated_forward(s.F, s.K, c.rows);
     GatedMaps maps{};
     const int box = static_cast<int>(std::min<int64_t>(128, c.rows)), weights = plan.few ? 64 : 128;
@@ -696,13 +755,7 @@ cudaError_t launch_gated_forward(const GatedShape &s, const GatedCall &c, const 
     if (e != cudaSuccess) return e;
     if (plan.few) {
         GatedRowsParams p{};
-        p.h = c.h; p.gu = c.gu; p.ldh = s.h_row; p.rows = c.rows; p.F = s.F; p.n_tiles = plan.n_tiles; p.box_rows = box;
-        p.k_blocks = plan.k_blocks; p.per_split = plan.per_split; p.splits = plan.splits; p.stages = plan.stages; p.tile_n = plan.tile_n;
-        p.tensor_columns = plan.tensor_columns; p.status = w.status; p.spin_limit = c.spin_limit; p.test_skip_load = c.test_skip_load;
-        *launches = 1;
-        return by_rows_kernel(s.dtype, s.act, [&](auto kernel) {
-            return launch_pdl(kernel, dim3(plan.grid), dim3(kRowsThreads), plan.smem, st, plan.splits, maps.a, maps.b0, maps.b1, p);
-        });
+        return launch_rows<false>({maps.a, {maps.b0}, {maps.b1}}, p, plan, s, c, w, st, launches);
     }
     GatedParams p{};
     p.gu = c.gu;

@@ -23,6 +23,9 @@ struct AuxJob {
     int64_t units;                                     // rows times pieces
     int cols, padded, pieces;                          // padded: columns that are written; pieces of 256 of them
     int aligned;                                       // slopes: rows of gu and dh are, to 16 bytes
+    int64_t rows;                                      // of a copy
+    int copies;                                        // shifted ones, or 0
+    uint8_t shift[kMostPhases];
 };
 struct AuxArgs {
     AuxJob job[kJobs];
@@ -34,6 +37,18 @@ __device__ __forceinline__ void pack(const AuxJob &a, int64_t row, int c0) {
     Strip<T, 8, 8> s;
     s.load_any(static_cast<const T *>(a.x) + row * a.row + c0, a.cols - c0);
     s.store(static_cast<T *>(a.to) + row * a.to_row + c0, a.padded - c0);
+}
+
+// Copies of few rows, one element at a time.
+__device__ __forceinline__ void pack_shifted(const AuxJob &a, int64_t row, int c0) {
+    const int copy = static_cast<int>(row / a.rows), c = c0 + (threadIdx.x & 31) * 8 - a.shift[copy];
+    if (c + a.shift[copy] >= a.padded) return;
+    const uint16_t *from = static_cast<const uint16_t *>(a.x) + (row - copy * a.rows) * a.row + c;
+    uint32_t v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c + e >= 0 && c + e < a.cols ? from[e] : 0;
+    *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.to) + row * a.to_row + c + a.shift[copy]) =
+        make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
 }
 
 template <typename T, bool ALIGNED, int ACT>
@@ -90,6 +105,8 @@ __global__ void __launch_bounds__(kWarps * 32) gated_operands_kernel(const __gri
         if (j == kJobs - 1) {
             if (a.aligned) slopes<T, true, ACT>(a, row, c0);
             else slopes<T, false, ACT>(a, row, c0);
+        } else if (a.copies) {
+            pack_shifted(a, row, c0);
         } else {
             pack<T>(a, row, c0);
         }
@@ -105,7 +122,9 @@ cudaError_t launch_gated_operands(const GatedShape &s, const GatedPack (&packs)[
         AuxJob &a = args.job[i];
         a.x = packs[i].from; a.to = packs[i].to; a.row = packs[i].row; a.to_row = packs[i].to_row; a.cols = s.K; a.padded = static_cast<int>(packs[i].to_row);
         a.pieces = static_cast<int>(ceil_div(a.padded, kColumns));
-        a.units = packs[i].rows * a.pieces;
+        a.rows = packs[i].rows; a.copies = packs[i].copies;
+        std::copy(packs[i].shift, packs[i].shift + kMostPhases, a.shift);
+        a.units = packs[i].rows * std::max(1, a.copies) * a.pieces;
     }
     if (dgu) {
         AuxJob &a = args.job[kJobs - 1];

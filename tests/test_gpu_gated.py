@@ -388,3 +388,48 @@ def test_gradient_where_the_gate_leaves_the_range_of_the_type(name):
     assert torch.equal(dwg[0::2, 1], torch.full_like(dwg[0::2, 1], M * 2.0 ** -8)) and torch.equal(dwg[0::2, 0], torch.full_like(dwg[0::2, 0], M * 1.0))
     assert torch.isinf(dwu[0::2, :2]).all() and not dwg[1::2].any()
     assert b.check() is None
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("M, K, F", [(1, 6899, 300), (5, 200, 72), (40, 77, 335), (128, 1000, 1333), (2, 64, 8), (1, 3, 9), (1, 5, 4), (3, 57, 17), (100, 120, 20), (17, 449, 1030)])
+def test_weights_that_lie_anywhere(M, K, F, dtype):
+    """Weights a row apart that is no whole number of 16-byte units, at bases that begin alike in a unit and that do not, between NaNs; and a row of
+    either that is not finite, which spoils its own output alone."""
+    import torch
+    from paper_2001_00138_b200 import binding as B
+    tt, dt = types(dtype)
+    g = torch.Generator(device="cuda").manual_seed(M + K + F)
+
+    def make(r, c):
+        keep = torch.rand(r, c, generator=g, device="cuda") < min(1.0, 200.0 / K)
+        return (torch.randint(-2, 3, (r, c), generator=g, device="cuda") * keep).to(tt)
+
+    x, wg, wu = make(M, K), make(F, K), make(F, K)
+    p, u = x.double() @ wg.double().t(), x.double() @ wu.double().t()
+    for wslack in (0, 1, 2, 3, 4, 7):
+        if (K + wslack) % 8 == 0:
+            continue
+        b = B.Gated(F, K, max_rows=M + 3, dtype=dt, act=B.ACT_RELU, w_row=K + wslack, x_row=K + 3)
+        for og, ou in ((0, 0), (1, 1), (5, 5), (7, 15), (2, 3), (0, 4)):
+            (_, xs), (_, gs), (_, us) = spaced(x, 3, 1), spaced(wg, wslack, og), spaced(wu, wslack, ou)
+            if (K + 3) % 8 == 0:
+                xs = spaced(x, 3, 0)[1]
+            fh, h = spaced(torch.zeros(M, F, dtype=tt), 0, 1)
+            gu = torch.full((M, 2, F), float("nan"), dtype=tt, device="cuda")
+            b.run(xs, gs, us, h, M, gu=gu, stream=stream())
+            b.check()
+            same(gu[:, 0], p, f"g {wslack} {og} {ou}")
+            same(gu[:, 1], u, f"u {wslack} {og} {ou}")
+            same(h, (p.clamp_min(0) * u).to(tt).double(), f"h {wslack} {og} {ou}")
+            assert untouched(fh, h)
+            one, two = F // 3, F // 2
+            gs[one, K - 1] = float("inf")
+            us[two, 0] = float("nan")
+            gu.fill_(7)
+            b.run(xs, gs, us, h, M, gu=gu, stream=stream())
+            b.check()
+            keep = torch.ones(F, dtype=torch.bool, device="cuda")
+            keep[one], keep[two] = False, False
+            same(h[:, keep], (p.clamp_min(0) * u).to(tt).double()[:, keep], f"h beside {wslack} {og} {ou}")
+            assert torch.isnan(gu[:, 1, two]).all() and not torch.isfinite(gu[:, 0, one]).any()
+        b.free()
