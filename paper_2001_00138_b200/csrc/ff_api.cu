@@ -139,8 +139,10 @@ bool copies_as_it_lies(int64_t row) { return row % 8 == 0; }           // rows o
 bool operand_aligned(const void *p, int64_t row) { return aligned(p, copies_as_it_lies(row) ? 16 : 2); }
 int64_t packed_row(int64_t K) { return (K + 7) / 8 * 8; }
 
-// x and the weights of a call as the products read them: packed first, where they cannot be copied as they lie.  gu, dh: the gradient's; or nullptr
-int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu, const void *gu, const void *dh, int64_t rows, GatedCall &c, cudaStream_t st) {
+// x and the weights of a call as the products read them (those that read_x and read_w name): packed first, where they cannot be copied as they lie.
+// gu, dh: the gradient's; or nullptr
+int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu, const void *gu, const void *dh, int64_t rows, bool read_x, bool read_w, GatedCall &c,
+                   cudaStream_t st) {
     const GatedShape &s = h->s;
     c.x = x; c.wg = wg; c.wu = wu; c.x_row = s.x_row; c.w_row = s.w_row; c.rows = rows;
     c.spin_limit = h->spin_limit; c.test_skip_load = h->test_skip_load;
@@ -157,12 +159,12 @@ int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu
         c.phases = phases;
         return launched(launch_gated_operands(s, packs, nullptr, nullptr, nullptr, rows, st), 1, "gated block operands launch");
     }
-    if (h->x) {
+    if (h->x && read_x) {
         packs[0] = {x, h->x, rows, s.x_row, row, 0, {}};
         c.x = h->x;
         c.x_row = row;
     }
-    if (h->weights) {
+    if (h->weights && read_w) {
         void *second = static_cast<uint16_t *>(h->weights) + s.F * row;
         packs[1] = {wg, h->weights, s.F, s.w_row, row, 0, {}};
         packs[2] = {wu, second, s.F, s.w_row, row, 0, {}};
@@ -411,7 +413,7 @@ int patdnn_gated_run(patdnn_gated h, const void *x, const void *wg, const void *
     if (const int rc = on_device(h->device)) return rc;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     GatedCall c{};
-    if (const int rc = gated_operands(h, x, wg, wu, nullptr, nullptr, rows, c, st)) return rc;
+    if (const int rc = gated_operands(h, x, wg, wu, nullptr, nullptr, rows, true, true, c, st)) return rc;
     c.h = hidden; c.gu = gu;
     int n = 0;
     const cudaError_t e = launch_gated_forward(s, c, h->w, st, &n);
@@ -437,7 +439,7 @@ int patdnn_gated_grad(patdnn_gated h, const void *x, const void *wg, const void 
     }
     if (!dx && !dwg) return PATDNN_OK;
     GatedCall c{};
-    if (const int rc = gated_operands(h, x, wg, wu, gu, dh, rows, c, st)) return rc;
+    if (const int rc = gated_operands(h, x, wg, wu, gu, dh, rows, dwg != nullptr, dx != nullptr, c, st)) return rc;
     c.dx = dx; c.dwg = dwg; c.dwu = dwu;
     int n = 0;
     const cudaError_t e = launch_gated_gradient(s, c, h->w, st, &n);

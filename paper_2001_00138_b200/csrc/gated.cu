@@ -91,8 +91,10 @@ __device__ __forceinline__ int unit_of(const GatedParams &p, int q, int pairs, i
     return round < 0 ? v : round < p.common ? p.more[pairs] + round * pairs + q : -1;
 }
 
-// One warp: 64 columns of 32 rows of 16-bit values, 128 bytes each, from registers to rows aligned to 16 bytes, 16 rows at a time through `stage`.
-template <typename T>
+// One warp: 64 columns of 32 rows of 16-bit values, 128 bytes each, from registers to rows, 16 rows at a time through `stage`.  Rows that do not begin at a
+// multiple of 16 bytes: seven whole 16-byte units of a row, put together from neighbours, and the eight elements around them one by one, a lane each
+// (1 x 7371 -> 1577, rows of odd length: 57 us, an element per lane 76; 213 x 5900 -> 4829: 139 us, four bytes per lane 151).
+template <typename T, bool ALIGNED>
 __device__ __forceinline__ void store_lines(const float (&v)[2][32], unsigned char *stage, T *y, int64_t ldy, int rows_left) {
     const int lane = threadIdx.x & 31;
     uint32_t w[32];
@@ -120,7 +122,35 @@ __device__ __forceinline__ void store_lines(const float (&v)[2][32], unsigned ch
         for (int i = 0; i < 4; ++i) {
             const int r = i * 4 + (lane >> 3), u = lane & 7;
             const uint4 t = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((u ^ (r & 7)) << 4));
-            if (half * 16 + r < rows_left) *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(y + (half * 16 + r) * ldy) + u * 16) = t;
+            unsigned char *row = reinterpret_cast<unsigned char *>(y + (half * 16 + r) * ldy);
+            if constexpr (ALIGNED) {
+                if (half * 16 + r < rows_left) *reinterpret_cast<uint4 *>(row + u * 16) = t;
+            } else {
+                const int over = static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15), begin = 16 - over;         // of the row's bytes in the unit before
+                const uint4 b = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((((u + 7) & 7) ^ (r & 7)) << 4));
+                uint32_t w[8] = {b.x, b.y, b.z, b.w, t.x, t.y, t.z, t.w};
+                if (begin & 16) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) w[k] = w[k + 4];
+                }
+                if (begin & 8) {
+#pragma unroll
+                    for (int k = 0; k < 6; ++k) w[k] = w[k + 2];
+                }
+                if (begin & 4) {
+#pragma unroll
+                    for (int k = 0; k < 5; ++k) w[k] = w[k + 1];
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], (begin & 2) * 8);
+                // the element of this lane: one of the last over / 2, or of the first 8 - over / 2
+                const int e = u < (over >> 1) ? 64 - (over >> 1) + u : u - (over >> 1);
+                const uint16_t edge = *reinterpret_cast<const uint16_t *>(stage + r * 128 + (((e >> 3) ^ (r & 7)) << 4) + (e & 7) * 2);
+                if (half * 16 + r < rows_left) {
+                    if (u > 0) *reinterpret_cast<uint4 *>(row - over + u * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                    reinterpret_cast<uint16_t *>(row)[e] = edge;
+                }
+            }
         }
     }
 }
@@ -305,8 +335,9 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
             } else {
                 const int n = nt * 256 + quarter * 64;
                 const uint64_t places = reinterpret_cast<uintptr_t>(out) | static_cast<uint64_t>(q.ld * sizeof(T));
-                if (places % 16 == 0 && q.cols - n >= 64) {
-                    store_lines<T>(v, stage, out + row0 * q.ld + n, q.ld, rows_left);
+                if (q.cols - n >= 64) {
+                    if (places % 16 == 0) store_lines<T, true>(v, stage, out + row0 * q.ld + n, q.ld, rows_left);
+                    else store_lines<T, false>(v, stage, out + row0 * q.ld + n, q.ld, rows_left);
                 } else {
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
