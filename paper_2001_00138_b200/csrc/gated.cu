@@ -626,7 +626,7 @@ static GatedPlan plan_few(int f_tiles, int k_blocks, int64_t rows) {
     p.n_tiles = f_tiles;
     const int64_t ctas = static_cast<int64_t>(p.m_tiles) * f_tiles;
     p.splits = 1;
-    while (p.splits < 8 && ctas * p.splits * 2 <= sm_count() && k_blocks >= p.splits * 8) p.splits *= 2;
+    while (p.splits < 8 && ctas * p.splits * 2 <= cluster_room(sm_count(), p.splits * 2) && k_blocks >= p.splits * 8) p.splits *= 2;
     p.per_split = static_cast<int>(ceil_div(k_blocks, p.splits));
     p.grid = static_cast<int>(ctas * p.splits);
     const int stage = kHalf + p.tile_n * 128;

@@ -467,12 +467,12 @@ Mx8Launch plan_mx8_linear(Mx8Params &p) {
     // (Lanes push consecutive words to a finisher; 16 bytes per lane, further apart, took 2 us more.)
     const int least = p.tile_n <= 64 ? 2 : p.col_tiles < 16 ? p.col_tiles : 4;
     p.splits = 1;
-    while (p.splits < 8 && tiles * p.splits * 2 <= sm_count() && p.col_tiles >= p.splits * 2 * least) p.splits *= 2;
+    while (p.splits < 8 && tiles * p.splits * 2 <= cluster_room(sm_count(), p.splits * 2) && p.col_tiles >= p.splits * 2 * least) p.splits *= 2;
     p.tiles_per_split = static_cast<int>(ceil_div(p.col_tiles, p.splits));
     // Pairs of CTAs where an estimate in cycles says so: a column tile takes about as long in both kernels (512 cycles of MMAs for 256 x 256
     // on two SMs; the traffic of 128 x 128 through one SM's shared memory), so rounds over the SMs decide.
     const int64_t pairs = std::max(1, sm_count() / 2), pair_tiles = ceil_div(p.rows, 256) * ceil_div(p.F, 256);
-    const int64_t alone = ceil_div(tiles * p.splits, sm_count()) * (p.tiles_per_split * 600 + 2500);
+    const int64_t alone = ceil_div(tiles * p.splits, cluster_room(sm_count(), p.splits)) * (p.tiles_per_split * 600 + 2500);
     const int64_t paired = ceil_div(pair_tiles, pairs) * p.col_tiles * 560 + 3500;
     if (!p.x_raw && paired < alone) {
         l.persistent = true;

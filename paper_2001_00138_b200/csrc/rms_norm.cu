@@ -397,7 +397,7 @@ RmsPlan plan_of(int C, int64_t rows, int E, int warps, int ctas_per_sm) {
     while (p.cluster * p.warps * 32 * E < C) p.cluster *= 2;
     p.threads = std::min(8, std::max(1, warps / p.warps)) * p.warps * 32;
     const int groups = p.L < 32 ? p.threads / p.L : p.threads / 32 / p.warps;
-    const int64_t ctas = ceil_div(rows, groups), most = sm_count() * std::max(1, ctas_per_sm * warps * 32 / p.threads) / p.cluster;
+    const int64_t ctas = ceil_div(rows, groups), most = cluster_room(sm_count(), p.cluster) * std::max(1, ctas_per_sm * warps * 32 / p.threads) / p.cluster;
     p.grid = static_cast<int>(std::min(ctas, std::max<int64_t>(1, most))) * p.cluster;
     return p;
 }

@@ -112,7 +112,7 @@ def gradient_reference(s, gamma, rstd, dy, ds):
 @pytest.mark.parametrize("slack, offset", [(0, 0), (8, 8), (2, 2), (3, 1)])
 def test_gradient(M, C, dtype, slack, offset):
     """dx: u, xh and their product with the mean have 3 roundings, the mean (ADDS + 4) of the mean magnitude, three more behind; dgamma: at most
-    M / 18 + 80 additions on the longest way (18 clusters at least share the rows of the longest rows, or all M where there are fewer)."""
+    M / 18 + 80 additions on the longest way (15 clusters at least share the rows of the longest rows: M / 15 + 15, less than that up to 5000 rows)."""
     import torch
     from paper_2001_00138_b200 import binding as B
     tt, dt, (_, s), (_, dy), gamma = case(M, C, dtype, slack, M + 2 * C, offset)
