@@ -17,7 +17,7 @@ namespace patdnn {
 namespace {
 
 constexpr int kMostWarps = 16;
-constexpr int kGradSmem = 226 * 1024;                  // dynamic shared memory of a CTA of the gradient, at most
+constexpr int kGradSmem = 225 * 1024;                  // dynamic shared memory of a CTA of the gradient, at most
 
 struct RmsArgs {
     const void *x, *residual, *dsum;
@@ -47,15 +47,28 @@ __device__ __forceinline__ void cluster_barrier() {
 // The sum over a row of every warp's value, the same bits in all of its threads.  Two sets of slots in turn: a set is written again only
 // behind the barrier of the call between.  A lane reads one slot (of a cluster four), and five shuffles add them: reading them one by one takes
 // as long as a row's loads.
+// In a cluster the values are sent with stores that count their bytes on a barrier of the CTA that gets them: a cluster barrier would wait for the rows
+// that were stored before it as well (3000 x 16384 bf16: 103 us, so 71; its gradient 103 and 82).  A peer sends its next but one value only behind this CTA's next ones, which
+// its warps send when they have read the present ones.
+struct RowSlots {
+    float set[2][8][kMostWarps];                       // [2][row group, or CTA of the cluster][warp of the row]; zeros where there is none
+    unsigned long long sent[2];                        // barriers
+};
+constexpr int kMostPolls = 1 << 20;                    // of a wait (each suspends for a while); behind them the sum is NaN
 template <int L> struct RowSum {
-    float (*slots)[8][kMostWarps];                     // [2][row group, or CTA of the cluster][warp of the row]; zeros where there is none
+    RowSlots &slots;
     int warps, cluster, row_group;
     uint32_t rank;
-    int turn;
+    int calls;
     __device__ __forceinline__ void clear() {
         if (L < 32 || (warps == 1 && cluster == 1)) return;
-        float *all = &slots[0][0][0];
+        float *all = &slots.set[0][0][0];
         for (int i = threadIdx.x; i < 2 * 8 * kMostWarps; i += blockDim.x) all[i] = 0.f;
+        if (cluster > 1 && threadIdx.x == 0) {
+            for (unsigned long long &b : slots.sent)
+                asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(&b))) : "memory");
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
         __syncthreads();
         if (cluster > 1) cluster_barrier();            // the peers run, and their slots can be written
     }
@@ -63,25 +76,32 @@ template <int L> struct RowSum {
         v = lanes_sum<L>(v);
         if (L < 32 || (warps == 1 && cluster == 1)) return v;
         const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % warps;
-        float(&set)[8][kMostWarps] = slots[turn];
-        turn ^= 1;
+        float(&set)[8][kMostWarps] = slots.set[calls & 1];
+        const uint32_t bar = static_cast<uint32_t>(__cvta_generic_to_shared(&slots.sent[calls & 1])), parity = calls >> 1 & 1;
+        ++calls;
         if (cluster == 1) {
             if (lane == 0) set[row_group][warp] = v;
             asm volatile("bar.sync %0, %1;" ::"r"(row_group + 1), "r"(warps * 32) : "memory");
             v = set[row_group][lane & (kMostWarps - 1)];
             return lanes_sum<kMostWarps>(v);
         }
+        if (threadIdx.x == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(cluster * warps * 4) : "memory");
         if (lane < cluster) {                          // lane l tells CTA l
             const uint32_t local = static_cast<uint32_t>(__cvta_generic_to_shared(&set[rank][warp]));
-            uint32_t remote;
+            uint32_t remote, remote_bar;
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(lane));
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote), "f"(v) : "memory");
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote_bar) : "r"(bar), "r"(lane));
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];" ::"r"(remote), "r"(__float_as_uint(v)), "r"(remote_bar) : "memory");
         }
-        cluster_barrier();
+        uint32_t there = 0;
+        for (int polls = 0; polls < kMostPolls && !there; ++polls)
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                         : "=r"(there) : "r"(bar), "r"(parity) : "memory");
+        __syncwarp();
         v = 0.f;
 #pragma unroll
         for (int k = 0; k < 4; ++k) v += set[2 * k + (lane >> 4)][lane & (kMostWarps - 1)];
-        return lanes_sum<32>(v);
+        return lanes_sum<32>(there ? v : __uint_as_float(0x7fffffffu));
     }
 };
 
@@ -99,7 +119,7 @@ template <int A, int E, int L> __device__ __forceinline__ void load_gamma(float 
 // MX: the output is 8-bit blocks.  L: lanes of a row; 32, or 16 or 8 where they take all of it.
 template <typename T, int A, int E, int L, bool MX>
 __global__ void __launch_bounds__(kMostWarps * 32) rms_norm_kernel(RmsArgs a) {
-    __shared__ float slots[2][8][kMostWarps];
+    __shared__ RowSlots slots;
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & (L - 1);
     const int groups = L < 32 ? blockDim.x / L : (blockDim.x >> 5) / a.warps, group = L < 32 ? threadIdx.x / L : warp / a.warps;   // rows at a time
@@ -131,11 +151,6 @@ __global__ void __launch_bounds__(kMostWarps * 32) rms_norm_kernel(RmsArgs a) {
 #pragma unroll
             for (int e = 0; e < E; ++e) v[e] += r[e];
         }
-        if (a.sum && on) {
-            Strip<T, A, E, L> out;
-            out.narrow_from(v);
-            out.store(static_cast<T *>(a.sum) + row * a.r_row + c0, left);
-        }
         if (row + step < a.rows) {
             in.load(x + (row + step) * a.x_row, left);
             if (a.residual) add.load(res + (row + step) * a.r_row, left);
@@ -144,6 +159,11 @@ __global__ void __launch_bounds__(kMostWarps * 32) rms_norm_kernel(RmsArgs a) {
 #pragma unroll
         for (int e = 0; e < E; ++e) squares = fmaf(v[e], v[e], squares);
         float total = row_sum(squares), eps = a.eps, scale = 1.f;
+        if (a.sum && on) {                             // (behind the sum: a cluster's barrier waits for stores before it)
+            Strip<T, A, E, L> out;
+            out.narrow_from(v);
+            out.store(static_cast<T *>(a.sum) + row * a.r_row + c0, left);
+        }
         const bool beyond = !(total <= 1e38f) || (total < 1e-27f && a.eps < 1e-18f);
         if (L < 32 ? __any_sync(0xffffffffu, beyond) : beyond) {       // squares beyond fp32's range: the row times a power of two, and eps its square
             if (beyond) scale = total < 1.f ? 0x1p80f : 0x1p-80f;
@@ -194,7 +214,7 @@ template <typename T, int A, int E, int L, bool ASYNC>
 __global__ void __launch_bounds__((ASYNC ? grad_warps(E) : kMostWarps) * 32) rms_grad_kernel(RmsArgs a) {
     using Copies = RmsCopies<T, A, E, ASYNC>;
     constexpr int S = Copies::kStages, NA = E / A, UNIT = Copies::kUnit;
-    __shared__ float slots[2][8][kMostWarps];
+    __shared__ RowSlots slots;
     extern __shared__ __align__(16) unsigned char smem[];              // gamma and the copies; at the end dgamma of every set of warps
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & (L - 1);
@@ -395,7 +415,8 @@ RmsPlan plan_of(int C, int64_t rows, int E, int warps, int ctas_per_sm) {
     p.cluster = 1;
     p.warps = std::min<int>(kMostWarps, static_cast<int>(ceil_div(C, 32 * E)));
     while (p.cluster * p.warps * 32 * E < C) p.cluster *= 2;
-    p.threads = std::min(8, std::max(1, warps / p.warps)) * p.warps * 32;
+    if (p.cluster > 1) p.warps = static_cast<int>(ceil_div(C, p.cluster * 32 * E));        // its CTAs take about as much of a row each
+    p.threads = (p.cluster > 1 ? 1 : std::min(8, std::max(1, warps / p.warps))) * p.warps * 32;
     const int groups = p.L < 32 ? p.threads / p.L : p.threads / 32 / p.warps;
     const int64_t ctas = ceil_div(rows, groups), most = cluster_room(sm_count(), p.cluster) * std::max(1, ctas_per_sm * warps * 32 / p.threads) / p.cluster;
     p.grid = static_cast<int>(std::min(ctas, std::max<int64_t>(1, most))) * p.cluster;
