@@ -341,3 +341,37 @@ def test_gradient_of_rows_of_every_length(dtype):
             size = rs * (u.abs() * 3 + xh.abs() * (m.abs() * 4 + (u * xh).abs().mean(1, keepdim=True) * (adds(C) + 4))) + want.abs() * 2
             check(dx, want, 1.01 * R.EPS24 * size + R.UNIT[dtype] * 1.01 * want.abs() + R.TINY[dtype], f"dx {M} x {C}")
             check(dgamma, (dy.double() * xh).sum(0), (M / 18 + 80) * R.EPS24 * (dy.double() * xh).abs().sum(0), f"dgamma {M} x {C}")
+
+
+@pytest.mark.parametrize("M, C", [(1500, 9000), (700, 20008), (300, 40001)])
+def test_long_rows_many_times_over(M, C):
+    """Clusters of two, four and eight CTAs that exchange sums for many rows; the same bits from the same call, alone and beside another stream's."""
+    import torch
+    from paper_2001_00138_b200 import binding as B
+    tt, dt, (_, x), (_, r), gamma = case(M, C, "bf16", 0, M + C)
+    h, other = B.RmsNorm(C, dtype=dt, eps=EPS), B.RmsNorm(C, dtype=dt, eps=EPS)
+    total, y, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(M, device="cuda")
+    h.run(x, gamma, y, M, residual=r, sum=total, rstd=rstd, stream=stream())
+    torch.cuda.synchronize()
+    s, rs, want = forward_reference(x, r, gamma)
+    check(rstd[:, None], rs, (adds(C) + 8) / 2 * R.EPS24 * rs * 1.01, "rstd")
+    check(y, want, ((adds(C) + 8) / 2 + 3) * 1.01 * R.EPS24 * want.abs() + R.UNIT["bf16"] * 1.01 * want.abs() + R.TINY["bf16"], "y")
+    dx, dgamma = torch.empty_like(x), torch.empty(C, device="cuda")
+    h.grad(total, gamma, rstd, r, dx, dgamma, M, dsum=x, stream=stream())
+    torch.cuda.synchronize()
+    want, xh, u, m = gradient_reference(total, gamma, rstd, r, x)
+    rs = rstd.double()[:, None]
+    size = rs * (u.abs() * 3 + xh.abs() * (m.abs() * 4 + (u * xh).abs().mean(1, keepdim=True) * (adds(C) + 4))) + want.abs() * 2
+    check(dx, want, 1.01 * R.EPS24 * size + R.UNIT["bf16"] * 1.01 * want.abs() + R.TINY["bf16"], "dx")
+    check(dgamma, (r.double() * xh).sum(0), (M / 15 + 95) * R.EPS24 * (r.double() * xh).abs().sum(0), "dgamma")
+    side = torch.cuda.Stream()
+    y2, dx2, dgamma2, y3, dx3, dgamma3 = (torch.full_like(t, float("nan")) for t in (y, dx, dgamma, y, dx, dgamma))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        h.run(x, gamma, y2, M, residual=r, stream=stream())
+        other.grad(total, gamma, rstd, r, dx3, dgamma3, M, dsum=x, stream=side.cuda_stream)
+        h.grad(total, gamma, rstd, r, dx2, dgamma2, M, dsum=x, stream=stream())
+        other.run(x, gamma, y3, M, residual=r, stream=side.cuda_stream)
+    torch.cuda.synchronize()
+    for a, b in ((y, y2), (y, y3), (dx, dx2), (dx, dx3), (dgamma, dgamma2), (dgamma, dgamma3)):
+        assert torch.equal(a, b)
