@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
             }
             const int64_t row0 = static_cast<int64_t>(mt) * 256 + rank * 128 + quadrant * 32;
             const int rows_left = static_cast<int>(max(static_cast<int64_t>(-1), min(static_cast<int64_t>(32), q.rows - row0)));
-            if (!mbar_wait(done + 8 * buf, (t >> 1) & 1, ctx, 126)) break;
+            if (!warp_wait(done + 8 * buf, (t >> 1) & 1, ctx, 126)) break;
             tc_fence_after();
             // 64 columns of the accumulator; forward: 32 of the gate's and the same 32 of the up projection's
             float v[2][32];
@@ -538,7 +538,7 @@ gated_rows_kernel(const __grid_constant__ GatedRowsMaps<PHASED> maps, const __gr
         if (leader) umma_commit(done);
     }
     __syncwarp();
-    const bool ok = mbar_wait(done, 0, ctx, 144);
+    const bool ok = warp_wait(done, 0, ctx, 144);
     tc_fence_after();
     // CTA r of the cluster finishes the rows j with j % splits == r
     const int shift = 31 - __clz(p.splits), owned = (p.tile_n + p.splits - 1) >> shift;          // splits is a power of two

@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx4_linear_kernel(Mx4Params p)
     }
     __syncwarp();
     pdl_wait();
-    const bool ok = mbar_wait(done, 0, ctx, 104);
+    const bool ok = warp_wait(done, 0, ctx, 104);
     tc_fence_after();
     const int f = ft * 128 + (warp & 3) * 32 + lane;
     const float bias = p.bias && f < p.F ? p.bias[f] : 0.f;
@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx4_rows_kernel(Mx4Params p) 
             if (cols == 64) bias[32 + lane] = ahead1;
             ahead0 = bias_of(ft * p.tile_n + quarter * cols + lane);
             ahead1 = bias_of(ft * p.tile_n + quarter * cols + 32 + lane);
-            if (!mbar_wait(done, phase, ctx, 115)) break;
+            if (!warp_wait(done, phase, ctx, 115)) break;
             phase ^= 1;
             tc_fence_after();
             uint32_t v[64];

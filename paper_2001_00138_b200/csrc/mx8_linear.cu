@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) mx8_linear_kernel(Mx8Params p)
     }
     __syncwarp();
     pdl_wait();
-    const bool ok = mbar_wait(done, 0, ctx, 104);
+    const bool ok = warp_wait(done, 0, ctx, 104);
     tc_fence_after();
     const int place = (warp & 3) * 32 + lane, f = ft * 128 + place;      // lanes are outputs: a warp stores 32 consecutive ones of a row
     const float bias = p.bias && f < p.F ? p.bias[f] : 0.f;
@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) mx8_pair_kernel(const __grid_
 #pragma unroll
             for (int c = lane; c < 64; c += 32) bias[c] = p.bias && f0 + c < p.F ? p.bias[f0 + c] : 0.f;
             __syncwarp();
-            if (!mbar_wait(done, phase, ctx, 135)) break;
+            if (!warp_wait(done, phase, ctx, 135)) break;
             phase ^= 1;
             tc_fence_after();
             uint32_t v[64];
