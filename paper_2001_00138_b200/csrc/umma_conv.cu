@@ -521,7 +521,7 @@ conv_umma_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         }
     } else {
         // epilogue warps: warp w owns TMEM lanes 32*(w%4) .. +31; lane = output pixel m of the box
-        if (mbar_wait(bar_acc, 0, status, 3)) {
+        if (__all_sync(0xffffffffu, mbar_wait(bar_acc, 0, status, 3))) {
             tc_fence_after();
             if (ks == 1) {
 #pragma unroll 1
@@ -808,48 +808,51 @@ conv_umma_halo_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_con
         if (static_cast<int>(blockIdx.x) < n_tiles) { fetch(blockIdx.x); stash(patch0); }
         asm volatile("bar.sync 2, %0;" ::"n"(kGatherThreads) : "memory");
         int ia = 0;
+        bool dead = false;                                       // a wait ran out: keep meeting the barrier, which has no bound, and skip the work
         for (int t = blockIdx.x; t < n_tiles; t += gridDim.x, ++ia) {
             const float *patch = patch0 + (ia & 1) * pstride;
             const bool more = t + static_cast<int>(gridDim.x) < n_tiles;
             if (more) fetch(t + gridDim.x);                      // loads in flight while the rows are built
             const int sa = ia % NA, ua = ia / NA;
-            if (ua > 0 && !mbar_wait(bar_ea + 8 * sa, (ua - 1) & 1, status, 4)) break;
-            unsigned char *abase = smem + static_cast<size_t>(sa) * a_stage;
-            for (int row = g; row < MT * kTileM; row += kGatherThreads) {
-                const int ty = row / p.TW, tx = row - ty * p.TW;
-                unsigned char *r_hi = abase + row * 128, *r_lo = r_hi + a_plane;
-                const int sw = row & 7;                          // 128-byte swizzle: 16-byte chunk index XOR (row mod 8)
-                const float *pp = patch + ty * pw + tx;
+            if (!dead && ua > 0) dead = !__all_sync(0xffffffffu, mbar_wait(bar_ea + 8 * sa, (ua - 1) & 1, status, 4));
+            if (!dead) {
+                unsigned char *abase = smem + static_cast<size_t>(sa) * a_stage;
+                for (int row = g; row < MT * kTileM; row += kGatherThreads) {
+                    const int ty = row / p.TW, tx = row - ty * p.TW;
+                    unsigned char *r_hi = abase + row * 128, *r_lo = r_hi + a_plane;
+                    const int sw = row & 7;                          // 128-byte swizzle: 16-byte chunk index XOR (row mod 8)
+                    const float *pp = patch + ty * pw + tx;
 #pragma unroll
-                for (int ch = 0; ch < 8; ++ch) {
-                    uint32_t hi[4], lo[4];
+                    for (int ch = 0; ch < 8; ++ch) {
+                        uint32_t hi[4], lo[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float v2[2];
+                        for (int e = 0; e < 4; ++e) {
+                            float v2[2];
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            const int kk = 8 * ch + 2 * e + u;   // compile-time: the loops are fully unrolled
-                            const int c = kk / 9, tap = kk - 9 * c, r = tap / 3, sx = tap - 3 * r;
-                            v2[u] = (c < p.C) ? pp[c * pplane + r * pw + sx] : 0.f;
+                            for (int u = 0; u < 2; ++u) {
+                                const int kk = 8 * ch + 2 * e + u;   // compile-time: the loops are fully unrolled
+                                const int c = kk / 9, tap = kk - 9 * c, r = tap / 3, sx = tap - 3 * r;
+                                v2[u] = (c < p.C) ? pp[c * pplane + r * pw + sx] : 0.f;
+                            }
+                            if constexpr (S == 2) {
+                                const __nv_bfloat162 h2 = __floats2bfloat162_rn(v2[0], v2[1]);
+                                const float2 hf = __bfloat1622float2(h2);
+                                const __nv_bfloat162 l2 = __floats2bfloat162_rn(v2[0] - hf.x, v2[1] - hf.y);
+                                hi[e] = *reinterpret_cast<const uint32_t *>(&h2);
+                                lo[e] = *reinterpret_cast<const uint32_t *>(&l2);
+                            } else {
+                                const __half2 h2 = __floats2half2_rn(v2[0], v2[1]);
+                                hi[e] = *reinterpret_cast<const uint32_t *>(&h2);
+                            }
                         }
-                        if constexpr (S == 2) {
-                            const __nv_bfloat162 h2 = __floats2bfloat162_rn(v2[0], v2[1]);
-                            const float2 hf = __bfloat1622float2(h2);
-                            const __nv_bfloat162 l2 = __floats2bfloat162_rn(v2[0] - hf.x, v2[1] - hf.y);
-                            hi[e] = *reinterpret_cast<const uint32_t *>(&h2);
-                            lo[e] = *reinterpret_cast<const uint32_t *>(&l2);
-                        } else {
-                            const __half2 h2 = __floats2half2_rn(v2[0], v2[1]);
-                            hi[e] = *reinterpret_cast<const uint32_t *>(&h2);
-                        }
+                        *reinterpret_cast<uint4 *>(r_hi + ((ch ^ sw) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                        if constexpr (S == 2) *reinterpret_cast<uint4 *>(r_lo + ((ch ^ sw) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                     }
-                    *reinterpret_cast<uint4 *>(r_hi + ((ch ^ sw) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                    if constexpr (S == 2) *reinterpret_cast<uint4 *>(r_lo + ((ch ^ sw) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                 }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // generic-proxy writes -> visible to the MMA
+                __syncwarp();
+                if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_fa + 8 * sa) : "memory");
             }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // generic-proxy writes -> visible to the MMA
-            __syncwarp();
-            if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_fa + 8 * sa) : "memory");
             if (more) stash(patch0 + ((ia + 1) & 1) * pstride);
             asm volatile("bar.sync 2, %0;" ::"n"(kGatherThreads) : "memory");   // next patch complete, this one free
         }
@@ -861,6 +864,7 @@ conv_umma_halo_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_con
         const int ty = m / p.TW, txx = m - ty * p.TW;
         const int et = threadIdx.x - 64;                         // 0..255 among the epilogue threads
         int j = 0;
+        bool dead = false;                                       // a wait ran out: keep meeting the barrier, which has no bound, and skip the work
         for (int t = blockIdx.x; t < n_tiles; t += gridDim.x, ++j) {
             const int buf = j & 1;
             int ft, x0, y0, n;
@@ -868,7 +872,8 @@ conv_umma_halo_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_con
             const int f0 = ft * BN;
             for (int i = et; i < BN; i += 256) s_bias[buf][i] = (f0 + i < p.F) ? p.bias[f0 + i] : 0.f;
             asm volatile("bar.sync 1, 256;" ::: "memory");     // the eight epilogue warps only
-            if (!mbar_wait(bar_af + 8 * buf, (j >> 1) & 1, status, 3)) break;
+            if (!dead) dead = !__all_sync(0xffffffffu, mbar_wait(bar_af + 8 * buf, (j >> 1) & 1, status, 3));
+            if (dead) continue;
             tc_fence_after();
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
@@ -1109,6 +1114,7 @@ conv_umma_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_con
         const int ty = m / p.TW, txx = m - ty * p.TW;
         const int et = threadIdx.x - 64;
         int j = 0;
+        bool dead = false;                                       // a wait ran out: keep meeting the barrier, which has no bound, and skip the work
         for (int q = cluster_id; q < n_pairs; q += n_clusters, ++j) {
             const int buf = j & 1;
             int ft, x0, y0, n;
@@ -1116,7 +1122,8 @@ conv_umma_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_con
             const int f0 = ft * BN;
             for (int i = et; i < BN; i += 256) s_bias[buf][i] = (f0 + i < p.F) ? p.bias[f0 + i] : 0.f;
             asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (!mbar_wait(bar_af + 8 * buf, (j >> 1) & 1, status, 3)) break;
+            if (!dead) dead = !__all_sync(0xffffffffu, mbar_wait(bar_af + 8 * buf, (j >> 1) & 1, status, 3));
+            if (dead) continue;
             tc_fence_after();
             const int y = y0 + ty, x = x0 + txx;
             const bool pix_ok = n < p.N && y < p.H && x < p.W;
