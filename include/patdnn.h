@@ -398,7 +398,13 @@ PATDNN_API int patdnn_linear_free(patdnn_linear h);
  *   E_DTYPE    dtype unknown
  *   E_NO_DEVICE  another device is current than when the handle was made
  * A handle owns the gradient's workspace: gradient calls that can overlap on the GPU need a handle each; patdnn_rms_run and _run_mx8 use
- * none.  rows = 0 launches nothing (the gradient writes zeros to dgamma).  Asynchronous on `stream`, but for patdnn_rms_create.
+ * none.  rows = 0 launches nothing (the gradient writes zeros to dgamma).  Asynchronous on `stream`, but for patdnn_rms_create, which waits for the
+ * device, and patdnn_rms_check.
+ * Rows of more than 4096 to 8192 columns are shared by the CTAs of a cluster, which wait for one another's sums; these waits are bounded:
+ *   patdnn_rms_check       waits for the device; E_DEVICE_TIMEOUT if such a wait of this handle ran out: rows whose sum it was, and rows after them, are
+ *                          NaN (their dx, in the gradient)
+ *   patdnn_rms_debug_wait  as patdnn_linear_debug_wait; the first CTA of every cluster waits for a value that nobody sends at the skip_sum-th sum of its
+ *                          own walk (a sum per row; 0 = never)
  */
 typedef struct patdnn_rms_s *patdnn_rms;
 typedef struct {
@@ -421,6 +427,8 @@ PATDNN_API int patdnn_rms_run_mx8(patdnn_rms h, const void *x, const void *resid
  * DEVICE float [C].  Both are overwritten. */
 PATDNN_API int patdnn_rms_grad(patdnn_rms h, const void *s, const float *gamma, const float *rstd, const void *dy, const void *dsum, void *dx,
                                float *dgamma, int64_t rows, void *stream);
+PATDNN_API int patdnn_rms_check(patdnn_rms h);
+PATDNN_API int patdnn_rms_debug_wait(patdnn_rms h, uint32_t polls, int32_t skip_sum);
 PATDNN_API int patdnn_rms_free(patdnn_rms h);
 
 /*

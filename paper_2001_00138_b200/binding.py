@@ -32,7 +32,8 @@ EXPORTED_SYMBOLS = (
     "patdnn_mx4_bytes", "patdnn_mx4_quantize", "patdnn_mx4_dequantize",
     "patdnn_linear_encode", "patdnn_linear_run", "patdnn_linear_run_mx4", "patdnn_linear_check", "patdnn_linear_plan", "patdnn_linear_debug_wait",
     "patdnn_linear_free",
-    "patdnn_rms_create", "patdnn_rms_run", "patdnn_rms_run_mx8", "patdnn_rms_grad", "patdnn_rms_free",
+    "patdnn_rms_create", "patdnn_rms_run", "patdnn_rms_run_mx8", "patdnn_rms_grad", "patdnn_rms_check", "patdnn_rms_debug_wait",
+    "patdnn_rms_free",
     "patdnn_mx8_bytes", "patdnn_mx8_quantize", "patdnn_mx8_dequantize",
     "patdnn_linear8_encode", "patdnn_linear8_run", "patdnn_linear8_run_mx8", "patdnn_linear8_check", "patdnn_linear8_plan",
     "patdnn_linear8_debug_wait", "patdnn_linear8_free",
@@ -155,6 +156,8 @@ def load() -> ctypes.CDLL:
     lib.patdnn_rms_run.argtypes = [vp] * 7 + [i64, vp]
     lib.patdnn_rms_run_mx8.argtypes = [vp] * 7 + [i64, vp]
     lib.patdnn_rms_grad.argtypes = [vp] * 8 + [i64, vp]
+    lib.patdnn_rms_check.argtypes = [vp]
+    lib.patdnn_rms_debug_wait.argtypes = [vp, ctypes.c_uint32, i32]
     lib.patdnn_rms_free.argtypes = [vp]
     lib.patdnn_mx8_bytes.argtypes = lib.patdnn_mx4_bytes.argtypes
     lib.patdnn_mx8_quantize.argtypes = lib.patdnn_mx4_quantize.argtypes
@@ -506,6 +509,14 @@ class RmsNorm:
         """patdnn_rms_grad: gradients of ``run`` with its sum and rstd; overwrites dx and dgamma."""
         _check(load().patdnn_rms_grad(self._h, _ptr(s), _ptr(gamma), _ptr(rstd), _ptr(dy), _opt(dsum), _ptr(dx), _ptr(dgamma), rows, stream),
                "patdnn_rms_grad")
+
+    def check(self) -> None:
+        """patdnn_rms_check: synchronise and raise if a device-side bounded wait (of rows that several CTAs share) expired."""
+        _check(load().patdnn_rms_check(self._h), "patdnn_rms_check")
+
+    def debug_wait(self, polls: int, skip_sum: int = 0) -> None:
+        """patdnn_rms_debug_wait: bound of the device-side waits (polls; 0 = default) and the test hook that withholds one sum."""
+        _check(load().patdnn_rms_debug_wait(self._h, polls, skip_sum), "patdnn_rms_debug_wait")
 
     def free(self) -> None:
         if self._h:

@@ -71,12 +71,18 @@ struct RmsShape {
     float eps;
     int64_t x_row, r_row, y_row;            // strides in elements
 };
+struct RmsWait {                            // of the clusters that share a row
+    int *status;
+    uint32_t spin_limit;                    // polls of a bounded wait (0 = the default)
+    int test_skip;                          // test hook: the first CTA of every cluster waits for a value too many at this (1-based) sum over a row of its walk (0 = off)
+};
 struct RmsCall {
     const void *x, *residual;               // residual may be nullptr
     const float *gamma;
     void *sum, *y, *mx;                     // sum, and one of y and mx, may be nullptr
     float *rstd;                            // may be nullptr
     int64_t rows;
+    RmsWait wait;
 };
 cudaError_t launch_rms_norm(const RmsShape &s, const RmsCall &c, cudaStream_t st);
 struct RmsGradCall {
@@ -85,6 +91,7 @@ struct RmsGradCall {
     void *dx;
     float *dgamma, *ws;
     int64_t rows;
+    RmsWait wait;
 };
 cudaError_t prepare_rms();                  // opt in to the dynamic shared memory
 size_t rms_workspace_floats(const RmsShape &s);

@@ -21,7 +21,14 @@ struct patdnn_rms_s {
     RmsShape s{};
     int device = -1;
     float *ws = nullptr;                    // the gradient's partial sums
-    ~patdnn_rms_s() { cudaFree(ws); }
+    int *status = nullptr;
+    uint32_t spin_limit = 0;                // patdnn_rms_debug_wait
+    int test_skip = 0;
+    RmsWait wait() const { return {status, spin_limit, test_skip}; }
+    ~patdnn_rms_s() {
+        cudaFree(ws);
+        cudaFree(status);
+    }
 };
 
 struct patdnn_linear8_s {
@@ -101,6 +108,17 @@ template <typename H> int failed(H *h, cudaError_t e, const char *what) {
 
 bool too_many_tiles(int64_t rows, int64_t F) { return ceil_div(rows, 128) * ceil_div(F, 128) > INT32_MAX / 8; }   // CTAs of one launch
 
+// Waits for the device, reports a bounded wait that ran out and clears the word.
+int check_status(int device, int *status) {
+    if (const int rc = on_device(device)) return rc;
+    CU(cudaDeviceSynchronize());
+    int word = 0;
+    CU(cudaMemcpy(&word, status, sizeof(int), cudaMemcpyDeviceToHost));
+    if (!word) return PATDNN_OK;
+    CU(cudaMemset(status, 0, sizeof(int)));
+    return PATDNN_E_DEVICE_TIMEOUT;
+}
+
 // mx: 8-bit rows, or nullptr with the rows themselves at x
 int product(patdnn_linear8 h, const void *mx, const void *x, int64_t ldx, int64_t rows, void *y, int64_t ldy, cudaStream_t st) {
     if (too_many_tiles(rows, h->d.F)) return PATDNN_E_SHAPE;
@@ -126,7 +144,7 @@ int rms_forward(patdnn_rms h, const void *x, const void *residual, const float *
     if (!x || !gamma || !out) return PATDNN_E_NULL;
     if (const int rc = on_device(h->device)) return rc;
     RmsCall c{};
-    c.x = x; c.residual = residual; c.gamma = gamma; c.sum = sum; c.rstd = rstd; c.rows = rows;
+    c.x = x; c.residual = residual; c.gamma = gamma; c.sum = sum; c.rstd = rstd; c.rows = rows; c.wait = h->wait();
     (mx ? c.mx : c.y) = out;
     return launched(launch_rms_norm(s, c, st), 1, "RMS norm launch");
 }
@@ -197,7 +215,10 @@ int patdnn_rms_create(const patdnn_rms_desc *desc, patdnn_rms *out) {
     h->s = s;
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = allocate(&h->ws, rms_workspace_floats(s));
+    if (e == cudaSuccess) e = allocate(&h->status, 4);
+    if (e == cudaSuccess) e = cudaMemset(h->status, 0, 16);
     if (e == cudaSuccess) e = prepare_rms();
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();                  // the status word is zero on every stream from here on
     if (e != cudaSuccess) return failed(h, e, "patdnn_rms_create");
     *out = h;
     return PATDNN_OK;
@@ -228,9 +249,22 @@ int patdnn_rms_grad(patdnn_rms h, const void *s, const float *gamma, const float
     }
     RmsGradCall c{};
     c.s = s; c.dy = dy; c.dsum = dsum; c.gamma = gamma; c.rstd = rstd; c.dx = dx; c.dgamma = dgamma; c.ws = h->ws; c.rows = rows;
+    c.wait = h->wait();
     int n = 0;
     const cudaError_t e = launch_rms_grad(h->s, c, st, &n);
     return launched(e, n, "RMS norm gradient launch");
+}
+
+int patdnn_rms_check(patdnn_rms h) {
+    return h ? check_status(h->device, h->status) : PATDNN_E_NULL;
+}
+
+int patdnn_rms_debug_wait(patdnn_rms h, uint32_t polls, int32_t skip_sum) {
+    if (!h) return PATDNN_E_NULL;
+    if (skip_sum < 0) return PATDNN_E_SHAPE;
+    h->spin_limit = polls;
+    h->test_skip = skip_sum;
+    return PATDNN_OK;
 }
 
 int patdnn_rms_free(patdnn_rms h) {
@@ -339,14 +373,7 @@ int patdnn_linear8_plan(int32_t F, int32_t K, int64_t rows, int32_t from_8_bit_r
 }
 
 int patdnn_linear8_check(patdnn_linear8 h) {
-    if (!h) return PATDNN_E_NULL;
-    if (const int rc = on_device(h->device)) return rc;
-    CU(cudaDeviceSynchronize());
-    int word = 0;
-    CU(cudaMemcpy(&word, h->status, sizeof(int), cudaMemcpyDeviceToHost));
-    if (!word) return PATDNN_OK;
-    CU(cudaMemset(h->status, 0, sizeof(int)));
-    return PATDNN_E_DEVICE_TIMEOUT;
+    return h ? check_status(h->device, h->status) : PATDNN_E_NULL;
 }
 
 int patdnn_linear8_debug_wait(patdnn_linear8 h, uint32_t polls, int32_t skip_load_iteration) {
@@ -462,14 +489,7 @@ int patdnn_gated_plan(int32_t F, int32_t K, int64_t rows, int32_t product, patdn
 }
 
 int patdnn_gated_check(patdnn_gated h) {
-    if (!h) return PATDNN_E_NULL;
-    if (const int rc = on_device(h->device)) return rc;
-    CU(cudaDeviceSynchronize());
-    int word = 0;
-    CU(cudaMemcpy(&word, h->w.status, sizeof(int), cudaMemcpyDeviceToHost));
-    if (!word) return PATDNN_OK;
-    CU(cudaMemset(h->w.status, 0, sizeof(int)));
-    return PATDNN_E_DEVICE_TIMEOUT;
+    return h ? check_status(h->device, h->w.status) : PATDNN_E_NULL;
 }
 
 int patdnn_gated_debug_wait(patdnn_gated h, uint32_t polls, int32_t skip_load_iteration) {

@@ -12,6 +12,7 @@
 
 #include "kernels.hpp"
 #include "mx8_device.cuh"
+#include "umma_ptx.cuh"
 
 namespace patdnn {
 namespace {
@@ -28,6 +29,9 @@ struct RmsArgs {
     int64_t rows, x_row, r_row, y_row, scales_at;
     int C, warps, cluster, col_tiles, groups;          // warps: of a row, per CTA
     float eps;
+    int *status;                                       // clusters: of a wait that ran out
+    uint32_t spin_limit;
+    int test_skip;
 };
 
 template <int L> __device__ __forceinline__ float lanes_sum(float v) {
@@ -54,12 +58,16 @@ struct alignas(128) RowSlots {                         // what lies behind begin
     float set[2][8][kMostWarps];                       // [2][row group, or CTA of the cluster][warp of the row]; zeros where there is none
     unsigned long long sent[2];                        // barriers
 };
-constexpr int kMostPolls = 1 << 20;                    // of a wait (each suspends for a while); behind them the sum is NaN
+// A lane whose wait runs out gives up, and reports it at the end: it waits for nothing and sends nothing any more, so that sums that lack its values are never complete,
+// and adds a NaN, so that this row and all later ones of its warp are NaN, never a wrong number.
+constexpr int kRowSumCode = 151;                       // status word
 template <int L> struct RowSum {
     RowSlots &slots;
+    const RmsArgs &a;
     int warps, cluster, row_group;
     uint32_t rank;
     int calls;
+    uint32_t there;                                    // 0: this lane has given up
     __device__ __forceinline__ void clear() {
         if (L < 32 || (warps == 1 && cluster == 1)) return;
         float *all = &slots.set[0][0][0];
@@ -85,16 +93,17 @@ template <int L> struct RowSum {
             v = set[row_group][lane & (kMostWarps - 1)];
             return lanes_sum<kMostWarps>(v);
         }
-        if (threadIdx.x == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(cluster * warps * 4) : "memory");
-        if (lane < cluster) {                          // lane l tells CTA l
+        if (threadIdx.x == 0 && there)
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((cluster * warps + (calls == a.test_skip && rank == 0)) * 4) : "memory");
+        if (lane < cluster && there) {                 // lane l tells CTA l
             const uint32_t local = static_cast<uint32_t>(__cvta_generic_to_shared(&set[rank][warp]));
             uint32_t remote, remote_bar;
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(lane));
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote_bar) : "r"(bar), "r"(lane));
             asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];" ::"r"(remote), "r"(__float_as_uint(v)), "r"(remote_bar) : "memory");
         }
-        uint32_t there = 0;
-        for (int polls = 0; polls < kMostPolls && !there; ++polls)
+        uint32_t polls = there ? a.spin_limit : 0;
+        for (there = 0; polls > 0 && !there; --polls)
             asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
                          : "=r"(there) : "r"(bar), "r"(parity) : "memory");
         __syncwarp();
@@ -102,6 +111,20 @@ template <int L> struct RowSum {
 #pragma unroll
         for (int k = 0; k < 4; ++k) v += set[2 * k + (lane >> 4)][lane & (kMostWarps - 1)];
         return lanes_sum<32>(there ? v : __uint_as_float(0x7fffffffu));
+    }
+    // In front of a sum that only some rows take: a warp with a lane that has given up sends nothing at all, since its turns are not the others' any more.
+    __device__ __forceinline__ void agree() {
+        if (cluster > 1) there = __all_sync(0xffffffffu, there);
+    }
+    // A CTA's slots are written by its peers: it may not end before they have.  Where a wait ran out, what was sent may still be on its way when
+    // everybody has stopped sending: a few hundred microseconds for it.
+    __device__ __forceinline__ void finish() {
+        if (cluster == 1) return;
+        cluster_barrier();
+        if (!there) {
+            atomicCAS(a.status, 0, kRowSumCode);
+            for (int i = 0; i < 200; ++i) __nanosleep(1000);
+        }
     }
 };
 
@@ -125,7 +148,7 @@ __global__ void __launch_bounds__(kMostWarps * 32) rms_norm_kernel(RmsArgs a) {
     const int groups = L < 32 ? blockDim.x / L : (blockDim.x >> 5) / a.warps, group = L < 32 ? threadIdx.x / L : warp / a.warps;   // rows at a time
     const uint32_t rank = a.cluster > 1 ? rank_in_cluster() : 0;
     const int c0 = L < 32 ? 0 : (static_cast<int>(rank) * a.warps + warp % a.warps) * 32 * E, left = a.C - c0;
-    RowSum<L> row_sum{slots, a.warps, a.cluster, group, rank, 0};
+    RowSum<L> row_sum{slots, a, a.warps, a.cluster, group, rank, 0, 1};
     row_sum.clear();
     const int64_t step = static_cast<int64_t>(gridDim.x / a.cluster) * groups;
     int64_t row = static_cast<int64_t>(blockIdx.x / a.cluster) * groups + group;
@@ -166,6 +189,7 @@ __global__ void __launch_bounds__(kMostWarps * 32) rms_norm_kernel(RmsArgs a) {
         }
         const bool beyond = !(total <= 1e38f) || (total < 1e-27f && a.eps < 1e-18f);
         if (L < 32 ? __any_sync(0xffffffffu, beyond) : beyond) {       // squares beyond fp32's range: the row times a power of two, and eps its square
+            row_sum.agree();
             if (beyond) scale = total < 1.f ? 0x1p80f : 0x1p-80f;
             eps = eps * scale * scale;
             squares = 0.f;
@@ -190,8 +214,7 @@ __global__ void __launch_bounds__(kMostWarps * 32) rms_norm_kernel(RmsArgs a) {
             out.store(static_cast<T *>(a.y) + row * a.y_row + c0, on ? left : 0);
         }
     }
-    // a CTA's slots are written by its peers: it may not end before they have
-    if (a.cluster > 1) cluster_barrier();
+    row_sum.finish();
 }
 
 // x: s; y: dx (strides x_row); residual: dy (y_row); dsum (r_row); ws: partial sums of dgamma, [CTA][C], clusters counting as one CTA
@@ -223,7 +246,7 @@ __global__ void __launch_bounds__((ASYNC ? grad_warps(E) : kMostWarps) * 32) rms
     const int first = L < 32 ? 0 : static_cast<int>(rank) * a.warps * 32 * E;          // column of the CTA
     const int c0 = first + (L < 32 ? 0 : warp % a.warps * 32 * E), left = a.C - c0;
     const int covered = L < 32 ? L * E : a.warps * 32 * E;
-    RowSum<L> row_sum{slots, a.warps, a.cluster, group, rank, 0};
+    RowSum<L> row_sum{slots, a, a.warps, a.cluster, group, rank, 0, 1};
     row_sum.clear();
     const int64_t step = static_cast<int64_t>(gridDim.x / a.cluster) * groups;
     int64_t row = static_cast<int64_t>(blockIdx.x / a.cluster) * groups + group;
@@ -376,7 +399,7 @@ __global__ void __launch_bounds__((ASYNC ? grad_warps(E) : kMostWarps) * 32) rms
         for (int k = 0; k < sets; ++k) v += sums[k * covered + c];
         part[c] = v;
     }
-    if (a.cluster > 1) cluster_barrier();
+    row_sum.finish();
 }
 
 // dgamma = the partial sums of 32 columns per CTA, added in a fixed order: warp w takes parts w, w + 32, ..., whose loads are all in flight
@@ -459,6 +482,7 @@ cudaError_t launch_rms_norm(const RmsShape &s, const RmsCall &c, cudaStream_t st
     a.scales_at = m.scales_at; a.col_tiles = static_cast<int>(m.col_tiles); a.groups = static_cast<int>(m.groups);
     const RmsPlan p = plan_forward(s.C, c.rows);
     a.warps = p.warps; a.cluster = p.cluster;
+    a.status = c.wait.status; a.spin_limit = c.wait.spin_limit ? c.wait.spin_limit : kSpinLimit; a.test_skip = c.wait.test_skip;
     const int width = strip_width(s.dtype, {c.x, c.residual, c.sum, c.y}, {s.x_row, c.residual || c.sum ? s.r_row : 0, c.y ? s.y_row : 0});
     return by_strip(s.dtype, width, [&](auto t, auto v) {
         return by_columns(p, [&](auto e, auto l) {
@@ -501,6 +525,7 @@ cudaError_t launch_rms_grad(const RmsShape &s, const RmsGradCall &c, cudaStream_
     a.rows = c.rows; a.x_row = s.x_row; a.r_row = s.r_row; a.y_row = s.y_row; a.C = s.C;
     const RmsPlan p = plan_backward(s.C, c.rows, s.dtype);
     a.warps = p.warps; a.cluster = p.cluster;
+    a.status = c.wait.status; a.spin_limit = c.wait.spin_limit ? c.wait.spin_limit : kSpinLimit; a.test_skip = c.wait.test_skip;
     const int width = strip_width(s.dtype, {c.s, c.dy, c.dsum, c.dx}, {s.x_row, s.r_row, s.y_row});
     const int parts = p.grid / p.cluster;              // (a part alone is dgamma itself)
     if (parts == 1) a.ws = c.dgamma;
