@@ -123,6 +123,10 @@ constexpr int kGatedUnitFloats = 256 * 256; // partial sums of a (tile, split) u
 constexpr int kGatedUnits = 2;              // such units that a call may need, per pair of SMs (see plan_gated_gradient)
 struct GatedWork {                          // a handle's buffers
     void *dgu;                              // [max_rows][2 Fp]: dg, du in the handle's type, Fp = F rounded up to 64; nullptr without gradients
+    void *by_column;                        // half: the same for dwg and dwu (see gated_aux.cu); else nullptr
+    uint32_t *row_top, *column_top;         // half: bits of the largest magnitudes, [max_rows] and [2 Fp], in one buffer of `tops` words, zeros between calls
+    float *row_unscale, *column_unscale;    // half: what undoes the scales, likewise
+    int64_t tops;
     float *partial;
     int *status;
 };
@@ -141,8 +145,8 @@ int pairs_most();                           // pairs of CTAs that run at a time
 cudaError_t prepare_gated();
 cudaError_t launch_gated_forward(const GatedShape &s, const GatedCall &c, const GatedWork &w, cudaStream_t st, int *launches);
 cudaError_t launch_gated_gradient(const GatedShape &s, const GatedCall &c, const GatedWork &w, cudaStream_t st, int *launches);   // from dgu
-// In front of them, one launch: K columns of 16-bit rows to rows `to_row` apart, zeros behind them (rows = 0: nothing to pack), and, where dgu is not
-// nullptr, dgu from gu [rows][2 F] and dh
+// In front of them: K columns of 16-bit rows to rows `to_row` apart, zeros behind them (rows = 0: nothing to pack), and, where there are slopes, dg and du from
+// gu [rows][2 F] and dh
 // copies > 0: as many copies of all rows, copy i shifted by shift[i] columns, zeros in front
 struct GatedPack {
     const void *from;
@@ -154,6 +158,17 @@ struct GatedPack {
 inline int gated_shift(const void *base, int64_t w_row, int phase) {                   // elements between a row and the 16-byte unit in which it begins
     return static_cast<int>((reinterpret_cast<uintptr_t>(base) + static_cast<uintptr_t>(phase) * w_row * 2) % 16 / 2);
 }
-cudaError_t launch_gated_operands(const GatedShape &s, const GatedPack (&packs)[3], const void *gu, const void *dh, void *dgu, int64_t rows, cudaStream_t st);
+struct GatedSlopes {
+    const void *gu, *dh;
+    void *dgu, *by_column;                  // half: either may be nullptr
+    uint32_t *row_top, *column_top;         // half
+    float *row_unscale, *column_unscale;
+};
+cudaError_t launch_gated_operands(const GatedShape &s, const GatedPack (&packs)[3], const GatedSlopes *slopes, int64_t rows, cudaStream_t st, int *launches);
+// Half: the power of two that brings magnitudes whose largest has these bits (0: there is none) below 2^15, and what undoes it.  (Magnitudes below 2^-100, whose
+// gradients are below half's range whatever they are multiplied with, are taken as 2^-100, so that both factors are normal.)
+constexpr uint32_t kLeastTop = 27, kMostTop = 240;
+__device__ __forceinline__ float gated_scale(uint32_t top) { return __uint_as_float((254 + 14 - min(max(top >> 23, kLeastTop), kMostTop)) << 23); }
+__device__ __forceinline__ float gated_unscale(uint32_t top) { return __uint_as_float((min(max(top >> 23, kLeastTop), kMostTop) - 14) << 23); }
 
 }  // namespace patdnn

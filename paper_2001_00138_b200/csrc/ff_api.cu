@@ -59,6 +59,9 @@ struct patdnn_gated_s {
     int test_skip_load = 0;
     ~patdnn_gated_s() {
         cudaFree(w.dgu);
+        cudaFree(w.by_column);
+        cudaFree(w.row_top);
+        cudaFree(w.row_unscale);
         cudaFree(w.partial);
         cudaFree(w.status);
         cudaFree(x);
@@ -158,24 +161,26 @@ bool operand_aligned(const void *p, int64_t row) { return aligned(p, copies_as_i
 int64_t packed_row(int64_t K) { return (K + 7) / 8 * 8; }
 
 // x and the weights of a call as the products read them (those that read_x and read_w name): packed first, where they cannot be copied as they lie.
-// gu, dh: the gradient's; or nullptr
-int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu, const void *gu, const void *dh, int64_t rows, bool read_x, bool read_w, GatedCall &c,
-                   cudaStream_t st) {
+// slopes: the gradient's; or nullptr
+int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu, const GatedSlopes *slopes, int64_t rows, bool read_x, bool read_w, GatedCall &c, cudaStream_t st) {
     const GatedShape &s = h->s;
     c.x = x; c.wg = wg; c.wu = wu; c.x_row = s.x_row; c.w_row = s.w_row; c.rows = rows;
     c.spin_limit = h->spin_limit; c.test_skip_load = h->test_skip_load;
     const int64_t row = packed_row(s.K);
     GatedPack packs[3] = {};
+    int n = 0;
+    cudaError_t e;
     // Few rows: a copy of x per phase instead of packed weights, as long as those are fewer rows (8 x 6899 -> 4222: 26 us, 80 packed; 128 x 1001 -> 1001:
     // 9.9 and 10.2; 128 x 6899 -> 700: 25.5 and 20.2)
     const int phases = gated_phases(s.w_row);
-    if (h->shifted && !gu && rows <= kPhasedRows && phases <= s.F && s.K + kMostPhases <= phases * s.w_row && phases * rows <= s.F && gated_shift(wg, s.w_row, 0) == gated_shift(wu, s.w_row, 0)) {
+    if (h->shifted && !slopes && rows <= kPhasedRows && phases <= s.F && s.K + kMostPhases <= phases * s.w_row && phases * rows <= s.F && gated_shift(wg, s.w_row, 0) == gated_shift(wu, s.w_row, 0)) {
         packs[0] = {x, h->shifted, rows, s.x_row, gated_phased_row(s.K), phases, {}};
         for (int j = 0; j < phases; ++j) packs[0].shift[j] = static_cast<uint8_t>(gated_shift(wg, s.w_row, j));
         c.x = h->shifted;
         c.x_row = gated_phased_row(s.K);
         c.phases = phases;
-        return launched(launch_gated_operands(s, packs, nullptr, nullptr, nullptr, rows, st), 1, "gated block operands launch");
+        e = launch_gated_operands(s, packs, nullptr, rows, st, &n);
+        return launched(e, n, "gated block operands launch");
     }
     if (h->x && read_x) {
         packs[0] = {x, h->x, rows, s.x_row, row, 0, {}};
@@ -190,8 +195,9 @@ int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu
         c.wu = second;
         c.w_row = row;
     }
-    if (!h->x && !h->weights && !gu) return PATDNN_OK;
-    return launched(launch_gated_operands(s, packs, gu, dh, gu ? h->w.dgu : nullptr, rows, st), 1, "gated block operands launch");
+    if (!h->x && !h->weights && !slopes) return PATDNN_OK;
+    e = launch_gated_operands(s, packs, slopes, rows, st, &n);
+    return launched(e, n, "gated block operands launch");
 }
 
 }  // namespace
@@ -408,13 +414,24 @@ int patdnn_gated_create(const patdnn_gated_desc *desc, patdnn_gated *out) {
     h->s = s;
     h->max_rows = desc->max_rows;
     const size_t row = static_cast<size_t>(packed_row(s.K));
-    uint16_t *dgu = nullptr, *x = nullptr, *weights = nullptr, *shifted = nullptr;
+    uint16_t *dgu = nullptr, *by_column = nullptr, *x = nullptr, *weights = nullptr, *shifted = nullptr;
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = allocate(&h->w.partial, static_cast<size_t>(pairs_most()) * kGatedUnits * kGatedUnitFloats);
     if (e == cudaSuccess) e = allocate(&h->w.status, 4);
     if (e == cudaSuccess) e = cudaMemset(h->w.status, 0, 16);
     if (e == cudaSuccess && desc->grad) e = allocate(&dgu, static_cast<size_t>(desc->max_rows) * 2 * gated_padded(s.F));
     h->w.dgu = dgu;
+    if (e == cudaSuccess && desc->grad && s.dtype == PATDNN_F16) {
+        e = allocate(&by_column, static_cast<size_t>(desc->max_rows) * 2 * gated_padded(s.F));
+        h->w.by_column = by_column;
+        const size_t rows = (static_cast<size_t>(desc->max_rows) + 3) / 4 * 4;          // (columns are read 16 bytes at a time)
+        h->w.tops = static_cast<int64_t>(rows) + 2 * gated_padded(s.F);
+        if (e == cudaSuccess) e = allocate(&h->w.row_top, static_cast<size_t>(h->w.tops));
+        if (e == cudaSuccess) e = cudaMemset(h->w.row_top, 0, static_cast<size_t>(h->w.tops) * sizeof(uint32_t));
+        if (e == cudaSuccess) e = allocate(&h->w.row_unscale, static_cast<size_t>(h->w.tops));
+        h->w.column_top = h->w.row_top + rows;
+        h->w.column_unscale = h->w.row_unscale + rows;
+    }
     if (e == cudaSuccess && !copies_as_it_lies(s.x_row)) e = allocate(&x, static_cast<size_t>(desc->max_rows) * row);
     h->x = x;
     if (e == cudaSuccess && !copies_as_it_lies(s.w_row)) e = allocate(&weights, 2 * static_cast<size_t>(s.F) * row);
@@ -440,7 +457,7 @@ int patdnn_gated_run(patdnn_gated h, const void *x, const void *wg, const void *
     if (const int rc = on_device(h->device)) return rc;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     GatedCall c{};
-    if (const int rc = gated_operands(h, x, wg, wu, nullptr, nullptr, rows, true, true, c, st)) return rc;
+    if (const int rc = gated_operands(h, x, wg, wu, nullptr, rows, true, true, c, st)) return rc;
     c.h = hidden; c.gu = gu;
     int n = 0;
     const cudaError_t e = launch_gated_forward(s, c, h->w, st, &n);
@@ -466,7 +483,12 @@ int patdnn_gated_grad(patdnn_gated h, const void *x, const void *wg, const void 
     }
     if (!dx && !dwg) return PATDNN_OK;
     GatedCall c{};
-    if (const int rc = gated_operands(h, x, wg, wu, gu, dh, rows, dwg != nullptr, dx != nullptr, c, st)) return rc;
+    GatedSlopes slopes{gu, dh, h->w.dgu, nullptr, h->w.row_top, h->w.column_top, h->w.row_unscale, h->w.column_unscale};
+    if (s.dtype == PATDNN_F16) {
+        if (!dx) slopes.dgu = nullptr;
+        if (dwg) slopes.by_column = h->w.by_column;
+    }
+    if (const int rc = gated_operands(h, x, wg, wu, &slopes, rows, dwg != nullptr, dx != nullptr, c, st)) return rc;
     c.dx = dx; c.dwg = dwg; c.dwu = dwu;
     int n = 0;
     const cudaError_t e = launch_gated_gradient(s, c, h->w, st, &n);

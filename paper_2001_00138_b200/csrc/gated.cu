@@ -40,6 +40,7 @@ struct Product {
     int units;                                         // tiles times splits
     int slot;                                          // of its first unit among the partial sums
     int band;                                          // tiles of rows to a band
+    const float *unscale;                              // half, gradient: of a row of the output; weights: those of the up projection are f_padded further on
 };
 // Pair q of P takes the units q, q + P, ... of the first product, then of the second those from more[q] to more[q + 1], which even the pairs out, and
 // the units more[P] + q, more[P] + q + P, ..., `common` of them: what runs at a time lies together, as the bands of tiles want it.
@@ -48,6 +49,8 @@ struct GatedParams {
     void *gu;                                          // forward: both projections, or nullptr
     int stages;
     int f_padded;                                      // columns from dg to du
+    uint32_t *tops;                                    // half, gradient: words that are cleared for the next call
+    int64_t top_words;
     float *partial;
     int *status;
     uint32_t spin_limit;
@@ -281,6 +284,8 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
         if (leader && !ok) commit_pair(own_done + 8 * (last & 1));
         __syncwarp();
         if (last >= 0) mbar_wait(done + 8 * (last & 1), (last >> 1) & 1, ctx, 125);
+    } else if (GRAD && std::is_same<T, __half>::value && warp == 3) {
+        for (int64_t i = blockIdx.x * 32 + lane; i < p.top_words; i += gridDim.x * 32) p.tops[i] = 0;
     } else if (warp >= 4) {
         const int e = warp - 4, quadrant = e & 3, quarter = e >> 2;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quadrant * 32) << 16);
@@ -292,9 +297,11 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
             int mt, nt;
             banded(tile, q.band, q.m_tiles, q.n_tiles, mt, nt);
             T *out = static_cast<T *>(q.out0);
+            int64_t factors = 0;
             if (GRAD && which == 1 && mt >= q.f_blocks) {
                 mt -= q.f_blocks;
                 out = static_cast<T *>(q.out1);
+                factors = p.f_padded;
             }
             const int64_t row0 = static_cast<int64_t>(mt) * 256 + rank * 128 + quadrant * 32;
             const int rows_left = static_cast<int>(max(static_cast<int64_t>(-1), min(static_cast<int64_t>(32), q.rows - row0)));
@@ -305,10 +312,21 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
             const uint32_t from = lanes + buf * 256 + quarter * (GRAD ? 64 : 32);
             tmem_ld32_async(from, reinterpret_cast<uint32_t *>(v[0]));
             tmem_ld32_async(from + (GRAD ? 32 : 128), reinterpret_cast<uint32_t *>(v[1]));
+            float factor = 1.f;
+            if constexpr (GRAD && std::is_same<T, __half>::value)
+                if (lane < rows_left) factor = q.unscale[factors + row0 + lane];
             asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
             tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive_pair(drained0 + 8 * buf);
+            if constexpr (GRAD && std::is_same<T, __half>::value) {
+#pragma unroll
+                for (int i = 0; i < 64; i += 2) {      // (in pairs: one by one they spill)
+                    const float2 two = split(mul_(pair_of(v[i >> 5][i & 31], v[i >> 5][(i & 31) + 1]), pair_of(factor, factor)));
+                    v[i >> 5][i & 31] = two.x;
+                    v[i >> 5][(i & 31) + 1] = two.y;
+                }
+            }
             auto put = [&](const float (&w)[32], T *base, int64_t ld, int col, int left) {
                 const uint64_t places = reinterpret_cast<uintptr_t>(base) | static_cast<uint64_t>(ld * sizeof(T));
                 const int aligned = places % 16 == 0 ? 16 : places % 4 == 0 ? 4 : 2;
@@ -802,10 +820,11 @@ cudaError_t launch_gated_gradient(const GatedShape &s, const GatedCall &c, const
     const int64_t dgu_row = 2 * static_cast<int64_t>(padded);
     GatedMaps maps{};
     GatedParams p{};
-    p.f_padded = padded;
+    p.f_padded = padded; p.tops = w.row_top; p.top_words = w.tops;
     Product &x = p.of[0] = product_of(plan[0], 0), &dw = p.of[1] = product_of(plan[1], plan[0].splits > 1 ? x.units : 0);
     cudaError_t e = cudaSuccess;
     if (c.dx) {
+        x.unscale = w.row_unscale;
         x.out0 = c.dx; x.rows = c.rows; x.ld = s.x_row; x.cols = s.K; x.f_blocks = padded / 64;
         x.box_rows = static_cast<int>(std::min<int64_t>(128, c.rows));
         e = make_map(&maps.a, s.dtype, w.dgu, c.rows, dgu_row, dgu_row, x.box_rows);
@@ -813,8 +832,9 @@ cudaError_t launch_gated_gradient(const GatedShape &s, const GatedCall &c, const
         if (e == cudaSuccess) e = make_map(&maps.b1, s.dtype, c.wu, s.F, s.K, c.w_row, 64);
     }
     if (c.dwg && e == cudaSuccess) {
+        dw.unscale = w.column_unscale;
         dw.out0 = c.dwg; dw.out1 = c.dwu; dw.rows = s.F; dw.ld = s.w_row; dw.cols = s.K; dw.f_blocks = dw.m_tiles / 2;
-        e = make_map(&maps.wa, s.dtype, w.dgu, c.rows, dgu_row, dgu_row, 64);
+        e = make_map(&maps.wa, s.dtype, w.by_column ? w.by_column : w.dgu, c.rows, dgu_row, dgu_row, 64);
         if (e == cudaSuccess) e = make_map(&maps.wb, s.dtype, c.x, c.rows, s.K, c.x_row, 64);
     }
     if (e != cudaSuccess) return e;
