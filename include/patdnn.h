@@ -472,7 +472,7 @@ PATDNN_API int patdnn_linear8_free(patdnn_linear8 h);
  * more.  F16: a power of two per row (for dx) and per column (for dwg, dwu) of dg and du keeps them in the type's range, whatever dh, g and u
  * multiply to; what is below 2^-29 of the largest of its row or column loses bits, what is below 2^-40 is taken as 0.  At g = 0 ReLU passes no
  * gradient.  A row of x that is not finite spoils its row of h alone.  Where g or u leaves the range of the type, gu holds an infinity; SiLU has its
- * limits there (0 and slope 0 at -infinity, slope 1 at infinity).
+ * limits there (0 and slope 0 at -infinity, slope 1 at infinity).  Nothing passes where dh or the slope is 0, whatever gu holds there.
  *   desc       copied; rows of consecutive elements; strides in elements, 0 = dense: x_row of x and dx, w_row of the four weight tensors,
  *              h_row of h and dh; gu is dense, [rows][2][F], g before u.  grad != 0: gradients will be asked for (more workspace)
  *   patdnn_gated_run       gu DEVICE or NULL; hidden and gu overlap no input

@@ -156,3 +156,42 @@ def test_calls_of_one_handle_do_not_leave_magnitudes_behind():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(c.dx, fresh.dx) and torch.equal(c.dwg, fresh.dwg) and torch.equal(c.dwu, fresh.dwu), scale
+
+
+@pytest.mark.parametrize("name", ACTS)
+@pytest.mark.parametrize("M, K, F", [(1, 64, 8), (40, 200, 333), (300, 136, 264)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_nothing_flows_through_a_stored_infinity_where_dh_or_the_slope_is_zero(M, K, F, dtype, name):
+    """gu holds an infinity where g or u left the type's range: a number that is too large for it, whose product with a dh of 0 (a masked row, an output
+    that nobody used), or with the slope of a shut gate, is 0 and not NaN.  Beside them everything is as with any finite number there."""
+    import torch
+    c = Case(M, K, F, dtype, name, False, seed=4)
+    c.forward()
+    g = torch.Generator(device="cuda").manual_seed(M)
+    masked = torch.rand(M, F, generator=g, device="cuda") < 0.3
+    shut = torch.rand(M, F, generator=g, device="cuda") < 0.2 if name != "none" else torch.zeros_like(masked)
+    c.dh.masked_fill_(masked, 0)
+    gate, up = c.gu[:, 0], c.gu[:, 1]
+    if name != "none":
+        gate.masked_fill_(shut, float("-inf"))
+    c.backward()
+    want = [t.clone() for t in (c.dx, c.dwg, c.dwu)]
+    assert all(torch.isfinite(t).all() for t in want)
+    sign = torch.where(torch.rand(M, F, generator=g, device="cuda") < 0.5, 1.0, -1.0)
+    up.copy_(torch.where(masked | shut, sign * float("inf"), up.float()))
+    gate.copy_(torch.where(masked & ~shut, sign * float("inf"), gate.float()))
+    c.backward()
+    for got, w in zip((c.dx, c.dwg, c.dwu), want):
+        assert torch.equal(got, w)
+    # whatever else a masked place holds
+    up.masked_fill_(masked, float("nan"))
+    gate.masked_fill_(masked, float("nan"))
+    c.backward()
+    for got, w in zip((c.dx, c.dwg, c.dwu), want):
+        assert torch.equal(got, w)
+    # a NaN that a gradient reaches: its row of dx and its row of dwg are NaN, others are as before
+    up[M // 2, F // 3], gate[M // 2, F // 3], c.dh[M // 2, F // 3] = float("nan"), 1.0, 1.0
+    c.backward()
+    rows, cols = torch.arange(M, device="cuda") != M // 2, torch.arange(F, device="cuda") != F // 3
+    assert torch.isnan(c.dwg[F // 3]).all() and torch.isnan(c.dx[M // 2]).all() and torch.isfinite(c.dwu).all()
+    assert torch.equal(c.dx[rows], want[0][rows]) and torch.equal(c.dwg[cols], want[1][cols]) and torch.equal(c.dwu[cols], want[2][cols])
