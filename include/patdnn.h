@@ -467,7 +467,8 @@ PATDNN_API int patdnn_linear8_free(patdnn_linear8 h);
  * Gated feed-forward block (addition): both projections, the activation and the product in one kernel, and their gradients.
  *   g = x wg^T, u = x wu^T, h = act(g) * u                          x [rows][K], wg and wu [F][K], h [rows][F]
  *   dg = dh * u * act'(g), du = dh * act(g);  dx = dg wg + du wu, dwg = dg^T x, dwu = du^T x
- * Sums are fp32 on the tensor cores, in a fixed order; g and u stay in fp32 for h, which is rounded once.  For the gradient the run stores
+ * Sums are fp32 on the tensor cores, in an order that depends on sizes, strides and where wg and wu begin in a 16-byte unit, and on nothing else; g and u
+ * stay in fp32 for h, which is rounded once.  For the gradient the run stores
  * g and u rounded to the tensors' type (gu), and dg and du are rounded to it as operands of the products; dx, dwg and dwu are rounded once
  * more.  F16: a power of two per row (for dx) and per column (for dwg, dwu) of dg and du keeps them in the type's range, whatever dh, g and u
  * multiply to; what is below 2^-29 of the largest of its row or column loses bits, what is below 2^-40 is taken as 0.  At g = 0 ReLU passes no
@@ -504,7 +505,10 @@ PATDNN_API int patdnn_gated_grad(patdnn_gated h, const void *x, const void *wg, 
 PATDNN_API int patdnn_gated_check(patdnn_gated h);
 PATDNN_API int patdnn_gated_debug_wait(patdnn_gated h, uint32_t polls, int32_t skip_load_iteration);
 
-/* How a product of the block is launched (inspection; touches no device).  product: 0 for h, 1 for dx, 2 for dwg and dwu.  Errors: E_NULL, E_SHAPE. */
+/* How a product of the block is launched (inspection; touches no device).  product: 0 for h, 1 for dx, 2 for dwg and dwu.  patdnn_gated_plan: of weights whose
+ * rows are whole 16-byte units apart; patdnn_gated_plan_strided: of weights w_row elements apart (0 = whole units).  Where those are not whole units, few rows
+ * take weights that begin at the same place of a 16-byte unit as they lie, which is what is reported, and others packed, as patdnn_gated_plan says; the
+ * sums of the two are added in different orders.  Errors: E_NULL, E_SHAPE. */
 typedef struct {
     int32_t row_tiles, column_tiles;    /* tiles of the product */
     int32_t blocks;                     /* of 64 along the summed dimension */
@@ -516,6 +520,7 @@ typedef struct {
     int32_t few_rows;                   /* 1: the kernel that streams the weights, tiles of 128 rows and 64 outputs; 0: pairs of CTAs */
 } patdnn_gated_plan_info;
 PATDNN_API int patdnn_gated_plan(int32_t F, int32_t K, int64_t rows, int32_t product, patdnn_gated_plan_info *info);
+PATDNN_API int patdnn_gated_plan_strided(int32_t F, int32_t K, int64_t rows, int32_t product, int64_t w_row, patdnn_gated_plan_info *info);
 PATDNN_API int patdnn_gated_free(patdnn_gated h);
 
 /* Number of this library's kernels launched by the process since the last reset (addition, for reports). */

@@ -37,7 +37,7 @@ EXPORTED_SYMBOLS = (
     "patdnn_mx8_bytes", "patdnn_mx8_quantize", "patdnn_mx8_dequantize",
     "patdnn_linear8_encode", "patdnn_linear8_run", "patdnn_linear8_run_mx8", "patdnn_linear8_check", "patdnn_linear8_plan",
     "patdnn_linear8_debug_wait", "patdnn_linear8_free",
-    "patdnn_gated_create", "patdnn_gated_run", "patdnn_gated_grad", "patdnn_gated_check", "patdnn_gated_plan", "patdnn_gated_debug_wait",
+    "patdnn_gated_create", "patdnn_gated_run", "patdnn_gated_grad", "patdnn_gated_check", "patdnn_gated_plan", "patdnn_gated_plan_strided", "patdnn_gated_debug_wait",
     "patdnn_gated_free",
 )
 
@@ -170,6 +170,7 @@ def load() -> ctypes.CDLL:
     lib.patdnn_gated_grad.argtypes = [vp] * 9 + [i64, vp]
     lib.patdnn_gated_check.argtypes = [vp]
     lib.patdnn_gated_plan.argtypes = [i32, i32, i64, i32, ctypes.POINTER(_GatedPlan)]
+    lib.patdnn_gated_plan_strided.argtypes = [i32, i32, i64, i32, i64, ctypes.POINTER(_GatedPlan)]
     lib.patdnn_gated_debug_wait.argtypes = [vp, ctypes.c_uint32, i32]
     lib.patdnn_gated_free.argtypes = [vp]
     lib.patdnn_launch_count.restype = ctypes.c_int64
@@ -638,10 +639,11 @@ class Gated:
             pass
 
 
-def gated_plan(F: int, K: int, rows: int, product: int = 0) -> dict:
-    """patdnn_gated_plan: how a product of the gated block is launched (0: h, 1: dx, 2: dwg and dwu); needs no device."""
+def gated_plan(F: int, K: int, rows: int, product: int = 0, w_row: int = 0) -> dict:
+    """patdnn_gated_plan_strided: how a product of the gated block is launched (0: h, 1: dx, 2: dwg and dwu), its weights ``w_row`` elements apart (0 =
+    whole 16-byte units); needs no device."""
     info = _GatedPlan()
-    _check(load().patdnn_gated_plan(F, K, rows, product, ctypes.byref(info)), "patdnn_gated_plan")
+    _check(load().patdnn_gated_plan_strided(F, K, rows, product, w_row, ctypes.byref(info)), "patdnn_gated_plan_strided")
     return {n: int(getattr(info, n)) for n, _ in info._fields_}
 
 

@@ -160,6 +160,13 @@ bool copies_as_it_lies(int64_t row) { return row % 8 == 0; }           // rows o
 bool operand_aligned(const void *p, int64_t row) { return aligned(p, copies_as_it_lies(row) ? 16 : 2); }
 int64_t packed_row(int64_t K) { return (K + 7) / 8 * 8; }
 
+// Few rows, weights whose rows are not whole 16-byte units apart: a copy of x per phase instead of packed weights, as long as those are fewer rows (8 x 6899 ->
+// 4222: 26 us, 74 packed; 128 x 1001 -> 1001: 9.9 and 10.2; 128 x 6899 -> 700: 25.5 and 20.2).  0: not this way; else the phases.
+int phases_of(int F, int K, int64_t w_row, int64_t rows) {
+    const int phases = gated_phases(w_row);
+    return phases > 1 && rows <= kPhasedRows && phases <= F && K + kMostPhases <= phases * w_row && phases * rows <= F ? phases : 0;
+}
+
 // x and the weights of a call as the products read them (those that read_x and read_w name): packed first, where they cannot be copied as they lie.
 // slopes: the gradient's; or nullptr
 int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu, const GatedSlopes *slopes, int64_t rows, bool read_x, bool read_w, GatedCall &c, cudaStream_t st) {
@@ -170,10 +177,8 @@ int gated_operands(patdnn_gated h, const void *x, const void *wg, const void *wu
     GatedPack packs[3] = {};
     int n = 0;
     cudaError_t e;
-    // Few rows: a copy of x per phase instead of packed weights, as long as those are fewer rows (8 x 6899 -> 4222: 26 us, 80 packed; 128 x 1001 -> 1001:
-    // 9.9 and 10.2; 128 x 6899 -> 700: 25.5 and 20.2)
-    const int phases = gated_phases(s.w_row);
-    if (h->shifted && !slopes && rows <= kPhasedRows && phases <= s.F && s.K + kMostPhases <= phases * s.w_row && phases * rows <= s.F && gated_shift(wg, s.w_row, 0) == gated_shift(wu, s.w_row, 0)) {
+    const int phases = slopes ? 0 : phases_of(s.F, s.K, s.w_row, rows);
+    if (phases && gated_shift(wg, s.w_row, 0) == gated_shift(wu, s.w_row, 0)) {
         packs[0] = {x, h->shifted, rows, s.x_row, gated_phased_row(s.K), phases, {}};
         for (int j = 0; j < phases; ++j) packs[0].shift[j] = static_cast<uint8_t>(gated_shift(wg, s.w_row, j));
         c.x = h->shifted;
@@ -496,13 +501,19 @@ int patdnn_gated_grad(patdnn_gated h, const void *x, const void *wg, const void 
 }
 
 int patdnn_gated_plan(int32_t F, int32_t K, int64_t rows, int32_t product, patdnn_gated_plan_info *info) {
+    return patdnn_gated_plan_strided(F, K, rows, product, 0, info);
+}
+
+int patdnn_gated_plan_strided(int32_t F, int32_t K, int64_t rows, int32_t product, int64_t w_row, patdnn_gated_plan_info *info) {
     if (!info) return PATDNN_E_NULL;
+    if (w_row && (w_row < K || w_row > (int64_t(1) << 31))) return PATDNN_E_SHAPE;
     if (!size_ok(F, K) || F < 1 || F > kMostColumns || !size_ok(rows, K) || !size_ok(rows, F) || rows < 1 || gated_too_large(rows, F, K) || product < 0 ||
         product > 2)
         return PATDNN_E_SHAPE;
     GatedPlan gradient[2];
     plan_gated_gradient(F, K, rows, true, true, gradient);
-    const GatedPlan p = product ? gradient[product - 1] : plan_gated_forward(F, K, rows);
+    const int phases = product || !w_row ? 0 : phases_of(F, K, w_row, rows);
+    const GatedPlan p = product ? gradient[product - 1] : phases ? plan_gated_phased(F, K, rows, phases) : plan_gated_forward(F, K, rows);
     *info = patdnn_gated_plan_info{};
     info->row_tiles = p.m_tiles; info->column_tiles = p.n_tiles; info->blocks = p.k_blocks; info->splits = p.splits; info->blocks_per_split = p.per_split;
     info->grid = p.grid; info->stages = p.stages; info->smem_bytes = p.smem;
