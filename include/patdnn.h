@@ -470,8 +470,8 @@ PATDNN_API int patdnn_linear8_free(patdnn_linear8 h);
  * Sums are fp32 on the tensor cores, in an order that depends on sizes, strides and where wg and wu begin in a 16-byte unit, and on nothing else; g and u
  * stay in fp32 for h, which is rounded once.  For the gradient the run stores
  * g and u rounded to the tensors' type (gu), and dg and du are rounded to it as operands of the products; dx, dwg and dwu are rounded once
- * more.  F16: a power of two per row (for dx) and per column (for dwg, dwu) of dg and du keeps them in the type's range, whatever dh, g and u
- * multiply to; what is below 2^-29 of the largest of its row or column loses bits, what is below 2^-40 is taken as 0.  At g = 0 ReLU passes no
+ * more.  F16: rows (for dx) and columns (for dwg, dwu) of dg and du whose largest magnitude is not between 2^-3 and 2^15 are scaled by a power of two, so
+ * that they keep to the type's range whatever dh, g and u multiply to; what is below 2^-40 of the largest is taken as 0.  At g = 0 ReLU passes no
  * gradient.  A row of x that is not finite spoils its row of h alone.  Where g or u leaves the range of the type, gu holds an infinity; SiLU has its
  * limits there (0 and slope 0 at -infinity, slope 1 at infinity).  Nothing passes where dh or the slope is 0, whatever gu holds there.
  *   desc       copied; rows of consecutive elements; strides in elements, 0 = dense: x_row of x and dx, w_row of the four weight tensors,

@@ -123,7 +123,7 @@ constexpr int kGatedUnitFloats = 256 * 256; // partial sums of a (tile, split) u
 constexpr int kGatedUnits = 2;              // such units that a call may need, per pair of SMs (see plan_gated_gradient)
 struct GatedWork {                          // a handle's buffers
     void *dgu;                              // [max_rows][2 Fp]: dg, du in the handle's type, Fp = F rounded up to 64; nullptr without gradients
-    void *by_column;                        // half: the same for dwg and dwu (see gated_aux.cu); else nullptr
+    void *by_column;                        // half: a copy for dwg and dwu (see gated_aux.cu); else nullptr
     uint32_t *row_top, *column_top;         // half: bits of the largest magnitudes, [max_rows] and [2 Fp], in one buffer of `tops` words, zeros between calls
     float *row_unscale, *column_unscale;    // half: what undoes the scales, likewise
     int64_t tops;
@@ -165,10 +165,14 @@ struct GatedSlopes {
     float *row_unscale, *column_unscale;
 };
 cudaError_t launch_gated_operands(const GatedShape &s, const GatedPack (&packs)[3], const GatedSlopes *slopes, int64_t rows, cudaStream_t st, int *launches);
-// Half: the power of two that brings magnitudes whose largest has these bits (0: there is none) below 2^15, and what undoes it.  (Magnitudes below 2^-100, whose
-// gradients are below half's range whatever they are multiplied with, are taken as 2^-100, so that both factors are normal.)
-constexpr uint32_t kLeastTop = 27, kMostTop = 240;
-__device__ __forceinline__ float gated_scale(uint32_t top) { return __uint_as_float((254 + 14 - min(max(top >> 23, kLeastTop), kMostTop)) << 23); }
-__device__ __forceinline__ float gated_unscale(uint32_t top) { return __uint_as_float((min(max(top >> 23, kLeastTop), kMostTop) - 14) << 23); }
+// Half: whether magnitudes whose largest has these bits are scaled, the power of two that brings it between 2^14 and 2^15, and what undoes it.  (Magnitudes below
+// 2^-100, whose gradients are below half's range whatever they are multiplied with, are taken as 2^-100, so that both factors are normal.)
+__device__ __forceinline__ bool gated_scaled(uint32_t top) {
+    constexpr uint32_t kLeast = (127 - 3) << 23, kMost = (127 + 15) << 23, kInfinity = 0x7f800000u;
+    return (top - 1 < kLeast - 1) || (top >= kMost && top < kInfinity);
+}
+__device__ __forceinline__ uint32_t gated_top_field(uint32_t top) { return max(top >> 23, 27u); }
+__device__ __forceinline__ float gated_scale(uint32_t top) { return gated_scaled(top) ? __uint_as_float((254 + 14 - gated_top_field(top)) << 23) : 1.f; }
+__device__ __forceinline__ float gated_unscale(uint32_t top) { return gated_scaled(top) ? __uint_as_float((gated_top_field(top) - 14) << 23) : 1.f; }
 
 }  // namespace patdnn

@@ -5,10 +5,11 @@
 // rounded to the type of the products that read them, which take no wider operands at this rate: at most 2^-8 of each term for bf16 (2^-11 for half),
 // independent of one another, so that a product's relative error grows to about sqrt(2) times that of the result's own rounding.
 // Half: dg and du may leave its range where the gradients do not (dh = u = 300), or fall below it (dh = 1e-5, act(g) = 1e-3, summed over thousands of
-// rows).  They are multiplied by a power of two before they are rounded, which puts the largest finite magnitude of a row (for dx), or of a
-// column (for dwg, dwu), between 2^14 and 2^15, and the products' rows are divided by it in fp32: what is below 2^-29 of the largest loses bits, what is
-// below 2^-40 is 0.  It takes a pass for the magnitudes in front, and a copy of dg and du for either product (4096 x 8192: 53 and 96 us, where one copy
-// as it is takes 57).
+// rows).  dx is given a copy of them, dwg and dwu another, and the largest magnitudes of every row and column of them are found on the way.  Where that is between
+// 2^-3 and 2^15 the copies stay as they are: half's steps below 2^-14 are 2^-22 of it at most.  Any other row is then written once more into the one copy, any other
+// column into the other, times the power of two that puts the largest magnitude between 2^14 and 2^15 (what is below 2^-29 of it loses bits, what is below
+// 2^-40 is 0), and the products' rows are divided by it in fp32.  (4096 x 8192: 79 us for the first pass and 6 for the second; with one copy and no
+// magnitudes 57.  Finding the magnitudes first, and scaling all of both copies, 53 and 96.)
 #include <algorithm>
 
 #include "feed_forward.hpp"
@@ -23,7 +24,7 @@ constexpr int kJobs = 4;                               // three matrices to pack
 
 struct AuxJob {
     const void *x, *dh;                                // slopes: gu, dh
-    void *to, *by_column;                              // half: to scaled by rows and by_column by columns, or nullptr
+    void *to, *by_column;                              // half: the copies for dx and for dwg and dwu, or nullptr
     uint32_t *row_top, *column_top;
     float *row_unscale, *column_unscale;
     int64_t row, dh_row, to_row;                       // strides in elements
@@ -63,136 +64,106 @@ template <typename T> __device__ __forceinline__ uint32_t nonzero2(uint32_t pair
     if constexpr (std::is_same<T, __half>::value) return __hneu2_mask(*reinterpret_cast<const __half2 *>(&pair), __half2half2(__ushort_as_half(0)));
     else return __hneu2_mask(*reinterpret_cast<const __nv_bfloat162 *>(&pair), __bfloat162bfloat162(__ushort_as_bfloat16(0)));
 }
-// dg and du of 8 columns per lane of a row.
-template <typename T, bool ALIGNED, int ACT>
-__device__ __forceinline__ void slopes(const AuxJob &a, int64_t row, int c0, float (&dg)[8], float (&du)[8]) {
-    const int left = a.cols - c0;
-    Strip<T, 8, 8> sg, su, sd;
-    const T *g = static_cast<const T *>(a.x) + row * a.row + c0, *dh = static_cast<const T *>(a.dh) + row * a.dh_row + c0;
-    if constexpr (ALIGNED) {
-        sg.load(g, left);
-        su.load(g + a.cols, left);
-        sd.load(dh, left);
-    } else {
-        sg.load_any(g, left);
-        su.load_any(g + a.cols, left);
-        sd.load_any(dh, left);
-    }
-    // Nothing passes where dh is 0 or the slope is, whatever gu holds there: an infinity in it is a number too large for the type, and a masked row may hold
-    // anything.  (On packed pairs, and with selections: 3 us of 111 for 4096 x 8192; element by element 10.)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const uint32_t open = nonzero2<T>(sd.v[0].w[k]);
-        sg.v[0].w[k] &= open;
-        su.v[0].w[k] &= open;
-    }
-    float fd[8];
-    sg.widen_to(dg);
-    su.widen_to(du);
-    sd.widen_to(fd);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float g = dg[e], through = fd[e] * du[e];
-        if constexpr (ACT == PATDNN_ACT_RELU) {        // slope 0 at 0; a NaN passes
-            dg[e] = g > 0.f ? through : g <= 0.f ? 0.f : g;
-            du[e] = fd[e] * (g < 0.f ? 0.f : g);
-        } else if constexpr (ACT == PATDNN_ACT_SILU) {
-            const float s = sigmoid(g);                // at infinities (g left the range of the type) the limits: 0 and 0, or g and 1
-            const float act = s == 0.f ? 0.f : g * s, slope = s == 1.f ? 1.f : fmaf(act, 1.f - s, s);
-            dg[e] = s == 0.f ? 0.f : through * slope;
-            du[e] = fd[e] * act;
+// 8 columns per lane of a row of gu and dh.
+template <typename T> struct SlopeRow {
+    Strip<T, 8, 8> g, u, dh;
+    template <bool ALIGNED> __device__ __forceinline__ void load(const AuxJob &a, int64_t row, int c0) {
+        const int left = a.cols - c0;
+        const T *from = static_cast<const T *>(a.x) + row * a.row + c0, *of_h = static_cast<const T *>(a.dh) + row * a.dh_row + c0;
+        if constexpr (ALIGNED) {
+            g.load(from, left);
+            u.load(from + a.cols, left);
+            dh.load(of_h, left);
         } else {
-            dg[e] = through;
-            du[e] = fd[e] * g;
+            g.load_any(from, left);
+            u.load_any(from + a.cols, left);
+            dh.load_any(of_h, left);
         }
     }
-}
+    // d[0]: dg, d[1]: du
+    template <int ACT> __device__ __forceinline__ void slopes(float (&d)[2][8]) {
+        // Nothing passes where dh is 0 or the slope is, whatever gu holds there: an infinity in it is a number too large for the type, and a masked row may hold
+        // anything.  (On packed pairs, and with selections: 3 us of 111 for 4096 x 8192; element by element 10.)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t open = nonzero2<T>(dh.v[0].w[k]);
+            g.v[0].w[k] &= open;
+            u.v[0].w[k] &= open;
+        }
+        float fd[8];
+        g.widen_to(d[0]);
+        u.widen_to(d[1]);
+        dh.widen_to(fd);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float z = d[0][e], through = fd[e] * d[1][e];
+            if constexpr (ACT == PATDNN_ACT_RELU) {    // slope 0 at 0; a NaN passes
+                d[0][e] = z > 0.f ? through : z <= 0.f ? 0.f : z;
+                d[1][e] = fd[e] * (z < 0.f ? 0.f : z);
+            } else if constexpr (ACT == PATDNN_ACT_SILU) {
+                const float s = sigmoid(z);            // at infinities (g left the range of the type) the limits: 0 and 0, or g and 1
+                const float act = s == 0.f ? 0.f : z * s, slope = s == 1.f ? 1.f : fmaf(act, 1.f - s, s);
+                d[0][e] = s == 0.f ? 0.f : through * slope;
+                d[1][e] = fd[e] * act;
+            } else {
+                d[0][e] = through;
+                d[1][e] = fd[e] * z;
+            }
+        }
+    }
+};
 
-// A row; half: a.set rows
 template <typename T, bool ALIGNED, int ACT>
 __device__ __forceinline__ void store_slopes(const AuxJob &a, int64_t row, int c0) {
-    const int left = a.padded - c0, c = c0 + (threadIdx.x & 31) * 8;
-    if constexpr (!std::is_same<T, __half>::value) {
-        float dg[8], du[8];
-        slopes<T, ALIGNED, ACT>(a, row, c0, dg, du);
-        T *to = static_cast<T *>(a.to) + row * a.to_row + c0;
-        Strip<T, 8, 8> s;
-        s.narrow_from(dg);
-        s.store(to, left);
-        s.narrow_from(du);
-        s.store(to + a.padded, left);
-    } else {
-        Fv<8> of_column[2];
-        const bool columns = a.by_column && c < a.padded;
-        if (columns) {
+    SlopeRow<T> s;
+    float d[2][8];
+    s.template load<ALIGNED>(a, row, c0);
+    s.template slopes<ACT>(d);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint4 *top = reinterpret_cast<const uint4 *>(a.column_top + k * a.padded + c);
-                const uint4 lo = top[0], hi = top[1];
-                const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-                of_column[k] = Fv<8>::make([&](int e) { return gated_scale(w[e]); });
-                if (row == 0) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) a.column_unscale[k * a.padded + c + e] = gated_unscale(w[e]);
-                }
-            }
-        }
-        const int64_t last = min(row + a.set, a.rows);
-        for (; row < last; ++row) {
-            float d[2][8];
-            slopes<T, ALIGNED, ACT>(a, row, c0, d[0], d[1]);
-            const int64_t at = row * a.to_row + c0;
-            const uint32_t row_top = a.row_top[row];
-            const Fv<8> of_row = Fv<8>::all(gated_scale(row_top));
-            if (c == 0) a.row_unscale[row] = gated_unscale(row_top);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const Fv<8> v = Fv<8>::make([&](int e) { return d[k][e]; });
-                Strip<T, 8, 8> s;
-                if (a.to) {
-                    s.v[0] = narrow<T, 8>(v * of_row);
-                    s.store(static_cast<T *>(a.to) + at + k * a.padded, left);
-                }
-                if (columns) {
-                    s.v[0] = narrow<T, 8>(v * of_column[k]);
-                    s.store(static_cast<T *>(a.by_column) + at + k * a.padded, left);
-                }
-            }
-        }
+    for (int k = 0; k < 2; ++k) {
+        Strip<T, 8, 8> out;
+        out.narrow_from(d[k]);
+        out.store(static_cast<T *>(a.to) + row * a.to_row + k * a.padded + c0, a.padded - c0);
     }
 }
 
-// The largest magnitudes of dg and du, per row and per column of either, as bits (which are in their order; a NaN has none, and where one is an infinity all of
-// that row of the product is).  A CTA takes 256 columns; its warps take `rows`
-// rows each, four at a time, and join what they have of the columns.  Maxima do not depend on the order; the words are 0 before (the products clear them for
-// the next call).
+// Half: both copies as they are, and the largest magnitudes as bits (which are in their order; a NaN has none).  A CTA takes 256 columns; its warps take `rows` rows
+// each, two at a time, and join what they have of the columns.  Maxima do not depend on the order; the words are 0 before (the products clear them for the
+// next call).
 template <bool ALIGNED, int ACT>
-__global__ void __launch_bounds__(kWarps * 32, 3) gated_magnitudes_kernel(const __grid_constant__ AuxJob a, int rows) {
+__global__ void __launch_bounds__(kWarps * 32, 3) gated_slopes_kernel(const __grid_constant__ AuxJob a, int rows) {
+    constexpr int kTogether = 2;
     __shared__ __align__(16) uint32_t tops[2][kWarps][kColumns];
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t set = blockIdx.x / a.pieces, first = (set * kWarps + warp) * rows, last = min(first + rows, a.rows) - 1;
+    const int64_t set = blockIdx.x / a.pieces, first = (set * kWarps + warp) * rows, last = min(first + rows, a.rows);
     const int c0 = static_cast<int>(blockIdx.x - set * a.pieces) * kColumns;
     pdl_wait();
     float top[2][8] = {};
-    for (int64_t row = first; row <= last; row += 4) {
-        float of_row[4];
+    for (int64_t row = first; row < last; row += kTogether) {
+        SlopeRow<__half> s[kTogether];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float dg[8], du[8];
-            slopes<__half, ALIGNED, ACT>(a, min(row + k, last), c0, dg, du);           // (the last one again changes nothing)
-            of_row[k] = 0.f;
+        for (int k = 0; k < kTogether; ++k) s[k].load<ALIGNED>(a, min(row + k, last - 1), c0);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                top[0][e] = fmaxf(top[0][e], fabsf(dg[e]));
-                top[1][e] = fmaxf(top[1][e], fabsf(du[e]));
-                of_row[k] = fmaxf(of_row[k], fmaxf(fabsf(dg[e]), fabsf(du[e])));
+        for (int k = 0; k < kTogether; ++k) {
+            if (row + k >= last) break;
+            float d[2][8], of_row = 0.f;
+            s[k].slopes<ACT>(d);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    top[i][e] = fmaxf(top[i][e], fabsf(d[i][e]));
+                    of_row = fmaxf(of_row, fabsf(d[i][e]));
+                }
+                Strip<__half, 8, 8> out;
+                out.narrow_from(d[i]);
+                const int64_t at = (row + k) * a.to_row + i * a.padded + c0;
+                if (a.to) out.store(static_cast<__half *>(a.to) + at, a.padded - c0);
+                if (a.by_column) out.store(static_cast<__half *>(a.by_column) + at, a.padded - c0);
             }
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(of_row[k]));
-            if (lane == 0) atomicMax(a.row_top + min(row + k, last), most);
+            const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(of_row));
+            if (lane == 0) atomicMax(a.row_top + row + k, most);
         }
     }
 #pragma unroll
@@ -211,8 +182,58 @@ __global__ void __launch_bounds__(kWarps * 32, 3) gated_magnitudes_kernel(const 
     }
 }
 
+// Half: the rows and columns of `set` rows and 256 columns that need a scale, once more; and what undoes the scales.
+template <bool ALIGNED, int ACT>
+__device__ __forceinline__ void store_scaled(const AuxJob &a, int64_t row, int c0) {
+    const int lane = threadIdx.x & 31, c = c0 + lane * 8, count = static_cast<int>(min(static_cast<int64_t>(a.set), a.rows - row));
+    Fv<8> of_column[2];
+    bool some = false;
+    if (a.by_column && c < a.padded) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint4 *top = reinterpret_cast<const uint4 *>(a.column_top + k * a.padded + c);
+            const uint4 lo = top[0], hi = top[1];
+            const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+            of_column[k] = Fv<8>::make([&](int e) { return gated_scale(w[e]); });
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                some = some || gated_scaled(w[e]);
+                if (row == 0) a.column_unscale[k * a.padded + c + e] = gated_unscale(w[e]);
+            }
+        }
+    }
+    const bool columns = __any_sync(0xffffffffu, some);
+    const uint32_t row_top = a.to && lane < count ? a.row_top[row + lane] : 0;
+    const uint32_t of_rows = __ballot_sync(0xffffffffu, gated_scaled(row_top));
+    if (c0 == 0 && lane < count) a.row_unscale[row + lane] = gated_unscale(row_top);
+    if (!columns && !of_rows) return;
+    for (int i = 0; i < count; ++i) {
+        const bool this_row = of_rows >> i & 1;
+        if (!columns && !this_row) continue;
+        const Fv<8> of_row = Fv<8>::all(gated_scale(__shfl_sync(0xffffffffu, row_top, i)));
+        SlopeRow<__half> s;
+        float d[2][8];
+        s.load<ALIGNED>(a, row + i, c0);
+        s.slopes<ACT>(d);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const Fv<8> v = Fv<8>::make([&](int e) { return d[k][e]; });
+            const int64_t at = (row + i) * a.to_row + k * a.padded + c0;
+            Strip<__half, 8, 8> out;
+            if (this_row) {
+                out.v[0] = narrow<__half, 8>(v * of_row);
+                out.store(static_cast<__half *>(a.to) + at, a.padded - c0);
+            }
+            if (some) {
+                out.v[0] = narrow<__half, 8>(v * of_column[k]);
+                out.store(static_cast<__half *>(a.by_column) + at, a.padded - c0);
+            }
+        }
+    }
+}
+
 template <typename T, int ACT>
-__global__ void __launch_bounds__(kWarps * 32, std::is_same<T, __half>::value ? 3 : 4) gated_operands_kernel(const __grid_constant__ AuxArgs args) {
+__global__ void __launch_bounds__(kWarps * 32, 4) gated_operands_kernel(const __grid_constant__ AuxArgs args) {
     pdl_trigger();
     pdl_wait();
     const int64_t step = static_cast<int64_t>(gridDim.x) * kWarps;
@@ -221,13 +242,16 @@ __global__ void __launch_bounds__(kWarps * 32, std::is_same<T, __half>::value ? 
         int j = 0;
         while (u >= args.job[j].units) u -= args.job[j++].units;
         const AuxJob &a = args.job[j];
-        if (std::is_same<T, __half>::value && j == kJobs - 1) u = a.units - 1 - u;     // backwards through what L2 still holds of the magnitudes' pass
-        int64_t row = u / a.pieces;
+        const int64_t row = u / a.pieces;
         const int c0 = static_cast<int>(u - row * a.pieces) * kColumns;
-        if (std::is_same<T, __half>::value && j == kJobs - 1) row *= a.set;
         if (j == kJobs - 1) {
-            if (a.aligned) store_slopes<T, true, ACT>(a, row, c0);
-            else store_slopes<T, false, ACT>(a, row, c0);
+            if constexpr (std::is_same<T, __half>::value) {
+                if (a.aligned) store_scaled<true, ACT>(a, row * a.set, c0);
+                else store_scaled<false, ACT>(a, row * a.set, c0);
+            } else {
+                if (a.aligned) store_slopes<T, true, ACT>(a, row, c0);
+                else store_slopes<T, false, ACT>(a, row, c0);
+            }
         } else if (a.copies) {
             pack_shifted(a, row, c0);
         } else {
@@ -261,14 +285,15 @@ cudaError_t launch_gated_operands(const GatedShape &s, const GatedPack (&packs)[
         a.units = rows * a.pieces;
         a.aligned = strip_width(s.dtype, {slopes->gu, slopes->dh}, {s.F, s.h_row}) == 8;
         if (s.dtype == PATDNN_F16) {
-            a.set = a.units <= static_cast<int64_t>(sm_count()) * 64 ? 1 : 8;          // (the columns' scales are read once per set: 4096 x 8192 154 us a row at a time)
+            const bool small = a.units <= static_cast<int64_t>(sm_count()) * 64;
+            a.set = small ? 2 : 32;                    // (that all of them need a scale: 777 x 1333, products included, 36 us, with sets of 8 54; that none does: 30 either way)
             a.units = ceil_div(rows, a.set) * a.pieces;
-            // rows of a warp: four where there are few CTAs, else as many as make a column's maxima cheap
-            const int of_warp = ceil_div(rows, kWarps * 4) * a.pieces <= static_cast<int64_t>(sm_count()) * 8 ? 4 : 16;
+            // rows of a warp: two where there are few (four: 3 us more), else as many as make a column's maxima cheap
+            const int of_warp = small ? 2 : 16;
             const dim3 grid(static_cast<unsigned>(ceil_div(rows, kWarps * of_warp) * a.pieces));
             const cudaError_t e = by_act(s.act, [&](auto act) {
-                return a.aligned ? launch_pdl(gated_magnitudes_kernel<true, act.value>, grid, dim3(kWarps * 32), 0, st, 1, a, of_warp)
-                                 : launch_pdl(gated_magnitudes_kernel<false, act.value>, grid, dim3(kWarps * 32), 0, st, 1, a, of_warp);
+                return a.aligned ? launch_pdl(gated_slopes_kernel<true, act.value>, grid, dim3(kWarps * 32), 0, st, 1, a, of_warp)
+                                 : launch_pdl(gated_slopes_kernel<false, act.value>, grid, dim3(kWarps * 32), 0, st, 1, a, of_warp);
             });
             if (e != cudaSuccess) return e;
             *launches = 2;
