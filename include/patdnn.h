@@ -440,7 +440,8 @@ PATDNN_API int patdnn_rms_free(patdnn_rms h);
  *   patdnn_mx8_bytes       size of the buffer for rows x cols, which depends on these alone; 16-byte aligned buffers are needed
  *   patdnn_mx8_quantize    x DEVICE [rows][ld] of dtype -> mx DEVICE
  *   patdnn_mx8_dequantize  mx DEVICE -> out DEVICE [rows][ld] of dtype, rounded once (in float and bfloat16 every value is exact, but for
- *                          values that rounded up to 2^128, which become infinities; in half, values above 65504 or below 2^-14 round)
+ *                          values that rounded up to 2^128, which become infinities, and in bfloat16 those below 2^-130 of a matrix that was
+ *                          float; in half, values above 65504 or below 2^-14 round)
  * Errors: E_NULL, E_SHAPE (rows < 0, cols < 1, ld < cols, cols > 2^20, rows * cols > 2^40, buffer not aligned), E_DTYPE, E_CUDA.
  * rows = 0 launches nothing.  Asynchronous.
  */
