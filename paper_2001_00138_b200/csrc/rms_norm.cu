@@ -187,10 +187,10 @@ __global__ void __launch_bounds__(kMostWarps * 32) rms_norm_kernel(RmsArgs a) {
             out.narrow_from(v);
             out.store(static_cast<T *>(a.sum) + row * a.r_row + c0, left);
         }
-        const bool beyond = !(total <= 1e38f) || (total < 1e-27f && a.eps < 1e-18f);
+        const bool tiny = total < 1e-27f && a.eps < 1e-18f, beyond = tiny || !(total <= 1e38f) || a.eps > 1e38f;
         if (L < 32 ? __any_sync(0xffffffffu, beyond) : beyond) {       // squares beyond fp32's range: the row times a power of two, and eps its square
             row_sum.agree();
-            if (beyond) scale = total < 1.f ? 0x1p80f : 0x1p-80f;
+            if (beyond) scale = tiny ? 0x1p80f : total <= 1e38f ? 0.25f : 0x1p-80f;            // (0.25: it is eps that is large)
             eps = eps * scale * scale;
             squares = 0.f;
 #pragma unroll
