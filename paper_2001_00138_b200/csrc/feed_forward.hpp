@@ -124,9 +124,8 @@ constexpr int kGatedUnits = 2;              // such units that a call may need, 
 struct GatedWork {                          // a handle's buffers
     void *dgu;                              // [max_rows][2 Fp]: dg, du in the handle's type, Fp = F rounded up to 64; nullptr without gradients
     void *by_column;                        // half: a copy for dwg and dwu (see gated_aux.cu); else nullptr
-    uint32_t *row_top, *column_top;         // half: bits of the largest magnitudes, [max_rows] and [2 Fp], in one buffer of `tops` words, zeros between calls
+    uint32_t *row_top, *column_top;         // half: bits of the largest magnitudes, [max_rows] and [2 Fp], in one buffer, zeros between calls
     float *row_unscale, *column_unscale;    // half: what undoes the scales, likewise
-    int64_t tops;
     float *partial;
     int *status;
 };

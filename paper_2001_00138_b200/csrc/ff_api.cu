@@ -429,11 +429,10 @@ int patdnn_gated_create(const patdnn_gated_desc *desc, patdnn_gated *out) {
     if (e == cudaSuccess && desc->grad && s.dtype == PATDNN_F16) {
         e = allocate(&by_column, static_cast<size_t>(desc->max_rows) * 2 * gated_padded(s.F));
         h->w.by_column = by_column;
-        const size_t rows = (static_cast<size_t>(desc->max_rows) + 3) / 4 * 4;          // (columns are read 16 bytes at a time)
-        h->w.tops = static_cast<int64_t>(rows) + 2 * gated_padded(s.F);
-        if (e == cudaSuccess) e = allocate(&h->w.row_top, static_cast<size_t>(h->w.tops));
-        if (e == cudaSuccess) e = cudaMemset(h->w.row_top, 0, static_cast<size_t>(h->w.tops) * sizeof(uint32_t));
-        if (e == cudaSuccess) e = allocate(&h->w.row_unscale, static_cast<size_t>(h->w.tops));
+        const size_t rows = (static_cast<size_t>(desc->max_rows) + 3) / 4 * 4, words = rows + 2 * static_cast<size_t>(gated_padded(s.F));   // (columns are read 16 bytes at a time)
+        if (e == cudaSuccess) e = allocate(&h->w.row_top, words);
+        if (e == cudaSuccess) e = cudaMemset(h->w.row_top, 0, words * sizeof(uint32_t));
+        if (e == cudaSuccess) e = allocate(&h->w.row_unscale, words);
         h->w.column_top = h->w.row_top + rows;
         h->w.column_unscale = h->w.row_unscale + rows;
     }

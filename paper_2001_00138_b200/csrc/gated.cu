@@ -7,7 +7,7 @@
 // Pairs of CTAs (cta_group::2) work on tiles of 256 rows x 256 columns: each CTA copies its 128 rows of A and 128 of the 256 rows of B, 32 KB
 // per 64 of the summed dimension, for 512 cycles of MMAs.  Forward operands have the summed dimension innermost (K-major); where it is the
 // outer one (wg and wu for dx; dg, du and x for dwg, dwu) the MMAs read the tiles as they lie, transposed (MN-major), so nothing is ever
-// transposed in memory.  Persistent: warp 0 copies, warp 1 of the pair's first CTA multiplies, warps 4 to 11 drain one accumulator (two, of
+// transposed in memory.  Persistent: warp 0 copies, warp 1 of the pair's first CTA multiplies, warps 4 to 19 drain one accumulator (two, of
 // 256 columns each, fill tensor memory) while the other one is summed.
 // Forward of few rows: another kernel, whose M operand are the weights (see there).
 // Both products of the gradient are one launch, the tiles of the second filling up what the first leaves of the rounds over the SMs.  Few
@@ -49,8 +49,8 @@ struct GatedParams {
     void *gu;                                          // forward: both projections, or nullptr
     int stages;
     int f_padded;                                      // columns from dg to du
-    uint32_t *tops;                                    // half, gradient: words that are cleared for the next call
-    int64_t top_words;
+    uint32_t *row_top, *column_top;                    // half, gradient: what is cleared for the next call, a word per row of x and 2 f_padded
+    int64_t top_rows;
     float *partial;
     int *status;
     uint32_t spin_limit;
@@ -285,7 +285,9 @@ __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constan
         __syncwarp();
         if (last >= 0) mbar_wait(done + 8 * (last & 1), (last >> 1) & 1, ctx, 125);
     } else if (GRAD && std::is_same<T, __half>::value && warp == 3) {
-        for (int64_t i = blockIdx.x * 32 + lane; i < p.top_words; i += gridDim.x * 32) p.tops[i] = 0;
+        for (int64_t i = blockIdx.x * 32 + lane; i < p.top_rows + 2 * p.f_padded; i += gridDim.x * 32)
+            if (i < p.top_rows) p.row_top[i] = 0;
+            else p.column_top[i - p.top_rows] = 0;
     } else if (warp >= 4) {
         const int e = warp - 4, quadrant = e & 3, quarter = e >> 2;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quadrant * 32) << 16);
@@ -820,7 +822,7 @@ cudaError_t launch_gated_gradient(const GatedShape &s, const GatedCall &c, const
     const int64_t dgu_row = 2 * static_cast<int64_t>(padded);
     GatedMaps maps{};
     GatedParams p{};
-    p.f_padded = padded; p.tops = w.row_top; p.top_words = w.tops;
+    p.f_padded = padded; p.row_top = w.row_top; p.column_top = w.column_top; p.top_rows = c.rows;
     Product &x = p.of[0] = product_of(plan[0], 0), &dw = p.of[1] = product_of(plan[1], plan[0].splits > 1 ? x.units : 0);
     cudaError_t e = cudaSuccess;
     if (c.dx) {
