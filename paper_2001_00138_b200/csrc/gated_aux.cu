@@ -1,7 +1,7 @@
 // Elementwise work of the gated feed-forward block in front of its products, one launch: rows that the tensor-core copies cannot read as they
 // lie are packed, and the gradients of both projections are formed from what the forward pass kept:  dg = dh u act'(g), du = dh act(g).
 //
-// Memory bound (4096 x 8192 bf16: 50 us for 336 MB, 6.7 TB/s with part of it in L2).  A warp takes 256 columns of a row, 8 per lane.  dg and du are
+// Memory bound (4096 x 8192 bf16: 58 us for 336 MB from cold caches, 5.8 TB/s).  A warp takes 256 columns of a row, 8 per lane.  dg and du are
 // rounded to the type of the products that read them, which take no wider operands at this rate: at most 2^-8 of each term for bf16 (2^-11 for half),
 // independent of one another, so that a product's relative error grows to about sqrt(2) times that of the result's own rounding.
 // Half: dg and du may leave its range where the gradients do not (dh = u = 300), or fall below it (dh = 1e-5, act(g) = 1e-3, summed over thousands of
@@ -83,7 +83,7 @@ template <typename T> struct SlopeRow {
     // d[0]: dg, d[1]: du
     template <int ACT> __device__ __forceinline__ void slopes(float (&d)[2][8]) {
         // Nothing passes where dh is 0 or the slope is, whatever gu holds there: an infinity in it is a number too large for the type, and a masked row may hold
-        // anything.  (On packed pairs, and with selections: 3 us of 111 for 4096 x 8192; element by element 10.)
+        // anything.  (On packed pairs, and with selections: 2 us of 111 for 4096 x 8192; element by element 10.)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const uint32_t open = nonzero2<T>(dh.v[0].w[k]);
@@ -233,7 +233,7 @@ __device__ __forceinline__ void store_scaled(const AuxJob &a, int64_t row, int c
 }
 
 template <typename T, int ACT>
-__global__ void __launch_bounds__(kWarps * 32, 4) gated_operands_kernel(const __grid_constant__ AuxArgs args) {
+__global__ void __launch_bounds__(kWarps * 32, std::is_same<T, __half>::value ? 4 : 5) gated_operands_kernel(const __grid_constant__ AuxArgs args) {
     pdl_trigger();
     pdl_wait();
     const int64_t step = static_cast<int64_t>(gridDim.x) * kWarps;
