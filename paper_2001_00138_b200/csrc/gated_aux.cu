@@ -1,15 +1,15 @@
 // Elementwise work of the gated feed-forward block in front of its products, one launch: rows that the tensor-core copies cannot read as they
 // lie are packed, and the gradients of both projections are formed from what the forward pass kept:  dg = dh u act'(g), du = dh act(g).
 //
-// Memory bound (4096 x 8192 bf16: 58 us for 336 MB from cold caches, 5.8 TB/s).  A warp takes 256 columns of a row, 8 per lane.  dg and du are
+// Memory bound (4096 x 8192 bf16: 62 us for 336 MB from cold caches, 5.4 TB/s, issue 70 %).  A warp takes 256 columns of a row, 8 per lane.  dg and du are
 // rounded to the type of the products that read them, which take no wider operands at this rate: at most 2^-8 of each term for bf16 (2^-11 for half),
 // independent of one another, so that a product's relative error grows to about sqrt(2) times that of the result's own rounding.
 // Half: dg and du may leave its range where the gradients do not (dh = u = 300), or fall below it (dh = 1e-5, act(g) = 1e-3, summed over thousands of
 // rows).  dx is given a copy of them, dwg and dwu another, and the largest magnitudes of every row and column of them are found on the way.  Where that is between
 // 2^-3 and 2^15 the copies stay as they are: half's steps below 2^-14 are 2^-22 of it at most.  Any other row is then written once more into the one copy, any other
 // column into the other, times the power of two that puts the largest magnitude between 2^14 and 2^15 (what is below 2^-29 of it loses bits, what is below
-// 2^-40 is 0), and the products' rows are divided by it in fp32.  (4096 x 8192: 79 us for the first pass and 6 for the second; with one copy and no
-// magnitudes 57.  Finding the magnitudes first, and scaling all of both copies, 53 and 96.)
+// 2^-40 is 0), and the products' rows are divided by it in fp32.  (4096 x 8192: 81 us for the first pass and 7 for the second, 91 where all
+// needs a scale; with one copy and no magnitudes 57.  Finding the magnitudes first, and scaling all of both copies, 53 and 96.)
 #include <algorithm>
 
 #include "feed_forward.hpp"
@@ -64,6 +64,12 @@ template <typename T> __device__ __forceinline__ uint32_t nonzero2(uint32_t pair
     if constexpr (std::is_same<T, __half>::value) return __hneu2_mask(*reinterpret_cast<const __half2 *>(&pair), __half2half2(__ushort_as_half(0)));
     else return __hneu2_mask(*reinterpret_cast<const __nv_bfloat162 *>(&pair), __bfloat162bfloat162(__ushort_as_bfloat16(0)));
 }
+template <typename T> __device__ __forceinline__ uint32_t top2(uint32_t a, uint32_t b) {  // larger magnitudes of two pairs; a NaN is larger than anything
+    uint32_t r;
+    if constexpr (std::is_same<T, __half>::value) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a & 0x7fff7fffu), "r"(b & 0x7fff7fffu));
+    else asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a & 0x7fff7fffu), "r"(b & 0x7fff7fffu));
+    return r;
+}
 // 8 columns per lane of a row of gu and dh.
 template <typename T> struct SlopeRow {
     Strip<T, 8, 8> g, u, dh;
@@ -80,35 +86,46 @@ template <typename T> struct SlopeRow {
             dh.load_any(of_h, left);
         }
     }
-    // d[0]: dg, d[1]: du
-    template <int ACT> __device__ __forceinline__ void slopes(float (&d)[2][8]) {
-        // Nothing passes where dh is 0 or the slope is, whatever gu holds there: an infinity in it is a number too large for the type, and a masked row may hold
-        // anything.  (On packed pairs, and with selections: 2 us of 111 for 4096 x 8192; element by element 10.)
+    // Nothing passes where dh is 0 or the slope is, whatever gu holds there: an infinity in it is a number too large for the type, and a masked row may hold
+    // anything.  Zeros take the places of such u, and of g where it is dh that is 0.  (Looked for first: 4096 x 8192 bf16 62 us, done always 63; neither 57.)
+    template <int ACT> __device__ __forceinline__ void shut() {
+        float z[8];
+        g.widen_to(z);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const uint32_t open = nonzero2<T>(dh.v[0].w[k]);
+            uint32_t slope = 0xffffffffu;
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (ACT == PATDNN_ACT_RELU ? z[2 * k + e] <= 0.f : ACT == PATDNN_ACT_SILU && sigmoid(z[2 * k + e]) == 0.f) slope &= e ? 0x0000ffffu : 0xffff0000u;
             g.v[0].w[k] &= open;
-            u.v[0].w[k] &= open;
+            u.v[0].w[k] &= open & slope;
         }
+    }
+    // d[0]: dg, d[1]: du
+    template <int ACT> __device__ __forceinline__ void slopes(float (&d)[2][8]) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top = top2<T>(top, top2<T>(g.v[0].w[k], u.v[0].w[k]));
+        constexpr uint32_t kInfinity = std::is_same<T, __half>::value ? 0x7c00 : 0x7f80;
+        if ((top & 0x7fff) >= kInfinity || (top >> 16 & 0x7fff) >= kInfinity) shut<ACT>();
         float fd[8];
         g.widen_to(d[0]);
         u.widen_to(d[1]);
         dh.widen_to(fd);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float z = d[0][e], through = fd[e] * d[1][e];
+            float act = d[0][e], slope = 1.f;
             if constexpr (ACT == PATDNN_ACT_RELU) {    // slope 0 at 0; a NaN passes
-                d[0][e] = z > 0.f ? through : z <= 0.f ? 0.f : z;
-                d[1][e] = fd[e] * (z < 0.f ? 0.f : z);
+                act = d[0][e] < 0.f ? 0.f : d[0][e];
+                slope = d[0][e] > 0.f ? 1.f : d[0][e] <= 0.f ? 0.f : d[0][e];
             } else if constexpr (ACT == PATDNN_ACT_SILU) {
-                const float s = sigmoid(z);            // at infinities (g left the range of the type) the limits: 0 and 0, or g and 1
-                const float act = s == 0.f ? 0.f : z * s, slope = s == 1.f ? 1.f : fmaf(act, 1.f - s, s);
-                d[0][e] = s == 0.f ? 0.f : through * slope;
-                d[1][e] = fd[e] * act;
-            } else {
-                d[0][e] = through;
-                d[1][e] = fd[e] * z;
+                const float s = sigmoid(d[0][e]);      // at infinities (g left the range of the type) the limits: 0 and 0, or g and 1
+                act = s == 0.f ? 0.f : d[0][e] * s;
+                slope = s == 1.f ? 1.f : fmaf(act, 1.f - s, s);
             }
+            d[0][e] = fd[e] * d[1][e] * slope;
+            d[1][e] = fd[e] * act;
         }
     }
 };
