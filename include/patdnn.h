@@ -398,8 +398,8 @@ PATDNN_API int patdnn_linear_free(patdnn_linear h);
  *   E_DTYPE    dtype unknown
  *   E_NO_DEVICE  another device is current than when the handle was made
  * A handle owns the gradient's workspace: gradient calls that can overlap on the GPU need a handle each; patdnn_rms_run and _run_mx8 use
- * none.  rows = 0 launches nothing (the gradient writes zeros to dgamma).  Asynchronous on `stream`, but for patdnn_rms_create, which waits for the
- * device, and patdnn_rms_check.
+ * none.  rows = 0 launches nothing (the gradient writes zeros to dgamma).  Asynchronous on `stream`, but for patdnn_rms_create and
+ * patdnn_rms_check.
  * Rows of more than 4096 to 8192 columns are shared by the CTAs of a cluster, which wait for one another's sums; these waits are bounded:
  *   patdnn_rms_check       waits for the device; E_DEVICE_TIMEOUT if such a wait of this handle ran out: rows whose sum it was, and rows after them, are
  *                          NaN (their dx, in the gradient)

@@ -20,15 +20,12 @@ using namespace patdnn;
 struct patdnn_rms_s {
     RmsShape s{};
     int device = -1;
-    float *ws = nullptr;                    // the gradient's partial sums
+    float *ws = nullptr;                    // the gradient's partial sums, and behind them
     int *status = nullptr;
     uint32_t spin_limit = 0;                // patdnn_rms_debug_wait
     int test_skip = 0;
     RmsWait wait() const { return {status, spin_limit, test_skip}; }
-    ~patdnn_rms_s() {
-        cudaFree(ws);
-        cudaFree(status);
-    }
+    ~patdnn_rms_s() { cudaFree(ws); }
 };
 
 struct patdnn_linear8_s {
@@ -59,9 +56,7 @@ struct patdnn_gated_s {
     int test_skip_load = 0;
     ~patdnn_gated_s() {
         cudaFree(w.dgu);
-        cudaFree(w.by_column);
         cudaFree(w.row_top);
-        cudaFree(w.row_unscale);
         cudaFree(w.partial);
         cudaFree(w.status);
         cudaFree(x);
@@ -225,11 +220,11 @@ int patdnn_rms_create(const patdnn_rms_desc *desc, patdnn_rms *out) {
     if (!h) return PATDNN_E_ALLOC;
     h->s = s;
     cudaError_t e = cudaGetDevice(&h->device);
-    if (e == cudaSuccess) e = allocate(&h->ws, rms_workspace_floats(s));
-    if (e == cudaSuccess) e = allocate(&h->status, 4);
-    if (e == cudaSuccess) e = cudaMemset(h->status, 0, 16);
+    const size_t floats = rms_workspace_floats(s);
+    if (e == cudaSuccess) e = allocate(&h->ws, floats + 4);
+    h->status = reinterpret_cast<int *>(h->ws + floats);
+    if (e == cudaSuccess) e = cudaMemset(h->status, 0, 16);             // (kernels write the word only after seconds of waiting, nothing reads it but patdnn_rms_check)
     if (e == cudaSuccess) e = prepare_rms();
-    if (e == cudaSuccess) e = cudaDeviceSynchronize();                  // the status word is zero on every stream from here on
     if (e != cudaSuccess) return failed(h, e, "patdnn_rms_create");
     *out = h;
     return PATDNN_OK;
@@ -419,20 +414,21 @@ int patdnn_gated_create(const patdnn_gated_desc *desc, patdnn_gated *out) {
     h->s = s;
     h->max_rows = desc->max_rows;
     const size_t row = static_cast<size_t>(packed_row(s.K));
-    uint16_t *dgu = nullptr, *by_column = nullptr, *x = nullptr, *weights = nullptr, *shifted = nullptr;
+    uint16_t *dgu = nullptr, *x = nullptr, *weights = nullptr, *shifted = nullptr;
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = allocate(&h->w.partial, static_cast<size_t>(pairs_most()) * kGatedUnits * kGatedUnitFloats);
     if (e == cudaSuccess) e = allocate(&h->w.status, 4);
     if (e == cudaSuccess) e = cudaMemset(h->w.status, 0, 16);
-    if (e == cudaSuccess && desc->grad) e = allocate(&dgu, static_cast<size_t>(desc->max_rows) * 2 * gated_padded(s.F));
+    const size_t copy = static_cast<size_t>(desc->max_rows) * 2 * gated_padded(s.F);    // dg and du
+    const bool scaled = desc->grad && s.dtype == PATDNN_F16;
+    if (e == cudaSuccess && desc->grad) e = allocate(&dgu, scaled ? 2 * copy : copy);
     h->w.dgu = dgu;
-    if (e == cudaSuccess && desc->grad && s.dtype == PATDNN_F16) {
-        e = allocate(&by_column, static_cast<size_t>(desc->max_rows) * 2 * gated_padded(s.F));
-        h->w.by_column = by_column;
+    if (e == cudaSuccess && scaled) {
+        h->w.by_column = dgu + copy;
         const size_t rows = (static_cast<size_t>(desc->max_rows) + 3) / 4 * 4, words = rows + 2 * static_cast<size_t>(gated_padded(s.F));   // (columns are read 16 bytes at a time)
-        if (e == cudaSuccess) e = allocate(&h->w.row_top, words);
+        e = allocate(&h->w.row_top, 2 * words);
         if (e == cudaSuccess) e = cudaMemset(h->w.row_top, 0, words * sizeof(uint32_t));
-        if (e == cudaSuccess) e = allocate(&h->w.row_unscale, words);
+        h->w.row_unscale = reinterpret_cast<float *>(h->w.row_top + words);
         h->w.column_top = h->w.row_top + rows;
         h->w.column_unscale = h->w.row_unscale + rows;
     }
