@@ -34,13 +34,6 @@ inline Mx8Shape mx8_shape(int64_t rows, int64_t cols) {
 cudaError_t launch_mx8_quantize(const Mx8Shape &m, const void *x, int dtype, int64_t ld, void *mx, cudaStream_t st);
 cudaError_t launch_mx8_dequantize(const Mx8Shape &m, const void *mx, void *out, int dtype, int64_t ld, cudaStream_t st);
 
-// Dynamic shared memory that a kernel may be launched with on the current device.  (The dozens of kernels of an operator are allowed theirs once, not with
-// every handle: a millisecond.  Asked of the device, so that it holds after a reset too.)
-template <typename K> int smem_allowed(K kernel) {
-    cudaFuncAttributes a{};
-    return cudaFuncGetAttributes(&a, kernel) == cudaSuccess ? a.maxDynamicSharedSizeBytes : 0;
-}
-
 // CTAs in clusters of `size` that run at a time, one to an SM: a cluster lies inside one group of SMs, and the groups are no multiples of four or
 // eight (148 SMs: 132 and 120 CTAs).  More would wait for a second wave.
 inline int cluster_room(int sms, int size) { return size <= 2 ? sms : size == 4 ? sms - sms / 9 : sms * 13 / 16; }

@@ -731,7 +731,6 @@ void plan_gated_gradient(int F, int K, int64_t rows, bool dx, bool dw, GatedPlan
 }
 
 cudaError_t prepare_gated() {
-    if (smem_allowed(gated_rows_kernel<__nv_bfloat16, PATDNN_ACT_SILU, true>) == kSmem) return cudaSuccess;    // what is set last
     auto allow = [](auto kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); };
     for (int dtype : {PATDNN_F16, PATDNN_BF16})
         for (int act : {PATDNN_ACT_NONE, PATDNN_ACT_RELU, PATDNN_ACT_SILU}) {

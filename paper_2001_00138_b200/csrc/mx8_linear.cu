@@ -440,7 +440,6 @@ cudaError_t scales_map(CUtensorMap *map, const uint8_t *base, int64_t row_tiles,
 
 cudaError_t prepare_mx8_linear() {
     const cudaFuncAttribute what = cudaFuncAttributeMaxDynamicSharedMemorySize;
-    if (smem_allowed(mx8_linear_kernel<__nv_bfloat16, PATDNN_ACT_SILU, true>) == kLinearSmem) return cudaSuccess;               // what is set last
     cudaError_t e = cudaSuccess;
     for (int dtype = 0; dtype < 3 && e == cudaSuccess; ++dtype)
         for (int act = PATDNN_ACT_NONE; act <= PATDNN_ACT_SILU && e == cudaSuccess; ++act)

@@ -493,7 +493,6 @@ cudaError_t launch_rms_norm(const RmsShape &s, const RmsCall &c, cudaStream_t st
 }
 
 cudaError_t prepare_rms() {
-    if (smem_allowed(rms_grad_kernel<__nv_bfloat16, 1, 16, 32, false>) == 100 * 1024) return cudaSuccess;      // what is set last
     for (int dtype : {PATDNN_F32, PATDNN_F16, PATDNN_BF16})
         for (int width : {dtype == PATDNN_F32 ? 4 : 8, 2, 1})
             for (int k = 0; k < 4; ++k) {
