@@ -156,7 +156,7 @@ bool operand_aligned(const void *p, int64_t row) { return aligned(p, copies_as_i
 int64_t packed_row(int64_t K) { return (K + 7) / 8 * 8; }
 
 // Few rows, weights whose rows are not whole 16-byte units apart: a copy of x per phase instead of packed weights, as long as those are fewer rows (8 x 6899 ->
-// 4222: 26 us, 74 packed; 128 x 1001 -> 1001: 9.9 and 10.2; 128 x 6899 -> 700: 25.5 and 20.2).  0: not this way; else the phases.
+// 4222: 25 us, 79 packed; 128 x 1001 -> 1001: 9.9 and 10.2; 128 x 6899 -> 700: 25.5 and 20.2).  0: not this way; else the phases.
 int phases_of(int F, int K, int64_t w_row, int64_t rows) {
     const int phases = gated_phases(w_row);
     return phases > 1 && rows <= kPhasedRows && phases <= F && K + kMostPhases <= phases * w_row && phases * rows <= F ? phases : 0;

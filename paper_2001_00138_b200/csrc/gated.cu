@@ -452,8 +452,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) gated_join_kernel(const __gri
 // memory of the one that finishes a row of x, where g and u of an output meet.
 // PHASED: rows of the weights are not whole 16-byte units apart, which tensor maps cannot describe; but of 2, 4 or 8 rows every first, every second and so on are.
 // A tile takes 64 rows of one such phase, from the 16-byte unit in which each begins: all of them are `shift` columns further right than they should be,
-// and so is the copy of x that the phase is multiplied with.  What lies in front of the rows is zeroed where it has arrived.  (8 x 6899 -> 4222: 26 us;
-// packing the weights in front 80; rows that are whole units apart 22.)
+// and so is the copy of x that the phase is multiplied with.  What lies in front of the rows is zeroed where it has arrived.  (8 x 6899 -> 4222: 25 us;
+// packing the weights in front 79; rows that are whole units apart 24.)
 constexpr int kRowsThreads = 256;
 constexpr int kMostRowsStages = 12;
 

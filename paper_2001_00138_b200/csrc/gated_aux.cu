@@ -1,7 +1,7 @@
 // Elementwise work of the gated feed-forward block in front of its products, one launch: rows that the tensor-core copies cannot read as they
 // lie are packed, and the gradients of both projections are formed from what the forward pass kept:  dg = dh u act'(g), du = dh act(g).
 //
-// Memory bound (4096 x 8192 bf16: 62 us for 336 MB from cold caches, 5.4 TB/s, issue 70 %).  A warp takes 256 columns of a row, 8 per lane.  dg and du are
+// Memory bound (4096 x 8192 bf16: 61 us for 336 MB from cold caches, 5.5 TB/s, issue 70 %).  A warp takes 256 columns of a row, 8 per lane.  dg and du are
 // rounded to the type of the products that read them, which take no wider operands at this rate: at most 2^-8 of each term for bf16 (2^-11 for half),
 // independent of one another, so that a product's relative error grows to about sqrt(2) times that of the result's own rounding.
 // Half: dg and du may leave its range where the gradients do not (dh = u = 300), or fall below it (dh = 1e-5, act(g) = 1e-3, summed over thousands of
@@ -9,7 +9,7 @@
 // 2^-3 and 2^15 the copies stay as they are: half's steps below 2^-14 are 2^-22 of it at most.  Any other row is then written once more into the one copy, any other
 // column into the other, times the power of two that puts the largest magnitude between 2^14 and 2^15 (what is below 2^-29 of it loses bits, what is below
 // 2^-40 is 0), and the products' rows are divided by it in fp32.  (4096 x 8192: 81 us for the first pass and 7 for the second, 91 where all
-// needs a scale; with one copy and no magnitudes 57.  Finding the magnitudes first, and scaling all of both copies, 53 and 96.)
+// needs a scale; with one copy and no magnitudes 58.  Finding the magnitudes first, and scaling all of both copies, 53 and 96.)
 #include <algorithm>
 
 #include "feed_forward.hpp"
@@ -87,7 +87,7 @@ template <typename T> struct SlopeRow {
         }
     }
     // Nothing passes where dh is 0 or the slope is, whatever gu holds there: an infinity in it is a number too large for the type, and a masked row may hold
-    // anything.  Zeros take the places of such u, and of g where it is dh that is 0.  (Looked for first: 4096 x 8192 bf16 62 us, done always 63; neither 57.)
+    // anything.  Zeros take the places of such u, and of g where it is dh that is 0.  (Looked for first: 4096 x 8192 bf16 61 us, done always 63; neither 58.)
     template <int ACT> __device__ __forceinline__ void shut() {
         float z[8];
         g.widen_to(z);
