@@ -1,7 +1,7 @@
 // Elementwise work of the gated feed-forward block in front of its products, one launch: rows that the tensor-core copies cannot read as they
 // lie are packed, and the gradients of both projections are formed from what the forward pass kept:  dg = dh u act'(g), du = dh act(g).
 //
-// Memory bound (4096 x 8192 bf16: 61 us for 336 MB from cold caches, 5.5 TB/s, issue 70 %).  A warp takes 256 columns of a row, 8 per lane.  dg and du are
+// Memory bound (4096 x 8192 bf16: 61 us for 336 MB from cold caches, 5.5 TB/s, issue 66 %).  A warp takes 256 columns of a row, 8 per lane.  dg and du are
 // rounded to the type of the products that read them, which take no wider operands at this rate: at most 2^-8 of each term for bf16 (2^-11 for half),
 // independent of one another, so that a product's relative error grows to about sqrt(2) times that of the result's own rounding.
 // Half: dg and du may leave its range where the gradients do not (dh = u = 300), or fall below it (dh = 1e-5, act(g) = 1e-3, summed over thousands of
