@@ -77,7 +77,7 @@ struct Strip {
 #pragma unroll
                 for (int k = 0; k < static_cast<int>(sizeof(v[j].w) / 4); ++k) v[j].w[k] = 0;
                 if constexpr (A > 1) {
-                    if (c >= left) continue;           // (2072 x 12000 bf16, norm: 42 us; 65 where warps without a lane that is in part there went through what follows)
+                    if (c >= left) continue;           // (2072 x 12000 bf16, norm: 43 us; 65 where warps without a lane that is in part there went through what follows)
 #pragma unroll
                     for (int e = 0; e < A; ++e)
                         if (c + e < left) {

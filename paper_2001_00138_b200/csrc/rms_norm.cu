@@ -52,7 +52,7 @@ __device__ __forceinline__ void cluster_barrier() {
 // behind the barrier of the call between.  A lane reads one slot (of a cluster four), and five shuffles add them: reading them one by one takes
 // as long as a row's loads.
 // In a cluster the values are sent with stores that count their bytes on a barrier of the CTA that gets them: a cluster barrier would wait for the rows
-// that were stored before it as well (3000 x 16384 bf16: 103 us, so 71; its gradient 103 and 74).  A peer sends its next but one value only behind this CTA's next ones, which
+// that were stored before it as well (3000 x 16384 bf16: 103 us, so 71; its gradient 103 and 76).  A peer sends its next but one value only behind this CTA's next ones, which
 // its warps send when they have read the present ones.
 struct alignas(128) RowSlots {                         // what lies behind begins at a multiple of 128 too, as copies of whole lines want it
     float set[2][8][kMostWarps];                       // [2][row group, or CTA of the cluster][warp of the row]; zeros where there is none
