@@ -469,12 +469,12 @@ PATDNN_API int patdnn_linear8_free(patdnn_linear8 h);
  *   g = x wg^T, u = x wu^T, h = act(g) * u                          x [rows][K], wg and wu [F][K], h [rows][F]
  *   dg = dh * u * act'(g), du = dh * act(g);  dx = dg wg + du wu, dwg = dg^T x, dwu = du^T x
  * Sums are fp32 on the tensor cores, in an order that depends on sizes, strides and where wg and wu begin in a 16-byte unit, and on nothing else; g and u
- * stay in fp32 for h, which is rounded once.  For the gradient the run stores
- * g and u rounded to the tensors' type (gu), and dg and du are rounded to it as operands of the products; dx, dwg and dwu are rounded once
- * more.  F16: rows (for dx) and columns (for dwg, dwu) of dg and du whose largest magnitude is not between 2^-3 and 2^15 are scaled by a power of two, so
- * that they keep to the type's range whatever dh, g and u multiply to; what is below 2^-40 of the largest is taken as 0.  At g = 0 ReLU passes no
- * gradient.  A row of x that is not finite spoils its row of h alone.  Where g or u leaves the range of the type, gu holds an infinity; SiLU has its
- * limits there (0 and slope 0 at -infinity, slope 1 at infinity).  Nothing passes where dh or the slope is 0, whatever gu holds there.
+ * stay in fp32 for h, which is rounded once.  For the gradient the run stores g and u rounded to the tensors' type (gu), and dg and du are rounded to it as
+ * operands of the products; dx, dwg and dwu are rounded once more.  F16: rows (for dx) and columns (for dwg, dwu) of dg and du whose largest magnitude
+ * is not between 2^-3 and 2^15 are scaled by a power of two, so that they keep to the type's range whatever dh, g and u multiply to; what is below
+ * 2^-22 of the largest may become 0.  At g = 0 ReLU passes no gradient.  A row of x that is not finite spoils its row of h alone.  Where g or u leaves
+ * the range of the type, gu holds an infinity; SiLU has its limits there (0 and slope 0 at -infinity, slope 1 at infinity).  Nothing passes where dh or
+ * the slope is 0, whatever gu holds there.
  *   desc       copied; rows of consecutive elements; strides in elements, 0 = dense: x_row of x and dx, w_row of the four weight tensors,
  *              h_row of h and dh; gu is dense, [rows][2][F], g before u.  grad != 0: gradients will be asked for (more workspace)
  *   patdnn_gated_run       gu DEVICE or NULL; hidden and gu overlap no input
@@ -485,8 +485,8 @@ PATDNN_API int patdnn_linear8_free(patdnn_linear8 h);
  * above 2^31, a tensor that is not aligned to its elements, or x, wg or wu with rows that are whole 16-byte units apart and not aligned to 16
  * bytes), E_DTYPE (F16 and BF16 only), E_SCRATCH (a gradient without desc.grad), E_ALLOC, E_CUDA, E_NO_DEVICE (another device is current).
  * A handle owns its workspace (39 MB, and what max_rows needs for gradients, max_rows * F * 4 bytes for BF16 and twice that for F16, and for rows that
- * are not whole 16-byte units apart, which are packed or copied first): calls that can overlap need a handle each, others may share one, whatever their weights.  rows = 0 launches nothing (the
- * gradient writes zeros to dwg and dwu).  patdnn_gated_create waits for the device; the calls are asynchronous on `stream`.
+ * are not whole 16-byte units apart, which are packed or copied first): calls that can overlap need a handle each, others may share one, whatever their
+ * weights.  rows = 0 launches nothing (the gradient writes zeros to dwg and dwu).  patdnn_gated_create waits for the device; the calls are asynchronous on `stream`.
  */
 typedef struct patdnn_gated_s *patdnn_gated;
 typedef struct {

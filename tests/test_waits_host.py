@@ -56,3 +56,12 @@ def test_whole_warps_read_tensor_memory_in_the_convolutions():
         for m in re.finditer(r"mbar_wait\(bar_(?:acc|af)\b", text):
             around = text[max(0, m.start() - 40):m.end() + 140]
             assert "__all_sync(" in around or "__any_sync(" in around, (name, around)
+
+
+def test_waits_of_no_handle():
+    from paper_2001_00138_b200 import binding as B
+    lib = B.load()
+    for call in (lib.patdnn_rms_check, lib.patdnn_linear8_check, lib.patdnn_gated_check):
+        assert call(None) == 1                             # E_NULL
+    for call in (lib.patdnn_rms_debug_wait, lib.patdnn_linear8_debug_wait, lib.patdnn_gated_debug_wait):
+        assert call(None, 1024, 1) == 1
